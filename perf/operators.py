@@ -4,7 +4,7 @@ A case is one pass through the entry points of `paper_2505_14201_amd.flashd` tha
 kept in pages: `attn_fwd_tree` (attention of each sequence's new tokens over its cached keys, the
 new tokens seeing each other as a chain or as a tree), `cache_append` (norm and rotation of projected
 q and k, k and v written into the pages) and `cache_fork`, `cache_reserve`, `cache_commit` (sequences
-branch, get pages, keep accepted tokens).  With `own` false the same results come from elementary
+branch, get pages and give them back, keep accepted tokens).  With `own` false the same results come from elementary
 torch operations.
 
 Fields of a case: op ("tree", "append", "branch", "accept"), dtype of q, k, v and o, kv ("same": the
@@ -58,7 +58,7 @@ def listed():
               hi=4000, n=16, tree=True, rot=32, interleaved=True),
         # 32 sequences branch in two; shared pages that are part filled are copied, 8 layers.
         _case("branch", op="branch", B=32, lo=100, hi=4000, layers=8),
-        # What was accepted of 16 drafts moves together in all of 32 layers, the rest is dropped.
+        # What was accepted of 16 drafts moves together in all of 32 layers.
         _case("accept", op="accept", B=32, page=16, lo=100, hi=1000, n=16, tree=True, layers=32,
               keep=6),
     ]
@@ -340,7 +340,12 @@ def _plain_reserve(s, table, lens):
     page = c["page"]
     start, length = s["q_start"].long(), lens.long()
     some = start[1:] - start[:-1]
+    # a sequence has exactly the pages of its keys: what lies behind goes back first
     col = torch.arange(table.shape[1], device=table.device)
+    last = -(-(length + some) // page)
+    gone = (table >= 0) & (col >= last[:, None])
+    refs.index_add_(0, table.long().clamp(min=0).flatten(), -gone.flatten().to(torch.int32))
+    table.masked_fill_(gone, -1)
     first = length // page
     part = length % page
     mine = table.long().gather(1, first.clamp(max=table.shape[1] - 1)[:, None])[:, 0]
@@ -351,7 +356,7 @@ def _plain_reserve(s, table, lens):
     holders = torch.zeros_like(refs).index_add_(0, page_of, share.to(torch.int32))
     lowest = torch.full_like(refs, len(each)).long().scatter_reduce_(0, page_of, torch.where(share, each, len(each)), "amin")
     share &= (holders != refs)[page_of] | (lowest[page_of] != each)
-    new = (table < 0) & (col >= first[:, None]) & (col < -(-(length + some) // page)[:, None]) & (some > 0)[:, None]
+    new = (table < 0) & (col >= first[:, None]) & (col < last[:, None]) & (some > 0)[:, None]
     wanted = torch.cat([share[:, None], new], 1)
     rank = (wanted.flatten().long().cumsum(0) - 1).view(wanted.shape)
     free = torch.sort((refs != 0).to(torch.int32), stable=True).indices
@@ -376,9 +381,7 @@ def _plain_reserve(s, table, lens):
 
 
 def _plain_commit(s):
-    c, table, refs = s["c"], s["table"], s["refs"]
-    page, lens = c["page"], s["lens"].long()
-    some = (s["q_start"][1:] - s["q_start"][:-1]).long()
+    table, page, lens = s["table"], s["c"]["page"], s["lens"].long()
     i = torch.arange(s["keep"].shape[1], device=table.device)
     b, i = (i < s["n_keep"][:, None]).nonzero().unbind(1)
     src, dst = lens[b] + s["keep"][b, i], lens[b] + i
@@ -387,10 +390,6 @@ def _plain_commit(s):
     k[:, dp, :, dst % page] = k[:, sp, :, src % page]
     v[:, dp, :, dst % page] = v[:, sp, :, src % page]
     s["lens_out"].copy_(lens + s["n_keep"])
-    col = torch.arange(table.shape[1], device=table.device)
-    gone = (col >= -(-s["lens_out"].long() // page)[:, None]) & (col < -(-(lens + some) // page)[:, None]) & (table >= 0)
-    refs.index_add_(0, table.long().clamp(min=0).flatten(), -gone.flatten().to(torch.int32))
-    table.masked_fill_(gone, -1)
 
 
 def run(s):
@@ -415,7 +414,7 @@ def run(s):
             return {"k": s["kcache"], "v": s["vcache"], "refs": s["refs"], "table": s["table_out"],
                     "lens": s["lens_out"], "report": s["report"]}
         flashd.cache_reserve(s["kcache"], s["vcache"], s["refs"], s["table"], s["lens"], s["q_start"], s["report"])
-        flashd.cache_commit(s["kcache"], s["vcache"], s["refs"], s["table"], s["lens"], s["q_start"], s["lens_out"],
+        flashd.cache_commit(s["kcache"], s["vcache"], s["table"], s["lens"], s["q_start"], s["lens_out"],
                             keep=s["keep"], n_keep=s["n_keep"])
         return {"k": s["kcache"], "v": s["vcache"], "refs": s["refs"], "table": s["table"], "lens": s["lens_out"],
                 "report": s["report"]}
