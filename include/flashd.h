@@ -65,7 +65,9 @@ typedef enum {
     FLASHD_E_WORKSPACE = -7,  /* workspace missing or smaller than flashd_workspace_bytes */
     FLASHD_E_HIP = -8,        /* a HIP call (allocation, launch) failed                 */
     FLASHD_E_ARCH = -9,       /* the current device is not gfx950                       */
-    FLASHD_E_VARIANT = -10    /* variant/splits not valid for this problem              */
+    FLASHD_E_VARIANT = -10,   /* variant/splits not valid for this problem              */
+    FLASHD_E_CACHE = -11,     /* a paged cache's page size, strides or layer are not valid */
+    FLASHD_E_OVERLAP = -12    /* an output lies on an input it must not share memory with  */
 } flashd_status;
 
 /* How the recurrence is evaluated.  All variants compute the same result. */
@@ -267,8 +269,149 @@ int flashd_skip_stats(const void* q, const void* k, int B, int Hq, int Hkv, int 
                       unsigned long long* counts, void* stream);
 
 /*
- * Frees the split-K / fp8 scratch memory that flashd_attn_fwd, flashd_attn_fwd_state and
- * flashd_attn_fwd_kv8 have cached for the CURRENT device: the live buffer of every stream
+ * ---- Keys and values in pages --------------------------------------------------------------
+ *
+ * A cache shared by sequences of different lengths.  K and V are pools of P pages, a page holding
+ * `page` keys of every kv head; row b of the page table names the pages of sequence b in the order of its keys.
+ *
+ *   pools     page p of layer y begins y * layer_stride + p * page_stride elements into k and into v
+ *             and is [Hkv][page][d], contiguous.  So [layers][P][Hkv][page][d] may be one tensor, or a page's
+ *             K and V lie side by side.  Different pages (and layers) must not share memory.
+ *   table     int [B][max_pages]: page numbers, the pages a sequence owns first, then -1.
+ *   lens      int [B]: the keys each sequence has in the cache.
+ *   refs      int [P]: how many table entries name each page; a page with 0 is free.
+ *   q_start   int [B + 1]: the new tokens of sequence b are rows q_start[b] .. q_start[b + 1] - 1 of packed
+ *             tensors [T][heads][d], its key number lens[b] + i the i-th of them.  Starts at 0 and does not fall;
+ *             a sequence may have no new tokens, and rows from q_start[B] on belong to none: they
+ *             are neither read into any result nor written.
+ *
+ * One step of a serving loop, the tokens of each sequence drafted as a chain or as a tree:
+ *   flashd_cache_reserve   pages for the new tokens
+ *   flashd_cache_append    norm, rotation, and K and V into the pages (every layer)
+ *   flashd_attn_fwd_tree   attention of the new tokens (every layer)
+ *   flashd_cache_commit    the accepted ones move together: the lengths grow
+ * and flashd_cache_fork where sequences branch, end or change places.
+ *
+ * All of these, and what they are called with, are device memory except the struct itself, which
+ * is read before the call returns.  The library reads table, lens, q_start, refs and the like only on the device,
+ * in the order of the stream, so a step can be recorded into a HIP graph and replayed with other numbers
+ * in the same places.  Numbers found there never lead outside the buffers given: a page number outside
+ * [0, P) is no page (its keys weigh nothing, what would be written to it is dropped), a
+ * sequence ends at max_pages * page keys and its tokens at row T.
+ * Limits: B at most 4096, page 16, 32, 64, 128 or 256, max_pages * page at most 10^9, B * max_pages and T * Hq below 2^31.
+ * Pointers to elements of pools and packed tensors and the strides of rows, pages and layers are
+ * multiples of 16 bytes, other pointers of their element's size (else FLASHD_E_ALIGN).
+ */
+#define FLASHD_CACHE_FP8 3        /* storage type of a cache: e4m3 as in flashd_attn_fwd_kv8 */
+#define FLASHD_CACHE_MAX_SEQS 4096
+
+typedef struct flashd_cache {
+    void* k;
+    void* v;
+    int* table;
+    const int* lens;
+    long long page_stride;    /* elements; at least Hkv * page * d */
+    long long layer_stride;   /* elements; not looked at with one layer */
+    int layers;
+    int P;
+    int page;
+    int max_pages;
+    int B;
+    int Hkv;
+    int d;
+    int dtype;                /* a flashd_dtype, or FLASHD_CACHE_FP8 */
+    float kscale, vscale;     /* FLASHD_CACHE_FP8: the real key is kscale * k8, the real value vscale * v8 */
+} flashd_cache;
+
+/*
+ * Sequences branch, end or change places: new sequence i (of B_out) becomes parent[i]'s twin: it
+ * gets its table row and length; with parent[i] outside [0, B) it is empty.  refs follows: +1 for the
+ * entries of table_out, -1 for those of c->table, so that the pages of sequences that nobody continues become
+ * free and those that several continue are shared.  Nothing is copied: flashd_cache_reserve copies the
+ * page that two twins would both write to.
+ *   parent     int [B_out]
+ *   table_out  int [B_out][max_pages], lens_out int [B_out]; neither may overlap table or lens
+ */
+int flashd_cache_fork(const flashd_cache* c, int* refs, const int* parent, int B_out, int* table_out,
+                      int* lens_out, void* stream);
+
+/*
+ * Gives each sequence exactly the pages of lens[b] keys and its new tokens: pages behind those go back, and
+ * missing ones are taken from the free pages, lowest numbers to the lowest sequences.  A sequence with new
+ * tokens whose last page is part filled and shared gets a page of its own there, and the keys
+ * in it (all layers, K and V) are copied; of sequences that are a page's only holders the first keeps it.
+ * c->table and refs are updated.
+ *   report  int [1 + B], overwritten: report[0] = 0, or how many pages are missing (free ones, and columns of
+ *           the table): then no sequence has got any and no page has been copied (pages given
+ *           back stay so).  report[1 + b] = the page that sequence b's last page was copied from, or -1.
+ */
+int flashd_cache_reserve(const flashd_cache* c, int* refs, const int* q_start, int* report, void* stream);
+
+/*
+ * The new tokens' projections become queries and cached keys and values, in one pass:
+ *   q_out = rotate(norm(q, q_weight)),  K = rotate(norm(k, k_weight)),  V = v,
+ *   norm(x, w) = x / sqrt(mean(x^2) + eps) * w over the d elements of a head (w NULL: x as it is),
+ *   rotate: each pair (x, y) among the first `rot` elements becomes (x cos a - y sin a, y cos a + x sin a) with
+ *   a = position * inv_freq[i]; pair i is elements (i, i + rot / 2), or (2 i, 2 i + 1) with `interleaved`.
+ * The arithmetic is fp32 with one rounding to the storage type; a is formed in fp64.
+ * Cache of FLASHD_CACHE_FP8: K / kscale and V / vscale are rounded to e4m3, what passes 448 becomes 448.
+ *   q, q_out        [T][Hq][d], k, v [T][Hkv][d] in storage type `dtype` (the cache's, or f16/bf16 with an fp8 cache, else
+ *                   FLASHD_E_VARIANT); rows of a token contiguous, tokens *_stride elements apart.
+ *                   q_out may be q; otherwise outputs overlap no input.
+ *   positions       int [T], or NULL: a token's position is its key number
+ *   inv_freq        float [rot / 2]; NULL with rot == 0.  rot is a multiple of 16, at most d.
+ *   q_weight, k_weight   [d] in `dtype`, or NULL
+ * Tokens without a page (reserve reported them missing) get their q_out; K and V are dropped.
+ * T == 0 is a call without work.
+ */
+int flashd_cache_append(const flashd_cache* c, int layer, const void* q, long long q_stride, const void* k,
+                        long long k_stride, const void* v, long long v_stride, void* q_out,
+                        long long q_out_stride, int T, int Hq, const int* q_start, const int* positions,
+                        const float* inv_freq, int rot, int interleaved, const void* q_weight,
+                        const void* k_weight, float eps, int dtype, void* stream);
+
+/*
+ * Attention of the new tokens: token i of sequence b sees the sequence's first lens[b] keys and of the keys of
+ * its new tokens (which flashd_cache_append has put behind them) those that its row of `tree` names.
+ *   q, o     [T][Hq][d] in storage type `dtype` (the cache's, or f16/bf16 with an fp8 cache, else FLASHD_E_VARIANT),
+ *            tokens *_stride elements apart; o must not overlap q.  Head h reads kv head h / (Hq / Hkv).
+ *   tree     unsigned long long [T][tree_words]: bit j % 64 of word j / 64 of a token's row is 1 iff
+ *            it sees new token j of its sequence (itself only if its own bit is set; tokens past the
+ *            last word are not seen).  NULL: a chain, token i sees tokens 0 .. i.
+ *            A token that sees no key gets zeros.  Keys that a token does not see leave its
+ *            output as it is whatever they hold (infinities and NaN included).
+ *   max_q    the most new tokens of a sequence; sizes the launch, not the result: any value >= 1 is right.
+ *   workspace   device memory of at least flashd_tree_workspace_bytes(...), 16-byte aligned, or NULL: taken
+ *            from the grow-only cache of the stream as in flashd_attn_fwd.  Two calls must not use one
+ *            workspace at the same time.
+ * Scores, softmax and sums are fp32; weights are rounded to `dtype` before the product with V.  For fixed inputs and
+ * max_q the output is bitwise reproducible.  T == 0 is a call without work.
+ */
+int flashd_attn_fwd_tree(const flashd_cache* c, int layer, const void* q, long long q_stride, void* o,
+                         long long o_stride, int T, int max_q, int Hq, const int* q_start,
+                         const unsigned long long* tree, int tree_words, float scale, int dtype,
+                         void* stream, void* workspace, size_t workspace_bytes);
+
+/* Bytes of workspace of flashd_attn_fwd_tree: does not depend on B, T or any length.  0 for invalid
+ * arguments. */
+size_t flashd_tree_workspace_bytes(int Hq, int Hkv, int max_q, int d, int dtype);
+
+/*
+ * Keeps the accepted ones of each sequence's new tokens: the keys and values (all layers) of token keep[b][i]
+ * move to key lens[b] + i, lens_out[b] = lens[b] + n_keep[b].  Pages left over stay the sequence's
+ * until the next flashd_cache_reserve.
+ *   keep     int [B][max_keep]: tokens of the sequence, ascending; a list ends before an entry that is not larger
+ *            than the one before it or is no token of the sequence.  NULL (max_keep 0): the first n_keep[b]
+ *            tokens, nothing moves.
+ *   n_keep   int [B], or NULL: max_keep, or all new tokens without `keep`
+ *   lens_out int [B]; must not overlap lens
+ */
+int flashd_cache_commit(const flashd_cache* c, const int* q_start, const int* keep, int max_keep,
+                        const int* n_keep, int* lens_out, void* stream);
+
+/*
+ * Frees the split-K / fp8 scratch memory that flashd_attn_fwd, flashd_attn_fwd_state,
+ * flashd_attn_fwd_kv8 and flashd_attn_fwd_tree have cached for the CURRENT device: the live buffer of every stream
  * that has been used and the buffers those streams have outgrown (which are kept until this
  * call, since work enqueued earlier may still read them).  The frees wait for the device, so
  * work already enqueued is not disturbed; do not call it while another host thread is inside

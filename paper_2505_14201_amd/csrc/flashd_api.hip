@@ -439,6 +439,11 @@ int run(const void* q, const void* k, const void* v, void* o, const Shape& s, in
 
 }  // namespace
 
+namespace flashd {
+int api_check_arch() { return check_arch(); }
+int api_cached_workspace(void* stream, size_t bytes, void** out) { return cached_workspace(stream, bytes, out); }
+}  // namespace flashd
+
 extern "C" {
 
 int flashd_attn_fwd(const void* q, const void* k, const void* v, void* o, int B, int Hq, int Hkv,
@@ -582,6 +587,8 @@ const char* flashd_status_string(int status) {
     case FLASHD_E_HIP: return "a HIP call failed";
     case FLASHD_E_ARCH: return "the current device is not gfx950";
     case FLASHD_E_VARIANT: return "variant or splits not valid for this problem";
+    case FLASHD_E_CACHE: return "page size, strides or layer of the paged cache not valid";
+    case FLASHD_E_OVERLAP: return "an output overlaps an input";
     default: return "unknown status";
     }
 }

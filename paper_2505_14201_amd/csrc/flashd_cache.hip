@@ -1,0 +1,467 @@
+// Writing the paged cache: projected keys and values with norm and rotation on the way
+// (append_kernel), and the bookkeeping of sequences that branch, grow and drop what was drafted
+// (fork_kernel, reserve_kernel with copy_rows_kernel, commit_kernel).
+#include "flashd_common.h"
+#include "flashd_kernels.h"
+#include "flashd_paged.h"
+
+namespace flashd {
+
+typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
+typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
+
+// ---- norm, rotation and cache write --------------------------------------------------------
+//
+// Per token and head: x <- x / sqrt(mean x^2 + eps) * w, then (u, v) <- (u cos a - v sin a,
+// v cos a + u sin a) for the pairs of the first `rot` elements, a_i = position * inv_freq_i.  The angle
+// is formed in fp64 and reduced to a turn there: at position 10^5 an fp32 product would be off
+// by 4e-3 radians.  Everything else is fp32 with one rounding at the store.
+//
+// A row of d elements lies in d / 8 lanes, 8 elements each (one 16-byte load), so the partner of an
+// element of a half-split pair is a whole lane away and the sum of squares takes d / 8 lanes.  A
+// workgroup takes one token's rows (its q, k and v heads), so that the angles are formed once for
+// all of them.
+template <typename T, int D, bool FP8>
+__global__ __launch_bounds__(256) void append_kernel(Paged c, AppendArgs a) {
+    constexpr int LPR = D / 8;                  // lanes per row
+    constexpr int RPP = 256 / LPR;              // rows per pass of the workgroup
+    __shared__ float cs[D / 2], sn[D / 2];
+    __shared__ int part[4];
+    const int tid = threadIdx.x;
+    const int t = blockIdx.x;
+    const int l = tid % LPR;
+    const int rows = a.Hq + 2 * c.Hkv;
+    const int row = blockIdx.y * RPP + tid / LPR;
+
+    // the row of this lane; rows past the last take part in everything but the loads and stores
+    const bool is_q = row < a.Hq;
+    const bool is_k = !is_q && row < a.Hq + c.Hkv;
+    const bool is_v = !is_q && !is_k && row < rows;
+    float x[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+    if (is_q) Store<T>::load8(a.q, (size_t)t * a.q_stride + (size_t)row * D + 8 * l, x);
+    else if (is_k) Store<T>::load8(a.k, (size_t)t * a.k_stride + (size_t)(row - a.Hq) * D + 8 * l, x);
+    else if (is_v) Store<T>::load8(a.v, (size_t)t * a.v_stride + (size_t)(row - a.Hq - c.Hkv) * D + 8 * l, x);
+
+    // the token's sequence: the last one that begins at or before it
+    int before = 0;
+    for (int i = tid; i <= c.B; i += 256) before += c.q_start[i] <= t ? 1 : 0;
+#pragma unroll
+    for (int s = 32; s > 0; s >>= 1) before += __shfl_xor(before, s);
+    if ((tid & 63) == 0) part[tid >> 6] = before;
+    __syncthreads();
+    const int b = part[0] + part[1] + part[2] + part[3] - 1;
+    if (b < 0 || b >= c.B) return;              // rows that belong to no sequence stay as they are
+    const Seq s = seq_at(c, b);
+    const int i = t - s.row0;
+    const int key = s.len + i;
+
+    const int half = a.rot / 2;
+    if (tid < half) {
+        const int pos = a.positions != nullptr ? a.positions[t] : key;
+        const double turns = (double)pos * (double)a.inv_freq[tid] * 0.15915494309189533577;
+        float sv, cv;
+        sincospif((float)(2.0 * (turns - rint(turns))), &sv, &cv);
+        cs[tid] = cv;
+        sn[tid] = sv;
+    }
+    __syncthreads();
+
+    const void* wp = is_q ? a.q_weight : is_k ? a.k_weight : nullptr;
+    float sum = 0.0f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) sum = fmaf(x[e], x[e], sum);
+#pragma unroll
+    for (int m = LPR / 2; m > 0; m >>= 1) sum += __shfl_xor(sum, m);
+    if (wp != nullptr) {
+        float w[8];
+        Store<T>::load8(wp, 8 * l, w);
+        const float r = 1.0f / sqrtf(sum * (1.0f / D) + a.eps);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = x[e] * r * w[e];
+    }
+    if (half > 0) {
+        if (a.interleaved) {
+            if ((is_q || is_k) && 8 * l < a.rot) {
+#pragma unroll
+                for (int e = 0; e < 8; e += 2) {
+                    const float cv = cs[4 * l + e / 2], sv = sn[4 * l + e / 2];
+                    const float u = x[e], v = x[e + 1];
+                    x[e] = fmaf(u, cv, -(v * sv));
+                    x[e + 1] = fmaf(v, cv, u * sv);
+                }
+            }
+        } else {
+            // rot is a multiple of 16: half a rotation is whole lanes
+            const int hl = half / 8;
+            const int lane = tid & 63;
+            const int from = l < hl ? lane + hl : lane - hl;
+            float y[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) y[e] = __shfl(x[e], from & 63);
+            if ((is_q || is_k) && l < 2 * hl) {
+                const int at = 8 * (l < hl ? l : l - hl);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const float sv = l < hl ? -sn[at + e] : sn[at + e];
+                    x[e] = fmaf(x[e], cs[at + e], y[e] * sv);
+                }
+            }
+        }
+    }
+
+    if (is_q) {
+        const size_t at = (size_t)t * a.qo_stride + (size_t)row * D + 8 * l;
+        Store<T>::store4(a.q_out, at, {x[0], x[1], x[2], x[3]});
+        Store<T>::store4(a.q_out, at + 4, {x[4], x[5], x[6], x[7]});
+    } else if ((is_k || is_v) && (unsigned)i < (unsigned)s.n) {
+        const int page = page_at(c, b, key >> c.page_log2);
+        if (page < 0) return;
+        const int h = is_k ? row - a.Hq : row - a.Hq - c.Hkv;
+        char* base = (is_k ? c.k : c.v) + (size_t)page * c.page_bytes + (size_t)h * c.head_bytes;
+        const size_t at = (size_t)(key & ((1 << c.page_log2) - 1)) * D + 8 * l;
+        if constexpr (FP8) {
+            // e4m3 ends at 448: what is larger is stored as that (NaN stays NaN)
+            const float scale = is_k ? c.kscale : c.vscale;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                x[e] = x[e] / scale;
+                x[e] = x[e] > 448.0f ? 448.0f : x[e] < -448.0f ? -448.0f : x[e];
+            }
+            u32x2 w;
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                int p = __builtin_amdgcn_cvt_pk_fp8_f32(x[4 * e], x[4 * e + 1], 0, false);
+                p = __builtin_amdgcn_cvt_pk_fp8_f32(x[4 * e + 2], x[4 * e + 3], p, true);
+                w[e] = (unsigned)p;
+            }
+            *reinterpret_cast<u32x2*>(base + at) = w;
+        } else {
+            Store<T>::store4(base, at, {x[0], x[1], x[2], x[3]});
+            Store<T>::store4(base, at + 4, {x[4], x[5], x[6], x[7]});
+        }
+    }
+}
+
+template <typename T, bool FP8>
+static hipError_t launch_append_t(const Paged& c, const AppendArgs& a, hipStream_t st) {
+    const int rows = a.Hq + 2 * c.Hkv, per = 256 / (c.d / 8);
+    const dim3 grid((unsigned)c.T, (unsigned)((rows + per - 1) / per)), block(256);
+    if (c.d == 64) hipLaunchKernelGGL((append_kernel<T, 64, FP8>), grid, block, 0, st, c, a);
+    else hipLaunchKernelGGL((append_kernel<T, 128, FP8>), grid, block, 0, st, c, a);
+    return hipGetLastError();
+}
+
+hipError_t launch_cache_append(const Paged& c, const AppendArgs& a, hipStream_t st) {
+    switch (a.dtype) {
+    case 0: return launch_append_t<F32, false>(c, a, st);
+    case 1: return a.fp8 ? launch_append_t<F16, true>(c, a, st) : launch_append_t<F16, false>(c, a, st);
+    default: return a.fp8 ? launch_append_t<BF16, true>(c, a, st) : launch_append_t<BF16, false>(c, a, st);
+    }
+}
+
+// ---- forking --------------------------------------------------------------------------------
+//
+// table_out[i] = table[parent[i]]; refs[p] counts the table entries that name page p, so every entry
+// that changes takes one off the page it named and puts one on the page it names.  Sums of whole
+// numbers: the order of the atomics does not matter.
+__global__ __launch_bounds__(256) void fork_kernel(Paged c, int* refs, const int* parent, int B_out,
+                                                   int* table_out, int* lens_out) {
+    const int i = blockIdx.y;
+    const int col = blockIdx.x * 256 + threadIdx.x;
+    int from = -1;
+    if (i < B_out) {
+        from = parent[i];
+        if ((unsigned)from >= (unsigned)c.B) from = -1;
+        if (col == 0) lens_out[i] = from < 0 ? 0 : c.lens[from];
+    }
+    if (col >= c.max_pages) return;
+    const int now = i < c.B ? c.table[(size_t)i * c.max_pages + col] : -1;
+    const int next = from < 0 ? -1 : c.table[(size_t)from * c.max_pages + col];
+    if (i < B_out) table_out[(size_t)i * c.max_pages + col] = next;
+    if (next != now) {
+        if ((unsigned)next < (unsigned)c.P) atomicAdd(&refs[next], 1);
+        if ((unsigned)now < (unsigned)c.P) atomicSub(&refs[now], 1);
+    }
+}
+
+hipError_t launch_cache_fork(const Paged& c, int* refs, const int* parent, int B_out, int* table_out,
+                             int* lens_out, hipStream_t st) {
+    const dim3 grid((unsigned)((c.max_pages + 255) / 256), (unsigned)(B_out > c.B ? B_out : c.B)), block(256);
+    hipLaunchKernelGGL(fork_kernel, grid, block, 0, st, c, refs, parent, B_out, table_out, lens_out);
+    return hipGetLastError();
+}
+
+// ---- reserving ------------------------------------------------------------------------------
+//
+// One workgroup, so that which sequence gets which page does not depend on the order of anything:
+//   1. pages behind a sequence's keys go back (refs - 1);
+//   2. a sequence wants the pages from its first empty column to its last, and one more where its
+//      last page is part filled and shared (unless it is the first of sequences that are the
+//      page's only holders and all grow: that one keeps it);
+//   3. free pages (refs 0) are numbered in ascending order, k-th free page -> k-th wanted page.
+// Should there be too few, step 3 is left out and the number missing reported.
+constexpr int kReserveThreads = 1024;
+constexpr int kReserveWaves = kReserveThreads / kWave;
+constexpr int kReserveBlocks = 4096;      // the pool is counted in at most that many blocks of 256 m pages
+
+// Exclusive prefix sum over the workgroup's threads; `total` is their sum.
+__device__ __forceinline__ int block_scan(int x, int* waves, int& total) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    int in = x;
+#pragma unroll
+    for (int s = 1; s < 64; s <<= 1) {
+        const int y = __shfl_up(in, s);
+        if (lane >= s) in += y;
+    }
+    __syncthreads();                       // (the sums of an earlier scan have been read)
+    if (lane == 63) waves[wave] = in;
+    __syncthreads();
+    int before = 0;
+    total = 0;
+#pragma unroll
+    for (int w = 0; w < kReserveWaves; ++w) {
+        const int y = waves[w];
+        before += w < wave ? y : 0;
+        total += y;
+    }
+    return before + in - x;
+}
+
+__global__ __launch_bounds__(kReserveThreads) void reserve_kernel(Paged c, int* refs, int* report) {
+    __shared__ int at[kCacheMaxSeqs + 1];        // wanted pages of the sequences before b
+    __shared__ int last[kCacheMaxSeqs];          // part-filled last page of a sequence that grows, or -1
+    __shared__ int count[kReserveBlocks];        // free pages of the blocks before, from `first` on
+    __shared__ int waves[kReserveWaves];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int mask = (1 << c.page_log2) - 1;
+
+    // 1. back to the pool
+    for (int b = tid; b < c.B; b += kReserveThreads) {
+        const Seq s = seq_at(c, b);
+        int* row = c.table + (size_t)b * c.max_pages;
+        const int len = s.len, end = (len + s.n + mask) >> c.page_log2;
+        for (int col = end; col < c.max_pages; ++col) {
+            const int p = row[col];
+            if (p < 0) break;                    // owned pages come first in a row
+            row[col] = -1;
+            if (p < c.P) atomicSub(&refs[p], 1);
+        }
+        last[b] = s.n > 0 && (len & mask) != 0 ? page_at(c, b, len >> c.page_log2) : -1;
+    }
+    // what follows sees refs as these atomics leave them, not what a load has put into the compute
+    // unit's cache before
+    __threadfence();
+    __syncthreads();
+    __threadfence();
+
+    // 2. what each wants
+    int run = 0, beyond = 0;
+    for (int b0 = 0; b0 < c.B; b0 += kReserveThreads) {
+        const int b = b0 + tid;
+        int want = 0, past = 0;
+        if (b < c.B) {
+            const Seq s = seq_at(c, b);
+            const int tokens = max(min(c.q_start[b + 1], c.T) - s.row0, 0);
+            // tokens that the table has no columns for
+            past = (tokens - s.n + mask) >> c.page_log2;
+            const int* row = c.table + (size_t)b * c.max_pages;
+            const int end = (s.len + s.n + mask) >> c.page_log2;
+            int lo = min((s.len + mask) >> c.page_log2, end), hi = end;
+            if (s.n == 0) lo = end;
+            if (lo < hi && row[lo] < 0) hi = lo;
+            else if (lo < hi && row[hi - 1] >= 0) lo = hi;
+            while (lo < hi) {                    // the first empty column
+                const int mid = (lo + hi) >> 1;
+                if (row[mid] < 0) hi = mid;
+                else lo = mid + 1;
+            }
+            want = end - lo;
+            const int p = last[b];
+            if (p >= 0) {
+                const int refs_p = refs[p];
+                if (refs_p > 1) {
+                    int holders = 0, before = 0;
+                    for (int o = 0; o < c.B; ++o) {
+                        const bool same = last[o] == p;
+                        holders += same ? 1 : 0;
+                        before += same && o < b ? 1 : 0;
+                    }
+                    if (holders < refs_p || before > 0) want |= 1 << 30;    // and a copy
+                }
+            }
+        }
+        const int mine = (want & 0x3fffffff) + (want >> 30);
+        int all;
+        const int ex = block_scan(mine, waves, all);
+        if (b < c.B) {
+            at[b] = run + ex;
+            report[1 + b] = want >> 30 ? last[b] : -1;
+        }
+        run += all;
+        block_scan(past, waves, all);
+        beyond += all;
+    }
+    if (tid == 0) at[c.B] = run;
+
+    // free pages, by blocks of 256 m pages that each fall to one wavefront
+    const int m = (c.P + 256 * kReserveBlocks - 1) / (256 * kReserveBlocks);
+    const int blocks = (c.P + 256 * m - 1) / (256 * m);
+    for (int k = wave; k < blocks; k += kReserveWaves) {
+        int n = 0;
+        for (int j = 0; j < 4 * m; ++j) {
+            const int p = k * 256 * m + 64 * j + lane;
+            n += __popcll(__ballot(p < c.P && refs[p] == 0));
+        }
+        if (lane == 0) count[k] = n;
+    }
+    __syncthreads();
+    int free_pages = 0;
+    for (int k0 = 0; k0 < blocks; k0 += kReserveThreads) {
+        const int k = k0 + tid;
+        int all;
+        const int ex = block_scan(k < blocks ? count[k] : 0, waves, all);
+        if (k < blocks) count[k] = free_pages + ex;
+        free_pages += all;
+    }
+    __syncthreads();
+    const int missing = max(run - free_pages, 0) + beyond;
+    if (tid == 0) report[0] = missing;
+    if (missing > 0) {
+        for (int b = tid; b < c.B; b += kReserveThreads) report[1 + b] = -1;
+        return;
+    }
+
+    // 3. the k-th free page to the k-th wanted one
+    for (int k = wave; k < blocks; k += kReserveWaves) {
+        int rank = count[k];
+        for (int j = 0; j < 4 * m && rank < run; ++j) {
+            const int p = k * 256 * m + 64 * j + lane;
+            const bool is = p < c.P && refs[p] == 0;
+            const uint64_t all = __ballot(is);
+            const int mine = rank + __popcll(all & ((1ull << lane) - 1));
+            if (is && mine < run) {
+                int lo = 0, hi = c.B;            // the sequence: the last with at[b] <= mine
+                while (hi - lo > 1) {
+                    const int mid = (lo + hi) >> 1;
+                    if (at[mid] <= mine) lo = mid;
+                    else hi = mid;
+                }
+                const Seq s = seq_at(c, lo);
+                int* row = c.table + (size_t)lo * c.max_pages;
+                const int end = (s.len + s.n + mask) >> c.page_log2;
+                const int left = at[lo + 1] - mine;          // wanted pages from this one to the last
+                const bool copied = mine == at[lo] && report[1 + lo] >= 0;
+                if (copied) atomicSub(&refs[last[lo]], 1);
+                row[copied ? s.len >> c.page_log2 : end - left] = p;
+                refs[p] = 1;
+            }
+            rank += __popcll(all);
+        }
+    }
+}
+
+// Rows of the part-filled page that report names into the page that the sequence now has there.
+// Workgroup (b, j) takes every gridDim.y-th of the 2 * layers * Hkv pieces.
+__global__ __launch_bounds__(256) void copy_rows_kernel(Paged c, const int* report) {
+    const int b = blockIdx.x;
+    const int from = report[1 + b];
+    if ((unsigned)from >= (unsigned)c.P) return;
+    const Seq s = seq_at(c, b);
+    const int to = page_at(c, b, s.len >> c.page_log2);
+    if (to < 0) return;
+    const int64_t bytes = (int64_t)(s.len & ((1 << c.page_log2) - 1)) * c.d * c.esz;
+    for (int j = blockIdx.y; j < 2 * c.layers * c.Hkv; j += gridDim.y) {
+        const int h = j % c.Hkv, layer = j / c.Hkv >> 1;
+        char* base = (j / c.Hkv & 1 ? c.v : c.k) + (size_t)layer * c.layer_bytes + (size_t)h * c.head_bytes;
+        const u32x4* src = reinterpret_cast<const u32x4*>(base + (size_t)from * c.page_bytes);
+        u32x4* dst = reinterpret_cast<u32x4*>(base + (size_t)to * c.page_bytes);
+        for (int64_t i = threadIdx.x; i < bytes / 16; i += 256) dst[i] = src[i];
+    }
+}
+
+hipError_t launch_cache_reserve(const Paged& c, int* refs, int* report, hipStream_t st) {
+    hipLaunchKernelGGL(reserve_kernel, dim3(1), dim3(kReserveThreads), 0, st, c, refs, report);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    const long pieces = 2L * c.layers * c.Hkv;
+    hipLaunchKernelGGL(copy_rows_kernel, dim3((unsigned)c.B, (unsigned)(pieces < 64 ? pieces : 64)), dim3(256), 0,
+                       st, c, report);
+    return hipGetLastError();
+}
+
+// ---- committing -----------------------------------------------------------------------------
+//
+// Of a sequence's new tokens those that keep[] names (ascending) move together behind its keys: key
+// len + keep[i] -> len + i.  As keep[i] >= i, rows may be moved in ascending groups, each group read whole
+// before it is written: what a group writes lies before everything that later groups read.  A
+// wavefront moves the rows of one (layer, K or V, head).
+template <int RB>       // bytes of a row
+__global__ __launch_bounds__(256) void commit_kernel(Paged c, const int* keep, int max_keep,
+                                                     const int* n_keep, int* lens_out) {
+    constexpr int LPR = RB / 16;                  // lanes per row
+    constexpr int GROUP = kWave / LPR;            // rows per load
+    const int b = blockIdx.x;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const Seq s = seq_at(c, b);
+    int kept = n_keep != nullptr ? min(max(n_keep[b], 0), s.n) : s.n;
+    const int* list = keep != nullptr ? keep + (size_t)b * max_keep : nullptr;
+    if (keep != nullptr) {
+        // the list ends where it stops ascending or leaves the sequence's tokens
+        kept = min(kept, max_keep);
+        int good = 0;
+        for (int i0 = 0; i0 < kept; i0 += kWave) {
+            const int i = i0 + lane;
+            const int x = i < kept ? list[i] : 0;
+            const int y = i > 0 && i < kept ? list[i - 1] : -1;
+            const uint64_t bad = __ballot(i < kept && !(x > y && x < s.n));
+            const int here = min(kept - i0, kWave);
+            if (bad != 0) {
+                good += min(here, (int)__builtin_ctzll(bad));
+                break;
+            }
+            good += here;
+        }
+        kept = good;
+    }
+    if (blockIdx.y == 0 && threadIdx.x == 0) lens_out[b] = s.len + kept;
+    if (keep == nullptr) return;
+
+    const int mask = (1 << c.page_log2) - 1;
+    for (int j = blockIdx.y * 4 + wave; j < 2 * c.layers * c.Hkv; j += 4 * gridDim.y) {
+        const int h = j % c.Hkv, layer = j / c.Hkv >> 1;
+        char* base = (j / c.Hkv & 1 ? c.v : c.k) + (size_t)layer * c.layer_bytes + (size_t)h * c.head_bytes;
+        for (int i0 = 0; i0 < kept; i0 += GROUP) {
+            const int i = i0 + lane / LPR;
+            bool ok = i < kept;
+            const int from = ok ? list[i] : 0;
+            ok = ok && from != i;
+            const int sk = s.len + from, dk = s.len + i;
+            const int sp = ok ? page_at(c, b, sk >> c.page_log2) : -1, dp = ok ? page_at(c, b, dk >> c.page_log2) : -1;
+            ok = sp >= 0 && dp >= 0;
+            u32x4 x = {0u, 0u, 0u, 0u};
+            if (ok)
+                x = *reinterpret_cast<const u32x4*>(base + (size_t)sp * c.page_bytes + (size_t)(sk & mask) * RB + 16 * (lane % LPR));
+            // the wavefront's loads have all returned before the first of its stores is issued
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            if (ok)
+                *reinterpret_cast<u32x4*>(base + (size_t)dp * c.page_bytes + (size_t)(dk & mask) * RB + 16 * (lane % LPR)) = x;
+        }
+    }
+}
+
+hipError_t launch_cache_commit(const Paged& c, const int* keep, int max_keep, const int* n_keep,
+                               int* lens_out, hipStream_t st) {
+    const long pieces = 2L * c.layers * c.Hkv;
+    long y = keep == nullptr ? 1 : (pieces + 3) / 4;
+    if (y > 256) y = 256;
+    const dim3 grid((unsigned)c.B, (unsigned)y), block(256);
+    switch (c.d * c.esz) {
+    case 64: hipLaunchKernelGGL(commit_kernel<64>, grid, block, 0, st, c, keep, max_keep, n_keep, lens_out); break;
+    case 128: hipLaunchKernelGGL(commit_kernel<128>, grid, block, 0, st, c, keep, max_keep, n_keep, lens_out); break;
+    case 256: hipLaunchKernelGGL(commit_kernel<256>, grid, block, 0, st, c, keep, max_keep, n_keep, lens_out); break;
+    default: hipLaunchKernelGGL(commit_kernel<512>, grid, block, 0, st, c, keep, max_keep, n_keep, lens_out); break;
+    }
+    return hipGetLastError();
+}
+
+}  // namespace flashd

@@ -62,4 +62,9 @@ hipError_t launch_widen_fp8(const void* k8, const void* v8, void* k, void* v, si
 hipError_t launch_skip_stats(const Problem& p, float lo, float hi, unsigned long long* counts,
                              hipStream_t st);
 
+// Of the C ABI layer (flashd_api.hip), for entry points in other files: FLASHD_OK if the current device is
+// gfx950; scratch memory of a stream from the grow-only cache.
+int api_check_arch();
+int api_cached_workspace(void* stream, size_t bytes, void** out);
+
 }  // namespace flashd

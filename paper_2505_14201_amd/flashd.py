@@ -24,12 +24,27 @@ VARIANT_TILE_256 = 5
 MAX_SPLITS = 64
 STATIC_SCRATCH_BYTES = 32 << 20
 
+CACHE_FP8 = 3
+CACHE_MAX_SEQS = 4096
+
 _DTYPE = {torch.float32: F32, torch.float16: F16, torch.bfloat16: BF16}
+_CACHE_DTYPE = {**_DTYPE, torch.float8_e4m3fn: CACHE_FP8}
 
 EXPORTS = ("flashd_attn_fwd", "flashd_attn_fwd_ex", "flashd_workspace_bytes",
            "flashd_auto_splits", "flashd_auto_variant", "flashd_status_string", "flashd_version", "flashd_skip_stats", "flashd_attn_fwd_state",
            "flashd_attn_fwd_kv8", "flashd_attn_fwd_static", "flashd_attn_fwd_skipv",
-           "flashd_release_workspace")
+           "flashd_release_workspace", "flashd_cache_fork", "flashd_cache_reserve", "flashd_cache_append",
+           "flashd_attn_fwd_tree", "flashd_tree_workspace_bytes", "flashd_cache_commit")
+
+
+class Cache(ctypes.Structure):
+    """struct flashd_cache of include/flashd.h."""
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("table", ctypes.c_void_p),
+                ("lens", ctypes.c_void_p), ("page_stride", ctypes.c_longlong),
+                ("layer_stride", ctypes.c_longlong), ("layers", ctypes.c_int), ("P", ctypes.c_int),
+                ("page", ctypes.c_int), ("max_pages", ctypes.c_int), ("B", ctypes.c_int),
+                ("Hkv", ctypes.c_int), ("d", ctypes.c_int), ("dtype", ctypes.c_int),
+                ("kscale", ctypes.c_float), ("vscale", ctypes.c_float)]
 
 
 class FlashdError(RuntimeError):
@@ -66,6 +81,16 @@ def _load() -> ctypes.CDLL:
     lib.flashd_attn_fwd_kv8.argtypes = [p, p, p, p, i, i, i, i, i, i, i, f, f, f, i, p]
     lib.flashd_skip_stats.restype = i
     lib.flashd_skip_stats.argtypes = [p, p, i, i, i, i, i, i, i, f, i, f, f, p, p]
+    n, c = ctypes.c_longlong, ctypes.POINTER(Cache)
+    for name, args in (("fork", [c, p, p, i, p, p, p]), ("reserve", [c, p, p, p, p]),
+                       ("append", [c, i, p, n, p, n, p, n, p, n, i, i, p, p, p, i, i, p, p, f, i, p]),
+                       ("commit", [c, p, p, i, p, p, p])):
+        fn = getattr(lib, "flashd_cache_" + name)
+        fn.restype, fn.argtypes = i, args
+    lib.flashd_attn_fwd_tree.restype = i
+    lib.flashd_attn_fwd_tree.argtypes = [c, i, p, n, p, n, i, i, i, p, p, i, f, i, p, p, z]
+    lib.flashd_tree_workspace_bytes.restype = z
+    lib.flashd_tree_workspace_bytes.argtypes = [i] * 5
     lib.flashd_release_workspace.restype = i
     lib.flashd_release_workspace.argtypes = []
     lib.flashd_status_string.restype = ctypes.c_char_p
@@ -311,3 +336,185 @@ def attn_fwd_kv8(q, k8, v8, o, causal: bool, scale: float, kscale: float, vscale
     _enqueue(_lib.flashd_attn_fwd_kv8, q.get_device(), stream, (q.data_ptr(), k8.data_ptr(),
              v8.data_ptr(), o.data_ptr(), B, Hq, Hkv, Lq, Lk, d, int(bool(causal)), float(scale),
              float(kscale), float(vscale), _DTYPE[q.dtype]))
+
+
+# ---- keys and values in pages ----------------------------------------------------------------------
+#
+# kcache and vcache are [P, Hkv, page, d] (or [layers, P, Hkv, page, d] for the calls that work on all
+# layers), pages and layers at any stride; table is int32 [B, max_pages], lens int32 [B], q_start int32
+# [B + 1], refs int32 [P].  What they mean is described in include/flashd.h.
+
+def _ints(name, t, shape, device):
+    if t.dtype != torch.int32 or not t.is_contiguous() or t.get_device() != device or t.dim() != len(shape) or \
+            any(want is not None and have != want for have, want in zip(t.shape, shape)):
+        want = ", ".join("any" if x is None else str(x) for x in shape)
+        raise ValueError(f"{name} must be a contiguous int32 tensor [{want}] on the cache's GPU")
+
+
+def _cache(kcache, vcache, table, lens, kscale=1.0, vscale=1.0, layers=False):
+    """The struct for tensors of a cache; `layers`: five dimensions are allowed."""
+    if not kcache.is_cuda or not vcache.is_cuda:
+        raise ValueError("kcache and vcache must live on the GPU")
+    shape, stride, dtype = kcache.shape, kcache.stride(), kcache.dtype
+    if vcache.shape != shape or vcache.stride() != stride or vcache.dtype != dtype or dtype not in _CACHE_DTYPE \
+            or vcache.get_device() != kcache.get_device():
+        raise ValueError("kcache and vcache must have one shape, stride, device and type "
+                         "(float32, float16, bfloat16 or float8_e4m3fn)")
+    if len(shape) != 4 and not (layers and len(shape) == 5):
+        raise ValueError("expected kcache, vcache: " + ("[(layers,) P, Hkv, page, d]" if layers else "[P, Hkv, page, d]"))
+    P, Hkv, page, d = shape[-4:]
+    if stride[-3:] != (page * d, d, 1):
+        raise ValueError("a page of kcache and vcache must be contiguous")
+    device = kcache.get_device()
+    _ints("table", table, (None, None), device)
+    B, max_pages = table.shape
+    _ints("lens", lens, (B,), device)
+    if min(P, Hkv, page, d, B, max_pages, shape[0]) < 1:
+        raise ValueError("the cache has a dimension of size 0")
+    if max(P, page, max_pages) > 0x7fffffff:
+        raise FlashdError(-2)                      # FLASHD_E_SHAPE: more than the C call's ints hold
+    return Cache(kcache.data_ptr(), vcache.data_ptr(), table.data_ptr(), lens.data_ptr(),
+                 stride[-4] if P > 1 else Hkv * page * d, stride[0] if len(shape) == 5 else 0,
+                 shape[0] if len(shape) == 5 else 1, P, page, max_pages, B, Hkv, d, _CACHE_DTYPE[dtype],
+                 kscale, vscale)
+
+
+def _packed(name, t, T, heads, d, dtype, device):
+    """The stride of a token of a packed tensor [T, heads, d], whose rows must be contiguous."""
+    if t.get_device() != device or t.dtype != dtype or t.dim() != 3 or tuple(t.shape) != (T, heads, d):
+        raise ValueError(f"{name} must be [{T}, {heads}, {d}] of type {dtype} on the cache's GPU")
+    if T > 0x7fffffff:
+        raise FlashdError(-2)
+    s = t.stride()
+    if s[2] != 1 or (heads > 1 and s[1] != d):
+        raise ValueError(f"the heads of a token of {name} must be contiguous")
+    return s[0] if T > 1 else heads * d
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+def cache_fork(parent, refs, table, lens, table_out, lens_out, stream=None) -> None:
+    """flashd_cache_fork: sequence i of table_out [B_out, max_pages] and lens_out goes on where
+    sequence parent[i] of table and lens ended (empty if that is none); refs follows."""
+    if not table.is_cuda:
+        raise ValueError("table must live on the GPU")
+    device = table.get_device()
+    _ints("table", table, (None, None), device)
+    B, max_pages = table.shape
+    _ints("lens", lens, (B,), device)
+    _ints("parent", parent, (None,), device)
+    n = parent.shape[0]
+    _ints("table_out", table_out, (n, max_pages), device)
+    _ints("lens_out", lens_out, (n,), device)
+    _ints("refs", refs, (None,), device)
+    # (the pools themselves are not touched: any valid address and page size stand for them)
+    c = Cache(16, 16, table.data_ptr(), lens.data_ptr(), 16 * 64, 0, 1, refs.shape[0], 16, max_pages, B, 1, 64, F16, 1.0, 1.0)
+    _enqueue(_lib.flashd_cache_fork, device, stream, (c, refs.data_ptr(), parent.data_ptr(), n,
+             table_out.data_ptr(), lens_out.data_ptr()))
+
+
+def cache_reserve(kcache, vcache, refs, table, lens, q_start, report, stream=None) -> None:
+    """flashd_cache_reserve: every sequence gets exactly the pages of its keys and new tokens.
+    `report`: int32 [1 + B], receives the number of pages missing (0: all went well) and for each
+    sequence the page that its shared last page was copied from, or -1."""
+    c = _cache(kcache, vcache, table, lens, layers=True)
+    device = kcache.get_device()
+    _ints("refs", refs, (c.P,), device)
+    _ints("q_start", q_start, (c.B + 1,), device)
+    _ints("report", report, (c.B + 1,), device)
+    _enqueue(_lib.flashd_cache_reserve, device, stream, (c, refs.data_ptr(), q_start.data_ptr(),
+             report.data_ptr()))
+
+
+def cache_append(q, k, v, q_out, kcache, vcache, table, lens, q_start, positions=None, inv_freq=None,
+                 q_weight=None, k_weight=None, eps: float = 1e-6, interleaved: bool = False,
+                 kscale: float = 1.0, vscale: float = 1.0, stream=None) -> None:
+    """flashd_cache_append: q_out [T, Hq, d] <- norm and rotation of q; k (the same) and v [T, Hkv, d] into
+    the pages of one layer's cache.  q, k and v may be slices of one projection's output.  Without
+    weights nothing is normed, without inv_freq (float32 [rot / 2]) nothing is rotated; positions
+    (int32 [T]) default to the tokens' key numbers."""
+    c = _cache(kcache, vcache, table, lens, kscale, vscale)
+    device = kcache.get_device()
+    if q.dim() != 3 or q.dtype not in _DTYPE:
+        raise ValueError("expected q: [T, Hq, d] of type float32, float16 or bfloat16")
+    T, Hq, d = q.shape
+    if d != c.d:
+        raise ValueError("head dimension mismatch between q and kcache")
+    dtype = q.dtype
+    qs = _packed("q", q, T, Hq, d, dtype, device)
+    ks = _packed("k", k, T, c.Hkv, d, dtype, device)
+    vs = _packed("v", v, T, c.Hkv, d, dtype, device)
+    os_ = _packed("q_out", q_out, T, Hq, d, dtype, device)
+    _ints("q_start", q_start, (c.B + 1,), device)
+    if positions is not None:
+        _ints("positions", positions, (T,), device)
+    for name, w in (("q_weight", q_weight), ("k_weight", k_weight)):
+        if w is not None and (tuple(w.shape) != (d,) or w.dtype != dtype or w.get_device() != device or not w.is_contiguous()):
+            raise ValueError(f"{name} must be a contiguous tensor [d] of q's type")
+    rot = 0
+    if inv_freq is not None:
+        if inv_freq.dim() != 1 or inv_freq.dtype != torch.float32 or inv_freq.get_device() != device \
+                or not inv_freq.is_contiguous():
+            raise ValueError("inv_freq must be a contiguous float32 tensor [rot / 2] on the cache's GPU")
+        rot = 2 * inv_freq.shape[0]
+    if T == 0:
+        return
+    _enqueue(_lib.flashd_cache_append, device, stream, (c, 0, q.data_ptr(), qs, k.data_ptr(), ks, v.data_ptr(), vs,
+             q_out.data_ptr(), os_, T, Hq, q_start.data_ptr(), _ptr(positions), _ptr(inv_freq), rot,
+             int(bool(interleaved)), _ptr(q_weight), _ptr(k_weight), float(eps), _DTYPE[dtype]))
+
+
+def tree_workspace_bytes(Hq, Hkv, max_q, d, dtype) -> int:
+    return int(_lib.flashd_tree_workspace_bytes(Hq, Hkv, max_q, d, dtype))
+
+
+def attn_fwd_tree(q, kcache, vcache, o, table, lens, q_start, max_q: int, scale: float, tree=None,
+                  kscale: float = 1.0, vscale: float = 1.0, workspace=None, stream=None) -> None:
+    """flashd_attn_fwd_tree: o [T, Hq, d] <- attention of the new tokens' queries q over one layer's
+    cache.  `tree`: int64 [T, words], the new tokens of its sequence that each token sees, one bit
+    each; without it token i sees tokens 0 .. i.  max_q: the most new tokens of a sequence (a hint).
+    `workspace`: a contiguous tensor of at least tree_workspace_bytes(...) bytes; without it scratch
+    memory is kept per stream."""
+    c = _cache(kcache, vcache, table, lens, kscale, vscale)
+    device = kcache.get_device()
+    if q.dim() != 3 or q.dtype not in _DTYPE:
+        raise ValueError("expected q: [T, Hq, d] of type float32, float16 or bfloat16")
+    T, Hq, d = q.shape
+    if d != c.d:
+        raise ValueError("head dimension mismatch between q and kcache")
+    qs = _packed("q", q, T, Hq, d, q.dtype, device)
+    os_ = _packed("o", o, T, Hq, d, q.dtype, device)
+    _ints("q_start", q_start, (c.B + 1,), device)
+    words = 0
+    if tree is not None:
+        if tree.dtype != torch.int64 or tree.dim() != 2 or tree.shape[0] != T or not tree.is_contiguous() \
+                or tree.get_device() != device:
+            raise ValueError("tree must be a contiguous int64 tensor [T, words] on the cache's GPU")
+        words = tree.shape[1]
+    ws_ptr, ws_bytes = None, 0
+    if workspace is not None:
+        if workspace.get_device() != device or not workspace.is_contiguous():
+            raise ValueError("workspace must be a contiguous tensor on the cache's GPU")
+        ws_ptr, ws_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    if T == 0:
+        return
+    _enqueue(_lib.flashd_attn_fwd_tree, device, stream, (c, 0, q.data_ptr(), qs, o.data_ptr(), os_, T, int(max_q), Hq,
+             q_start.data_ptr(), _ptr(tree), words, float(scale), _DTYPE[q.dtype]), (ws_ptr, ws_bytes))
+
+
+def cache_commit(kcache, vcache, table, lens, q_start, lens_out, keep=None, n_keep=None, stream=None) -> None:
+    """flashd_cache_commit: the tokens that keep (int32 [B, max_keep], ascending) names move together
+    behind their sequence's keys, in every layer; lens_out [B] <- lens + n_keep.  Without `keep` the
+    first n_keep new tokens stay, without n_keep all."""
+    c = _cache(kcache, vcache, table, lens, layers=True)
+    device = kcache.get_device()
+    _ints("q_start", q_start, (c.B + 1,), device)
+    _ints("lens_out", lens_out, (c.B,), device)
+    if keep is not None:
+        _ints("keep", keep, (c.B, None), device)
+    if n_keep is not None:
+        _ints("n_keep", n_keep, (c.B,), device)
+    _enqueue(_lib.flashd_cache_commit, device, stream, (c, q_start.data_ptr(), _ptr(keep),
+             0 if keep is None else keep.shape[1], _ptr(n_keep), lens_out.data_ptr()))
