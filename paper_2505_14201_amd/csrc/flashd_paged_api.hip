@@ -224,7 +224,7 @@ int flashd_attn_fwd_tree(const flashd_cache* c, int layer, const void* q, long l
     a.o_stride = o_stride;
     a.words = tree != nullptr ? 2 * tree_words : 0;
     a.Hq = Hq;
-    a.max_q = max_q < T ? max_q : T;
+    a.max_q = max_q;
     a.dtype = dtype;
     a.fp8 = c->dtype == FLASHD_CACHE_FP8;
     a.scale = scale;

@@ -16,15 +16,17 @@
 #include "flashd_kernels.h"
 #include "flashd_mma.h"
 #include "flashd_paged.h"
+#include "flashd_rows.h"
+#include "flashd_tile_parts.h"
 
 #include <type_traits>
 
 namespace flashd {
 
-constexpr int kTreeBlock = 32;          // keys per step of a wavefront
+constexpr int kTreeBlock = 32;          // keys of a block: a wavefront's step
 constexpr int kTreeWaves = 4;
-constexpr int kTreeMostGroups = 512;    // workgroups of a launch
-constexpr int kTreeMinBlocks = 4;       // blocks a workgroup takes at least, one per wavefront
+constexpr int kTreeMostGroups = 512;    // workgroups of a launch, two per compute unit
+constexpr int kTreeMinBlocks = 4;       // blocks a workgroup takes at least
 
 template <typename T> struct Mma16;
 template <> struct Mma16<BF16> {
@@ -54,122 +56,193 @@ struct TreeRun {
     Paged c;
     TreeArgs a;
     FastDiv group;          // query heads per kv head
-    float* parts;           // [2 groups][16][d] unnormalised outputs
-    float2* stats;          // [2 groups][16] reference and sum of weights
+    float* parts;           // [2 groups][rows of a tile][d] unnormalised outputs
+    float2* stats;          // [2 groups][rows of a tile] reference and sum of weights
     TreeSplit* splits;      // [groups]
+    int* groups;            // how many workgroups have work
 };
-
-constexpr int kTreeRows = 16;
 
 // ---- the share of a workgroup ------------------------------------------------------------------
 
-__device__ __forceinline__ int tree_tiles(const Seq& s, int G) {
-    return (int)(((long long)s.n * G + kTreeRows - 1) / kTreeRows);
-}
-__device__ __forceinline__ int tree_blocks(const Seq& s) {
-    return (s.len + s.n + kTreeBlock - 1) / kTreeBlock;
+// A value that is the same in every lane, in a scalar register
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ long long uniform(long long x) {
+    return (long long)((uint64_t)(uint32_t)uniform((int)(x >> 32)) << 32 | (uint32_t)uniform((int)x));
 }
 
 // A workgroup's way along the row of blocks, and the piece of a unit that it is at (all the same in every
-// thread).
+// thread, in scalar registers).  M: rows of a tile; KB: keys of a block of the row.  Of a chain's row tile only the blocks count
+// that its last token sees.
+template <int M, int KB>
 struct Walk {
     long long at, end;      // blocks of the long row
     long long per;          // blocks of every workgroup
-    long long in_b, in_seq; // blocks of the present sequence before `at`, and in all
-    int b;                  // present sequence
+    int w;                  // the workgroup's place along the row
+    int b, h, tile;         // present unit
     Seq s;
-    int blocks, tiles;      // of the present sequence: blocks per unit, row tiles
-    // the piece
-    int h, first, nrows;    // kv head; first row (token, head of the group) of the tile, rows
-    int blk0, blk1;         // its blocks of the unit
+    int tiles;              // row tiles of the sequence
+    int blocks;             // blocks of the unit
+    int blk0, blk1;         // the piece
+    int first, nrows;       // its first row (token, head of the group), and rows
 
     __device__ __forceinline__ bool whole() const { return blk0 == 0 && blk1 == blocks; }
+    __device__ __forceinline__ int keys() const { return s.len + s.n; }
 
-    __device__ __forceinline__ void enter(const Paged& c, int G, int seq) {
+    __device__ __forceinline__ int blocks_of(const TreeRun& r, int t) const {
+        int keys = s.len + s.n;
+        if (r.a.tree == nullptr) {
+            const long long end = (long long)(t + 1) * M;       // rows up to the tile's last
+            const int token = end < (long long)s.n * (int)r.group.d ? (int)fast_div((uint32_t)(end - 1), r.group) : s.n - 1;
+            keys = s.len + token + 1;
+        }
+        return (keys + KB - 1) / KB;
+    }
+    // Sequence `seq`; returns the blocks of one kv head's units.
+    __device__ __forceinline__ long long enter(const TreeRun& r, int seq) {
         b = seq;
-        s = seq_at(c, b);
-        blocks = tree_blocks(s);
-        tiles = tree_tiles(s, G);
-        in_seq = (long long)tiles * c.Hkv * blocks;
+        s = seq_at(r.c, b);
+        tiles = (int)(((long long)s.n * (int)r.group.d + M - 1) / M);
+        long long sum = 0;
+        if (r.a.tree != nullptr) sum = tiles > 0 ? (long long)tiles * blocks_of(r, 0) : 0;
+        else for (int t = 0; t < tiles; ++t) sum += blocks_of(r, t);
+        return sum;
+    }
+    __device__ __forceinline__ void set_unit(const TreeRun& r) {
+        blocks = blocks_of(r, tile);
+        first = tile * M;
+        nrows = min(M, s.n * (int)r.group.d - first);
+    }
+    __device__ __forceinline__ void set_piece(int from) {
+        const long long left = end - at;
+        blk0 = from;
+        blk1 = (int)(left < blocks - from ? from + left : blocks);
     }
 
-    // The next piece; false at the end of the share.
-    __device__ __forceinline__ bool next(const Paged& c, int G) {
-        if (at >= end) return false;
-        while (in_b >= in_seq) {            // on to the next sequence with new tokens
-            if (b + 1 >= c.B) return false;
-            enter(c, G, b + 1);
-            in_b = 0;
+    // Every thread of the workgroup takes a run of sequences, whose blocks are then summed over the threads;
+    // the one that has the share's first block in its run finds the sequence.
+    __device__ __forceinline__ void begin(const TreeRun& r) {
+        __shared__ long long wave_sum[kTreeWaves];
+        __shared__ long long found_before;
+        __shared__ int found_b;
+        const Paged& c = r.c;
+        const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+        const int each = (c.B + kTreeWaves * kWave - 1) / (kTreeWaves * kWave);
+        const int b0 = tid * each, b1 = min(b0 + each, c.B);
+        long long mine = 0;
+        Walk any;
+        for (int i = b0; i < b1; ++i) mine += any.enter(r, i) * c.Hkv;
+        long long in = mine;
+#pragma unroll
+        for (int k = 1; k < 64; k <<= 1) {
+            const long long y = __shfl_up(in, k);
+            if (lane >= k) in += y;
         }
-        const int unit = (int)(in_b / blocks);
-        blk0 = (int)(in_b - (long long)unit * blocks);
-        const long long left = end - at;
-        blk1 = (int)(left < blocks - blk0 ? blk0 + left : blocks);
-        h = unit / tiles;
-        first = (unit - h * tiles) * kTreeRows;
-        nrows = min(kTreeRows, s.n * G - first);
+        if (lane == 63) wave_sum[wave] = in;
+        if (tid == 0) found_b = -1;
+        __syncthreads();
+        long long before = in - mine, total = 0;
+#pragma unroll
+        for (int k = 0; k < kTreeWaves; ++k) {
+            before += k < wave ? wave_sum[k] : 0;
+            total += wave_sum[k];
+        }
+        total = uniform(total);
+        constexpr int kLeast = kTreeMinBlocks * kTreeBlock / KB;
+        long long groups = (total + kLeast - 1) / kLeast;
+        if (groups > gridDim.x) groups = gridDim.x;
+        per = groups > 0 ? (total + groups - 1) / groups : 1;
+        // Workgroup ids go round-robin over the 8 XCDs; neighbours along the row, which may read the same
+        // keys, go to one.
+        const int of_xcd = (int)((groups + 7) >> 3);
+        const int k = (int)blockIdx.x >> 3;
+        w = ((int)blockIdx.x & 7) * of_xcd + k;
+        at = k < of_xcd && w < groups ? per * w : total;
+        end = at + per < total ? at + per : total;
+        if (blockIdx.x == 0 && tid == 0) *r.groups = (int)groups;
+        if (at < end && at >= before && at < before + mine) {
+            for (int i = b0; i < b1; ++i) {
+                const long long sum = any.enter(r, i) * c.Hkv;
+                if (at < before + sum) {
+                    found_b = i;
+                    found_before = before;
+                    break;
+                }
+                before += sum;
+            }
+        }
+        if (tid == 0 && k < of_xcd && w < groups) r.splits[w].parts = 0;
+        __syncthreads();
+        const int found = uniform(found_b);
+        if (found < 0) {
+            end = at;
+            return;
+        }
+        const long long head = uniform(enter(r, found)), in_b = at - uniform(found_before);
+        h = uniform((int)(in_b / head));
+        int from;
+        if (r.a.tree != nullptr) {
+            const int each_tile = blocks_of(r, 0);
+            const long long rest = in_b - h * head;
+            tile = uniform((int)(rest / each_tile));
+            from = (int)(rest - (long long)tile * each_tile);
+        } else {
+            long long rest = in_b - h * head;
+            for (tile = 0; rest >= blocks_of(r, tile); ++tile) rest -= blocks_of(r, tile);
+            from = (int)rest;
+        }
+        set_unit(r);
+        set_piece(from);
+    }
+    // On to the next piece; false at the end of the share.
+    __device__ __forceinline__ bool next(const TreeRun& r) {
+        at += blk1 - blk0;
+        if (at >= end) return false;
+        if (++tile == tiles) {
+            tile = 0;
+            if (++h == r.c.Hkv) {
+                h = 0;
+                do {
+                    if (b + 1 >= r.c.B) return false;
+                    enter(r, b + 1);
+                } while (tiles == 0);
+            }
+        }
+        set_unit(r);
+        set_piece(0);
         return true;
     }
-    __device__ __forceinline__ void done() {
-        at += blk1 - blk0;
-        in_b += blk1 - blk0;
+    __device__ __forceinline__ int slot() const { return 2 * w + (blk0 == 0 ? 1 : 0); }
+    __device__ __forceinline__ void note_split(const TreeRun& r) const {
+        TreeSplit sp;
+        sp.row0 = s.row0;
+        sp.h = h;
+        sp.first = first;
+        sp.rows = nrows;
+        sp.parts = (int)((at + blocks - 1) / per) - w + 1;
+        sp.pad[0] = sp.pad[1] = sp.pad[2] = 0;
+        r.splits[w] = sp;
     }
 };
 
-// Every thread of the workgroup takes a run of sequences, whose blocks are then summed over the threads.
-__device__ __forceinline__ Walk begin_walk(const Paged& c, int G) {
-    __shared__ long long wave_sum[kTreeWaves];
-    __shared__ long long found_before;
-    __shared__ int found_b;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int each = (c.B + kTreeWaves * kWave - 1) / (kTreeWaves * kWave);
-    const int b0 = tid * each, b1 = min(b0 + each, c.B);
-    Walk r;
-    long long mine = 0;
-    for (int b = b0; b < b1; ++b) {
-        r.enter(c, G, b);
-        mine += r.in_seq;
+// Element offset of row `rw` (token, head of the group) of the piece's sequence in q or o
+template <class W>
+__device__ __forceinline__ size_t row_at(const TreeRun& r, const W& u, int rw, int64_t stride, int d) {
+    const int token = (int)fast_div((uint32_t)rw, r.group);
+    return (size_t)(u.s.row0 + token) * stride + (size_t)(u.h * (int)r.group.d + rw - token * (int)r.group.d) * d;
+}
+
+// A finished row's four columns from t on: the output, or the unit's partial state.
+template <typename T, int D, int M, class W>
+__device__ __forceinline__ void put_row(const TreeRun& r, const W& u, int fr, int t, f32x4 o, float top, float lt,
+                                        float vscale) {
+    if (u.whole()) {
+        if (lt != 0.0f) o *= vscale / lt;
+        Store<T>::store4(r.a.o, row_at(r, u, u.first + fr, r.a.o_stride, D) + t, {o[0], o[1], o[2], o[3]});
+    } else {
+        const size_t at = (size_t)u.slot() * M + fr;
+        *reinterpret_cast<f32x4*>(r.parts + at * D + t) = o;
+        if (t == 0) r.stats[at] = float2{top, lt};
     }
-    long long in = mine;
-#pragma unroll
-    for (int s = 1; s < 64; s <<= 1) {
-        const long long y = __shfl_up(in, s);
-        if (lane >= s) in += y;
-    }
-    if (lane == 63) wave_sum[wave] = in;
-    if (tid == 0) found_b = -1;
-    __syncthreads();
-    long long before = in - mine, total = 0;
-#pragma unroll
-    for (int w = 0; w < kTreeWaves; ++w) {
-        before += w < wave ? wave_sum[w] : 0;
-        total += wave_sum[w];
-    }
-    long long groups = (total + kTreeMinBlocks - 1) / kTreeMinBlocks;
-    if (groups > gridDim.x) groups = gridDim.x;
-    r.per = groups > 0 ? (total + groups - 1) / groups : 1;
-    r.at = r.per * blockIdx.x;
-    r.end = r.at + r.per < total ? r.at + r.per : total;
-    if (r.at < r.end && r.at >= before && r.at < before + mine) {
-        for (int b = b0; b < b1; ++b) {
-            r.enter(c, G, b);
-            if (r.at < before + r.in_seq) {
-                found_b = b;
-                found_before = before;
-                break;
-            }
-            before += r.in_seq;
-        }
-    }
-    __syncthreads();
-    const int b = __builtin_amdgcn_readfirstlane(found_b);
-    if (b < 0) {
-        r.end = r.at;
-        return r;
-    }
-    r.in_b = r.at - found_before;
-    r.enter(c, G, b);
-    return r;
 }
 
 // The bits of the 32 keys from j0 on that the token `i` (row `t` of the packed tensors) sees.
@@ -232,65 +305,47 @@ __device__ __forceinline__ void weigh(float (&x)[8], f32x8& p, f32x4 (&U)[NDB], 
     for (int e = 0; e < 8; ++e) p[e] = exp2_fast(x[e] - ref);
 }
 
-// Joins the wavefronts' states of a piece: the output if the piece is a whole unit, else a partial state.
-template <typename T, int D>
-__device__ __forceinline__ void finish_piece(const TreeRun& r, const Walk& u, const f32x4 (&U)[D / 16], float R,
-                                             float l, float* fold, float vscale) {
+// Joins the four wavefronts' states of a piece whose keys they have shared out: row tiles of 16 NR rows.
+template <typename T, int D, int NR, class Wk>
+__device__ __forceinline__ void finish_rows(const TreeRun& r, const Wk& u, const f32x4 (&U)[NR][D / 16],
+                                            const float (&R)[NR], const float (&l)[NR], float* fold, float vscale) {
     constexpr int W = kTreeWaves, FROW = D + 4, NDB = D / 16;
     __shared__ float fold_r[W][16], fold_l[W][16];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, col = lane & 15, q = lane >> 4;
-    l = quad_sum(l);
-    __syncthreads();                                     // stages are dead, `fold` is their memory
 #pragma unroll
-    for (int i = 0; i < NDB; ++i)
-        *reinterpret_cast<f32x4*>(&fold[(wave * 16 + col) * FROW + 16 * i + 4 * q]) = U[i];
-    if (q == 0) {
-        fold_r[wave][col] = R;
-        fold_l[wave][col] = l;
-    }
-    __syncthreads();
-    const bool whole = u.whole();
-    const int G = (int)r.group.d;
-    const int slot = 2 * (int)blockIdx.x + (u.blk0 == 0 ? 1 : 0);
-    for (int idx = tid; idx < u.nrows * (D / 4); idx += W * kWave) {
-        const int fr = idx / (D / 4);
-        const int t = 4 * (idx % (D / 4));
-        float top = fold_r[0][fr];
+    for (int k = 0; k < NR; ++k) {
+        const float lk = quad_sum(l[k]);
+        __syncthreads();                                 // stages are dead, `fold` is their memory
 #pragma unroll
-        for (int w = 1; w < W; ++w) top = fmaxf(top, fold_r[w][fr]);
-        float lt = 0.0f;
-        f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-        for (int w = 0; w < W; ++w) {
-            // a wavefront without a key of the row is left out (its U may hold 0 * infinity)
-            const bool none = fold_l[w][fr] == 0.0f;
-            const float f = none ? 0.0f : exp2_fast(fold_r[w][fr] - top);
-            const f32x4 x = *reinterpret_cast<const f32x4*>(&fold[(w * 16 + fr) * FROW + t]);
-            lt = fmaf(f, fold_l[w][fr], lt);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) o[e] = fmaf(f, none ? 0.0f : x[e], o[e]);
+        for (int i = 0; i < NDB; ++i)
+            *reinterpret_cast<f32x4*>(&fold[(wave * 16 + col) * FROW + 16 * i + 4 * q]) = U[k][i];
+        if (q == 0) {
+            fold_r[wave][col] = R[k];
+            fold_l[wave][col] = lk;
         }
-        if (whole) {
-            if (lt != 0.0f) o *= vscale / lt;
-            const int rw = u.first + fr;
-            const int tk = (int)fast_div((uint32_t)rw, r.group);
-            Store<T>::store4(r.a.o, (size_t)(u.s.row0 + tk) * r.a.o_stride + (size_t)(u.h * G + rw - tk * G) * D + t,
-                             {o[0], o[1], o[2], o[3]});
-        } else {
-            *reinterpret_cast<f32x4*>(r.parts + ((size_t)slot * kTreeRows + fr) * D + t) = o;
-            if (t == 0) r.stats[slot * kTreeRows + fr] = float2{top, lt};
+        __syncthreads();
+        for (int idx = tid; idx < min(u.nrows - 16 * k, 16) * (D / 4); idx += W * kWave) {
+            const int fr = idx / (D / 4);
+            const int t = 4 * (idx % (D / 4));
+            float top = fold_r[0][fr];
+#pragma unroll
+            for (int w = 1; w < W; ++w) top = fmaxf(top, fold_r[w][fr]);
+            float lt = 0.0f;
+            f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int w = 0; w < W; ++w) {
+                // a wavefront without a key of the row is left out (its U may hold 0 * infinity)
+                const bool none = fold_l[w][fr] == 0.0f;
+                const float f = none ? 0.0f : exp2_fast(fold_r[w][fr] - top);
+                const f32x4 x = *reinterpret_cast<const f32x4*>(&fold[(w * 16 + fr) * FROW + t]);
+                lt = fmaf(f, fold_l[w][fr], lt);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[e] = fmaf(f, none ? 0.0f : x[e], o[e]);
+            }
+            put_row<T, D, 16 * NR>(r, u, 16 * k + fr, t, o, top, lt, vscale);
         }
     }
-    if (u.blk0 == 0 && !whole && tid == 0) {
-        TreeSplit sp;
-        sp.row0 = u.s.row0;
-        sp.h = u.h;
-        sp.first = u.first;
-        sp.rows = u.nrows;
-        sp.parts = (int)((u.at + u.blocks - 1) / u.per) - (int)blockIdx.x + 1;
-        sp.pad[0] = sp.pad[1] = sp.pad[2] = 0;
-        r.splits[blockIdx.x] = sp;
-    }
+    if (u.blk0 == 0 && !u.whole() && tid == 0) u.note_split(r);
     __syncthreads();
 }
 
@@ -298,26 +353,28 @@ __device__ __forceinline__ void finish_piece(const TreeRun& r, const Walk& u, co
 // l & 1 of block l / 2.  -1 where there is no page, or no key.
 struct PageWindow {
     int pages, from;
-    __device__ __forceinline__ int at(const Paged& c, const Walk& u, int wave, int lane, int blk, int half) {
+    template <class W>
+    __device__ __forceinline__ int at(const Paged& c, const W& u, int wave, int lane, int blk, int half) {
         const int k = (blk - u.blk0) / kTreeWaves;
         if (k / 32 != from) {
             from = k / 32;
             const int mine = u.blk0 + wave + kTreeWaves * (32 * from + (lane >> 1));
             const int key = mine * kTreeBlock + 16 * (lane & 1);
             pages = -1;
-            if (mine < u.blk1 && key < u.s.len + u.s.n) pages = page_at(c, u.b, key >> c.page_log2);
+            if (mine < u.blk1 && key < u.keys()) pages = page_at(c, u.b, key >> c.page_log2);
         }
         return __builtin_amdgcn_readlane(pages, 2 * (k & 31) + half);
     }
 };
 
 // 16 keys of a block: their bytes up to the sequence's last key, or nothing without a page.
-__device__ __forceinline__ __amdgpu_buffer_rsrc_t half_window(const Paged& c, const Walk& u, const char* pool,
+template <class W>
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t half_window(const Paged& c, const W& u, const char* pool,
                                                               int page, int key) {
     const int row = (int)(c.head_bytes >> c.page_log2);
     const char* at = pool + (int64_t)max(page, 0) * c.page_bytes + u.h * c.head_bytes +
                      (int64_t)(key & ((1 << c.page_log2) - 1)) * row;
-    return kv_window(at, page < 0 ? 0 : (int64_t)min(16, u.s.len + u.s.n - key) * row);
+    return kv_window(at, page < 0 ? 0 : (int64_t)min(16, u.keys() - key) * row);
 }
 
 // ---- 16 rows, keys shared out over the wavefronts (f16 / bf16) -----------------------------------
@@ -331,8 +388,7 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t half_window(const Paged& c, co
 // keys behind it, and pages that are none, read zeros.
 //
 // In blocks with new keys a weight of zero may meet a value that is infinite or NaN (a token that some rows see
-// and others do not): 0 * infinity must not reach the others, so such blocks leave the matrix cores and
-// add their visible keys one by one.
+// and others do not), and 0 * infinity must not reach the others: see take_apart().
 
 // any of 8 values of the storage type (16 fp8 values) is infinite or NaN
 template <typename T, bool FP8>
@@ -351,13 +407,45 @@ __device__ __forceinline__ bool not_finite(u32x4 x) {
     return bad;
 }
 
-template <typename T> __device__ __forceinline__ float one_value(uint32_t half);
-template <> __device__ __forceinline__ float one_value<BF16>(uint32_t half) { return __uint_as_float(half << 16); }
-template <> __device__ __forceinline__ float one_value<F16>(uint32_t half) {
-    return (float)__builtin_bit_cast(_Float16, (unsigned short)half);
+// The products of such a block: the values that are no numbers are left out of the product with the weights and
+// counted by one with the bits of what is seen, +infinities as 1, -infinities as 64, NaN as 4096 (a block has 32
+// keys, and the sum is exact); what_is_seen() says what a count adds to an output.
+template <typename T>
+__device__ __forceinline__ void take_apart(u32x4 x, u32x4& numbers, u32x4& codes) {
+    constexpr bool B = Mma<T>::kRoundedSum;
+    constexpr uint32_t e = B ? 0x7f80u : 0x7c00u, m = B ? 0x7fu : 0x3ffu;
+    constexpr uint32_t one = B ? 0x3f80u : 0x3c00u, minus = B ? 0x4280u : 0x5400u, nan = B ? 0x4580u : 0x6c00u;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        uint32_t keep = 0, code = 0;
+#pragma unroll
+        for (int h = 0; h < 32; h += 16) {
+            const uint32_t y = x[i] >> h & 0xffffu;
+            const bool bad = (y & e) == e;
+            keep |= bad ? 0u : y << h;
+            code |= bad ? ((y & m) != 0 ? nan : y >> 15 ? minus : one) << h : 0u;
+        }
+        numbers[i] = keep;
+        codes[i] = code;
+    }
+}
+__device__ __forceinline__ float what_is_seen(float count) {
+    const int n = (int)count;
+    const float inf = __builtin_inff();
+    const bool plus = (n & 63) != 0, minus = (n >> 6 & 63) != 0;
+    return n >= 4096 || (plus && minus) ? __builtin_nanf("") : plus ? inf : minus ? -inf : 0.0f;
+}
+// 8 bits, lowest first, as ones and zeros of the storage type
+template <typename T>
+__device__ __forceinline__ u32x4 ones_of(uint32_t bits) {
+    u32x4 x;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        x[i] = (bits >> (2 * i) & 1u ? Mma<T>::kOnes & 0xffffu : 0u) | (bits >> (2 * i + 1) & 1u ? Mma<T>::kOnes & 0xffff0000u : 0u);
+    return x;
 }
 
-template <typename T, int D, bool FP8>
+template <typename T, int D, bool FP8, int NR>
 __global__ __launch_bounds__(kTreeWaves * kWave, 2) void tree_rows_kernel(TreeRun r) {
     constexpr int W = kTreeWaves;
     constexpr int NKK = D / 32;
@@ -379,21 +467,24 @@ __global__ __launch_bounds__(kTreeWaves * kWave, 2) void tree_rows_kernel(TreeRu
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int col = lane & 15;
     const int q = lane >> 4;
-    const int G = (int)r.group.d;
     const float ninf = -__builtin_inff();
     uint16_t* vs = reinterpret_cast<uint16_t*>(lds) + wave * STAGE;
 
-    Walk u = begin_walk(c, G);
-    if (tid == 0) r.splits[blockIdx.x].parts = 0;
-    for (; u.next(c, G); u.done()) {
-        // the query row of this lane's column; columns past the last row stand in for it
-        const int row = u.first + min(col, u.nrows - 1);
-        const int token = (int)fast_div((uint32_t)row, r.group);
-        const int head = u.h * G + row - token * G;
-        const uint16_t* qg = static_cast<const uint16_t*>(a.q) + (size_t)(u.s.row0 + token) * a.q_stride + (size_t)head * D;
-        u32x4 qf[NKK];
+    Walk<16 * NR, kTreeBlock> u;
+    u.begin(r);
+    if (u.at >= u.end) return;
+    do {
+        // the query rows of this lane's column; columns past the last row stand in for it
+        int token[NR];
+        u32x4 qf[NR][NKK];
 #pragma unroll
-        for (int kk = 0; kk < NKK; ++kk) qf[kk] = *reinterpret_cast<const u32x4*>(qg + 32 * kk + 8 * q);
+        for (int k = 0; k < NR; ++k) {
+            const int row = u.first + min(16 * k + col, u.nrows - 1);
+            token[k] = (int)fast_div((uint32_t)row, r.group);
+            const uint16_t* qg = static_cast<const uint16_t*>(a.q) + row_at(r, u, row, a.q_stride, D);
+#pragma unroll
+            for (int kk = 0; kk < NKK; ++kk) qf[k][kk] = *reinterpret_cast<const u32x4*>(qg + 32 * kk + 8 * q);
+        }
         const float c_log2 = (FP8 ? a.scale * c.kscale : a.scale) * kLog2e;
 
         auto fetch = [&](const char* pool, u32x4 (&reg)[NV], int blk, int p0, int p1) __attribute__((always_inline)) {
@@ -425,10 +516,15 @@ __global__ __launch_bounds__(kTreeWaves * kWave, 2) void tree_rows_kernel(TreeRu
             __builtin_amdgcn_wave_barrier();
         };
 
-        f32x4 U[NDB];
+        f32x4 U[NR][NDB];
+        float R[NR], l[NR];
 #pragma unroll
-        for (int i = 0; i < NDB; ++i) U[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-        float R = ninf, l = 0.0f;
+        for (int k = 0; k < NR; ++k) {
+            R[k] = ninf;
+            l[k] = 0.0f;
+#pragma unroll
+            for (int i = 0; i < NDB; ++i) U[k][i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        }
 
         PageWindow pages{-1, -1};
         u32x4 kreg[NV], vreg[NV];
@@ -452,15 +548,18 @@ __global__ __launch_bounds__(kTreeWaves * kWave, 2) void tree_rows_kernel(TreeRu
             }
             stage(kreg, KROW);
             if (more) fetch(c.k, kreg, blk + W, n0, n1);
-            f32x4 acc[2];
+            f32x4 acc[NR][2];
 #pragma unroll
-            for (int t = 0; t < 2; ++t) acc[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+            for (int k = 0; k < NR; ++k)
+#pragma unroll
+                for (int t = 0; t < 2; ++t) acc[k][t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
             for (int kk = 0; kk < NKK; ++kk)
 #pragma unroll
                 for (int t = 0; t < 2; ++t) {
                     const u32x4 x = *reinterpret_cast<const u32x4*>(&vs[(16 * t + col) * KROW + 32 * kk + 8 * q]);
-                    acc[t] = Mma16<T>::mfma(x, qf[kk], acc[t]);
+#pragma unroll
+                    for (int k = 0; k < NR; ++k) acc[k][t] = Mma16<T>::mfma(x, qf[k][kk], acc[k][t]);
                 }
             stage_done();
             stage(vreg, VROW);
@@ -473,49 +572,54 @@ __global__ __launch_bounds__(kTreeWaves * kWave, 2) void tree_rows_kernel(TreeRu
             }
             if (more) fetch(c.v, vreg, blk + W, n0, n1);
 
-            uint32_t bits = ~0u;
-            if (masked) bits = have & seen_bits(a, u.s, token, u.s.row0 + token, j0);
-            float x[8];
+            u32x4 bfrag[NR];
+            uint32_t bits[NR];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                x[e] = acc[e >> 2][e & 3] * c_log2;
-                if (masked && !(bits >> (16 * (e >> 2) + 4 * q + (e & 3)) & 1u)) x[e] = ninf;
+            for (int k = 0; k < NR; ++k) {
+                bits[k] = ~0u;
+                if (masked) bits[k] = have & seen_bits(a, u.s, token[k], u.s.row0 + token[k], j0);
+                float x[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    x[e] = acc[k][e >> 2][e & 3] * c_log2;
+                    if (masked && !(bits[k] >> (16 * (e >> 2) + 4 * q + (e & 3)) & 1u)) x[e] = ninf;
+                }
+                f32x8 pv;
+                weigh(x, pv, U[k], R[k], l[k], LazyLimit<T>::kMoveLog2);
+                bfrag[k] = Mma<T>::pack8(pv);
+                f32x4 ps = {0.0f, 0.0f, 0.0f, 0.0f};
+                Mma<T>::sum8(pv, bfrag[k], ps);
+                l[k] += (ps[0] + ps[1]) + (ps[2] + ps[3]);
             }
-            f32x8 pv;
-            weigh(x, pv, U, R, l, LazyLimit<T>::kMoveLog2);
-            const u32x4 bfrag = Mma<T>::pack8(pv);
-            f32x4 ps = {0.0f, 0.0f, 0.0f, 0.0f};
-            Mma<T>::sum8(pv, bfrag, ps);
-            l += (ps[0] + ps[1]) + (ps[2] + ps[3]);
-
+            const uint16_t* base = &vs[(4 * q + (col >> 2)) * VROW + 4 * (col & 3)];
+            typedef s16x4 __attribute__((address_space(3))) * lds_ptr;
+            auto v_operand = [&](int i) __attribute__((always_inline)) {
+                const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                    (lds_ptr)(base + 16 * i)));
+                const u32x2 hi = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                    (lds_ptr)(base + 16 * VROW + 16 * i)));
+                return u32x4{lo[0], lo[1], hi[0], hi[1]};
+            };
             if (!apart) {
-                const uint16_t* base = &vs[(4 * q + (col >> 2)) * VROW + 4 * (col & 3)];
-                typedef s16x4 __attribute__((address_space(3))) * lds_ptr;
 #pragma unroll
                 for (int i = 0; i < NDB; ++i) {
-                    const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                        (lds_ptr)(base + 16 * i)));
-                    const u32x2 hi = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                        (lds_ptr)(base + 16 * VROW + 16 * i)));
-                    U[i] = Mma16<T>::mfma(u32x4{lo[0], lo[1], hi[0], hi[1]}, bfrag, U[i]);
+                    const u32x4 v = v_operand(i);
+#pragma unroll
+                    for (int k = 0; k < NR; ++k) U[k][i] = Mma16<T>::mfma(v, bfrag[k], U[k][i]);
                 }
             } else {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const float mine = one_value<T>(e & 1 ? bfrag[e >> 1] >> 16 : bfrag[e >> 1] & 0xffffu);
-                    for (int k = 0; k < 4; ++k) {
-                        const int j = 16 * (e >> 2) + 4 * k + (e & 3);
-                        const float w = __shfl(mine, 16 * k + col);
-                        const bool seen = (bits >> j & 1u) != 0;
+                for (int i = 0; i < NDB; ++i) {
+                    u32x4 v, codes;
+                    take_apart<T>(v_operand(i), v, codes);
 #pragma unroll
-                        for (int i = 0; i < NDB; ++i) {
-                            const u32x2 y = *reinterpret_cast<const u32x2*>(&vs[j * VROW + 16 * i + 4 * q]);
+                    for (int k = 0; k < NR; ++k) {
+                        U[k][i] = Mma16<T>::mfma(v, bfrag[k], U[k][i]);
+                        const uint32_t mine = (bits[k] >> (4 * q) & 15u) | (bits[k] >> (16 + 4 * q) & 15u) << 4;
+                        const f32x4 n = Mma16<T>::mfma(codes, ones_of<T>(mine), f32x4{0.0f, 0.0f, 0.0f, 0.0f});
 #pragma unroll
-                            for (int d = 0; d < 4; ++d) {
-                                const float v = one_value<T>(d & 1 ? y[d >> 1] >> 16 : y[d >> 1] & 0xffffu);
-                                U[i][d] = seen ? fmaf(w, v, U[i][d]) : U[i][d];
-                            }
-                        }
+                        for (int d = 0; d < 4; ++d) U[k][i][d] += what_is_seen(n[d]);
+                        __builtin_amdgcn_sched_barrier(0);                       // few registers at a time
                     }
                 }
             }
@@ -523,8 +627,282 @@ __global__ __launch_bounds__(kTreeWaves * kWave, 2) void tree_rows_kernel(TreeRu
             p0 = n0;
             p1 = n1;
         }
-        finish_piece<T, D>(r, u, U, R, l, reinterpret_cast<float*>(lds), FP8 ? c.vscale : 1.0f);
+        finish_rows<T, D, NR>(r, u, U, R, l, reinterpret_cast<float*>(lds), FP8 ? c.vscale : 1.0f);
+    } while (u.next(r));
+}
+
+// ---- 64 or 128 rows: the wavefronts read the keys together (f16 / bf16) -----------------------------
+//
+// With more rows than 32 the products outweigh the keys' way through LDS, so the four wavefronts share one
+// double-buffered tile of 64 keys, in the layout of flashd_tile_parts.h, and the 32 x 32 x 16 products: wavefront
+// w has rows 32 (w % RW) .. + 31 of the tile and every KW-th 32-key block (RW KW = 4; two wavefronts to a
+// row's keys for up to 64 rows, none share for 128).  Each wavefront brings the 16 keys of a tile that it would
+// in that layout: they lie in one page, so its copies have one scalar base.
+template <typename T, int D, bool FP8> struct TileLoader;
+
+// straight from global memory to LDS
+template <typename T, int D> struct TileLoader<T, D, false> {
+    DmaLane<D> dl;
+    __device__ __forceinline__ TileLoader(int lane) : dl(0, lane) {}
+    // copy N of a wavefront: 1 KB of K and of V (the immediate offset counts on both sides)
+    template <int N>
+    __device__ __forceinline__ void issue(__amdgpu_buffer_rsrc_t k, __amdgpu_buffer_rsrc_t v, uint16_t* kw, uint16_t* vw) {
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(k, (lptr_t)kw, 16, dl.koff[N], 0, 1024 * N, 0);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(v, (lptr_t)vw, 16, dl.voff, 0, 1024 * N, 0);
     }
+    __device__ __forceinline__ void start(__amdgpu_buffer_rsrc_t k, __amdgpu_buffer_rsrc_t v, uint16_t* ks, uint16_t* vs,
+                                          int wave) {
+        constexpr int NI = DmaLane<D>::NI;
+        uint16_t* kw = ks + wave * (NI * 512);
+        uint16_t* vw = vs + wave * (NI * 512);
+        issue<0>(k, v, kw, vw);
+        issue<1>(k, v, kw, vw);
+        if constexpr (NI == 4) {
+            issue<2>(k, v, kw, vw);
+            issue<3>(k, v, kw, vw);
+        }
+    }
+    __device__ __forceinline__ void finish(uint16_t*, uint16_t*, int, int) { wait_copies(); }
+};
+
+// fp8: through registers, widened on the way
+template <typename T, int D> struct TileLoader<T, D, true> {
+    static constexpr int NI = D / 64;           // 1 KB each: 16 rows of D bytes
+    static constexpr int LPR = D / 16;
+    u32x4 k[NI], v[NI];
+    __device__ __forceinline__ TileLoader(int) {}
+    __device__ __forceinline__ void start(__amdgpu_buffer_rsrc_t kw, __amdgpu_buffer_rsrc_t vw, uint16_t*, uint16_t*, int) {
+        const int lane = threadIdx.x & 63;
+#pragma unroll
+        for (int n = 0; n < NI; ++n) {
+            k[n] = kv_load<0>(kw, 1024 * n + 16 * lane);
+            v[n] = kv_load<0>(vw, 1024 * n + 16 * lane);
+        }
+    }
+    __device__ __forceinline__ void finish(uint16_t* ks, uint16_t* vs, int wave, int lane) {
+        using C = TileCfg<D>;
+#pragma unroll
+        for (int n = 0; n < NI; ++n) {
+            const int row = 16 * wave + (64 / LPR) * n + lane / LPR;
+            const int ch = 2 * (lane % LPR);
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                *reinterpret_cast<u32x4*>(&ks[row * D + 8 * ((ch + i) ^ C::swz_k(row))]) = widen8<T>(k[n][2 * i], k[n][2 * i + 1]);
+                *reinterpret_cast<u32x4*>(&vs[row * D + 8 * ((ch + i) ^ C::swz_v(row))]) = widen8<T>(v[n][2 * i], v[n][2 * i + 1]);
+            }
+        }
+    }
+};
+
+template <typename T, int D, bool FP8, int RW>
+__global__ __launch_bounds__(kTreeWaves * kWave, 2) void tree_tile_kernel(TreeRun r) {
+    using C = TileCfg<D>;
+    constexpr int KW = kTreeWaves / RW;
+    constexpr int M = 32 * RW;
+    constexpr int NB = 2 / KW;                  // 32-key blocks of a tile that are a wavefront's
+    constexpr int NKK = D / 16;
+    constexpr int NDB = D / 32;
+    constexpr int kTile = kBC * D;
+    constexpr int CH = D / 4;                   // 16-byte chunks of a folded row
+    __shared__ __align__(1024) uint16_t lds[4 * kTile];
+    __shared__ float fold_r[kTreeWaves][32], fold_l[kTreeWaves][32];
+    static_assert(kTreeWaves * 32 * D * 4 <= (int)sizeof(lds), "the fold lies in the tiles' LDS");
+
+    const Paged& c = r.c;
+    const TreeArgs& a = r.a;
+    const int tid = threadIdx.x;
+    const int lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int rw = wave & (RW - 1), kw = wave / RW;
+    const int col = lane & 31;
+    const int hh = lane >> 5;
+    const float ninf = -__builtin_inff();
+
+    Walk<M, kBC> u;
+    u.begin(r);
+    if (u.at >= u.end) return;
+
+    // Operand addresses inside a tile (elements) of the wavefront's first block: those of operand kk of K and
+    // of column block i of V differ by 16 kk and 32 i under the swizzle's exclusive or.
+    const int kaddr0 = (32 * kw + col) * D + 8 * (hh ^ C::swz_k(col));
+    const int vaddr0 = (32 * kw + 4 * hh + ((lane & 15) >> 2)) * D +
+                       8 * ((2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ C::swz_v((lane & 15) >> 2)) + 4 * (lane & 1);
+    TileLoader<T, D, FP8> load(lane);
+
+    do {
+        const int row = u.first + min(32 * rw + col, u.nrows - 1);
+        const int token = (int)fast_div((uint32_t)row, r.group);
+        const uint16_t* qg = static_cast<const uint16_t*>(a.q) + row_at(r, u, row, a.q_stride, D);
+        u32x4 qf[NKK];
+#pragma unroll
+        for (int kk = 0; kk < NKK; ++kk) qf[kk] = *reinterpret_cast<const u32x4*>(qg + 16 * kk + 8 * hh);
+        // a negative scale is taken into Q (exact), so that the largest dot product is the top score
+        float c_log2 = (FP8 ? a.scale * c.kscale : a.scale) * kLog2e;
+        if (c_log2 < 0.0f) {
+            c_log2 = -c_log2;
+#pragma unroll
+            for (int kk = 0; kk < NKK; ++kk) qf[kk] ^= u32x4{0x80008000u, 0x80008000u, 0x80008000u, 0x80008000u};
+        }
+        // keys from `clear` on may be hidden from a row of the wavefront, those from `dark` on are from all
+        int clear = u.s.len, dark = u.keys();
+        if (a.tree == nullptr) {
+            clear += (int)fast_div((uint32_t)(u.first + min(32 * rw, u.nrows - 1)), r.group) + 1;
+            dark = u.s.len + (int)fast_div((uint32_t)(u.first + min(32 * rw + 31, u.nrows - 1)), r.group) + 1;
+        }
+        if (32 * rw >= u.nrows) dark = 0;
+
+        // pages of 16 tiles' 16-key groups, lane l that of group l of them; the next 16 tiles' a few tiles ahead
+        auto look_up = [&](int tile0) __attribute__((always_inline)) {
+            const int key = tile0 * kBC + 16 * lane;
+            return tile0 + (lane >> 2) < u.blk1 && key < u.keys() ? page_at(c, u.b, key >> c.page_log2) : -1;
+        };
+        int pages = look_up(u.blk0), pages_next = -1;
+        uint64_t gaps = __builtin_amdgcn_ballot_w64(pages < 0);
+        auto start_copy = [&](int t, int slot) __attribute__((always_inline)) {
+            const int page = __builtin_amdgcn_readlane(pages, 4 * ((t - u.blk0) & 15) + wave);
+            const int key = t * kBC + 16 * wave;
+            uint16_t* ks = lds + slot * kTile;
+            load.start(half_window(c, u, c.k, page, key), half_window(c, u, c.v, page, key), ks, ks + 2 * kTile, wave);
+        };
+
+        f32x16 U[NDB];
+#pragma unroll
+        for (int i = 0; i < NDB; ++i)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) U[i][e] = 0.0f;
+        RowState st = {ninf, 0.0f, 0.0f};
+
+        start_copy(u.blk0, 0);
+        load.finish(lds, lds + 2 * kTile, wave, lane);
+        __syncthreads();
+
+        // Period t: the copies of tile t + 1 into the other slot, which was last read in period t - 1; the
+        // math of tile t; the end of the copies; barrier.
+        // (One body for both slots and both blocks: in two or four copies the products' operands have constant addresses, but
+        // the code that masks need, in each of them, then costs the registers that hold U.)
+#pragma unroll 1
+        for (int t = u.blk0; t < u.blk1; ++t) {
+            const int in = (t - u.blk0) & 15;
+            const uint32_t hole = (uint32_t)(gaps >> (4 * in)) & 15u;      // groups of this tile without a page
+            const bool more = t + 1 < u.blk1;
+            if (in == 7) pages_next = look_up(t + 9);
+            if (in == 15) {
+                pages = pages_next;
+                gaps = __builtin_amdgcn_ballot_w64(pages < 0);
+            }
+            const int slot = in & 1;
+            if (more) start_copy(t + 1, slot ^ 1);
+            const uint16_t* ks = lds + slot * kTile;
+            const uint16_t* vs = ks + 2 * kTile;
+#pragma unroll 1
+            for (int n = 0; n < NB; ++n) {
+                const int j0 = t * kBC + 32 * (kw + n);
+                if (j0 >= dark) continue;
+                int kaddr = kaddr0 + 32 * n * D, vaddr = vaddr0 + 32 * n * D;
+                asm volatile("" : "+v"(kaddr), "+v"(vaddr));        // the addresses of operands are formed here, not kept
+                u32x4 ka[NKK];
+#pragma unroll
+                for (int kk = 0; kk < NKK; ++kk) ka[kk] = *reinterpret_cast<const u32x4*>(&ks[kaddr ^ 16 * kk]);
+                f32x16 acc;
+#pragma unroll
+                for (int e = 0; e < 16; ++e) acc[e] = 0.0f;
+#pragma unroll
+                for (int kk = 0; kk < NKK; ++kk) acc = Mma<T>::mfma(ka[kk], qf[kk], acc);
+                // V operands on their way while the coefficients are formed
+                u32x4 va[2 * NDB];
+#pragma unroll
+                for (int m = 0; m < 2 * NDB; ++m) va[m] = tile_v_operand<D>(vs, vaddr ^ 32 * (m % NDB), 16 * (m / NDB));
+
+                const uint32_t lost = hole >> (2 * (kw + n)) & 3u;
+                const bool masked = lost != 0 || j0 + 32 > clear;
+                u32x4 bfrag[2];
+                if (!masked) {
+                    top_first_pack<T, NDB, false>(acc, bfrag, st, U, c_log2, false, 0);
+                } else {
+                    uint32_t bits = seen_bits(a, u.s, token, u.s.row0 + token, j0);
+                    if (lost & 1u) bits &= 0xffff0000u;
+                    if (lost & 2u) bits &= 0x0000ffffu;
+                    const uint32_t mine = bits >> (4 * hh);
+                    // (a scale of 0 or NaN would take a hidden key away from -inf: it is applied here)
+                    const float by = c_log2 > 0.0f ? 1.0f : c_log2;
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) acc[e] = mine >> (8 * (e >> 2) + (e & 3)) & 1u ? acc[e] * by : ninf;
+                    top_first_pack<T, NDB, false>(acc, bfrag, st, U, c_log2 > 0.0f ? c_log2 : 1.0f, false, 0);
+                    bool apart = false;
+#pragma unroll
+                    for (int m = 0; m < 2 * NDB; ++m) apart |= not_finite<T, false>(va[m]);
+                    if (__builtin_amdgcn_ballot_w64(apart) != 0) {
+#pragma unroll
+                        for (int i = 0; i < NDB; ++i) {
+                            f32x16 count;
+#pragma unroll
+                            for (int e = 0; e < 16; ++e) count[e] = 0.0f;
+#pragma unroll
+                            for (int g = 0; g < 2; ++g) {
+                                const uint32_t of = mine >> (16 * g);
+                                u32x4 v, codes;
+                                take_apart<T>(va[g * NDB + i], v, codes);
+                                __builtin_amdgcn_sched_barrier(0);
+                                U[i] = Mma<T>::mfma(v, bfrag[g], U[i]);
+                                count = Mma<T>::mfma(codes, ones_of<T>((of & 15u) | (of >> 8 & 15u) << 4), count);
+                            }
+#pragma unroll
+                            for (int e = 0; e < 16; ++e) {
+                                U[i][e] += what_is_seen(count[e]);
+                                if ((e & 3) == 3) __builtin_amdgcn_sched_barrier(0);     // few registers at a time
+                            }
+                        }
+                        continue;
+                    }
+                }
+#pragma unroll
+                for (int m = 0; m < 2 * NDB; ++m) U[m % NDB] = Mma<T>::mfma(va[m], bfrag[m / NDB], U[m % NDB]);
+            }
+            if (more) load.finish(lds + (slot ^ 1) * kTile, lds + (2 + (slot ^ 1)) * kTile, wave, lane);
+            __syncthreads();
+        }
+
+        // ---- rows through LDS; with KW = 2 the two states of a row are joined.  Chunk t of row c lies at t ^ c.
+        const float l = pair_sum(st.l);
+        float* fold = reinterpret_cast<float*>(lds);
+        // (the lanes' arithmetic from here on stays here: kept over the loops it would take their registers)
+        int elane = lane;
+        asm volatile("" : "+v"(elane));
+        const int col = elane & 31, hh = elane >> 5, tid = 64 * wave + elane;
+#pragma unroll
+        for (int i = 0; i < NDB; ++i)
+#pragma unroll
+            for (int y = 0; y < 4; ++y)
+                *reinterpret_cast<f32x4*>(&fold[((wave * 32 + col) * CH + ((8 * i + 2 * y + hh) ^ (col & (CH - 1)))) * 4]) =
+                    f32x4{U[i][4 * y], U[i][4 * y + 1], U[i][4 * y + 2], U[i][4 * y + 3]};
+        if (hh == 0) {
+            fold_r[wave][col] = st.R;
+            fold_l[wave][col] = l;
+        }
+        __syncthreads();
+        for (int idx = tid; idx < u.nrows * CH; idx += kTreeWaves * kWave) {
+            const int fr = idx / CH, ch = idx % CH;
+            const int w0 = fr >> 5, rc = fr & 31;
+            float top = fold_r[w0][rc];
+#pragma unroll
+            for (int k = 1; k < KW; ++k) top = fmaxf(top, fold_r[w0 + RW * k][rc]);
+            float lt = 0.0f;
+            f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int k = 0; k < KW; ++k) {
+                const int w = w0 + RW * k;
+                const bool none = fold_l[w][rc] == 0.0f;
+                const float f = none ? 0.0f : exp2_fast(fold_r[w][rc] - top);
+                const f32x4 x = *reinterpret_cast<const f32x4*>(&fold[((w * 32 + rc) * CH + (ch ^ (rc & (CH - 1)))) * 4]);
+                lt = fmaf(f, fold_l[w][rc], lt);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[e] = fmaf(f, none ? 0.0f : x[e], o[e]);
+            }
+            put_row<T, D, M>(r, u, fr, 4 * ch, o, top, lt, FP8 ? c.vscale : 1.0f);
+        }
+        if (u.blk0 == 0 && !u.whole() && tid == 0) u.note_split(r);
+        __syncthreads();
+    } while (u.next(r));
 }
 
 // ---- the same in fp32 ------------------------------------------------------------------------------
@@ -547,25 +925,25 @@ __global__ __launch_bounds__(kTreeWaves * kWave, 2) void tree_rows_f32_kernel(Tr
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int col = lane & 15;
     const int q = lane >> 4;
-    const int G = (int)r.group.d;
     const float ninf = -__builtin_inff();
 
-    Walk u = begin_walk(c, G);
-    if (tid == 0) r.splits[blockIdx.x].parts = 0;
-    for (; u.next(c, G); u.done()) {
+    Walk<16, kTreeBlock> u;
+    u.begin(r);
+    if (u.at >= u.end) return;
+    do {
         const int row = u.first + min(col, u.nrows - 1);
         const int token = (int)fast_div((uint32_t)row, r.group);
-        const int head = u.h * G + row - token * G;
-        const float* qg = static_cast<const float*>(a.q) + (size_t)(u.s.row0 + token) * a.q_stride + (size_t)head * D;
+        const float* qg = static_cast<const float*>(a.q) + row_at(r, u, row, a.q_stride, D);
         f32x4 qf[NDB];
 #pragma unroll
         for (int m = 0; m < NDB; ++m) qf[m] = *reinterpret_cast<const f32x4*>(qg + 16 * m + 4 * q);
         const float c_log2 = a.scale * kLog2e;
 
-        f32x4 U[NDB];
+        f32x4 Us[1][NDB];
+        f32x4 (&U)[NDB] = Us[0];
 #pragma unroll
         for (int i = 0; i < NDB; ++i) U[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-        float R = ninf, l = 0.0f;
+        float R[1] = {ninf}, l[1] = {0.0f};
         PageWindow pages{-1, -1};
         for (int blk = u.blk0 + wave; blk < u.blk1; blk += W) {
             const int j0 = blk * kTreeBlock;
@@ -595,8 +973,8 @@ __global__ __launch_bounds__(kTreeWaves * kWave, 2) void tree_rows_f32_kernel(Tr
                 if (masked && !(bits >> (16 * (e >> 2) + 4 * q + (e & 3)) & 1u)) x[e] = ninf;
             }
             f32x8 pv;
-            weigh(x, pv, U, R, l, LazyLimit<BF16>::kMoveLog2);
-            l += ((pv[0] + pv[1]) + (pv[2] + pv[3])) + ((pv[4] + pv[5]) + (pv[6] + pv[7]));
+            weigh(x, pv, U, R[0], l[0], LazyLimit<BF16>::kMoveLog2);
+            l[0] += ((pv[0] + pv[1]) + (pv[2] + pv[3])) + ((pv[4] + pv[5]) + (pv[6] + pv[7]));
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 const auto w = half_window(c, u, c.v, p[e >> 2], j0 + 16 * (e >> 2));
@@ -626,20 +1004,21 @@ __global__ __launch_bounds__(kTreeWaves * kWave, 2) void tree_rows_f32_kernel(Tr
                 }
             }
         }
-        finish_piece<F32, D>(r, u, U, R, l, fold, 1.0f);
-    }
+        finish_rows<F32, D, 1>(r, u, Us, R, l, fold, 1.0f);
+    } while (u.next(r));
 }
 
 // ---- join the parts of split units -------------------------------------------------------------
 //
 // Workgroup (w, y) joins rows y, y + gridDim.y, ... of the unit that began in workgroup w and went on
-// in others: D / 4 lanes take 4 columns each, 1024 / D groups of lanes share the parts.
-template <typename T, int D>
+// in others: D / 4 lanes take 4 columns each, 1024 / D groups of lanes share the parts.  M: rows of a tile.
+template <typename T, int D, int M>
 __global__ __launch_bounds__(256) void merge_tree_kernel(TreeRun r, float vscale) {
     constexpr int LPR = D / 4;
     constexpr int NG = 256 / LPR;
     __shared__ __align__(16) float sum[NG][D];
     __shared__ float2 part_stat[NG];
+    if ((int)blockIdx.x >= *r.groups) return;
     const TreeSplit sp = r.splits[blockIdx.x];
     if (sp.parts == 0) return;
     const int g = threadIdx.x / LPR, t = 4 * (threadIdx.x % LPR);
@@ -649,7 +1028,7 @@ __global__ __launch_bounds__(256) void merge_tree_kernel(TreeRun r, float vscale
         float top = ninf, lt = 0.0f;
         f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
         for (int k = g; k < sp.parts; k += NG) {
-            const size_t at = (size_t)(2 * ((int)blockIdx.x + k) + (k == 0 ? 1 : 0)) * kTreeRows + fr;
+            const size_t at = (size_t)(2 * ((int)blockIdx.x + k) + (k == 0 ? 1 : 0)) * M + fr;
             const float2 st = r.stats[at];
             if (st.y == 0.0f) continue;                  // no key of this row
             const f32x4 u = *reinterpret_cast<const f32x4*>(r.parts + at * D + t);
@@ -688,25 +1067,53 @@ __global__ __launch_bounds__(256) void merge_tree_kernel(TreeRun r, float vscale
     }
 }
 
+// ---- host ------------------------------------------------------------------------------------------
+
+// Rows of a tile: the least that hold the tokens of a sequence with one row for each head of a group.
+static int tree_rows(int Hq, int Hkv, int max_q, int dtype) {
+    const long rows = (long)max_q * (Hq / Hkv);
+    return dtype == 0 || rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : 128;
+}
+
 size_t attn_tree_workspace(int Hq, int Hkv, int max_q, int d, int dtype) {
-    (void)Hq; (void)Hkv; (void)max_q; (void)dtype;
-    return (size_t)2 * kTreeMostGroups * kTreeRows * (d + 2) * sizeof(float) + kTreeMostGroups * sizeof(TreeSplit);
+    const int rows = tree_rows(Hq, Hkv, max_q, dtype);
+    return (size_t)2 * kTreeMostGroups * rows * (d + 2) * sizeof(float) + kTreeMostGroups * sizeof(TreeSplit) + 16;
+}
+
+template <typename T, int D, int M>
+static hipError_t launch_tree_m(TreeRun& r, hipStream_t st) {
+    const dim3 grid(kTreeMostGroups), block(kTreeWaves * kWave);
+    r.stats = reinterpret_cast<float2*>(r.parts + (size_t)2 * kTreeMostGroups * M * D);
+    r.splits = reinterpret_cast<TreeSplit*>(r.stats + (size_t)2 * kTreeMostGroups * M);
+    r.groups = reinterpret_cast<int*>(r.splits + kTreeMostGroups);
+    if constexpr (std::is_same_v<T, F32>) {
+        hipLaunchKernelGGL((tree_rows_f32_kernel<D>), grid, block, 0, st, r);
+    } else if constexpr (M <= 32) {
+        if (r.a.fp8) hipLaunchKernelGGL((tree_rows_kernel<T, D, true, M / 16>), grid, block, 0, st, r);
+        else hipLaunchKernelGGL((tree_rows_kernel<T, D, false, M / 16>), grid, block, 0, st, r);
+    } else {
+        if (r.a.fp8) hipLaunchKernelGGL((tree_tile_kernel<T, D, true, M / 32>), grid, block, 0, st, r);
+        else hipLaunchKernelGGL((tree_tile_kernel<T, D, false, M / 32>), grid, block, 0, st, r);
+    }
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL((merge_tree_kernel<T, D, M>), dim3(kTreeMostGroups, M / 8), dim3(256), 0, st, r,
+                       r.a.fp8 ? r.c.vscale : 1.0f);
+    return hipGetLastError();
 }
 
 template <typename T, int D>
 static hipError_t launch_tree_t(TreeRun& r, hipStream_t st) {
-    const dim3 grid(kTreeMostGroups), block(kTreeWaves * kWave);
     if constexpr (std::is_same_v<T, F32>) {
-        hipLaunchKernelGGL((tree_rows_f32_kernel<D>), grid, block, 0, st, r);
+        return launch_tree_m<T, D, 16>(r, st);
     } else {
-        if (r.a.fp8) hipLaunchKernelGGL((tree_rows_kernel<T, D, true>), grid, block, 0, st, r);
-        else hipLaunchKernelGGL((tree_rows_kernel<T, D, false>), grid, block, 0, st, r);
+        switch (tree_rows(r.a.Hq, r.c.Hkv, r.a.max_q, r.a.dtype)) {
+        case 16: return launch_tree_m<T, D, 16>(r, st);
+        case 32: return launch_tree_m<T, D, 32>(r, st);
+        case 64: return launch_tree_m<T, D, 64>(r, st);
+        default: return launch_tree_m<T, D, 128>(r, st);
+        }
     }
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((merge_tree_kernel<T, D>), dim3(kTreeMostGroups, 4), dim3(256), 0, st, r,
-                       r.a.fp8 ? r.c.vscale : 1.0f);
-    return hipGetLastError();
 }
 
 hipError_t launch_attn_tree(const Paged& c, const TreeArgs& a, hipStream_t st) {
@@ -715,8 +1122,6 @@ hipError_t launch_attn_tree(const Paged& c, const TreeArgs& a, hipStream_t st) {
     r.a = a;
     r.group = make_fast_div((uint32_t)(a.Hq / c.Hkv));
     r.parts = a.ws;
-    r.stats = reinterpret_cast<float2*>(a.ws + (size_t)2 * kTreeMostGroups * kTreeRows * c.d);
-    r.splits = reinterpret_cast<TreeSplit*>(r.stats + (size_t)2 * kTreeMostGroups * kTreeRows);
     const bool small = c.d == 64;
     if (a.dtype == 0) return small ? launch_tree_t<F32, 64>(r, st) : launch_tree_t<F32, 128>(r, st);
     if (a.dtype == 1) return small ? launch_tree_t<F16, 64>(r, st) : launch_tree_t<F16, 128>(r, st);
