@@ -97,10 +97,12 @@ struct Walk {
         }
         return (keys + KB - 1) / KB;
     }
-    // Sequence `seq`; returns the blocks of one kv head's units.
+    // Sequence `seq`; returns the blocks of one kv head's units.  SAME: it is the same one in every thread.
+    template <bool SAME>
     __device__ __forceinline__ long long enter(const TreeRun& r, int seq) {
         b = seq;
         s = seq_at(r.c, b);
+        if constexpr (SAME) s = Seq{uniform(s.row0), uniform(s.n), uniform(s.len)};
         tiles = (int)(((long long)s.n * (int)r.group.d + M - 1) / M);
         long long sum = 0;
         if (r.a.tree != nullptr) sum = tiles > 0 ? (long long)tiles * blocks_of(r, 0) : 0;
@@ -130,7 +132,7 @@ struct Walk {
         const int b0 = tid * each, b1 = min(b0 + each, c.B);
         long long mine = 0;
         Walk any;
-        for (int i = b0; i < b1; ++i) mine += any.enter(r, i) * c.Hkv;
+        for (int i = b0; i < b1; ++i) mine += any.template enter<false>(r, i) * c.Hkv;
         long long in = mine;
 #pragma unroll
         for (int k = 1; k < 64; k <<= 1) {
@@ -161,7 +163,7 @@ struct Walk {
         if (blockIdx.x == 0 && tid == 0) *r.groups = (int)groups;
         if (at < end && at >= before && at < before + mine) {
             for (int i = b0; i < b1; ++i) {
-                const long long sum = any.enter(r, i) * c.Hkv;
+                const long long sum = any.template enter<false>(r, i) * c.Hkv;
                 if (at < before + sum) {
                     found_b = i;
                     found_before = before;
@@ -177,7 +179,7 @@ struct Walk {
             end = at;
             return;
         }
-        const long long head = uniform(enter(r, found)), in_b = at - uniform(found_before);
+        const long long head = uniform(enter<true>(r, found)), in_b = at - uniform(found_before);
         h = uniform((int)(in_b / head));
         int from;
         if (r.a.tree != nullptr) {
@@ -203,7 +205,7 @@ struct Walk {
                 h = 0;
                 do {
                     if (b + 1 >= r.c.B) return false;
-                    enter(r, b + 1);
+                    enter<true>(r, b + 1);
                 } while (tiles == 0);
             }
         }
@@ -367,14 +369,23 @@ struct PageWindow {
     }
 };
 
+// A run of bytes behind which reads give zeros: the words of a buffer descriptor.
+struct Window {
+    u32x4 words;
+    __device__ __forceinline__ __amdgpu_buffer_rsrc_t rsrc() const {
+        return __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void*>((uint64_t)words[1] << 32 | words[0]), 0,
+                                                 (int)words[2], (int)words[3]);
+    }
+};
+
 // 16 keys of a block: their bytes up to the sequence's last key, or nothing without a page.
 template <class W>
-__device__ __forceinline__ __amdgpu_buffer_rsrc_t half_window(const Paged& c, const W& u, const char* pool,
-                                                              int page, int key) {
+__device__ __forceinline__ Window half_window(const Paged& c, const W& u, const char* pool, int page, int key) {
     const int row = (int)(c.head_bytes >> c.page_log2);
-    const char* at = pool + (int64_t)max(page, 0) * c.page_bytes + u.h * c.head_bytes +
-                     (int64_t)(key & ((1 << c.page_log2) - 1)) * row;
-    return kv_window(at, page < 0 ? 0 : (int64_t)min(16, u.keys() - key) * row);
+    const uint64_t at = (uint64_t)(pool + (int64_t)max(page, 0) * c.page_bytes + u.h * c.head_bytes +
+                                   (int64_t)(key & ((1 << c.page_log2) - 1)) * row);
+    const int keys = page < 0 ? 0 : min(16, u.keys() - key);
+    return Window{u32x4{(uint32_t)uniform((int)at), (uint32_t)uniform((int)(at >> 32)), (uint32_t)uniform(max(keys, 0) * row), 0x00020000u}};
 }
 
 // ---- 16 rows, keys shared out over the wavefronts (f16 / bf16) -----------------------------------
@@ -407,27 +418,35 @@ __device__ __forceinline__ bool not_finite(u32x4 x) {
     return bad;
 }
 
-// The products of such a block: the values that are no numbers are left out of the product with the weights and
-// counted by one with the bits of what is seen, +infinities as 1, -infinities as 64, NaN as 4096 (a block has 32
-// keys, and the sum is exact); what_is_seen() says what a count adds to an output.
+// The products of such a block: the values that are no numbers are left out of the product with the weights
+// (numbers_of) and counted by one with the bits of what is seen, +infinities as 1, -infinities as 64, NaN as 4096
+// (codes_of; a block has 32 keys, and the sum is exact); what_is_seen() says what a count adds to an output.
 template <typename T>
-__device__ __forceinline__ void take_apart(u32x4 x, u32x4& numbers, u32x4& codes) {
+__device__ __forceinline__ u32x4 numbers_of(u32x4 x) {
+    constexpr uint32_t e = Mma<T>::kRoundedSum ? 0x7f80u : 0x7c00u;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if ((x[i] & e) == e) x[i] &= 0xffff0000u;
+        if ((x[i] >> 16 & e) == e) x[i] &= 0x0000ffffu;
+    }
+    return x;
+}
+template <typename T>
+__device__ __forceinline__ u32x4 codes_of(u32x4 x) {
     constexpr bool B = Mma<T>::kRoundedSum;
     constexpr uint32_t e = B ? 0x7f80u : 0x7c00u, m = B ? 0x7fu : 0x3ffu;
     constexpr uint32_t one = B ? 0x3f80u : 0x3c00u, minus = B ? 0x4280u : 0x5400u, nan = B ? 0x4580u : 0x6c00u;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        uint32_t keep = 0, code = 0;
+        uint32_t code = 0;
 #pragma unroll
         for (int h = 0; h < 32; h += 16) {
             const uint32_t y = x[i] >> h & 0xffffu;
-            const bool bad = (y & e) == e;
-            keep |= bad ? 0u : y << h;
-            code |= bad ? ((y & m) != 0 ? nan : y >> 15 ? minus : one) << h : 0u;
+            code |= (y & e) != e ? 0u : ((y & m) != 0 ? nan : y >> 15 ? minus : one) << h;
         }
-        numbers[i] = keep;
-        codes[i] = code;
+        x[i] = code;
     }
+    return x;
 }
 __device__ __forceinline__ float what_is_seen(float count) {
     const int n = (int)count;
@@ -490,7 +509,7 @@ __global__ __launch_bounds__(kTreeWaves * kWave, 2) void tree_rows_kernel(TreeRu
         auto fetch = [&](const char* pool, u32x4 (&reg)[NV], int blk, int p0, int p1) __attribute__((always_inline)) {
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
-                const auto w = half_window(c, u, pool, half ? p1 : p0, blk * kTreeBlock + 16 * half);
+                const auto w = half_window(c, u, pool, half ? p1 : p0, blk * kTreeBlock + 16 * half).rsrc();
 #pragma unroll
                 for (int n = 0; n < NV / 2; ++n) reg[half * (NV / 2) + n] = kv_load<2>(w, 1024 * n + 16 * lane);
             }
@@ -600,28 +619,34 @@ __global__ __launch_bounds__(kTreeWaves * kWave, 2) void tree_rows_kernel(TreeRu
                     (lds_ptr)(base + 16 * VROW + 16 * i)));
                 return u32x4{lo[0], lo[1], hi[0], hi[1]};
             };
-            if (!apart) {
+            if (apart) {
 #pragma unroll
                 for (int i = 0; i < NDB; ++i) {
-                    const u32x4 v = v_operand(i);
-#pragma unroll
-                    for (int k = 0; k < NR; ++k) U[k][i] = Mma16<T>::mfma(v, bfrag[k], U[k][i]);
-                }
-            } else {
-#pragma unroll
-                for (int i = 0; i < NDB; ++i) {
-                    u32x4 v, codes;
-                    take_apart<T>(v_operand(i), v, codes);
+                    const u32x4 codes = codes_of<T>(v_operand(i));
 #pragma unroll
                     for (int k = 0; k < NR; ++k) {
-                        U[k][i] = Mma16<T>::mfma(v, bfrag[k], U[k][i]);
                         const uint32_t mine = (bits[k] >> (4 * q) & 15u) | (bits[k] >> (16 + 4 * q) & 15u) << 4;
                         const f32x4 n = Mma16<T>::mfma(codes, ones_of<T>(mine), f32x4{0.0f, 0.0f, 0.0f, 0.0f});
 #pragma unroll
                         for (int d = 0; d < 4; ++d) U[k][i][d] += what_is_seen(n[d]);
-                        __builtin_amdgcn_sched_barrier(0);                       // few registers at a time
                     }
+                    __builtin_amdgcn_sched_barrier(0);           // few registers at a time
                 }
+                stage_done();
+#pragma unroll 1
+                for (int n = 0; n < D / 16; ++n) {
+                    u32x4* x = reinterpret_cast<u32x4*>(&vs[(n * kWave + lane) / (D / 8) * VROW + 8 * (lane % (D / 8))]);
+                    *x = numbers_of<T>(*x);
+                }
+                __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+                __builtin_amdgcn_wave_barrier();
+                __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+            }
+#pragma unroll
+            for (int i = 0; i < NDB; ++i) {
+                const u32x4 v = v_operand(i);
+#pragma unroll
+                for (int k = 0; k < NR; ++k) U[k][i] = Mma16<T>::mfma(v, bfrag[k], U[k][i]);
             }
             stage_done();
             p0 = n0;
@@ -638,31 +663,57 @@ __global__ __launch_bounds__(kTreeWaves * kWave, 2) void tree_rows_kernel(TreeRu
 // w has rows 32 (w % RW) .. + 31 of the tile and every KW-th 32-key block (RW KW = 4; two wavefronts to a
 // row's keys for up to 64 rows, none share for 128).  Each wavefront brings the 16 keys of a tile that it would
 // in that layout: they lie in one page, so its copies have one scalar base.
+// (The copies are written as instructions: where the compiler knows of a copy into LDS under way, it waits for it before
+// every read of LDS that it cannot tell apart from the copy's target, and with the slot in a register it can tell
+// none: the copies of tile t + 1 then ended before the math of tile t began.)
+__device__ __forceinline__ uint32_t lds_address(const void* p) {
+    return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) char*)p;
+}
 template <typename T, int D, bool FP8> struct TileLoader;
 
 // straight from global memory to LDS
 template <typename T, int D> struct TileLoader<T, D, false> {
-    DmaLane<D> dl;
-    __device__ __forceinline__ TileLoader(int lane) : dl(0, lane) {}
-    // copy N of a wavefront: 1 KB of K and of V (the immediate offset counts on both sides)
-    template <int N>
-    __device__ __forceinline__ void issue(__amdgpu_buffer_rsrc_t k, __amdgpu_buffer_rsrc_t v, uint16_t* kw, uint16_t* vw) {
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(k, (lptr_t)kw, 16, dl.koff[N], 0, 1024 * N, 0);
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(v, (lptr_t)vw, 16, dl.voff, 0, 1024 * N, 0);
+    uint32_t koff, voff;         // bytes; copy n takes koff ^ 64 n (DmaLane in flashd_tile_parts.h)
+    __device__ __forceinline__ TileLoader(int lane) {
+        const DmaLane<D> dl(0, lane);
+        koff = dl.koff[0];
+        voff = dl.voff;
     }
-    __device__ __forceinline__ void start(__amdgpu_buffer_rsrc_t k, __amdgpu_buffer_rsrc_t v, uint16_t* ks, uint16_t* vs,
-                                          int wave) {
+    // A wavefront's copies, 1 KB each (the immediate offset counts on both sides).  M0 holds the target; one wait state
+    // has to pass between writing it and the copy.  It is left as it was.
+    __device__ __forceinline__ void start(const Window& k, const Window& v, uint16_t* ks, uint16_t* vs, int wave) {
         constexpr int NI = DmaLane<D>::NI;
-        uint16_t* kw = ks + wave * (NI * 512);
-        uint16_t* vw = vs + wave * (NI * 512);
-        issue<0>(k, v, kw, vw);
-        issue<1>(k, v, kw, vw);
-        if constexpr (NI == 4) {
-            issue<2>(k, v, kw, vw);
-            issue<3>(k, v, kw, vw);
-        }
+        const uint32_t kw = lds_address(ks) + 1024 * NI * wave, vw = lds_address(vs) + 1024 * NI * wave;
+        uint32_t m0, k0 = koff;
+        asm volatile("" : "+v"(k0));         // the other offsets are formed here, not kept
+        if constexpr (NI == 4)
+            asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %8\n\ts_nop 0\n\t"
+                         "buffer_load_dwordx4 %1, %6, 0 offen lds\n\t"
+                         "buffer_load_dwordx4 %2, %6, 0 offen offset:1024 lds\n\t"
+                         "buffer_load_dwordx4 %3, %6, 0 offen offset:2048 lds\n\t"
+                         "buffer_load_dwordx4 %4, %6, 0 offen offset:3072 lds\n\t"
+                         "s_mov_b32 m0, %9\n\ts_nop 0\n\t"
+                         "buffer_load_dwordx4 %5, %7, 0 offen lds\n\t"
+                         "buffer_load_dwordx4 %5, %7, 0 offen offset:1024 lds\n\t"
+                         "buffer_load_dwordx4 %5, %7, 0 offen offset:2048 lds\n\t"
+                         "buffer_load_dwordx4 %5, %7, 0 offen offset:3072 lds\n\t"
+                         "s_mov_b32 m0, %0"
+                         : "=&s"(m0)
+                         : "v"(k0), "v"(k0 ^ 64u), "v"(k0 ^ 128u), "v"(k0 ^ 192u), "v"(voff),
+                           "s"(k.words), "s"(v.words), "s"(kw), "s"(vw) : "memory");
+        else
+            asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %6\n\ts_nop 0\n\t"
+                         "buffer_load_dwordx4 %1, %4, 0 offen lds\n\t"
+                         "buffer_load_dwordx4 %2, %4, 0 offen offset:1024 lds\n\t"
+                         "s_mov_b32 m0, %7\n\ts_nop 0\n\t"
+                         "buffer_load_dwordx4 %3, %5, 0 offen lds\n\t"
+                         "buffer_load_dwordx4 %3, %5, 0 offen offset:1024 lds\n\t"
+                         "s_mov_b32 m0, %0"
+                         : "=&s"(m0)
+                         : "v"(k0), "v"(k0 ^ 64u), "v"(voff), "s"(k.words), "s"(v.words), "s"(kw), "s"(vw)
+                         : "memory");
     }
-    __device__ __forceinline__ void finish(uint16_t*, uint16_t*, int, int) { wait_copies(); }
+    __device__ __forceinline__ void finish(uint16_t*, uint16_t*, int, int) { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 };
 
 // fp8: through registers, widened on the way
@@ -671,12 +722,13 @@ template <typename T, int D> struct TileLoader<T, D, true> {
     static constexpr int LPR = D / 16;
     u32x4 k[NI], v[NI];
     __device__ __forceinline__ TileLoader(int) {}
-    __device__ __forceinline__ void start(__amdgpu_buffer_rsrc_t kw, __amdgpu_buffer_rsrc_t vw, uint16_t*, uint16_t*, int) {
+    __device__ __forceinline__ void start(const Window& kw, const Window& vw, uint16_t*, uint16_t*, int) {
         const int lane = threadIdx.x & 63;
+        const auto kr = kw.rsrc(), vr = vw.rsrc();
 #pragma unroll
         for (int n = 0; n < NI; ++n) {
-            k[n] = kv_load<0>(kw, 1024 * n + 16 * lane);
-            v[n] = kv_load<0>(vw, 1024 * n + 16 * lane);
+            k[n] = kv_load<0>(kr, 1024 * n + 16 * lane);
+            v[n] = kv_load<0>(vr, 1024 * n + 16 * lane);
         }
     }
     __device__ __forceinline__ void finish(uint16_t* ks, uint16_t* vs, int wave, int lane) {
@@ -808,10 +860,15 @@ __global__ __launch_bounds__(kTreeWaves * kWave, 2) void tree_tile_kernel(TreeRu
                 for (int e = 0; e < 16; ++e) acc[e] = 0.0f;
 #pragma unroll
                 for (int kk = 0; kk < NKK; ++kk) acc = Mma<T>::mfma(ka[kk], qf[kk], acc);
+                // all of K's operands are asked for before the first product (LDS returns in order)
+                __builtin_amdgcn_sched_group_barrier(0x100, NKK, 0);
+                __builtin_amdgcn_sched_group_barrier(0x008, NKK, 0);
+                __builtin_amdgcn_sched_barrier(0);
                 // V operands on their way while the coefficients are formed
                 u32x4 va[2 * NDB];
 #pragma unroll
                 for (int m = 0; m < 2 * NDB; ++m) va[m] = tile_v_operand<D>(vs, vaddr ^ 32 * (m % NDB), 16 * (m / NDB));
+                __builtin_amdgcn_sched_barrier(0);
 
                 const uint32_t lost = hole >> (2 * (kw + n)) & 3u;
                 const bool masked = lost != 0 || j0 + 32 > clear;
@@ -840,19 +897,16 @@ __global__ __launch_bounds__(kTreeWaves * kWave, 2) void tree_tile_kernel(TreeRu
 #pragma unroll
                             for (int g = 0; g < 2; ++g) {
                                 const uint32_t of = mine >> (16 * g);
-                                u32x4 v, codes;
-                                take_apart<T>(va[g * NDB + i], v, codes);
-                                __builtin_amdgcn_sched_barrier(0);
-                                U[i] = Mma<T>::mfma(v, bfrag[g], U[i]);
-                                count = Mma<T>::mfma(codes, ones_of<T>((of & 15u) | (of >> 8 & 15u) << 4), count);
+                                count = Mma<T>::mfma(codes_of<T>(va[g * NDB + i]), ones_of<T>((of & 15u) | (of >> 8 & 15u) << 4), count);
+                                va[g * NDB + i] = numbers_of<T>(va[g * NDB + i]);
+                                __builtin_amdgcn_sched_barrier(0);       // few registers at a time
                             }
 #pragma unroll
                             for (int e = 0; e < 16; ++e) {
                                 U[i][e] += what_is_seen(count[e]);
-                                if ((e & 3) == 3) __builtin_amdgcn_sched_barrier(0);     // few registers at a time
+                                if ((e & 3) == 3) __builtin_amdgcn_sched_barrier(0);
                             }
                         }
-                        continue;
                     }
                 }
 #pragma unroll
@@ -953,7 +1007,7 @@ __global__ __launch_bounds__(kTreeWaves * kWave, 2) void tree_rows_f32_kernel(Tr
 #pragma unroll
             for (int t = 0; t < 2; ++t) {
                 acc[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-                const auto w = half_window(c, u, c.k, p[t], j0 + 16 * t);
+                const auto w = half_window(c, u, c.k, p[t], j0 + 16 * t).rsrc();
                 f32x4 k[NDB];
 #pragma unroll
                 for (int m = 0; m < NDB; ++m) k[m] = __builtin_bit_cast(f32x4, kv_load<2>(w, (col * D + 16 * m + 4 * q) * 4));
@@ -977,7 +1031,7 @@ __global__ __launch_bounds__(kTreeWaves * kWave, 2) void tree_rows_f32_kernel(Tr
             l[0] += ((pv[0] + pv[1]) + (pv[2] + pv[3])) + ((pv[4] + pv[5]) + (pv[6] + pv[7]));
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                const auto w = half_window(c, u, c.v, p[e >> 2], j0 + 16 * (e >> 2));
+                const auto w = half_window(c, u, c.v, p[e >> 2], j0 + 16 * (e >> 2)).rsrc();
                 float v[NDB];
                 bool bad = false;
 #pragma unroll
@@ -1010,40 +1064,102 @@ __global__ __launch_bounds__(kTreeWaves * kWave, 2) void tree_rows_f32_kernel(Tr
 
 // ---- join the parts of split units -------------------------------------------------------------
 //
-// Workgroup (w, y) joins rows y, y + gridDim.y, ... of the unit that began in workgroup w and went on
-// in others: D / 4 lanes take 4 columns each, 1024 / D groups of lanes share the parts.  M: rows of a tile.
+// The rows of all split units, one after the other, are dealt out evenly: a fixed number of workgroups, each of which
+// sums up how many there are (256 at a time) and walks its share.  D / 4 lanes take 4 columns each of a row; the
+// 1024 / D such groups of a workgroup take a row each, or share the parts of one row where a unit has many (more
+// than kMergeShare: one long sequence over the whole chip).  M: rows of a tile.
+constexpr int kMergeShare = 12;
+constexpr int kMergeGroups = 512;
+
+// One row's parts k0, k0 + step, ...: unnormalised sum against `top`.
+template <int D, int M>
+__device__ __forceinline__ f32x4 merge_parts(const TreeRun& r, int w, int parts, int fr, int t, int k0, int step,
+                                             float& top, float& lt) {
+    constexpr int AHEAD = 4;             // parts read together
+    f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (int k = k0; k < parts; k += AHEAD * step) {
+        float2 st[AHEAD];
+        f32x4 u[AHEAD];
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+            const int part = min(k + i * step, parts - 1);
+            const size_t at = (size_t)(2 * (w + part) + (part == 0 ? 1 : 0)) * M + fr;
+            st[i] = r.stats[at];
+            u[i] = *reinterpret_cast<const f32x4*>(r.parts + at * D + t);
+        }
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+            if (k + i * step >= parts || st[i].y == 0.0f) continue;         // no key of this row
+            const float now = fmaxf(top, st[i].x);
+            const float f0 = top == -__builtin_inff() ? 0.0f : exp2_fast(top - now), f1 = exp2_fast(st[i].x - now);
+            lt = fmaf(lt, f0, st[i].y * f1);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[e] = fmaf(o[e], f0, u[i][e] * f1);
+            top = now;
+        }
+    }
+    return o;
+}
+
 template <typename T, int D, int M>
 __global__ __launch_bounds__(256) void merge_tree_kernel(TreeRun r, float vscale) {
     constexpr int LPR = D / 4;
     constexpr int NG = 256 / LPR;
     __shared__ __align__(16) float sum[NG][D];
     __shared__ float2 part_stat[NG];
-    if ((int)blockIdx.x >= *r.groups) return;
-    const TreeSplit sp = r.splits[blockIdx.x];
-    if (sp.parts == 0) return;
-    const int g = threadIdx.x / LPR, t = 4 * (threadIdx.x % LPR);
-    const int G = (int)r.group.d;
+    __shared__ int before[kTreeMostGroups + 1];          // items of the splits before
+    __shared__ int wave_sum[kTreeWaves];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int groups = uniform(*r.groups);
     const float ninf = -__builtin_inff();
-    for (int fr = blockIdx.y; fr < sp.rows; fr += gridDim.y) {
-        float top = ninf, lt = 0.0f;
-        f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
-        for (int k = g; k < sp.parts; k += NG) {
-            const size_t at = (size_t)(2 * ((int)blockIdx.x + k) + (k == 0 ? 1 : 0)) * M + fr;
-            const float2 st = r.stats[at];
-            if (st.y == 0.0f) continue;                  // no key of this row
-            const f32x4 u = *reinterpret_cast<const f32x4*>(r.parts + at * D + t);
-            const float now = fmaxf(top, st.x);
-            const float f0 = top == ninf ? 0.0f : exp2_fast(top - now), f1 = exp2_fast(st.x - now);
-            lt = fmaf(lt, f0, st.y * f1);
+    auto items_of = [](const TreeSplit& sp) {
+        return sp.parts == 0 ? 0 : sp.parts > kMergeShare ? sp.rows : (sp.rows + NG - 1) / NG;
+    };
+    int total = 0;
+    for (int w0 = 0; w0 < groups; w0 += 256) {
+        const int mine = w0 + tid < groups ? items_of(r.splits[w0 + tid]) : 0;
+        int in = mine;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) o[e] = fmaf(o[e], f0, u[e] * f1);
-            top = now;
+        for (int k = 1; k < 64; k <<= 1) {
+            const int y = __shfl_up(in, k);
+            if (lane >= k) in += y;
         }
         __syncthreads();
-        *reinterpret_cast<f32x4*>(&sum[g][t]) = o;
-        if (t == 0) part_stat[g] = float2{top, lt};
+        if (lane == 63) wave_sum[wave] = in;
         __syncthreads();
-        if (g == 0) {
+        int ahead = 0, all = 0;
+#pragma unroll
+        for (int k = 0; k < kTreeWaves; ++k) {
+            ahead += k < wave ? wave_sum[k] : 0;
+            all += wave_sum[k];
+        }
+        if (w0 + tid < kTreeMostGroups) before[w0 + tid] = total + ahead + in - mine;
+        total += uniform(all);
+    }
+    __syncthreads();
+    const int g = tid / LPR, t = 4 * (tid % LPR);
+    const int G = (int)r.group.d;
+    for (int item = blockIdx.x; item < total; item += gridDim.x) {
+        int lo = 0, hi = groups;             // the split: the last whose items begin at or before this one
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) >> 1;
+            if (before[mid] <= item) lo = mid;
+            else hi = mid;
+        }
+        const int w = uniform(lo);
+        const TreeSplit sp = r.splits[w];
+        const int parts = uniform(sp.parts), of = item - before[w];
+        float top = ninf, lt = 0.0f;
+        f32x4 o;
+        int fr;
+        if (parts > kMergeShare) {
+            fr = of;
+            o = merge_parts<D, M>(r, w, parts, fr, t, g, NG, top, lt);
+            __syncthreads();
+            *reinterpret_cast<f32x4*>(&sum[g][t]) = o;
+            if (t == 0) part_stat[g] = float2{top, lt};
+            __syncthreads();
+            if (g != 0) continue;
             float all = ninf;
 #pragma unroll
             for (int k = 0; k < NG; ++k) all = fmaxf(all, part_stat[k].x);
@@ -1058,12 +1174,16 @@ __global__ __launch_bounds__(256) void merge_tree_kernel(TreeRun r, float vscale
 #pragma unroll
                 for (int e = 0; e < 4; ++e) o[e] = fmaf(f, u[e], o[e]);
             }
-            if (lt != 0.0f) o *= vscale / lt;
-            const int rw = sp.first + fr;
-            const int tk = (int)fast_div((uint32_t)rw, r.group);
-            Store<T>::store4(r.a.o, (size_t)(sp.row0 + tk) * r.a.o_stride + (size_t)(sp.h * G + rw - tk * G) * D + t,
-                             {o[0], o[1], o[2], o[3]});
+        } else {
+            fr = of * NG + g;
+            if (fr >= sp.rows) continue;
+            o = merge_parts<D, M>(r, w, parts, fr, t, 0, 1, top, lt);
         }
+        if (lt != 0.0f) o *= vscale / lt;
+        const int rw = sp.first + fr;
+        const int tk = (int)fast_div((uint32_t)rw, r.group);
+        Store<T>::store4(r.a.o, (size_t)(sp.row0 + tk) * r.a.o_stride + (size_t)(sp.h * G + rw - tk * G) * D + t,
+                         {o[0], o[1], o[2], o[3]});
     }
 }
 
@@ -1097,7 +1217,7 @@ static hipError_t launch_tree_m(TreeRun& r, hipStream_t st) {
     }
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((merge_tree_kernel<T, D, M>), dim3(kTreeMostGroups, M / 8), dim3(256), 0, st, r,
+    hipLaunchKernelGGL((merge_tree_kernel<T, D, M>), dim3(kMergeGroups), dim3(256), 0, st, r,
                        r.a.fp8 ? r.c.vscale : 1.0f);
     return hipGetLastError();
 }
