@@ -62,6 +62,20 @@ struct TreeRun {
     int* groups;            // how many workgroups have work
 };
 
+// The kernel's arguments, read anew where they are asked for.  What only the beginning and the end of a piece need
+// is taken from here: kept over the loop in scalar registers, of which there are a hundred, it would push what the loop
+// needs out of them.
+__device__ __forceinline__ TreeRun args_now() {
+    typedef const __attribute__((address_space(4))) uint32_t* words_ptr;
+    words_ptr p = (words_ptr)__builtin_amdgcn_kernarg_segment_ptr();
+    asm volatile("" : "+s"(p));
+    struct Words { uint32_t w[sizeof(TreeRun) / 4]; } x;
+    static_assert(sizeof(TreeRun) % 4 == 0, "read word by word");
+#pragma unroll
+    for (size_t i = 0; i < sizeof(TreeRun) / 4; ++i) x.w[i] = p[i];
+    return __builtin_bit_cast(TreeRun, x);
+}
+
 // ---- the share of a workgroup ------------------------------------------------------------------
 
 // A value that is the same in every lane, in a scalar register
@@ -69,6 +83,12 @@ __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirs
 __device__ __forceinline__ long long uniform(long long x) {
     return (long long)((uint64_t)(uint32_t)uniform((int)(x >> 32)) << 32 | (uint32_t)uniform((int)x));
 }
+
+struct WalkScratch {
+    long long wave_sum[kTreeWaves];
+    long long found_before;
+    int found_b;
+};
 
 // A workgroup's way along the row of blocks, and the piece of a unit that it is at (all the same in every
 // thread, in scalar registers).  M: rows of a tile; KB: keys of a block of the row.  Of a chain's row tile only the blocks count
@@ -122,10 +142,10 @@ struct Walk {
 
     // Every thread of the workgroup takes a run of sequences, whose blocks are then summed over the threads;
     // the one that has the share's first block in its run finds the sequence.
-    __device__ __forceinline__ void begin(const TreeRun& r) {
-        __shared__ long long wave_sum[kTreeWaves];
-        __shared__ long long found_before;
-        __shared__ int found_b;
+    __device__ __forceinline__ void begin(const TreeRun& r, WalkScratch* scratch) {
+        long long (&wave_sum)[kTreeWaves] = scratch->wave_sum;
+        long long& found_before = scratch->found_before;
+        int& found_b = scratch->found_b;
         const Paged& c = r.c;
         const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
         const int each = (c.B + kTreeWaves * kWave - 1) / (kTreeWaves * kWave);
@@ -175,11 +195,13 @@ struct Walk {
         if (tid == 0 && k < of_xcd && w < groups) r.splits[w].parts = 0;
         __syncthreads();
         const int found = uniform(found_b);
+        const long long found_at = uniform(found_before);
+        __syncthreads();                                 // the scratch is the kernel's again
         if (found < 0) {
             end = at;
             return;
         }
-        const long long head = uniform(enter<true>(r, found)), in_b = at - uniform(found_before);
+        const long long head = uniform(enter<true>(r, found)), in_b = at - found_at;
         h = uniform((int)(in_b / head));
         int from;
         if (r.a.tree != nullptr) {
@@ -401,20 +423,29 @@ __device__ __forceinline__ Window half_window(const Paged& c, const W& u, const 
 // In blocks with new keys a weight of zero may meet a value that is infinite or NaN (a token that some rows see
 // and others do not), and 0 * infinity must not reach the others: see take_apart().
 
-// any of 8 values of the storage type (16 fp8 values) is infinite or NaN
+// (All of this on pairs of halves, by carries into their top bits: comparisons hand their results to scalar registers, and the
+// dozens of a block's values in flight took those that the loops around hold their addresses in.)
+template <typename T> struct Half {
+    static constexpr bool B = Mma<T>::kRoundedSum;                          // bf16, else f16
+    static constexpr uint32_t kExp = B ? 0x7f807f80u : 0x7c007c00u, kOne = B ? 0x00800080u : 0x04000400u;
+    static constexpr uint32_t kMan = B ? 0x007f007fu : 0x03ff03ffu, kTop = 0x80008000u;
+    static constexpr uint32_t kPlus = B ? 0x3f803f80u : 0x3c003c00u, kMinus = B ? 0x42804280u : 0x54005400u,
+                              kNan = B ? 0x45804580u : 0x6c006c00u;         // 1, 64 and 4096
+    // top bits of the halves that are infinite or NaN
+    static __device__ __forceinline__ uint32_t bad(uint32_t x) { return ((x & kExp) + kOne) & kTop; }
+    // top bits -> whole halves
+    static __device__ __forceinline__ uint32_t spread(uint32_t top) { return (top >> 15) * 0xffffu; }
+};
+// all ones if bit i of x is set
+__device__ __forceinline__ uint32_t bit_mask(uint32_t x, int i) { return (uint32_t)((int)(x << (31 - i)) >> 31); }
+
+// nonzero if any of 8 values of the storage type (16 fp8 values) is infinite or NaN
 template <typename T, bool FP8>
-__device__ __forceinline__ bool not_finite(u32x4 x) {
-    bool bad = false;
+__device__ __forceinline__ uint32_t not_finite(u32x4 x) {
+    uint32_t bad = 0;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        if constexpr (FP8) {
-            const uint32_t y = x[i] & 0x7f7f7f7fu;       // NaN is 0x7f: the only byte that adding 1 carries from
-            bad |= ((y + 0x01010101u) & 0x80808080u) != 0;
-        } else {
-            constexpr uint32_t e = Mma<T>::kRoundedSum ? 0x7f80u : 0x7c00u;
-            bad |= (x[i] & e) == e || (x[i] >> 16 & e) == e;
-        }
-    }
+    for (int i = 0; i < 4; ++i)          // fp8: NaN is 0x7f, the only byte that adding 1 carries from
+        bad |= FP8 ? ((x[i] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u : Half<T>::bad(x[i]);
     return bad;
 }
 
@@ -423,28 +454,17 @@ __device__ __forceinline__ bool not_finite(u32x4 x) {
 // (codes_of; a block has 32 keys, and the sum is exact); what_is_seen() says what a count adds to an output.
 template <typename T>
 __device__ __forceinline__ u32x4 numbers_of(u32x4 x) {
-    constexpr uint32_t e = Mma<T>::kRoundedSum ? 0x7f80u : 0x7c00u;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        if ((x[i] & e) == e) x[i] &= 0xffff0000u;
-        if ((x[i] >> 16 & e) == e) x[i] &= 0x0000ffffu;
-    }
+    for (int i = 0; i < 4; ++i) x[i] &= ~Half<T>::spread(Half<T>::bad(x[i]));
     return x;
 }
 template <typename T>
 __device__ __forceinline__ u32x4 codes_of(u32x4 x) {
-    constexpr bool B = Mma<T>::kRoundedSum;
-    constexpr uint32_t e = B ? 0x7f80u : 0x7c00u, m = B ? 0x7fu : 0x3ffu;
-    constexpr uint32_t one = B ? 0x3f80u : 0x3c00u, minus = B ? 0x4280u : 0x5400u, nan = B ? 0x4580u : 0x6c00u;
+    using H = Half<T>;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        uint32_t code = 0;
-#pragma unroll
-        for (int h = 0; h < 32; h += 16) {
-            const uint32_t y = x[i] >> h & 0xffffu;
-            code |= (y & e) != e ? 0u : ((y & m) != 0 ? nan : y >> 15 ? minus : one) << h;
-        }
-        x[i] = code;
+        const uint32_t bad = H::bad(x[i]), nan = bad & ((x[i] & H::kMan) + 0x7fff7fffu), inf = bad & ~nan;
+        x[i] = (H::spread(nan) & H::kNan) | (H::spread(inf & x[i]) & H::kMinus) | (H::spread(inf & ~x[i]) & H::kPlus);
     }
     return x;
 }
@@ -460,8 +480,13 @@ __device__ __forceinline__ u32x4 ones_of(uint32_t bits) {
     u32x4 x;
 #pragma unroll
     for (int i = 0; i < 4; ++i)
-        x[i] = (bits >> (2 * i) & 1u ? Mma<T>::kOnes & 0xffffu : 0u) | (bits >> (2 * i + 1) & 1u ? Mma<T>::kOnes & 0xffff0000u : 0u);
+        x[i] = (bit_mask(bits, 2 * i) & (Mma<T>::kOnes & 0xffffu)) | (bit_mask(bits, 2 * i + 1) & (Mma<T>::kOnes & 0xffff0000u));
     return x;
+}
+// x if bit i of bits is set, else -inf
+__device__ __forceinline__ float if_seen(uint32_t bits, int i, float x) {
+    const uint32_t m = bit_mask(bits, i);
+    return __uint_as_float((m & __float_as_uint(x)) | (~m & 0xff800000u));
 }
 
 template <typename T, int D, bool FP8, int NR>
@@ -490,7 +515,7 @@ __global__ __launch_bounds__(kTreeWaves * kWave, 2) void tree_rows_kernel(TreeRu
     uint16_t* vs = reinterpret_cast<uint16_t*>(lds) + wave * STAGE;
 
     Walk<16 * NR, kTreeBlock> u;
-    u.begin(r);
+    u.begin(r, reinterpret_cast<WalkScratch*>(lds));
     if (u.at >= u.end) return;
     do {
         // the query rows of this lane's column; columns past the last row stand in for it
@@ -504,6 +529,9 @@ __global__ __launch_bounds__(kTreeWaves * kWave, 2) void tree_rows_kernel(TreeRu
 #pragma unroll
             for (int kk = 0; kk < NKK; ++kk) qf[k][kk] = *reinterpret_cast<const u32x4*>(qg + 32 * kk + 8 * q);
         }
+        // Here before the loop, as the compiler knows: in every turn of it, it would else wait for them, and so for the keys
+        // under way.
+        wait_copies();
         const float c_log2 = (FP8 ? a.scale * c.kscale : a.scale) * kLog2e;
 
         auto fetch = [&](const char* pool, u32x4 (&reg)[NV], int blk, int p0, int p1) __attribute__((always_inline)) {
@@ -585,9 +613,10 @@ __global__ __launch_bounds__(kTreeWaves * kWave, 2) void tree_rows_kernel(TreeRu
             const bool masked = have != ~0u || j0 + kTreeBlock > u.s.len;
             bool apart = false;
             if (masked) {
+                uint32_t bad = 0;
 #pragma unroll
-                for (int n = 0; n < NV; ++n) apart |= not_finite<T, FP8>(vreg[n]);
-                apart = __builtin_amdgcn_ballot_w64(apart) != 0;
+                for (int n = 0; n < NV; ++n) bad |= not_finite<T, FP8>(vreg[n]);
+                apart = __builtin_amdgcn_ballot_w64(bad != 0) != 0;
             }
             if (more) fetch(c.v, vreg, blk + W, n0, n1);
 
@@ -601,7 +630,7 @@ __global__ __launch_bounds__(kTreeWaves * kWave, 2) void tree_rows_kernel(TreeRu
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     x[e] = acc[k][e >> 2][e & 3] * c_log2;
-                    if (masked && !(bits[k] >> (16 * (e >> 2) + 4 * q + (e & 3)) & 1u)) x[e] = ninf;
+                    if (masked) x[e] = if_seen(bits[k] >> (4 * q), 16 * (e >> 2) + (e & 3), x[e]);
                 }
                 f32x8 pv;
                 weigh(x, pv, U[k], R[k], l[k], LazyLimit<T>::kMoveLog2);
@@ -658,62 +687,68 @@ __global__ __launch_bounds__(kTreeWaves * kWave, 2) void tree_rows_kernel(TreeRu
 
 // ---- 64 or 128 rows: the wavefronts read the keys together (f16 / bf16) -----------------------------
 //
-// With more rows than 32 the products outweigh the keys' way through LDS, so the four wavefronts share one
-// double-buffered tile of 64 keys, in the layout of flashd_tile_parts.h, and the 32 x 32 x 16 products: wavefront
-// w has rows 32 (w % RW) .. + 31 of the tile and every KW-th 32-key block (RW KW = 4; two wavefronts to a
+// With more rows than 32 the products outweigh the keys' way through LDS, so the four wavefronts share
+// tiles of 64 keys, in the layout of flashd_tile_parts.h, and the 32 x 32 x 16 products: wavefront w has rows 32 (w % RW) .. + 31 of the tile and every KW-th 32-key block (RW KW = 4; two wavefronts to a
 // row's keys for up to 64 rows, none share for 128).  Each wavefront brings the 16 keys of a tile that it would
 // in that layout: they lie in one page, so its copies have one scalar base.
 // (The copies are written as instructions: where the compiler knows of a copy into LDS under way, it waits for it before
 // every read of LDS that it cannot tell apart from the copy's target, and with the slot in a register it can tell
 // none: the copies of tile t + 1 then ended before the math of tile t began.)
+// A barrier behind the wavefront's reads and writes of LDS (__syncthreads would wait for the copies as well)
+__device__ __forceinline__ void barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 __device__ __forceinline__ uint32_t lds_address(const void* p) {
     return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) char*)p;
+}
+// The lane's number, formed anew: what depends on it is then formed where it is used.  Kept over the loop those addresses were
+// spilled, and the wait for one to come back is one for every copy under way.
+__device__ __forceinline__ int lane_now() {
+    int x;
+    asm volatile("v_mbcnt_lo_u32_b32 %0, -1, 0\n\tv_mbcnt_hi_u32_b32 %0, -1, %0" : "=v"(x));
+    return x;
 }
 template <typename T, int D, bool FP8> struct TileLoader;
 
 // straight from global memory to LDS
 template <typename T, int D> struct TileLoader<T, D, false> {
-    uint32_t koff, voff;         // bytes; copy n takes koff ^ 64 n (DmaLane in flashd_tile_parts.h)
-    __device__ __forceinline__ TileLoader(int lane) {
-        const DmaLane<D> dl(0, lane);
-        koff = dl.koff[0];
-        voff = dl.voff;
-    }
-    // A wavefront's copies, 1 KB each (the immediate offset counts on both sides).  M0 holds the target; one wait state
-    // has to pass between writing it and the copy.  It is left as it was.
-    __device__ __forceinline__ void start(const Window& k, const Window& v, uint16_t* ks, uint16_t* vs, int wave) {
-        constexpr int NI = DmaLane<D>::NI;
-        const uint32_t kw = lds_address(ks) + 1024 * NI * wave, vw = lds_address(vs) + 1024 * NI * wave;
-        uint32_t m0, k0 = koff;
-        asm volatile("" : "+v"(k0));         // the other offsets are formed here, not kept
+    // A wavefront's copies of a tile of K or V, 1 KB each (the immediate offset counts on both sides).  M0 holds the
+    // target; one wait state has to pass between writing it and the copy.  It is left as it was.
+    static constexpr int NI = DmaLane<D>::NI;
+    __device__ __forceinline__ void copy(const Window& w, uint16_t* to, int wave, uint32_t o0, uint32_t o1, uint32_t o2, uint32_t o3) {
+        const uint32_t at = lds_address(to) + 1024 * NI * wave;
+        uint32_t m0;
         if constexpr (NI == 4)
-            asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %8\n\ts_nop 0\n\t"
-                         "buffer_load_dwordx4 %1, %6, 0 offen lds\n\t"
-                         "buffer_load_dwordx4 %2, %6, 0 offen offset:1024 lds\n\t"
-                         "buffer_load_dwordx4 %3, %6, 0 offen offset:2048 lds\n\t"
-                         "buffer_load_dwordx4 %4, %6, 0 offen offset:3072 lds\n\t"
-                         "s_mov_b32 m0, %9\n\ts_nop 0\n\t"
-                         "buffer_load_dwordx4 %5, %7, 0 offen lds\n\t"
-                         "buffer_load_dwordx4 %5, %7, 0 offen offset:1024 lds\n\t"
-                         "buffer_load_dwordx4 %5, %7, 0 offen offset:2048 lds\n\t"
-                         "buffer_load_dwordx4 %5, %7, 0 offen offset:3072 lds\n\t"
-                         "s_mov_b32 m0, %0"
-                         : "=&s"(m0)
-                         : "v"(k0), "v"(k0 ^ 64u), "v"(k0 ^ 128u), "v"(k0 ^ 192u), "v"(voff),
-                           "s"(k.words), "s"(v.words), "s"(kw), "s"(vw) : "memory");
-        else
             asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %6\n\ts_nop 0\n\t"
-                         "buffer_load_dwordx4 %1, %4, 0 offen lds\n\t"
-                         "buffer_load_dwordx4 %2, %4, 0 offen offset:1024 lds\n\t"
-                         "s_mov_b32 m0, %7\n\ts_nop 0\n\t"
-                         "buffer_load_dwordx4 %3, %5, 0 offen lds\n\t"
-                         "buffer_load_dwordx4 %3, %5, 0 offen offset:1024 lds\n\t"
+                         "buffer_load_dwordx4 %1, %5, 0 offen lds\n\t"
+                         "buffer_load_dwordx4 %2, %5, 0 offen offset:1024 lds\n\t"
+                         "buffer_load_dwordx4 %3, %5, 0 offen offset:2048 lds\n\t"
+                         "buffer_load_dwordx4 %4, %5, 0 offen offset:3072 lds\n\t"
                          "s_mov_b32 m0, %0"
-                         : "=&s"(m0)
-                         : "v"(k0), "v"(k0 ^ 64u), "v"(voff), "s"(k.words), "s"(v.words), "s"(kw), "s"(vw)
-                         : "memory");
+                         : "=&s"(m0) : "v"(o0), "v"(o1), "v"(o2), "v"(o3), "s"(w.words), "s"(at) : "memory");
+        else
+            asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %4\n\ts_nop 0\n\t"
+                         "buffer_load_dwordx4 %1, %3, 0 offen lds\n\t"
+                         "buffer_load_dwordx4 %2, %3, 0 offen offset:1024 lds\n\t"
+                         "s_mov_b32 m0, %0"
+                         : "=&s"(m0) : "v"(o0), "v"(o1), "s"(w.words), "s"(at) : "memory");
     }
-    __device__ __forceinline__ void finish(uint16_t*, uint16_t*, int, int) { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+    // (offsets as in DmaLane of flashd_tile_parts.h: copy n of K takes those of the first ^ 64 n)
+    __device__ __forceinline__ void start_k(const Window& w, uint16_t* to, int wave) {
+        const int lane = lane_now(), row = lane / TileCfg<D>::CPR;
+        const uint32_t k0 = 2 * (row * D + 8 * ((lane % TileCfg<D>::CPR) ^ TileCfg<D>::swz_k(row)));
+        copy(w, to, wave, k0, k0 ^ 64u, k0 ^ 128u, k0 ^ 192u);
+    }
+    __device__ __forceinline__ void start_v(const Window& w, uint16_t* to, int wave) {
+        const int lane = lane_now(), row = lane / TileCfg<D>::CPR;
+        const uint32_t v0 = 2 * (row * D + 8 * ((lane % TileCfg<D>::CPR) ^ TileCfg<D>::swz_v(row)));
+        copy(w, to, wave, v0, v0, v0, v0);
+    }
+    // Waits until all but the wavefront's `tiles` last tiles (of K or of V) have landed.
+    static __device__ __forceinline__ void wait_but(int tiles) {
+        if (tiles >= 3) asm volatile("s_waitcnt vmcnt(%0)" :: "n"(3 * NI) : "memory");
+        else if (tiles == 2) asm volatile("s_waitcnt vmcnt(%0)" :: "n"(2 * NI) : "memory");
+        else if (tiles == 1) asm volatile("s_waitcnt vmcnt(%0)" :: "n"(NI) : "memory");
+        else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    }
 };
 
 // fp8: through registers, widened on the way
@@ -721,9 +756,8 @@ template <typename T, int D> struct TileLoader<T, D, true> {
     static constexpr int NI = D / 64;           // 1 KB each: 16 rows of D bytes
     static constexpr int LPR = D / 16;
     u32x4 k[NI], v[NI];
-    __device__ __forceinline__ TileLoader(int) {}
-    __device__ __forceinline__ void start(const Window& kw, const Window& vw, uint16_t*, uint16_t*, int) {
-        const int lane = threadIdx.x & 63;
+    __device__ __forceinline__ void start(const Window& kw, const Window& vw) {
+        const int lane = lane_now();
         const auto kr = kw.rsrc(), vr = vw.rsrc();
 #pragma unroll
         for (int n = 0; n < NI; ++n) {
@@ -756,66 +790,63 @@ __global__ __launch_bounds__(kTreeWaves * kWave, 2) void tree_tile_kernel(TreeRu
     constexpr int NDB = D / 32;
     constexpr int kTile = kBC * D;
     constexpr int CH = D / 4;                   // 16-byte chunks of a folded row
-    __shared__ __align__(1024) uint16_t lds[4 * kTile];
-    __shared__ float fold_r[kTreeWaves][32], fold_l[kTreeWaves][32];
-    static_assert(kTreeWaves * 32 * D * 4 <= (int)sizeof(lds), "the fold lies in the tiles' LDS");
+    // Three tiles of K and two of V, 80 KB at D = 128: all of LDS in two workgroups per compute unit.  What else needs
+    // LDS lies in the same memory at other times.
+    __shared__ __align__(1024) uint16_t lds[5 * kTile];
+    uint16_t* const vlds = lds + 3 * kTile;
+    float (*fold_r)[32] = reinterpret_cast<float (*)[32]>(lds + 4 * kTile), (*fold_l)[32] = fold_r + kTreeWaves;
+    static_assert(kTreeWaves * 32 * D * 4 <= 4 * kTile * 2 && 2 * kTreeWaves * 32 * 4 <= kTile * 2, "the fold lies in the tiles' LDS");
 
-    const Paged& c = r.c;
-    const TreeArgs& a = r.a;
-    const int tid = threadIdx.x;
-    const int lane = tid & 63;
-    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    (void)r;                                    // read through args_now()
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int rw = wave & (RW - 1), kw = wave / RW;
-    const int col = lane & 31;
-    const int hh = lane >> 5;
     const float ninf = -__builtin_inff();
 
     Walk<M, kBC> u;
-    u.begin(r);
+    u.begin(args_now(), reinterpret_cast<WalkScratch*>(lds));
     if (u.at >= u.end) return;
 
-    // Operand addresses inside a tile (elements) of the wavefront's first block: those of operand kk of K and
-    // of column block i of V differ by 16 kk and 32 i under the swizzle's exclusive or.
-    const int kaddr0 = (32 * kw + col) * D + 8 * (hh ^ C::swz_k(col));
-    const int vaddr0 = (32 * kw + 4 * hh + ((lane & 15) >> 2)) * D +
-                       8 * ((2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ C::swz_v((lane & 15) >> 2)) + 4 * (lane & 1);
-    TileLoader<T, D, FP8> load(lane);
+    TileLoader<T, D, FP8> load;
 
     do {
-        const int row = u.first + min(32 * rw + col, u.nrows - 1);
-        const int token = (int)fast_div((uint32_t)row, r.group);
-        const uint16_t* qg = static_cast<const uint16_t*>(a.q) + row_at(r, u, row, a.q_stride, D);
-        u32x4 qf[NKK];
-#pragma unroll
-        for (int kk = 0; kk < NKK; ++kk) qf[kk] = *reinterpret_cast<const u32x4*>(qg + 16 * kk + 8 * hh);
-        // a negative scale is taken into Q (exact), so that the largest dot product is the top score
-        float c_log2 = (FP8 ? a.scale * c.kscale : a.scale) * kLog2e;
-        if (c_log2 < 0.0f) {
-            c_log2 = -c_log2;
-#pragma unroll
-            for (int kk = 0; kk < NKK; ++kk) qf[kk] ^= u32x4{0x80008000u, 0x80008000u, 0x80008000u, 0x80008000u};
-        }
+        const TreeRun now_r = args_now();
+        const TreeArgs& a = now_r.a;
         // keys from `clear` on may be hidden from a row of the wavefront, those from `dark` on are from all
         int clear = u.s.len, dark = u.keys();
         if (a.tree == nullptr) {
-            clear += (int)fast_div((uint32_t)(u.first + min(32 * rw, u.nrows - 1)), r.group) + 1;
-            dark = u.s.len + (int)fast_div((uint32_t)(u.first + min(32 * rw + 31, u.nrows - 1)), r.group) + 1;
+            clear += (int)fast_div((uint32_t)(u.first + min(32 * rw, u.nrows - 1)), now_r.group) + 1;
+            dark = u.s.len + (int)fast_div((uint32_t)(u.first + min(32 * rw + 31, u.nrows - 1)), now_r.group) + 1;
         }
         if (32 * rw >= u.nrows) dark = 0;
 
-        // pages of 16 tiles' 16-key groups, lane l that of group l of them; the next 16 tiles' a few tiles ahead
-        auto look_up = [&](int tile0) __attribute__((always_inline)) {
-            const int key = tile0 * kBC + 16 * lane;
-            return tile0 + (lane >> 2) < u.blk1 && key < u.keys() ? page_at(c, u.b, key >> c.page_log2) : -1;
+        // What the loop needs of the arguments, each in a register of its own (as loaded, in groups of four and more, they
+        // are spilled and fetched back group by group).
+        constexpr int ROW = D * (FP8 ? 1 : 2);
+        const char* kpool = now_r.c.k + u.h * now_r.c.head_bytes;
+        const char* vpool = now_r.c.v + u.h * now_r.c.head_bytes;
+        int64_t page_bytes = now_r.c.page_bytes;
+        int page_log2 = now_r.c.page_log2, pool_pages = now_r.c.P, last_key = u.keys(), blk0 = u.blk0, tiles = u.blk1 - u.blk0;
+        // The page of the wavefront's 16 keys of tile i of the piece, by a scalar load (a vector load's wait would
+        // be one for the copies under way as well); -1 behind the last key.
+        typedef const __attribute__((address_space(4))) int* table_ptr;
+        table_ptr trow = (table_ptr)(uintptr_t)(now_r.c.table + (size_t)u.b * now_r.c.max_pages);
+        asm volatile("" : "+s"(kpool), "+s"(vpool), "+s"(page_bytes), "+s"(page_log2), "+s"(pool_pages), "+s"(last_key),
+                          "+s"(blk0), "+s"(tiles), "+s"(trow));
+        auto page_of = [&](int i) __attribute__((always_inline)) {
+            const int key = (blk0 + i) * kBC + 16 * wave;
+            return i < tiles && key < last_key ? trow[key >> page_log2] : -1;
         };
-        int pages = look_up(u.blk0), pages_next = -1;
-        uint64_t gaps = __builtin_amdgcn_ballot_w64(pages < 0);
-        auto start_copy = [&](int t, int slot) __attribute__((always_inline)) {
-            const int page = __builtin_amdgcn_readlane(pages, 4 * ((t - u.blk0) & 15) + wave);
-            const int key = t * kBC + 16 * wave;
-            uint16_t* ks = lds + slot * kTile;
-            load.start(half_window(c, u, c.k, page, key), half_window(c, u, c.v, page, key), ks, ks + 2 * kTile, wave);
+        auto window = [&](const char* pool, int i, int page) __attribute__((always_inline)) {
+            const int key = (blk0 + i) * kBC + 16 * wave;
+            const bool there = (unsigned)page < (unsigned)pool_pages;
+            const uint64_t at = (uint64_t)(pool + (there ? page : 0) * page_bytes + (key & ((1 << page_log2) - 1)) * ROW);
+            const int left = last_key - key, keys = !there || left < 0 ? 0 : left < 16 ? left : 16;
+            return Window{u32x4{(uint32_t)uniform((int)at), (uint32_t)uniform((int)(at >> 32)), (uint32_t)uniform(keys * ROW), 0x00020000u}};
         };
+        int page1 = page_of(0), page2 = page_of(1);      // of tiles now + 1 and now + 2, once now is 0
+        const Window k0 = window(kpool, 0, page1), v0 = window(vpool, 0, page1), k1 = window(kpool, 1, page2);
+        page1 = page2;
+        page2 = page_of(2);
 
         f32x16 U[NDB];
 #pragma unroll
@@ -824,47 +855,96 @@ __global__ __launch_bounds__(kTreeWaves * kWave, 2) void tree_tile_kernel(TreeRu
             for (int e = 0; e < 16; ++e) U[i][e] = 0.0f;
         RowState st = {ninf, 0.0f, 0.0f};
 
-        start_copy(u.blk0, 0);
-        load.finish(lds, lds + 2 * kTile, wave, lane);
-        __syncthreads();
-
-        // Period t: the copies of tile t + 1 into the other slot, which was last read in period t - 1; the
-        // math of tile t; the end of the copies; barrier.
-        // (One body for both slots and both blocks: in two or four copies the products' operands have constant addresses, but
-        // the code that masks need, in each of them, then costs the registers that hold U.)
+        // Tile i of the piece: K in slot i % 3, V in slot i % 2, copied in the order K0 V0 K1 | V1 K2 | V2 K3 | ..., the
+        // last two of these while tile i is worked on.  So a tile of V has a period to arrive and one of K two: with one
+        // tile of each ahead the copies' latency was longer than the math.  Two barriers a period: at its start every
+        // wavefront's copies of K_i have landed and all have done with tile i - 1, whose slots the copies to start
+        // then may fill; before the output product V_i has landed.
+        // (One body for all slots and both blocks: copies of it with constant operand addresses cost the code
+        // that masks need several times, and with it the registers that hold U.)
+        const int lane = lane_now(), col = lane & 31, hh = lane >> 5;
+        if constexpr (FP8) {
+            load.start(k0, v0);
+            load.finish(lds, vlds, wave, lane);
+        } else {
+            load.start_k(k0, lds, wave);
+            load.start_v(v0, vlds, wave);
+            if (tiles > 1) load.start_k(k1, lds + kTile, wave);
+        }
+        // a table with holes: which of the tile's keys have no page is looked up tile by tile
+        bool gaps = false;
+        for (int k = (blk0 * kBC >> page_log2) + lane; k << page_log2 < min((blk0 + tiles) * kBC, last_key); k += kWave)
+            gaps |= page_at(now_r.c, u.b, k) < 0;
+        gaps = __builtin_amdgcn_ballot_w64(gaps) != 0;
+        const int row = u.first + min(32 * rw + col, u.nrows - 1);
+        const uint16_t* qg = static_cast<const uint16_t*>(a.q) + row_at(now_r, u, row, a.q_stride, D);
+        u32x4 qf[NKK];
+#pragma unroll
+        for (int kk = 0; kk < NKK; ++kk) qf[kk] = *reinterpret_cast<const u32x4*>(qg + 16 * kk + 8 * hh);
+        // Here to stay before the loop, as the compiler knows: it would else wait for them, and so for all copies, in every turn.
+        wait_copies();
+        // a negative scale is taken into Q (exact), so that the largest dot product is the top score
+        float c_log2 = (FP8 ? a.scale * now_r.c.kscale : a.scale) * kLog2e;
+        if (c_log2 < 0.0f) {
+            c_log2 = -c_log2;
+#pragma unroll
+            for (int kk = 0; kk < NKK; ++kk) qf[kk] ^= u32x4{0x80008000u, 0x80008000u, 0x80008000u, 0x80008000u};
+        }
+        int kslot = 0;
 #pragma unroll 1
-        for (int t = u.blk0; t < u.blk1; ++t) {
-            const int in = (t - u.blk0) & 15;
-            const uint32_t hole = (uint32_t)(gaps >> (4 * in)) & 15u;      // groups of this tile without a page
-            const bool more = t + 1 < u.blk1;
-            if (in == 7) pages_next = look_up(t + 9);
-            if (in == 15) {
-                pages = pages_next;
-                gaps = __builtin_amdgcn_ballot_w64(pages < 0);
+        for (int now = 0; now < tiles; ++now) {
+            const int t = blk0 + now;
+            const bool more = now + 1 < tiles;
+            if constexpr (!FP8) load.wait_but(more ? 2 : 1);
+            barrier();
+            const int knext = kslot == 2 ? 0 : kslot + 1;
+            if constexpr (FP8) {
+                if (more) load.start(window(kpool, now + 1, page1), window(vpool, now + 1, page1));
+            } else {
+                if (more) load.start_v(window(vpool, now + 1, page1), vlds + ((now + 1) & 1) * kTile, wave);
+                if (now + 2 < tiles) load.start_k(window(kpool, now + 2, page2), lds + (knext == 2 ? 0 : knext + 1) * kTile, wave);
             }
-            const int slot = in & 1;
-            if (more) start_copy(t + 1, slot ^ 1);
-            const uint16_t* ks = lds + slot * kTile;
-            const uint16_t* vs = ks + 2 * kTile;
+            page1 = page2;
+            page2 = page_of(now + 3);
+            const uint16_t* ks = lds + kslot * kTile;
+            const uint16_t* vs = vlds + (now & 1) * kTile;
+            uint32_t hole = 0;                           // 16-key groups of this tile without a page
+            if (gaps) {
+                const int key = t * kBC + 16 * (lane_now() & 3);
+                const TreeRun m = args_now();
+                hole = (uint32_t)__builtin_amdgcn_ballot_w64(key >= last_key || page_at(m.c, u.b, key >> page_log2) < 0) & 15u;
+            }
 #pragma unroll 1
             for (int n = 0; n < NB; ++n) {
                 const int j0 = t * kBC + 32 * (kw + n);
-                if (j0 >= dark) continue;
-                int kaddr = kaddr0 + 32 * n * D, vaddr = vaddr0 + 32 * n * D;
-                asm volatile("" : "+v"(kaddr), "+v"(vaddr));        // the addresses of operands are formed here, not kept
-                u32x4 ka[NKK];
-#pragma unroll
-                for (int kk = 0; kk < NKK; ++kk) ka[kk] = *reinterpret_cast<const u32x4*>(&ks[kaddr ^ 16 * kk]);
+                const bool work = j0 < dark;
                 f32x16 acc;
+                if (work) {
+                    // operand kk's address is that of the first ^ 16 kk elements, under the swizzle's exclusive or
+                    const int x = lane_now();
+                    const int kaddr = (32 * (kw + n) + (x & 31)) * D + 8 * ((x >> 5) ^ C::swz_k(x & 31));
+                    u32x4 ka[NKK];
 #pragma unroll
-                for (int e = 0; e < 16; ++e) acc[e] = 0.0f;
+                    for (int kk = 0; kk < NKK; ++kk) ka[kk] = *reinterpret_cast<const u32x4*>(&ks[kaddr ^ 16 * kk]);
 #pragma unroll
-                for (int kk = 0; kk < NKK; ++kk) acc = Mma<T>::mfma(ka[kk], qf[kk], acc);
-                // all of K's operands are asked for before the first product (LDS returns in order)
-                __builtin_amdgcn_sched_group_barrier(0x100, NKK, 0);
-                __builtin_amdgcn_sched_group_barrier(0x008, NKK, 0);
-                __builtin_amdgcn_sched_barrier(0);
+                    for (int e = 0; e < 16; ++e) acc[e] = 0.0f;
+#pragma unroll
+                    for (int kk = 0; kk < NKK; ++kk) acc = Mma<T>::mfma(ka[kk], qf[kk], acc);
+                    // all of K's operands are asked for before the first product (LDS returns in order)
+                    __builtin_amdgcn_sched_group_barrier(0x100, NKK, 0);
+                    __builtin_amdgcn_sched_group_barrier(0x008, NKK, 0);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                if constexpr (!FP8) {
+                    if (n == 0) {
+                        load.wait_but((more ? 2 : 0) + (now + 2 < tiles ? 1 : 0));
+                        barrier();
+                    }
+                }
+                if (!work) continue;
                 // V operands on their way while the coefficients are formed
+                const int x = lane_now(), xq = (x & 15) >> 2;
+                const int vaddr = (32 * (kw + n) + 4 * (x >> 5) + xq) * D + 8 * ((2 * (x >> 4 & 1) + ((x & 3) >> 1)) ^ C::swz_v(xq)) + 4 * (x & 1);
                 u32x4 va[2 * NDB];
 #pragma unroll
                 for (int m = 0; m < 2 * NDB; ++m) va[m] = tile_v_operand<D>(vs, vaddr ^ 32 * (m % NDB), 16 * (m / NDB));
@@ -872,23 +952,28 @@ __global__ __launch_bounds__(kTreeWaves * kWave, 2) void tree_tile_kernel(TreeRu
 
                 const uint32_t lost = hole >> (2 * (kw + n)) & 3u;
                 const bool masked = lost != 0 || j0 + 32 > clear;
-                u32x4 bfrag[2];
-                if (!masked) {
-                    top_first_pack<T, NDB, false>(acc, bfrag, st, U, c_log2, false, 0);
-                } else {
-                    uint32_t bits = seen_bits(a, u.s, token, u.s.row0 + token, j0);
+                float scale = c_log2;
+                uint32_t mine = ~0u;
+                if (masked) {
+                    const TreeRun m = args_now();
+                    const int token = (int)fast_div((uint32_t)(u.first + min(32 * rw + (x & 31), u.nrows - 1)), m.group);
+                    uint32_t bits = seen_bits(m.a, u.s, token, u.s.row0 + token, j0);
                     if (lost & 1u) bits &= 0xffff0000u;
                     if (lost & 2u) bits &= 0x0000ffffu;
-                    const uint32_t mine = bits >> (4 * hh);
+                    mine = bits >> (4 * (x >> 5));
                     // (a scale of 0 or NaN would take a hidden key away from -inf: it is applied here)
                     const float by = c_log2 > 0.0f ? 1.0f : c_log2;
+                    scale = c_log2 > 0.0f ? c_log2 : 1.0f;
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) acc[e] = mine >> (8 * (e >> 2) + (e & 3)) & 1u ? acc[e] * by : ninf;
-                    top_first_pack<T, NDB, false>(acc, bfrag, st, U, c_log2 > 0.0f ? c_log2 : 1.0f, false, 0);
-                    bool apart = false;
+                    for (int e = 0; e < 16; ++e) acc[e] = if_seen(mine, 8 * (e >> 2) + (e & 3), acc[e] * by);
+                }
+                u32x4 bfrag[2];
+                top_first_pack<T, NDB, false>(acc, bfrag, st, U, scale, false, 0);
+                if (masked) {
+                    uint32_t apart = 0;
 #pragma unroll
                     for (int m = 0; m < 2 * NDB; ++m) apart |= not_finite<T, false>(va[m]);
-                    if (__builtin_amdgcn_ballot_w64(apart) != 0) {
+                    if (__builtin_amdgcn_ballot_w64(apart != 0) != 0) {
 #pragma unroll
                         for (int i = 0; i < NDB; ++i) {
                             f32x16 count;
@@ -904,7 +989,7 @@ __global__ __launch_bounds__(kTreeWaves * kWave, 2) void tree_tile_kernel(TreeRu
 #pragma unroll
                             for (int e = 0; e < 16; ++e) {
                                 U[i][e] += what_is_seen(count[e]);
-                                if ((e & 3) == 3) __builtin_amdgcn_sched_barrier(0);
+                                __builtin_amdgcn_sched_barrier(0);
                             }
                         }
                     }
@@ -912,26 +997,27 @@ __global__ __launch_bounds__(kTreeWaves * kWave, 2) void tree_tile_kernel(TreeRu
 #pragma unroll
                 for (int m = 0; m < 2 * NDB; ++m) U[m % NDB] = Mma<T>::mfma(va[m], bfrag[m / NDB], U[m % NDB]);
             }
-            if (more) load.finish(lds + (slot ^ 1) * kTile, lds + (2 + (slot ^ 1)) * kTile, wave, lane);
-            __syncthreads();
+            if constexpr (FP8) {
+                if (more) load.finish(lds + knext * kTile, vlds + ((now + 1) & 1) * kTile, wave, lane_now());
+            }
+            kslot = knext;
         }
+        __syncthreads();
 
         // ---- rows through LDS; with KW = 2 the two states of a row are joined.  Chunk t of row c lies at t ^ c.
         const float l = pair_sum(st.l);
         float* fold = reinterpret_cast<float*>(lds);
-        // (the lanes' arithmetic from here on stays here: kept over the loops it would take their registers)
-        int elane = lane;
-        asm volatile("" : "+v"(elane));
-        const int col = elane & 31, hh = elane >> 5, tid = 64 * wave + elane;
+        const int elane = lane_now(), ecol = elane & 31, tid = 64 * wave + elane;
+        const TreeRun end_r = args_now();
 #pragma unroll
         for (int i = 0; i < NDB; ++i)
 #pragma unroll
             for (int y = 0; y < 4; ++y)
-                *reinterpret_cast<f32x4*>(&fold[((wave * 32 + col) * CH + ((8 * i + 2 * y + hh) ^ (col & (CH - 1)))) * 4]) =
+                *reinterpret_cast<f32x4*>(&fold[((wave * 32 + ecol) * CH + ((8 * i + 2 * y + (elane >> 5)) ^ (ecol & (CH - 1)))) * 4]) =
                     f32x4{U[i][4 * y], U[i][4 * y + 1], U[i][4 * y + 2], U[i][4 * y + 3]};
-        if (hh == 0) {
-            fold_r[wave][col] = st.R;
-            fold_l[wave][col] = l;
+        if (elane < 32) {
+            fold_r[wave][ecol] = st.R;
+            fold_l[wave][ecol] = l;
         }
         __syncthreads();
         for (int idx = tid; idx < u.nrows * CH; idx += kTreeWaves * kWave) {
@@ -952,11 +1038,11 @@ __global__ __launch_bounds__(kTreeWaves * kWave, 2) void tree_tile_kernel(TreeRu
 #pragma unroll
                 for (int e = 0; e < 4; ++e) o[e] = fmaf(f, none ? 0.0f : x[e], o[e]);
             }
-            put_row<T, D, M>(r, u, fr, 4 * ch, o, top, lt, FP8 ? c.vscale : 1.0f);
+            put_row<T, D, M>(end_r, u, fr, 4 * ch, o, top, lt, FP8 ? end_r.c.vscale : 1.0f);
         }
-        if (u.blk0 == 0 && !u.whole() && tid == 0) u.note_split(r);
+        if (u.blk0 == 0 && !u.whole() && tid == 0) u.note_split(end_r);
         __syncthreads();
-    } while (u.next(r));
+    } while (u.next(args_now()));
 }
 
 // ---- the same in fp32 ------------------------------------------------------------------------------
@@ -982,7 +1068,7 @@ __global__ __launch_bounds__(kTreeWaves * kWave, 2) void tree_rows_f32_kernel(Tr
     const float ninf = -__builtin_inff();
 
     Walk<16, kTreeBlock> u;
-    u.begin(r);
+    u.begin(r, reinterpret_cast<WalkScratch*>(fold));
     if (u.at >= u.end) return;
     do {
         const int row = u.first + min(col, u.nrows - 1);
