@@ -429,8 +429,8 @@ template <typename T> struct Half {
     static constexpr bool B = Mma<T>::kRoundedSum;                          // bf16, else f16
     static constexpr uint32_t kExp = B ? 0x7f807f80u : 0x7c007c00u, kOne = B ? 0x00800080u : 0x04000400u;
     static constexpr uint32_t kMan = B ? 0x007f007fu : 0x03ff03ffu, kTop = 0x80008000u;
-    static constexpr uint32_t kPlus = B ? 0x3f803f80u : 0x3c003c00u, kMinus = B ? 0x42804280u : 0x54005400u,
-                              kNan = B ? 0x45804580u : 0x6c006c00u;         // 1, 64 and 4096
+    static constexpr uint32_t kPlus = B ? 0x3f803f80u : 0x3c003c00u, kMinus = B ? 0x43004300u : 0x58005800u,
+                              kNan = B ? 0x46804680u : 0x74007400u;         // 1, 128 and 16384
     // top bits of the halves that are infinite or NaN
     static __device__ __forceinline__ uint32_t bad(uint32_t x) { return ((x & kExp) + kOne) & kTop; }
     // top bits -> whole halves
@@ -450,8 +450,8 @@ __device__ __forceinline__ uint32_t not_finite(u32x4 x) {
 }
 
 // The products of such a block: the values that are no numbers are left out of the product with the weights
-// (numbers_of) and counted by one with the bits of what is seen, +infinities as 1, -infinities as 64, NaN as 4096
-// (codes_of; a block has 32 keys, and the sum is exact); what_is_seen() says what a count adds to an output.
+// (numbers_of) and counted by one with the bits of what is seen, +infinities as 1, -infinities as 128, NaN as
+// 16384 (codes_of; of at most 64 keys, so the sum is exact and keeps them apart); what_is_seen() says what a count adds to an output.
 template <typename T>
 __device__ __forceinline__ u32x4 numbers_of(u32x4 x) {
 #pragma unroll
@@ -471,8 +471,8 @@ __device__ __forceinline__ u32x4 codes_of(u32x4 x) {
 __device__ __forceinline__ float what_is_seen(float count) {
     const int n = (int)count;
     const float inf = __builtin_inff();
-    const bool plus = (n & 63) != 0, minus = (n >> 6 & 63) != 0;
-    return n >= 4096 || (plus && minus) ? __builtin_nanf("") : plus ? inf : minus ? -inf : 0.0f;
+    const bool plus = (n & 127) != 0, minus = (n >> 7 & 127) != 0;
+    return n >= 16384 || (plus && minus) ? __builtin_nanf("") : plus ? inf : minus ? -inf : 0.0f;
 }
 // 8 bits, lowest first, as ones and zeros of the storage type
 template <typename T>
@@ -742,13 +742,9 @@ template <typename T, int D> struct TileLoader<T, D, false> {
         const uint32_t v0 = 2 * (row * D + 8 * ((lane % TileCfg<D>::CPR) ^ TileCfg<D>::swz_v(row)));
         copy(w, to, wave, v0, v0, v0, v0);
     }
-    // Waits until all but the wavefront's `tiles` last tiles (of K or of V) have landed.
-    static __device__ __forceinline__ void wait_but(int tiles) {
-        if (tiles >= 3) asm volatile("s_waitcnt vmcnt(%0)" :: "n"(3 * NI) : "memory");
-        else if (tiles == 2) asm volatile("s_waitcnt vmcnt(%0)" :: "n"(2 * NI) : "memory");
-        else if (tiles == 1) asm volatile("s_waitcnt vmcnt(%0)" :: "n"(NI) : "memory");
-        else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    }
+    // Waits until all but the wavefront's N last tiles (of K or of V) have landed.
+    template <int N>
+    static __device__ __forceinline__ void wait_but() { asm volatile("s_waitcnt vmcnt(%0)" :: "n"(N * NI) : "memory"); }
 };
 
 // fp8: through registers, widened on the way
@@ -780,6 +776,45 @@ template <typename T, int D> struct TileLoader<T, D, true> {
     }
 };
 
+// The scores (acc, overwritten) of NB 32-key blocks of a row: the reference moves to their top score where that lies more
+// than kMoveLog2 above it, as in top_first_pack() of flashd_rows.h, looked at once for all of them; keys that the
+// row does not see are -inf and scale is positive.
+template <typename T, int NB, int NDB>
+__device__ __forceinline__ void weigh_blocks(f32x16 (&acc)[NB], u32x4 (&bfrag)[2 * NB], RowState& st, f32x16 (&U)[NDB],
+                                             float scale) {
+    const float ninf = -__builtin_inff();
+    float top[2] = {acc[0][0], acc[0][1]};
+#pragma unroll
+    for (int n = 0; n < NB; ++n)
+#pragma unroll
+        for (int e = 2 * (n == 0); e < 16; e += 2) {
+            top[0] = fmaxf(top[0], acc[n][e]);
+            top[1] = fmaxf(top[1], acc[n][e + 1]);
+        }
+    const float t = pair_max(fmaxf(top[0], top[1])) * scale;
+    if (__builtin_amdgcn_ballot_w64(t > st.R + LazyLimit<T>::kMoveLog2) != 0) {
+        const bool move = t > st.R + LazyLimit<T>::kMoveLog2;
+        const float f = move ? exp2_fast(st.R - t) : 1.0f;       // 0 for a row without keys
+        st.R = move ? t : st.R;
+        st.l *= f;
+#pragma unroll
+        for (int i = 0; i < NDB; ++i)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) U[i][e] *= f;
+    }
+    const float ref = st.R == ninf ? 0.0f : st.R;                // no key yet: weights of zero
+    f32x4 ps = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int g = 0; g < 2 * NB; ++g) {
+        f32x8 p;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) p[e] = exp2_fast(fmaf(acc[g >> 1][8 * (g & 1) + e], scale, -ref));
+        bfrag[g] = Mma<T>::pack8(p);
+        Mma<T>::sum8(p, bfrag[g], ps);
+    }
+    st.l += (ps[0] + ps[1]) + (ps[2] + ps[3]);
+}
+
 template <typename T, int D, bool FP8, int RW>
 __global__ __launch_bounds__(kTreeWaves * kWave, 2) void tree_tile_kernel(TreeRun r) {
     using C = TileCfg<D>;
@@ -788,6 +823,7 @@ __global__ __launch_bounds__(kTreeWaves * kWave, 2) void tree_tile_kernel(TreeRu
     constexpr int NB = 2 / KW;                  // 32-key blocks of a tile that are a wavefront's
     constexpr int NKK = D / 16;
     constexpr int NDB = D / 32;
+    static_assert(32 * NB < 128, "codes_of counts the keys of a wavefront's blocks");
     constexpr int kTile = kBC * D;
     constexpr int CH = D / 4;                   // 16-byte chunks of a folded row
     // Three tiles of K and two of V, 80 KB at D = 128: all of LDS in two workgroups per compute unit.  What else needs
@@ -847,6 +883,8 @@ __global__ __launch_bounds__(kTreeWaves * kWave, 2) void tree_tile_kernel(TreeRu
         const Window k0 = window(kpool, 0, page1), v0 = window(vpool, 0, page1), k1 = window(kpool, 1, page2);
         page1 = page2;
         page2 = page_of(2);
+        // what is copied while tile 0 is worked on; behind the last tile windows are empty and copies bring zeros
+        Window vnext = window(vpool, 1, page1), knext = window(kpool, 2, page2);
 
         f32x16 U[NDB];
 #pragma unroll
@@ -869,7 +907,7 @@ __global__ __launch_bounds__(kTreeWaves * kWave, 2) void tree_tile_kernel(TreeRu
         } else {
             load.start_k(k0, lds, wave);
             load.start_v(v0, vlds, wave);
-            if (tiles > 1) load.start_k(k1, lds + kTile, wave);
+            load.start_k(k1, lds + kTile, wave);
         }
         // a table with holes: which of the tile's keys have no page is looked up tile by tile
         bool gaps = false;
@@ -894,15 +932,15 @@ __global__ __launch_bounds__(kTreeWaves * kWave, 2) void tree_tile_kernel(TreeRu
 #pragma unroll 1
         for (int now = 0; now < tiles; ++now) {
             const int t = blk0 + now;
-            const bool more = now + 1 < tiles;
-            if constexpr (!FP8) load.wait_but(more ? 2 : 1);
-            barrier();
-            const int knext = kslot == 2 ? 0 : kslot + 1;
+            const int k1slot = kslot == 2 ? 0 : kslot + 1;
             if constexpr (FP8) {
-                if (more) load.start(window(kpool, now + 1, page1), window(vpool, now + 1, page1));
+                barrier();
+                if (now + 1 < tiles) load.start(window(kpool, now + 1, page1), vnext);
             } else {
-                if (more) load.start_v(window(vpool, now + 1, page1), vlds + ((now + 1) & 1) * kTile, wave);
-                if (now + 2 < tiles) load.start_k(window(kpool, now + 2, page2), lds + (knext == 2 ? 0 : knext + 1) * kTile, wave);
+                load.template wait_but<2>();
+                barrier();
+                load.start_v(vnext, vlds + ((now + 1) & 1) * kTile, wave);
+                load.start_k(knext, lds + (k1slot == 2 ? 0 : k1slot + 1) * kTile, wave);
             }
             page1 = page2;
             page2 = page_of(now + 3);
@@ -914,77 +952,104 @@ __global__ __launch_bounds__(kTreeWaves * kWave, 2) void tree_tile_kernel(TreeRu
                 const TreeRun m = args_now();
                 hole = (uint32_t)__builtin_amdgcn_ballot_w64(key >= last_key || page_at(m.c, u.b, key >> page_log2) < 0) & 15u;
             }
-#pragma unroll 1
-            for (int n = 0; n < NB; ++n) {
-                const int j0 = t * kBC + 32 * (kw + n);
-                const bool work = j0 < dark;
-                f32x16 acc;
-                if (work) {
-                    // operand kk's address is that of the first ^ 16 kk elements, under the swizzle's exclusive or
-                    const int x = lane_now();
-                    const int kaddr = (32 * (kw + n) + (x & 31)) * D + 8 * ((x >> 5) ^ C::swz_k(x & 31));
-                    u32x4 ka[NKK];
+            const int j0 = t * kBC + 32 * kw;            // first of the wavefront's keys of this tile
+            const bool work = j0 < dark;
+            f32x16 acc[NB];
+            if (work) {
+                // operand kk's address is that of the first ^ 16 kk elements, under the swizzle's exclusive or
+                const int x = lane_now();
+                const int kaddr = (32 * kw + (x & 31)) * D + 8 * ((x >> 5) ^ C::swz_k(x & 31));
 #pragma unroll
-                    for (int kk = 0; kk < NKK; ++kk) ka[kk] = *reinterpret_cast<const u32x4*>(&ks[kaddr ^ 16 * kk]);
+                for (int n = 0; n < NB; ++n)
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) acc[e] = 0.0f;
+                    for (int e = 0; e < 16; ++e) acc[n][e] = 0.0f;
+                // Reads run 8 ahead of the products (LDS returns in order); the chains of the two blocks alternate.
+                constexpr int AHEAD = NKK * NB < 8 ? NKK * NB : 8;
+                u32x4 ka[NKK * NB];
 #pragma unroll
-                    for (int kk = 0; kk < NKK; ++kk) acc = Mma<T>::mfma(ka[kk], qf[kk], acc);
-                    // all of K's operands are asked for before the first product (LDS returns in order)
-                    __builtin_amdgcn_sched_group_barrier(0x100, NKK, 0);
-                    __builtin_amdgcn_sched_group_barrier(0x008, NKK, 0);
-                    __builtin_amdgcn_sched_barrier(0);
+                for (int m = 0; m < AHEAD; ++m) ka[m] = *reinterpret_cast<const u32x4*>(&ks[(kaddr ^ 16 * (m / NB)) + 32 * D * (m % NB)]);
+#pragma unroll
+                for (int m = 0; m < NKK * NB; ++m) {
+                    acc[m % NB] = Mma<T>::mfma(ka[m], qf[m / NB], acc[m % NB]);
+                    if (m + AHEAD < NKK * NB)
+                        ka[m + AHEAD] = *reinterpret_cast<const u32x4*>(&ks[(kaddr ^ 16 * ((m + AHEAD) / NB)) + 32 * D * ((m + AHEAD) % NB)]);
                 }
-                if constexpr (!FP8) {
-                    if (n == 0) {
-                        load.wait_but((more ? 2 : 0) + (now + 2 < tiles ? 1 : 0));
-                        barrier();
-                    }
+                __builtin_amdgcn_sched_group_barrier(0x100, AHEAD, 0);
+#pragma unroll
+                for (int m = AHEAD; m < NKK * NB; ++m) {
+                    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                    __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
                 }
-                if (!work) continue;
+                __builtin_amdgcn_sched_group_barrier(0x008, AHEAD, 0);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            vnext = window(vpool, now + 2, page1);
+            if constexpr (!FP8) {
+                knext = window(kpool, now + 3, page2);
+                load.template wait_but<3>();
+                barrier();
+            }
+            if (work) {
                 // V operands on their way while the coefficients are formed
                 const int x = lane_now(), xq = (x & 15) >> 2;
-                const int vaddr = (32 * (kw + n) + 4 * (x >> 5) + xq) * D + 8 * ((2 * (x >> 4 & 1) + ((x & 3) >> 1)) ^ C::swz_v(xq)) + 4 * (x & 1);
-                u32x4 va[2 * NDB];
+                const int vaddr = (32 * kw + 4 * (x >> 5) + xq) * D + 8 * ((2 * (x >> 4 & 1) + ((x & 3) >> 1)) ^ C::swz_v(xq)) + 4 * (x & 1);
+                auto v_operand = [&](int n, int m) __attribute__((always_inline)) {
+                    return tile_v_operand<D>(vs, vaddr ^ 32 * (m % NDB), 32 * n + 16 * (m / NDB));
+                };
+                auto read_v = [&](u32x4 (&va)[2 * NDB], int n) __attribute__((always_inline)) {
 #pragma unroll
-                for (int m = 0; m < 2 * NDB; ++m) va[m] = tile_v_operand<D>(vs, vaddr ^ 32 * (m % NDB), 16 * (m / NDB));
-                __builtin_amdgcn_sched_barrier(0);
+                    for (int m = 0; m < 2 * NDB; ++m) va[m] = v_operand(n, m);
+                    __builtin_amdgcn_sched_barrier(0);
+                };
+                u32x4 va[NB][2 * NDB];
+                read_v(va[0], 0);
 
-                const uint32_t lost = hole >> (2 * (kw + n)) & 3u;
-                const bool masked = lost != 0 || j0 + 32 > clear;
+                const uint32_t lost = hole >> (2 * kw);
+                const bool masked = lost != 0 || j0 + 32 * NB > clear;
                 float scale = c_log2;
-                uint32_t mine = ~0u;
+                uint32_t mine[NB];
                 if (masked) {
                     const TreeRun m = args_now();
                     const int token = (int)fast_div((uint32_t)(u.first + min(32 * rw + (x & 31), u.nrows - 1)), m.group);
-                    uint32_t bits = seen_bits(m.a, u.s, token, u.s.row0 + token, j0);
-                    if (lost & 1u) bits &= 0xffff0000u;
-                    if (lost & 2u) bits &= 0x0000ffffu;
-                    mine = bits >> (4 * (x >> 5));
                     // (a scale of 0 or NaN would take a hidden key away from -inf: it is applied here)
                     const float by = c_log2 > 0.0f ? 1.0f : c_log2;
                     scale = c_log2 > 0.0f ? c_log2 : 1.0f;
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) acc[e] = if_seen(mine, 8 * (e >> 2) + (e & 3), acc[e] * by);
-                }
-                u32x4 bfrag[2];
-                top_first_pack<T, NDB, false>(acc, bfrag, st, U, scale, false, 0);
-                if (masked) {
-                    uint32_t apart = 0;
+                    for (int n = 0; n < NB; ++n) {
+                        uint32_t bits = seen_bits(m.a, u.s, token, u.s.row0 + token, j0 + 32 * n);
+                        if (lost >> (2 * n) & 1u) bits &= 0xffff0000u;
+                        if (lost >> (2 * n) & 2u) bits &= 0x0000ffffu;
+                        mine[n] = bits >> (4 * (x >> 5));
 #pragma unroll
-                    for (int m = 0; m < 2 * NDB; ++m) apart |= not_finite<T, false>(va[m]);
-                    if (__builtin_amdgcn_ballot_w64(apart != 0) != 0) {
+                        for (int e = 0; e < 16; ++e) acc[n][e] = if_seen(mine[n], 8 * (e >> 2) + (e & 3), acc[n][e] * by);
+                    }
+                }
+                u32x4 bfrag[2 * NB];
+                weigh_blocks<T, NB, NDB>(acc, bfrag, st, U, scale);
+                bool apart = false;
+                if (masked) {
+                    // (operands are read anew here, a few at a time: the registers are taken)
+                    uint32_t bad = 0;
+#pragma unroll
+                    for (int n = 0; n < NB; ++n)
+#pragma unroll
+                        for (int m = 0; m < 2 * NDB; ++m) {
+                            bad |= not_finite<T, false>(v_operand(n, m));
+                            __builtin_amdgcn_sched_barrier(0);
+                        }
+                    apart = __builtin_amdgcn_ballot_w64(bad != 0) != 0;
+                    if (apart) {
 #pragma unroll
                         for (int i = 0; i < NDB; ++i) {
                             f32x16 count;
 #pragma unroll
                             for (int e = 0; e < 16; ++e) count[e] = 0.0f;
 #pragma unroll
-                            for (int g = 0; g < 2; ++g) {
-                                const uint32_t of = mine >> (16 * g);
-                                count = Mma<T>::mfma(codes_of<T>(va[g * NDB + i]), ones_of<T>((of & 15u) | (of >> 8 & 15u) << 4), count);
-                                va[g * NDB + i] = numbers_of<T>(va[g * NDB + i]);
-                                __builtin_amdgcn_sched_barrier(0);       // few registers at a time
+                            for (int g = 0; g < 2 * NB; ++g) {
+                                const uint32_t of = mine[g >> 1] >> (16 * (g & 1));
+                                count = Mma<T>::mfma(codes_of<T>(v_operand(g >> 1, (g & 1) * NDB + i)),
+                                                     ones_of<T>((of & 15u) | (of >> 8 & 15u) << 4), count);
+                                __builtin_amdgcn_sched_barrier(0);
                             }
 #pragma unroll
                             for (int e = 0; e < 16; ++e) {
@@ -995,13 +1060,24 @@ __global__ __launch_bounds__(kTreeWaves * kWave, 2) void tree_tile_kernel(TreeRu
                     }
                 }
 #pragma unroll
-                for (int m = 0; m < 2 * NDB; ++m) U[m % NDB] = Mma<T>::mfma(va[m], bfrag[m / NDB], U[m % NDB]);
+                for (int n = 1; n < NB; ++n) read_v(va[n], n);
+                if (apart) {
+#pragma unroll
+                    for (int n = 0; n < NB; ++n)
+#pragma unroll
+                        for (int m = 0; m < 2 * NDB; ++m) va[n][m] = numbers_of<T>(va[n][m]);
+                }
+#pragma unroll
+                for (int n = 0; n < NB; ++n)
+#pragma unroll
+                    for (int m = 0; m < 2 * NDB; ++m) U[m % NDB] = Mma<T>::mfma(va[n][m], bfrag[2 * n + m / NDB], U[m % NDB]);
             }
             if constexpr (FP8) {
-                if (more) load.finish(lds + knext * kTile, vlds + ((now + 1) & 1) * kTile, wave, lane_now());
+                if (now + 1 < tiles) load.finish(lds + k1slot * kTile, vlds + ((now + 1) & 1) * kTile, wave, lane_now());
             }
-            kslot = knext;
+            kslot = k1slot;
         }
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");         // the last, empty copies: LDS is used otherwise now
         __syncthreads();
 
         // ---- rows through LDS; with KW = 2 the two states of a row are joined.  Chunk t of row c lies at t ^ c.
