@@ -21,7 +21,11 @@ typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
 // element of a half-split pair is a whole lane away and the sum of squares takes d / 8 lanes.  A
 // workgroup takes one token's rows (its q, k and v heads), so that the angles are formed once for
 // all of them.
-template <typename T, int D, bool FP8>
+//
+// PASSES: how many rows a lane's place in the workgroup takes, all loaded before anything else.  Long
+// calls want few workgroups per token (the search for its sequence and its angles are done in each of them): 12696 tokens of
+// 32 + 2 x 8 heads of 128 took 92 us with a workgroup for every 16 rows.  Short ones want the rows spread.
+template <typename T, int D, bool FP8, int PASSES>
 __global__ __launch_bounds__(256) void append_kernel(Paged c, AppendArgs a) {
     constexpr int LPR = D / 8;                  // lanes per row
     constexpr int RPP = 256 / LPR;              // rows per pass of the workgroup
@@ -31,16 +35,18 @@ __global__ __launch_bounds__(256) void append_kernel(Paged c, AppendArgs a) {
     const int t = blockIdx.x;
     const int l = tid % LPR;
     const int rows = a.Hq + 2 * c.Hkv;
-    const int row = blockIdx.y * RPP + tid / LPR;
+    const int row0 = blockIdx.y * (RPP * PASSES) + tid / LPR;
 
-    // the row of this lane; rows past the last take part in everything but the loads and stores
-    const bool is_q = row < a.Hq;
-    const bool is_k = !is_q && row < a.Hq + c.Hkv;
-    const bool is_v = !is_q && !is_k && row < rows;
-    float x[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
-    if (is_q) Store<T>::load8(a.q, (size_t)t * a.q_stride + (size_t)row * D + 8 * l, x);
-    else if (is_k) Store<T>::load8(a.k, (size_t)t * a.k_stride + (size_t)(row - a.Hq) * D + 8 * l, x);
-    else if (is_v) Store<T>::load8(a.v, (size_t)t * a.v_stride + (size_t)(row - a.Hq - c.Hkv) * D + 8 * l, x);
+    float x[PASSES][8];
+#pragma unroll
+    for (int p = 0; p < PASSES; ++p) {
+        const int row = row0 + p * RPP;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[p][e] = 0.0f;
+        if (row < a.Hq) Store<T>::load8(a.q, (size_t)t * a.q_stride + (size_t)row * D + 8 * l, x[p]);
+        else if (row < a.Hq + c.Hkv) Store<T>::load8(a.k, (size_t)t * a.k_stride + (size_t)(row - a.Hq) * D + 8 * l, x[p]);
+        else if (row < rows) Store<T>::load8(a.v, (size_t)t * a.v_stride + (size_t)(row - a.Hq - c.Hkv) * D + 8 * l, x[p]);
+    }
 
     // the token's sequence: the last one that begins at or before it
     int before = 0;
@@ -49,11 +55,12 @@ __global__ __launch_bounds__(256) void append_kernel(Paged c, AppendArgs a) {
     for (int s = 32; s > 0; s >>= 1) before += __shfl_xor(before, s);
     if ((tid & 63) == 0) part[tid >> 6] = before;
     __syncthreads();
-    const int b = part[0] + part[1] + part[2] + part[3] - 1;
+    const int b = __builtin_amdgcn_readfirstlane(part[0] + part[1] + part[2] + part[3] - 1);
     if (b < 0 || b >= c.B) return;              // rows that belong to no sequence stay as they are
     const Seq s = seq_at(c, b);
     const int i = t - s.row0;
     const int key = s.len + i;
+    const int page = (unsigned)i < (unsigned)s.n ? page_at(c, b, key >> c.page_log2) : -1;
 
     const int half = a.rot / 2;
     if (tid < half) {
@@ -66,89 +73,101 @@ __global__ __launch_bounds__(256) void append_kernel(Paged c, AppendArgs a) {
     }
     __syncthreads();
 
-    const void* wp = is_q ? a.q_weight : is_k ? a.k_weight : nullptr;
-    float sum = 0.0f;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) sum = fmaf(x[e], x[e], sum);
+    for (int p = 0; p < PASSES; ++p) {
+        const int row = row0 + p * RPP;
+        const bool is_q = row < a.Hq;
+        const bool is_k = !is_q && row < a.Hq + c.Hkv;
+        const bool turns = is_q || is_k;
+        const void* wp = is_q ? a.q_weight : is_k ? a.k_weight : nullptr;
+        if (a.q_weight != nullptr || a.k_weight != nullptr) {
+            float sum = 0.0f;
 #pragma unroll
-    for (int m = LPR / 2; m > 0; m >>= 1) sum += __shfl_xor(sum, m);
-    if (wp != nullptr) {
-        float w[8];
-        Store<T>::load8(wp, 8 * l, w);
-        const float r = 1.0f / sqrtf(sum * (1.0f / D) + a.eps);
+            for (int e = 0; e < 8; ++e) sum = fmaf(x[p][e], x[p][e], sum);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = x[e] * r * w[e];
-    }
-    if (half > 0) {
-        if (a.interleaved) {
-            if ((is_q || is_k) && 8 * l < a.rot) {
+            for (int m = LPR / 2; m > 0; m >>= 1) sum += __shfl_xor(sum, m);
+            if (wp != nullptr) {
+                float w[8];
+                Store<T>::load8(wp, 8 * l, w);
+                const float r = 1.0f / sqrtf(sum * (1.0f / D) + a.eps);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[p][e] = x[p][e] * r * w[e];
+            }
+        }
+        if (half > 0 && a.interleaved) {
+            if (turns && 8 * l < a.rot) {
 #pragma unroll
                 for (int e = 0; e < 8; e += 2) {
                     const float cv = cs[4 * l + e / 2], sv = sn[4 * l + e / 2];
-                    const float u = x[e], v = x[e + 1];
-                    x[e] = fmaf(u, cv, -(v * sv));
-                    x[e + 1] = fmaf(v, cv, u * sv);
+                    const float u = x[p][e], v = x[p][e + 1];
+                    x[p][e] = fmaf(u, cv, -(v * sv));
+                    x[p][e + 1] = fmaf(v, cv, u * sv);
                 }
             }
-        } else {
+        } else if (half > 0) {
             // rot is a multiple of 16: half a rotation is whole lanes
             const int hl = half / 8;
             const int lane = tid & 63;
             const int from = l < hl ? lane + hl : lane - hl;
             float y[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) y[e] = __shfl(x[e], from & 63);
-            if ((is_q || is_k) && l < 2 * hl) {
+            for (int e = 0; e < 8; ++e) y[e] = __shfl(x[p][e], from & 63);
+            if (turns && l < 2 * hl) {
                 const int at = 8 * (l < hl ? l : l - hl);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     const float sv = l < hl ? -sn[at + e] : sn[at + e];
-                    x[e] = fmaf(x[e], cs[at + e], y[e] * sv);
+                    x[p][e] = fmaf(x[p][e], cs[at + e], y[e] * sv);
                 }
             }
         }
-    }
 
-    if (is_q) {
-        const size_t at = (size_t)t * a.qo_stride + (size_t)row * D + 8 * l;
-        Store<T>::store4(a.q_out, at, {x[0], x[1], x[2], x[3]});
-        Store<T>::store4(a.q_out, at + 4, {x[4], x[5], x[6], x[7]});
-    } else if ((is_k || is_v) && (unsigned)i < (unsigned)s.n) {
-        const int page = page_at(c, b, key >> c.page_log2);
-        if (page < 0) return;
-        const int h = is_k ? row - a.Hq : row - a.Hq - c.Hkv;
-        char* base = (is_k ? c.k : c.v) + (size_t)page * c.page_bytes + (size_t)h * c.head_bytes;
-        const size_t at = (size_t)(key & ((1 << c.page_log2) - 1)) * D + 8 * l;
-        if constexpr (FP8) {
-            // e4m3 ends at 448: what is larger is stored as that (NaN stays NaN)
-            const float scale = is_k ? c.kscale : c.vscale;
+        if (is_q) {
+            const size_t at = (size_t)t * a.qo_stride + (size_t)row * D + 8 * l;
+            Store<T>::store4(a.q_out, at, {x[p][0], x[p][1], x[p][2], x[p][3]});
+            Store<T>::store4(a.q_out, at + 4, {x[p][4], x[p][5], x[p][6], x[p][7]});
+        } else if (row < rows && page >= 0) {
+            const int h = is_k ? row - a.Hq : row - a.Hq - c.Hkv;
+            char* base = (is_k ? c.k : c.v) + (size_t)page * c.page_bytes + (size_t)h * c.head_bytes;
+            const size_t at = (size_t)(key & ((1 << c.page_log2) - 1)) * D + 8 * l;
+            if constexpr (FP8) {
+                // e4m3 ends at 448: what is larger is stored as that (NaN stays NaN)
+                const float scale = is_k ? c.kscale : c.vscale;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                x[e] = x[e] / scale;
-                x[e] = x[e] > 448.0f ? 448.0f : x[e] < -448.0f ? -448.0f : x[e];
-            }
-            u32x2 w;
+                for (int e = 0; e < 8; ++e) {
+                    const float z = x[p][e] / scale;
+                    x[p][e] = z > 448.0f ? 448.0f : z < -448.0f ? -448.0f : z;
+                }
+                u32x2 w;
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                int p = __builtin_amdgcn_cvt_pk_fp8_f32(x[4 * e], x[4 * e + 1], 0, false);
-                p = __builtin_amdgcn_cvt_pk_fp8_f32(x[4 * e + 2], x[4 * e + 3], p, true);
-                w[e] = (unsigned)p;
+                for (int e = 0; e < 2; ++e) {
+                    int z = __builtin_amdgcn_cvt_pk_fp8_f32(x[p][4 * e], x[p][4 * e + 1], 0, false);
+                    z = __builtin_amdgcn_cvt_pk_fp8_f32(x[p][4 * e + 2], x[p][4 * e + 3], z, true);
+                    w[e] = (unsigned)z;
+                }
+                *reinterpret_cast<u32x2*>(base + at) = w;
+            } else {
+                Store<T>::store4(base, at, {x[p][0], x[p][1], x[p][2], x[p][3]});
+                Store<T>::store4(base, at + 4, {x[p][4], x[p][5], x[p][6], x[p][7]});
             }
-            *reinterpret_cast<u32x2*>(base + at) = w;
-        } else {
-            Store<T>::store4(base, at, {x[0], x[1], x[2], x[3]});
-            Store<T>::store4(base, at + 4, {x[4], x[5], x[6], x[7]});
         }
     }
 }
 
+template <typename T, int D, bool FP8>
+static hipError_t launch_append_d(const Paged& c, const AppendArgs& a, hipStream_t st) {
+    const int rows = a.Hq + 2 * c.Hkv, per = 256 / (D / 8), passes = (rows + per - 1) / per;
+    const dim3 block(256);
+    // a workgroup per token and 16 (32 at d = 64) rows until that fills the chip with two workgroups per compute unit
+    if ((long)c.T * passes <= 512) hipLaunchKernelGGL((append_kernel<T, D, FP8, 1>), dim3((unsigned)c.T, (unsigned)passes), block, 0, st, c, a);
+    else if (passes <= 2) hipLaunchKernelGGL((append_kernel<T, D, FP8, 2>), dim3((unsigned)c.T, 1), block, 0, st, c, a);
+    else if (passes <= 3) hipLaunchKernelGGL((append_kernel<T, D, FP8, 3>), dim3((unsigned)c.T, 1), block, 0, st, c, a);
+    else hipLaunchKernelGGL((append_kernel<T, D, FP8, 4>), dim3((unsigned)c.T, (unsigned)((passes + 3) / 4)), block, 0, st, c, a);
+    return hipGetLastError();
+}
 template <typename T, bool FP8>
 static hipError_t launch_append_t(const Paged& c, const AppendArgs& a, hipStream_t st) {
-    const int rows = a.Hq + 2 * c.Hkv, per = 256 / (c.d / 8);
-    const dim3 grid((unsigned)c.T, (unsigned)((rows + per - 1) / per)), block(256);
-    if (c.d == 64) hipLaunchKernelGGL((append_kernel<T, 64, FP8>), grid, block, 0, st, c, a);
-    else hipLaunchKernelGGL((append_kernel<T, 128, FP8>), grid, block, 0, st, c, a);
-    return hipGetLastError();
+    return c.d == 64 ? launch_append_d<T, 64, FP8>(c, a, st) : launch_append_d<T, 128, FP8>(c, a, st);
 }
 
 hipError_t launch_cache_append(const Paged& c, const AppendArgs& a, hipStream_t st) {
@@ -230,76 +249,80 @@ __device__ __forceinline__ int block_scan(int x, int* waves, int& total) {
 __global__ __launch_bounds__(kReserveThreads) void reserve_kernel(Paged c, int* refs, int* report) {
     __shared__ int at[kCacheMaxSeqs + 1];        // wanted pages of the sequences before b
     __shared__ int last[kCacheMaxSeqs];          // part-filled last page of a sequence that grows, or -1
-    __shared__ int count[kReserveBlocks];        // free pages of the blocks before, from `first` on
+    __shared__ int2 cols[kCacheMaxSeqs];         // that page's column (with kCopy: a copy is wanted), and the column behind the last
+    __shared__ int count[kReserveBlocks];        // free pages of the blocks before
     __shared__ int waves[kReserveWaves];
+    __shared__ int beyond;
+    constexpr int kCopy = 1 << 30;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int mask = (1 << c.page_log2) - 1;
+    const int each = (c.B + kReserveThreads - 1) / kReserveThreads;
+    if (tid == 0) beyond = 0;
 
     // 1. back to the pool
-    for (int b = tid; b < c.B; b += kReserveThreads) {
+    for (int k = 0; k < each; ++k) {
+        const int b = k * kReserveThreads + tid;
+        if (b >= c.B) break;
         const Seq s = seq_at(c, b);
         int* row = c.table + (size_t)b * c.max_pages;
-        const int len = s.len, end = (len + s.n + mask) >> c.page_log2;
+        const int end = (s.len + s.n + mask) >> c.page_log2;
+        const int part = s.n > 0 && (s.len & mask) != 0 ? page_at(c, b, s.len >> c.page_log2) : -1;
         for (int col = end; col < c.max_pages; ++col) {
             const int p = row[col];
             if (p < 0) break;                    // owned pages come first in a row
             row[col] = -1;
             if (p < c.P) atomicSub(&refs[p], 1);
         }
-        last[b] = s.n > 0 && (len & mask) != 0 ? page_at(c, b, len >> c.page_log2) : -1;
+        last[b] = part;
+        cols[b] = int2{s.len >> c.page_log2, end};
     }
-    // what follows sees refs as these atomics leave them, not what a load has put into the compute
-    // unit's cache before
-    __threadfence();
+    // (refs have not been read yet, so what follows finds them as these atomics, waited for at the barrier,
+    // have left them)
+    __builtin_amdgcn_s_waitcnt(0);
     __syncthreads();
-    __threadfence();
 
     // 2. what each wants
-    int run = 0, beyond = 0;
-    for (int b0 = 0; b0 < c.B; b0 += kReserveThreads) {
-        const int b = b0 + tid;
-        int want = 0, past = 0;
+    int run = 0;
+    for (int k = 0; k < each; ++k) {
+        const int b = k * kReserveThreads + tid;
+        int want = 0;
+        bool copy = false;
         if (b < c.B) {
             const Seq s = seq_at(c, b);
             const int tokens = max(min(c.q_start[b + 1], c.T) - s.row0, 0);
             // tokens that the table has no columns for
-            past = (tokens - s.n + mask) >> c.page_log2;
+            if (tokens > s.n) atomicAdd(&beyond, (tokens - s.n + mask) >> c.page_log2);
             const int* row = c.table + (size_t)b * c.max_pages;
-            const int end = (s.len + s.n + mask) >> c.page_log2;
-            int lo = min((s.len + mask) >> c.page_log2, end), hi = end;
-            if (s.n == 0) lo = end;
-            if (lo < hi && row[lo] < 0) hi = lo;
-            else if (lo < hi && row[hi - 1] >= 0) lo = hi;
+            const int end = cols[b].y, p = last[b];
+            const int refs_p = p >= 0 ? refs[p] : 0;
+            int lo = s.n == 0 ? end : min((s.len + mask) >> c.page_log2, end), hi = end;
+            if (lo < hi) {
+                const int first = row[lo], behind = row[hi - 1];
+                if (first < 0) hi = lo;
+                else if (behind >= 0) lo = hi;
+            }
             while (lo < hi) {                    // the first empty column
                 const int mid = (lo + hi) >> 1;
                 if (row[mid] < 0) hi = mid;
                 else lo = mid + 1;
             }
             want = end - lo;
-            const int p = last[b];
-            if (p >= 0) {
-                const int refs_p = refs[p];
-                if (refs_p > 1) {
-                    int holders = 0, before = 0;
-                    for (int o = 0; o < c.B; ++o) {
-                        const bool same = last[o] == p;
-                        holders += same ? 1 : 0;
-                        before += same && o < b ? 1 : 0;
-                    }
-                    if (holders < refs_p || before > 0) want |= 1 << 30;    // and a copy
+            if (refs_p > 1) {
+                int holders = 0, before = 0;
+                for (int o = 0; o < c.B; ++o) {
+                    const bool same = last[o] == p;
+                    holders += same ? 1 : 0;
+                    before += same && o < b ? 1 : 0;
                 }
+                copy = holders < refs_p || before > 0;
             }
+            report[1 + b] = copy ? p : -1;
+            if (copy) cols[b].x |= kCopy;
         }
-        const int mine = (want & 0x3fffffff) + (want >> 30);
         int all;
-        const int ex = block_scan(mine, waves, all);
-        if (b < c.B) {
-            at[b] = run + ex;
-            report[1 + b] = want >> 30 ? last[b] : -1;
-        }
+        const int ex = block_scan(want + (copy ? 1 : 0), waves, all);
+        if (b < c.B) at[b] = run + ex;
         run += all;
-        block_scan(past, waves, all);
-        beyond += all;
     }
     if (tid == 0) at[c.B] = run;
 
@@ -308,9 +331,15 @@ __global__ __launch_bounds__(kReserveThreads) void reserve_kernel(Paged c, int* 
     const int blocks = (c.P + 256 * m - 1) / (256 * m);
     for (int k = wave; k < blocks; k += kReserveWaves) {
         int n = 0;
-        for (int j = 0; j < 4 * m; ++j) {
-            const int p = k * 256 * m + 64 * j + lane;
-            n += __popcll(__ballot(p < c.P && refs[p] == 0));
+        for (int j = 0; j < 4 * m; j += 4) {
+            bool is[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int p = k * 256 * m + 64 * (j + i) + lane;
+                is[i] = p < c.P && refs[p] == 0;
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) n += __popcll(__ballot(is[i]));
         }
         if (lane == 0) count[k] = n;
     }
@@ -346,13 +375,11 @@ __global__ __launch_bounds__(kReserveThreads) void reserve_kernel(Paged c, int* 
                     if (at[mid] <= mine) lo = mid;
                     else hi = mid;
                 }
-                const Seq s = seq_at(c, lo);
-                int* row = c.table + (size_t)lo * c.max_pages;
-                const int end = (s.len + s.n + mask) >> c.page_log2;
-                const int left = at[lo + 1] - mine;          // wanted pages from this one to the last
-                const bool copied = mine == at[lo] && report[1 + lo] >= 0;
+                const int2 to = cols[lo];
+                const bool copied = mine == at[lo] && (to.x & kCopy) != 0;
                 if (copied) atomicSub(&refs[last[lo]], 1);
-                row[copied ? s.len >> c.page_log2 : end - left] = p;
+                // (of the fresh pages the last one goes to the last column)
+                c.table[(size_t)lo * c.max_pages + (copied ? to.x & (kCopy - 1) : to.y - (at[lo + 1] - mine))] = p;
                 refs[p] = 1;
             }
             rank += __popcll(all);
@@ -400,6 +427,8 @@ __global__ __launch_bounds__(256) void commit_kernel(Paged c, const int* keep, i
                                                      const int* n_keep, int* lens_out) {
     constexpr int LPR = RB / 16;                  // lanes per row
     constexpr int GROUP = kWave / LPR;            // rows per load
+    constexpr int GROUPS = GROUP >= 8 ? 1 : GROUP >= 4 ? 2 : 4;     // loads of a piece under way
+    constexpr int PIECES = 4 / GROUPS * 2;        // pieces under way
     const int b = blockIdx.x;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const Seq s = seq_at(c, b);
@@ -426,25 +455,42 @@ __global__ __launch_bounds__(256) void commit_kernel(Paged c, const int* keep, i
     if (blockIdx.y == 0 && threadIdx.x == 0) lens_out[b] = s.len + kept;
     if (keep == nullptr) return;
 
+    // Where the rows of a group lie is the same in every piece.
     const int mask = (1 << c.page_log2) - 1;
-    for (int j = blockIdx.y * 4 + wave; j < 2 * c.layers * c.Hkv; j += 4 * gridDim.y) {
-        const int h = j % c.Hkv, layer = j / c.Hkv >> 1;
-        char* base = (j / c.Hkv & 1 ? c.v : c.k) + (size_t)layer * c.layer_bytes + (size_t)h * c.head_bytes;
-        for (int i0 = 0; i0 < kept; i0 += GROUP) {
-            const int i = i0 + lane / LPR;
-            bool ok = i < kept;
-            const int from = ok ? list[i] : 0;
-            ok = ok && from != i;
-            const int sk = s.len + from, dk = s.len + i;
-            const int sp = ok ? page_at(c, b, sk >> c.page_log2) : -1, dp = ok ? page_at(c, b, dk >> c.page_log2) : -1;
-            ok = sp >= 0 && dp >= 0;
-            u32x4 x = {0u, 0u, 0u, 0u};
-            if (ok)
-                x = *reinterpret_cast<const u32x4*>(base + (size_t)sp * c.page_bytes + (size_t)(sk & mask) * RB + 16 * (lane % LPR));
+    const int all = 2 * c.layers * c.Hkv;
+    const int first = blockIdx.y * 4 + wave, step = 4 * gridDim.y;
+    for (int i0 = 0; i0 < kept; i0 += GROUP * GROUPS) {
+        int64_t from[GROUPS], to[GROUPS];
+        bool moves[GROUPS];
+#pragma unroll
+        for (int g = 0; g < GROUPS; ++g) {
+            const int i = i0 + g * GROUP + lane / LPR;
+            const int x = i < kept ? list[i] : i;
+            const int sk = s.len + x, dk = s.len + i;
+            const int sp = x != i ? page_at(c, b, sk >> c.page_log2) : -1, dp = x != i ? page_at(c, b, dk >> c.page_log2) : -1;
+            moves[g] = sp >= 0 && dp >= 0;
+            from[g] = (int64_t)sp * c.page_bytes + (sk & mask) * RB + 16 * (lane % LPR);
+            to[g] = (int64_t)dp * c.page_bytes + (dk & mask) * RB + 16 * (lane % LPR);
+        }
+        for (int j0 = first; j0 < all; j0 += PIECES * step) {
+            u32x4 x[PIECES][GROUPS];
+            char* base[PIECES];
+#pragma unroll
+            for (int k = 0; k < PIECES; ++k) {
+                const int j = j0 + k * step;
+                const int h = j % c.Hkv, layer = j / c.Hkv >> 1;
+                base[k] = (j / c.Hkv & 1 ? c.v : c.k) + (size_t)layer * c.layer_bytes + (size_t)h * c.head_bytes;
+#pragma unroll
+                for (int g = 0; g < GROUPS; ++g)
+                    if (j < all && moves[g]) x[k][g] = *reinterpret_cast<const u32x4*>(base[k] + from[g]);
+            }
             // the wavefront's loads have all returned before the first of its stores is issued
             asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-            if (ok)
-                *reinterpret_cast<u32x4*>(base + (size_t)dp * c.page_bytes + (size_t)(dk & mask) * RB + 16 * (lane % LPR)) = x;
+#pragma unroll
+            for (int k = 0; k < PIECES; ++k)
+#pragma unroll
+                for (int g = 0; g < GROUPS; ++g)
+                    if (j0 + k * step < all && moves[g]) *reinterpret_cast<u32x4*>(base[k] + to[g]) = x[k][g];
         }
     }
 }
@@ -452,8 +498,10 @@ __global__ __launch_bounds__(256) void commit_kernel(Paged c, const int* keep, i
 hipError_t launch_cache_commit(const Paged& c, const int* keep, int max_keep, const int* n_keep,
                                int* lens_out, hipStream_t st) {
     const long pieces = 2L * c.layers * c.Hkv;
-    long y = keep == nullptr ? 1 : (pieces + 3) / 4;
-    if (y > 256) y = 256;
+    // four wavefronts a workgroup, two rounds of their pieces each, unless that leaves compute units without work
+    long y = keep == nullptr ? 1 : (pieces + 31) / 32;
+    if (keep != nullptr && y * c.B < 512) y = (512 + c.B - 1) / c.B;
+    if (keep != nullptr && y > (pieces + 3) / 4) y = (pieces + 3) / 4;
     const dim3 grid((unsigned)c.B, (unsigned)y), block(256);
     switch (c.d * c.esz) {
     case 64: hipLaunchKernelGGL(commit_kernel<64>, grid, block, 0, st, c, keep, max_keep, n_keep, lens_out); break;

@@ -25,7 +25,7 @@ namespace flashd {
 
 constexpr int kTreeBlock = 32;          // keys of a block: a wavefront's step
 constexpr int kTreeWaves = 4;
-constexpr int kTreeMostGroups = 512;    // workgroups of a launch, two per compute unit
+constexpr int kTreeMostGroups = 768;    // workgroups of a launch, three per compute unit (see rows_per_cu) or two
 constexpr int kTreeMinBlocks = 4;       // blocks a workgroup takes at least
 
 template <typename T> struct Mma16;
@@ -489,8 +489,12 @@ __device__ __forceinline__ float if_seen(uint32_t bits, int i, float x) {
     return __uint_as_float((m & __float_as_uint(x)) | (~m & 0xff800000u));
 }
 
+// Workgroups per compute unit: what one has under way is its wavefronts' next block of K and of V.  Of fp8, or at
+// d = 64, that is half as much, and three workgroups' registers fit.
+constexpr int rows_per_cu(int D, bool FP8, int NR) { return (D == 64 || FP8) && NR == 1 ? 3 : 2; }
+
 template <typename T, int D, bool FP8, int NR>
-__global__ __launch_bounds__(kTreeWaves * kWave, 2) void tree_rows_kernel(TreeRun r) {
+__global__ __launch_bounds__(kTreeWaves * kWave, rows_per_cu(D, FP8, NR)) void tree_rows_kernel(TreeRun r) {
     constexpr int W = kTreeWaves;
     constexpr int NKK = D / 32;
     constexpr int NDB = D / 16;
@@ -706,17 +710,31 @@ __device__ __forceinline__ int lane_now() {
     asm volatile("v_mbcnt_lo_u32_b32 %0, -1, 0\n\tv_mbcnt_hi_u32_b32 %0, -1, %0" : "=v"(x));
     return x;
 }
-template <typename T, int D, bool FP8> struct TileLoader;
+template <typename T, int D, bool FP8, bool ONCE> struct TileLoader;
 
 // straight from global memory to LDS
-template <typename T, int D> struct TileLoader<T, D, false> {
+template <typename T, int D, bool ONCE> struct TileLoader<T, D, false, ONCE> {
     // A wavefront's copies of a tile of K or V, 1 KB each (the immediate offset counts on both sides).  M0 holds the
     // target; one wait state has to pass between writing it and the copy.  It is left as it was.
     static constexpr int NI = DmaLane<D>::NI;
     __device__ __forceinline__ void copy(const Window& w, uint16_t* to, int wave, uint32_t o0, uint32_t o1, uint32_t o2, uint32_t o3) {
         const uint32_t at = lds_address(to) + 1024 * NI * wave;
         uint32_t m0;
-        if constexpr (NI == 4)
+        if constexpr (NI == 4 && ONCE)
+            asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %6\n\ts_nop 0\n\t"
+                         "buffer_load_dwordx4 %1, %5, 0 offen nt lds\n\t"
+                         "buffer_load_dwordx4 %2, %5, 0 offen offset:1024 nt lds\n\t"
+                         "buffer_load_dwordx4 %3, %5, 0 offen offset:2048 nt lds\n\t"
+                         "buffer_load_dwordx4 %4, %5, 0 offen offset:3072 nt lds\n\t"
+                         "s_mov_b32 m0, %0"
+                         : "=&s"(m0) : "v"(o0), "v"(o1), "v"(o2), "v"(o3), "s"(w.words), "s"(at) : "memory");
+        else if constexpr (NI == 2 && ONCE)
+            asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %4\n\ts_nop 0\n\t"
+                         "buffer_load_dwordx4 %1, %3, 0 offen nt lds\n\t"
+                         "buffer_load_dwordx4 %2, %3, 0 offen offset:1024 nt lds\n\t"
+                         "s_mov_b32 m0, %0"
+                         : "=&s"(m0) : "v"(o0), "v"(o1), "s"(w.words), "s"(at) : "memory");
+        else if constexpr (NI == 4)
             asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %6\n\ts_nop 0\n\t"
                          "buffer_load_dwordx4 %1, %5, 0 offen lds\n\t"
                          "buffer_load_dwordx4 %2, %5, 0 offen offset:1024 lds\n\t"
@@ -748,7 +766,7 @@ template <typename T, int D> struct TileLoader<T, D, false> {
 };
 
 // fp8: through registers, widened on the way
-template <typename T, int D> struct TileLoader<T, D, true> {
+template <typename T, int D, bool ONCE> struct TileLoader<T, D, true, ONCE> {
     static constexpr int NI = D / 64;           // 1 KB each: 16 rows of D bytes
     static constexpr int LPR = D / 16;
     u32x4 k[NI], v[NI];
@@ -842,7 +860,7 @@ __global__ __launch_bounds__(kTreeWaves * kWave, 2) void tree_tile_kernel(TreeRu
     u.begin(args_now(), reinterpret_cast<WalkScratch*>(lds));
     if (u.at >= u.end) return;
 
-    TileLoader<T, D, FP8> load;
+    TileLoader<T, D, FP8, RW == 2> load;        // (up to 64 rows a sequence is one row tile: its keys are read once)
 
     do {
         const TreeRun now_r = args_now();
@@ -1364,15 +1382,15 @@ size_t attn_tree_workspace(int Hq, int Hkv, int max_q, int d, int dtype) {
 
 template <typename T, int D, int M>
 static hipError_t launch_tree_m(TreeRun& r, hipStream_t st) {
-    const dim3 grid(kTreeMostGroups), block(kTreeWaves * kWave);
+    const dim3 grid(512), block(kTreeWaves * kWave);
     r.stats = reinterpret_cast<float2*>(r.parts + (size_t)2 * kTreeMostGroups * M * D);
     r.splits = reinterpret_cast<TreeSplit*>(r.stats + (size_t)2 * kTreeMostGroups * M);
     r.groups = reinterpret_cast<int*>(r.splits + kTreeMostGroups);
     if constexpr (std::is_same_v<T, F32>) {
         hipLaunchKernelGGL((tree_rows_f32_kernel<D>), grid, block, 0, st, r);
     } else if constexpr (M <= 32) {
-        if (r.a.fp8) hipLaunchKernelGGL((tree_rows_kernel<T, D, true, M / 16>), grid, block, 0, st, r);
-        else hipLaunchKernelGGL((tree_rows_kernel<T, D, false, M / 16>), grid, block, 0, st, r);
+        if (r.a.fp8) hipLaunchKernelGGL((tree_rows_kernel<T, D, true, M / 16>), dim3(256 * rows_per_cu(D, true, M / 16)), block, 0, st, r);
+        else hipLaunchKernelGGL((tree_rows_kernel<T, D, false, M / 16>), dim3(256 * rows_per_cu(D, false, M / 16)), block, 0, st, r);
     } else {
         if (r.a.fp8) hipLaunchKernelGGL((tree_tile_kernel<T, D, true, M / 32>), grid, block, 0, st, r);
         else hipLaunchKernelGGL((tree_tile_kernel<T, D, false, M / 32>), grid, block, 0, st, r);

@@ -115,6 +115,7 @@ except ImportError as e:
     class _native:
         """Stands in for the native part: leaves every call to the Python form."""
         bind = attn_fwd = attn_fwd_kv8 = attn_fwd_state = staticmethod(lambda *args: None)
+        bind_paged = cache_fork = cache_reserve = cache_append = attn_fwd_tree = cache_commit = bind
 
 
 def raw() -> ctypes.CDLL:
@@ -395,9 +396,26 @@ def _ptr(t):
     return None if t is None else t.data_ptr()
 
 
+# The native forms of the five functions below, as of the three above.
+_native.bind_paged(*(ctypes.cast(f, ctypes.c_void_p).value
+                     for f in (_lib.flashd_cache_fork, _lib.flashd_cache_reserve, _lib.flashd_cache_append,
+                               _lib.flashd_attn_fwd_tree, _lib.flashd_cache_commit)))
+
+
+def _taken(rc) -> bool:
+    """Whether a native form has made the call; raises on a status other than 0."""
+    if rc is None:
+        return False
+    if rc != 0:
+        raise FlashdError(rc)
+    return True
+
+
 def cache_fork(parent, refs, table, lens, table_out, lens_out, stream=None) -> None:
     """flashd_cache_fork: sequence i of table_out [B_out, max_pages] and lens_out goes on where
     sequence parent[i] of table and lens ended (empty if that is none); refs follows."""
+    if stream is None and _taken(_native.cache_fork(parent, refs, table, lens, table_out, lens_out)):
+        return
     if not table.is_cuda:
         raise ValueError("table must live on the GPU")
     device = table.get_device()
@@ -419,6 +437,8 @@ def cache_reserve(kcache, vcache, refs, table, lens, q_start, report, stream=Non
     """flashd_cache_reserve: every sequence gets exactly the pages of its keys and new tokens.
     `report`: int32 [1 + B], receives the number of pages missing (0: all went well) and for each
     sequence the page that its shared last page was copied from, or -1."""
+    if stream is None and _taken(_native.cache_reserve(kcache, vcache, refs, table, lens, q_start, report)):
+        return
     c = _cache(kcache, vcache, table, lens, layers=True)
     device = kcache.get_device()
     _ints("refs", refs, (c.P,), device)
@@ -435,6 +455,9 @@ def cache_append(q, k, v, q_out, kcache, vcache, table, lens, q_start, positions
     the pages of one layer's cache.  q, k and v may be slices of one projection's output.  Without
     weights nothing is normed, without inv_freq (float32 [rot / 2]) nothing is rotated; positions
     (int32 [T]) default to the tokens' key numbers."""
+    if stream is None and _taken(_native.cache_append(q, k, v, q_out, kcache, vcache, table, lens, q_start, positions, inv_freq, q_weight, k_weight,
+                                                      eps, interleaved, kscale, vscale)):
+        return
     c = _cache(kcache, vcache, table, lens, kscale, vscale)
     device = kcache.get_device()
     if q.dim() != 3 or q.dtype not in _DTYPE:
@@ -477,6 +500,9 @@ def attn_fwd_tree(q, kcache, vcache, o, table, lens, q_start, max_q: int, scale:
     each; without it token i sees tokens 0 .. i.  max_q: the most new tokens of a sequence (a hint).
     `workspace`: a contiguous tensor of at least tree_workspace_bytes(...) bytes; without it scratch
     memory is kept per stream."""
+    if stream is None and _taken(_native.attn_fwd_tree(q, kcache, vcache, o, table, lens, q_start, max_q, scale, tree, kscale, vscale,
+                                                       workspace)):
+        return
     c = _cache(kcache, vcache, table, lens, kscale, vscale)
     device = kcache.get_device()
     if q.dim() != 3 or q.dtype not in _DTYPE:
@@ -508,6 +534,8 @@ def cache_commit(kcache, vcache, table, lens, q_start, lens_out, keep=None, n_ke
     """flashd_cache_commit: the tokens that keep (int32 [B, max_keep], ascending) names move together
     behind their sequence's keys, in every layer; lens_out [B] <- lens + n_keep.  Without `keep` the
     first n_keep new tokens stay, without n_keep all."""
+    if stream is None and _taken(_native.cache_commit(kcache, vcache, table, lens, q_start, lens_out, keep, n_keep)):
+        return
     c = _cache(kcache, vcache, table, lens, layers=True)
     device = kcache.get_device()
     _ints("q_start", q_start, (c.B + 1,), device)
