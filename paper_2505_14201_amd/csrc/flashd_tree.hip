@@ -400,6 +400,10 @@ struct Window {
     }
 };
 
+__device__ __forceinline__ Window make_window(uint64_t at, int bytes) {
+    return Window{u32x4{(uint32_t)uniform((int)at), (uint32_t)uniform((int)(at >> 32)), (uint32_t)uniform(bytes), 0x00020000u}};
+}
+
 // 16 keys of a block: their bytes up to the sequence's last key, or nothing without a page.
 template <class W>
 __device__ __forceinline__ Window half_window(const Paged& c, const W& u, const char* pool, int page, int key) {
@@ -407,7 +411,7 @@ __device__ __forceinline__ Window half_window(const Paged& c, const W& u, const 
     const uint64_t at = (uint64_t)(pool + (int64_t)max(page, 0) * c.page_bytes + u.h * c.head_bytes +
                                    (int64_t)(key & ((1 << c.page_log2) - 1)) * row);
     const int keys = page < 0 ? 0 : min(16, u.keys() - key);
-    return Window{u32x4{(uint32_t)uniform((int)at), (uint32_t)uniform((int)(at >> 32)), (uint32_t)uniform(max(keys, 0) * row), 0x00020000u}};
+    return make_window(at, max(keys, 0) * row);
 }
 
 // ---- 16 rows, keys shared out over the wavefronts (f16 / bf16) -----------------------------------
@@ -508,8 +512,7 @@ __global__ __launch_bounds__(kTreeWaves * kWave, rows_per_cu(D, FP8, NR)) void t
     constexpr int kLds = 2 * W * STAGE > 4 * W * 16 * FROW ? 2 * W * STAGE : 4 * W * 16 * FROW;
     __shared__ __align__(16) char lds[kLds];
 
-    const Paged& c = r.c;
-    const TreeArgs& a = r.a;
+    (void)r;                                             // read through args_now()
     const int tid = threadIdx.x;
     const int lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -519,29 +522,49 @@ __global__ __launch_bounds__(kTreeWaves * kWave, rows_per_cu(D, FP8, NR)) void t
     uint16_t* vs = reinterpret_cast<uint16_t*>(lds) + wave * STAGE;
 
     Walk<16 * NR, kTreeBlock> u;
-    u.begin(r, reinterpret_cast<WalkScratch*>(lds));
+    u.begin(args_now(), reinterpret_cast<WalkScratch*>(lds));
     if (u.at >= u.end) return;
     do {
         // the query rows of this lane's column; columns past the last row stand in for it
-        int token[NR];
+        const TreeRun now_r = args_now();
         u32x4 qf[NR][NKK];
 #pragma unroll
         for (int k = 0; k < NR; ++k) {
             const int row = u.first + min(16 * k + col, u.nrows - 1);
-            token[k] = (int)fast_div((uint32_t)row, r.group);
-            const uint16_t* qg = static_cast<const uint16_t*>(a.q) + row_at(r, u, row, a.q_stride, D);
+            const uint16_t* qg = static_cast<const uint16_t*>(now_r.a.q) + row_at(now_r, u, row, now_r.a.q_stride, D);
 #pragma unroll
             for (int kk = 0; kk < NKK; ++kk) qf[k][kk] = *reinterpret_cast<const u32x4*>(qg + 32 * kk + 8 * q);
         }
         // Here before the loop, as the compiler knows: in every turn of it, it would else wait for them, and so for the keys
         // under way.
         wait_copies();
-        const float c_log2 = (FP8 ? a.scale * c.kscale : a.scale) * kLog2e;
+        const float c_log2 = (FP8 ? now_r.a.scale * now_r.c.kscale : now_r.a.scale) * kLog2e;
 
+        // What the loop needs of the arguments, each in a register of its own (see tree_tile_kernel).
+        constexpr int ROWB = D * ESZ;
+        const char* kpool = now_r.c.k + u.h * now_r.c.head_bytes;
+        const char* vpool = now_r.c.v + u.h * now_r.c.head_bytes;
+        int64_t page_bytes = now_r.c.page_bytes;
+        int page_log2 = now_r.c.page_log2, pool_pages = now_r.c.P, last_key = u.keys(), blk_end = u.blk1, len = u.s.len;
+        typedef const __attribute__((address_space(4))) int* table_ptr;
+        table_ptr trow = (table_ptr)(uintptr_t)(now_r.c.table + (size_t)u.b * now_r.c.max_pages);
+        asm volatile("" : "+s"(kpool), "+s"(vpool), "+s"(page_bytes), "+s"(page_log2), "+s"(pool_pages), "+s"(last_key),
+                          "+s"(blk_end), "+s"(len), "+s"(trow));
+        // page of a half of a block, by a scalar load; -1 behind the piece and behind the last key
+        auto page_of = [&](int blk, int half) __attribute__((always_inline)) {
+            const int key = blk * kTreeBlock + 16 * half;
+            const int p = blk < blk_end && key < last_key ? trow[key >> page_log2] : -1;
+            return (unsigned)p < (unsigned)pool_pages ? p : -1;
+        };
+        // (Always issued, with an empty window where there is nothing to fetch: with a branch around it the compiler could
+        // not count the loads under way, and waited for the next block's K before it used this one's V.)
         auto fetch = [&](const char* pool, u32x4 (&reg)[NV], int blk, int p0, int p1) __attribute__((always_inline)) {
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
-                const auto w = half_window(c, u, pool, half ? p1 : p0, blk * kTreeBlock + 16 * half).rsrc();
+                const int p = half ? p1 : p0, key = blk * kTreeBlock + 16 * half;
+                const uint64_t at = (uint64_t)(pool + max(p, 0) * page_bytes + (key & ((1 << page_log2) - 1)) * ROWB);
+                const int left = last_key - key, keys = p < 0 || left < 0 ? 0 : left < 16 ? left : 16;
+                const auto w = make_window(at, keys * ROWB).rsrc();
 #pragma unroll
                 for (int n = 0; n < NV / 2; ++n) reg[half * (NV / 2) + n] = kv_load<2>(w, 1024 * n + 16 * lane);
             }
@@ -577,28 +600,22 @@ __global__ __launch_bounds__(kTreeWaves * kWave, rows_per_cu(D, FP8, NR)) void t
             for (int i = 0; i < NDB; ++i) U[k][i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
         }
 
-        PageWindow pages{-1, -1};
         u32x4 kreg[NV], vreg[NV];
-        int p0 = -1, p1 = -1;
         int blk = u.blk0 + wave;
-        if (blk < u.blk1) {
-            p0 = pages.at(c, u, wave, lane, blk, 0);
-            p1 = pages.at(c, u, wave, lane, blk, 1);
-            fetch(c.k, kreg, blk, p0, p1);
-            fetch(c.v, vreg, blk, p0, p1);
-        }
-        for (; blk < u.blk1; blk += W) {
+        int p0 = page_of(blk, 0), p1 = page_of(blk, 1), n0 = page_of(blk + W, 0), n1 = page_of(blk + W, 1);
+        // K before V, as in the loop: mixed, the wait for K would be one for V
+        __builtin_amdgcn_sched_barrier(0);
+        fetch(kpool, kreg, blk, p0, p1);
+        __builtin_amdgcn_sched_barrier(0);
+        fetch(vpool, vreg, blk, p0, p1);
+        __builtin_amdgcn_sched_barrier(0);
+        for (; blk < blk_end; blk += W) {
             const int j0 = blk * kTreeBlock;
-            const bool more = blk + W < u.blk1;
             // a half without a page, or behind the last key, has no keys
             const uint32_t have = (p0 < 0 ? 0u : 0x0000ffffu) | (p1 < 0 ? 0u : 0xffff0000u);
-            int n0 = -1, n1 = -1;
-            if (more) {
-                n0 = pages.at(c, u, wave, lane, blk + W, 0);
-                n1 = pages.at(c, u, wave, lane, blk + W, 1);
-            }
+            const int m0 = page_of(blk + 2 * W, 0), m1 = page_of(blk + 2 * W, 1);
             stage(kreg, KROW);
-            if (more) fetch(c.k, kreg, blk + W, n0, n1);
+            fetch(kpool, kreg, blk + W, n0, n1);
             f32x4 acc[NR][2];
 #pragma unroll
             for (int k = 0; k < NR; ++k)
@@ -614,7 +631,7 @@ __global__ __launch_bounds__(kTreeWaves * kWave, rows_per_cu(D, FP8, NR)) void t
                 }
             stage_done();
             stage(vreg, VROW);
-            const bool masked = have != ~0u || j0 + kTreeBlock > u.s.len;
+            const bool masked = have != ~0u || j0 + kTreeBlock > len;
             bool apart = false;
             if (masked) {
                 uint32_t bad = 0;
@@ -622,14 +639,18 @@ __global__ __launch_bounds__(kTreeWaves * kWave, rows_per_cu(D, FP8, NR)) void t
                 for (int n = 0; n < NV; ++n) bad |= not_finite<T, FP8>(vreg[n]);
                 apart = __builtin_amdgcn_ballot_w64(bad != 0) != 0;
             }
-            if (more) fetch(c.v, vreg, blk + W, n0, n1);
+            fetch(vpool, vreg, blk + W, n0, n1);
 
             u32x4 bfrag[NR];
             uint32_t bits[NR];
 #pragma unroll
             for (int k = 0; k < NR; ++k) {
                 bits[k] = ~0u;
-                if (masked) bits[k] = have & seen_bits(a, u.s, token[k], u.s.row0 + token[k], j0);
+                if (masked) {
+                    const TreeRun m = args_now();
+                    const int token = (int)fast_div((uint32_t)(u.first + min(16 * k + col, u.nrows - 1)), m.group);
+                    bits[k] = have & seen_bits(m.a, u.s, token, u.s.row0 + token, j0);
+                }
                 float x[8];
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
@@ -684,9 +705,12 @@ __global__ __launch_bounds__(kTreeWaves * kWave, rows_per_cu(D, FP8, NR)) void t
             stage_done();
             p0 = n0;
             p1 = n1;
+            n0 = m0;
+            n1 = m1;
         }
-        finish_rows<T, D, NR>(r, u, U, R, l, reinterpret_cast<float*>(lds), FP8 ? c.vscale : 1.0f);
-    } while (u.next(r));
+        const TreeRun end_r = args_now();
+        finish_rows<T, D, NR>(end_r, u, U, R, l, reinterpret_cast<float*>(lds), FP8 ? end_r.c.vscale : 1.0f);
+    } while (u.next(args_now()));
 }
 
 // ---- 64 or 128 rows: the wavefronts read the keys together (f16 / bf16) -----------------------------
@@ -895,7 +919,7 @@ __global__ __launch_bounds__(kTreeWaves * kWave, 2) void tree_tile_kernel(TreeRu
             const bool there = (unsigned)page < (unsigned)pool_pages;
             const uint64_t at = (uint64_t)(pool + (there ? page : 0) * page_bytes + (key & ((1 << page_log2) - 1)) * ROW);
             const int left = last_key - key, keys = !there || left < 0 ? 0 : left < 16 ? left : 16;
-            return Window{u32x4{(uint32_t)uniform((int)at), (uint32_t)uniform((int)(at >> 32)), (uint32_t)uniform(keys * ROW), 0x00020000u}};
+            return make_window(at, keys * ROW);
         };
         int page1 = page_of(0), page2 = page_of(1);      // of tiles now + 1 and now + 2, once now is 0
         const Window k0 = window(kpool, 0, page1), v0 = window(vpool, 0, page1), k1 = window(kpool, 1, page2);
