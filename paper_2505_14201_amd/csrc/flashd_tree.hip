@@ -49,7 +49,7 @@ struct TreeSplit {
     int first;      // first row (token, head of the group) of the tile
     int rows;       // rows of the tile
     int parts;
-    int pad[3];
+    int w;          // place along the row of blocks of the workgroup with its first part
 };
 
 struct TreeRun {
@@ -58,8 +58,8 @@ struct TreeRun {
     FastDiv group;          // query heads per kv head
     float* parts;           // [2 groups][rows of a tile][d] unnormalised outputs
     float2* stats;          // [2 groups][rows of a tile] reference and sum of weights
-    TreeSplit* splits;      // [groups]
-    int* groups;            // how many workgroups have work
+    TreeSplit* splits;      // [groups], of the unit that a workgroup begins and does not end
+    int groups;             // workgroups of the launch
 };
 
 // The kernel's arguments, read anew where they are asked for.  What only the beginning and the end of a piece need
@@ -84,6 +84,11 @@ __device__ __forceinline__ long long uniform(long long x) {
     return (long long)((uint64_t)(uint32_t)uniform((int)(x >> 32)) << 32 | (uint32_t)uniform((int)x));
 }
 
+// a / b of numbers that are small as a rule (a division of 64 bits takes hundreds of instructions)
+__device__ __forceinline__ long long quotient(long long a, long long b) {
+    return ((a | b) >> 32) == 0 ? (long long)((uint32_t)a / (uint32_t)b) : a / b;
+}
+
 struct WalkScratch {
     long long wave_sum[kTreeWaves];
     long long found_before;
@@ -93,7 +98,8 @@ struct WalkScratch {
 // A workgroup's way along the row of blocks, and the piece of a unit that it is at (all the same in every
 // thread, in scalar registers).  M: rows of a tile; KB: keys of a block of the row.  Of a chain's row tile only the blocks count
 // that its last token sees.
-template <int M, int KB>
+// GRID: workgroups of the launch.
+template <int M, int KB, int GRID>
 struct Walk {
     long long at, end;      // blocks of the long row
     long long per;          // blocks of every workgroup
@@ -169,18 +175,19 @@ struct Walk {
             total += wave_sum[k];
         }
         total = uniform(total);
+        // all workgroups, or as many as have kLeast blocks each
         constexpr int kLeast = kTreeMinBlocks * kTreeBlock / KB;
-        long long groups = (total + kLeast - 1) / kLeast;
-        if (groups > gridDim.x) groups = gridDim.x;
-        per = groups > 0 ? (total + groups - 1) / groups : 1;
+        const bool few = total <= (long long)kLeast * GRID;
+        per = few ? kLeast : (total + GRID - 1) / GRID;
+        const int groups = few ? (int)((total + kLeast - 1) / kLeast) : (int)quotient(total + per - 1, per);
         // Workgroup ids go round-robin over the 8 XCDs; neighbours along the row, which may read the same
         // keys, go to one.
-        const int of_xcd = (int)((groups + 7) >> 3);
+        const int of_xcd = (groups + 7) >> 3;
         const int k = (int)blockIdx.x >> 3;
         w = ((int)blockIdx.x & 7) * of_xcd + k;
         at = k < of_xcd && w < groups ? per * w : total;
         end = at + per < total ? at + per : total;
-        if (blockIdx.x == 0 && tid == 0) *r.groups = (int)groups;
+        if (tid == 0) r.splits[blockIdx.x].parts = 0;
         if (at < end && at >= before && at < before + mine) {
             for (int i = b0; i < b1; ++i) {
                 const long long sum = any.template enter<false>(r, i) * c.Hkv;
@@ -192,7 +199,6 @@ struct Walk {
                 before += sum;
             }
         }
-        if (tid == 0 && k < of_xcd && w < groups) r.splits[w].parts = 0;
         __syncthreads();
         const int found = uniform(found_b);
         const long long found_at = uniform(found_before);
@@ -202,12 +208,12 @@ struct Walk {
             return;
         }
         const long long head = uniform(enter<true>(r, found)), in_b = at - found_at;
-        h = uniform((int)(in_b / head));
+        h = uniform((int)quotient(in_b, head));
         int from;
         if (r.a.tree != nullptr) {
             const int each_tile = blocks_of(r, 0);
             const long long rest = in_b - h * head;
-            tile = uniform((int)(rest / each_tile));
+            tile = uniform((int)quotient(rest, each_tile));
             from = (int)(rest - (long long)tile * each_tile);
         } else {
             long long rest = in_b - h * head;
@@ -242,9 +248,9 @@ struct Walk {
         sp.h = h;
         sp.first = first;
         sp.rows = nrows;
-        sp.parts = (int)((at + blocks - 1) / per) - w + 1;
-        sp.pad[0] = sp.pad[1] = sp.pad[2] = 0;
-        r.splits[w] = sp;
+        sp.parts = (int)quotient(at + blocks - 1, per) - w + 1;
+        sp.w = w;
+        r.splits[blockIdx.x] = sp;
     }
 };
 
@@ -521,7 +527,7 @@ __global__ __launch_bounds__(kTreeWaves * kWave, rows_per_cu(D, FP8, NR)) void t
     const float ninf = -__builtin_inff();
     uint16_t* vs = reinterpret_cast<uint16_t*>(lds) + wave * STAGE;
 
-    Walk<16 * NR, kTreeBlock> u;
+    Walk<16 * NR, kTreeBlock, 256 * rows_per_cu(D, FP8, NR)> u;
     u.begin(args_now(), reinterpret_cast<WalkScratch*>(lds));
     if (u.at >= u.end) return;
     do {
@@ -880,7 +886,7 @@ __global__ __launch_bounds__(kTreeWaves * kWave, 2) void tree_tile_kernel(TreeRu
     const int rw = wave & (RW - 1), kw = wave / RW;
     const float ninf = -__builtin_inff();
 
-    Walk<M, kBC> u;
+    Walk<M, kBC, 512> u;
     u.begin(args_now(), reinterpret_cast<WalkScratch*>(lds));
     if (u.at >= u.end) return;
 
@@ -1185,7 +1191,7 @@ __global__ __launch_bounds__(kTreeWaves * kWave, 2) void tree_rows_f32_kernel(Tr
     const int q = lane >> 4;
     const float ninf = -__builtin_inff();
 
-    Walk<16, kTreeBlock> u;
+    Walk<16, kTreeBlock, 512> u;
     u.begin(r, reinterpret_cast<WalkScratch*>(fold));
     if (u.at >= u.end) return;
     do {
@@ -1269,11 +1275,14 @@ __global__ __launch_bounds__(kTreeWaves * kWave, 2) void tree_rows_f32_kernel(Tr
 // ---- join the parts of split units -------------------------------------------------------------
 //
 // The rows of all split units, one after the other, are dealt out evenly: a fixed number of workgroups, each of which
-// sums up how many there are (256 at a time) and walks its share.  D / 4 lanes take 4 columns each of a row; the
-// 1024 / D such groups of a workgroup take a row each, or share the parts of one row where a unit has many (more
-// than kMergeShare: one long sequence over the whole chip).  M: rows of a tile.
+// sums up how many there are and walks its share.  D / 4 lanes take 4 columns each of a row; the 1024 / D such
+// groups of a workgroup take a row each, or share the parts of one row where a unit has many (more than
+// kMergeShare: one long sequence over the whole chip).  Each thread of a workgroup keeps the splits of a few of the
+// launch's workgroups, and the one that holds the next rows' hands it over through LDS: between a workgroup's start
+// and its rows lies one read from memory.  M: rows of a tile.  What bounds it is the time of its reads, so that many workgroups
+// are under way at once where there are many rows.
 constexpr int kMergeShare = 12;
-constexpr int kMergeGroups = 512;
+constexpr int merge_groups(int M) { return M <= 32 ? 512 : M == 64 ? 1024 : 2048; }
 
 // One row's parts k0, k0 + step, ...: unnormalised sum against `top`.
 template <int D, int M>
@@ -1306,60 +1315,74 @@ __device__ __forceinline__ f32x4 merge_parts(const TreeRun& r, int w, int parts,
 }
 
 template <typename T, int D, int M>
-__global__ __launch_bounds__(256) void merge_tree_kernel(TreeRun r, float vscale) {
+__global__ __launch_bounds__(256, 4) void merge_tree_kernel(TreeRun r, float vscale) {
     constexpr int LPR = D / 4;
     constexpr int NG = 256 / LPR;
+    constexpr int EACH = kTreeMostGroups / 256;
     __shared__ __align__(16) float sum[NG][D];
     __shared__ float2 part_stat[NG];
-    __shared__ int before[kTreeMostGroups + 1];          // items of the splits before
-    __shared__ int wave_sum[kTreeWaves];
+    __shared__ int next[sizeof(TreeSplit) / 4];
+    __shared__ int next_item;
+    __shared__ int wave_sum[EACH][kTreeWaves];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int groups = uniform(*r.groups);
     const float ninf = -__builtin_inff();
-    auto items_of = [](const TreeSplit& sp) {
-        return sp.parts == 0 ? 0 : sp.parts > kMergeShare ? sp.rows : (sp.rows + NG - 1) / NG;
-    };
-    int total = 0;
-    for (int w0 = 0; w0 < groups; w0 += 256) {
-        const int mine = w0 + tid < groups ? items_of(r.splits[w0 + tid]) : 0;
-        int in = mine;
+    // Word by word: a struct is kept in LDS, where the compiler finds its place from the launch's size, which it
+    // reads from the host's memory (12 us).
+    constexpr int WORDS = sizeof(TreeSplit) / 4, ROWS = offsetof(TreeSplit, rows) / 4, PARTS = offsetof(TreeSplit, parts) / 4;
+    int mine[EACH][WORDS];
+    int items[EACH], before[EACH];
 #pragma unroll
-        for (int k = 1; k < 64; k <<= 1) {
-            const int y = __shfl_up(in, k);
-            if (lane >= k) in += y;
-        }
-        __syncthreads();
-        if (lane == 63) wave_sum[wave] = in;
-        __syncthreads();
-        int ahead = 0, all = 0;
+    for (int k = 0; k < EACH; ++k) {
+        const int* sp = reinterpret_cast<const int*>(r.splits + min(256 * k + tid, r.groups - 1));
 #pragma unroll
-        for (int k = 0; k < kTreeWaves; ++k) {
-            ahead += k < wave ? wave_sum[k] : 0;
-            all += wave_sum[k];
+        for (int i = 0; i < WORDS; ++i) mine[k][i] = sp[i];
+    }
+#pragma unroll
+    for (int k = 0; k < EACH; ++k) {
+        const int rows = mine[k][ROWS], parts = mine[k][PARTS];
+        items[k] = 256 * k + tid >= r.groups || parts == 0 ? 0 : parts > kMergeShare ? rows : (rows + NG - 1) / NG;
+        int in = items[k];
+#pragma unroll
+        for (int step = 1; step < 64; step <<= 1) {
+            const int y = __shfl_up(in, step);
+            if (lane >= step) in += y;
         }
-        if (w0 + tid < kTreeMostGroups) before[w0 + tid] = total + ahead + in - mine;
-        total += uniform(all);
+        if (lane == 63) wave_sum[k][wave] = in;
+        before[k] = in - items[k];
     }
     __syncthreads();
+    int total = 0;
+#pragma unroll
+    for (int k = 0; k < EACH; ++k) {
+#pragma unroll
+        for (int i = 0; i < kTreeWaves; ++i) {
+            if (i == wave) before[k] += total;
+            total += wave_sum[k][i];
+        }
+    }
+    total = uniform(total);
     const int g = tid / LPR, t = 4 * (tid % LPR);
     const int G = (int)r.group.d;
     for (int item = blockIdx.x; item < total; item += gridDim.x) {
-        int lo = 0, hi = groups;             // the split: the last whose items begin at or before this one
-        while (hi - lo > 1) {
-            const int mid = (lo + hi) >> 1;
-            if (before[mid] <= item) lo = mid;
-            else hi = mid;
+        __syncthreads();                     // the last item's sums and split are read
+#pragma unroll
+        for (int k = 0; k < EACH; ++k) {
+            if (item >= before[k] && item - before[k] < items[k]) {
+#pragma unroll
+                for (int i = 0; i < WORDS; ++i) next[i] = mine[k][i];
+                next_item = item - before[k];
+            }
         }
-        const int w = uniform(lo);
-        const TreeSplit sp = r.splits[w];
-        const int parts = uniform(sp.parts), of = item - before[w];
+        __syncthreads();
+        TreeSplit sp;
+        __builtin_memcpy(&sp, next, sizeof(sp));
+        const int w = uniform(sp.w), parts = uniform(sp.parts), of = uniform(next_item);
         float top = ninf, lt = 0.0f;
         f32x4 o;
         int fr;
         if (parts > kMergeShare) {
             fr = of;
             o = merge_parts<D, M>(r, w, parts, fr, t, g, NG, top, lt);
-            __syncthreads();
             *reinterpret_cast<f32x4*>(&sum[g][t]) = o;
             if (t == 0) part_stat[g] = float2{top, lt};
             __syncthreads();
@@ -1401,27 +1424,30 @@ static int tree_rows(int Hq, int Hkv, int max_q, int dtype) {
 
 size_t attn_tree_workspace(int Hq, int Hkv, int max_q, int d, int dtype) {
     const int rows = tree_rows(Hq, Hkv, max_q, dtype);
-    return (size_t)2 * kTreeMostGroups * rows * (d + 2) * sizeof(float) + kTreeMostGroups * sizeof(TreeSplit) + 16;
+    return (size_t)2 * kTreeMostGroups * rows * (d + 2) * sizeof(float) + kTreeMostGroups * sizeof(TreeSplit);
 }
 
 template <typename T, int D, int M>
 static hipError_t launch_tree_m(TreeRun& r, hipStream_t st) {
-    const dim3 grid(512), block(kTreeWaves * kWave);
+    const dim3 block(kTreeWaves * kWave);
     r.stats = reinterpret_cast<float2*>(r.parts + (size_t)2 * kTreeMostGroups * M * D);
     r.splits = reinterpret_cast<TreeSplit*>(r.stats + (size_t)2 * kTreeMostGroups * M);
-    r.groups = reinterpret_cast<int*>(r.splits + kTreeMostGroups);
+    if constexpr (std::is_same_v<T, F32>) r.groups = 512;
+    else if constexpr (M <= 32) r.groups = 256 * (r.a.fp8 ? rows_per_cu(D, true, M / 16) : rows_per_cu(D, false, M / 16));
+    else r.groups = 512;
+    const dim3 grid(r.groups);
     if constexpr (std::is_same_v<T, F32>) {
         hipLaunchKernelGGL((tree_rows_f32_kernel<D>), grid, block, 0, st, r);
     } else if constexpr (M <= 32) {
-        if (r.a.fp8) hipLaunchKernelGGL((tree_rows_kernel<T, D, true, M / 16>), dim3(256 * rows_per_cu(D, true, M / 16)), block, 0, st, r);
-        else hipLaunchKernelGGL((tree_rows_kernel<T, D, false, M / 16>), dim3(256 * rows_per_cu(D, false, M / 16)), block, 0, st, r);
+        if (r.a.fp8) hipLaunchKernelGGL((tree_rows_kernel<T, D, true, M / 16>), grid, block, 0, st, r);
+        else hipLaunchKernelGGL((tree_rows_kernel<T, D, false, M / 16>), grid, block, 0, st, r);
     } else {
         if (r.a.fp8) hipLaunchKernelGGL((tree_tile_kernel<T, D, true, M / 32>), grid, block, 0, st, r);
         else hipLaunchKernelGGL((tree_tile_kernel<T, D, false, M / 32>), grid, block, 0, st, r);
     }
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((merge_tree_kernel<T, D, M>), dim3(kMergeGroups), dim3(256), 0, st, r,
+    hipLaunchKernelGGL((merge_tree_kernel<T, D, M>), dim3(merge_groups(M)), block, 0, st, r,
                        r.a.fp8 ? r.c.vscale : 1.0f);
     return hipGetLastError();
 }
