@@ -27,6 +27,15 @@ constexpr int kTreeBlock = 32;          // keys of a block: a wavefront's step
 constexpr int kTreeWaves = 4;
 constexpr int kTreeMostGroups = 768;    // workgroups of a launch, three per compute unit (see rows_per_cu) or two
 constexpr int kTreeMinBlocks = 4;       // blocks a workgroup takes at least
+// What the start of a unit counts, in blocks (of 64 keys in the tile kernel): with 0, 1, 2, 3, 4 and 6 the tile kernel took 28.8,
+// 27.8, 26.8, 26.3, 25.4 and 25.8 us for 128 units of 17 to 64 tiles, and for long units it made no difference; the rows kernel
+// took 103.8 us with 0 and 103.7 with 8, its own steps being shorter.
+constexpr int kRowsStart = 0, kTileStart = 3;
+
+// Waits until all but the last N loads have arrived.
+template <int N> __device__ __forceinline__ void wait_loads() {
+    __builtin_amdgcn_s_waitcnt((N & 15) | (N >> 4) << 14 | 0x0f70);
+}
 
 template <typename T> struct Mma16;
 template <> struct Mma16<BF16> {
@@ -84,30 +93,62 @@ __device__ __forceinline__ long long uniform(long long x) {
     return (long long)((uint64_t)(uint32_t)uniform((int)(x >> 32)) << 32 | (uint32_t)uniform((int)x));
 }
 
-// a / b of numbers that are small as a rule (a division of 64 bits takes hundreds of instructions)
+// a / b of whole numbers, 0 <= a < 2^52 and b > 0, by a division of doubles (one of 64-bit integers takes ten times the
+// instructions).  The quotient is rounded, so that its floor can be one too large.
 __device__ __forceinline__ long long quotient(long long a, long long b) {
-    return ((a | b) >> 32) == 0 ? (long long)((uint32_t)a / (uint32_t)b) : a / b;
+    const long long q = (long long)((double)a / (double)b);
+    return q * b > a ? q - 1 : q;
+}
+
+// sum over i < n of floor((a i + b) / m), for a, b >= 0 and m > 0.  Whole multiples of m in a and b are counted directly.
+// What is left counts points under a line with slope below 1; seen from the other axis, of its k = floor((a (n - 1) + b) / m)
+// rows row j = 1..k lacks the first ceil((j m - b) / a) of n points: a sum of the same form with a in m's place.
+__device__ __forceinline__ long long sum_of_floors(long long n, long long a, long long b, long long m) {
+    long long sum = 0, sign = 1;
+    while (n > 0) {
+        if (a >= m) {
+            const long long q = quotient(a, m);
+            sum += sign * q * ((n * (n - 1)) >> 1);
+            a -= q * m;
+        }
+        if (b >= m) {
+            const long long q = quotient(b, m);
+            sum += sign * q * n;
+            b -= q * m;
+        }
+        const long long k = quotient(a * (n - 1) + b, m);
+        if (k == 0) break;
+        sum += sign * n * k;
+        sign = -sign;
+        b = m - b + a - 1;
+        const long long slope = a;
+        a = m;
+        m = slope;
+        n = k;
+    }
+    return sum;
 }
 
 struct WalkScratch {
     long long wave_sum[kTreeWaves];
-    long long found_before;
+    long long found_before, found_places;
     int found_b;
 };
 
 // A workgroup's way along the row of blocks, and the piece of a unit that it is at (all the same in every
 // thread, in scalar registers).  M: rows of a tile; KB: keys of a block of the row.  Of a chain's row tile only the blocks count
-// that its last token sees.
-// GRID: workgroups of the launch.
-template <int M, int KB, int GRID>
+// that its last token sees.  A unit begins with START places without a block, for the time that its first keys and its
+// queries take to arrive: a workgroup with more units gets fewer blocks.  GRID: workgroups of the launch.
+template <int M, int KB, int GRID, int START>
 struct Walk {
-    long long at, end;      // blocks of the long row
-    long long per;          // blocks of every workgroup
+    long long at, end;      // places of the long row
+    long long per;          // places of every workgroup
     int w;                  // the workgroup's place along the row
     int b, h, tile;         // present unit
     Seq s;
     int tiles;              // row tiles of the sequence
     int blocks;             // blocks of the unit
+    int from;               // the place in the unit at which the piece begins
     int blk0, blk1;         // the piece
     int first, nrows;       // its first row (token, head of the group), and rows
 
@@ -123,32 +164,39 @@ struct Walk {
         }
         return (keys + KB - 1) / KB;
     }
-    // Sequence `seq`; returns the blocks of one kv head's units.  SAME: it is the same one in every thread.
+    // Sequence `seq`.  SAME: it is the same one in every thread.
     template <bool SAME>
-    __device__ __forceinline__ long long enter(const TreeRun& r, int seq) {
+    __device__ __forceinline__ void enter(const TreeRun& r, int seq) {
         b = seq;
         s = seq_at(r.c, b);
         if constexpr (SAME) s = Seq{uniform(s.row0), uniform(s.n), uniform(s.len)};
         tiles = (int)(((long long)s.n * (int)r.group.d + M - 1) / M);
-        long long sum = 0;
-        if (r.a.tree != nullptr) sum = tiles > 0 ? (long long)tiles * blocks_of(r, 0) : 0;
-        else for (int t = 0; t < tiles; ++t) sum += blocks_of(r, t);
-        return sum;
+    }
+    // Places of one kv head's units.  (A chain's tile t < tiles - 1 has ceil((len + ceil((t + 1) M / G)) / KB) blocks,
+    // which is ceil((len G + (t + 1) M) / (G KB)).)
+    __device__ __forceinline__ long long places(const TreeRun& r) const {
+        if (tiles == 0) return 0;
+        const long long last = blocks_of(r, tiles - 1) + START;
+        if (r.a.tree != nullptr) return tiles * last;
+        const long long G = (int)r.group.d, m = G * KB;
+        return last + (long long)(tiles - 1) * START + sum_of_floors(tiles - 1, M, s.len * G + M + m - 1, m);
     }
     __device__ __forceinline__ void set_unit(const TreeRun& r) {
         blocks = blocks_of(r, tile);
         first = tile * M;
         nrows = min(M, s.n * (int)r.group.d - first);
     }
-    __device__ __forceinline__ void set_piece(int from) {
+    __device__ __forceinline__ void set_piece(int place) {
         const long long left = end - at;
-        blk0 = from;
-        blk1 = (int)(left < blocks - from ? from + left : blocks);
+        from = place;
+        const int to = left < START + blocks - from ? from + (int)left : START + blocks;
+        blk0 = max(from - START, 0);
+        blk1 = max(to - START, 0);
     }
 
-    // Every thread of the workgroup takes a run of sequences, whose blocks are then summed over the threads;
-    // the one that has the share's first block in its run finds the sequence.
-    __device__ __forceinline__ void begin(const TreeRun& r, WalkScratch* scratch) {
+    // Every thread of the workgroup takes a run of sequences, whose places are then summed over the threads;
+    // the one that has the share's first place in its run finds the sequence.  False: no share.
+    __device__ __forceinline__ bool begin(const TreeRun& r, WalkScratch* scratch) {
         long long (&wave_sum)[kTreeWaves] = scratch->wave_sum;
         long long& found_before = scratch->found_before;
         int& found_b = scratch->found_b;
@@ -156,9 +204,13 @@ struct Walk {
         const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
         const int each = (c.B + kTreeWaves * kWave - 1) / (kTreeWaves * kWave);
         const int b0 = tid * each, b1 = min(b0 + each, c.B);
-        long long mine = 0;
+        long long mine = 0, own = 0;             // of the run, and of its last sequence
         Walk any;
-        for (int i = b0; i < b1; ++i) mine += any.template enter<false>(r, i) * c.Hkv;
+        for (int i = b0; i < b1; ++i) {
+            any.template enter<false>(r, i);
+            own = any.places(r) * c.Hkv;
+            mine += own;
+        }
         long long in = mine;
 #pragma unroll
         for (int k = 1; k < 64; k <<= 1) {
@@ -175,11 +227,11 @@ struct Walk {
             total += wave_sum[k];
         }
         total = uniform(total);
-        // all workgroups, or as many as have kLeast blocks each
+        // all workgroups, or as many as have kLeast places each
         constexpr int kLeast = kTreeMinBlocks * kTreeBlock / KB;
         const bool few = total <= (long long)kLeast * GRID;
-        per = few ? kLeast : (total + GRID - 1) / GRID;
-        const int groups = few ? (int)((total + kLeast - 1) / kLeast) : (int)quotient(total + per - 1, per);
+        per = few ? kLeast : quotient(total + GRID - 1, GRID);
+        const int groups = (int)quotient(total + per - 1, per);
         // Workgroup ids go round-robin over the 8 XCDs; neighbours along the row, which may read the same
         // keys, go to one.
         const int of_xcd = (groups + 7) >> 3;
@@ -189,56 +241,76 @@ struct Walk {
         end = at + per < total ? at + per : total;
         if (tid == 0) r.splits[blockIdx.x].parts = 0;
         if (at < end && at >= before && at < before + mine) {
-            for (int i = b0; i < b1; ++i) {
-                const long long sum = any.template enter<false>(r, i) * c.Hkv;
-                if (at < before + sum) {
-                    found_b = i;
-                    found_before = before;
-                    break;
+            int i = b0;
+            if (each > 1) {                      // (a run of one sequence: `own` is its places)
+                for (;; ++i) {
+                    any.template enter<false>(r, i);
+                    own = any.places(r) * c.Hkv;
+                    if (at < before + own) break;
+                    before += own;
                 }
-                before += sum;
             }
+            found_b = i;
+            found_before = before;
+            scratch->found_places = own;
         }
         __syncthreads();
         const int found = uniform(found_b);
-        const long long found_at = uniform(found_before);
+        const long long in_b = at - uniform(found_before), head = uniform(quotient(scratch->found_places, c.Hkv));
         __syncthreads();                                 // the scratch is the kernel's again
-        if (found < 0) {
-            end = at;
-            return;
-        }
-        const long long head = uniform(enter<true>(r, found)), in_b = at - found_at;
+        if (found < 0) return false;
+        enter<true>(r, found);
         h = uniform((int)quotient(in_b, head));
-        int from;
-        if (r.a.tree != nullptr) {
-            const int each_tile = blocks_of(r, 0);
-            const long long rest = in_b - h * head;
+        long long rest = in_b - h * head;
+        if (r.a.tree != nullptr || tiles == 1) {
+            const int each_tile = blocks_of(r, 0) + START;
             tile = uniform((int)quotient(rest, each_tile));
-            from = (int)(rest - (long long)tile * each_tile);
+            rest -= (long long)tile * each_tile;
         } else {
-            long long rest = in_b - h * head;
-            for (tile = 0; rest >= blocks_of(r, tile); ++tile) rest -= blocks_of(r, tile);
-            from = (int)rest;
-        }
-        set_unit(r);
-        set_piece(from);
-    }
-    // On to the next piece; false at the end of the share.
-    __device__ __forceinline__ bool next(const TreeRun& r) {
-        at += blk1 - blk0;
-        if (at >= end) return false;
-        if (++tile == tiles) {
+            // every wavefront by itself, 64 tiles at a time
             tile = 0;
-            if (++h == r.c.Hkv) {
-                h = 0;
-                do {
-                    if (b + 1 >= r.c.B) return false;
-                    enter<true>(r, b + 1);
-                } while (tiles == 0);
+            for (int t0 = 0;; t0 += kWave) {
+                const int its = t0 + lane < tiles ? blocks_of(r, t0 + lane) + START : 0;
+                long long sum = its;
+#pragma unroll
+                for (int step = 1; step < 64; step <<= 1) {
+                    const long long y = __shfl_up(sum, step);
+                    if (lane >= step) sum += y;
+                }
+                const uint64_t beyond = __builtin_amdgcn_ballot_w64(sum > rest);
+                const int hit = beyond != 0 ? __builtin_ctzll(beyond) : kWave - 1;
+                const long long upto = uniform(__shfl(sum, hit));
+                if (beyond != 0) {
+                    tile = t0 + hit;
+                    rest -= upto - __builtin_amdgcn_readlane(its, hit);
+                    break;
+                }
+                rest -= upto;
             }
         }
         set_unit(r);
-        set_piece(0);
+        set_piece(uniform((int)rest));
+        return blk0 < blk1 || next(r);
+    }
+    // On to the next piece with keys; false at the end of the share.
+    __device__ __forceinline__ bool next(const TreeRun& r) {
+        int place = from;
+        do {
+            at += min((long long)START + blocks - place, end - at);
+            if (at >= end) return false;
+            if (++tile == tiles) {
+                tile = 0;
+                if (++h == r.c.Hkv) {
+                    h = 0;
+                    do {
+                        if (b + 1 >= r.c.B) return false;
+                        enter<true>(r, b + 1);
+                    } while (tiles == 0);
+                }
+            }
+            set_unit(r);
+            set_piece(place = 0);
+        } while (blk0 == blk1);
         return true;
     }
     __device__ __forceinline__ int slot() const { return 2 * w + (blk0 == 0 ? 1 : 0); }
@@ -248,7 +320,7 @@ struct Walk {
         sp.h = h;
         sp.first = first;
         sp.rows = nrows;
-        sp.parts = (int)quotient(at + blocks - 1, per) - w + 1;
+        sp.parts = (int)quotient(at + START + blocks - from - 1, per) - w + 1;
         sp.w = w;
         r.splits[blockIdx.x] = sp;
     }
@@ -527,9 +599,8 @@ __global__ __launch_bounds__(kTreeWaves * kWave, rows_per_cu(D, FP8, NR)) void t
     const float ninf = -__builtin_inff();
     uint16_t* vs = reinterpret_cast<uint16_t*>(lds) + wave * STAGE;
 
-    Walk<16 * NR, kTreeBlock, 256 * rows_per_cu(D, FP8, NR)> u;
-    u.begin(args_now(), reinterpret_cast<WalkScratch*>(lds));
-    if (u.at >= u.end) return;
+    Walk<16 * NR, kTreeBlock, 256 * rows_per_cu(D, FP8, NR), kRowsStart> u;
+    if (!u.begin(args_now(), reinterpret_cast<WalkScratch*>(lds))) return;
     do {
         // the query rows of this lane's column; columns past the last row stand in for it
         const TreeRun now_r = args_now();
@@ -541,9 +612,7 @@ __global__ __launch_bounds__(kTreeWaves * kWave, rows_per_cu(D, FP8, NR)) void t
 #pragma unroll
             for (int kk = 0; kk < NKK; ++kk) qf[k][kk] = *reinterpret_cast<const u32x4*>(qg + 32 * kk + 8 * q);
         }
-        // Here before the loop, as the compiler knows: in every turn of it, it would else wait for them, and so for the keys
-        // under way.
-        wait_copies();
+        __builtin_amdgcn_sched_barrier(0);
         const float c_log2 = (FP8 ? now_r.a.scale * now_r.c.kscale : now_r.a.scale) * kLog2e;
 
         // What the loop needs of the arguments, each in a register of its own (see tree_tile_kernel).
@@ -615,6 +684,9 @@ __global__ __launch_bounds__(kTreeWaves * kWave, rows_per_cu(D, FP8, NR)) void t
         __builtin_amdgcn_sched_barrier(0);
         fetch(vpool, vreg, blk, p0, p1);
         __builtin_amdgcn_sched_barrier(0);
+        // The queries are here before the loop, as the compiler knows: in every turn of it, it would else wait for them,
+        // and so for the keys under way.
+        wait_loads<2 * NV>();
         for (; blk < blk_end; blk += W) {
             const int j0 = blk * kTreeBlock;
             // a half without a page, or behind the last key, has no keys
@@ -886,9 +958,8 @@ __global__ __launch_bounds__(kTreeWaves * kWave, 2) void tree_tile_kernel(TreeRu
     const int rw = wave & (RW - 1), kw = wave / RW;
     const float ninf = -__builtin_inff();
 
-    Walk<M, kBC, 512> u;
-    u.begin(args_now(), reinterpret_cast<WalkScratch*>(lds));
-    if (u.at >= u.end) return;
+    Walk<M, kBC, 512, kTileStart> u;
+    if (!u.begin(args_now(), reinterpret_cast<WalkScratch*>(lds))) return;
 
     TileLoader<T, D, FP8, RW == 2> load;        // (up to 64 rows a sequence is one row tile: its keys are read once)
 
@@ -1191,9 +1262,8 @@ __global__ __launch_bounds__(kTreeWaves * kWave, 2) void tree_rows_f32_kernel(Tr
     const int q = lane >> 4;
     const float ninf = -__builtin_inff();
 
-    Walk<16, kTreeBlock, 512> u;
-    u.begin(r, reinterpret_cast<WalkScratch*>(fold));
-    if (u.at >= u.end) return;
+    Walk<16, kTreeBlock, 512, kRowsStart> u;
+    if (!u.begin(r, reinterpret_cast<WalkScratch*>(fold))) return;
     do {
         const int row = u.first + min(col, u.nrows - 1);
         const int token = (int)fast_div((uint32_t)row, r.group);
