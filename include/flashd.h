@@ -276,7 +276,8 @@ int flashd_skip_stats(const void* q, const void* k, int B, int Hq, int Hkv, int 
  *
  *   pools     page p of layer y begins y * layer_stride + p * page_stride elements into k and into v
  *             and is [Hkv][page][d], contiguous.  So [layers][P][Hkv][page][d] may be one tensor, or a page's
- *             K and V lie side by side.  Different pages (and layers) must not share memory.
+ *             K and V lie side by side.  Different pages (and layers) must not share memory, nor
+ *             K and V where they are written.
  *   table     int [B][max_pages]: page numbers, the pages a sequence owns first, then -1.
  *   lens      int [B]: the keys each sequence has in the cache.
  *   refs      int [P]: how many table entries name each page; a page with 0 is free.
@@ -357,7 +358,8 @@ int flashd_cache_reserve(const flashd_cache* c, int* refs, const int* q_start, i
  * Cache of FLASHD_CACHE_FP8: K / kscale and V / vscale are rounded to e4m3, what passes 448 becomes 448.
  *   q, q_out        [T][Hq][d], k, v [T][Hkv][d] in storage type `dtype` (the cache's, or f16/bf16 with an fp8 cache, else
  *                   FLASHD_E_VARIANT); rows of a token contiguous, tokens *_stride elements apart.
- *                   q_out may be q; otherwise outputs overlap no input.
+ *                   q_out may be q (k and v may then lie between its tokens, as one projection leaves them);
+ *                   otherwise outputs overlap no input.
  *   positions       int [T], or NULL: a token's position is its key number
  *   inv_freq        float [rot / 2]; NULL with rot == 0.  rot is a multiple of 16, at most d.
  *   q_weight, k_weight   [d] in `dtype`, or NULL
@@ -383,7 +385,7 @@ int flashd_cache_append(const flashd_cache* c, int layer, const void* q, long lo
  *   max_q    the most new tokens of a sequence; sizes the launch, not the result: any value >= 1 is right.
  *   workspace   device memory of at least flashd_tree_workspace_bytes(...), 16-byte aligned, or NULL: taken
  *            from the grow-only cache of the stream as in flashd_attn_fwd.  Two calls must not use one
- *            workspace at the same time.
+ *            workspace at the same time; a call recorded into a graph brings its own (NULL: FLASHD_E_WORKSPACE).
  * Scores, softmax and sums are fp32; weights are rounded to `dtype` before the product with V.  For fixed inputs and
  * max_q the output is bitwise reproducible.  T == 0 is a call without work.
  */

@@ -94,6 +94,28 @@ int64_t pool_extent(const Paged& p) {
     return (int64_t)(p.P - 1) * p.page_bytes + (int64_t)(p.layers - 1) * p.layer_bytes + (int64_t)p.Hkv * p.head_bytes;
 }
 
+// Whether rows of abytes at a share memory with rows of bbytes at b, both `stride` bytes apart, T of each
+bool rows_overlap(const void* a, int64_t abytes, const void* b, int64_t bbytes, int64_t stride, int T) {
+    if (!overlap(a, (T - 1) * stride + abytes, b, (T - 1) * stride + bbytes)) return false;
+    const int64_t off = (int64_t)((uintptr_t)b - (uintptr_t)a) % stride, at = off < 0 ? off + stride : off;
+    return T == 1 || at < abytes || at + bbytes > stride;
+}
+
+// Whether a page of K may share memory with one of V: not where the pools lie apart, nor where V's pages (or layers)
+// lie between K's.
+bool kv_overlap(const Paged& p) {
+    if (!overlap(p.k, pool_extent(p), p.v, pool_extent(p))) return false;
+    const int64_t strides[2] = {p.page_bytes, p.layers > 1 ? p.layer_bytes : 0}, counts[2] = {p.P, p.layers};
+    for (int i = 0; i < 2; ++i) {
+        const int64_t stride = strides[i], other = strides[1 - i];
+        if (stride == 0) continue;
+        const int64_t held = p.Hkv * p.head_bytes + (other < stride ? (counts[1 - i] - 1) * other : 0);
+        const int64_t off = (int64_t)((uintptr_t)p.v - (uintptr_t)p.k) % stride, at = off < 0 ? off + stride : off;
+        if (at >= held && at + held <= stride) return false;
+    }
+    return true;
+}
+
 int done(hipError_t e) { return e == hipSuccess ? FLASHD_OK : FLASHD_E_HIP; }
 
 }  // namespace
@@ -131,6 +153,7 @@ int flashd_cache_reserve(const flashd_cache* c, int* refs, const int* q_start, i
     if (overlap(report, rep, c->table, (int64_t)c->B * c->max_pages * 4) || overlap(report, rep, c->lens, rep - 4) ||
         overlap(report, rep, q_start, rep) || overlap(report, rep, refs, (int64_t)c->P * 4))
         return FLASHD_E_OVERLAP;
+    if (kv_overlap(p)) return FLASHD_E_OVERLAP;
     rc = flashd::api_check_arch();
     if (rc != FLASHD_OK) return rc;
     return done(flashd::launch_cache_reserve(p, refs, report, static_cast<hipStream_t>(stream)));
@@ -161,11 +184,19 @@ int flashd_cache_append(const flashd_cache* c, int layer, const void* q, long lo
     // Tokens of k and v may lie between those of q (one projection's output), so q_out in place of q
     // may share their range, but not their elements; other outputs may not.
     const bool in_place = q_out == q && q_out_stride == q_stride;
+    if (in_place && T > 0) {
+        const int es = esize(dtype);
+        const int64_t qb = (int64_t)Hq * c->d * es, kb = (int64_t)c->Hkv * c->d * es;
+        // (tokens of another stride than q's: not between them)
+        if (k_stride == q_stride ? rows_overlap(q, qb, k, kb, q_stride * es, T) : overlap(q, nq, k, nk)) return FLASHD_E_OVERLAP;
+        if (v_stride == q_stride ? rows_overlap(q, qb, v, kb, q_stride * es, T) : overlap(q, nq, v, nv)) return FLASHD_E_OVERLAP;
+    }
     if (!in_place && (overlap(q_out, no, q, nq) || overlap(q_out, no, k, nk) || overlap(q_out, no, v, nv))) return FLASHD_E_OVERLAP;
     const int64_t pool = pool_extent(p) - (p.layers - 1) * p.layer_bytes;
     for (const void* x : {static_cast<const void*>(p.k), static_cast<const void*>(p.v)})
         if (overlap(x, pool, q, nq) || overlap(x, pool, k, nk) || overlap(x, pool, v, nv) || overlap(x, pool, q_out, no))
             return FLASHD_E_OVERLAP;
+    if (kv_overlap(p)) return FLASHD_E_OVERLAP;
     rc = flashd::api_check_arch();
     if (rc != FLASHD_OK || T == 0) return rc;
     AppendArgs a;
@@ -213,6 +244,10 @@ int flashd_attn_fwd_tree(const flashd_cache* c, int layer, const void* q, long l
     rc = flashd::api_check_arch();
     if (rc != FLASHD_OK || T == 0) return rc;
     if (workspace == nullptr) {
+        // A graph would keep the stream's buffer, which other graphs and calls use as well.
+        hipStreamCaptureStatus capturing = hipStreamCaptureStatusNone;
+        if (hipStreamIsCapturing(static_cast<hipStream_t>(stream), &capturing) != hipSuccess) (void)hipGetLastError();
+        if (capturing != hipStreamCaptureStatusNone) return FLASHD_E_WORKSPACE;
         rc = flashd::api_cached_workspace(stream, (need + 255) & ~(size_t)255, &workspace);
         if (rc != FLASHD_OK) return rc;
     }
@@ -245,6 +280,7 @@ int flashd_cache_commit(const flashd_cache* c, const int* q_start, const int* ke
         overlap(lens_out, lens, q_start, lens + 4) || (n_keep && overlap(lens_out, lens, n_keep, lens)) ||
         (keep && overlap(lens_out, lens, keep, lens * max_keep)))
         return FLASHD_E_OVERLAP;
+    if (kv_overlap(p)) return FLASHD_E_OVERLAP;
     rc = flashd::api_check_arch();
     if (rc != FLASHD_OK) return rc;
     return done(flashd::launch_cache_commit(p, keep, max_keep, n_keep, lens_out, static_cast<hipStream_t>(stream)));

@@ -99,6 +99,32 @@ def test_of_the_packed_tensors():
     assert raw.flashd_attn_fwd_tree(c, 0, Q, 256, O, 256, 5, 3, 4, START, None, 0, 0.1, flashd.F32, None, None, 0) == E_VARIANT
 
 
+def test_of_keys_and_values_in_one_place():
+    page = 2 * 16 * 64                                                 # elements; 2 bytes each
+    for call in (append, reserve, commit):
+        assert call(c=cache(v=K)) == E_OVERLAP and call(c=cache(v=K + 2 * page)) == E_OVERLAP        # pages on pages
+        assert call(c=cache(v=K + page, page_stride=2 * page)) == E_OVERLAP                 # half a page on
+        two = dict(layers=2, layer_stride=20 * page)
+        assert call(c=cache(v=K + 2 * page, **two)) == E_OVERLAP and call(c=cache(v=K + 2 * 19 * page, **two)) == E_OVERLAP
+        if NO_GPU:
+            assert call(c=cache(v=K + 2 * 10 * page, **two)) == E_HIP                       # a layer's K, then its V
+            assert call(c=cache(v=K + 2 * page, page_stride=2 * page)) == E_HIP
+            # layers of a page next to each other, its K first
+            assert call(c=cache(v=K + 2 * 2 * page, layers=2, layer_stride=page, page_stride=4 * page)) == E_HIP
+        assert call(c=cache(v=K + 2 * page, layers=2, layer_stride=page, page_stride=4 * page)) == E_OVERLAP
+
+
+def test_of_an_append_in_place():
+    """q_out = q: k and v lie apart, or between the tokens of q."""
+    one = dict(q=Q, o=Q, qs=512, os=512, ks=512, vs=512, v=VN)
+    assert append(**{**one, "k": Q}) == E_OVERLAP and append(**{**one, "k": Q + 256}) == E_OVERLAP
+    assert append(**{**one, "k": Q + 1024 - 128}) == E_OVERLAP         # into the next token
+    assert append(**{**one, "k": Q + 512, "ks": 256}) == E_OVERLAP     # of another stride
+    assert append(**{**one, "k": Q + 512, "v": Q + 512 - 16}) == E_OVERLAP
+    if NO_GPU:
+        assert append(**{**one, "k": Q + 512, "v": Q + 768}) == E_HIP
+
+
 def test_of_the_bookkeeping():
     for name in ("refs", "parent", "table_out", "lens_out"):
         assert fork(**{name: None}) == E_NULL
