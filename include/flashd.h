@@ -299,7 +299,8 @@ int flashd_skip_stats(const void* q, const void* k, int B, int Hq, int Hkv, int 
  * in the same places.  Numbers found there never lead outside the buffers given: a page number outside
  * [0, P) is no page (its keys weigh nothing, what would be written to it is dropped), a
  * sequence ends at max_pages * page keys and its tokens at row T.
- * Limits: B at most 4096, page 16, 32, 64, 128 or 256, max_pages * page at most 10^9, B * max_pages and T * Hq below 2^31.
+ * Limits: B at most 4096, page 16, 32, 64, 128 or 256, max_pages * page at most 10^9, T 10^7, B * max_pages and T * Hq
+ * below 2^31.
  * Pointers to elements of pools and packed tensors and the strides of rows, pages and layers are
  * multiples of 16 bytes, other pointers of their element's size (else FLASHD_E_ALIGN).
  */

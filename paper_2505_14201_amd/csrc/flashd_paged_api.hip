@@ -72,7 +72,7 @@ int take_cache(const flashd_cache* c, int layer, const int* q_start, int T, Page
 
 // The packed tensors' part: T rows of Hq heads, and their storage type against the cache's.
 int take_rows(const flashd_cache* c, int T, int Hq, int dtype) {
-    if (T < 0 || T > 1000000000 || Hq < 1 || Hq > 65535 || (int64_t)T * Hq > 0x7fffffff) return FLASHD_E_SHAPE;
+    if (T < 0 || T > 10000000 || Hq < 1 || Hq > 65535 || (int64_t)T * Hq > 0x7fffffff) return FLASHD_E_SHAPE;
     if (dtype != FLASHD_F32 && dtype != FLASHD_F16 && dtype != FLASHD_BF16) return FLASHD_E_DTYPE;
     if (Hq % c->Hkv != 0) return FLASHD_E_GQA;
     if (c->dtype == FLASHD_CACHE_FP8 ? dtype == FLASHD_F32 : dtype != c->dtype) return FLASHD_E_VARIANT;

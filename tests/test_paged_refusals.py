@@ -77,6 +77,7 @@ def test_of_the_packed_tensors():
             assert call(**{name: None}) == E_NULL
         assert call(layer=1) == E_CACHE and call(layer=-1) == E_CACHE
         assert call(T=-1) == E_SHAPE and call(Hq=0) == E_SHAPE and call(T=1000000000, Hq=4) == E_SHAPE
+        assert call(T=10000001) == E_SHAPE
         assert call(Hq=5, qs=5 * 64, os=5 * 64) == E_GQA
         assert call(c=cache(dtype=flashd.F16)) == E_VARIANT           # q in another type than the cache
         assert call(qs=4 * 64 - 8) == E_SHAPE and call(os=0) == E_SHAPE
