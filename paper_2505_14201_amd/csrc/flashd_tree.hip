@@ -793,9 +793,9 @@ __global__ __launch_bounds__(kTreeWaves * kWave, rows_per_cu(D, FP8, NR)) void t
 
 // ---- 64 or 128 rows: the wavefronts read the keys together (f16 / bf16) -----------------------------
 //
-// With more rows than 32 the products outweigh the keys' way through LDS, so the four wavefronts share
-// tiles of 64 keys, in the layout of flashd_tile_parts.h, and the 32 x 32 x 16 products: wavefront w has rows 32 (w % RW) .. + 31 of the tile and every KW-th 32-key block (RW KW = 4; two wavefronts to a
-// row's keys for up to 64 rows, none share for 128).  Each wavefront brings the 16 keys of a tile that it would
+// With more rows the products outweigh the keys' way through LDS, so the four wavefronts share tiles of 64 keys, in the
+// layout of flashd_tile_parts.h, and the 32 x 32 x 16 products: wavefront w has rows 32 (w % RW) .. + 31 of the tile and
+// every KW-th 32-key block (RW KW = 4; two wavefronts to a row's keys for up to 64 rows, none share for 128).  Each wavefront brings the 16 keys of a tile that it would
 // in that layout: they lie in one page, so its copies have one scalar base.
 // (The copies are written as instructions: where the compiler knows of a copy into LDS under way, it waits for it before
 // every read of LDS that it cannot tell apart from the copy's target, and with the slot in a register it can tell
@@ -867,22 +867,59 @@ template <typename T, int D, bool ONCE> struct TileLoader<T, D, false, ONCE> {
     static __device__ __forceinline__ void wait_but() { asm volatile("s_waitcnt vmcnt(%0)" :: "n"(N * NI) : "memory"); }
 };
 
-// fp8: through registers, widened on the way
+// fp8: the bytes go straight from global memory to LDS, three tiles ahead, where each wavefront takes up its own 16 keys
+// again and writes them widened to where all read them.  (Through registers there was one tile ahead, 32 KB per compute unit: 64 trees
+// of 6 tokens over 500 to 8192 keys took 175 us.)
 template <typename T, int D, bool ONCE> struct TileLoader<T, D, true, ONCE> {
-    static constexpr int NI = D / 64;           // 1 KB each: 16 rows of D bytes
+    static constexpr int NI = D / 64;           // copies of 1 KB: the wavefront's 16 rows of D bytes
     static constexpr int LPR = D / 16;
+    static constexpr int kRaw = 2 * NI * 1024;  // bytes of the wavefront's K, then its V, of a tile
     u32x4 k[NI], v[NI];
-    __device__ __forceinline__ void start(const Window& kw, const Window& vw) {
-        const int lane = lane_now();
-        const auto kr = kw.rsrc(), vr = vw.rsrc();
+    __device__ __forceinline__ void copy(const Window& w, uint32_t at) {
+        const uint32_t from = 16 * lane_now();
+        uint32_t m0;
+        if constexpr (NI == 2 && ONCE)
+            asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %3\n\ts_nop 0\n\t"
+                         "buffer_load_dwordx4 %1, %2, 0 offen nt lds\n\t"
+                         "buffer_load_dwordx4 %1, %2, 0 offen offset:1024 nt lds\n\t"
+                         "s_mov_b32 m0, %0"
+                         : "=&s"(m0) : "v"(from), "s"(w.words), "s"(at) : "memory");
+        else if constexpr (NI == 2)
+            asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %3\n\ts_nop 0\n\t"
+                         "buffer_load_dwordx4 %1, %2, 0 offen lds\n\t"
+                         "buffer_load_dwordx4 %1, %2, 0 offen offset:1024 lds\n\t"
+                         "s_mov_b32 m0, %0"
+                         : "=&s"(m0) : "v"(from), "s"(w.words), "s"(at) : "memory");
+        else if constexpr (ONCE)
+            asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %3\n\ts_nop 0\n\t"
+                         "buffer_load_dwordx4 %1, %2, 0 offen nt lds\n\t"
+                         "s_mov_b32 m0, %0"
+                         : "=&s"(m0) : "v"(from), "s"(w.words), "s"(at) : "memory");
+        else
+            asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %3\n\ts_nop 0\n\t"
+                         "buffer_load_dwordx4 %1, %2, 0 offen lds\n\t"
+                         "s_mov_b32 m0, %0"
+                         : "=&s"(m0) : "v"(from), "s"(w.words), "s"(at) : "memory");
+    }
+    __device__ __forceinline__ void start(const Window& kw, const Window& vw, uint16_t* raw, int wave) {
+        const uint32_t at = lds_address(raw) + kRaw * wave;
+        copy(kw, at);
+        copy(vw, at + 1024 * NI);
+    }
+    // Waits until all but the wavefront's N last tiles have landed.
+    template <int N>
+    static __device__ __forceinline__ void wait_but() { asm volatile("s_waitcnt vmcnt(%0)" :: "n"(2 * N * NI) : "memory"); }
+    __device__ __forceinline__ void take(const uint16_t* raw, int wave) {
+        const u32x4* at = reinterpret_cast<const u32x4*>(reinterpret_cast<const char*>(raw) + kRaw * wave) + lane_now();
 #pragma unroll
         for (int n = 0; n < NI; ++n) {
-            k[n] = kv_load<0>(kr, 1024 * n + 16 * lane);
-            v[n] = kv_load<0>(vr, 1024 * n + 16 * lane);
+            k[n] = at[64 * n];
+            v[n] = at[64 * (NI + n)];
         }
     }
-    __device__ __forceinline__ void finish(uint16_t* ks, uint16_t* vs, int wave, int lane) {
+    __device__ __forceinline__ void put(uint16_t* ks, uint16_t* vs, int wave) {
         using C = TileCfg<D>;
+        const int lane = lane_now();
 #pragma unroll
         for (int n = 0; n < NI; ++n) {
             const int row = 16 * wave + (64 / LPR) * n + lane / LPR;
@@ -949,7 +986,10 @@ __global__ __launch_bounds__(kTreeWaves * kWave, 2) void tree_tile_kernel(TreeRu
     // Three tiles of K and two of V, 80 KB at D = 128: all of LDS in two workgroups per compute unit.  What else needs
     // LDS lies in the same memory at other times.
     __shared__ __align__(1024) uint16_t lds[5 * kTile];
-    uint16_t* const vlds = lds + 3 * kTile;
+    // (fp8: one of each, as numbers of 16 bits, and three tiles of K and V as they are stored.)
+    uint16_t* const vlds = lds + (FP8 ? 1 : 3) * kTile;
+    uint16_t* const raw = lds + 2 * kTile;
+    static_assert(!FP8 || 4 * TileLoader<T, D, true, RW == 2>::kRaw == kTile * 2, "a tile's bytes");
     float (*fold_r)[32] = reinterpret_cast<float (*)[32]>(lds + 4 * kTile), (*fold_l)[32] = fold_r + kTreeWaves;
     static_assert(kTreeWaves * 32 * D * 4 <= 4 * kTile * 2 && 2 * kTreeWaves * 32 * 4 <= kTile * 2, "the fold lies in the tiles' LDS");
 
@@ -998,12 +1038,24 @@ __global__ __launch_bounds__(kTreeWaves * kWave, 2) void tree_tile_kernel(TreeRu
             const int left = last_key - key, keys = !there || left < 0 ? 0 : left < 16 ? left : 16;
             return make_window(at, keys * ROW);
         };
-        int page1 = page_of(0), page2 = page_of(1);      // of tiles now + 1 and now + 2, once now is 0
-        const Window k0 = window(kpool, 0, page1), v0 = window(vpool, 0, page1), k1 = window(kpool, 1, page2);
-        page1 = page2;
-        page2 = page_of(2);
-        // what is copied while tile 0 is worked on; behind the last tile windows are empty and copies bring zeros
-        Window vnext = window(vpool, 1, page1), knext = window(kpool, 2, page2);
+        // the copies of tile 0's turn; behind the last tile windows are empty and copies bring zeros
+        int page1 = page_of(1), page2 = page_of(2);      // of tiles now + 1 and now + 2
+        Window vnext, knext;
+        if constexpr (FP8) {
+            const int page0 = page_of(0), page3 = page_of(3);
+            load.start(window(kpool, 0, page0), window(vpool, 0, page0), raw, wave);
+            load.start(window(kpool, 1, page1), window(vpool, 1, page1), raw + kTile, wave);
+            load.start(window(kpool, 2, page2), window(vpool, 2, page2), raw + 2 * kTile, wave);
+            knext = window(kpool, 3, page3);
+            vnext = window(vpool, 3, page3);
+        } else {
+            const int page0 = page_of(0);
+            load.start_k(window(kpool, 0, page0), lds, wave);
+            load.start_v(window(vpool, 0, page0), vlds, wave);
+            load.start_k(window(kpool, 1, page1), lds + kTile, wave);
+            vnext = window(vpool, 1, page1);
+            knext = window(kpool, 2, page2);
+        }
 
         f32x16 U[NDB];
 #pragma unroll
@@ -1020,14 +1072,6 @@ __global__ __launch_bounds__(kTreeWaves * kWave, 2) void tree_tile_kernel(TreeRu
         // (One body for all slots and both blocks: copies of it with constant operand addresses cost the code
         // that masks need several times, and with it the registers that hold U.)
         const int lane = lane_now(), col = lane & 31, hh = lane >> 5;
-        if constexpr (FP8) {
-            load.start(k0, v0);
-            load.finish(lds, vlds, wave, lane);
-        } else {
-            load.start_k(k0, lds, wave);
-            load.start_v(v0, vlds, wave);
-            load.start_k(k1, lds + kTile, wave);
-        }
         // a table with holes: which of the tile's keys have no page is looked up tile by tile
         bool gaps = false;
         for (int k = (blk0 * kBC >> page_log2) + lane; k << page_log2 < min((blk0 + tiles) * kBC, last_key); k += kWave)
@@ -1052,9 +1096,16 @@ __global__ __launch_bounds__(kTreeWaves * kWave, 2) void tree_tile_kernel(TreeRu
         for (int now = 0; now < tiles; ++now) {
             const int t = blk0 + now;
             const int k1slot = kslot == 2 ? 0 : kslot + 1;
+            int page4;
             if constexpr (FP8) {
+                // Its 16 keys are the wavefront's own affair up to the first barrier, behind which nobody reads the tile before
+                load.template wait_but<2>();
+                load.take(raw + kslot * kTile, wave);
                 barrier();
-                if (now + 1 < tiles) load.start(window(kpool, now + 1, page1), vnext);
+                load.start(knext, vnext, raw + kslot * kTile, wave);
+                page4 = page_of(now + 4);
+                load.put(lds, vlds, wave);
+                barrier();
             } else {
                 load.template wait_but<2>();
                 barrier();
@@ -1063,8 +1114,8 @@ __global__ __launch_bounds__(kTreeWaves * kWave, 2) void tree_tile_kernel(TreeRu
             }
             page1 = page2;
             page2 = page_of(now + 3);
-            const uint16_t* ks = lds + kslot * kTile;
-            const uint16_t* vs = vlds + (now & 1) * kTile;
+            const uint16_t* ks = FP8 ? lds : lds + kslot * kTile;
+            const uint16_t* vs = FP8 ? vlds : vlds + (now & 1) * kTile;
             uint32_t hole = 0;                           // 16-key groups of this tile without a page
             if (gaps) {
                 const int key = t * kBC + 16 * (lane_now() & 3);
@@ -1102,8 +1153,11 @@ __global__ __launch_bounds__(kTreeWaves * kWave, 2) void tree_tile_kernel(TreeRu
                 __builtin_amdgcn_sched_group_barrier(0x008, AHEAD, 0);
                 __builtin_amdgcn_sched_barrier(0);
             }
-            vnext = window(vpool, now + 2, page1);
-            if constexpr (!FP8) {
+            if constexpr (FP8) {
+                knext = window(kpool, now + 4, page4);
+                vnext = window(vpool, now + 4, page4);
+            } else {
+                vnext = window(vpool, now + 2, page1);
                 knext = window(kpool, now + 3, page2);
                 load.template wait_but<3>();
                 barrier();
@@ -1190,9 +1244,6 @@ __global__ __launch_bounds__(kTreeWaves * kWave, 2) void tree_tile_kernel(TreeRu
                 for (int n = 0; n < NB; ++n)
 #pragma unroll
                     for (int m = 0; m < 2 * NDB; ++m) U[m % NDB] = Mma<T>::mfma(va[n][m], bfrag[2 * n + m / NDB], U[m % NDB]);
-            }
-            if constexpr (FP8) {
-                if (now + 1 < tiles) load.finish(lds + k1slot * kTile, vlds + ((now + 1) & 1) * kTile, wave, lane_now());
             }
             kslot = k1slot;
         }
@@ -1486,14 +1537,19 @@ __global__ __launch_bounds__(256, 4) void merge_tree_kernel(TreeRun r, float vsc
 
 // ---- host ------------------------------------------------------------------------------------------
 
-// Rows of a tile: the least that hold the tokens of a sequence with one row for each head of a group.
-static int tree_rows(int Hq, int Hkv, int max_q, int dtype) {
+// Rows of a tile, chosen by how many the longest sequence has (tokens times heads of a group): the least that hold them, so that
+// its keys are read once; above 64 the tiles share a sequence's keys through L2.  32 rows only pay from an fp8 cache, where the keys'
+// way through LDS counts for more than their bytes: 24 rows, 64 sequences of 500 to 8192 keys, d = 128: 147 us with 32 and
+// 144 with 64, d = 64: 101 and 116; from bf16, 32 such sequences: 144 and 117, d = 64: 64 and 64.  16 rows against 64 for 4 rows of
+// 64 sequences: 192 and 198 us, fp8 115 and 156, one short sequence 15 and 19.  128 against 64 for chunks of 1000
+// tokens: 401 and 562.
+static int tree_rows(int Hq, int Hkv, int max_q, int dtype, bool fp8) {
     const long rows = (long)max_q * (Hq / Hkv);
-    return dtype == 0 || rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : 128;
+    return dtype == 0 || rows <= 16 ? 16 : rows <= 32 && fp8 ? 32 : rows <= 64 ? 64 : 128;
 }
 
 size_t attn_tree_workspace(int Hq, int Hkv, int max_q, int d, int dtype) {
-    const int rows = tree_rows(Hq, Hkv, max_q, dtype);
+    const int rows = tree_rows(Hq, Hkv, max_q, dtype, false);
     return (size_t)2 * kTreeMostGroups * rows * (d + 2) * sizeof(float) + kTreeMostGroups * sizeof(TreeSplit);
 }
 
@@ -1502,18 +1558,18 @@ static hipError_t launch_tree_m(TreeRun& r, hipStream_t st) {
     const dim3 block(kTreeWaves * kWave);
     r.stats = reinterpret_cast<float2*>(r.parts + (size_t)2 * kTreeMostGroups * M * D);
     r.splits = reinterpret_cast<TreeSplit*>(r.stats + (size_t)2 * kTreeMostGroups * M);
-    if constexpr (std::is_same_v<T, F32>) r.groups = 512;
-    else if constexpr (M <= 32) r.groups = 256 * (r.a.fp8 ? rows_per_cu(D, true, M / 16) : rows_per_cu(D, false, M / 16));
-    else r.groups = 512;
-    const dim3 grid(r.groups);
-    if constexpr (std::is_same_v<T, F32>) {
-        hipLaunchKernelGGL((tree_rows_f32_kernel<D>), grid, block, 0, st, r);
-    } else if constexpr (M <= 32) {
-        if (r.a.fp8) hipLaunchKernelGGL((tree_rows_kernel<T, D, true, M / 16>), grid, block, 0, st, r);
-        else hipLaunchKernelGGL((tree_rows_kernel<T, D, false, M / 16>), grid, block, 0, st, r);
+    auto launch = [&](auto* kernel, int groups) {
+        r.groups = groups;
+        hipLaunchKernelGGL(kernel, dim3((unsigned)groups), block, 0, st, r);
+    };
+    if constexpr (std::is_same_v<T, F32>) launch(tree_rows_f32_kernel<D>, 512);
+    else if constexpr (M == 32) launch(tree_rows_kernel<T, D, true, 2>, 256 * rows_per_cu(D, true, 2));
+    else if constexpr (M == 16) {
+        if (r.a.fp8) launch(tree_rows_kernel<T, D, true, 1>, 256 * rows_per_cu(D, true, 1));
+        else launch(tree_rows_kernel<T, D, false, 1>, 256 * rows_per_cu(D, false, 1));
     } else {
-        if (r.a.fp8) hipLaunchKernelGGL((tree_tile_kernel<T, D, true, M / 32>), grid, block, 0, st, r);
-        else hipLaunchKernelGGL((tree_tile_kernel<T, D, false, M / 32>), grid, block, 0, st, r);
+        if (r.a.fp8) launch(tree_tile_kernel<T, D, true, M / 32>, 512);
+        else launch(tree_tile_kernel<T, D, false, M / 32>, 512);
     }
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
@@ -1527,7 +1583,7 @@ static hipError_t launch_tree_t(TreeRun& r, hipStream_t st) {
     if constexpr (std::is_same_v<T, F32>) {
         return launch_tree_m<T, D, 16>(r, st);
     } else {
-        switch (tree_rows(r.a.Hq, r.c.Hkv, r.a.max_q, r.a.dtype)) {
+        switch (tree_rows(r.a.Hq, r.c.Hkv, r.a.max_q, r.a.dtype, r.a.fp8 != 0)) {
         case 16: return launch_tree_m<T, D, 16>(r, st);
         case 32: return launch_tree_m<T, D, 32>(r, st);
         case 64: return launch_tree_m<T, D, 64>(r, st);
