@@ -248,7 +248,7 @@ __device__ __forceinline__ int block_scan(int x, int* waves, int& total) {
 
 __global__ __launch_bounds__(kReserveThreads) void reserve_kernel(Paged c, int* refs, int* report) {
     __shared__ int at[kCacheMaxSeqs + 1];        // wanted pages of the sequences before b
-    __shared__ int last[kCacheMaxSeqs];          // part-filled last page of a sequence that grows, or -1
+    __shared__ __align__(16) int last[kCacheMaxSeqs];        // part-filled last page of a sequence that grows, or -1
     __shared__ int2 cols[kCacheMaxSeqs];         // that page's column (with kCopy: a copy is wanted), and the column behind the last
     __shared__ int count[kReserveBlocks];        // free pages of the blocks before
     __shared__ int waves[kReserveWaves];
@@ -258,6 +258,7 @@ __global__ __launch_bounds__(kReserveThreads) void reserve_kernel(Paged c, int* 
     const int mask = (1 << c.page_log2) - 1;
     const int each = (c.B + kReserveThreads - 1) / kReserveThreads;
     if (tid == 0) beyond = 0;
+    if (tid < (-c.B & 3)) last[c.B + tid] = -1;          // read four at a time
 
     // 1. back to the pool
     for (int k = 0; k < each; ++k) {
@@ -309,10 +310,16 @@ __global__ __launch_bounds__(kReserveThreads) void reserve_kernel(Paged c, int* 
             want = end - lo;
             if (refs_p > 1) {
                 int holders = 0, before = 0;
-                for (int o = 0; o < c.B; ++o) {
-                    const bool same = last[o] == p;
-                    holders += same ? 1 : 0;
-                    before += same && o < b ? 1 : 0;
+#pragma unroll 4
+                for (int o = 0; o < c.B; o += 4) {
+                    const int4 x = *reinterpret_cast<const int4*>(&last[o]);
+                    const int four[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const bool same = four[i] == p;
+                        holders += same ? 1 : 0;
+                        before += same && o + i < b ? 1 : 0;
+                    }
                 }
                 copy = holders < refs_p || before > 0;
             }
