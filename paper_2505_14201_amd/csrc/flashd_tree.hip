@@ -503,7 +503,7 @@ __device__ __forceinline__ Window half_window(const Paged& c, const W& u, const 
 // keys behind it, and pages that are none, read zeros.
 //
 // In blocks with new keys a weight of zero may meet a value that is infinite or NaN (a token that some rows see
-// and others do not), and 0 * infinity must not reach the others: see take_apart().
+// and others do not), and 0 * infinity must not reach the others: see codes_of().
 
 // (All of this on pairs of halves, by carries into their top bits: comparisons hand their results to scalar registers, and the
 // dozens of a block's values in flight took those that the loops around hold their addresses in.)
@@ -571,6 +571,14 @@ __device__ __forceinline__ float if_seen(uint32_t bits, int i, float x) {
     return __uint_as_float((m & __float_as_uint(x)) | (~m & 0xff800000u));
 }
 
+// The lane's number, formed anew: what depends on it is then formed where it is used.  Kept over the loop those addresses were
+// spilled, and the wait for one to come back is one for every copy under way.
+__device__ __forceinline__ int lane_now() {
+    int x;
+    asm volatile("v_mbcnt_lo_u32_b32 %0, -1, 0\n\tv_mbcnt_hi_u32_b32 %0, -1, %0" : "=v"(x));
+    return x;
+}
+
 // Workgroups per compute unit: what one has under way is its wavefronts' next block of K and of V.  Of fp8, or at
 // d = 64, that is half as much, and three workgroups' registers fit.
 constexpr int rows_per_cu(int D, bool FP8, int NR) { return (D == 64 || FP8) && NR == 1 ? 3 : 2; }
@@ -586,6 +594,11 @@ __global__ __launch_bounds__(kTreeWaves * kWave, rows_per_cu(D, FP8, NR)) void t
     constexpr int KROW = D + 8;
     constexpr int VROW = D + 16;
     constexpr int STAGE = kTreeBlock * VROW;
+    // fp8: a lane writes 32 bytes, in two pieces.  In the second half of a row of 256 bytes pieces 2 i and 2 i + 1 change
+    // places, so that the first pieces of a row's 8 lanes fall on all banks, and the addresses are formed where they are used.
+    // With 32 rows that took 147 us to 138 (24 rows, 64 sequences of 500 to 8192 keys); with 16, where 44 % of the time that LDS is busy
+    // goes to such conflicts, it made 111 us 114.
+    constexpr bool SWAP = FP8 && D == 128 && NR == 2;
     constexpr int FROW = D + 4;
     constexpr int kLds = 2 * W * STAGE > 4 * W * 16 * FROW ? 2 * W * STAGE : 4 * W * 16 * FROW;
     __shared__ __align__(16) char lds[kLds];
@@ -645,13 +658,15 @@ __global__ __launch_bounds__(kTreeWaves * kWave, rows_per_cu(D, FP8, NR)) void t
             }
         };
         auto stage = [&](const u32x4 (&reg)[NV], int ROW) __attribute__((always_inline)) {
+            const int x0 = SWAP ? lane_now() : lane;
 #pragma unroll
             for (int n = 0; n < NV; ++n) {
-                const int ch = n * kWave + lane;
+                const int ch = n * kWave + x0;
                 uint16_t* dst = &vs[(ch / CPR) * ROW + (FP8 ? 16 : 8) * (ch % CPR)];
                 if constexpr (FP8) {
-                    *reinterpret_cast<u32x4*>(dst) = widen8<T>(reg[n][0], reg[n][1]);
-                    *reinterpret_cast<u32x4*>(dst + 8) = widen8<T>(reg[n][2], reg[n][3]);
+                    const int x = SWAP ? 8 * (ch % CPR >> 2) : 0;
+                    *reinterpret_cast<u32x4*>(dst + x) = widen8<T>(reg[n][0], reg[n][1]);
+                    *reinterpret_cast<u32x4*>(dst + (8 ^ x)) = widen8<T>(reg[n][2], reg[n][3]);
                 } else {
                     *reinterpret_cast<u32x4*>(dst) = reg[n];
                 }
@@ -694,6 +709,8 @@ __global__ __launch_bounds__(kTreeWaves * kWave, rows_per_cu(D, FP8, NR)) void t
             const int m0 = page_of(blk + 2 * W, 0), m1 = page_of(blk + 2 * W, 1);
             stage(kreg, KROW);
             fetch(kpool, kreg, blk + W, n0, n1);
+            const int z = SWAP ? lane_now() : lane, kcol = (z & 15) * KROW;
+            const uint16_t* const krow[2] = {&vs[kcol + 8 * (z >> 4)], &vs[kcol + 8 * (z >> 4 ^ (SWAP ? 1 : 0))]};
             f32x4 acc[NR][2];
 #pragma unroll
             for (int k = 0; k < NR; ++k)
@@ -703,7 +720,7 @@ __global__ __launch_bounds__(kTreeWaves * kWave, rows_per_cu(D, FP8, NR)) void t
             for (int kk = 0; kk < NKK; ++kk)
 #pragma unroll
                 for (int t = 0; t < 2; ++t) {
-                    const u32x4 x = *reinterpret_cast<const u32x4*>(&vs[(16 * t + col) * KROW + 32 * kk + 8 * q]);
+                    const u32x4 x = *reinterpret_cast<const u32x4*>(&krow[kk >> 1][16 * t * KROW + 32 * kk]);
 #pragma unroll
                     for (int k = 0; k < NR; ++k) acc[k][t] = Mma16<T>::mfma(x, qf[k][kk], acc[k][t]);
                 }
@@ -742,9 +759,11 @@ __global__ __launch_bounds__(kTreeWaves * kWave, rows_per_cu(D, FP8, NR)) void t
                 Mma<T>::sum8(pv, bfrag[k], ps);
                 l[k] += (ps[0] + ps[1]) + (ps[2] + ps[3]);
             }
-            const uint16_t* base = &vs[(4 * q + (col >> 2)) * VROW + 4 * (col & 3)];
+            const int y = SWAP ? lane_now() : lane, vrow = (4 * (y >> 4) + (y >> 2 & 3)) * VROW;
+            const uint16_t* const bases[2] = {&vs[vrow + 4 * (y & 3)], &vs[vrow + (4 * (y & 3) ^ 8)]};
             typedef s16x4 __attribute__((address_space(3))) * lds_ptr;
             auto v_operand = [&](int i) __attribute__((always_inline)) {
+                const uint16_t* base = bases[SWAP && i >= 4 ? 1 : 0];
                 const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
                     (lds_ptr)(base + 16 * i)));
                 const u32x2 hi = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
@@ -804,13 +823,6 @@ __global__ __launch_bounds__(kTreeWaves * kWave, rows_per_cu(D, FP8, NR)) void t
 __device__ __forceinline__ void barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 __device__ __forceinline__ uint32_t lds_address(const void* p) {
     return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) char*)p;
-}
-// The lane's number, formed anew: what depends on it is then formed where it is used.  Kept over the loop those addresses were
-// spilled, and the wait for one to come back is one for every copy under way.
-__device__ __forceinline__ int lane_now() {
-    int x;
-    asm volatile("v_mbcnt_lo_u32_b32 %0, -1, 0\n\tv_mbcnt_hi_u32_b32 %0, -1, %0" : "=v"(x));
-    return x;
 }
 template <typename T, int D, bool FP8, bool ONCE> struct TileLoader;
 
@@ -1539,8 +1551,8 @@ __global__ __launch_bounds__(256, 4) void merge_tree_kernel(TreeRun r, float vsc
 
 // Rows of a tile, chosen by how many the longest sequence has (tokens times heads of a group): the least that hold them, so that
 // its keys are read once; above 64 the tiles share a sequence's keys through L2.  32 rows only pay from an fp8 cache, where the keys'
-// way through LDS counts for more than their bytes: 24 rows, 64 sequences of 500 to 8192 keys, d = 128: 147 us with 32 and
-// 144 with 64, d = 64: 101 and 116; from bf16, 32 such sequences: 144 and 117, d = 64: 64 and 64.  16 rows against 64 for 4 rows of
+// way through LDS counts for more than their bytes: 24 rows, 64 sequences of 500 to 8192 keys, d = 128: 138 us with 32 and
+// 145 with 64, d = 64: 87 and 108; from bf16, 32 such sequences: 144 and 117, d = 64: 64 and 64.  16 rows against 64 for 4 rows of
 // 64 sequences: 192 and 198 us, fp8 115 and 156, one short sequence 15 and 19.  128 against 64 for chunks of 1000
 // tokens: 401 and 562.
 static int tree_rows(int Hq, int Hkv, int max_q, int dtype, bool fp8) {
