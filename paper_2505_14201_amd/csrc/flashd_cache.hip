@@ -24,7 +24,10 @@ typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
 //
 // PASSES: how many rows a lane's place in the workgroup takes, all loaded before anything else.  Long
 // calls want few workgroups per token (the search for its sequence and its angles are done in each of them): 12696 tokens of
-// 32 + 2 x 8 heads of 128 took 92 us with a workgroup for every 16 rows.  Short ones want the rows spread.
+// 32 + 2 x 8 heads of 128 take 78 us (312 MB, 4.0 TB/s; a plain copy moves 5.2) and took 92 with a workgroup for every 16
+// rows.  Short ones want the rows spread: 64 tokens take 4.3 us, all of it latency.  (Workgroups that walk many tokens, the
+// next one's rows on their way, were not ahead: 76 us with as many as fit on the chip at once, 83 to 102 with more or
+// fewer.)
 template <typename T, int D, bool FP8, int PASSES>
 __global__ __launch_bounds__(256) void append_kernel(Paged c, AppendArgs a) {
     constexpr int LPR = D / 8;                  // lanes per row
@@ -182,7 +185,7 @@ hipError_t launch_cache_append(const Paged& c, const AppendArgs& a, hipStream_t 
 //
 // table_out[i] = table[parent[i]]; refs[p] counts the table entries that name page p, so every entry
 // that changes takes one off the page it named and puts one on the page it names.  Sums of whole
-// numbers: the order of the atomics does not matter.
+// numbers: the order of the atomics does not matter.  64 sequences from 32: 3 us, the launch's latency.
 __global__ __launch_bounds__(256) void fork_kernel(Paged c, int* refs, const int* parent, int B_out,
                                                    int* table_out, int* lens_out) {
     const int i = blockIdx.y;
@@ -219,6 +222,8 @@ hipError_t launch_cache_fork(const Paged& c, int* refs, const int* parent, int B
 //      page's only holders and all grow: that one keeps it);
 //   3. free pages (refs 0) are numbered in ascending order, k-th free page -> k-th wanted page.
 // Should there be too few, step 3 is left out and the number missing reported.
+// Latency bounds it, eight reads one after the other: 5.2 us for 32 sequences, 11 for 64 whose table and counts another
+// kernel has just written (they come from beyond this die's L2).
 constexpr int kReserveThreads = 1024;
 constexpr int kReserveWaves = kReserveThreads / kWave;
 constexpr int kReserveBlocks = 4096;      // the pool is counted in at most that many blocks of 256 m pages
@@ -395,7 +400,7 @@ __global__ __launch_bounds__(kReserveThreads) void reserve_kernel(Paged c, int* 
 }
 
 // Rows of the part-filled page that report names into the page that the sequence now has there.
-// Workgroup (b, j) takes every gridDim.y-th of the 2 * layers * Hkv pieces.
+// Workgroup (b, j) takes every gridDim.y-th of the 2 * layers * Hkv pieces.  67 MB, read and written, in 13 us: 5.1 TB/s.
 __global__ __launch_bounds__(256) void copy_rows_kernel(Paged c, const int* report) {
     const int b = blockIdx.x;
     const int from = report[1 + b];
@@ -428,7 +433,8 @@ hipError_t launch_cache_reserve(const Paged& c, int* refs, int* report, hipStrea
 // Of a sequence's new tokens those that keep[] names (ascending) move together behind its keys: key
 // len + keep[i] -> len + i.  As keep[i] >= i, rows may be moved in ascending groups, each group read whole
 // before it is written: what a group writes lies before everything that later groups read.  A
-// wavefront moves the rows of one (layer, K or V, head).
+// wavefront moves the rows of one (layer, K or V, head), eight such pieces under way.  Up to 6 rows for each of 32 sequences, 32
+// layers of 2 x 8 heads of 128: 42 MB, read and written, in 9.5 us, 4.4 TB/s.
 template <int RB>       // bytes of a row
 __global__ __launch_bounds__(256) void commit_kernel(Paged c, const int* keep, int max_keep,
                                                      const int* n_keep, int* lens_out) {

@@ -502,6 +502,10 @@ __device__ __forceinline__ Window half_window(const Paged& c, const W& u, const 
 // has a base address of its own, through a buffer descriptor that ends at the sequence's last key:
 // keys behind it, and pages that are none, read zeros.
 //
+// HBM bounds it: a token for each of 64 sequences of 500 to 8192 keys, 32 / 8 heads of 128, takes 178 us for 1.17 GB read once,
+// 6.6 TB/s; from fp8, four tokens each, 100 us for 588 MB, 5.9 TB/s, a wavefront waiting for memory or for its turn
+// three quarters of its time.  One sequence of 1000 keys takes 6.6 us, the latency of finding a share, its pages and its keys.
+//
 // In blocks with new keys a weight of zero may meet a value that is infinite or NaN (a token that some rows see
 // and others do not), and 0 * infinity must not reach the others: see codes_of().
 
@@ -816,6 +820,14 @@ __global__ __launch_bounds__(kTreeWaves * kWave, rows_per_cu(D, FP8, NR)) void t
 // layout of flashd_tile_parts.h, and the 32 x 32 x 16 products: wavefront w has rows 32 (w % RW) .. + 31 of the tile and
 // every KW-th 32-key block (RW KW = 4; two wavefronts to a row's keys for up to 64 rows, none share for 128).  Each wavefront brings the 16 keys of a tile that it would
 // in that layout: they lie in one page, so its copies have one scalar base.
+//
+// Up to 64 rows HBM bounds it: trees of 16 tokens after 500 to 8192 keys (32 sequences, 32 / 8 heads of 128) take 110 us for
+// 600 MB, 5.5 TB/s, one of 12 after 131000 keys 91 us, 5.9 TB/s; the start of a piece, when nothing of it has arrived, and
+// the unequal pace of the workgroups are the rest.  With 128 rows it is the instructions: chunks of 573 to 1000 tokens after 3180 to
+// 7000 keys are 277 GFLOP in 351 us, 790 TFLOP/s; the matrix pipe works 37 % of the cycles, the vector units 44 %, and
+// a wavefront's vector instructions do not run beside its own matrix instructions: with the weights of a tile formed between the
+// output products of the tile before it took 386 us.
+//
 // (The copies are written as instructions: where the compiler knows of a copy into LDS under way, it waits for it before
 // every read of LDS that it cannot tell apart from the copy's target, and with the slot in a register it can tell
 // none: the copies of tile t + 1 then ended before the math of tile t began.)
@@ -1309,7 +1321,8 @@ __global__ __launch_bounds__(kTreeWaves * kWave, 2) void tree_tile_kernel(TreeRu
 // operand: the lane's float4 at dims 16 m + 4 q serves four products, each summing dims 16 m + 4 q' + e over
 // q'.  The scores it gets are keys 4 q + r of its row: as B operand of O^T = V^T P^T product r sums
 // the keys 4 q' + r over q', for which the lane's A element is V[4 q + r][16 i + c].  Nothing goes
-// through LDS.
+// through LDS.  One token for each of 64 sequences of 500 to 8192 keys, 32 / 8 heads of 128: 465 us with the merge, 2.34 GB, 5.0
+// TB/s; more than 16 rows read their keys anew for each 16 and run at 46 TFLOP/s.
 template <int D>
 __global__ __launch_bounds__(kTreeWaves * kWave, 2) void tree_rows_f32_kernel(TreeRun r) {
     constexpr int W = kTreeWaves;
@@ -1412,7 +1425,8 @@ __global__ __launch_bounds__(kTreeWaves * kWave, 2) void tree_rows_f32_kernel(Tr
 // groups of a workgroup take a row each, or share the parts of one row where a unit has many (more than
 // kMergeShare: one long sequence over the whole chip).  Each thread of a workgroup keeps the splits of a few of the
 // launch's workgroups, and the one that holds the next rows' hands it over through LDS: between a workgroup's start
-// and its rows lies one read from memory.  M: rows of a tile.  What bounds it is the time of its reads, so that many workgroups
+// and its rows lies one read from memory.  M: rows of a tile.  8 units of 4 rows in 8 parts take 3.9 us, 512 of 128 rows in 2 and 3
+// parts (67 MB) 18.6.  What bounds it is the time of its reads, so that many workgroups
 // are under way at once where there are many rows.
 constexpr int kMergeShare = 12;
 constexpr int merge_groups(int M) { return M <= 32 ? 512 : M == 64 ? 1024 : 2048; }
