@@ -298,7 +298,8 @@ int flashd_skip_stats(const void* q, const void* k, int B, int Hq, int Hkv, int 
  * in the order of the stream, so a step can be recorded into a HIP graph and replayed with other numbers
  * in the same places.  Numbers found there never lead outside the buffers given: a page number outside
  * [0, P) is no page (its keys weigh nothing, what would be written to it is dropped), a
- * sequence ends at max_pages * page keys and its tokens at row T.
+ * sequence ends at max_pages * page keys and its tokens at row T (tokens behind that end have no key, and
+ * flashd_attn_fwd_tree does not write their rows).
  * Limits: B at most 4096, page 16, 32, 64, 128 or 256, max_pages * page at most 10^9, T 10^7, B * max_pages and T * Hq
  * below 2^31.
  * Pointers to elements of pools and packed tensors and the strides of rows, pages and layers are

@@ -441,7 +441,14 @@ int run(const void* q, const void* k, const void* v, void* o, const Shape& s, in
 
 namespace flashd {
 int api_check_arch() { return check_arch(); }
-int api_cached_workspace(void* stream, size_t bytes, void** out) { return cached_workspace(stream, bytes, out); }
+int api_cached_workspace(void* stream, size_t bytes, void** out) {
+    try {
+        return cached_workspace(stream, bytes, out);
+    } catch (...) {                          // no host memory for the entry: nothing leaves a C function
+        *out = nullptr;
+        return FLASHD_E_HIP;
+    }
+}
 }  // namespace flashd
 
 extern "C" {

@@ -282,6 +282,31 @@ def test_steps_without_tokens():
     torch.cuda.synchronize()
 
 
+def test_tokens_behind_the_end_of_the_table():
+    """Two columns of 16 keys: of 5 tokens behind 30 keys two have a key, as reserve says; the others' queries are
+    formed, their outputs left as they were."""
+    c = pu.make([30, 3], [2, 2], 2, 64, 16, "bf16", seed=78)
+    q = pu.queries(pu.Paged(c.k, c.v, c.table, [30, 3], [5, 2]), 4, "bf16", seed=79)
+    k, v, table, lens, _ = c.gpu()
+    starts = pu.ints([0, 5, 7]).cuda()
+    refs = torch.zeros(k.shape[0], dtype=torch.int32, device="cuda")
+    refs[table[table >= 0].long()] = 1
+    report = torch.empty(3, dtype=torch.int32, device="cuda")
+    flashd.cache_reserve(k, v, refs, table, lens, starts, report)
+    assert int(report[0]) == 1
+    qg, out = q.cuda(), torch.full((7, 4, 64), 9.0, dtype=torch.bfloat16, device="cuda")
+    for hint in HINTS:
+        o = torch.full_like(out, 7)
+        flashd.attn_fwd_tree(qg, k, v, o, table, lens, starts, hint, 0.125)
+        torch.cuda.synchronize()
+        assert (o[2:5] == 7).all()
+        check(c, torch.cat([q[:2], q[5:]]), "bf16", 0.125, got=torch.cat([o[:2], o[5:]]).cpu())
+    new = torch.ones(7, 2, 64, dtype=torch.bfloat16, device="cuda")
+    flashd.cache_append(qg, new, new, out, k, v, table, lens, starts)
+    torch.cuda.synchronize()
+    assert torch.equal(out, qg)
+
+
 def test_wild_numbers_on_the_device_stay_inside():
     """Lengths, starts and pages that no program should leave there: nothing outside the tensors is touched and the
     call ends.  (Starts that fall, lengths below zero and past the table, pages behind the pool.)"""
