@@ -31,6 +31,11 @@ constexpr int kTreeMinBlocks = 4;       // blocks a workgroup takes at least
 // 27.8, 26.8, 26.3, 25.4 and 25.8 us for 128 units of 17 to 64 tiles, and for long units it made no difference; the rows kernel
 // took 103.8 us with 0 and 103.7 with 8, its own steps being shorter.
 constexpr int kRowsStart = 0, kTileStart = 3;
+// By how many 64ths the first workgroup of a compute unit gets more than the mean and the second less: the older wavefronts are
+// served first, so that with equal shares the first ones of the tile kernel ended after 309 us and the second after 384 (chunks
+// of 1000 tokens).  With 0, 4, 6, 8, 10 and 14 the kernel took 365, 355, 351, 345, 343 and 352 us, for trees of 16 tokens with 0, 2,
+// 4, 6, 8 and 10 111, 109, 110, 109, 108 and 110.  The rows kernel is bound by HBM from first to last: 177 and 176 us with 0 to 20.
+constexpr int kRowsLead = 0, kTileLead = 8;
 
 // Waits until all but the last N loads have arrived.
 template <int N> __device__ __forceinline__ void wait_loads() {
@@ -138,11 +143,14 @@ struct WalkScratch {
 // A workgroup's way along the row of blocks, and the piece of a unit that it is at (all the same in every
 // thread, in scalar registers).  M: rows of a tile; KB: keys of a block of the row.  Of a chain's row tile only the blocks count
 // that its last token sees.  A unit begins with START places without a block, for the time that its first keys and its
-// queries take to arrive: a workgroup with more units gets fewer blocks.  GRID: workgroups of the launch.
-template <int M, int KB, int GRID, int START>
+// queries take to arrive: a workgroup with more units gets fewer blocks.  GRID: workgroups of the launch, LEAD: by how many
+// 64ths the share of a compute unit's first workgroup is above the mean, and that of its last below it.
+template <int M, int KB, int GRID, int START, int LEAD>
 struct Walk {
+    static constexpr int kSlots = GRID / 256;       // workgroups of a compute unit
+    static constexpr int kOfXcd = GRID / 8;         // workgroups of an XCD, 32 of each slot
     long long at, end;      // places of the long row
-    long long per;          // places of every workgroup
+    long long per, lead;    // places of a workgroup, and what first and last slots have more and less
     int w;                  // the workgroup's place along the row
     int b, h, tile;         // present unit
     Seq s;
@@ -151,6 +159,19 @@ struct Walk {
     int from;               // the place in the unit at which the piece begins
     int blk0, blk1;         // the piece
     int first, nrows;       // its first row (token, head of the group), and rows
+
+    // Along the row come, XCD by XCD, the 32 workgroups of each slot.
+    __device__ __forceinline__ long long size(int slot) const {
+        return slot == 0 ? per + lead : slot == kSlots - 1 ? per - lead : per;
+    }
+    __device__ __forceinline__ long long begin_of(int slot) const { return slot == 0 ? 0 : 32 * (slot * per + lead); }
+    __device__ __forceinline__ int holder(long long place) const {
+        const long long x = quotient(place, kOfXcd * per), r = place - x * (kOfXcd * per);
+        int slot = 0;
+#pragma unroll
+        for (int j = 1; j < kSlots; ++j) slot = r >= begin_of(j) ? j : slot;
+        return (int)x * kOfXcd + 32 * slot + (int)quotient(r - begin_of(slot), size(slot));
+    }
 
     __device__ __forceinline__ bool whole() const { return blk0 == 0 && blk1 == blocks; }
     __device__ __forceinline__ int keys() const { return s.len + s.n; }
@@ -231,14 +252,17 @@ struct Walk {
         constexpr int kLeast = kTreeMinBlocks * kTreeBlock / KB;
         const bool few = total <= (long long)kLeast * GRID;
         per = few ? kLeast : quotient(total + GRID - 1, GRID);
-        const int groups = (int)quotient(total + per - 1, per);
+        lead = few ? 0 : (per * LEAD) >> 6;
         // Workgroup ids go round-robin over the 8 XCDs; neighbours along the row, which may read the same
-        // keys, go to one.
-        const int of_xcd = (groups + 7) >> 3;
+        // keys, go to one.  An XCD's first 32 go to a compute unit each, the next 32 beside them, and so on.
+        const int of_xcd = few ? ((int)quotient(total + kLeast - 1, kLeast) + 7) >> 3 : kOfXcd;
         const int k = (int)blockIdx.x >> 3;
         w = ((int)blockIdx.x & 7) * of_xcd + k;
-        at = k < of_xcd && w < groups ? per * w : total;
-        end = at + per < total ? at + per : total;
+        const int place = w % kOfXcd;
+        at = w / kOfXcd * (kOfXcd * per) + begin_of(place >> 5) + (place & 31) * size(place >> 5);
+        end = at + size(place >> 5);
+        if (k >= of_xcd || at > total) at = total;
+        if (end > total) end = total;
         if (tid == 0) r.splits[blockIdx.x].parts = 0;
         if (at < end && at >= before && at < before + mine) {
             int i = b0;
@@ -320,7 +344,7 @@ struct Walk {
         sp.h = h;
         sp.first = first;
         sp.rows = nrows;
-        sp.parts = (int)quotient(at + START + blocks - from - 1, per) - w + 1;
+        sp.parts = holder(at + START + blocks - from - 1) - w + 1;
         sp.w = w;
         r.splits[blockIdx.x] = sp;
     }
@@ -616,7 +640,7 @@ __global__ __launch_bounds__(kTreeWaves * kWave, rows_per_cu(D, FP8, NR)) void t
     const float ninf = -__builtin_inff();
     uint16_t* vs = reinterpret_cast<uint16_t*>(lds) + wave * STAGE;
 
-    Walk<16 * NR, kTreeBlock, 256 * rows_per_cu(D, FP8, NR), kRowsStart> u;
+    Walk<16 * NR, kTreeBlock, 256 * rows_per_cu(D, FP8, NR), kRowsStart, kRowsLead> u;
     if (!u.begin(args_now(), reinterpret_cast<WalkScratch*>(lds))) return;
     do {
         // the query rows of this lane's column; columns past the last row stand in for it
@@ -824,7 +848,7 @@ __global__ __launch_bounds__(kTreeWaves * kWave, rows_per_cu(D, FP8, NR)) void t
 // Up to 64 rows HBM bounds it: trees of 16 tokens after 500 to 8192 keys (32 sequences, 32 / 8 heads of 128) take 110 us for
 // 600 MB, 5.5 TB/s, one of 12 after 131000 keys 91 us, 5.9 TB/s; the start of a piece, when nothing of it has arrived, and
 // the unequal pace of the workgroups are the rest.  With 128 rows it is the instructions: chunks of 573 to 1000 tokens after 3180 to
-// 7000 keys are 277 GFLOP in 351 us, 790 TFLOP/s; the matrix pipe works 37 % of the cycles, the vector units 44 %, and
+// 7000 keys are 277 GFLOP in 344 us, 805 TFLOP/s; the matrix pipe works 37 % of the cycles, the vector units 44 %, and
 // a wavefront's vector instructions do not run beside its own matrix instructions: with the weights of a tile formed between the
 // output products of the tile before it took 386 us.
 //
@@ -1022,7 +1046,7 @@ __global__ __launch_bounds__(kTreeWaves * kWave, 2) void tree_tile_kernel(TreeRu
     const int rw = wave & (RW - 1), kw = wave / RW;
     const float ninf = -__builtin_inff();
 
-    Walk<M, kBC, 512, kTileStart> u;
+    Walk<M, kBC, 512, kTileStart, kTileLead> u;
     if (!u.begin(args_now(), reinterpret_cast<WalkScratch*>(lds))) return;
 
     TileLoader<T, D, FP8, RW == 2> load;        // (up to 64 rows a sequence is one row tile: its keys are read once)
@@ -1338,7 +1362,7 @@ __global__ __launch_bounds__(kTreeWaves * kWave, 2) void tree_rows_f32_kernel(Tr
     const int q = lane >> 4;
     const float ninf = -__builtin_inff();
 
-    Walk<16, kTreeBlock, 512, kRowsStart> u;
+    Walk<16, kTreeBlock, 512, kRowsStart, kRowsLead> u;
     if (!u.begin(r, reinterpret_cast<WalkScratch*>(fold))) return;
     do {
         const int row = u.first + min(col, u.nrows - 1);
