@@ -145,7 +145,9 @@ struct WalkScratch {
 // that its last token sees.  A unit begins with START places without a block, for the time that its first keys and its
 // queries take to arrive: a workgroup with more units gets fewer blocks.  GRID: workgroups of the launch, LEAD: by how many
 // 64ths the share of a compute unit's first workgroup is above the mean, and that of its last below it.
-template <int M, int KB, int GRID, int START, int LEAD>
+// LATE: a share that begins inside a unit takes that piece last, so that workgroups of one head, whose other units begin at
+// their first key, meet the same keys at the same time.
+template <int M, int KB, int GRID, int START, int LEAD, bool LATE>
 struct Walk {
     static constexpr int kSlots = GRID / 256;       // workgroups of a compute unit
     static constexpr int kOfXcd = GRID / 8;         // workgroups of an XCD, 32 of each slot
@@ -159,6 +161,9 @@ struct Walk {
     int from;               // the place in the unit at which the piece begins
     int blk0, blk1;         // the piece
     int first, nrows;       // its first row (token, head of the group), and rows
+    bool later = false;     // the share's first piece is still to be done: its place
+    long long later_at;
+    int later_b, later_h, later_tile, later_from;
 
     // Along the row come, XCD by XCD, the 32 workgroups of each slot.
     __device__ __forceinline__ long long size(int slot) const {
@@ -314,10 +319,34 @@ struct Walk {
         }
         set_unit(r);
         set_piece(uniform((int)rest));
+        if constexpr (LATE) {
+            if (blk0 > 0 && end - at > START + blocks - from) {
+                later_at = at;
+                later_b = b;
+                later_h = h;
+                later_tile = tile;
+                later_from = from;
+                later = true;
+                return next(r);
+            }
+        }
         return blk0 < blk1 || next(r);
     }
     // On to the next piece with keys; false at the end of the share.
     __device__ __forceinline__ bool next(const TreeRun& r) {
+        if (advance(r)) return true;
+        if (!LATE || !later) return false;
+        later = false;
+        at = later_at;
+        enter<true>(r, later_b);
+        h = later_h;
+        tile = later_tile;
+        set_unit(r);
+        end = at + START + blocks - later_from;
+        set_piece(later_from);
+        return true;
+    }
+    __device__ __forceinline__ bool advance(const TreeRun& r) {
         int place = from;
         do {
             at += min((long long)START + blocks - place, end - at);
@@ -640,7 +669,7 @@ __global__ __launch_bounds__(kTreeWaves * kWave, rows_per_cu(D, FP8, NR)) void t
     const float ninf = -__builtin_inff();
     uint16_t* vs = reinterpret_cast<uint16_t*>(lds) + wave * STAGE;
 
-    Walk<16 * NR, kTreeBlock, 256 * rows_per_cu(D, FP8, NR), kRowsStart, kRowsLead> u;
+    Walk<16 * NR, kTreeBlock, 256 * rows_per_cu(D, FP8, NR), kRowsStart, kRowsLead, false> u;
     if (!u.begin(args_now(), reinterpret_cast<WalkScratch*>(lds))) return;
     do {
         // the query rows of this lane's column; columns past the last row stand in for it
@@ -1046,7 +1075,7 @@ __global__ __launch_bounds__(kTreeWaves * kWave, 2) void tree_tile_kernel(TreeRu
     const int rw = wave & (RW - 1), kw = wave / RW;
     const float ninf = -__builtin_inff();
 
-    Walk<M, kBC, 512, kTileStart, kTileLead> u;
+    Walk<M, kBC, 512, kTileStart, kTileLead, RW == 4> u;
     if (!u.begin(args_now(), reinterpret_cast<WalkScratch*>(lds))) return;
 
     TileLoader<T, D, FP8, RW == 2> load;        // (up to 64 rows a sequence is one row tile: its keys are read once)
@@ -1362,7 +1391,7 @@ __global__ __launch_bounds__(kTreeWaves * kWave, 2) void tree_rows_f32_kernel(Tr
     const int q = lane >> 4;
     const float ninf = -__builtin_inff();
 
-    Walk<16, kTreeBlock, 512, kRowsStart, kRowsLead> u;
+    Walk<16, kTreeBlock, 512, kRowsStart, kRowsLead, false> u;
     if (!u.begin(r, reinterpret_cast<WalkScratch*>(fold))) return;
     do {
         const int row = u.first + min(col, u.nrows - 1);
