@@ -3,12 +3,34 @@
 // (fork_kernel, reserve_kernel with copy_rows_kernel, commit_kernel).
 #include "flashd_common.h"
 #include "flashd_kernels.h"
+#include "flashd_mma.h"
 #include "flashd_paged.h"
+
+#include <type_traits>
 
 namespace flashd {
 
-typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
-typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
+// 8 elements that are read once
+template <typename T>
+__device__ __forceinline__ void load_once(const void* p, size_t i, float (&x)[8]) {
+    constexpr int NW = sizeof(typename T::raw) / 2;
+    const u32x4* at = reinterpret_cast<const u32x4*>(static_cast<const typename T::raw*>(p) + i);
+    u32x4 w[NW];
+#pragma unroll
+    for (int k = 0; k < NW; ++k) w[k] = __builtin_nontemporal_load(at + k);
+    Store<T>::load8(w, 0, x);
+}
+// 8 elements, rounded to nearest even two by two (one by one in integers that took a fifth of the kernel's instructions)
+template <typename T>
+__device__ __forceinline__ void store8(void* p, size_t i, const float (&x)[8]) {
+    if constexpr (std::is_same_v<T, F32>) {
+        Store<T>::store4(p, i, {x[0], x[1], x[2], x[3]});
+        Store<T>::store4(p, i + 4, {x[4], x[5], x[6], x[7]});
+    } else {
+        *reinterpret_cast<u32x4*>(static_cast<typename T::raw*>(p) + i) =
+            Mma<T>::pack8(f32x8{x[0], x[1], x[2], x[3], x[4], x[5], x[6], x[7]});
+    }
+}
 
 // ---- norm, rotation and cache write --------------------------------------------------------
 //
@@ -22,12 +44,11 @@ typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
 // workgroup takes one token's rows (its q, k and v heads), so that the angles are formed once for
 // all of them.
 //
-// PASSES: how many rows a lane's place in the workgroup takes, all loaded before anything else.  Long
-// calls want few workgroups per token (the search for its sequence and its angles are done in each of them): 12696 tokens of
-// 32 + 2 x 8 heads of 128 take 78 us (312 MB, 4.0 TB/s; a plain copy moves 5.2) and took 92 with a workgroup for every 16
-// rows.  Short ones want the rows spread: 64 tokens take 4.3 us, all of it latency.  (Workgroups that walk many tokens, the
-// next one's rows on their way, were not ahead: 76 us with as many as fit on the chip at once, 83 to 102 with more or
-// fewer.)
+// PASSES: how many rows a lane's place in the workgroup takes, all loaded before anything else.  Long calls want few
+// workgroups per token, as the search for its sequence and its angles are done in each of them: with one for every 16 rows 12696
+// tokens of 32 + 2 x 8 heads of 128 took 92 us where this took 78.  Short ones want the rows spread.  Those tokens take 62 us now, 312 MB
+// at 5.0 TB/s (a plain copy moves 5.2); 64 tokens take 4.2, all of it latency.  Workgroups that walk many tokens, the next
+// one's rows on their way, were not ahead (76 to 102 where this took 78).
 template <typename T, int D, bool FP8, int PASSES>
 __global__ __launch_bounds__(256) void append_kernel(Paged c, AppendArgs a) {
     constexpr int LPR = D / 8;                  // lanes per row
@@ -46,9 +67,9 @@ __global__ __launch_bounds__(256) void append_kernel(Paged c, AppendArgs a) {
         const int row = row0 + p * RPP;
 #pragma unroll
         for (int e = 0; e < 8; ++e) x[p][e] = 0.0f;
-        if (row < a.Hq) Store<T>::load8(a.q, (size_t)t * a.q_stride + (size_t)row * D + 8 * l, x[p]);
-        else if (row < a.Hq + c.Hkv) Store<T>::load8(a.k, (size_t)t * a.k_stride + (size_t)(row - a.Hq) * D + 8 * l, x[p]);
-        else if (row < rows) Store<T>::load8(a.v, (size_t)t * a.v_stride + (size_t)(row - a.Hq - c.Hkv) * D + 8 * l, x[p]);
+        if (row < a.Hq) load_once<T>(a.q, (size_t)t * a.q_stride + (size_t)row * D + 8 * l, x[p]);
+        else if (row < a.Hq + c.Hkv) load_once<T>(a.k, (size_t)t * a.k_stride + (size_t)(row - a.Hq) * D + 8 * l, x[p]);
+        else if (row < rows) load_once<T>(a.v, (size_t)t * a.v_stride + (size_t)(row - a.Hq - c.Hkv) * D + 8 * l, x[p]);
     }
 
     // the token's sequence: the last one that begins at or before it
@@ -127,8 +148,7 @@ __global__ __launch_bounds__(256) void append_kernel(Paged c, AppendArgs a) {
 
         if (is_q) {
             const size_t at = (size_t)t * a.qo_stride + (size_t)row * D + 8 * l;
-            Store<T>::store4(a.q_out, at, {x[p][0], x[p][1], x[p][2], x[p][3]});
-            Store<T>::store4(a.q_out, at + 4, {x[p][4], x[p][5], x[p][6], x[p][7]});
+            store8<T>(a.q_out, at, x[p]);
         } else if (row < rows && page >= 0) {
             const int h = is_k ? row - a.Hq : row - a.Hq - c.Hkv;
             char* base = (is_k ? c.k : c.v) + (size_t)page * c.page_bytes + (size_t)h * c.head_bytes;
@@ -150,8 +170,7 @@ __global__ __launch_bounds__(256) void append_kernel(Paged c, AppendArgs a) {
                 }
                 *reinterpret_cast<u32x2*>(base + at) = w;
             } else {
-                Store<T>::store4(base, at, {x[p][0], x[p][1], x[p][2], x[p][3]});
-                Store<T>::store4(base, at + 4, {x[p][4], x[p][5], x[p][6], x[p][7]});
+                store8<T>(base, at, x[p]);
             }
         }
     }

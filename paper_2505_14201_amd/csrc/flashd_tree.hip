@@ -877,7 +877,7 @@ __global__ __launch_bounds__(kTreeWaves * kWave, rows_per_cu(D, FP8, NR)) void t
 // Up to 64 rows HBM bounds it: trees of 16 tokens after 500 to 8192 keys (32 sequences, 32 / 8 heads of 128) take 110 us for
 // 600 MB, 5.5 TB/s, one of 12 after 131000 keys 91 us, 5.9 TB/s; the start of a piece, when nothing of it has arrived, and
 // the unequal pace of the workgroups are the rest.  With 128 rows it is the instructions: chunks of 573 to 1000 tokens after 3180 to
-// 7000 keys are 277 GFLOP in 344 us, 805 TFLOP/s; the matrix pipe works 37 % of the cycles, the vector units 44 %, and
+// 7000 keys are 277 GFLOP in 326 us, 850 TFLOP/s; the matrix pipe works 40 % of the cycles, the vector units 47 %, and
 // a wavefront's vector instructions do not run beside its own matrix instructions: with the weights of a tile formed between the
 // output products of the tile before it took 386 us.
 //
