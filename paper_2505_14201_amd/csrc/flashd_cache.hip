@@ -241,10 +241,11 @@ hipError_t launch_cache_fork(const Paged& c, int* refs, const int* parent, int B
 //      page's only holders and all grow: that one keeps it);
 //   3. free pages (refs 0) are numbered in ascending order, k-th free page -> k-th wanted page.
 // Should there be too few, step 3 is left out and the number missing reported.
-// Latency bounds it, eight reads one after the other: 5.2 us for 32 sequences, 11 for 64 whose table and counts another
+// Latency bounds it, six reads one after the other: 4.1 us for 32 sequences, 9.8 for 64 whose table and counts another
 // kernel has just written (they come from beyond this die's L2).
 constexpr int kReserveThreads = 1024;
 constexpr int kReserveWaves = kReserveThreads / kWave;
+constexpr int kReserveEach = kCacheMaxSeqs / kReserveThreads;     // sequences of a thread
 constexpr int kReserveBlocks = 4096;      // the pool is counted in at most that many blocks of 256 m pages
 
 // Exclusive prefix sum over the workgroup's threads; `total` is their sum.
@@ -284,14 +285,23 @@ __global__ __launch_bounds__(kReserveThreads) void reserve_kernel(Paged c, int* 
     if (tid == 0) beyond = 0;
     if (tid < (-c.B & 3)) last[c.B + tid] = -1;          // read four at a time
 
-    // 1. back to the pool
-    for (int k = 0; k < each; ++k) {
+    // 1. back to the pool.  (`lo_page`, `end_page`: what the row has in the first column that it may want a page for and
+    // in the last one, read here beside the others)
+    int lo_page[kReserveEach], end_page[kReserveEach];
+#pragma unroll
+    for (int k = 0; k < kReserveEach; ++k) {
         const int b = k * kReserveThreads + tid;
-        if (b >= c.B) break;
+        lo_page[k] = end_page[k] = -1;
+        if (b >= c.B) continue;
         const Seq s = seq_at(c, b);
         int* row = c.table + (size_t)b * c.max_pages;
         const int end = (s.len + s.n + mask) >> c.page_log2;
         const int part = s.n > 0 && (s.len & mask) != 0 ? page_at(c, b, s.len >> c.page_log2) : -1;
+        const int lo = (s.len + mask) >> c.page_log2;
+        if (lo < end) {
+            lo_page[k] = row[lo];
+            end_page[k] = row[end - 1];
+        }
         for (int col = end; col < c.max_pages; ++col) {
             const int p = row[col];
             if (p < 0) break;                    // owned pages come first in a row
@@ -306,9 +316,22 @@ __global__ __launch_bounds__(kReserveThreads) void reserve_kernel(Paged c, int* 
     __builtin_amdgcn_s_waitcnt(0);
     __syncthreads();
 
+    // The pool is counted by blocks of 256 m pages that each fall to one wavefront.  Its first block is kept, as long as it is
+    // one read per lane and 64 pages; it is on its way while step 2 looks at rows.
+    const int m = (c.P + 256 * kReserveBlocks - 1) / (256 * kReserveBlocks);
+    const int blocks = (c.P + 256 * m - 1) / (256 * m);
+    int held[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int p = wave * 256 + 64 * i + lane;
+        held[i] = m == 1 && p < c.P ? refs[p] : 1;
+    }
+
     // 2. what each wants
     int run = 0;
-    for (int k = 0; k < each; ++k) {
+#pragma unroll
+    for (int k = 0; k < kReserveEach; ++k) {
+        if (k >= each) break;
         const int b = k * kReserveThreads + tid;
         int want = 0;
         bool copy = false;
@@ -322,9 +345,8 @@ __global__ __launch_bounds__(kReserveThreads) void reserve_kernel(Paged c, int* 
             const int refs_p = p >= 0 ? refs[p] : 0;
             int lo = s.n == 0 ? end : min((s.len + mask) >> c.page_log2, end), hi = end;
             if (lo < hi) {
-                const int first = row[lo], behind = row[hi - 1];
-                if (first < 0) hi = lo;
-                else if (behind >= 0) lo = hi;
+                if (lo_page[k] < 0) hi = lo;
+                else if (end_page[k] >= 0) lo = hi;
             }
             while (lo < hi) {                    // the first empty column
                 const int mid = (lo + hi) >> 1;
@@ -357,11 +379,15 @@ __global__ __launch_bounds__(kReserveThreads) void reserve_kernel(Paged c, int* 
     }
     if (tid == 0) at[c.B] = run;
 
-    // free pages, by blocks of 256 m pages that each fall to one wavefront
-    const int m = (c.P + 256 * kReserveBlocks - 1) / (256 * kReserveBlocks);
-    const int blocks = (c.P + 256 * m - 1) / (256 * m);
+    // free pages
     for (int k = wave; k < blocks; k += kReserveWaves) {
         int n = 0;
+        if (k == wave && m == 1) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) n += __popcll(__ballot(held[i] == 0));
+            if (lane == 0) count[k] = n;
+            continue;
+        }
         for (int j = 0; j < 4 * m; j += 4) {
             bool is[4];
 #pragma unroll
@@ -396,7 +422,9 @@ __global__ __launch_bounds__(kReserveThreads) void reserve_kernel(Paged c, int* 
         int rank = count[k];
         for (int j = 0; j < 4 * m && rank < run; ++j) {
             const int p = k * 256 * m + 64 * j + lane;
-            const bool is = p < c.P && refs[p] == 0;
+            bool is = false;
+            if (k != wave || m != 1) is = p < c.P && refs[p] == 0;
+            else is = (j == 0 ? held[0] : j == 1 ? held[1] : j == 2 ? held[2] : held[3]) == 0;
             const uint64_t all = __ballot(is);
             const int mine = rank + __popcll(all & ((1ull << lane) - 1));
             if (is && mine < run) {
