@@ -461,7 +461,8 @@ __device__ __forceinline__ void weigh(float (&x)[8], f32x8& p, f32x4 (&U)[NDB], 
 }
 
 // Joins the four wavefronts' states of a piece whose keys they have shared out: row tiles of 16 NR rows.
-template <typename T, int D, int NR, class Wk>
+// BY16: U[i] of lane (q, col) is columns 16 i + 4 q .. + 3, else 64 (i / 4) + 16 q + 4 (i % 4) .. + 3.
+template <typename T, int D, int NR, bool BY16, class Wk>
 __device__ __forceinline__ void finish_rows(const TreeRun& r, const Wk& u, const f32x4 (&U)[NR][D / 16],
                                             const float (&R)[NR], const float (&l)[NR], float* fold, float vscale) {
     constexpr int W = kTreeWaves, FROW = D + 4, NDB = D / 16;
@@ -473,7 +474,8 @@ __device__ __forceinline__ void finish_rows(const TreeRun& r, const Wk& u, const
         __syncthreads();                                 // stages are dead, `fold` is their memory
 #pragma unroll
         for (int i = 0; i < NDB; ++i)
-            *reinterpret_cast<f32x4*>(&fold[(wave * 16 + col) * FROW + 16 * i + 4 * q]) = U[k][i];
+            *reinterpret_cast<f32x4*>(&fold[(wave * 16 + col) * FROW + (BY16 ? 16 * i + 4 * q : 64 * (i >> 2) + 16 * q + 4 * (i & 3))]) =
+                U[k][i];
         if (q == 0) {
             fold_r[wave][col] = R[k];
             fold_l[wave][col] = lk;
@@ -504,24 +506,6 @@ __device__ __forceinline__ void finish_rows(const TreeRun& r, const Wk& u, const
     __syncthreads();
 }
 
-// The pages of a wavefront's blocks blk0 + wave, + W, ...: looked up 32 blocks at a time, lane l for half
-// l & 1 of block l / 2.  -1 where there is no page, or no key.
-struct PageWindow {
-    int pages, from;
-    template <class W>
-    __device__ __forceinline__ int at(const Paged& c, const W& u, int wave, int lane, int blk, int half) {
-        const int k = (blk - u.blk0) / kTreeWaves;
-        if (k / 32 != from) {
-            from = k / 32;
-            const int mine = u.blk0 + wave + kTreeWaves * (32 * from + (lane >> 1));
-            const int key = mine * kTreeBlock + 16 * (lane & 1);
-            pages = -1;
-            if (mine < u.blk1 && key < u.keys()) pages = page_at(c, u.b, key >> c.page_log2);
-        }
-        return __builtin_amdgcn_readlane(pages, 2 * (k & 31) + half);
-    }
-};
-
 // A run of bytes behind which reads give zeros: the words of a buffer descriptor.
 struct Window {
     u32x4 words;
@@ -533,16 +517,6 @@ struct Window {
 
 __device__ __forceinline__ Window make_window(uint64_t at, int bytes) {
     return Window{u32x4{(uint32_t)uniform((int)at), (uint32_t)uniform((int)(at >> 32)), (uint32_t)uniform(bytes), 0x00020000u}};
-}
-
-// 16 keys of a block: their bytes up to the sequence's last key, or nothing without a page.
-template <class W>
-__device__ __forceinline__ Window half_window(const Paged& c, const W& u, const char* pool, int page, int key) {
-    const int row = (int)(c.head_bytes >> c.page_log2);
-    const uint64_t at = (uint64_t)(pool + (int64_t)max(page, 0) * c.page_bytes + u.h * c.head_bytes +
-                                   (int64_t)(key & ((1 << c.page_log2) - 1)) * row);
-    const int keys = page < 0 ? 0 : min(16, u.keys() - key);
-    return make_window(at, max(keys, 0) * row);
 }
 
 // ---- 16 rows, keys shared out over the wavefronts (f16 / bf16) -----------------------------------
@@ -863,7 +837,7 @@ __global__ __launch_bounds__(kTreeWaves * kWave, rows_per_cu(D, FP8, NR)) void t
             n1 = m1;
         }
         const TreeRun end_r = args_now();
-        finish_rows<T, D, NR>(end_r, u, U, R, l, reinterpret_cast<float*>(lds), FP8 ? end_r.c.vscale : 1.0f);
+        finish_rows<T, D, NR, true>(end_r, u, U, R, l, reinterpret_cast<float*>(lds), FP8 ? end_r.c.vscale : 1.0f);
     } while (u.next(args_now()));
 }
 
@@ -1373,17 +1347,23 @@ __global__ __launch_bounds__(kTreeWaves * kWave, 2) void tree_tile_kernel(TreeRu
 // v_mfma_f32_16x16x4_f32: lane (q, c) gives element q of the four that are summed, row (or column) c.  K as the A
 // operand: the lane's float4 at dims 16 m + 4 q serves four products, each summing dims 16 m + 4 q' + e over
 // q'.  The scores it gets are keys 4 q + r of its row: as B operand of O^T = V^T P^T product r sums
-// the keys 4 q' + r over q', for which the lane's A element is V[4 q + r][16 i + c].  Nothing goes
-// through LDS.  One token for each of 64 sequences of 500 to 8192 keys, 32 / 8 heads of 128: 465 us with the merge, 2.34 GB, 5.0
-// TB/s; more than 16 rows read their keys anew for each 16 and run at 46 TFLOP/s.
-template <int D>
-__global__ __launch_bounds__(kTreeWaves * kWave, 2) void tree_rows_f32_kernel(TreeRun r) {
+// the keys 4 q' + r over q'.  The lane's float4 of V[4 q + r] at columns 64 g + 4 c serves four of them, product j for the columns
+// 64 g + 4 c' + j: of those the lane's results are 64 g + 16 q + 4 d + j, d = 0 .. 3.  Nothing goes through LDS; V
+// of a block is on its way while K is multiplied, K of the next one while V is.
+//
+// NR: 16-row column tiles, which read the keys once.  With two, and at d = 128, there is one workgroup per compute unit, whose registers
+// they need.  One token for each of 64 sequences of 500 to 8192 keys, 32 / 8 heads of 128: 382 us with the merge, 2.34 GB, 6.1 TB/s
+// (two workgroups, with spills: 424; without anything under way in the meantime 465); d = 64: 188 us.  Chunks of 115 to 200 tokens:
+// 610 us, 85 TFLOP/s of the 154 that a large product of the library reaches (1128 with 16 rows to a tile).
+constexpr int f32_per_cu(int D, int NR) { return D == 64 && NR == 1 ? 2 : 1; }
+template <int D, int NR>
+__global__ __launch_bounds__(kTreeWaves * kWave, f32_per_cu(D, NR)) void tree_rows_f32_kernel(TreeRun r) {
     constexpr int W = kTreeWaves;
     constexpr int NDB = D / 16;
+    constexpr int NG = D / 64;
     __shared__ __align__(16) float fold[W * 16 * (D + 4)];
 
-    const Paged& c = r.c;
-    const TreeArgs& a = r.a;
+    (void)r;                                             // read through args_now()
     const int tid = threadIdx.x;
     const int lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -1391,84 +1371,184 @@ __global__ __launch_bounds__(kTreeWaves * kWave, 2) void tree_rows_f32_kernel(Tr
     const int q = lane >> 4;
     const float ninf = -__builtin_inff();
 
-    Walk<16, kTreeBlock, 512, kRowsStart, kRowsLead, false> u;
-    if (!u.begin(r, reinterpret_cast<WalkScratch*>(fold))) return;
+    Walk<16 * NR, kTreeBlock, 256 * f32_per_cu(D, NR), kRowsStart, kRowsLead, false> u;
+    if (!u.begin(args_now(), reinterpret_cast<WalkScratch*>(fold))) return;
     do {
-        const int row = u.first + min(col, u.nrows - 1);
-        const int token = (int)fast_div((uint32_t)row, r.group);
-        const float* qg = static_cast<const float*>(a.q) + row_at(r, u, row, a.q_stride, D);
-        f32x4 qf[NDB];
+        const TreeRun now_r = args_now();
+        f32x4 qf[NR][NDB];
 #pragma unroll
-        for (int m = 0; m < NDB; ++m) qf[m] = *reinterpret_cast<const f32x4*>(qg + 16 * m + 4 * q);
-        const float c_log2 = a.scale * kLog2e;
+        for (int k = 0; k < NR; ++k) {
+            const int row = u.first + min(16 * k + col, u.nrows - 1);
+            const float* qg = static_cast<const float*>(now_r.a.q) + row_at(now_r, u, row, now_r.a.q_stride, D);
+#pragma unroll
+            for (int m = 0; m < NDB; ++m) qf[k][m] = *reinterpret_cast<const f32x4*>(qg + 16 * m + 4 * q);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        const float c_log2 = now_r.a.scale * kLog2e;
 
-        f32x4 Us[1][NDB];
-        f32x4 (&U)[NDB] = Us[0];
-#pragma unroll
-        for (int i = 0; i < NDB; ++i) U[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-        float R[1] = {ninf}, l[1] = {0.0f};
-        PageWindow pages{-1, -1};
-        for (int blk = u.blk0 + wave; blk < u.blk1; blk += W) {
-            const int j0 = blk * kTreeBlock;
-            const int p[2] = {pages.at(c, u, wave, lane, blk, 0), pages.at(c, u, wave, lane, blk, 1)};
-            const uint32_t have = (p[0] < 0 ? 0u : 0x0000ffffu) | (p[1] < 0 ? 0u : 0xffff0000u);
-            f32x4 acc[2];
+        // as in tree_rows_kernel
+        constexpr int ROWB = 4 * D;
+        const char* kpool = now_r.c.k + u.h * now_r.c.head_bytes;
+        const char* vpool = now_r.c.v + u.h * now_r.c.head_bytes;
+        int64_t page_bytes = now_r.c.page_bytes;
+        int page_log2 = now_r.c.page_log2, pool_pages = now_r.c.P, last_key = u.keys(), blk_end = u.blk1, len = u.s.len;
+        typedef const __attribute__((address_space(4))) int* table_ptr;
+        table_ptr trow = (table_ptr)(uintptr_t)(now_r.c.table + (size_t)u.b * now_r.c.max_pages);
+        asm volatile("" : "+s"(kpool), "+s"(vpool), "+s"(page_bytes), "+s"(page_log2), "+s"(pool_pages), "+s"(last_key),
+                          "+s"(blk_end), "+s"(len), "+s"(trow));
+        auto page_of = [&](int blk, int half) __attribute__((always_inline)) {
+            const int key = blk * kTreeBlock + 16 * half;
+            const int p = blk < blk_end && key < last_key ? trow[key >> page_log2] : -1;
+            return (unsigned)p < (unsigned)pool_pages ? p : -1;
+        };
+        auto half_window = [&](const char* pool, int blk, int half, int p) __attribute__((always_inline)) {
+            const int key = blk * kTreeBlock + 16 * half;
+            const uint64_t at = (uint64_t)(pool + max(p, 0) * page_bytes + (key & ((1 << page_log2) - 1)) * ROWB);
+            const int left = last_key - key, keys = p < 0 || left < 0 ? 0 : left < 16 ? left : 16;
+            return make_window(at, keys * ROWB).rsrc();
+        };
+        f32x4 kreg[2][NDB], vreg[8][NG];
+        auto fetch_k = [&](int blk, int p0, int p1) __attribute__((always_inline)) {
 #pragma unroll
             for (int t = 0; t < 2; ++t) {
-                acc[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-                const auto w = half_window(c, u, c.k, p[t], j0 + 16 * t).rsrc();
-                f32x4 k[NDB];
+                const auto w = half_window(kpool, blk, t, t ? p1 : p0);
 #pragma unroll
-                for (int m = 0; m < NDB; ++m) k[m] = __builtin_bit_cast(f32x4, kv_load<2>(w, (col * D + 16 * m + 4 * q) * 4));
+                for (int m = 0; m < NDB; ++m) kreg[t][m] = __builtin_bit_cast(f32x4, kv_load<2>(w, (col * D + 16 * m + 4 * q) * 4));
+            }
+        };
+        auto fetch_v = [&](int blk, int p0, int p1) __attribute__((always_inline)) {
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                const auto w = half_window(vpool, blk, t, t ? p1 : p0);
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+#pragma unroll
+                    for (int g = 0; g < NG; ++g)
+                        vreg[4 * t + e][g] = __builtin_bit_cast(f32x4, kv_load<2>(w, ((4 * q + e) * D + 64 * g + 4 * col) * 4));
+            }
+        };
+
+        f32x4 U[NR][NDB];                                // [4 g + j][d]: column 64 g + 16 q + 4 d + j
+        float R[NR], l[NR];
+#pragma unroll
+        for (int k = 0; k < NR; ++k) {
+            R[k] = ninf;
+            l[k] = 0.0f;
+#pragma unroll
+            for (int i = 0; i < NDB; ++i) U[k][i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        }
+        int blk = u.blk0 + wave;
+        int p0 = page_of(blk, 0), p1 = page_of(blk, 1), n0 = page_of(blk + W, 0), n1 = page_of(blk + W, 1);
+        __builtin_amdgcn_sched_barrier(0);
+        fetch_k(blk, p0, p1);
+        __builtin_amdgcn_sched_barrier(0);
+        fetch_v(blk, p0, p1);
+        __builtin_amdgcn_sched_barrier(0);
+        wait_loads<2 * NDB + 8 * NG>();                  // the queries are here, as the compiler knows
+        for (; blk < blk_end; blk += W) {
+            const int j0 = blk * kTreeBlock;
+            const uint32_t have = (p0 < 0 ? 0u : 0x0000ffffu) | (p1 < 0 ? 0u : 0xffff0000u);
+            const int m0 = page_of(blk + 2 * W, 0), m1 = page_of(blk + 2 * W, 1);
+            f32x4 acc[NR][2];
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+#pragma unroll
+                for (int k = 0; k < NR; ++k) acc[k][t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
                 for (int m = 0; m < NDB; ++m)
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
-                        acc[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(k[m][e], qf[m][e], acc[t], 0, 0, 0);
-            }
-            const bool masked = have != ~0u || j0 + kTreeBlock > u.s.len;
-            uint32_t bits = ~0u;
-            if (masked) bits = have & seen_bits(a, u.s, token, u.s.row0 + token, j0);
-            float x[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                x[e] = acc[e >> 2][e & 3] * c_log2;
-                if (masked && !(bits >> (16 * (e >> 2) + 4 * q + (e & 3)) & 1u)) x[e] = ninf;
+                        for (int k = 0; k < NR; ++k)
+                            acc[k][t] = __builtin_amdgcn_mfma_f32_16x16x4f32(kreg[t][m][e], qf[k][m][e], acc[k][t], 0, 0, 0);
             }
-            f32x8 pv;
-            weigh(x, pv, U, R[0], l[0], LazyLimit<BF16>::kMoveLog2);
-            l[0] += ((pv[0] + pv[1]) + (pv[2] + pv[3])) + ((pv[4] + pv[5]) + (pv[6] + pv[7]));
+            __builtin_amdgcn_sched_barrier(0);
+            fetch_k(blk + W, n0, n1);
+            __builtin_amdgcn_sched_barrier(0);
+            const bool masked = have != ~0u || j0 + kTreeBlock > len;
+            uint32_t bits[NR];
+            f32x8 pv[NR];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const auto w = half_window(c, u, c.v, p[e >> 2], j0 + 16 * (e >> 2)).rsrc();
-                float v[NDB];
+            for (int k = 0; k < NR; ++k) {
+                bits[k] = ~0u;
+                if (masked) {
+                    const TreeRun m = args_now();
+                    const int token = (int)fast_div((uint32_t)(u.first + min(16 * k + col, u.nrows - 1)), m.group);
+                    bits[k] = have & seen_bits(m.a, u.s, token, u.s.row0 + token, j0);
+                }
+                float x[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    x[e] = acc[k][e >> 2][e & 3] * c_log2;
+                    if (masked) x[e] = if_seen(bits[k] >> (4 * q), 16 * (e >> 2) + (e & 3), x[e]);
+                }
+                weigh(x, pv[k], U[k], R[k], l[k], LazyLimit<BF16>::kMoveLog2);
+                l[k] += ((pv[k][0] + pv[k][1]) + (pv[k][2] + pv[k][3])) + ((pv[k][4] + pv[k][5]) + (pv[k][6] + pv[k][7]));
+            }
+            bool apart = false;
+            if (masked) {
                 bool bad = false;
 #pragma unroll
-                for (int i = 0; i < NDB; ++i) {
-                    v[i] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(w, ((4 * q + (e & 3)) * D + 16 * i + col) * 4, 0, 2));
-                    bad |= !(fabsf(v[i]) <= 3.4028234e38f);
-                }
-                if (masked && __builtin_amdgcn_ballot_w64(bad) != 0) {
-                    for (int k = 0; k < 4; ++k) {
-                        const float wt = __shfl(pv[e], 16 * k + col);
-                        const bool seen = (bits >> (16 * (e >> 2) + 4 * k + (e & 3)) & 1u) != 0;
+                for (int e = 0; e < 8; ++e)
 #pragma unroll
-                        for (int i = 0; i < NDB; ++i)
+                    for (int g = 0; g < NG; ++g)
 #pragma unroll
-                            for (int d = 0; d < 4; ++d) {
-                                const float y = __shfl(v[i], 16 * k + 4 * q + d);
-                                U[i][d] = seen ? fmaf(wt, y, U[i][d]) : U[i][d];
-                            }
-                    }
-                } else {
-#pragma unroll
-                    for (int i = 0; i < NDB; ++i)
-                        U[i] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[i], pv[e], U[i], 0, 0, 0);
-                }
+                        for (int j = 0; j < 4; ++j) bad |= !(fabsf(vreg[e][g][j]) <= 3.4028234e38f);
+                apart = __builtin_amdgcn_ballot_w64(bad) != 0;
             }
+            if (apart) {
+                // an infinite or NaN value: key by key, only where the row sees it
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+#pragma unroll 1
+                    for (int z = 0; z < 4; ++z)
+#pragma unroll
+                        for (int g = 0; g < NG; ++g)
+#pragma unroll
+                            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                                for (int d = 0; d < 4; ++d) {
+                                    __builtin_amdgcn_sched_barrier(0);           // few registers at a time
+                                    const float y = __shfl(vreg[e][g][j], 16 * z + 4 * q + d);
+#pragma unroll
+                                    for (int k = 0; k < NR; ++k) {
+                                        const float wt = __shfl(pv[k][e], 16 * z + col);
+                                        const bool seen = (bits[k] >> (16 * (e >> 2) + 4 * z + (e & 3)) & 1u) != 0;
+                                        U[k][4 * g + j][d] = seen ? fmaf(wt, y, U[k][4 * g + j][d]) : U[k][4 * g + j][d];
+                                    }
+                                }
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+#pragma unroll
+                    for (int g = 0; g < NG; ++g)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j)
+#pragma unroll
+                            for (int k = 0; k < NR; ++k)
+                                U[k][4 * g + j] = __builtin_amdgcn_mfma_f32_16x16x4f32(vreg[e][g][j], pv[k][e], U[k][4 * g + j], 0, 0, 0);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            fetch_v(blk + W, n0, n1);
+            __builtin_amdgcn_sched_barrier(0);
+            p0 = n0;
+            p1 = n1;
+            n0 = m0;
+            n1 = m1;
         }
-        finish_rows<F32, D, 1>(r, u, Us, R, l, fold, 1.0f);
-    } while (u.next(r));
+        // column by column, as finish_rows takes them
+#pragma unroll
+        for (int k = 0; k < NR; ++k)
+#pragma unroll
+            for (int g = 0; g < NG; ++g) {
+                f32x4 x[4];
+#pragma unroll
+                for (int d = 0; d < 4; ++d) x[d] = f32x4{U[k][4 * g][d], U[k][4 * g + 1][d], U[k][4 * g + 2][d], U[k][4 * g + 3][d]};
+#pragma unroll
+                for (int d = 0; d < 4; ++d) U[k][4 * g + d] = x[d];
+            }
+        finish_rows<F32, D, NR, false>(args_now(), u, U, R, l, fold, 1.0f);
+    } while (u.next(args_now()));
 }
 
 // ---- join the parts of split units -------------------------------------------------------------
@@ -1624,7 +1704,8 @@ __global__ __launch_bounds__(256, 4) void merge_tree_kernel(TreeRun r, float vsc
 // tokens: 401 and 562.
 static int tree_rows(int Hq, int Hkv, int max_q, int dtype, bool fp8) {
     const long rows = (long)max_q * (Hq / Hkv);
-    return dtype == 0 || rows <= 16 ? 16 : rows <= 32 && fp8 ? 32 : rows <= 64 ? 64 : 128;
+    if (dtype == 0) return rows <= 16 ? 16 : 32;
+    return rows <= 16 ? 16 : rows <= 32 && fp8 ? 32 : rows <= 64 ? 64 : 128;
 }
 
 size_t attn_tree_workspace(int Hq, int Hkv, int max_q, int d, int dtype) {
@@ -1641,7 +1722,7 @@ static hipError_t launch_tree_m(TreeRun& r, hipStream_t st) {
         r.groups = groups;
         hipLaunchKernelGGL(kernel, dim3((unsigned)groups), block, 0, st, r);
     };
-    if constexpr (std::is_same_v<T, F32>) launch(tree_rows_f32_kernel<D>, 512);
+    if constexpr (std::is_same_v<T, F32>) launch(tree_rows_f32_kernel<D, M / 16>, 256 * f32_per_cu(D, M / 16));
     else if constexpr (M == 32) launch(tree_rows_kernel<T, D, true, 2>, 256 * rows_per_cu(D, true, 2));
     else if constexpr (M == 16) {
         if (r.a.fp8) launch(tree_rows_kernel<T, D, true, 1>, 256 * rows_per_cu(D, true, 1));
@@ -1659,16 +1740,13 @@ static hipError_t launch_tree_m(TreeRun& r, hipStream_t st) {
 
 template <typename T, int D>
 static hipError_t launch_tree_t(TreeRun& r, hipStream_t st) {
-    if constexpr (std::is_same_v<T, F32>) {
-        return launch_tree_m<T, D, 16>(r, st);
-    } else {
-        switch (tree_rows(r.a.Hq, r.c.Hkv, r.a.max_q, r.a.dtype, r.a.fp8 != 0)) {
-        case 16: return launch_tree_m<T, D, 16>(r, st);
-        case 32: return launch_tree_m<T, D, 32>(r, st);
-        case 64: return launch_tree_m<T, D, 64>(r, st);
-        default: return launch_tree_m<T, D, 128>(r, st);
-        }
+    const int rows = tree_rows(r.a.Hq, r.c.Hkv, r.a.max_q, r.a.dtype, r.a.fp8 != 0);
+    switch (rows) {
+    case 16: return launch_tree_m<T, D, 16>(r, st);
+    case 32: return launch_tree_m<T, D, 32>(r, st);
     }
+    if constexpr (std::is_same_v<T, F32>) return hipErrorInvalidValue;          // tree_rows() has no more for it
+    else return rows == 64 ? launch_tree_m<T, D, 64>(r, st) : launch_tree_m<T, D, 128>(r, st);
 }
 
 hipError_t launch_attn_tree(const Paged& c, const TreeArgs& a, hipStream_t st) {

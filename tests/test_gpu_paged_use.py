@@ -12,7 +12,7 @@ pytestmark = pytest.mark.gpu
 # hints whose rows, 4 to a token, choose 16, 32, 64 and 128 rows to a tile
 HINTS = (1, 6, 12, 20)
 TYPES = [("bf16", 128, False), ("f16", 128, False), ("bf16", 64, False), ("f16", 64, False), ("bf16", 128, True),
-         ("f16", 64, True), ("f16", 128, True), ("bf16", 64, True)]
+         ("f16", 64, True), ("f16", 128, True), ("bf16", 64, True), ("f32", 128, False), ("f32", 64, False)]
 
 
 def small(dtype, d, fp8, seed, lens=(150, 3, 97), some=(21, 1, 13), page=16, **kw):
@@ -71,7 +71,7 @@ def test_numbers_that_are_none(bad, hint, dtype, d, fp8):
             assert not spoilt or not torch.isfinite(got[t, :, 3]).any(), (b, i)
 
 
-@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
 @pytest.mark.parametrize("hint", HINTS)
 def test_growing_scores_of_every_kernel(hint, dtype):
     c = pu.make([900], [4], 1, 128, 32, dtype, seed=56, qk_std=4.0)
