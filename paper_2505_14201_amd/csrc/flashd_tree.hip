@@ -1701,7 +1701,7 @@ __global__ __launch_bounds__(256, 4) void merge_tree_kernel(TreeRun r, float vsc
 // way through LDS counts for more than their bytes: 24 rows, 64 sequences of 500 to 8192 keys, d = 128: 138 us with 32 and
 // 145 with 64, d = 64: 87 and 108; from bf16, 32 such sequences: 144 and 117, d = 64: 64 and 64.  16 rows against 64 for 4 rows of
 // 64 sequences: 192 and 198 us, fp8 115 and 156, one short sequence 15 and 19.  128 against 64 for chunks of 1000
-// tokens: 401 and 562.
+// tokens: 401 and 562.  fp32, 16 against 32: 4 rows 400 and 474 us, 20 rows 263 and 249, 32 rows 403 and 270.
 static int tree_rows(int Hq, int Hkv, int max_q, int dtype, bool fp8) {
     const long rows = (long)max_q * (Hq / Hkv);
     if (dtype == 0) return rows <= 16 ? 16 : 32;
