@@ -137,6 +137,7 @@ __device__ __forceinline__ long long sum_of_floors(long long n, long long a, lon
 struct WalkScratch {
     long long wave_sum[kTreeWaves];
     long long found_before, found_places;
+    Seq found_seq;
     int found_b;
 };
 
@@ -196,6 +197,10 @@ struct Walk {
         b = seq;
         s = seq_at(r.c, b);
         if constexpr (SAME) s = Seq{uniform(s.row0), uniform(s.n), uniform(s.len)};
+        tiles = (int)(((long long)s.n * (int)r.group.d + M - 1) / M);
+    }
+    __device__ __forceinline__ void set_seq(const TreeRun& r, const Seq& x) {       // one that was entered before
+        s = Seq{uniform(x.row0), uniform(x.n), uniform(x.len)};
         tiles = (int)(((long long)s.n * (int)r.group.d + M - 1) / M);
     }
     // Places of one kv head's units.  (A chain's tile t < tiles - 1 has ceil((len + ceil((t + 1) M / G)) / KB) blocks,
@@ -282,13 +287,16 @@ struct Walk {
             found_b = i;
             found_before = before;
             scratch->found_places = own;
+            scratch->found_seq = any.s;
         }
         __syncthreads();
         const int found = uniform(found_b);
         const long long in_b = at - uniform(found_before), head = uniform(quotient(scratch->found_places, c.Hkv));
+        const Seq found_seq = scratch->found_seq;
         __syncthreads();                                 // the scratch is the kernel's again
         if (found < 0) return false;
-        enter<true>(r, found);
+        b = found;
+        set_seq(r, found_seq);
         h = uniform((int)quotient(in_b, head));
         long long rest = in_b - h * head;
         if (r.a.tree != nullptr || tiles == 1) {
