@@ -98,6 +98,28 @@ __device__ __forceinline__ long long uniform(long long x) {
     return (long long)((uint64_t)(uint32_t)uniform((int)(x >> 32)) << 32 | (uint32_t)uniform((int)x));
 }
 
+// Sum over the lanes up to this one: within rows of 16 lanes, then the last of row 0 and of row 2 to the next row, then that of row 1 to
+// rows 2 and 3.  (Moves between lanes in the vector units; by LDS, as a shuffle goes, six of them one after the other take 0.3 us.)
+__device__ __forceinline__ int lanes_up_to(int x) {
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);       // from 1, 2, 4 and 8 lanes before
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);       // lane 15 of a row to rows 1 and 3
+    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);       // lane 31 to rows 2 and 3
+    return x;
+}
+__device__ __forceinline__ long long lanes_up_to(long long x) {
+    if (__builtin_amdgcn_ballot_w64((x >> 24) != 0) == 0) return lanes_up_to((int)x);      // the sum has 30 bits
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int k = 1; k < 64; k <<= 1) {
+        const long long y = __shfl_up(x, k);
+        if (lane >= k) x += y;
+    }
+    return x;
+}
+
 // a / b of whole numbers, 0 <= a < 2^52 and b > 0, by a division of doubles (one of 64-bit integers takes ten times the
 // instructions).  The quotient is rounded, so that its floor can be one too large.
 __device__ __forceinline__ long long quotient(long long a, long long b) {
@@ -136,7 +158,7 @@ __device__ __forceinline__ long long sum_of_floors(long long n, long long a, lon
 
 struct WalkScratch {
     long long wave_sum[kTreeWaves];
-    long long found_before, found_places;
+    long long found_before, found_head;
     Seq found_seq;
     int found_b;
 };
@@ -235,19 +257,14 @@ struct Walk {
         const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
         const int each = (c.B + kTreeWaves * kWave - 1) / (kTreeWaves * kWave);
         const int b0 = tid * each, b1 = min(b0 + each, c.B);
-        long long mine = 0, own = 0;             // of the run, and of its last sequence
+        long long mine = 0, own = 0;             // of the run, and of one kv head of its last sequence
         Walk any;
         for (int i = b0; i < b1; ++i) {
             any.template enter<false>(r, i);
-            own = any.places(r) * c.Hkv;
-            mine += own;
+            own = any.places(r);
+            mine += own * c.Hkv;
         }
-        long long in = mine;
-#pragma unroll
-        for (int k = 1; k < 64; k <<= 1) {
-            const long long y = __shfl_up(in, k);
-            if (lane >= k) in += y;
-        }
+        const long long in = lanes_up_to(mine);
         if (lane == 63) wave_sum[wave] = in;
         if (tid == 0) found_b = -1;
         __syncthreads();
@@ -261,11 +278,11 @@ struct Walk {
         // all workgroups, or as many as have kLeast places each
         constexpr int kLeast = kTreeMinBlocks * kTreeBlock / KB;
         const bool few = total <= (long long)kLeast * GRID;
-        per = few ? kLeast : quotient(total + GRID - 1, GRID);
+        per = few ? kLeast : (GRID & (GRID - 1)) == 0 ? (total + GRID - 1) / GRID : quotient(total + GRID - 1, GRID);
         lead = few ? 0 : (per * LEAD) >> 6;
         // Workgroup ids go round-robin over the 8 XCDs; neighbours along the row, which may read the same
         // keys, go to one.  An XCD's first 32 go to a compute unit each, the next 32 beside them, and so on.
-        const int of_xcd = few ? ((int)quotient(total + kLeast - 1, kLeast) + 7) >> 3 : kOfXcd;
+        const int of_xcd = few ? ((int)(total + kLeast - 1) / kLeast + 7) >> 3 : kOfXcd;
         const int k = (int)blockIdx.x >> 3;
         w = ((int)blockIdx.x & 7) * of_xcd + k;
         const int place = w % kOfXcd;
@@ -279,19 +296,19 @@ struct Walk {
             if (each > 1) {                      // (a run of one sequence: `own` is its places)
                 for (;; ++i) {
                     any.template enter<false>(r, i);
-                    own = any.places(r) * c.Hkv;
-                    if (at < before + own) break;
-                    before += own;
+                    own = any.places(r);
+                    if (at < before + own * c.Hkv) break;
+                    before += own * c.Hkv;
                 }
             }
             found_b = i;
             found_before = before;
-            scratch->found_places = own;
+            scratch->found_head = own;
             scratch->found_seq = any.s;
         }
         __syncthreads();
         const int found = uniform(found_b);
-        const long long in_b = at - uniform(found_before), head = uniform(quotient(scratch->found_places, c.Hkv));
+        const long long in_b = at - uniform(found_before), head = uniform(scratch->found_head);
         const Seq found_seq = scratch->found_seq;
         __syncthreads();                                 // the scratch is the kernel's again
         if (found < 0) return false;
@@ -299,21 +316,16 @@ struct Walk {
         set_seq(r, found_seq);
         h = uniform((int)quotient(in_b, head));
         long long rest = in_b - h * head;
-        if (r.a.tree != nullptr || tiles == 1) {
+        tile = 0;
+        if (tiles > 1 && r.a.tree != nullptr) {
             const int each_tile = blocks_of(r, 0) + START;
             tile = uniform((int)quotient(rest, each_tile));
             rest -= (long long)tile * each_tile;
-        } else {
+        } else if (tiles > 1) {
             // every wavefront by itself, 64 tiles at a time
-            tile = 0;
             for (int t0 = 0;; t0 += kWave) {
                 const int its = t0 + lane < tiles ? blocks_of(r, t0 + lane) + START : 0;
-                long long sum = its;
-#pragma unroll
-                for (int step = 1; step < 64; step <<= 1) {
-                    const long long y = __shfl_up(sum, step);
-                    if (lane >= step) sum += y;
-                }
+                const long long sum = lanes_up_to((long long)its);
                 const uint64_t beyond = __builtin_amdgcn_ballot_w64(sum > rest);
                 const int hit = beyond != 0 ? __builtin_ctzll(beyond) : kWave - 1;
                 const long long upto = uniform(__shfl(sum, hit));
@@ -539,7 +551,7 @@ __device__ __forceinline__ Window make_window(uint64_t at, int bytes) {
 //
 // HBM bounds it: a token for each of 64 sequences of 500 to 8192 keys, 32 / 8 heads of 128, takes 178 us for 1.17 GB read once,
 // 6.6 TB/s; from fp8, four tokens each, 100 us for 588 MB, 5.9 TB/s, a wavefront waiting for memory or for its turn
-// three quarters of its time.  One sequence of 1000 keys takes 6.6 us, the latency of finding a share, its pages and its keys.
+// three quarters of its time.  One sequence of 1000 keys takes 6.2 us, the latency of finding a share, its pages and its keys.
 //
 // In blocks with new keys a weight of zero may meet a value that is infinite or NaN (a token that some rows see
 // and others do not), and 0 * infinity must not reach the others: see codes_of().
@@ -1566,8 +1578,8 @@ __global__ __launch_bounds__(kTreeWaves * kWave, f32_per_cu(D, NR)) void tree_ro
 // groups of a workgroup take a row each, or share the parts of one row where a unit has many (more than
 // kMergeShare: one long sequence over the whole chip).  Each thread of a workgroup keeps the splits of a few of the
 // launch's workgroups, and the one that holds the next rows' hands it over through LDS: between a workgroup's start
-// and its rows lies one read from memory.  M: rows of a tile.  8 units of 4 rows in 8 parts take 3.9 us, 512 of 128 rows in 2 and 3
-// parts (67 MB) 18.6.  What bounds it is the time of its reads, so that many workgroups
+// and its rows lies one read from memory.  M: rows of a tile.  8 units of 4 rows in 8 parts take 3.5 us, 512 of 128 rows in 2 and 3
+// parts (67 MB) 18.  What bounds it is the time of its reads, so that many workgroups
 // are under way at once where there are many rows.
 constexpr int kMergeShare = 12;
 constexpr int merge_groups(int M) { return M <= 32 ? 512 : M == 64 ? 1024 : 2048; }
@@ -1629,12 +1641,7 @@ __global__ __launch_bounds__(256, 4) void merge_tree_kernel(TreeRun r, float vsc
     for (int k = 0; k < EACH; ++k) {
         const int rows = mine[k][ROWS], parts = mine[k][PARTS];
         items[k] = 256 * k + tid >= r.groups || parts == 0 ? 0 : parts > kMergeShare ? rows : (rows + NG - 1) / NG;
-        int in = items[k];
-#pragma unroll
-        for (int step = 1; step < 64; step <<= 1) {
-            const int y = __shfl_up(in, step);
-            if (lane >= step) in += y;
-        }
+        const int in = lanes_up_to(items[k]);
         if (lane == 63) wave_sum[k][wave] = in;
         before[k] = in - items[k];
     }
