@@ -53,6 +53,18 @@ __device__ __forceinline__ int page_at(const Paged& c, int b, int col) {
     return (unsigned)p < (unsigned)c.P ? p : -1;
 }
 
+// Sum over the lanes up to this one: within rows of 16 lanes, then the last of row 0 and of row 2 to the next row, then that of row 1 to
+// rows 2 and 3.  (Moves between lanes in the vector units; by LDS, as a shuffle goes, six of them one after the other take 0.3 us.)
+__device__ __forceinline__ int lanes_up_to(int x) {
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);       // from 1, 2, 4 and 8 lanes before
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);       // lane 15 of a row to rows 1 and 3
+    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);       // lane 31 to rows 2 and 3
+    return x;
+}
+
 // What cache_append works on beside the cache: strides in elements.
 struct AppendArgs {
     const void *q, *k, *v;

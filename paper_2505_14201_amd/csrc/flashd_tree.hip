@@ -98,17 +98,7 @@ __device__ __forceinline__ long long uniform(long long x) {
     return (long long)((uint64_t)(uint32_t)uniform((int)(x >> 32)) << 32 | (uint32_t)uniform((int)x));
 }
 
-// Sum over the lanes up to this one: within rows of 16 lanes, then the last of row 0 and of row 2 to the next row, then that of row 1 to
-// rows 2 and 3.  (Moves between lanes in the vector units; by LDS, as a shuffle goes, six of them one after the other take 0.3 us.)
-__device__ __forceinline__ int lanes_up_to(int x) {
-    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);       // from 1, 2, 4 and 8 lanes before
-    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
-    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
-    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
-    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);       // lane 15 of a row to rows 1 and 3
-    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);       // lane 31 to rows 2 and 3
-    return x;
-}
+// lanes_up_to() of numbers that are small as a rule
 __device__ __forceinline__ long long lanes_up_to(long long x) {
     if (__builtin_amdgcn_ballot_w64((x >> 24) != 0) == 0) return lanes_up_to((int)x);      // the sum has 30 bits
     const int lane = threadIdx.x & 63;
