@@ -26,7 +26,6 @@ namespace flashd {
 constexpr int kTreeBlock = 32;          // keys of a block: a wavefront's step
 constexpr int kTreeWaves = 4;
 constexpr int kTreeMostGroups = 768;    // workgroups of a launch, three per compute unit (see rows_per_cu) or two
-constexpr int kTreeMinBlocks = 4;       // blocks a workgroup takes at least
 // What the start of a unit counts, in blocks (of 64 keys in the tile kernel): with 0, 1, 2, 3, 4 and 6 the tile kernel took 28.8,
 // 27.8, 26.8, 26.3, 25.4 and 25.8 us for 128 units of 17 to 64 tiles, and for long units it made no difference; the rows kernel
 // took 103.8 us with 0 and 103.7 with 8, its own steps being shorter.
@@ -178,6 +177,15 @@ struct Walk {
     long long later_at;
     int later_b, later_h, later_tile, later_from;
 
+    // Places of a share where there are few in all, 0 where there are not: a share of fewer ends sooner, but leaves more parts to be
+    // joined.  Tile kernel (12 rows after 1000 keys, 48 after 4000, 64 each of 4 sequences; all with the merge): 15.8, 24.7, 26.1 us with 1,
+    // 18.5, 22.0, 26.2 with 2, 19.7, 21.4, 23.8 with 4.  Kernels whose wavefronts share out the blocks (one sequence of 1000
+    // keys, one of 4000, 8 of 100 to 1000): 13.8, 16.7, 19.4 us with 4, 14.1, 17.6, 18.2 with 8.
+    static __device__ __forceinline__ int few_places(long long total) {
+        if (KB == kBC) return total <= GRID / 2 ? 1 : total <= GRID ? 2 : total <= 4 * GRID ? 4 : 0;
+        return total <= 2 * GRID ? kTreeWaves : total <= 2 * kTreeWaves * GRID ? 2 * kTreeWaves : 0;
+    }
+
     // Along the row come, XCD by XCD, the 32 workgroups of each slot.
     __device__ __forceinline__ long long size(int slot) const {
         return slot == 0 ? per + lead : slot == kSlots - 1 ? per - lead : per;
@@ -265,14 +273,14 @@ struct Walk {
             total += wave_sum[k];
         }
         total = uniform(total);
-        // all workgroups, or as many as have kLeast places each
-        constexpr int kLeast = kTreeMinBlocks * kTreeBlock / KB;
-        const bool few = total <= (long long)kLeast * GRID;
-        per = few ? kLeast : (GRID & (GRID - 1)) == 0 ? (total + GRID - 1) / GRID : quotient(total + GRID - 1, GRID);
+        // all workgroups, or fewer with some places each
+        const int least = few_places(total);
+        const bool few = least > 0;
+        per = few ? least : (GRID & (GRID - 1)) == 0 ? (total + GRID - 1) / GRID : quotient(total + GRID - 1, GRID);
         lead = few ? 0 : (per * LEAD) >> 6;
         // Workgroup ids go round-robin over the 8 XCDs; neighbours along the row, which may read the same
         // keys, go to one.  An XCD's first 32 go to a compute unit each, the next 32 beside them, and so on.
-        const int of_xcd = few ? ((int)(total + kLeast - 1) / kLeast + 7) >> 3 : kOfXcd;
+        const int of_xcd = few ? ((int)(total + least - 1) / least + 7) >> 3 : kOfXcd;
         const int k = (int)blockIdx.x >> 3;
         w = ((int)blockIdx.x & 7) * of_xcd + k;
         const int place = w % kOfXcd;
