@@ -866,8 +866,8 @@ __global__ __launch_bounds__(kTreeWaves * kWave, rows_per_cu(D, FP8, NR)) void t
 // every KW-th 32-key block (RW KW = 4; two wavefronts to a row's keys for up to 64 rows, none share for 128).  Each wavefront brings the 16 keys of a tile that it would
 // in that layout: they lie in one page, so its copies have one scalar base.
 //
-// Up to 64 rows HBM bounds it: trees of 16 tokens after 500 to 8192 keys (32 sequences, 32 / 8 heads of 128) take 110 us for
-// 600 MB, 5.5 TB/s, one of 12 after 131000 keys 91 us, 5.9 TB/s; the start of a piece, when nothing of it has arrived, and
+// Up to 64 rows HBM bounds it: trees of 16 tokens after 500 to 8192 keys (32 sequences, 32 / 8 heads of 128) take 106 us for
+// 600 MB, 5.7 TB/s, one of 12 after 131000 keys 89 us, 6.0 TB/s; the start of a piece, when nothing of it has arrived, and
 // the unequal pace of the workgroups are the rest.  With 128 rows it is the instructions: chunks of 573 to 1000 tokens after 3180 to
 // 7000 keys are 277 GFLOP in 326 us, 850 TFLOP/s; the matrix pipe works 40 % of the cycles, the vector units 47 %, and
 // a wavefront's vector instructions do not run beside its own matrix instructions: with the weights of a tile formed between the
@@ -1107,6 +1107,18 @@ __global__ __launch_bounds__(kTreeWaves * kWave, 2) void tree_tile_kernel(TreeRu
             const int left = last_key - key, keys = !there || left < 0 ? 0 : left < 16 ? left : 16;
             return make_window(at, keys * ROW);
         };
+        // The queries and the first look at the table go ahead of the copies, and are waited for with them.
+        const int lane = lane_now(), col = lane & 31, hh = lane >> 5;
+        const int row = u.first + min(32 * rw + col, u.nrows - 1);
+        const uint16_t* qg = static_cast<const uint16_t*>(a.q) + row_at(now_r, u, row, a.q_stride, D);
+        u32x4 qf[NKK];
+#pragma unroll
+        for (int kk = 0; kk < NKK; ++kk) qf[kk] = *reinterpret_cast<const u32x4*>(qg + 16 * kk + 8 * hh);
+        // a table with holes: which of a tile's keys have no page is looked up tile by tile
+        const int first_col = (blk0 * kBC >> page_log2) + lane, last_here = min((blk0 + tiles) * kBC, last_key);
+        int first_page = 0;
+        if (first_col << page_log2 < last_here) first_page = now_r.c.table[(size_t)u.b * now_r.c.max_pages + first_col];
+        __builtin_amdgcn_sched_barrier(0);
         // the copies of tile 0's turn; behind the last tile windows are empty and copies bring zeros
         int page1 = page_of(1), page2 = page_of(2);      // of tiles now + 1 and now + 2
         Window vnext, knext;
@@ -1140,18 +1152,10 @@ __global__ __launch_bounds__(kTreeWaves * kWave, 2) void tree_tile_kernel(TreeRu
         // then may fill; before the output product V_i has landed.
         // (One body for all slots and both blocks: copies of it with constant operand addresses cost the code
         // that masks need several times, and with it the registers that hold U.)
-        const int lane = lane_now(), col = lane & 31, hh = lane >> 5;
-        // a table with holes: which of the tile's keys have no page is looked up tile by tile
-        bool gaps = false;
-        for (int k = (blk0 * kBC >> page_log2) + lane; k << page_log2 < min((blk0 + tiles) * kBC, last_key); k += kWave)
-            gaps |= page_at(now_r.c, u.b, k) < 0;
+        bool gaps = (unsigned)first_page >= (unsigned)pool_pages;
+        for (int k = first_col + kWave; k << page_log2 < last_here; k += kWave) gaps |= page_at(now_r.c, u.b, k) < 0;
         gaps = __builtin_amdgcn_ballot_w64(gaps) != 0;
-        const int row = u.first + min(32 * rw + col, u.nrows - 1);
-        const uint16_t* qg = static_cast<const uint16_t*>(a.q) + row_at(now_r, u, row, a.q_stride, D);
-        u32x4 qf[NKK];
-#pragma unroll
-        for (int kk = 0; kk < NKK; ++kk) qf[kk] = *reinterpret_cast<const u32x4*>(qg + 16 * kk + 8 * hh);
-        // Here to stay before the loop, as the compiler knows: it would else wait for them, and so for all copies, in every turn.
+        // The queries are here to stay before the loop, as the compiler knows: it would else wait for them, and so for all copies, in every turn.
         wait_copies();
         // a negative scale is taken into Q (exact), so that the largest dot product is the top score
         float c_log2 = (FP8 ? a.scale * now_r.c.kscale : a.scale) * kLog2e;
