@@ -4,12 +4,12 @@
 // For the new token i of sequence b and query head h, o = sum_j softmax_j(scale q.k_j) v_j over the
 // keys j < len (all of them) and the new keys len + j that the token's bits name (a chain: j <= i).
 // The heads of a kv group read the same keys, so the rows of a unit of work are pairs (token, head of the
-// group), 16 of them to a tile, and a unit is (sequence, kv head, row tile).
+// group), 16 to 128 of them to a tile (tree_rows()), and a unit is (sequence, kv head, row tile).
 //
 // Sequences differ in length by orders of magnitude and the host does not know by how much, so the
 // launch has a fixed number of workgroups and each finds its share of the work by itself: the units'
-// 32-key blocks form one long row, workgroup w takes blocks [w per, (w + 1) per).  All workgroups so stream the
-// same number of keys to within one block.  A unit that ends up in several workgroups is
+// blocks of 32 or 64 keys form one long row, of which each workgroup takes a stretch whose length depends only on the
+// row's (Walk).  A unit that ends up in several workgroups is
 // left as partial states (at most two per workgroup: its first unit, begun by the one before, and its
 // last) that merge_tree_kernel joins in the order of the keys: the result does not depend on timing.
 #include "flashd_common.h"
@@ -25,7 +25,7 @@ namespace flashd {
 
 constexpr int kTreeBlock = 32;          // keys of a block: a wavefront's step
 constexpr int kTreeWaves = 4;
-constexpr int kTreeMostGroups = 768;    // workgroups of a launch, three per compute unit (see rows_per_cu) or two
+constexpr int kTreeMostGroups = 768;    // workgroups of a launch at most: three per compute unit (rows_per_cu(); f32_per_cu() and two elsewhere)
 // What the start of a unit counts, in blocks (of 64 keys in the tile kernel): with 0, 1, 2, 3, 4 and 6 the tile kernel took 28.8,
 // 27.8, 26.8, 26.3, 25.4 and 25.8 us for 128 units of 17 to 64 tiles, and for long units it made no difference; the rows kernel
 // took 103.8 us with 0 and 103.7 with 8, its own steps being shorter.
