@@ -272,7 +272,7 @@ __global__ __launch_bounds__(kReserveThreads) void reserve_kernel(Paged c, int* 
     __shared__ int2 cols[kCacheMaxSeqs];         // that page's column (with kCopy: a copy is wanted), and the column behind the last
     __shared__ int count[kReserveBlocks];        // free pages of the blocks before
     __shared__ int waves[kReserveWaves];
-    __shared__ int beyond;
+    __shared__ unsigned long long beyond;
     constexpr int kCopy = 1 << 30;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int mask = (1 << c.page_log2) - 1;
@@ -332,9 +332,9 @@ __global__ __launch_bounds__(kReserveThreads) void reserve_kernel(Paged c, int* 
         bool copy = false;
         if (b < c.B) {
             const Seq s = seq_at(c, b);
-            const int tokens = max(min(c.q_start[b + 1], c.T) - s.row0, 0);
+            const int tokens = tokens_of(s.row0, c.q_start[b + 1], c.T);
             // tokens that the table has no columns for
-            if (tokens > s.n) atomicAdd(&beyond, (tokens - s.n + mask) >> c.page_log2);
+            if (tokens > s.n) atomicAdd(&beyond, (unsigned long long)columns_beyond(tokens, s.n, c.page_log2));
             const int* row = c.table + (size_t)b * c.max_pages;
             const int end = cols[b].y, p = last[b];
             const int refs_p = p >= 0 ? refs[p] : 0;
@@ -405,7 +405,7 @@ __global__ __launch_bounds__(kReserveThreads) void reserve_kernel(Paged c, int* 
         free_pages += all;
     }
     __syncthreads();
-    const int missing = max(run - free_pages, 0) + beyond;
+    const int missing = (int)min((unsigned long long)max(run - free_pages, 0) + beyond, 0x7fffffffull);
     if (tid == 0) report[0] = missing;
     if (missing > 0) {
         for (int b = tid; b < c.B; b += kReserveThreads) report[1 + b] = -1;

@@ -36,14 +36,30 @@ struct Seq {
     int len;        // keys in the cache before them
 };
 
-__device__ __forceinline__ Seq seq_at(const Paged& c, int b) {
+// New tokens of a sequence whose rows begin at `start` (>= 0) and end before `next`.  Whatever `next` is, it is brought between 0 and T before the
+// difference is formed, which then has no overflow.
+__host__ __device__ __forceinline__ int tokens_of(int start, int next, int T) {
+    const int end = next < 0 ? 0 : next < T ? next : T;
+    return end > start ? end - start : 0;
+}
+
+// `most`: keys that a row of the table has room for
+__host__ __device__ __forceinline__ Seq seq_of(int start, int next, int len, int T, int most) {
     Seq s;
-    const int most = c.max_pages << c.page_log2;
-    s.row0 = max(c.q_start[b], 0);
-    s.n = max(min(c.q_start[b + 1], c.T) - s.row0, 0);
-    s.len = min(max(c.lens[b], 0), most);
-    s.n = min(s.n, most - s.len);
+    s.row0 = start < 0 ? 0 : start;
+    s.len = len < 0 ? 0 : len < most ? len : most;
+    const int n = tokens_of(s.row0, next, T), room = most - s.len;
+    s.n = n < room ? n : room;
     return s;
+}
+
+// Columns that `tokens` new tokens need behind the end of the table, where the first n have a key.
+__host__ __device__ __forceinline__ int columns_beyond(int tokens, int n, int page_log2) {
+    return (int)(((uint32_t)(tokens - n) + (1u << page_log2) - 1u) >> page_log2);
+}
+
+__device__ __forceinline__ Seq seq_at(const Paged& c, int b) {
+    return seq_of(c.q_start[b], c.q_start[b + 1], c.lens[b], c.T, c.max_pages << c.page_log2);
 }
 
 // The page of column `col` (>= 0) of sequence b, -1 if there is none.
