@@ -331,7 +331,8 @@ typedef struct flashd_cache {
  * gets its table row and length; with parent[i] outside [0, B) it is empty.  refs follows: +1 for the
  * entries of table_out, -1 for those of c->table, so that the pages of sequences that nobody continues become
  * free and those that several continue are shared.  Nothing is copied: flashd_cache_reserve copies the
- * page that two twins would both write to.
+ * page that two twins would both write to.  Branch after a step's flashd_cache_commit, not before: rows that it moves
+ * lie in pages that must be the sequence's own.
  *   parent     int [B_out]
  *   table_out  int [B_out][max_pages], lens_out int [B_out]; neither may overlap table or lens
  */
@@ -343,7 +344,9 @@ int flashd_cache_fork(const flashd_cache* c, int* refs, const int* parent, int B
  * missing ones are taken from the free pages, lowest numbers to the lowest sequences.  A sequence with new
  * tokens whose last page is part filled and shared gets a page of its own there, and the keys
  * in it (all layers, K and V) are copied; of sequences that are a page's only holders the first keeps it.
- * c->table and refs are updated.
+ * Of pages behind its keys that it has already (left over from tokens that were not kept) those from the first one on that
+ * another row names too go back, and others are taken: after a twin of it was made, or its length set back.  So where new
+ * tokens are written to nobody else reads.  c->table and refs are updated.
  *   report  int [1 + B], overwritten: report[0] = 0, or how many pages are missing (free ones, and columns of
  *           the table): then no sequence has got any and no page has been copied (pages given
  *           back stay so).  report[1 + b] = the page that sequence b's last page was copied from, or -1.
@@ -408,6 +411,7 @@ size_t flashd_tree_workspace_bytes(int Hq, int Hkv, int max_q, int d, int dtype)
  *            than the one before it or is no token of the sequence.  NULL (max_keep 0): the first n_keep[b]
  *            tokens, nothing moves.
  *   n_keep   int [B], or NULL: max_keep, or all new tokens without `keep`
+ * With `keep` the pages of the new tokens are the sequence's own, as flashd_cache_reserve has left them: no other row names them.
  *   lens_out int [B]; must not overlap lens
  */
 int flashd_cache_commit(const flashd_cache* c, const int* q_start, const int* keep, int max_keep,

@@ -235,12 +235,14 @@ hipError_t launch_cache_fork(const Paged& c, int* refs, const int* parent, int B
 // ---- reserving ------------------------------------------------------------------------------
 //
 // One workgroup, so that which sequence gets which page does not depend on the order of anything:
-//   1. pages behind a sequence's keys go back (refs - 1);
-//   2. a sequence wants the pages from its first empty column to its last, and one more where its
+//   1. pages behind a sequence's keys and new tokens go back (refs - 1);
+//   2. so do, of a sequence with new tokens, the pages behind its keys from the first one on that another row names too (twins of
+//      a sequence that had pages left over, or of one whose length was set back): what is written there is its own;
+//   3. a sequence wants the pages from its first empty column to its last, and one more where its
 //      last page is part filled and shared (unless it is the first of sequences that are the
 //      page's only holders and all grow: that one keeps it);
-//   3. free pages (refs 0) are numbered in ascending order, k-th free page -> k-th wanted page.
-// Should there be too few, step 3 is left out and the number missing reported.
+//   4. free pages (refs 0) are numbered in ascending order, k-th free page -> k-th wanted page.
+// Should there be too few, step 4 is left out and the number missing reported.
 // Latency bounds it, six reads one after the other: 3.6 us for 32 sequences, 9.1 for 64 whose table and counts another
 // kernel has just written (they come from beyond this die's L2).
 constexpr int kReserveThreads = 1024;
@@ -266,6 +268,24 @@ __device__ __forceinline__ int block_scan(int x, int* waves, int& total) {
     return before + in - x;
 }
 
+// Of the columns lo <= col < end of a row the first whose page is named more than once; `end` where there is none up to the first
+// empty one.  Four columns at a time, whose reads run together.
+__device__ __forceinline__ int shared_column(const int* row, const int* refs, int P, int lo, int end) {
+    for (int col = lo; col < end; col += 4) {
+        int page[4], held[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) page[i] = col + i < end ? row[col + i] : -1;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) held[i] = (unsigned)page[i] < (unsigned)P ? refs[page[i]] : 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if (page[i] < 0) return end;
+            if (held[i] > 1) return col + i;
+        }
+    }
+    return end;
+}
+
 __global__ __launch_bounds__(kReserveThreads) void reserve_kernel(Paged c, int* refs, int* report) {
     __shared__ int at[kCacheMaxSeqs + 1];        // wanted pages of the sequences before b
     __shared__ __align__(16) int last[kCacheMaxSeqs];        // part-filled last page of a sequence that grows, or -1
@@ -273,16 +293,18 @@ __global__ __launch_bounds__(kReserveThreads) void reserve_kernel(Paged c, int* 
     __shared__ int count[kReserveBlocks];        // free pages of the blocks before
     __shared__ int waves[kReserveWaves];
     __shared__ unsigned long long beyond;
+    __shared__ int shared_behind;                // some sequence has a shared page behind its keys
     constexpr int kCopy = 1 << 30;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int mask = (1 << c.page_log2) - 1;
     const int each = (c.B + kReserveThreads - 1) / kReserveThreads;
-    if (tid == 0) beyond = 0;
+    if (tid == 0) beyond = 0, shared_behind = 0;
     if (tid < (-c.B & 3)) last[c.B + tid] = -1;          // read four at a time
 
     // 1. back to the pool.  (`lo_page`, `end_page`: what the row has in the first column that it may want a page for and
     // in the last one, read here beside the others)
     int lo_page[kReserveEach], end_page[kReserveEach];
+    unsigned long long lacking = 0;
 #pragma unroll
     for (int k = 0; k < kReserveEach; ++k) {
         const int b = k * kReserveThreads + tid;
@@ -304,73 +326,105 @@ __global__ __launch_bounds__(kReserveThreads) void reserve_kernel(Paged c, int* 
             if (p < c.P) atomicSub(&refs[p], 1);
         }
         last[b] = part;
-        cols[b] = int2{s.len >> c.page_log2, end};
+        cols[b].y = end;
+        // tokens that the table has no columns for
+        lacking += (unsigned long long)columns_beyond(tokens_of(s.row0, c.q_start[b + 1], c.T), s.n, c.page_log2);
     }
     // (refs have not been read yet, so what follows finds them as these atomics, waited for at the barrier,
     // have left them)
     __builtin_amdgcn_s_waitcnt(0);
     __syncthreads();
+    if (lacking > 0) atomicAdd(&beyond, lacking);
 
     // The pool is counted by blocks of 256 m pages that each fall to one wavefront.  Its first block is kept, as long as it is
-    // one read per lane and 64 pages; it is on its way while step 2 looks at rows.
+    // one read per lane and 64 pages; it is on its way while rows are looked at.
     const int m = (c.P + 256 * kReserveBlocks - 1) / (256 * kReserveBlocks);
     const int blocks = (c.P + 256 * m - 1) / (256 * m);
     int held[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int p = wave * 256 + 64 * i + lane;
-        held[i] = m == 1 && p < c.P ? refs[p] : 1;
-    }
+    int cut[kReserveEach];                       // the column from which step 2 gives back
 
-    // 2. what each wants
-    int run = 0;
+    // 2. and 3. what each wants.  Pages are looked at and nothing is changed, so that all see the same counts; where one of them has to go
+    // back, that is done for all and the wants formed anew (no page is shared by more rows than before, so the second time none has to).
+    int run;
+    for (;;) {
+        run = 0;
 #pragma unroll
-    for (int k = 0; k < kReserveEach; ++k) {
-        if (k >= each) break;
-        const int b = k * kReserveThreads + tid;
-        int want = 0;
-        bool copy = false;
-        if (b < c.B) {
-            const Seq s = seq_at(c, b);
-            const int tokens = tokens_of(s.row0, c.q_start[b + 1], c.T);
-            // tokens that the table has no columns for
-            if (tokens > s.n) atomicAdd(&beyond, (unsigned long long)columns_beyond(tokens, s.n, c.page_log2));
-            const int* row = c.table + (size_t)b * c.max_pages;
-            const int end = cols[b].y, p = last[b];
-            const int refs_p = p >= 0 ? refs[p] : 0;
-            int lo = s.n == 0 ? end : min((s.len + mask) >> c.page_log2, end), hi = end;
-            if (lo < hi) {
-                if (lo_page[k] < 0) hi = lo;
-                else if (end_page[k] >= 0) lo = hi;
-            }
-            while (lo < hi) {                    // the first empty column
-                const int mid = (lo + hi) >> 1;
-                if (row[mid] < 0) hi = mid;
-                else lo = mid + 1;
-            }
-            want = end - lo;
-            if (refs_p > 1) {
-                int holders = 0, before = 0;
-#pragma unroll 4
-                for (int o = 0; o < c.B; o += 4) {
-                    const int4 x = *reinterpret_cast<const int4*>(&last[o]);
-                    const int four[4] = {x.x, x.y, x.z, x.w};
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const bool same = four[i] == p;
-                        holders += same ? 1 : 0;
-                        before += same && o + i < b ? 1 : 0;
-                    }
-                }
-                copy = holders < refs_p || before > 0;
-            }
-            report[1 + b] = copy ? p : -1;
-            if (copy) cols[b].x |= kCopy;
+        for (int i = 0; i < 4; ++i) {
+            const int p = wave * 256 + 64 * i + lane;
+            held[i] = m == 1 && p < c.P ? refs[p] : 1;
         }
-        int all;
-        const int ex = block_scan(want + (copy ? 1 : 0), waves, all);
-        if (b < c.B) at[b] = run + ex;
-        run += all;
+#pragma unroll
+        for (int k = 0; k < kReserveEach; ++k) {
+            if (k >= each) break;
+            const int b = k * kReserveThreads + tid;
+            int want = 0;
+            bool copy = false;
+            if (b < c.B) {
+                const Seq s = seq_at(c, b);
+                const int* row = c.table + (size_t)b * c.max_pages;
+                const int end = cols[b].y, p = last[b];
+                const int refs_p = p >= 0 ? refs[p] : 0;
+                int lo = s.n == 0 ? end : min((s.len + mask) >> c.page_log2, end), hi = end;
+                cut[k] = end;
+                if (lo < end && lo_page[k] >= 0) {
+                    const int c0 = shared_column(row, refs, c.P, lo, end);
+                    cut[k] = c0;
+                    if (c0 < end) shared_behind = 1;
+                }
+                if (lo < hi) {
+                    if (lo_page[k] < 0) hi = lo;
+                    else if (end_page[k] >= 0) lo = hi;
+                }
+                while (lo < hi) {                    // the first empty column
+                    const int mid = (lo + hi) >> 1;
+                    if (row[mid] < 0) hi = mid;
+                    else lo = mid + 1;
+                }
+                want = end - lo;
+                if (refs_p > 1) {
+                    int holders = 0, before = 0;
+#pragma unroll 4
+                    for (int o = 0; o < c.B; o += 4) {
+                        const int4 x = *reinterpret_cast<const int4*>(&last[o]);
+                        const int four[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const bool same = four[i] == p;
+                            holders += same ? 1 : 0;
+                            before += same && o + i < b ? 1 : 0;
+                        }
+                    }
+                    copy = holders < refs_p || before > 0;
+                }
+                report[1 + b] = copy ? p : -1;
+                cols[b].x = (s.len >> c.page_log2) | (copy ? kCopy : 0);
+            }
+            int all;
+            const int ex = block_scan(want + (copy ? 1 : 0), waves, all);
+            if (b < c.B) at[b] = run + ex;
+            run += all;
+        }
+        if (shared_behind == 0) break;               // (set before the last scan's barriers)
+#pragma unroll
+        for (int k = 0; k < kReserveEach; ++k) {
+            const int b = k * kReserveThreads + tid;
+            if (k >= each || b >= c.B || cut[k] >= cols[b].y) continue;
+            int* row = c.table + (size_t)b * c.max_pages;
+            for (int col = cut[k]; col < cols[b].y; ++col) {
+                const int p = row[col];
+                if (p < 0) break;
+                row[col] = -1;
+                if (p < c.P) atomicSub(&refs[p], 1);
+            }
+            end_page[k] = -1;
+            if (cut[k] == min((seq_at(c, b).len + mask) >> c.page_log2, cols[b].y)) lo_page[k] = -1;
+        }
+        __builtin_amdgcn_s_waitcnt(0);
+        __syncthreads();
+        if (tid == 0) shared_behind = 0;
+        __syncthreads();
+        // counts that this compute unit has read lie in its cache as they were
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
     }
     if (tid == 0) at[c.B] = run;
 
@@ -412,7 +466,7 @@ __global__ __launch_bounds__(kReserveThreads) void reserve_kernel(Paged c, int* 
         return;
     }
 
-    // 3. the k-th free page to the k-th wanted one
+    // 4. the k-th free page to the k-th wanted one
     for (int k = wave; k < blocks; k += kReserveWaves) {
         int rank = count[k];
         for (int j = 0; j < 4 * m && rank < run; ++j) {

@@ -434,7 +434,7 @@ def cache_fork(parent, refs, table, lens, table_out, lens_out, stream=None) -> N
 
 
 def cache_reserve(kcache, vcache, refs, table, lens, q_start, report, stream=None) -> None:
-    """flashd_cache_reserve: every sequence gets exactly the pages of its keys and new tokens.
+    """flashd_cache_reserve: every sequence gets exactly the pages of its keys and new tokens; those it is to write to are its own.
     `report`: int32 [1 + B], receives the number of pages missing (0: all went well) and for each
     sequence the page that its shared last page was copied from, or -1."""
     if stream is None and _taken(_native.cache_reserve(kcache, vcache, refs, table, lens, q_start, report)):

@@ -1,0 +1,154 @@
+"""Sequences that branch, grow, keep part of what was drafted and are set back: pages and counts as the list model has them, every page
+that is written to named once, and every sequence's keys and values its own."""
+import random
+
+import pytest
+import torch
+
+from paper_2505_14201_amd import flashd
+from tests import paged_util as pu
+from tests.pages_model import Pages, check_own
+
+pytestmark = pytest.mark.gpu
+
+LAYERS, HKV, D = 2, 1, 64
+
+
+class World:
+    """Pools whose rows hold a token's number (K) and its negative (V), and per sequence the list of its tokens."""
+
+    def __init__(self, B, page, P, max_pages):
+        self.page, self.max_pages = page, max_pages
+        z = lambda *s: torch.zeros(*s, dtype=torch.int32, device="cuda")                # noqa: E731
+        self.k, self.v = (torch.zeros(LAYERS, P, HKV, page, D, device="cuda") for _ in "kv")
+        self.refs, self.lens = z(P), z(B)
+        self.table = torch.full((B, max_pages), -1, dtype=torch.int32, device="cuda")
+        self.model = Pages(self.table.cpu(), [0] * B, P)
+        self.held = [[] for _ in range(B)]
+        self.next = 1
+
+    def fork(self, parent):
+        t, l = torch.full((len(parent), self.max_pages), -9, dtype=torch.int32, device="cuda"), torch.zeros(len(parent), dtype=torch.int32, device="cuda")
+        flashd.cache_fork(pu.ints(parent).cuda(), self.refs, self.table, self.lens, t, l)
+        self.table, self.lens = t, l
+        self.held = [list(self.held[p]) if 0 <= p < len(self.held) else [] for p in parent]
+        self.model.fork(parent)
+        self.agrees()
+
+    def set_back(self, lens):
+        self.model.lens = list(lens)
+        self.lens = pu.ints(lens).cuda()
+        self.held = [h[:l] for h, l in zip(self.held, lens)]
+
+    def reserve(self, some):
+        self.some, starts = some, [0]
+        for m in some:
+            starts.append(starts[-1] + m)
+        self.starts, self.q_start = starts, pu.ints(starts).cuda()
+        report = torch.full((len(some) + 1,), -9, dtype=torch.int32, device="cuda")
+        flashd.cache_reserve(self.k, self.v, self.refs, self.table, self.lens, self.q_start, report)
+        want, _ = self.model.reserve(some, self.page)
+        assert report.tolist() == want
+        self.agrees()
+        return want[0]
+
+    def append(self):
+        """A number of its own for every new token, into every layer."""
+        T = self.starts[-1]
+        self.new = list(range(self.next, self.next + T))
+        self.next += T
+        if T:
+            ids = torch.tensor(self.new, dtype=torch.float32, device="cuda").view(T, 1, 1).expand(T, HKV, D).contiguous()
+            for y in range(LAYERS):
+                flashd.cache_append(ids.clone(), ids + 0.25 * y, -ids - 0.25 * y, torch.empty_like(ids), self.k[y], self.v[y], self.table,
+                                    self.lens, self.q_start)
+
+    def commit(self, keep):
+        most = max([len(x) for x in keep] + [1])
+        out = torch.full_like(self.lens, -9)
+        flashd.cache_commit(self.k, self.v, self.table, self.lens, self.q_start, out,
+                            keep=pu.ints([x + [0] * (most - len(x)) for x in keep]).cuda(), n_keep=pu.ints([len(x) for x in keep]).cuda())
+        self.lens = out
+        for b, x in enumerate(keep):
+            self.held[b] += [self.new[self.starts[b] + i] for i in x]
+        self.model.lens = [len(h) for h in self.held]
+
+    def agrees(self):
+        assert self.table.tolist() == self.model.table.tolist()
+        assert self.lens.tolist() == self.model.lens
+        assert self.refs.tolist() == self.model.refs
+
+    def contents(self, new=False, without=()):
+        """Every sequence's tokens (with those just appended) are in its pages."""
+        b = [x for x, h in enumerate(self.held) for _ in range(len(h) + new * self.some[x]) if x not in without]
+        j = [i for x, h in enumerate(self.held) for i in range(len(h) + new * self.some[x]) if x not in without]
+        ids = [t for x, h in enumerate(self.held) if x not in without
+               for t in h + (self.new[self.starts[x]:self.starts[x + 1]] if new else [])]
+        b, j, ids = (torch.tensor(x, dtype=torch.long, device="cuda") for x in (b, j, ids))
+        p = self.table.long()[b, j // self.page]
+        assert (p >= 0).all()
+        for y in range(LAYERS):
+            assert (self.k[y, p, :, j % self.page] == (ids + 0.25 * y).view(-1, 1, 1)).all()
+            assert (self.v[y, p, :, j % self.page] == -(ids + 0.25 * y).view(-1, 1, 1)).all()
+
+
+def step(w, some, keep):
+    assert w.reserve(some) == 0
+    check_own(w.table.tolist(), w.refs.tolist(), w.lens.tolist(), some, w.page)
+    w.append()
+    w.contents(new=True)
+    w.commit(keep)
+    w.contents()
+
+
+@pytest.mark.parametrize("B,page,P,max_pages", [(3, 16, 80, 8), (17, 32, 500, 20), (70, 16, 9000, 30), (1500, 16, 70000, 25)])
+def test_lives_of_sequences(B, page, P, max_pages):
+    rng = random.Random(B + 1)
+    w = World(B, page, P, max_pages)
+    for turn in range(8):
+        if turn:
+            parent = [rng.choice([b, b, b, rng.randrange(B), -1]) for b in range(B)]
+            if turn == 3:
+                parent = [rng.randrange(B) for _ in range(B + 5)]
+                B += 5
+            w.fork(parent)
+        if turn % 3 == 2:
+            w.set_back([rng.randint(0, l) if rng.random() < 0.3 else l for l in w.model.lens])
+        some = [rng.choice([0, 1, 1, 2, rng.randint(0, 2 * page)]) for _ in range(B)]
+        some = [min(m, max_pages * page - l) for m, l in zip(some, w.model.lens)]
+        step(w, some, [sorted(rng.sample(range(m), rng.randint(0, m))) for m in some])
+
+
+@pytest.mark.parametrize("keys,drafts,kept,then", [(15, 4, 1, 1), (16, 4, 0, 2), (20, 30, 1, 16), (20, 16, 0, 16), (33, 40, 0, 7), (0, 40, 0, 5), (48, 1, 0, 1)])
+def test_twins_of_a_sequence_with_pages_left_over(keys, drafts, kept, then):
+    """Branching right after part of the drafts was dropped: what is left over is nobody's to share."""
+    w = World(2, 16, 40, 8)
+    step(w, [keys, 3], [list(range(keys)), [0, 1, 2]])
+    step(w, [drafts, 1], [list(range(kept)), []])
+    w.fork([0, 1, 0, 0])
+    step(w, [then, 1, then, 0], [list(range(then)), [0], list(range(then)), []])
+    step(w, [1, 1, 1, 1], [[0], [0], [0], [0]])
+
+
+def test_a_twin_that_is_set_back():
+    """One twin's length falls to an earlier page, and to the middle of the page both are in: it must not write over the other's keys."""
+    w = World(1, 16, 40, 8)
+    step(w, [70], [list(range(70))])
+    w.fork([0, 0, 0, 0])
+    w.set_back([70, 32, 20, 66])
+    step(w, [1, 40, 40, 9], [[0], list(range(0, 40, 3)), [], list(range(9))])
+    w.fork([3, 2, 1, 0])
+    w.set_back([0, 5, 16, 70])
+    step(w, [100, 3, 20, 1], [[0], [0], list(range(20)), []])
+
+
+def test_shared_pages_behind_the_keys_of_long_rows():
+    """Hundreds of left-over columns, the first shared one in their middle."""
+    w = World(2, 16, 3000, 520)
+    step(w, [5, 8000], [[0], list(range(8000))])
+    w.fork([0, 1, 1])
+    w.set_back([1, 8000, 3000])
+    w.reserve([0, 0, 1000])                     # sequence 2 takes pages of its own behind key 3000
+    w.fork([0, 1, 2, 2])
+    w.set_back([1, 8000, 3000, 40])
+    step(w, [1, 1, 4000, 6000], [[0], [0], list(range(0, 4000, 7)), []])
