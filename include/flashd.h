@@ -278,7 +278,8 @@ int flashd_skip_stats(const void* q, const void* k, int B, int Hq, int Hkv, int 
  *             and is [Hkv][page][d], contiguous.  So [layers][P][Hkv][page][d] may be one tensor, or a page's
  *             K and V lie side by side.  Different pages (and layers) must not share memory, nor
  *             K and V where they are written.
- *   table     int [B][max_pages]: page numbers, the pages a sequence owns first, then -1.
+ *   table     int [B][max_pages]: page numbers, the pages a sequence owns first, then -1.  (-2 - p: page p, held back by
+ *             flashd_cache_reserve; named in refs, no page to all others.)
  *   lens      int [B]: the keys each sequence has in the cache.
  *   refs      int [P]: how many table entries name each page; a page with 0 is free.
  *   q_start   int [B + 1]: the new tokens of sequence b are rows q_start[b] .. q_start[b + 1] - 1 of packed
@@ -349,7 +350,10 @@ int flashd_cache_fork(const flashd_cache* c, int* refs, const int* parent, int B
  * tokens are written to nobody else reads.  c->table and refs are updated.
  *   report  int [1 + B], overwritten: report[0] = 0, or how many pages are missing (free ones, and columns of
  *           the table): then no sequence has got any and no page has been copied (pages given
- *           back stay so).  report[1 + b] = the page that sequence b's last page was copied from, or -1.
+ *           back stay so), and of each sequence with new tokens a part-filled page that others name as well is held back: its
+ *           entry is -2 - page, so that the rest of the step, which may be recorded, neither writes to it nor reads it.  Keep the
+ *           old lens then, let sequences end and call again: entries held back at column lens[b] / page are taken up again,
+ *           those behind go back.  report[1 + b] = the page that sequence b's last page was copied from, or -1.
  */
 int flashd_cache_reserve(const flashd_cache* c, int* refs, const int* q_start, int* report, void* stream);
 
@@ -368,7 +372,7 @@ int flashd_cache_reserve(const flashd_cache* c, int* refs, const int* q_start, i
  *   positions       int [T], or NULL: a token's position is its key number
  *   inv_freq        float [rot / 2]; NULL with rot == 0.  rot is a multiple of 16, at most d.
  *   q_weight, k_weight   [d] in `dtype`, or NULL
- * Tokens without a page (reserve reported them missing) get their q_out; K and V are dropped.
+ * Tokens without a page (reserve reported them missing, or holds the page back) get their q_out; K and V are dropped.
  * T == 0 is a call without work.
  */
 int flashd_cache_append(const flashd_cache* c, int layer, const void* q, long long q_stride, const void* k,

@@ -219,9 +219,10 @@ __global__ __launch_bounds__(256) void fork_kernel(Paged c, int* refs, const int
     const int now = i < c.B ? c.table[(size_t)i * c.max_pages + col] : -1;
     const int next = from < 0 ? -1 : c.table[(size_t)from * c.max_pages + col];
     if (i < B_out) table_out[(size_t)i * c.max_pages + col] = next;
-    if (next != now) {
-        if ((unsigned)next < (unsigned)c.P) atomicAdd(&refs[next], 1);
-        if ((unsigned)now < (unsigned)c.P) atomicSub(&refs[now], 1);
+    const int page = named_page(next), was = named_page(now);
+    if (page != was) {
+        if ((unsigned)page < (unsigned)c.P) atomicAdd(&refs[page], 1);
+        if ((unsigned)was < (unsigned)c.P) atomicSub(&refs[was], 1);
     }
 }
 
@@ -242,9 +243,10 @@ hipError_t launch_cache_fork(const Paged& c, int* refs, const int* parent, int B
 //      last page is part filled and shared (unless it is the first of sequences that are the
 //      page's only holders and all grow: that one keeps it);
 //   4. free pages (refs 0) are numbered in ascending order, k-th free page -> k-th wanted page.
-// Should there be too few, step 4 is left out and the number missing reported.
-// Latency bounds it, six reads one after the other: 3.6 us for 32 sequences, 9.1 for 64 whose table and counts another
-// kernel has just written (they come from beyond this die's L2).
+// Should there be too few, step 4 is left out and the number missing reported; a growing sequence's part-filled page that others name
+// too is then held back (named_page()), so that a step that runs on does not write to it, until the next call.
+// Latency bounds it, six reads one after the other: 3.9 us for 32 sequences (3.6 where no page lies behind a sequence's keys), 9.0 for
+// 64 whose table and counts another kernel has just written (they come from beyond this die's L2).
 constexpr int kReserveThreads = 1024;
 constexpr int kReserveWaves = kReserveThreads / kWave;
 constexpr int kReserveEach = kCacheMaxSeqs / kReserveThreads;     // sequences of a thread
@@ -268,8 +270,8 @@ __device__ __forceinline__ int block_scan(int x, int* waves, int& total) {
     return before + in - x;
 }
 
-// Of the columns lo <= col < end of a row the first whose page is named more than once; `end` where there is none up to the first
-// empty one.  Four columns at a time, whose reads run together.
+// Of the columns lo <= col < end of a row the first whose page is named more than once or held back; `end` where there is none up to
+// the first empty one.  Four columns at a time, whose reads run together.
 __device__ __forceinline__ int shared_column(const int* row, const int* refs, int P, int lo, int end) {
     for (int col = lo; col < end; col += 4) {
         int page[4], held[4];
@@ -279,8 +281,8 @@ __device__ __forceinline__ int shared_column(const int* row, const int* refs, in
         for (int i = 0; i < 4; ++i) held[i] = (unsigned)page[i] < (unsigned)P ? refs[page[i]] : 0;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            if (page[i] < 0) return end;
-            if (held[i] > 1) return col + i;
+            if (page[i] == -1) return end;
+            if (page[i] < -1 || held[i] > 1) return col + i;
         }
     }
     return end;
@@ -289,46 +291,49 @@ __device__ __forceinline__ int shared_column(const int* row, const int* refs, in
 __global__ __launch_bounds__(kReserveThreads) void reserve_kernel(Paged c, int* refs, int* report) {
     __shared__ int at[kCacheMaxSeqs + 1];        // wanted pages of the sequences before b
     __shared__ __align__(16) int last[kCacheMaxSeqs];        // part-filled last page of a sequence that grows, or -1
-    __shared__ int2 cols[kCacheMaxSeqs];         // that page's column (with kCopy: a copy is wanted), and the column behind the last
+    __shared__ int2 cols[kCacheMaxSeqs];         // that page's column (kShared: others name the page, kCopy: a copy is wanted), and the column behind the last
     __shared__ int count[kReserveBlocks];        // free pages of the blocks before
     __shared__ int waves[kReserveWaves];
     __shared__ unsigned long long beyond;
     __shared__ int shared_behind;                // some sequence has a shared page behind its keys
-    constexpr int kCopy = 1 << 30;
+    constexpr int kCopy = 1 << 30, kShared = 1 << 29;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int mask = (1 << c.page_log2) - 1;
     const int each = (c.B + kReserveThreads - 1) / kReserveThreads;
     if (tid == 0) beyond = 0, shared_behind = 0;
     if (tid < (-c.B & 3)) last[c.B + tid] = -1;          // read four at a time
 
-    // 1. back to the pool.  (`lo_page`, `end_page`: what the row has in the first column that it may want a page for and
-    // in the last one, read here beside the others)
-    int lo_page[kReserveEach], end_page[kReserveEach];
+    // 1. back to the pool.  (`from`: the first column that the row may want a page for; `lo_page`, `end_page`: what it has there and in the
+    // last one, read here beside the others)
+    int from[kReserveEach], lo_page[kReserveEach], end_page[kReserveEach];
     unsigned long long lacking = 0;
 #pragma unroll
     for (int k = 0; k < kReserveEach; ++k) {
         const int b = k * kReserveThreads + tid;
+        from[k] = 0;
         lo_page[k] = end_page[k] = -1;
         if (b >= c.B) continue;
-        const Seq s = seq_at(c, b);
+        const int next = c.q_start[b + 1];
+        const Seq s = seq_of(c.q_start[b], next, c.lens[b], c.T, c.max_pages << c.page_log2);
         int* row = c.table + (size_t)b * c.max_pages;
-        const int end = (s.len + s.n + mask) >> c.page_log2;
-        const int part = s.n > 0 && (s.len & mask) != 0 ? page_at(c, b, s.len >> c.page_log2) : -1;
-        const int lo = (s.len + mask) >> c.page_log2;
+        const int end = (s.len + s.n + mask) >> c.page_log2, lo = (s.len + mask) >> c.page_log2, first = s.len >> c.page_log2;
+        int part = lo > first ? row[first] : -1, p = end < c.max_pages ? row[end] : -1;
         if (lo < end) {
             lo_page[k] = row[lo];
             end_page[k] = row[end - 1];
         }
-        for (int col = end; col < c.max_pages; ++col) {
-            const int p = row[col];
-            if (p < 0) break;                    // owned pages come first in a row
+        if (part < -1) row[first] = part = named_page(part);        // held back by an earlier call that found too few pages
+        for (int col = end; p != -1;) {          // owned pages come first in a row
             row[col] = -1;
-            if (p < c.P) atomicSub(&refs[p], 1);
+            const int page = named_page(p);
+            if (page < c.P) atomicSub(&refs[page], 1);
+            p = ++col < c.max_pages ? row[col] : -1;
         }
-        last[b] = part;
-        cols[b].y = end;
+        from[k] = s.n > 0 ? lo : end;
+        last[b] = s.n > 0 && part < c.P ? part : -1;
+        cols[b] = int2{first, end};
         // tokens that the table has no columns for
-        lacking += (unsigned long long)columns_beyond(tokens_of(s.row0, c.q_start[b + 1], c.T), s.n, c.page_log2);
+        lacking += (unsigned long long)columns_beyond(tokens_of(s.row0, next, c.T), s.n, c.page_log2);
     }
     // (refs have not been read yet, so what follows finds them as these atomics, waited for at the barrier,
     // have left them)
@@ -340,14 +345,8 @@ __global__ __launch_bounds__(kReserveThreads) void reserve_kernel(Paged c, int* 
     // one read per lane and 64 pages; it is on its way while rows are looked at.
     const int m = (c.P + 256 * kReserveBlocks - 1) / (256 * kReserveBlocks);
     const int blocks = (c.P + 256 * m - 1) / (256 * m);
-    int held[4];
-    int cut[kReserveEach];                       // the column from which step 2 gives back
-
-    // 2. and 3. what each wants.  Pages are looked at and nothing is changed, so that all see the same counts; where one of them has to go
-    // back, that is done for all and the wants formed anew (no page is shared by more rows than before, so the second time none has to).
-    int run;
-    for (;;) {
-        run = 0;
+    int held[4], shares[kReserveEach];           // shares: how many rows name the part-filled page
+    auto look = [&]() __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int p = wave * 256 + 64 * i + lane;
@@ -355,76 +354,90 @@ __global__ __launch_bounds__(kReserveThreads) void reserve_kernel(Paged c, int* 
         }
 #pragma unroll
         for (int k = 0; k < kReserveEach; ++k) {
-            if (k >= each) break;
             const int b = k * kReserveThreads + tid;
-            int want = 0;
-            bool copy = false;
-            if (b < c.B) {
-                const Seq s = seq_at(c, b);
-                const int* row = c.table + (size_t)b * c.max_pages;
-                const int end = cols[b].y, p = last[b];
-                const int refs_p = p >= 0 ? refs[p] : 0;
-                int lo = s.n == 0 ? end : min((s.len + mask) >> c.page_log2, end), hi = end;
-                cut[k] = end;
-                if (lo < end && lo_page[k] >= 0) {
-                    const int c0 = shared_column(row, refs, c.P, lo, end);
-                    cut[k] = c0;
-                    if (c0 < end) shared_behind = 1;
-                }
-                if (lo < hi) {
-                    if (lo_page[k] < 0) hi = lo;
-                    else if (end_page[k] >= 0) lo = hi;
-                }
-                while (lo < hi) {                    // the first empty column
-                    const int mid = (lo + hi) >> 1;
-                    if (row[mid] < 0) hi = mid;
-                    else lo = mid + 1;
-                }
-                want = end - lo;
-                if (refs_p > 1) {
-                    int holders = 0, before = 0;
-#pragma unroll 4
-                    for (int o = 0; o < c.B; o += 4) {
-                        const int4 x = *reinterpret_cast<const int4*>(&last[o]);
-                        const int four[4] = {x.x, x.y, x.z, x.w};
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const bool same = four[i] == p;
-                            holders += same ? 1 : 0;
-                            before += same && o + i < b ? 1 : 0;
-                        }
-                    }
-                    copy = holders < refs_p || before > 0;
-                }
-                report[1 + b] = copy ? p : -1;
-                cols[b].x = (s.len >> c.page_log2) | (copy ? kCopy : 0);
-            }
-            int all;
-            const int ex = block_scan(want + (copy ? 1 : 0), waves, all);
-            if (b < c.B) at[b] = run + ex;
-            run += all;
+            shares[k] = k < each && b < c.B && last[b] >= 0 ? refs[last[b]] : 0;
         }
-        if (shared_behind == 0) break;               // (set before the last scan's barriers)
+    };
+    look();
+
+    // 2. pages behind the keys.  All are looked at before any goes back, so that all see the same counts.
+    int cut[kReserveEach];                       // the column from which they go
+#pragma unroll
+    for (int k = 0; k < kReserveEach; ++k) {
+        cut[k] = 0x7fffffff;
+        if (lo_page[k] == -1) continue;
+        const int b = k * kReserveThreads + tid, p = lo_page[k], end = cols[b].y;
+        cut[k] = p < -1 || (p < c.P && refs[p] > 1) ? from[k] : shared_column(c.table + (size_t)b * c.max_pages, refs, c.P, from[k] + 1, end);
+        if (cut[k] < end) shared_behind = 1;
+    }
+    __syncthreads();
+    if (shared_behind != 0) {
 #pragma unroll
         for (int k = 0; k < kReserveEach; ++k) {
             const int b = k * kReserveThreads + tid;
-            if (k >= each || b >= c.B || cut[k] >= cols[b].y) continue;
+            if (lo_page[k] == -1 || cut[k] >= cols[b].y) continue;
             int* row = c.table + (size_t)b * c.max_pages;
             for (int col = cut[k]; col < cols[b].y; ++col) {
                 const int p = row[col];
-                if (p < 0) break;
+                if (p == -1) break;
                 row[col] = -1;
-                if (p < c.P) atomicSub(&refs[p], 1);
+                const int page = named_page(p);
+                if (page < c.P) atomicSub(&refs[page], 1);
             }
             end_page[k] = -1;
-            if (cut[k] == min((seq_at(c, b).len + mask) >> c.page_log2, cols[b].y)) lo_page[k] = -1;
+            if (cut[k] == from[k]) lo_page[k] = -1;
         }
         __builtin_amdgcn_s_waitcnt(0);
         __syncthreads();
-        if (tid == 0) shared_behind = 0;
-        __syncthreads();
         // counts that this compute unit has read lie in its cache as they were
         __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
+        look();
+    }
+
+    // 3. what each wants
+    int run = 0;
+#pragma unroll
+    for (int k = 0; k < kReserveEach; ++k) {
+        if (k >= each) break;
+        const int b = k * kReserveThreads + tid;
+        int want = 0;
+        bool copy = false;
+        if (b < c.B) {
+            const int* row = c.table + (size_t)b * c.max_pages;
+            const int end = cols[b].y, p = last[b];
+            int lo = from[k], hi = end;
+            if (lo < hi) {
+                if (lo_page[k] == -1) hi = lo;
+                else if (end_page[k] != -1) lo = hi;
+            }
+            while (lo < hi) {                    // the first empty column
+                const int mid = (lo + hi) >> 1;
+                if (row[mid] == -1) hi = mid;
+                else lo = mid + 1;
+            }
+            want = end - lo;
+            if (shares[k] > 1) {
+                int holders = 0, before = 0;
+#pragma unroll 4
+                for (int o = 0; o < c.B; o += 4) {
+                    const int4 x = *reinterpret_cast<const int4*>(&last[o]);
+                    const int four[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const bool same = four[i] == p;
+                        holders += same ? 1 : 0;
+                        before += same && o + i < b ? 1 : 0;
+                    }
+                }
+                copy = holders < shares[k] || before > 0;
+                cols[b].x |= copy ? kCopy | kShared : kShared;
+            }
+            report[1 + b] = copy ? p : -1;
+        }
+        int all;
+        const int ex = block_scan(want + (copy ? 1 : 0), waves, all);
+        if (b < c.B) at[b] = run + ex;
+        run += all;
     }
     if (tid == 0) at[c.B] = run;
 
@@ -462,7 +475,12 @@ __global__ __launch_bounds__(kReserveThreads) void reserve_kernel(Paged c, int* 
     const int missing = (int)min((unsigned long long)max(run - free_pages, 0) + beyond, 0x7fffffffull);
     if (tid == 0) report[0] = missing;
     if (missing > 0) {
-        for (int b = tid; b < c.B; b += kReserveThreads) report[1 + b] = -1;
+        for (int b = tid; b < c.B; b += kReserveThreads) {
+            report[1 + b] = -1;
+            // a shared page stays unchanged though its copy is missing: what would be written to it has no page
+            const int x = cols[b].x;
+            if (x & kShared) c.table[(size_t)b * c.max_pages + (x & (kShared - 1))] = -2 - last[b];
+        }
         return;
     }
 
@@ -487,7 +505,7 @@ __global__ __launch_bounds__(kReserveThreads) void reserve_kernel(Paged c, int* 
                 const bool copied = mine == at[lo] && (to.x & kCopy) != 0;
                 if (copied) atomicSub(&refs[last[lo]], 1);
                 // (of the fresh pages the last one goes to the last column)
-                c.table[(size_t)lo * c.max_pages + (copied ? to.x & (kCopy - 1) : to.y - (at[lo + 1] - mine))] = p;
+                c.table[(size_t)lo * c.max_pages + (copied ? to.x & (kShared - 1) : to.y - (at[lo + 1] - mine))] = p;
                 refs[p] = 1;
             }
             rank += __popcll(all);

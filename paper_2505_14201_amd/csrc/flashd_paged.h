@@ -1,7 +1,7 @@
 // A cache of keys and values kept in pages, as the kernels that read and write it see it.
 //
 // K and V are pools of pages [P][Hkv][page][d], pages page_stride apart; row b of the table names the
-// pages of sequence b in the order of its keys, -1 where it has none.  New tokens of sequence b are rows
+// pages of sequence b in the order of its keys, -1 where it has none, -2 - p where page p is held back.  New tokens of sequence b are rows
 // q_start[b] .. q_start[b + 1] - 1 of packed [T][heads][d] tensors and stand at keys lens[b] + i.
 // All of that is device memory which the host never reads, so every number taken from it is checked
 // here before it becomes an address: a page outside the pool is no page, a sequence ends at the
@@ -39,17 +39,15 @@ struct Seq {
 // New tokens of a sequence whose rows begin at `start` (>= 0) and end before `next`.  Whatever `next` is, it is brought between 0 and T before the
 // difference is formed, which then has no overflow.
 __host__ __device__ __forceinline__ int tokens_of(int start, int next, int T) {
-    const int end = next < 0 ? 0 : next < T ? next : T;
-    return end > start ? end - start : 0;
+    return max(min(max(next, 0), T) - start, 0);
 }
 
 // `most`: keys that a row of the table has room for
 __host__ __device__ __forceinline__ Seq seq_of(int start, int next, int len, int T, int most) {
     Seq s;
-    s.row0 = start < 0 ? 0 : start;
-    s.len = len < 0 ? 0 : len < most ? len : most;
-    const int n = tokens_of(s.row0, next, T), room = most - s.len;
-    s.n = n < room ? n : room;
+    s.row0 = max(start, 0);
+    s.len = min(max(len, 0), most);
+    s.n = min(tokens_of(s.row0, next, T), most - s.len);
     return s;
 }
 
@@ -61,6 +59,10 @@ __host__ __device__ __forceinline__ int columns_beyond(int tokens, int n, int pa
 __device__ __forceinline__ Seq seq_at(const Paged& c, int b) {
     return seq_of(c.q_start[b], c.q_start[b + 1], c.lens[b], c.T, c.max_pages << c.page_log2);
 }
+
+// The page that an entry of the table names, -1 if none.  An entry of -2 - p names page p like one of p (it counts in refs), but holds it
+// back: to all who read or write keys it is no page.
+__host__ __device__ __forceinline__ int named_page(int entry) { return entry < -1 ? -2 - entry : entry; }
 
 // The page of column `col` (>= 0) of sequence b, -1 if there is none.
 __device__ __forceinline__ int page_at(const Paged& c, int b, int col) {

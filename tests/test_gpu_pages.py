@@ -92,6 +92,20 @@ class World:
             assert (self.v[y, p, :, j % self.page] == -(ids + 0.25 * y).view(-1, 1, 1)).all()
 
 
+def fails(w, some):
+    """Reserving finds too few pages, and the rest of the step runs on: nobody's keys change."""
+    assert w.reserve(some) > 0
+    check_own(w.table.tolist(), w.refs.tolist(), w.lens.tolist(), some, w.page, missing=True)
+    w.append()
+    w.contents(without=w.model.held_back(w.page))
+    q = torch.randn(max(w.starts[-1], 1), HKV, D, device="cuda")
+    for hint in (1, 20):
+        flashd.attn_fwd_tree(q, w.k[0], w.v[0], torch.empty_like(q), w.table, w.lens, w.q_start, hint, 0.1)
+    flashd.cache_commit(w.k, w.v, w.table, w.lens, w.q_start, torch.empty_like(w.lens),
+                        keep=torch.tensor([[0, 1]] * len(some), dtype=torch.int32, device="cuda") + 1)
+    w.contents(without=w.model.held_back(w.page))
+
+
 def step(w, some, keep):
     assert w.reserve(some) == 0
     check_own(w.table.tolist(), w.refs.tolist(), w.lens.tolist(), some, w.page)
@@ -152,3 +166,70 @@ def test_shared_pages_behind_the_keys_of_long_rows():
     w.fork([0, 1, 2, 2])
     w.set_back([1, 8000, 3000, 40])
     step(w, [1, 1, 4000, 6000], [[0], [0], list(range(0, 4000, 7)), []])
+
+
+def test_a_failed_reserve_holds_shared_pages_back():
+    """Three twins of 20 keys and one free page: none writes to the page they share, however often the step is run; without the third
+    there is enough, and all keys are there."""
+    w = World(1, 16, 3, 3)
+    step(w, [20], [list(range(20))])
+    w.fork([0, 0, 0])
+    was = w.k.clone(), w.v.clone()
+    for _ in range(3):
+        fails(w, [1, 2, 3])
+        assert w.table.tolist() == [[0, -3, -1]] * 3
+        assert torch.equal(w.k, was[0]) and torch.equal(w.v, was[1])
+    w.fork([0, 1, -1])
+    step(w, [1, 1, 0], [[0], [0], []])
+
+
+def test_a_twin_that_rests_keeps_its_keys_beside_a_failed_reserve():
+    """No free page: a twin set back into the middle of the page would write over a key of the one that rests."""
+    w = World(1, 16, 2, 3)
+    step(w, [20], [list(range(20))])
+    w.fork([0, 0])
+    w.set_back([20, 18])
+    fails(w, [0, 1])
+    w.contents(without={1})
+    w.reserve([0, 0])                           # taken up again without new tokens
+    w.contents()
+    w.fork([-1, 1])
+    step(w, [0, 3], [[], [0, 2]])
+
+
+def test_pages_held_back_branch_and_go_back_like_others():
+    w = World(2, 16, 4, 5)
+    step(w, [20, 5], [list(range(20)), list(range(5))])
+    w.fork([0, 0, 1])
+    fails(w, [1, 1, 30])
+    w.fork([1, 0, 0, 2])
+    fails(w, [1, 1, 20, 1])
+    w.set_back([10, 20, 0, 5])                  # the held back column lies behind the keys, or all of them go
+    w.reserve([0, 1, 0, 1])
+    w.contents()
+    w.fork([1, 3])
+    step(w, [14, 1], [[0], [0]])
+    w.fork([0, 0])
+    fails(w, [0, 100])                          # columns are missing: the page that both hold is held back as well
+    assert w.model.held_back(16) == {1}
+    step(w, [0, 1], [[], [0]])
+
+
+@pytest.mark.parametrize("B,page,P,max_pages", [(6, 16, 7, 6), (40, 32, 42, 8), (1100, 16, 1200, 8)])
+def test_lives_in_a_pool_that_is_too_small(B, page, P, max_pages):
+    rng = random.Random(B + 2)
+    w, failed = World(B, page, P, max_pages), 0
+    for _ in range(14):
+        w.fork([rng.choice([b, b, b, rng.randrange(B), -1]) for b in range(B)])
+        if rng.random() < 0.3:
+            w.set_back([rng.randint(0, l) if rng.random() < 0.3 else l for l in w.model.lens])
+        some = [rng.choice([0, 1, 2, rng.randint(0, 2 * page)]) for _ in range(B)]
+        some = [min(m, max_pages * page - l + rng.choice([0, 0, 0, 5])) for m, l in zip(some, w.model.lens)]
+        trial = Pages(w.table.cpu(), w.model.lens, P)
+        trial.rows = [list(r) for r in w.model.rows]
+        if trial.reserve(some, page)[0][0]:
+            failed += 1
+            fails(w, some)
+        else:
+            step(w, some, [sorted(rng.sample(range(m), rng.randint(0, m))) for m in some])
+    assert 3 < failed < 14

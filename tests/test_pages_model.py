@@ -43,3 +43,32 @@ def test_twins_of_a_sequence_with_pages_left_over():
     model.fork([0, 0])
     report, copies = model.reserve([1, 1], 16)
     assert report == [0, -1, -1] and copies == [] and model.rows == [[0, 1], [0, 2]] and model.refs[:4] == [2, 1, 1, 0]
+
+
+@pytest.mark.parametrize("seed", range(20))
+def test_nothing_shared_is_written_to_where_pages_are_missing(seed):
+    """A pool that is too small most of the time: sequences end at random and calls are made again."""
+    page, max_pages, B = 16, 6, 6
+    model = Pages(pu.ints([[-1] * max_pages] * B), [0] * B, 7)
+    failed = held = 0
+    for report, copies, lens, some in life(model, B, page, max_pages, seed, steps=40):
+        failed += report[0] > 0
+        held += len(model.held_back(page))
+        assert not model.held_back(page) or report[0] > 0
+        check_own(model.table.tolist(), model.refs, lens, some, page, missing=report[0] > 0)
+    assert failed > 3
+
+
+def test_a_shared_page_is_held_back_until_there_are_enough():
+    """Three twins of 20 keys and one free page, two copies wanted: all three are held back; without the third there is enough."""
+    model = Pages(pu.ints([[-1] * 3]), [0], 3)
+    model.reserve([20], 16)
+    model.lens = [20]
+    model.fork([0, 0, 0])
+    for _ in range(2):
+        assert model.reserve([1, 1, 1], 16) == ([1, -1, -1, -1], [])
+        assert model.rows == [[0, -3]] * 3 and model.refs == [3, 3, 0] and model.held_back(16) == {0, 1, 2}
+    model.fork([0, 1, -1])
+    assert model.refs == [2, 2, 0]
+    assert model.reserve([1, 1, 0], 16) == ([0, -1, 1, -1], [(1, 1, 2, 4)])
+    assert model.rows == [[0, 1], [0, 2], []] and model.refs == [2, 1, 1]
