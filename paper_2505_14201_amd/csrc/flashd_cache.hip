@@ -317,7 +317,8 @@ __global__ __launch_bounds__(kReserveThreads) void reserve_kernel(Paged c, int* 
         const Seq s = seq_of(c.q_start[b], next, c.lens[b], c.T, c.max_pages << c.page_log2);
         int* row = c.table + (size_t)b * c.max_pages;
         const int end = (s.len + s.n + mask) >> c.page_log2, lo = (s.len + mask) >> c.page_log2, first = s.len >> c.page_log2;
-        int part = lo > first ? row[first] : -1, p = end < c.max_pages ? row[end] : -1;
+        const int tail = lo > 0 ? row[lo - 1] : 0;
+        int part = lo > first ? tail : -1, p = end < c.max_pages ? row[end] : -1;
         if (lo < end) {
             lo_page[k] = row[lo];
             end_page[k] = row[end - 1];
@@ -330,6 +331,15 @@ __global__ __launch_bounds__(kReserveThreads) void reserve_kernel(Paged c, int* 
             p = ++col < c.max_pages ? row[col] : -1;
         }
         from[k] = s.n > 0 ? lo : end;
+        if (s.n > 0 && tail == -1) {             // not even its keys have pages
+            int z = lo - 1;
+            from[k] = 0;
+            while (from[k] < z) {
+                const int mid = (from[k] + z) >> 1;
+                if (row[mid] == -1) z = mid;
+                else from[k] = mid + 1;
+            }
+        }
         last[b] = s.n > 0 && part < c.P ? part : -1;
         cols[b] = int2{first, end};
         // tokens that the table has no columns for

@@ -233,3 +233,25 @@ def test_lives_in_a_pool_that_is_too_small(B, page, P, max_pages):
         else:
             step(w, some, [sorted(rng.sample(range(m), rng.randint(0, m))) for m in some])
     assert 3 < failed < 14
+
+
+def test_keys_without_pages_get_them():
+    """Lengths that the rows have no pages for: a sequence that grows gets the pages of its keys as well, and its tokens have one."""
+    P, page, lens, some = 40, 16, [20, 32, 5, 0, 64, 50, 49, 3, 16], [5, 1, 0, 3, 40, 2, 1, 2, 0]
+    table = torch.full((9, 8), -1, dtype=torch.int32)
+    table[4, :2], table[5, :3], table[6, :4] = pu.ints([30, 31]), pu.ints([32, 33, 34]), pu.ints([35, 36, 37, 38])
+    model = Pages(table, lens, P)
+    starts = [0]
+    for m in some:
+        starts.append(starts[-1] + m)
+    k, v = (torch.zeros(1, P, HKV, page, D, device="cuda") for _ in "kv")
+    refs, tab, lens_g, q_start = pu.ints(model.refs).cuda(), table.cuda(), pu.ints(lens).cuda(), pu.ints(starts).cuda()
+    report = torch.zeros(10, dtype=torch.int32, device="cuda")
+    flashd.cache_reserve(k, v, refs, tab, lens_g, q_start, report)
+    want, _ = model.reserve(some, page)
+    assert report.tolist() == want == [0] + [-1] * 9
+    assert tab.tolist() == model.table.tolist() and refs.tolist() == model.refs
+    check_own(tab.tolist(), refs.tolist(), lens, some, page)
+    x = torch.ones(starts[-1], HKV, D, device="cuda")
+    flashd.cache_append(x, x.clone(), x.clone(), torch.empty_like(x), k[0], v[0], tab, lens_g, q_start)
+    assert int(k.sum()) == starts[-1] * HKV * D and int(v.sum()) == starts[-1] * HKV * D
