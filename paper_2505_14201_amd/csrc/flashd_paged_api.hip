@@ -101,19 +101,25 @@ bool rows_overlap(const void* a, int64_t abytes, const void* b, int64_t bbytes, 
     return T == 1 || at < abytes || at + bbytes > stride;
 }
 
-// Whether a page of K may share memory with one of V: not where the pools lie apart, nor where V's pages (or layers)
-// lie between K's.
+// Whether a page of K shares memory with one of V: page (l', p') of V lies off + (l' - l) layer_bytes + (p' - p) page_bytes behind page
+// (l, p) of K.  Of the two differences the one with fewer values is gone through, and the other's nearest to the middle looked at.
 bool kv_overlap(const Paged& p) {
     if (!overlap(p.k, pool_extent(p), p.v, pool_extent(p))) return false;
-    const int64_t strides[2] = {p.page_bytes, p.layers > 1 ? p.layer_bytes : 0}, counts[2] = {p.P, p.layers};
-    for (int i = 0; i < 2; ++i) {
-        const int64_t stride = strides[i], other = strides[1 - i];
-        if (stride == 0) continue;
-        const int64_t held = p.Hkv * p.head_bytes + (other < stride ? (counts[1 - i] - 1) * other : 0);
-        const int64_t off = (int64_t)((uintptr_t)p.v - (uintptr_t)p.k) % stride, at = off < 0 ? off + stride : off;
-        if (at >= held && at + held <= stride) return false;
+    const int64_t one = p.Hkv * p.head_bytes, off = (int64_t)((uintptr_t)p.v - (uintptr_t)p.k);
+    const bool by_layer = p.layers <= p.P;
+    const int64_t outer = by_layer ? p.layer_bytes : p.page_bytes, inner = by_layer ? p.page_bytes : p.layer_bytes;
+    const int64_t most = (by_layer ? p.layers : p.P) - 1, last = (by_layer ? p.P : p.layers) - 1;
+    for (int64_t d = -most; d <= most; ++d) {
+        const int64_t rest = off + d * outer;
+        if (rest - last * inner >= one || rest + last * inner <= -one) continue;
+        const int64_t near = last == 0 ? 0 : -rest / inner;
+        for (int64_t e = near - 1; e <= near + 1; ++e) {
+            if (e < -last || e > last) continue;
+            const int64_t gap = rest + e * inner;
+            if (gap < one && gap > -one) return true;
+        }
     }
-    return true;
+    return false;
 }
 
 int done(hipError_t e) { return e == hipSuccess ? FLASHD_OK : FLASHD_E_HIP; }
