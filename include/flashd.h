@@ -67,7 +67,7 @@ typedef enum {
     FLASHD_E_ARCH = -9,       /* the current device is not gfx950                       */
     FLASHD_E_VARIANT = -10,   /* variant/splits not valid for this problem              */
     FLASHD_E_CACHE = -11,     /* a paged cache's page size, strides or layer are not valid */
-    FLASHD_E_OVERLAP = -12    /* an output lies on an input it must not share memory with  */
+    FLASHD_E_OVERLAP = -12    /* an output lies on an input or on another output          */
 } flashd_status;
 
 /* How the recurrence is evaluated.  All variants compute the same result. */
@@ -303,6 +303,7 @@ int flashd_skip_stats(const void* q, const void* k, int B, int Hq, int Hkv, int 
  * flashd_attn_fwd_tree does not write their rows).
  * Limits: B at most 4096, page 16, 32, 64, 128 or 256, max_pages * page at most 10^9, T 10^7, B * max_pages and T * Hq
  * below 2^31.
+ * What a call writes must not share memory with anything else that it is given (else FLASHD_E_OVERLAP), unless its description says so.
  * Pointers to elements of pools and packed tensors and the strides of rows, pages and layers are
  * multiples of 16 bytes, other pointers of their element's size (else FLASHD_E_ALIGN).
  */

@@ -2,6 +2,7 @@
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
+#include <initializer_list>
 
 #include "../../include/flashd.h"
 #include "flashd_common.h"
@@ -20,7 +21,18 @@ int esize(int dtype) { return dtype == FLASHD_F32 ? 4 : dtype == FLASHD_CACHE_FP
 
 bool overlap(const void* a, int64_t abytes, const void* b, int64_t bbytes) {
     const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
-    return x < y + (uintptr_t)bbytes && y < x + (uintptr_t)abytes;
+    return abytes > 0 && bbytes > 0 && x < y + (uintptr_t)bbytes && y < x + (uintptr_t)abytes;
+}
+
+// A run of memory that a call reads or writes; none where `at` is NULL
+struct Span {
+    const void* at;
+    int64_t bytes;
+};
+bool overlaps_any(Span out, std::initializer_list<Span> others) {
+    for (const Span& x : others)
+        if (x.at != nullptr && out.at != nullptr && overlap(out.at, out.bytes, x.at, x.bytes)) return true;
+    return false;
 }
 
 // The struct as the kernels take it, for one layer (layer >= 0) or all of them (-1).
@@ -94,6 +106,12 @@ int64_t pool_extent(const Paged& p) {
     return (int64_t)(p.P - 1) * p.page_bytes + (int64_t)(p.layers - 1) * p.layer_bytes + (int64_t)p.Hkv * p.head_bytes;
 }
 
+int64_t layer_extent(const Paged& p) { return pool_extent(p) - (p.layers - 1) * p.layer_bytes; }
+
+Span table_of(const Paged& p) { return {p.table, (int64_t)p.B * p.max_pages * 4}; }
+Span lens_of(const Paged& p) { return {p.lens, (int64_t)p.B * 4}; }
+Span starts_of(const Paged& p) { return {p.q_start, (int64_t)(p.B + 1) * 4}; }
+
 // Whether rows of abytes at a share memory with rows of bbytes at b, both `stride` bytes apart, T of each
 bool rows_overlap(const void* a, int64_t abytes, const void* b, int64_t bbytes, int64_t stride, int T) {
     if (!overlap(a, (T - 1) * stride + abytes, b, (T - 1) * stride + bbytes)) return false;
@@ -136,13 +154,10 @@ int flashd_cache_fork(const flashd_cache* c, int* refs, const int* parent, int B
     if (rc != FLASHD_OK) return rc;
     if (B_out < 1 || B_out > FLASHD_CACHE_MAX_SEQS || (int64_t)B_out * c->max_pages > 0x7fffffff) return FLASHD_E_SHAPE;
     if (((uintptr_t)refs | (uintptr_t)parent | (uintptr_t)table_out | (uintptr_t)lens_out) & 3u) return FLASHD_E_ALIGN;
-    const int64_t tin = (int64_t)c->B * c->max_pages * 4, tout = (int64_t)B_out * c->max_pages * 4;
-    const int64_t lin = (int64_t)c->B * 4, lout = (int64_t)B_out * 4;
-    if (overlap(table_out, tout, c->table, tin) || overlap(table_out, tout, c->lens, lin) ||
-        overlap(lens_out, lout, c->table, tin) || overlap(lens_out, lout, c->lens, lin) ||
-        overlap(table_out, tout, lens_out, lout) || overlap(table_out, tout, parent, lout) ||
-        overlap(lens_out, lout, parent, lout) || overlap(refs, (int64_t)c->P * 4, table_out, tout) ||
-        overlap(refs, (int64_t)c->P * 4, lens_out, lout))
+    const Span r{refs, (int64_t)c->P * 4}, out{table_out, (int64_t)B_out * c->max_pages * 4}, lens{lens_out, (int64_t)B_out * 4};
+    const Span from{parent, (int64_t)B_out * 4}, old = table_of(p), old_lens = lens_of(p);
+    if (overlaps_any(r, {out, lens, from, old, old_lens}) || overlaps_any(out, {lens, from, old, old_lens}) ||
+        overlaps_any(lens, {from, old, old_lens}))
         return FLASHD_E_OVERLAP;
     rc = flashd::api_check_arch();
     if (rc != FLASHD_OK) return rc;
@@ -155,10 +170,11 @@ int flashd_cache_reserve(const flashd_cache* c, int* refs, const int* q_start, i
     int rc = take_cache(c, -1, q_start, 0x7fffffff, p);
     if (rc != FLASHD_OK) return rc;
     if (((uintptr_t)refs | (uintptr_t)report) & 3u) return FLASHD_E_ALIGN;
-    const int64_t rep = (int64_t)(c->B + 1) * 4;
-    if (overlap(report, rep, c->table, (int64_t)c->B * c->max_pages * 4) || overlap(report, rep, c->lens, rep - 4) ||
-        overlap(report, rep, q_start, rep) || overlap(report, rep, refs, (int64_t)c->P * 4))
+    const Span r{refs, (int64_t)c->P * 4}, rep{report, (int64_t)(c->B + 1) * 4}, table = table_of(p), lens = lens_of(p), starts = starts_of(p);
+    if (overlaps_any(rep, {r, table, lens, starts}) || overlaps_any(r, {table, lens, starts}) || overlaps_any(table, {lens, starts}))
         return FLASHD_E_OVERLAP;
+    for (const void* pool : {p.k, p.v})
+        if (overlaps_any({pool, pool_extent(p)}, {r, rep, table, lens, starts})) return FLASHD_E_OVERLAP;
     if (kv_overlap(p)) return FLASHD_E_OVERLAP;
     rc = flashd::api_check_arch();
     if (rc != FLASHD_OK) return rc;
@@ -198,9 +214,12 @@ int flashd_cache_append(const flashd_cache* c, int layer, const void* q, long lo
         if (v_stride == q_stride ? rows_overlap(q, qb, v, kb, q_stride * es, T) : overlap(q, nq, v, nv)) return FLASHD_E_OVERLAP;
     }
     if (!in_place && (overlap(q_out, no, q, nq) || overlap(q_out, no, k, nk) || overlap(q_out, no, v, nv))) return FLASHD_E_OVERLAP;
-    const int64_t pool = pool_extent(p) - (p.layers - 1) * p.layer_bytes;
-    for (const void* x : {static_cast<const void*>(p.k), static_cast<const void*>(p.v)})
-        if (overlap(x, pool, q, nq) || overlap(x, pool, k, nk) || overlap(x, pool, v, nv) || overlap(x, pool, q_out, no))
+    const int64_t weights = (int64_t)c->d * esize(dtype);
+    const Span table = table_of(p), lens = lens_of(p), starts = starts_of(p), at{positions, (int64_t)T * 4}, inv{inv_freq, (int64_t)rot * 2},
+               qw{q_weight, weights}, kw{k_weight, weights};
+    if (overlaps_any({q_out, no}, {table, lens, starts, at, inv, qw, kw})) return FLASHD_E_OVERLAP;
+    for (const void* pool : {p.k, p.v})
+        if (overlaps_any({pool, layer_extent(p)}, {{q, nq}, {k, nk}, {v, nv}, {q_out, no}, table, lens, starts, at, inv, qw, kw}))
             return FLASHD_E_OVERLAP;
     if (kv_overlap(p)) return FLASHD_E_OVERLAP;
     rc = flashd::api_check_arch();
@@ -242,11 +261,12 @@ int flashd_attn_fwd_tree(const flashd_cache* c, int layer, const void* q, long l
     if (rc == FLASHD_OK) rc = take_stride(o_stride, T, Hq, c->d, dtype);
     if (rc != FLASHD_OK) return rc;
     if ((((uintptr_t)q | (uintptr_t)o | (uintptr_t)workspace) & 15u) != 0 || ((uintptr_t)tree & 7u) != 0) return FLASHD_E_ALIGN;
-    const int64_t no = extent(o_stride, T, Hq, c->d, dtype), pool = pool_extent(p) - (p.layers - 1) * p.layer_bytes;
-    if (overlap(o, no, q, extent(q_stride, T, Hq, c->d, dtype)) || overlap(o, no, p.k, pool) || overlap(o, no, p.v, pool))
-        return FLASHD_E_OVERLAP;
     const size_t need = flashd::attn_tree_workspace(Hq, c->Hkv, max_q, c->d, dtype);
+    const Span out{o, extent(o_stride, T, Hq, c->d, dtype)}, in{q, extent(q_stride, T, Hq, c->d, dtype)}, kp{p.k, layer_extent(p)},
+        vp{p.v, layer_extent(p)}, table = table_of(p), lens = lens_of(p), starts = starts_of(p), bits{tree, (int64_t)T * tree_words * 8};
+    if (overlaps_any(out, {in, kp, vp, table, lens, starts, bits})) return FLASHD_E_OVERLAP;
     if (workspace != nullptr && workspace_bytes < need) return FLASHD_E_WORKSPACE;
+    if (overlaps_any({workspace, (int64_t)need}, {out, in, kp, vp, table, lens, starts, bits})) return FLASHD_E_OVERLAP;
     rc = flashd::api_check_arch();
     if (rc != FLASHD_OK || T == 0) return rc;
     if (workspace == nullptr) {
@@ -281,11 +301,11 @@ int flashd_cache_commit(const flashd_cache* c, const int* q_start, const int* ke
     if (rc != FLASHD_OK) return rc;
     if (keep != nullptr ? max_keep < 1 || (int64_t)max_keep * c->B > 0x7fffffff : max_keep != 0) return FLASHD_E_SHAPE;
     if (((uintptr_t)keep | (uintptr_t)n_keep | (uintptr_t)lens_out) & 3u) return FLASHD_E_ALIGN;
-    const int64_t lens = (int64_t)c->B * 4;
-    if (overlap(lens_out, lens, c->lens, lens) || overlap(lens_out, lens, c->table, lens * c->max_pages) ||
-        overlap(lens_out, lens, q_start, lens + 4) || (n_keep && overlap(lens_out, lens, n_keep, lens)) ||
-        (keep && overlap(lens_out, lens, keep, lens * max_keep)))
-        return FLASHD_E_OVERLAP;
+    const Span out{lens_out, (int64_t)c->B * 4}, table = table_of(p), lens = lens_of(p), starts = starts_of(p),
+        list{keep, (int64_t)c->B * max_keep * 4}, counts{n_keep, (int64_t)c->B * 4};
+    if (overlaps_any(out, {table, lens, starts, list, counts})) return FLASHD_E_OVERLAP;
+    for (const void* pool : {p.k, p.v})
+        if (overlaps_any({pool, pool_extent(p)}, {out, table, lens, starts, list, counts})) return FLASHD_E_OVERLAP;
     if (kv_overlap(p)) return FLASHD_E_OVERLAP;
     rc = flashd::api_check_arch();
     if (rc != FLASHD_OK) return rc;
