@@ -396,7 +396,8 @@ int flashd_cache_append(const flashd_cache* c, int layer, const void* q, long lo
  *   workspace   device memory of at least flashd_tree_workspace_bytes(...), 16-byte aligned, or NULL: taken
  *            from the grow-only cache of the stream as in flashd_attn_fwd.  Two calls must not use one
  *            workspace at the same time; a call recorded into a graph brings its own (NULL: FLASHD_E_WORKSPACE).
- * Scores, softmax and sums are fp32; weights are rounded to `dtype` before the product with V.  For fixed inputs and
+ * Scores, softmax and sums are fp32; weights are rounded to `dtype` before the product with V.  Weights of bf16 reach 2^54 before they
+ * are brought down, so that values beyond 2^70 may have an infinite sum; f32 takes values of any size.  For fixed inputs and
  * max_q the output is bitwise reproducible.  T == 0 is a call without work.
  */
 int flashd_attn_fwd_tree(const flashd_cache* c, int layer, const void* q, long long q_stride, void* o,

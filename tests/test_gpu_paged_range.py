@@ -1,0 +1,45 @@
+"""Ends of what the paged cache's operators take: values near the end of fp32, many layers and heads."""
+import math
+
+import pytest
+import torch
+
+from paper_2505_14201_amd import flashd
+from tests import paged_util as pu
+from tests.test_gpu_tree import run
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("hint", (1, 12))               # 4 rows to a token: 16 and 32 rows to a tile
+@pytest.mark.parametrize("exponent,rise", [(100, "by turns"), (125, "by turns"), (100, 50.0), (124, 50.0), (125, 0.0), (125, 300.0)])
+@pytest.mark.parametrize("keys,d", [(900, 128), (5000, 64), (50000, 64)])
+def test_fp32_values_of_any_size(keys, d, exponent, rise, hint):
+    """Values of 2^exponent times N(0, 1) under scores that rise along the sequence by `rise` powers of two, or by 50 and back every 128
+    keys: every output is finite in fp32 (a mean of values below 2^128) and as near to fp64 as that of values of 1."""
+    c = pu.make([keys - 3], [3], 1, d, 32, "f32", seed=91, qk_std=0.02)
+    j = torch.arange(keys)
+    power = 50.0 * (j // 128 % 2) if rise == "by turns" else j * (rise / keys)
+    c.k[c.table[0].long()[j // 32], :, j % 32, 0] = (power * math.log(2)).float().view(-1, 1)
+    q = pu.queries(c, 4, "f32", seed=92)
+    q[..., 0] = 1.0
+    o, mass, size = pu.attention(c, q, 1.0)
+    bound = pu.attention_bound(c, "f32", o, mass, size)
+    c.v *= 2.0 ** exponent
+    assert torch.isfinite(c.v).all()
+    got = run(c, q, 1.0, max_q=hint)
+    assert bool(torch.isfinite(got).all())
+    worst = float(((got.double() * 2.0 ** -exponent - o).abs() / bound).max())
+    assert worst <= 1.0, worst
+
+
+def test_commit_in_a_million_layers_and_heads():
+    layers, heads = 65535, 17
+    k, v = (torch.randint(0, 120, (layers, 1, heads, 16, 64), dtype=torch.uint8, device="cuda") for _ in "kv")
+    was = [x[:, 0, :, 1].clone() for x in (k, v)]
+    table, lens, starts = (pu.ints(x).cuda() for x in ([[0]], [0], [0, 2]))
+    out = torch.zeros(1, dtype=torch.int32, device="cuda")
+    flashd.cache_commit(k.view(torch.float8_e4m3fn), v.view(torch.float8_e4m3fn), table, lens, starts, out, keep=pu.ints([[1]]).cuda())
+    torch.cuda.synchronize()
+    assert out.tolist() == [1]
+    assert torch.equal(k[:, 0, :, 0], was[0]) and torch.equal(v[:, 0, :, 0], was[1])
