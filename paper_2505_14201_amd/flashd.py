@@ -352,6 +352,12 @@ def _ints(name, t, shape, device):
         raise ValueError(f"{name} must be a contiguous int32 tensor [{want}] on the cache's GPU")
 
 
+def _fit(*sizes):
+    """FLASHD_E_SHAPE for sizes that the C call's ints do not hold (they would be cut off)."""
+    if max(sizes) > 0x7fffffff or min(sizes) < -0x80000000:
+        raise FlashdError(-2)
+
+
 def _cache(kcache, vcache, table, lens, kscale=1.0, vscale=1.0, layers=False):
     """The struct for tensors of a cache; `layers`: five dimensions are allowed."""
     if not kcache.is_cuda or not vcache.is_cuda:
@@ -372,8 +378,7 @@ def _cache(kcache, vcache, table, lens, kscale=1.0, vscale=1.0, layers=False):
     _ints("lens", lens, (B,), device)
     if min(P, Hkv, page, d, B, max_pages, shape[0]) < 1:
         raise ValueError("the cache has a dimension of size 0")
-    if max(P, page, max_pages) > 0x7fffffff:
-        raise FlashdError(-2)                      # FLASHD_E_SHAPE: more than the C call's ints hold
+    _fit(P, Hkv, page, d, B, max_pages, shape[0])
     return Cache(kcache.data_ptr(), vcache.data_ptr(), table.data_ptr(), lens.data_ptr(),
                  stride[-4] if P > 1 else Hkv * page * d, stride[0] if len(shape) == 5 else 0,
                  shape[0] if len(shape) == 5 else 1, P, page, max_pages, B, Hkv, d, _CACHE_DTYPE[dtype],
@@ -384,8 +389,7 @@ def _packed(name, t, T, heads, d, dtype, device):
     """The stride of a token of a packed tensor [T, heads, d], whose rows must be contiguous."""
     if t.get_device() != device or t.dtype != dtype or t.dim() != 3 or tuple(t.shape) != (T, heads, d):
         raise ValueError(f"{name} must be [{T}, {heads}, {d}] of type {dtype} on the cache's GPU")
-    if T > 0x7fffffff:
-        raise FlashdError(-2)
+    _fit(T, heads)
     s = t.stride()
     if s[2] != 1 or (heads > 1 and s[1] != d):
         raise ValueError(f"the heads of a token of {name} must be contiguous")
@@ -427,6 +431,7 @@ def cache_fork(parent, refs, table, lens, table_out, lens_out, stream=None) -> N
     _ints("table_out", table_out, (n, max_pages), device)
     _ints("lens_out", lens_out, (n,), device)
     _ints("refs", refs, (None,), device)
+    _fit(n, max_pages, B, refs.shape[0])
     # (the pools themselves are not touched: any valid address and page size stand for them)
     c = Cache(16, 16, table.data_ptr(), lens.data_ptr(), 16 * 64, 0, 1, refs.shape[0], 16, max_pages, B, 1, 64, F16, 1.0, 1.0)
     _enqueue(_lib.flashd_cache_fork, device, stream, (c, refs.data_ptr(), parent.data_ptr(), n,
@@ -482,6 +487,7 @@ def cache_append(q, k, v, q_out, kcache, vcache, table, lens, q_start, positions
                 or not inv_freq.is_contiguous():
             raise ValueError("inv_freq must be a contiguous float32 tensor [rot / 2] on the cache's GPU")
         rot = 2 * inv_freq.shape[0]
+        _fit(rot)
     if T == 0:
         return
     _enqueue(_lib.flashd_cache_append, device, stream, (c, 0, q.data_ptr(), qs, k.data_ptr(), ks, v.data_ptr(), vs,
@@ -519,6 +525,7 @@ def attn_fwd_tree(q, kcache, vcache, o, table, lens, q_start, max_q: int, scale:
                 or tree.get_device() != device:
             raise ValueError("tree must be a contiguous int64 tensor [T, words] on the cache's GPU")
         words = tree.shape[1]
+    _fit(words, max_q)
     ws_ptr, ws_bytes = None, 0
     if workspace is not None:
         if workspace.get_device() != device or not workspace.is_contiguous():
@@ -542,6 +549,7 @@ def cache_commit(kcache, vcache, table, lens, q_start, lens_out, keep=None, n_ke
     _ints("lens_out", lens_out, (c.B,), device)
     if keep is not None:
         _ints("keep", keep, (c.B, None), device)
+        _fit(keep.shape[1])
     if n_keep is not None:
         _ints("n_keep", n_keep, (c.B,), device)
     _enqueue(_lib.flashd_cache_commit, device, stream, (c, q_start.data_ptr(), _ptr(keep),

@@ -1,4 +1,5 @@
-"""Ends of what the paged cache's operators take: values near the end of fp32, many layers and heads."""
+"""Ends of what the paged cache's operators take: values near the end of fp32, many layers and heads, sizes
+that the C call's ints do not hold."""
 import math
 
 import pytest
@@ -43,3 +44,34 @@ def test_commit_in_a_million_layers_and_heads():
     torch.cuda.synchronize()
     assert out.tolist() == [1]
     assert torch.equal(k[:, 0, :, 0], was[0]) and torch.equal(v[:, 0, :, 0], was[1])
+
+
+def test_sizes_that_an_int_does_not_hold_are_refused():
+    """2^32 + 1 of anything is not taken for 1."""
+    many = 2 ** 32 + 1
+    z = lambda *s, t=torch.bfloat16: torch.zeros(*s, dtype=t, device="cuda")            # noqa: E731
+    i = lambda *s: torch.zeros(*s, dtype=torch.int32, device="cuda")                    # noqa: E731
+    kc, x, table, lens, starts = z(2, 1, 16, 64), z(1, 1, 64), i(1, 1), i(1), i(2)
+    with pytest.raises(flashd.FlashdError) as e:
+        flashd.attn_fwd_tree(x, kc, z(2, 1, 16, 64), torch.empty_like(x), table, lens, starts, 1, 0.1,
+                             tree=torch.empty(1, many, dtype=torch.int64, device="cuda"))
+    assert e.value.status == -2
+    with pytest.raises(flashd.FlashdError) as e:
+        flashd.attn_fwd_tree(x, kc, z(2, 1, 16, 64), torch.empty_like(x), table, lens, starts, many, 0.1)
+    assert e.value.status == -2
+    with pytest.raises(flashd.FlashdError) as e:
+        flashd.cache_append(x, x.clone(), x.clone(), torch.empty_like(x), kc, z(2, 1, 16, 64), table, lens, starts,
+                            inv_freq=torch.empty(2 ** 31, dtype=torch.float32, device="cuda"))
+    assert e.value.status == -2
+    with pytest.raises(flashd.FlashdError) as e:
+        flashd.cache_commit(kc, z(2, 1, 16, 64), table, lens, starts, i(1), keep=torch.empty(1, many, dtype=torch.int32, device="cuda"))
+    assert e.value.status == -2
+    with pytest.raises(flashd.FlashdError) as e:
+        flashd.cache_fork(i(1), torch.empty(many, dtype=torch.int32, device="cuda"), table, lens, i(1, 1), i(1))
+    assert e.value.status == -2
+    one = kc.view(1, 2, 1, 16, 64)
+    with pytest.raises(flashd.FlashdError) as e:
+        flashd.cache_reserve(one.expand(many, -1, -1, -1, -1), z(1, 2, 1, 16, 64).expand(many, -1, -1, -1, -1), i(2), table, lens, starts, i(2))
+    assert e.value.status == -2
+    torch.cuda.synchronize()
+    torch.cuda.empty_cache()
