@@ -547,9 +547,10 @@ __device__ __forceinline__ Window make_window(uint64_t at, int bytes) {
 // has a base address of its own, through a buffer descriptor that ends at the sequence's last key:
 // keys behind it, and pages that are none, read zeros.
 //
-// HBM bounds it: a token for each of 64 sequences of 500 to 8192 keys, 32 / 8 heads of 128, takes 178 us for 1.17 GB read once,
-// 6.6 TB/s; from fp8, four tokens each, 100 us for 588 MB, 5.9 TB/s, a wavefront waiting for memory or for its turn
-// three quarters of its time.  One sequence of 1000 keys takes 6.2 us, the latency of finding a share, its pages and its keys.
+// HBM bounds it: a token for each of 64 sequences of 500 to 8192 keys, 32 / 8 heads of 128, takes 189 us for 1.17 GB read once, 6.2 TB/s
+// (median of calls one after the other; the least of 12 took 182); from fp8, four tokens each, 110 us (104) for 586 MB, 5.3 TB/s, a
+// wavefront waiting for memory or for its turn three quarters of its time.  One sequence of 1000 keys takes 6.5 us, the latency of
+// finding a share, its pages and its keys.
 //
 // In blocks with new keys a weight of zero may meet a value that is infinite or NaN (a token that some rows see
 // and others do not), and 0 * infinity must not reach the others: see codes_of().
@@ -866,11 +867,12 @@ __global__ __launch_bounds__(kTreeWaves * kWave, rows_per_cu(D, FP8, NR)) void t
 // every KW-th 32-key block (RW KW = 4; two wavefronts to a row's keys for up to 64 rows, none share for 128).  Each wavefront brings the 16 keys of a tile that it would
 // in that layout: they lie in one page, so its copies have one scalar base.
 //
-// Up to 64 rows HBM bounds it: trees of 16 tokens after 500 to 8192 keys (32 sequences, 32 / 8 heads of 128) take 106 us for
-// 600 MB, 5.7 TB/s, one of 12 after 131000 keys 89 us, 6.0 TB/s; the start of a piece, when nothing of it has arrived, and
-// the unequal pace of the workgroups are the rest.  With 128 rows it is the instructions: chunks of 573 to 1000 tokens after 3180 to
-// 7000 keys are 277 GFLOP in 326 us, 850 TFLOP/s; the matrix pipe works 40 % of the cycles, the vector units 47 %, and
-// a wavefront's vector instructions do not run beside its own matrix instructions: with the weights of a tile formed between the
+// Up to 64 rows HBM bounds it: trees of 16 tokens after 500 to 8192 keys (32 sequences, 32 / 8 heads of 128) take 113 us for
+// 600 MB, 5.3 TB/s (median of calls one after the other; the least of 12 took 103), one of 12 after 131000 keys 97 us (90), 5.5 TB/s; the
+// start of a piece, when nothing of it has arrived, and the unequal pace of the workgroups are the rest.  With 128 rows it is the instructions:
+// chunks of 573 to 1000 tokens after 3180 to 7000 keys are 277 GFLOP in 372 us, 744 TFLOP/s, as the clock falls from call to call
+// (336 us and 824 at its best); of the cycles the matrix pipe works 40 %, the vector units 48 %.  A wavefront's 32 rows use each operand read
+// from LDS once, and its vector instructions do not run beside its own matrix instructions: with the weights of a tile formed between the
 // output products of the tile before it took 386 us.
 //
 // (The copies are written as instructions: where the compiler knows of a copy into LDS under way, it waits for it before
@@ -1374,9 +1376,9 @@ __global__ __launch_bounds__(kTreeWaves * kWave, 2) void tree_tile_kernel(TreeRu
 // of a block is on its way while K is multiplied, K of the next one while V is.
 //
 // NR: 16-row column tiles, which read the keys once.  With two, and at d = 128, there is one workgroup per compute unit, whose registers
-// they need.  One token for each of 64 sequences of 500 to 8192 keys, 32 / 8 heads of 128: 382 us with the merge, 2.34 GB, 6.1 TB/s
-// (two workgroups, with spills: 424; without anything under way in the meantime 465); d = 64: 188 us.  Chunks of 115 to 200 tokens:
-// 610 us, 85 TFLOP/s of the 154 that a large product of the library reaches (1128 with 16 rows to a tile).
+// they need.  One token for each of 64 sequences of 500 to 8192 keys, 32 / 8 heads of 128: 386 us with the merge, 2.34 GB, 6.1 TB/s
+// (two workgroups, with spills: 424; without anything under way in the meantime 465); d = 64: 184 us.  8 chunks of 100 to 200 tokens after
+// 500 to 4000 keys: 52 GFLOP in 705 us, 74 TFLOP/s of the 154 that a large product of the library reaches: each 32 rows read the keys anew.
 // The reference lies 32 to 40 log2 units above a row's top score, so that values of any size that fp32 holds have a finite sum: 10^9
 // keys of 2^(8 - 40) add up to less than a value.  What it costs are weights below 2^-86 of the top one, which become zero.
 constexpr float kF32Move = 8.0f, kF32Room = 40.0f;
