@@ -456,10 +456,10 @@ __device__ __forceinline__ float quad_sum(float x) {
 // A row's state in a wavefront: o = U / l, U against the reference R (log2 units); R = -inf and l = 0
 // without a key.  The lane's part of U is columns 16 i + 4 q .. + 3 of row col.
 //
-// A block's scores, in log2 units and -inf where the row does not see the key: moves the reference to `room` above the top one
-// where that lies more than `limit` above it and turns the scores into weights.
+// A block's scores, in log2 units and -inf where the row does not see the key: moves the reference
+// where the top one lies more than `limit` above it and turns the scores into weights, a power of two (`unit`) at the reference.
 template <int NDB>
-__device__ __forceinline__ void weigh(float (&x)[8], f32x8& p, f32x4 (&U)[NDB], float& R, float& l, float limit, float room = 0.0f) {
+__device__ __forceinline__ void weigh(float (&x)[8], f32x8& p, f32x4 (&U)[NDB], float& R, float& l, float limit, float unit = 1.0f) {
     const float ninf = -__builtin_inff();
     float top = x[0];
 #pragma unroll
@@ -467,15 +467,15 @@ __device__ __forceinline__ void weigh(float (&x)[8], f32x8& p, f32x4 (&U)[NDB], 
     top = quad_max(top);
     if (__builtin_amdgcn_ballot_w64(top > R + limit) != 0) {
         const bool move = top > R + limit;
-        const float f = move ? exp2_fast(R - (top + room)) : 1.0f;       // 0 for a row without keys
-        R = move ? top + room : R;
+        const float f = move ? exp2_fast(R - top) : 1.0f;       // 0 for a row without keys
+        R = move ? top : R;
         l *= f;
 #pragma unroll
         for (int i = 0; i < NDB; ++i) U[i] *= f;
     }
     const float ref = R == ninf ? 0.0f : R;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) p[e] = exp2_fast(x[e] - ref);
+    for (int e = 0; e < 8; ++e) p[e] = exp2_fast(x[e] - ref) * unit;
 }
 
 // Joins the four wavefronts' states of a piece whose keys they have shared out: row tiles of 16 NR rows.
@@ -1379,9 +1379,11 @@ __global__ __launch_bounds__(kTreeWaves * kWave, 2) void tree_tile_kernel(TreeRu
 // they need.  One token for each of 64 sequences of 500 to 8192 keys, 32 / 8 heads of 128: 386 us with the merge, 2.34 GB, 6.1 TB/s
 // (two workgroups, with spills: 424; without anything under way in the meantime 465); d = 64: 184 us.  8 chunks of 100 to 200 tokens after
 // 500 to 4000 keys: 52 GFLOP in 705 us, 74 TFLOP/s of the 154 that a large product of the library reaches: each 32 rows read the keys anew.
-// The reference lies 32 to 40 log2 units above a row's top score, so that values of any size that fp32 holds have a finite sum: 10^9
-// keys of 2^(8 - 40) add up to less than a value.  What it costs are weights below 2^-86 of the top one, which become zero.
-constexpr float kF32Move = 8.0f, kF32Room = 40.0f;
+// A weight is at most 2^(8 - 40): 10^9 of them add up to less than 1, so that values of any size that fp32 holds have a finite sum.  The factor is
+// applied to the weights: with the reference 40 above the top score the exponential's argument would be rounded to 2^-19 instead of
+// 2^-22, which made outputs 9e-7 from fp64 where they are 3.4 to 4.9e-7 now (2-norm, N(0, 1) inputs).  Weights below 2^-86 of the one at the
+// reference lose bits, and below 2^-109 they are zero.
+constexpr float kF32Move = 8.0f, kF32Unit = 0x1p-40f;
 constexpr int f32_per_cu(int D, int NR) { return D == 64 && NR == 1 ? 2 : 1; }
 template <int D, int NR>
 __global__ __launch_bounds__(kTreeWaves * kWave, f32_per_cu(D, NR)) void tree_rows_f32_kernel(TreeRun r) {
@@ -1509,7 +1511,7 @@ __global__ __launch_bounds__(kTreeWaves * kWave, f32_per_cu(D, NR)) void tree_ro
                     x[e] = acc[k][e >> 2][e & 3] * c_log2;
                     if (masked) x[e] = if_seen(bits[k] >> (4 * q), 16 * (e >> 2) + (e & 3), x[e]);
                 }
-                weigh(x, pv[k], U[k], R[k], l[k], kF32Move - kF32Room, kF32Room);
+                weigh(x, pv[k], U[k], R[k], l[k], kF32Move, kF32Unit);
                 l[k] += ((pv[k][0] + pv[k][1]) + (pv[k][2] + pv[k][3])) + ((pv[k][4] + pv[k][5]) + (pv[k][6] + pv[k][7]));
             }
             bool apart = false;

@@ -34,6 +34,27 @@ def test_fp32_values_of_any_size(keys, d, exponent, rise, hint):
     assert worst <= 1.0, worst
 
 
+@pytest.mark.parametrize("hint", (1, 12))
+def test_fp32_weights_are_as_near_as_fp32_holds_them(hint):
+    """The error of an output in units of what independent errors of the weights by a part of themselves would make of it.  In fp32: the
+    argument of the exponential lies within 8 of zero, half a step of it is at most 2^-22, 0.95e-7 of a weight (rms); its product 0.5e-7,
+    the exponential 1.2e-7, the sums of 64 keys 2.4e-7 as a share of sqrt(sum w^2 v^2): 2.9e-7 together, and not above 5e-7.  (An argument of
+    32 to 64 alone would be off by 7.6e-7.)"""
+    c = pu.make([63] * 40, [1] * 40, 1, 128, 32, "f32", seed=93)
+    gen = torch.Generator().manual_seed(94)
+    c.k[..., 0] = torch.randint(-256, 1, c.k.shape[:3], generator=gen) / 64.0
+    q = torch.zeros(40, 4, 128)
+    q[..., 0] = 1.0
+    got = run(c, q, 1.0, max_q=hint).double()
+    total = 0.0
+    for b in range(40):
+        k, v, _ = c.keys(b)
+        w = torch.softmax(k[0, :, 0], 0)
+        o = w @ v[0]
+        total += float((((got[b, 0] - o) / ((w[:, None] * (v[0] - o)) ** 2).sum(0).sqrt()) ** 2).mean())
+    assert (total / 40) ** 0.5 <= 5e-7
+
+
 def test_commit_in_a_million_layers_and_heads():
     layers, heads = 65535, 17
     k, v = (torch.randint(0, 120, (layers, 1, heads, 16, 64), dtype=torch.uint8, device="cuda") for _ in "kv")
