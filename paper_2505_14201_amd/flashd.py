@@ -441,7 +441,8 @@ def cache_fork(parent, refs, table, lens, table_out, lens_out, stream=None) -> N
 def cache_reserve(kcache, vcache, refs, table, lens, q_start, report, stream=None) -> None:
     """flashd_cache_reserve: every sequence gets exactly the pages of its keys and new tokens; those it is to write to are its own.
     `report`: int32 [1 + B], receives the number of pages missing (0: all went well) and for each
-    sequence the page that its shared last page was copied from, or -1."""
+    sequence the page that its shared last page was copied from, or -1.  Where pages are missing, shared last
+    pages are held back (entries of -2 - page) until the next call: the step's results and new lengths are void then."""
     if stream is None and _taken(_native.cache_reserve(kcache, vcache, refs, table, lens, q_start, report)):
         return
     c = _cache(kcache, vcache, table, lens, layers=True)
@@ -540,7 +541,7 @@ def attn_fwd_tree(q, kcache, vcache, o, table, lens, q_start, max_q: int, scale:
 def cache_commit(kcache, vcache, table, lens, q_start, lens_out, keep=None, n_keep=None, stream=None) -> None:
     """flashd_cache_commit: the tokens that keep (int32 [B, max_keep], ascending) names move together
     behind their sequence's keys, in every layer; lens_out [B] <- lens + n_keep.  Without `keep` the
-    first n_keep new tokens stay, without n_keep all."""
+    first n_keep new tokens stay, without n_keep all.  Comes before a cache_fork of the same tokens, not after it."""
     if stream is None and _taken(_native.cache_commit(kcache, vcache, table, lens, q_start, lens_out, keep, n_keep)):
         return
     c = _cache(kcache, vcache, table, lens, layers=True)
