@@ -291,6 +291,7 @@ int flashd_skip_stats(const void* q, const void* k, int B, int Hq, int Hkv, int 
  *   flashd_cache_reserve   pages for the new tokens
  *   flashd_cache_append    norm, rotation, and K and V into the pages (every layer)
  *   flashd_attn_fwd_tree   attention of the new tokens (every layer)
+ *   flashd_draft_verify    which of them are accepted, and the token that follows
  *   flashd_cache_commit    the accepted ones move together: the lengths grow
  * and flashd_cache_fork where sequences branch, end or change places.
  *
@@ -424,8 +425,48 @@ int flashd_cache_commit(const flashd_cache* c, const int* q_start, const int* ke
                         const int* n_keep, int* lens_out, void* stream);
 
 /*
+ * Which drafted tokens are accepted, by rejection sampling from given random numbers, so that each token kept has the probability
+ * that the target gives it.  New tokens stand in the packed rows as above: token i of sequence b is row q_start[b] + i; logits of its row are the target's about
+ * the token behind it.  Token 0 was decided before and is kept; each other one was drafted to continue parent[row], an earlier token.
+ *
+ *   p_i = softmax(logits_i / temperature[b]); cur = 0, r = p_0; for the tokens j = 1, 2, ... with parent cur:
+ *     accepted if uniform[row of j] q(x_j) < r(x_j), x_j its id: then cur = j, r = p_j;
+ *     else r <- max(r - q, 0) divided by its sum (r stays where nothing is left), q the row of `draft` of cur.
+ *   Without `draft` (drafts that are no samples: a lookup's, the likeliest ones) q is 1 at x_j and 0 elsewhere.
+ *   next[b] = the least id up to which r sums to more than uniform[row of token 0] times the sum of all.
+ *
+ * With temperature 0 (or below, or NaN) p_i is 1 at the largest logit, the first of equal ones, and 0 elsewhere.  Logits of -infinity
+ * and NaN have probability 0, those of +infinity share everything; behind a row of nothing else no token is accepted and next is -1.
+ * The arithmetic is fp64: results do not depend on the order of sums but where a random number is within some 1e-13 of a border.
+ *   logits   [T][V] in storage type `dtype`, rows logits_stride elements apart, at any multiple of an element; V at most
+ *            FLASHD_VERIFY_MAX_V
+ *   draft    [T][V] in `draft_dtype` (FLASHD_F32, F16 or BF16), rows draft_stride apart, or NULL: row i is the distribution that the tokens continuing
+ *            token i were drawn from (rows that no token continues are not read).  NaN and negative ones count 0.
+ *   tokens   int [T]: ids; those outside [0, V) have probability 0 (token 0's is not looked at)
+ *   parent   int [T]: the token of its sequence that a token continues, an earlier one (a token with another number here is not
+ *            reached); NULL: chains, token i continues i - 1
+ *   uniform  float [T]: random numbers in [0, 1)
+ *   temperature   float [B], or NULL: 1
+ *   keep     int [B][max_keep], overwritten: the tokens kept, ascending, as flashd_cache_commit takes them, -1 behind them.
+ *            A sequence ends at max_keep of them.
+ *   n_keep   int [B]: how many; 0 for a sequence without new tokens
+ *   next     int [B]: the token that follows the last one kept; -1 without new tokens
+ *   workspace   device memory of at least flashd_verify_workspace_bytes(T, V) bytes, 16-byte aligned, or NULL: as in
+ *            flashd_attn_fwd_tree.
+ * Bitwise reproducible.  T == 0: no sequence has new tokens.
+ */
+#define FLASHD_VERIFY_MAX_V (1 << 24)
+int flashd_draft_verify(const void* logits, long long logits_stride, const void* draft, long long draft_stride,
+                        const int* tokens, const int* parent, const float* uniform, const float* temperature,
+                        const int* q_start, int B, int T, int V, int dtype, int draft_dtype, int max_keep, int* keep,
+                        int* n_keep, int* next, void* stream, void* workspace, size_t workspace_bytes);
+
+/* Bytes of workspace of flashd_draft_verify.  0 for invalid arguments. */
+size_t flashd_verify_workspace_bytes(int T, int V);
+
+/*
  * Frees the split-K / fp8 scratch memory that flashd_attn_fwd, flashd_attn_fwd_state,
- * flashd_attn_fwd_kv8 and flashd_attn_fwd_tree have cached for the CURRENT device: the live buffer of every stream
+ * flashd_attn_fwd_kv8, flashd_attn_fwd_tree and flashd_draft_verify have cached for the CURRENT device: the live buffer of every stream
  * that has been used and the buffers those streams have outgrown (which are kept until this
  * call, since work enqueued earlier may still read them).  The frees wait for the device, so
  * work already enqueued is not disturbed; do not call it while another host thread is inside

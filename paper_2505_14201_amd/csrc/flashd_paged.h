@@ -112,6 +112,46 @@ struct TreeArgs {
 hipError_t launch_attn_tree(const Paged& c, const TreeArgs& a, hipStream_t st);
 size_t attn_tree_workspace(int Hq, int Hkv, int max_q, int d, int dtype);
 
+// Drafted tokens that are asked whether they stay: strides in elements.
+struct VerifyArgs {
+    const void *logits, *draft;         // draft NULL: drafts were not sampled
+    const int *tokens, *parent;         // parent NULL: chains
+    const float *uniform, *temperature; // temperature NULL: 1
+    const int* q_start;
+    int *keep, *n_keep, *next;
+    int64_t logits_stride, draft_stride;
+    int B, T, V, dtype, draft_dtype, max_keep;
+};
+
+hipError_t launch_verify(const VerifyArgs& a, void* ws, hipStream_t st);
+size_t verify_workspace(int T, int V);
+
+// New tokens whose attention weights are added to the keys' scores.
+struct ScoreArgs {
+    const void* q;
+    const uint32_t* tree;       // [T][words] bits, or NULL: a chain
+    const float *lse, *weight;  // [T][Hq], [T] or NULL
+    float* score;               // [B][Hkv][score_stride]
+    int64_t q_stride, score_stride;
+    int words;                  // 32-bit words of a row's bits
+    int Hq, dtype, fp8;
+    float scale, decay;
+};
+
+hipError_t launch_cache_score(const Paged& c, const ScoreArgs& a, hipStream_t st);
+
+// Keys that go, of all layers.
+struct EvictArgs {
+    const int *refs, *budgets;  // budgets NULL: `budget` of every sequence
+    float* score;               // [layers][B][Hkv][score_stride]
+    int64_t score_stride, score_layer_stride;
+    int budget, first, recent;
+    int* lens_out;
+};
+
+hipError_t launch_cache_evict(const Paged& c, const EvictArgs& a, void* ws, hipStream_t st);
+size_t evict_workspace(const Paged& c, int budget);
+
 hipError_t launch_cache_fork(const Paged& c, int* refs, const int* parent, int B_out, int* table_out,
                              int* lens_out, hipStream_t st);
 hipError_t launch_cache_reserve(const Paged& c, int* refs, int* report, hipStream_t st);

@@ -12,8 +12,11 @@
 namespace {
 
 using flashd::AppendArgs;
+using flashd::EvictArgs;
 using flashd::Paged;
+using flashd::ScoreArgs;
 using flashd::TreeArgs;
+using flashd::VerifyArgs;
 
 static_assert(FLASHD_CACHE_MAX_SEQS == flashd::kCacheMaxSeqs, "the header states the kernels' limit");
 
@@ -146,6 +149,16 @@ bool kv_overlap(const Paged& p) {
     return false;
 }
 
+// Where the caller has brought no workspace: the stream's.
+int stream_workspace(void* stream, size_t need, void** workspace) {
+    if (*workspace != nullptr) return FLASHD_OK;
+    // A graph would keep the stream's buffer, which other graphs and calls use as well.
+    hipStreamCaptureStatus capturing = hipStreamCaptureStatusNone;
+    if (hipStreamIsCapturing(static_cast<hipStream_t>(stream), &capturing) != hipSuccess) (void)hipGetLastError();
+    if (capturing != hipStreamCaptureStatusNone) return FLASHD_E_WORKSPACE;
+    return flashd::api_cached_workspace(stream, (need + 255) & ~(size_t)255, workspace);
+}
+
 int done(hipError_t e) { return e == hipSuccess ? FLASHD_OK : FLASHD_E_HIP; }
 
 }  // namespace
@@ -275,14 +288,8 @@ int flashd_attn_fwd_tree(const flashd_cache* c, int layer, const void* q, long l
     if (overlaps_any({workspace, (int64_t)need}, {out, in, kp, vp, table, lens, starts, bits})) return FLASHD_E_OVERLAP;
     rc = flashd::api_check_arch();
     if (rc != FLASHD_OK || T == 0) return rc;
-    if (workspace == nullptr) {
-        // A graph would keep the stream's buffer, which other graphs and calls use as well.
-        hipStreamCaptureStatus capturing = hipStreamCaptureStatusNone;
-        if (hipStreamIsCapturing(static_cast<hipStream_t>(stream), &capturing) != hipSuccess) (void)hipGetLastError();
-        if (capturing != hipStreamCaptureStatusNone) return FLASHD_E_WORKSPACE;
-        rc = flashd::api_cached_workspace(stream, (need + 255) & ~(size_t)255, &workspace);
-        if (rc != FLASHD_OK) return rc;
-    }
+    rc = stream_workspace(stream, need, &workspace);
+    if (rc != FLASHD_OK) return rc;
     TreeArgs a;
     a.q = q;
     a.o = o;
@@ -316,6 +323,64 @@ int flashd_cache_commit(const flashd_cache* c, const int* q_start, const int* ke
     rc = flashd::api_check_arch();
     if (rc != FLASHD_OK) return rc;
     return done(flashd::launch_cache_commit(p, keep, max_keep, n_keep, lens_out, static_cast<hipStream_t>(stream)));
+}
+
+size_t flashd_verify_workspace_bytes(int T, int V) {
+    if (T < 0 || T > 10000000 || V < 1 || V > FLASHD_VERIFY_MAX_V) return 0;
+    return flashd::verify_workspace(T, V);
+}
+
+int flashd_draft_verify(const void* logits, long long logits_stride, const void* draft, long long draft_stride,
+                        const int* tokens, const int* parent, const float* uniform, const float* temperature,
+                        const int* q_start, int B, int T, int V, int dtype, int draft_dtype, int max_keep, int* keep,
+                        int* n_keep, int* next, void* stream, void* workspace, size_t workspace_bytes) {
+    if (!logits || !tokens || !uniform || !q_start || !keep || !n_keep || !next) return FLASHD_E_NULL;
+    if (B < 1 || B > FLASHD_CACHE_MAX_SEQS || T < 0 || T > 10000000 || V < 1 || V > FLASHD_VERIFY_MAX_V || max_keep < 1 ||
+        (int64_t)max_keep * B > 0x7fffffff)
+        return FLASHD_E_SHAPE;
+    if (dtype < FLASHD_F32 || dtype > FLASHD_BF16 || (draft && (draft_dtype < FLASHD_F32 || draft_dtype > FLASHD_BF16)))
+        return FLASHD_E_DTYPE;
+    const long long most = 1000000000000;
+    if (logits_stride < V || logits_stride > most || (long double)logits_stride * T > 1.0e12L) return FLASHD_E_SHAPE;
+    if (draft && (draft_stride < V || draft_stride > most || (long double)draft_stride * T > 1.0e12L)) return FLASHD_E_SHAPE;
+    const int esz = esize(dtype), dsz = draft ? esize(draft_dtype) : 4;
+    if ((uintptr_t)logits % esz != 0 || (uintptr_t)draft % dsz != 0 || ((uintptr_t)workspace & 15u) != 0 ||
+        (((uintptr_t)tokens | (uintptr_t)parent | (uintptr_t)uniform | (uintptr_t)temperature | (uintptr_t)q_start | (uintptr_t)keep |
+          (uintptr_t)n_keep | (uintptr_t)next) & 3u) != 0)
+        return FLASHD_E_ALIGN;
+    const size_t need = flashd::verify_workspace(T, V);
+    if (workspace != nullptr && workspace_bytes < need) return FLASHD_E_WORKSPACE;
+    const Span rows{logits, extent(logits_stride, T, 1, V, dtype)}, drafts{draft, draft ? extent(draft_stride, T, 1, V, draft_dtype) : 0},
+        ids{tokens, (int64_t)T * 4}, from{parent, (int64_t)T * 4}, u{uniform, (int64_t)T * 4}, heat{temperature, (int64_t)B * 4},
+        starts{q_start, (int64_t)(B + 1) * 4}, kept{keep, (int64_t)B * max_keep * 4}, counts{n_keep, (int64_t)B * 4}, then{next, (int64_t)B * 4};
+    if (overlaps_any(kept, {rows, drafts, ids, from, u, heat, starts, counts, then}) ||
+        overlaps_any(counts, {rows, drafts, ids, from, u, heat, starts, then}) || overlaps_any(then, {rows, drafts, ids, from, u, heat, starts}) ||
+        overlaps_any({workspace, (int64_t)need}, {rows, drafts, ids, from, u, heat, starts, kept, counts, then}))
+        return FLASHD_E_OVERLAP;
+    int rc = flashd::api_check_arch();
+    if (rc != FLASHD_OK) return rc;
+    if (T > 0) rc = stream_workspace(stream, need, &workspace);
+    if (rc != FLASHD_OK) return rc;
+    VerifyArgs a;
+    a.logits = logits;
+    a.draft = draft;
+    a.tokens = tokens;
+    a.parent = parent;
+    a.uniform = uniform;
+    a.temperature = temperature;
+    a.q_start = q_start;
+    a.keep = keep;
+    a.n_keep = n_keep;
+    a.next = next;
+    a.logits_stride = logits_stride;
+    a.draft_stride = draft ? draft_stride : 0;
+    a.B = B;
+    a.T = T;
+    a.V = V;
+    a.dtype = dtype;
+    a.draft_dtype = draft ? draft_dtype : FLASHD_F32;
+    a.max_keep = max_keep;
+    return done(flashd::launch_verify(a, workspace, static_cast<hipStream_t>(stream)));
 }
 
 }  // extern "C"

@@ -26,6 +26,7 @@ STATIC_SCRATCH_BYTES = 32 << 20
 
 CACHE_FP8 = 3
 CACHE_MAX_SEQS = 4096
+VERIFY_MAX_V = 1 << 24
 
 _DTYPE = {torch.float32: F32, torch.float16: F16, torch.bfloat16: BF16}
 _CACHE_DTYPE = {**_DTYPE, torch.float8_e4m3fn: CACHE_FP8}
@@ -34,7 +35,8 @@ EXPORTS = ("flashd_attn_fwd", "flashd_attn_fwd_ex", "flashd_workspace_bytes",
            "flashd_auto_splits", "flashd_auto_variant", "flashd_status_string", "flashd_version", "flashd_skip_stats", "flashd_attn_fwd_state",
            "flashd_attn_fwd_kv8", "flashd_attn_fwd_static", "flashd_attn_fwd_skipv",
            "flashd_release_workspace", "flashd_cache_fork", "flashd_cache_reserve", "flashd_cache_append",
-           "flashd_attn_fwd_tree", "flashd_tree_workspace_bytes", "flashd_cache_commit")
+           "flashd_attn_fwd_tree", "flashd_tree_workspace_bytes", "flashd_cache_commit",
+           "flashd_draft_verify", "flashd_verify_workspace_bytes")
 
 
 class Cache(ctypes.Structure):
@@ -91,6 +93,10 @@ def _load() -> ctypes.CDLL:
     lib.flashd_attn_fwd_tree.argtypes = [c, i, p, n, p, n, i, i, i, p, p, i, f, i, p, p, z]
     lib.flashd_tree_workspace_bytes.restype = z
     lib.flashd_tree_workspace_bytes.argtypes = [i] * 5
+    lib.flashd_draft_verify.restype = i
+    lib.flashd_draft_verify.argtypes = [p, n, p, n, p, p, p, p, p, i, i, i, i, i, i, p, p, p, p, p, z]
+    lib.flashd_verify_workspace_bytes.restype = z
+    lib.flashd_verify_workspace_bytes.argtypes = [i] * 2
     lib.flashd_release_workspace.restype = i
     lib.flashd_release_workspace.argtypes = []
     lib.flashd_status_string.restype = ctypes.c_char_p
@@ -400,6 +406,15 @@ def _ptr(t):
     return None if t is None else t.data_ptr()
 
 
+def _workspace(workspace, device):
+    """Address and bytes of a caller's workspace."""
+    if workspace is None:
+        return None, 0
+    if workspace.get_device() != device or not workspace.is_contiguous():
+        raise ValueError("workspace must be a contiguous tensor on the cache's GPU")
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size()
+
+
 # The native forms of the five functions below, as of the three above.
 _native.bind_paged(*(ctypes.cast(f, ctypes.c_void_p).value
                      for f in (_lib.flashd_cache_fork, _lib.flashd_cache_reserve, _lib.flashd_cache_append,
@@ -527,11 +542,7 @@ def attn_fwd_tree(q, kcache, vcache, o, table, lens, q_start, max_q: int, scale:
             raise ValueError("tree must be a contiguous int64 tensor [T, words] on the cache's GPU")
         words = tree.shape[1]
     _fit(words, max_q)
-    ws_ptr, ws_bytes = None, 0
-    if workspace is not None:
-        if workspace.get_device() != device or not workspace.is_contiguous():
-            raise ValueError("workspace must be a contiguous tensor on the cache's GPU")
-        ws_ptr, ws_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    ws_ptr, ws_bytes = _workspace(workspace, device)
     if T == 0:
         return
     _enqueue(_lib.flashd_attn_fwd_tree, device, stream, (c, 0, q.data_ptr(), qs, o.data_ptr(), os_, T, int(max_q), Hq,
@@ -555,3 +566,61 @@ def cache_commit(kcache, vcache, table, lens, q_start, lens_out, keep=None, n_ke
         _ints("n_keep", n_keep, (c.B,), device)
     _enqueue(_lib.flashd_cache_commit, device, stream, (c, q_start.data_ptr(), _ptr(keep),
              0 if keep is None else keep.shape[1], _ptr(n_keep), lens_out.data_ptr()))
+
+
+def verify_workspace_bytes(T, V) -> int:
+    return int(_lib.flashd_verify_workspace_bytes(T, V))
+
+
+def _rows(name, t, T, V, device):
+    """The stride of a row of t [T, V], whose rows must be contiguous."""
+    if t.dtype not in _DTYPE or t.dim() != 2 or tuple(t.shape) != (T, V) or t.get_device() != device:
+        raise ValueError(f"{name} must be [{T}, {V}] of type float32, float16 or bfloat16 on the GPU of the logits")
+    if V > 1 and t.stride(1) != 1:
+        raise ValueError(f"rows of {name} must be contiguous")
+    return t.stride(0) if T > 1 else V
+
+
+def _floats(name, t, n, device):
+    if t.dtype != torch.float32 or tuple(t.shape) != n or t.get_device() != device or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous float32 tensor {list(n)} on the same GPU")
+
+
+def draft_verify(logits, tokens, uniform, q_start, keep, n_keep, next_token, parent=None, draft=None, temperature=None,
+                 workspace=None, stream=None) -> None:
+    """flashd_draft_verify: keep [B, max_keep], n_keep [B] and next_token [B] (int32) <- which of the new tokens are accepted
+    and what follows them, by rejection sampling with the random numbers uniform [T] (float32) against the target's
+    logits [T, V].  tokens, parent: int32 [T]; without `parent` each sequence is a chain.  draft [T, V]: the probabilities that the
+    drafts were drawn from, row by row of the token they continue; without it they were not sampled.
+    temperature: float32 [B].  `workspace`: a contiguous tensor of at least verify_workspace_bytes(T, V) bytes;
+    without it scratch memory is kept per stream."""
+    if not logits.is_cuda or logits.dim() != 2:
+        raise ValueError("logits must be [T, V] and live on the GPU")
+    device = logits.get_device()
+    T, V = logits.shape
+    if V < 1:
+        raise ValueError("logits have no columns")
+    stride = _rows("logits", logits, T, V, device)
+    dstride = 0 if draft is None else _rows("draft", draft, T, V, device)
+    _ints("keep", keep, (None, None), device)
+    B, max_keep = keep.shape
+    _ints("n_keep", n_keep, (B,), device)
+    _ints("next_token", next_token, (B,), device)
+    _ints("q_start", q_start, (B + 1,), device)
+    _ints("tokens", tokens, (T,), device)
+    if parent is not None:
+        _ints("parent", parent, (T,), device)
+    _floats("uniform", uniform, (T,), device)
+    if temperature is not None:
+        _floats("temperature", temperature, (B,), device)
+    _fit(T, V, max_keep, B)
+    ws_ptr, ws_bytes = _workspace(workspace, device)
+    if T == 0:
+        # (tensors without elements have no address: any valid one stands for them)
+        _enqueue(_lib.flashd_draft_verify, device, stream, (16, V, None, 0, 16, None, 16, None, q_start.data_ptr(), B, 0, V,
+                 _DTYPE[logits.dtype], 0, max_keep, keep.data_ptr(), n_keep.data_ptr(), next_token.data_ptr()), (None, 0))
+        return
+    _enqueue(_lib.flashd_draft_verify, device, stream, (logits.data_ptr(), stride, _ptr(draft), dstride, tokens.data_ptr(),
+             _ptr(parent), uniform.data_ptr(), _ptr(temperature), q_start.data_ptr(), B, T, V, _DTYPE[logits.dtype],
+             0 if draft is None else _DTYPE[draft.dtype], max_keep, keep.data_ptr(), n_keep.data_ptr(), next_token.data_ptr()),
+             (ws_ptr, ws_bytes))
