@@ -465,6 +465,25 @@ int flashd_draft_verify(const void* logits, long long logits_stride, const void*
 size_t flashd_verify_workspace_bytes(int T, int V);
 
 /*
+ * How much attention each key gets, summed up over the steps: what flashd_cache_evict chooses by.  For every sequence with new tokens, kv head h
+ * and key j < lens[b] + its new tokens,
+ *   score[b][h][j] <- decay * score[b][h][j] + sum of row_weight[t] exp(scale q[t][h'].k_j - lse[t][h'])
+ * over the new tokens (rows t) that see key j, as flashd_attn_fwd_tree has it, and the heads h' that read kv head h.  Keys from
+ * lens[b] on are new: their old scores count 0 and are not read; nor are any with decay 0.  Other scores are left as they are.
+ * After flashd_cache_commit: with the lengths from before it, and the rows of the tokens kept as a chain.  Where sequences branch
+ * or change places their rows of scores are the caller's to copy.
+ *   q, tree, scale, dtype   as in flashd_attn_fwd_tree.  Of the cache K is read; V is not looked at.
+ *   lse          float [T][Hq]: the log-sum-exp of each query's scores.  A row whose lse is infinite or NaN (one that sees no key has -infinity) does
+ *                not count.
+ *   row_weight   float [T], at least 0, or NULL: 1.  Tokens with 0 do not count, whatever their q holds.
+ *   score        float [B][Hkv] rows, score_stride elements apart: at least max_pages * page
+ * The arithmetic is fp32.  Bitwise reproducible.  T == 0 is a call without work.
+ */
+int flashd_cache_score(const flashd_cache* c, int layer, const void* q, long long q_stride, int T, int Hq, const int* q_start,
+                       const unsigned long long* tree, int tree_words, const float* lse, const float* row_weight, float scale,
+                       int dtype, float* score, long long score_stride, float decay, void* stream);
+
+/*
  * Frees the split-K / fp8 scratch memory that flashd_attn_fwd, flashd_attn_fwd_state,
  * flashd_attn_fwd_kv8, flashd_attn_fwd_tree and flashd_draft_verify have cached for the CURRENT device: the live buffer of every stream
  * that has been used and the buffers those streams have outgrown (which are kept until this

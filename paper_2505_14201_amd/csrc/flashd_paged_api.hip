@@ -149,6 +149,17 @@ bool kv_overlap(const Paged& p) {
     return false;
 }
 
+// Scores [(layers)][B][Hkv][stride]: a row has room for every key of a sequence.
+int take_scores(const flashd_cache* c, long long stride, long long layer_stride) {
+    const long long most = 1000000000000;
+    if (stride < (long long)c->max_pages * c->page || stride > most || (long double)stride * c->B * c->Hkv > 1.0e12L) return FLASHD_E_SHAPE;
+    if (c->layers > 1 && layer_stride != 0 &&
+        (layer_stride < stride * c->B * c->Hkv || (long double)layer_stride * c->layers > 1.0e12L))
+        return FLASHD_E_SHAPE;
+    return FLASHD_OK;
+}
+int64_t score_extent(const flashd_cache* c, long long stride) { return (int64_t)c->B * c->Hkv * stride * 4; }
+
 // Where the caller has brought no workspace: the stream's.
 int stream_workspace(void* stream, size_t need, void** workspace) {
     if (*workspace != nullptr) return FLASHD_OK;
@@ -323,6 +334,45 @@ int flashd_cache_commit(const flashd_cache* c, const int* q_start, const int* ke
     rc = flashd::api_check_arch();
     if (rc != FLASHD_OK) return rc;
     return done(flashd::launch_cache_commit(p, keep, max_keep, n_keep, lens_out, static_cast<hipStream_t>(stream)));
+}
+
+int flashd_cache_score(const flashd_cache* c, int layer, const void* q, long long q_stride, int T, int Hq, const int* q_start,
+                       const unsigned long long* tree, int tree_words, const float* lse, const float* row_weight, float scale,
+                       int dtype, float* score, long long score_stride, float decay, void* stream) {
+    Paged p;
+    if (!q || !q_start || !lse || !score) return FLASHD_E_NULL;
+    if (layer < 0) return FLASHD_E_CACHE;
+    int rc = take_cache(c, layer, q_start, T, p);
+    if (rc == FLASHD_OK) rc = take_rows(c, T, Hq, dtype);
+    if (rc != FLASHD_OK) return rc;
+    if (tree && (tree_words < 1 || tree_words > 1000000)) return FLASHD_E_SHAPE;
+    rc = take_stride(q_stride, T, Hq, c->d, dtype);
+    if (rc == FLASHD_OK) rc = take_scores(c, score_stride, 0);
+    if (rc != FLASHD_OK) return rc;
+    if (((uintptr_t)q & 15u) != 0 || ((uintptr_t)tree & 7u) != 0 ||
+        (((uintptr_t)lse | (uintptr_t)row_weight | (uintptr_t)score) & 3u) != 0)
+        return FLASHD_E_ALIGN;
+    const Span out{score, score_extent(c, score_stride)};
+    if (overlaps_any(out, {{q, extent(q_stride, T, Hq, c->d, dtype)}, {p.k, layer_extent(p)}, table_of(p), lens_of(p), starts_of(p),
+                           {tree, (int64_t)T * tree_words * 8}, {lse, (int64_t)T * Hq * 4}, {row_weight, (int64_t)T * 4}}))
+        return FLASHD_E_OVERLAP;
+    rc = flashd::api_check_arch();
+    if (rc != FLASHD_OK || T == 0) return rc;
+    ScoreArgs a;
+    a.q = q;
+    a.tree = reinterpret_cast<const uint32_t*>(tree);
+    a.lse = lse;
+    a.weight = row_weight;
+    a.score = score;
+    a.q_stride = q_stride;
+    a.score_stride = score_stride;
+    a.words = tree != nullptr ? 2 * tree_words : 0;
+    a.Hq = Hq;
+    a.dtype = dtype;
+    a.fp8 = c->dtype == FLASHD_CACHE_FP8;
+    a.scale = scale;
+    a.decay = decay;
+    return done(flashd::launch_cache_score(p, a, static_cast<hipStream_t>(stream)));
 }
 
 size_t flashd_verify_workspace_bytes(int T, int V) {

@@ -36,7 +36,7 @@ EXPORTS = ("flashd_attn_fwd", "flashd_attn_fwd_ex", "flashd_workspace_bytes",
            "flashd_attn_fwd_kv8", "flashd_attn_fwd_static", "flashd_attn_fwd_skipv",
            "flashd_release_workspace", "flashd_cache_fork", "flashd_cache_reserve", "flashd_cache_append",
            "flashd_attn_fwd_tree", "flashd_tree_workspace_bytes", "flashd_cache_commit",
-           "flashd_draft_verify", "flashd_verify_workspace_bytes")
+           "flashd_draft_verify", "flashd_verify_workspace_bytes", "flashd_cache_score")
 
 
 class Cache(ctypes.Structure):
@@ -95,6 +95,8 @@ def _load() -> ctypes.CDLL:
     lib.flashd_tree_workspace_bytes.argtypes = [i] * 5
     lib.flashd_draft_verify.restype = i
     lib.flashd_draft_verify.argtypes = [p, n, p, n, p, p, p, p, p, i, i, i, i, i, i, p, p, p, p, p, z]
+    lib.flashd_cache_score.restype = i
+    lib.flashd_cache_score.argtypes = [c, i, p, n, i, i, p, p, i, p, p, f, i, p, n, f, p]
     lib.flashd_verify_workspace_bytes.restype = z
     lib.flashd_verify_workspace_bytes.argtypes = [i] * 2
     lib.flashd_release_workspace.restype = i
@@ -406,6 +408,16 @@ def _ptr(t):
     return None if t is None else t.data_ptr()
 
 
+def _words(tree, T, device):
+    """Words of a row of a tree's bits, 0 without one."""
+    if tree is None:
+        return 0
+    if tree.dtype != torch.int64 or tree.dim() != 2 or tree.shape[0] != T or not tree.is_contiguous() \
+            or tree.get_device() != device:
+        raise ValueError("tree must be a contiguous int64 tensor [T, words] on the cache's GPU")
+    return tree.shape[1]
+
+
 def _workspace(workspace, device):
     """Address and bytes of a caller's workspace."""
     if workspace is None:
@@ -535,12 +547,7 @@ def attn_fwd_tree(q, kcache, vcache, o, table, lens, q_start, max_q: int, scale:
     qs = _packed("q", q, T, Hq, d, q.dtype, device)
     os_ = _packed("o", o, T, Hq, d, q.dtype, device)
     _ints("q_start", q_start, (c.B + 1,), device)
-    words = 0
-    if tree is not None:
-        if tree.dtype != torch.int64 or tree.dim() != 2 or tree.shape[0] != T or not tree.is_contiguous() \
-                or tree.get_device() != device:
-            raise ValueError("tree must be a contiguous int64 tensor [T, words] on the cache's GPU")
-        words = tree.shape[1]
+    words = _words(tree, T, device)
     _fit(words, max_q)
     ws_ptr, ws_bytes = _workspace(workspace, device)
     if T == 0:
@@ -624,3 +631,45 @@ def draft_verify(logits, tokens, uniform, q_start, keep, n_keep, next_token, par
              _ptr(parent), uniform.data_ptr(), _ptr(temperature), q_start.data_ptr(), B, T, V, _DTYPE[logits.dtype],
              0 if draft is None else _DTYPE[draft.dtype], max_keep, keep.data_ptr(), n_keep.data_ptr(), next_token.data_ptr()),
              (ws_ptr, ws_bytes))
+
+
+def cache_score(q, kcache, table, lens, q_start, lse, score, scale: float, tree=None, row_weight=None, decay: float = 1.0,
+                kscale: float = 1.0, stream=None) -> None:
+    """flashd_cache_score: score [B, Hkv, keys] (float32, a row has room for table.shape[1] pages) <- decay * score + the attention
+    weights that the new tokens' queries q [T, Hq, d] give to each key of one layer's cache, by the log-sum-exps lse [T, Hq] (float32)
+    that attn_fwd_tree has left.  row_weight [T] (float32): how much each token counts."""
+    c = _cache(kcache, kcache, table, lens, kscale)
+    device = kcache.get_device()
+    if q.dim() != 3 or q.dtype not in _DTYPE:
+        raise ValueError("expected q: [T, Hq, d] of type float32, float16 or bfloat16")
+    T, Hq, d = q.shape
+    if d != c.d:
+        raise ValueError("head dimension mismatch between q and kcache")
+    qs = _packed("q", q, T, Hq, d, q.dtype, device)
+    _ints("q_start", q_start, (c.B + 1,), device)
+    words = _words(tree, T, device)
+    _fit(words)
+    _floats("lse", lse, (T, Hq), device)
+    if row_weight is not None:
+        _floats("row_weight", row_weight, (T,), device)
+    stride, _ = _scores(score, c, device)
+    if T == 0:
+        return
+    _enqueue(_lib.flashd_cache_score, device, stream, (c, 0, q.data_ptr(), qs, T, Hq, q_start.data_ptr(), _ptr(tree), words,
+             lse.data_ptr(), _ptr(row_weight), float(scale), _DTYPE[q.dtype], score.data_ptr(), stride, float(decay)))
+
+
+def _scores(score, c, device, layers=False):
+    """The strides of a row and of a layer of score [(layers,) B, Hkv, keys]."""
+    shape, stride = score.shape, score.stride()
+    want = ((c.layers,) if layers and score.dim() == 4 else ()) + (c.B, c.Hkv)
+    if score.dtype != torch.float32 or score.get_device() != device or tuple(shape[:-1]) != want:
+        raise ValueError(f"score must be a float32 tensor {list(want)} + [keys] on the cache's GPU")
+    if layers and c.layers > 1 and score.dim() != 4:
+        raise ValueError("score must have a row for every layer")
+    row = stride[-2] if c.Hkv > 1 else stride[-3] if c.B > 1 else shape[-1]
+    if shape[-1] < 1 or (shape[-1] > 1 and stride[-1] != 1) or (c.B > 1 and c.Hkv > 1 and stride[-3] != c.Hkv * row):
+        raise ValueError("rows of score must be contiguous, and those of a layer equally far apart")
+    if shape[-1] < c.max_pages * c.page:
+        raise ValueError("a row of score must have room for all keys of a sequence")
+    return row, stride[0] if score.dim() == 4 and c.layers > 1 else 0
