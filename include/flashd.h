@@ -293,7 +293,8 @@ int flashd_skip_stats(const void* q, const void* k, int B, int Hq, int Hkv, int 
  *   flashd_attn_fwd_tree   attention of the new tokens (every layer)
  *   flashd_draft_verify    which of them are accepted, and the token that follows
  *   flashd_cache_commit    the accepted ones move together: the lengths grow
- * and flashd_cache_fork where sequences branch, end or change places.
+ * and flashd_cache_fork where sequences branch, end or change places, flashd_cache_score and flashd_cache_evict where a sequence's
+ * keys are to be no more than a budget.
  *
  * All of these, and what they are called with, are device memory except the struct itself, which
  * is read before the call returns.  The library reads table, lens, q_start, refs and the like only on the device,
@@ -484,8 +485,37 @@ int flashd_cache_score(const flashd_cache* c, int layer, const void* q, long lon
                        int dtype, float* score, long long score_stride, float decay, void* stream);
 
 /*
+ * Keys that got little attention go: of a sequence with more than m keys, m = budget (or budgets[b], where that is less), m stay in each
+ * layer and kv head: the first `first` ones, the last `recent` ones, and of the others those with the largest scores, of equal ones the earlier.  (Of
+ * `first` and `recent` the first goes before the last where both do not fit.)  Keys, values and scores of those that stay move
+ * together in their order to keys 0 .. m - 1; lens_out[b] = m, for other sequences lens[b].
+ * In each layer and head other keys may stay.  The keys keep the rotation that they have, but what counts in keys (a position that
+ * flashd_cache_append is not given, a distance) counts those that stayed: hand in `positions` from then on.
+ * A sequence stays as it is if one of its keys behind the first ones has no page, or a page that would be written to (of keys
+ * `first` .. m - 1) is named by more than one entry of the table (refs): a twin's keys are never moved.
+ * Keys behind m hold what they did or what was moved over them; pages left over stay the sequence's until the next flashd_cache_reserve.
+ *   c         as for flashd_cache_commit: all layers; K and V must not share memory
+ *   refs      int [P], as the other calls keep it; read
+ *   score     float [layers][B][Hkv] rows, score_stride elements apart: at least max_pages * page; layers score_layer_stride apart
+ *             (not looked at with one layer).  NaN counts as less than any number.
+ *   budget    the most keys that stay; budgets: int [B], or NULL.  A negative one leaves its sequence as it is.
+ *   first, recent   at least 0
+ *   lens_out  int [B]; must not overlap lens
+ *   workspace   device memory of at least flashd_evict_workspace_bytes(c, budget) bytes, 16-byte aligned, or NULL: as in
+ *             flashd_attn_fwd_tree.
+ * B * Hkv at most 2^20.
+ */
+int flashd_cache_evict(const flashd_cache* c, const int* refs, float* score, long long score_stride, long long score_layer_stride,
+                       int budget, const int* budgets, int first, int recent, int* lens_out, void* stream, void* workspace,
+                       size_t workspace_bytes);
+
+/* Bytes of workspace of flashd_cache_evict, some 64 MB at most, or 4 budget + 12 for each kv head of the sequences if that is more.
+ * 0 for invalid arguments. */
+size_t flashd_evict_workspace_bytes(const flashd_cache* c, int budget);
+
+/*
  * Frees the split-K / fp8 scratch memory that flashd_attn_fwd, flashd_attn_fwd_state,
- * flashd_attn_fwd_kv8, flashd_attn_fwd_tree and flashd_draft_verify have cached for the CURRENT device: the live buffer of every stream
+ * flashd_attn_fwd_kv8, flashd_attn_fwd_tree, flashd_draft_verify and flashd_cache_evict have cached for the CURRENT device: the live buffer of every stream
  * that has been used and the buffers those streams have outgrown (which are kept until this
  * call, since work enqueued earlier may still read them).  The frees wait for the device, so
  * work already enqueued is not disturbed; do not call it while another host thread is inside

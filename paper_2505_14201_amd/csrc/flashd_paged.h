@@ -140,6 +140,8 @@ struct ScoreArgs {
 
 hipError_t launch_cache_score(const Paged& c, const ScoreArgs& a, hipStream_t st);
 
+constexpr int kEvictMostUnits = 1 << 20;       // sequences times kv heads (times layers) of a launch
+
 // Keys that go, of all layers.
 struct EvictArgs {
     const int *refs, *budgets;  // budgets NULL: `budget` of every sequence

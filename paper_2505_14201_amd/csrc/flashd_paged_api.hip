@@ -150,13 +150,10 @@ bool kv_overlap(const Paged& p) {
 }
 
 // Scores [(layers)][B][Hkv][stride]: a row has room for every key of a sequence.
-int take_scores(const flashd_cache* c, long long stride, long long layer_stride) {
+int take_scores(const flashd_cache* c, long long stride) {
     const long long most = 1000000000000;
-    if (stride < (long long)c->max_pages * c->page || stride > most || (long double)stride * c->B * c->Hkv > 1.0e12L) return FLASHD_E_SHAPE;
-    if (c->layers > 1 && layer_stride != 0 &&
-        (layer_stride < stride * c->B * c->Hkv || (long double)layer_stride * c->layers > 1.0e12L))
-        return FLASHD_E_SHAPE;
-    return FLASHD_OK;
+    return stride < (long long)c->max_pages * c->page || stride > most || (long double)stride * c->B * c->Hkv > 1.0e12L ? FLASHD_E_SHAPE
+                                                                                                                     : FLASHD_OK;
 }
 int64_t score_extent(const flashd_cache* c, long long stride) { return (int64_t)c->B * c->Hkv * stride * 4; }
 
@@ -347,7 +344,7 @@ int flashd_cache_score(const flashd_cache* c, int layer, const void* q, long lon
     if (rc != FLASHD_OK) return rc;
     if (tree && (tree_words < 1 || tree_words > 1000000)) return FLASHD_E_SHAPE;
     rc = take_stride(q_stride, T, Hq, c->d, dtype);
-    if (rc == FLASHD_OK) rc = take_scores(c, score_stride, 0);
+    if (rc == FLASHD_OK) rc = take_scores(c, score_stride);
     if (rc != FLASHD_OK) return rc;
     if (((uintptr_t)q & 15u) != 0 || ((uintptr_t)tree & 7u) != 0 ||
         (((uintptr_t)lse | (uintptr_t)row_weight | (uintptr_t)score) & 3u) != 0)
@@ -373,6 +370,51 @@ int flashd_cache_score(const flashd_cache* c, int layer, const void* q, long lon
     a.scale = scale;
     a.decay = decay;
     return done(flashd::launch_cache_score(p, a, static_cast<hipStream_t>(stream)));
+}
+
+size_t flashd_evict_workspace_bytes(const flashd_cache* c, int budget) {
+    Paged p;
+    if (take_cache(c, -1, nullptr, 0, p) != FLASHD_OK || (int64_t)c->B * c->Hkv > flashd::kEvictMostUnits || budget < 0) return 0;
+    return flashd::evict_workspace(p, budget);
+}
+
+int flashd_cache_evict(const flashd_cache* c, const int* refs, float* score, long long score_stride, long long score_layer_stride,
+                       int budget, const int* budgets, int first, int recent, int* lens_out, void* stream, void* workspace,
+                       size_t workspace_bytes) {
+    Paged p;
+    if (!refs || !score || !lens_out) return FLASHD_E_NULL;
+    int rc = take_cache(c, -1, nullptr, 0, p);
+    if (rc == FLASHD_OK) rc = take_scores(c, score_stride);
+    if (rc != FLASHD_OK) return rc;
+    if (budget < 0 || first < 0 || recent < 0 || (int64_t)c->B * c->Hkv > flashd::kEvictMostUnits) return FLASHD_E_SHAPE;
+    const int64_t of_layer = (int64_t)c->B * c->Hkv * score_stride, layer = c->layers > 1 ? score_layer_stride : 0;
+    if (c->layers > 1 && (layer < of_layer || layer > 1000000000000 || (long double)layer * c->layers > 1.0e12L)) return FLASHD_E_SHAPE;
+    if ((((uintptr_t)refs | (uintptr_t)score | (uintptr_t)budgets | (uintptr_t)lens_out) & 3u) != 0 || ((uintptr_t)workspace & 15u) != 0)
+        return FLASHD_E_ALIGN;
+    const size_t need = flashd::evict_workspace(p, budget);
+    if (workspace != nullptr && workspace_bytes < need) return FLASHD_E_WORKSPACE;
+    const Span out{lens_out, (int64_t)c->B * 4}, scores{score, ((c->layers - 1) * layer + of_layer) * 4}, ws{workspace, (int64_t)need},
+        table = table_of(p), lens = lens_of(p), counts{refs, (int64_t)c->P * 4}, most{budgets, (int64_t)c->B * 4};
+    if (overlaps_any(out, {scores, ws, table, lens, counts, most}) || overlaps_any(scores, {ws, table, lens, counts, most}) ||
+        overlaps_any(ws, {table, lens, counts, most}))
+        return FLASHD_E_OVERLAP;
+    for (const void* pool : {p.k, p.v})
+        if (overlaps_any({pool, pool_extent(p)}, {out, scores, ws, table, lens, counts, most})) return FLASHD_E_OVERLAP;
+    if (kv_overlap(p)) return FLASHD_E_OVERLAP;
+    rc = flashd::api_check_arch();
+    if (rc == FLASHD_OK) rc = stream_workspace(stream, need, &workspace);
+    if (rc != FLASHD_OK) return rc;
+    EvictArgs a;
+    a.refs = refs;
+    a.budgets = budgets;
+    a.score = score;
+    a.score_stride = score_stride;
+    a.score_layer_stride = layer;
+    a.budget = budget;
+    a.first = first;
+    a.recent = recent;
+    a.lens_out = lens_out;
+    return done(flashd::launch_cache_evict(p, a, workspace, static_cast<hipStream_t>(stream)));
 }
 
 size_t flashd_verify_workspace_bytes(int T, int V) {

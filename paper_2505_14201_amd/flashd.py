@@ -36,7 +36,8 @@ EXPORTS = ("flashd_attn_fwd", "flashd_attn_fwd_ex", "flashd_workspace_bytes",
            "flashd_attn_fwd_kv8", "flashd_attn_fwd_static", "flashd_attn_fwd_skipv",
            "flashd_release_workspace", "flashd_cache_fork", "flashd_cache_reserve", "flashd_cache_append",
            "flashd_attn_fwd_tree", "flashd_tree_workspace_bytes", "flashd_cache_commit",
-           "flashd_draft_verify", "flashd_verify_workspace_bytes", "flashd_cache_score")
+           "flashd_draft_verify", "flashd_verify_workspace_bytes", "flashd_cache_score",
+           "flashd_cache_evict", "flashd_evict_workspace_bytes")
 
 
 class Cache(ctypes.Structure):
@@ -97,6 +98,10 @@ def _load() -> ctypes.CDLL:
     lib.flashd_draft_verify.argtypes = [p, n, p, n, p, p, p, p, p, i, i, i, i, i, i, p, p, p, p, p, z]
     lib.flashd_cache_score.restype = i
     lib.flashd_cache_score.argtypes = [c, i, p, n, i, i, p, p, i, p, p, f, i, p, n, f, p]
+    lib.flashd_cache_evict.restype = i
+    lib.flashd_cache_evict.argtypes = [c, p, p, n, n, i, p, i, i, p, p, p, z]
+    lib.flashd_evict_workspace_bytes.restype = z
+    lib.flashd_evict_workspace_bytes.argtypes = [c, i]
     lib.flashd_verify_workspace_bytes.restype = z
     lib.flashd_verify_workspace_bytes.argtypes = [i] * 2
     lib.flashd_release_workspace.restype = i
@@ -673,3 +678,29 @@ def _scores(score, c, device, layers=False):
     if shape[-1] < c.max_pages * c.page:
         raise ValueError("a row of score must have room for all keys of a sequence")
     return row, stride[0] if score.dim() == 4 and c.layers > 1 else 0
+
+
+def evict_workspace_bytes(kcache, vcache, table, lens, budget: int) -> int:
+    """Bytes of a workspace of cache_evict with these tensors."""
+    _fit(budget)
+    return int(_lib.flashd_evict_workspace_bytes(_cache(kcache, vcache, table, lens, layers=True), int(budget)))
+
+
+def cache_evict(kcache, vcache, refs, table, lens, score, lens_out, budget: int, budgets=None, first: int = 0, recent: int = 0,
+                workspace=None, stream=None) -> None:
+    """flashd_cache_evict: of every sequence with more keys than `budget` (or budgets[b], int32 [B]) that many stay in each layer and kv head: the
+    first and the recent ones, and those with the largest score [(layers,) B, Hkv, keys] (float32, as cache_score keeps it).  They and their
+    scores move together in their order; lens_out [B] <- the new lengths.  Sequences whose pages are
+    shared (refs) where keys would move stay as they are.  `workspace`: a contiguous tensor of at least
+    evict_workspace_bytes(...) bytes; without it scratch memory is kept per stream."""
+    c = _cache(kcache, vcache, table, lens, layers=True)
+    device = kcache.get_device()
+    _ints("refs", refs, (c.P,), device)
+    _ints("lens_out", lens_out, (c.B,), device)
+    if budgets is not None:
+        _ints("budgets", budgets, (c.B,), device)
+    stride, layer_stride = _scores(score, c, device, layers=True)
+    _fit(budget, first, recent)
+    ws_ptr, ws_bytes = _workspace(workspace, device)
+    _enqueue(_lib.flashd_cache_evict, device, stream, (c, refs.data_ptr(), score.data_ptr(), stride, layer_stride, int(budget), _ptr(budgets),
+             int(first), int(recent), lens_out.data_ptr()), (ws_ptr, ws_bytes))

@@ -1,0 +1,119 @@
+"""What flashd_cache_score and flashd_cache_evict refuse before anything reaches the GPU."""
+import pytest
+import torch
+
+from paper_2505_14201_amd import flashd
+from tests.test_abi import E_ALIGN, E_DTYPE, E_GQA, E_HEADDIM, E_NULL, E_SHAPE, E_VARIANT, E_WS
+from tests.test_paged_refusals import E_CACHE, E_OVERLAP, K, LENS, REFS, START, TABLE, V, cache
+
+Q, BITS, LSE, W, S, OUT, MOST, WS = (0x200000000000 + i * 0x10000000000 for i in range(8))
+POOL = 10 * 2 * 16 * 64 * 2          # bytes of cache()'s K or V
+
+
+def score(c=None, layer=0, q=Q, qs=4 * 64, T=5, Hq=4, start=START, bits=BITS, words=1, lse=LSE, weight=W, dtype=flashd.BF16,
+          to=S, stride=64, **kw):
+    return flashd.raw().flashd_cache_score(c or cache(**kw), layer, q, qs, T, Hq, start, bits, words, lse, weight, 0.1, dtype, to,
+                                           stride, 0.5, None)
+
+
+def evict(c=None, refs=REFS, to=S, stride=64, layer_stride=0, budget=20, budgets=MOST, first=1, recent=2, out=OUT, ws=WS,
+          ws_bytes=1 << 30, **kw):
+    return flashd.raw().flashd_cache_evict(c or cache(**kw), refs, to, stride, layer_stride, budget, budgets, first, recent, out, None,
+                                           ws, ws_bytes)
+
+
+@pytest.mark.parametrize("call", [score, evict])
+def test_of_the_cache(call):
+    for name in ("k", "v", "table", "lens"):
+        assert call(**{name: None}) == E_NULL
+    for name in ("B", "P", "layers", "Hkv", "max_pages"):
+        assert call(**{name: 0}) == E_SHAPE and call(**{name: -2}) == E_SHAPE
+    assert call(B=4097) == E_SHAPE and call(d=96) == E_HEADDIM and call(page=48) == E_CACHE
+    assert call(page_stride=2 * 16 * 64 - 8) == E_CACHE and call(k=K + 8) == E_ALIGN and call(lens=LENS + 1) == E_ALIGN
+    assert call(dtype=4 if call is evict else 3) == E_DTYPE
+
+
+@pytest.mark.parametrize("call", [score, evict])
+def test_of_the_scores(call):
+    assert call(to=None) == E_NULL and call(to=S + 2) == E_ALIGN
+    assert call(stride=63) == E_SHAPE and call(stride=-64) == E_SHAPE and call(stride=1 << 40) == E_SHAPE
+    assert call(max_pages=5) == E_SHAPE                             # a row has 64 places
+
+
+def test_of_cache_score():
+    for name in ("q", "start", "lse"):
+        assert score(**{name: None}) == E_NULL
+    assert score(layer=-1) == E_CACHE and score(layer=1) == E_CACHE
+    assert score(T=-1) == E_SHAPE and score(Hq=0) == E_SHAPE and score(Hq=3) == E_GQA and score(qs=255) == E_SHAPE
+    assert score(words=0) == E_SHAPE and score(words=1000001) == E_SHAPE
+    assert score(dtype=flashd.F16) == E_VARIANT
+    assert score(q=Q + 8) == E_ALIGN and score(qs=4 * 64 + 4) == E_ALIGN and score(bits=BITS + 4) == E_ALIGN
+    assert score(lse=LSE + 1) == E_ALIGN and score(weight=W + 2) == E_ALIGN and score(start=START + 2) == E_ALIGN
+    size = 3 * 2 * 64 * 4
+    for at, length in ((Q, 5 * 4 * 64 * 2), (K, POOL), (TABLE, 48), (LENS, 12), (START, 16), (BITS, 40), (LSE, 80), (W, 20)):
+        assert score(to=at) == E_OVERLAP and score(to=at + length - 4) == E_OVERLAP and score(to=at - size + 4) == E_OVERLAP
+
+
+def test_of_cache_evict():
+    for name in ("refs", "out"):
+        assert evict(**{name: None}) == E_NULL
+    assert evict(budget=-1) == E_SHAPE and evict(first=-1) == E_SHAPE and evict(recent=-1) == E_SHAPE
+    assert evict(B=4096, Hkv=257, page_stride=257 * 16 * 64) == E_SHAPE
+    assert evict(cache(layers=2, layer_stride=10 * 2 * 16 * 64), layer_stride=3 * 2 * 64 - 4) == E_SHAPE
+    assert evict(cache(layers=2, layer_stride=10 * 2 * 16 * 64), layer_stride=1 << 40) == E_SHAPE
+    for name, at in (("refs", REFS), ("budgets", MOST), ("out", OUT)):
+        assert evict(**{name: at + 2}) == E_ALIGN
+    assert evict(ws=WS + 8) == E_ALIGN
+    need = flashd.raw().flashd_evict_workspace_bytes(cache(), 20)
+    assert need >= 3 * 2 * 20 * 4 and evict(ws_bytes=need - 1) == E_WS
+    assert flashd.raw().flashd_evict_workspace_bytes(cache(), -1) == 0
+    assert flashd.raw().flashd_evict_workspace_bytes(cache(d=96), 20) == 0
+    # at most 64 MB, whatever the layers
+    many = cache(layers=60000, layer_stride=2 * 16 * 64, page_stride=60000 * 2 * 16 * 64, B=64, max_pages=1000, P=10)
+    assert flashd.raw().flashd_evict_workspace_bytes(many, 16000) < (64 << 20) + 100
+    assert evict(v=K) == E_OVERLAP and evict(v=K + 16 * 64 * 2) == E_OVERLAP
+    size = 3 * 2 * 64 * 4
+    for out, n in (("out", 12), ("to", size), ("ws", need)):
+        places = [(K, POOL), (V, POOL), (TABLE, 48), (LENS, 12), (REFS, 40), (MOST, 12)]
+        places += [(S, size)] * (out != "to") + [(WS, need)] * (out == "out")
+        for at, length in places:
+            assert evict(**{out: at}) == E_OVERLAP and evict(**{out: at + length - 16}) == E_OVERLAP or length < 16
+
+
+def test_of_their_python_forms():
+    t = torch.zeros
+    i = lambda *s: t(*s, dtype=torch.int32)     # noqa: E731
+    pool = t(3, 2, 16, 64)
+    with pytest.raises(ValueError, match="GPU"):
+        flashd.cache_score(t(4, 2, 64), pool, i(1, 2), i(1), i(2), t(4, 2), t(1, 2, 32), 0.1)
+    with pytest.raises(ValueError, match="GPU"):
+        flashd.cache_evict(pool, pool.clone(), i(3), i(1, 2), i(1), t(1, 2, 32), i(1), 5)
+
+
+@pytest.mark.gpu
+def test_of_their_python_forms_on_the_gpu():
+    t = lambda *s: torch.zeros(*s, device="cuda")     # noqa: E731
+    i = lambda *s: torch.zeros(*s, dtype=torch.int32, device="cuda")     # noqa: E731
+    pool, other = t(2, 3, 2, 16, 64), t(2, 3, 2, 16, 64)
+    good = dict(q=t(4, 2, 64), kcache=pool[0], table=i(2, 2), lens=i(2), q_start=i(3), lse=t(4, 2), score=t(2, 2, 32), scale=0.1)
+    flashd.cache_score(**good)
+    for name, bad in (("q", t(4, 2, 128)), ("q", t(4, 2, 64).half()), ("lse", t(2, 4).T), ("lse", t(4, 1)), ("score", t(2, 2, 31)),
+                      ("score", t(2, 1, 32)), ("score", t(2, 2, 64)[..., ::2]), ("score", t(2, 2, 32).double()), ("q_start", i(2)),
+                      ("row_weight", t(3)), ("tree", i(4, 1)), ("score", t(2, 32, 2).transpose(1, 2)), ("score", t(2, 3, 32)[:, :2])):
+        with pytest.raises((ValueError, flashd.FlashdError)):
+            flashd.cache_score(**{**good, name: bad})
+    good = dict(kcache=pool, vcache=other, refs=i(3), table=i(2, 2), lens=i(2), score=t(2, 2, 2, 32), lens_out=i(2), budget=5)
+    flashd.cache_evict(**good)
+    for name, bad in (("score", t(2, 2, 32)), ("score", t(1, 2, 2, 32)), ("score", t(2, 2, 2, 16)), ("refs", i(2)), ("lens_out", i(3)),
+                      ("budgets", i(1)), ("budget", -1), ("first", -1), ("budget", 1 << 40), ("workspace", t(1)), ("vcache", pool),
+                      ("lens_out", good["lens"])):
+        with pytest.raises((ValueError, flashd.FlashdError)):
+            flashd.cache_evict(**{**good, name: bad})
+    logits, n = t(4, 9), i(2)
+    good = dict(logits=logits, tokens=i(4), uniform=t(4), q_start=i(3), keep=i(2, 3), n_keep=n, next_token=i(2))
+    flashd.draft_verify(**good)
+    for name, bad in (("logits", t(4, 18)[:, ::2]), ("logits", t(4, 9).double()), ("tokens", i(3)), ("uniform", i(4)), ("uniform", t(8)[::2]),
+                      ("q_start", i(2)), ("keep", i(3, 3)), ("keep", i(2, 0)), ("n_keep", i(3)), ("next_token", n), ("parent", i(5)),
+                      ("draft", t(4, 8)), ("draft", logits.double()), ("temperature", t(3)), ("workspace", t(1))):
+        with pytest.raises((ValueError, flashd.FlashdError)):
+            flashd.draft_verify(**{**good, name: bad})

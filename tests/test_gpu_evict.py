@@ -1,0 +1,229 @@
+"""flashd_cache_evict against a plain model.  Everything it does is choosing and moving: results have to be equal, bit for
+bit."""
+import math
+
+import pytest
+import torch
+
+from paper_2505_14201_amd import flashd
+from tests.paged_util import DT, ints
+
+pytestmark = pytest.mark.gpu
+
+
+class Life:
+    """A cache of some layers on the CPU, with scores."""
+
+    def __init__(self, lens, Hkv=2, d=64, page=16, dtype="bf16", layers=1, seed=0, side_by_side=False, spare_columns=1):
+        gen = torch.Generator().manual_seed(seed)
+        B = len(lens)
+        cols = [-(-n // page) for n in lens]
+        P = sum(cols) + 2
+        self.lens, self.page = lens, page
+        self.table = torch.full((B, max(cols) + spare_columns), -1, dtype=torch.int32)
+        order = torch.randperm(P, generator=gen).to(torch.int32)
+        at = 0
+        for b, n in enumerate(cols):
+            self.table[b, :n] = order[at:at + n]
+            at += n
+        shape = (layers, P, Hkv, page, d)
+        if dtype == "fp8":
+            both = [(torch.randn(shape, generator=gen) * 30).to(torch.float8_e4m3fn) for _ in range(2)]
+        else:
+            both = [torch.randn(shape, generator=gen).to(DT[dtype]) for _ in range(2)]
+        self.k, self.v = both
+        self.side_by_side = side_by_side
+        self.score = torch.exp(3 * torch.randn(layers, B, Hkv, self.table.shape[1] * page + 4, generator=gen))
+
+    @property
+    def refs(self):
+        n = torch.zeros(self.k.shape[1], dtype=torch.int32)
+        for p in self.table.flatten().tolist():
+            if p != -1:
+                n[p if p >= 0 else -2 - p] += 1
+        return n
+
+    def evicted(self, budget, budgets=None, first=0, recent=0):
+        """k, v, score, lens as they are to be."""
+        k, v, score, out = self.bytes(self.k).clone(), self.bytes(self.v).clone(), self.score.clone(), []
+        refs = self.refs
+        for b, l in enumerate(self.lens):
+            m = budget if budgets is None else min(budget, budgets[b])
+            f = min(first, max(m, 0))
+            r = min(recent, m - f)
+            pages = self.table[b].tolist()
+            moves = range(f // self.page, -(-l // self.page)) if m > f else []
+            blocked = any(pages[c] < 0 or (c * self.page < m and refs[pages[c]] > 1) for c in moves)
+            if m < 0 or l <= m or blocked:
+                out.append(l)
+                continue
+            out.append(m)
+            for y in range(k.shape[0]):
+                for h in range(k.shape[2]):
+                    x = self.score[y, b, h, :l].tolist()
+                    rank = sorted(range(f, l - r), key=lambda j: (-(x[j] if x[j] == x[j] else -math.inf), x[j] != x[j], j))
+                    stay = list(range(f)) + sorted(rank[:m - f - r]) + list(range(l - r, l))
+                    at = [(pages[j // self.page], j % self.page) for j in stay]
+                    for pool, old in ((k, self.bytes(self.k)), (v, self.bytes(self.v))):
+                        for i, (p, o) in enumerate(at):
+                            if stay[i] != i:
+                                pool[y, pages[i // self.page], h, i % self.page] = old[y, p, h, o]
+                    score[y, b, h, :m] = self.score[y, b, h, stay]
+        return k, v, score, out
+
+    @staticmethod
+    def bytes(x):
+        return x.view(torch.uint8)
+
+
+def check(c, budget, budgets=None, **kw):
+    layers, P, Hkv, page, d = c.k.shape
+    if c.side_by_side:           # a page's layers, K and V lie next to each other
+        pool = torch.zeros(P, layers, 2, Hkv, page, d, dtype=c.k.dtype, device="cuda")
+        k, v = pool[:, :, 0].transpose(0, 1), pool[:, :, 1].transpose(0, 1)
+        k.copy_(c.k)
+        v.copy_(c.v)
+    else:
+        k, v = c.k.cuda(), c.v.cuda()
+    score, out = c.score.cuda(), ints([77] * len(c.lens)).cuda()
+    flashd.cache_evict(k, v, c.refs.cuda(), c.table.cuda(), ints(c.lens).cuda(), score, out, budget,
+                       budgets=None if budgets is None else ints(budgets).cuda(), **kw)
+    wk, wv, ws, lens = c.evicted(budget, budgets, **kw)
+    assert out.tolist() == lens
+    # keys behind the new length hold anything; what is another's, or before it, is as it should be
+    for got, want, old in ((k, wk, c.k), (v, wv, c.v)):
+        assert torch.equal(c.bytes(got.contiguous().cpu()), want)
+    assert torch.equal(score.cpu().view(torch.int32), ws.view(torch.int32))
+    return lens
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16", "fp8"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("budget", [0, 1, 15, 16, 17, 100, 129])
+def test_types_and_budgets(dtype, d, budget):
+    check(Life([130, 0, 1, 16, 17, 100, 101, 300], 2, d, 16, dtype, 2, seed=budget), budget, first=3, recent=5)
+
+
+@pytest.mark.parametrize("first,recent", [(0, 0), (16, 0), (0, 16), (40, 40), (64, 0), (0, 64), (100, 3), (3, 100), (63, 0), (31, 32)])
+@pytest.mark.parametrize("page", [16, 32, 64, 128, 256])
+def test_what_stays_in_any_case(first, recent, page):
+    check(Life([64, 65, 200, 70], 1, 64, page, "bf16", seed=first), 64, first=first, recent=recent)
+
+
+@pytest.mark.parametrize("layers,Hkv", [(1, 1), (3, 5), (7, 1)])
+@pytest.mark.parametrize("side_by_side", [False, True])
+def test_layers_and_heads(layers, Hkv, side_by_side):
+    check(Life([200, 90, 33], Hkv, 64, 32, "f16", layers, seed=Hkv, side_by_side=side_by_side), 60, first=2, recent=4)
+
+
+@pytest.mark.parametrize("L,budget", [(1025, 1024), (3000, 2999), (3000, 2048), (5000, 17), (9000, 4096), (20001, 20000), (70000, 30000)])
+def test_lengths(L, budget):
+    """Many rows from below the new length (moved in order), and many from behind it."""
+    check(Life([L], 1, 64, 256, "bf16", seed=L), budget, first=4, recent=7)
+
+
+def test_equal_scores_infinities_and_nan():
+    c = Life([500, 500, 500, 500, 500, 500], 1, 64, 16, "bf16", seed=1)
+    gen = torch.Generator().manual_seed(2)
+    c.score[0, 0] = 1.0
+    c.score[0, 1] = torch.randint(0, 3, c.score[0, 1].shape, generator=gen).float()
+    c.score[0, 2, :, ::2] = math.nan
+    c.score[0, 3, :, ::3] = math.inf
+    c.score[0, 3, :, 1::3] = -math.inf
+    c.score[0, 4] = torch.where(torch.rand(c.score[0, 4].shape, generator=gen) < 0.5, -0.0, 0.0)
+    c.score[0, 5] = -c.score[0, 5] * 1e-40
+    for budget in (1, 100, 260, 499):
+        check(c, budget, first=1, recent=2)
+
+
+def test_scores_that_differ_in_their_last_bits():
+    c = Life([4000], 2, 64, 64, "f16", seed=3)
+    bits = torch.randperm(c.score.numel(), generator=torch.Generator().manual_seed(4)).to(torch.int32) + 0x3f800000
+    c.score = bits.view(torch.float32).view(c.score.shape).clone()
+    check(c, 1777)
+
+
+def test_a_budget_for_each():
+    check(Life([100, 100, 100, 100, 5], 2, 64, 16, seed=5), 90, budgets=[50, 95, -1, 0, 7], first=1, recent=1)
+
+
+def test_shared_pages_and_pages_that_are_none():
+    page = 16
+    c = Life([200, 200, 200, 200, 200, 200], 1, 64, page, seed=6)
+    c.table[1, :4] = c.table[0, :4]          # twins of a prompt of 64 keys
+    c.table[3, 12] = c.table[2, 12]          # a page that is only read
+    c.table[4, 6] = -1
+    c.table[5, 9] = -2 - int(c.table[5, 9])  # held back
+    assert check(c, 100) == [200, 200, 100, 100, 200, 200]
+    assert check(c, 100, first=64) == [100, 100, 100, 100, 200, 200]     # the shared ones stay where they are
+    assert check(c, 100, first=60) == [200, 200, 100, 100, 200, 200]
+    assert check(c, 50, first=50) == [50] * 6                            # nothing moves
+
+
+def test_lengths_past_the_table():
+    c = Life([64], 1, 64, 16, seed=7, spare_columns=0)
+    k, v, score, out = c.k.cuda(), c.v.cuda(), c.score.cuda(), ints([0]).cuda()
+    for l, budget, want in ((1000, 100, 1000), (-5, 3, -5)):
+        flashd.cache_evict(k, v, c.refs.cuda(), c.table.cuda(), ints([l]).cuda(), score, out, budget)
+        assert out.tolist() == [want]
+        assert torch.equal(k.cpu(), c.k) and torch.equal(score.cpu(), c.score)
+
+
+def test_more_layers_than_a_launch_has_room_for():
+    """64 MB of ranks hold those of 2 layers (22.4 MB each)."""
+    c = Life([30], 1, 64, 16, seed=8, layers=8)
+    B, S = 4, 1400000                        # a long table, of which only the first columns name pages
+    c.lens = [30, 24, 29, 5]
+    pages = c.k.shape[1]
+    assert pages == 4
+    k = torch.randn(8, 8, 1, 16, 64).to(torch.bfloat16)
+    v = torch.randn_like(k)
+    table = torch.full((B, S // 16), -1, dtype=torch.int32)
+    table[:, :2] = torch.arange(8, dtype=torch.int32).view(4, 2)
+    refs = ints([1] * 8)
+    score = torch.rand(8, B, 1, 40)
+    far = torch.zeros(8, B, 1, S, device="cuda")
+    far[..., :40] = score.cuda()
+    kg, vg, out = k.cuda(), v.cuda(), ints([0] * B).cuda()
+    need = flashd.evict_workspace_bytes(kg, vg, table.cuda(), out, 2000000)
+    assert 2 * B * 4 * S < need < 3 * B * 4 * S
+    flashd.cache_evict(kg, vg, refs.cuda(), table.cuda(), ints(c.lens).cuda(), far, out, 2000000, budgets=ints([20, 20, 28, 20]).cuda())
+    assert out.tolist() == [20, 20, 28, 5]
+    for y in range(8):
+        for b, (l, m) in enumerate(zip(c.lens, (20, 20, 28, 5))):
+            stay = sorted(sorted(range(l), key=lambda j: (-float(score[y, b, 0, j]), j))[:m])
+            for pool, old in ((kg, k), (vg, v)):
+                got = pool[y, 2 * b:2 * b + 2, 0].reshape(32, 64)[:m].cpu()
+                assert torch.equal(got, old[y, 2 * b:2 * b + 2, 0].reshape(32, 64)[stay])
+
+
+def test_a_captured_call_is_replayed_with_other_numbers():
+    c = Life([300, 80, 150], 2, 64, 16, seed=9, layers=2)
+    k, v, table, lens, score, refs = c.k.cuda(), c.v.cuda(), c.table.cuda(), ints(c.lens).cuda(), c.score.cuda(), c.refs.cuda()
+    out, budgets = ints([0] * 3).cuda(), ints([100] * 3).cuda()
+    ws = torch.empty(flashd.evict_workspace_bytes(k, v, table, lens, 120), dtype=torch.uint8, device="cuda")
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+
+    def run(**kw):
+        flashd.cache_evict(k, v, refs, table, lens, score, out, 120, budgets=budgets, first=2, recent=3, **kw)
+
+    run(stream=side)
+    side.synchronize()
+    assert out.tolist() == [100, 80, 100]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        run(workspace=ws)
+    for now in ([90, 10, 120], [130, 79, 1], [-1, 0, 64]):
+        k.copy_(c.k)
+        v.copy_(c.v)
+        score.copy_(c.score)
+        budgets.copy_(ints(now))
+        graph.replay()
+        torch.cuda.synchronize()
+        wk, wv, ws_, want = c.evicted(120, now, first=2, recent=3)
+        assert out.tolist() == want
+        assert torch.equal(c.bytes(k.cpu()), wk) and torch.equal(c.bytes(v.cpu()), wv) and torch.equal(score.cpu(), ws_)
+    with pytest.raises(flashd.FlashdError):
+        with torch.cuda.graph(torch.cuda.CUDAGraph()):
+            run()
