@@ -77,7 +77,7 @@ def test_of_cache_evict():
         places = [(K, POOL), (V, POOL), (TABLE, 48), (LENS, 12), (REFS, 40), (MOST, 12)]
         places += [(S, size)] * (out != "to") + [(WS, need)] * (out == "out")
         for at, length in places:
-            assert evict(**{out: at}) == E_OVERLAP and evict(**{out: at + length - 16}) == E_OVERLAP or length < 16
+            assert evict(**{out: at}) == E_OVERLAP and evict(**{out: at + (length - 1) // 16 * 16}) == E_OVERLAP
 
 
 def test_of_their_python_forms():
