@@ -407,7 +407,17 @@ int flashd_attn_fwd_tree(const flashd_cache* c, int layer, const void* q, long l
                          const unsigned long long* tree, int tree_words, float scale, int dtype,
                          void* stream, void* workspace, size_t workspace_bytes);
 
-/* Bytes of workspace of flashd_attn_fwd_tree: does not depend on B, T or any length.  0 for invalid
+/*
+ * The same, and each query's log-sum-exp (natural logarithm) of the scores of the keys that it sees, as flashd_cache_score takes them:
+ *   lse      float [T][Hq], for the rows that have an output; -infinity where a token sees no key.  Must not share memory with anything.
+ * The output is that of flashd_attn_fwd_tree, bit for bit.
+ */
+int flashd_attn_fwd_tree_lse(const flashd_cache* c, int layer, const void* q, long long q_stride, void* o,
+                             long long o_stride, int T, int max_q, int Hq, const int* q_start,
+                             const unsigned long long* tree, int tree_words, float scale, int dtype, float* lse,
+                             void* stream, void* workspace, size_t workspace_bytes);
+
+/* Bytes of workspace of flashd_attn_fwd_tree and flashd_attn_fwd_tree_lse: does not depend on B, T or any length.  0 for invalid
  * arguments. */
 size_t flashd_tree_workspace_bytes(int Hq, int Hkv, int max_q, int d, int dtype);
 
@@ -474,7 +484,7 @@ size_t flashd_verify_workspace_bytes(int T, int V);
  * After flashd_cache_commit: with the lengths from before it, and the rows of the tokens kept as a chain.  Where sequences branch
  * or change places their rows of scores are the caller's to copy.
  *   q, tree, scale, dtype   as in flashd_attn_fwd_tree.  Of the cache K is read; V is not looked at.
- *   lse          float [T][Hq]: the log-sum-exp of each query's scores.  A row whose lse is infinite or NaN (one that sees no key has -infinity) does
+ *   lse          float [T][Hq], as flashd_attn_fwd_tree_lse leaves it: the log-sum-exp of each query's scores.  A row whose lse is infinite or NaN (one that sees no key has -infinity) does
  *                not count.
  *   row_weight   float [T], at least 0, or NULL: 1.  Tokens with 0 do not count, whatever their q holds.
  *   score        float [B][Hkv] rows, score_stride elements apart: at least max_pages * page

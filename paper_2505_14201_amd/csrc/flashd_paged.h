@@ -107,6 +107,7 @@ struct TreeArgs {
     int Hq, max_q, dtype, fp8;
     float scale;
     float* ws;
+    float* lse;                 // [T][Hq], or NULL
 };
 
 hipError_t launch_attn_tree(const Paged& c, const TreeArgs& a, hipStream_t st);

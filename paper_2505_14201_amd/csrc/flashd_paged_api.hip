@@ -169,6 +169,50 @@ int stream_workspace(void* stream, size_t need, void** workspace) {
 
 int done(hipError_t e) { return e == hipSuccess ? FLASHD_OK : FLASHD_E_HIP; }
 
+int attn_fwd_tree(const flashd_cache* c, int layer, const void* q, long long q_stride, void* o, long long o_stride, int T, int max_q,
+                  int Hq, const int* q_start, const unsigned long long* tree, int tree_words, float scale, int dtype, float* lse,
+                  void* stream, void* workspace, size_t workspace_bytes) {
+    Paged p;
+    if (!q || !o || !q_start) return FLASHD_E_NULL;
+    if (layer < 0) return FLASHD_E_CACHE;
+    int rc = take_cache(c, layer, q_start, T, p);
+    if (rc == FLASHD_OK) rc = take_rows(c, T, Hq, dtype);
+    if (rc != FLASHD_OK) return rc;
+    if (max_q < 1 || (tree && (tree_words < 1 || tree_words > 1000000))) return FLASHD_E_SHAPE;
+    rc = take_stride(q_stride, T, Hq, c->d, dtype);
+    if (rc == FLASHD_OK) rc = take_stride(o_stride, T, Hq, c->d, dtype);
+    if (rc != FLASHD_OK) return rc;
+    if ((((uintptr_t)q | (uintptr_t)o | (uintptr_t)workspace) & 15u) != 0 || ((uintptr_t)tree & 7u) != 0 || ((uintptr_t)lse & 3u) != 0)
+        return FLASHD_E_ALIGN;
+    const size_t need = flashd::attn_tree_workspace(Hq, c->Hkv, max_q, c->d, dtype);
+    const Span out{o, extent(o_stride, T, Hq, c->d, dtype)}, in{q, extent(q_stride, T, Hq, c->d, dtype)}, kp{p.k, layer_extent(p)},
+        vp{p.v, layer_extent(p)}, table = table_of(p), lens = lens_of(p), starts = starts_of(p), bits{tree, (int64_t)T * tree_words * 8},
+        sums{lse, (int64_t)T * Hq * 4};
+    if (overlaps_any(out, {in, kp, vp, table, lens, starts, bits, sums}) || overlaps_any(sums, {in, kp, vp, table, lens, starts, bits}))
+        return FLASHD_E_OVERLAP;
+    if (workspace != nullptr && workspace_bytes < need) return FLASHD_E_WORKSPACE;
+    if (overlaps_any({workspace, (int64_t)need}, {out, in, kp, vp, table, lens, starts, bits, sums})) return FLASHD_E_OVERLAP;
+    rc = flashd::api_check_arch();
+    if (rc != FLASHD_OK || T == 0) return rc;
+    rc = stream_workspace(stream, need, &workspace);
+    if (rc != FLASHD_OK) return rc;
+    TreeArgs a;
+    a.q = q;
+    a.o = o;
+    a.tree = reinterpret_cast<const uint32_t*>(tree);
+    a.q_stride = q_stride;
+    a.o_stride = o_stride;
+    a.words = tree != nullptr ? 2 * tree_words : 0;
+    a.Hq = Hq;
+    a.max_q = max_q;
+    a.dtype = dtype;
+    a.fp8 = c->dtype == FLASHD_CACHE_FP8;
+    a.scale = scale;
+    a.ws = static_cast<float*>(workspace);
+    a.lse = lse;
+    return done(flashd::launch_attn_tree(p, a, static_cast<hipStream_t>(stream)));
+}
+
 }  // namespace
 
 extern "C" {
@@ -277,41 +321,17 @@ int flashd_attn_fwd_tree(const flashd_cache* c, int layer, const void* q, long l
                          long long o_stride, int T, int max_q, int Hq, const int* q_start,
                          const unsigned long long* tree, int tree_words, float scale, int dtype,
                          void* stream, void* workspace, size_t workspace_bytes) {
-    Paged p;
-    if (!q || !o || !q_start) return FLASHD_E_NULL;
-    if (layer < 0) return FLASHD_E_CACHE;
-    int rc = take_cache(c, layer, q_start, T, p);
-    if (rc == FLASHD_OK) rc = take_rows(c, T, Hq, dtype);
-    if (rc != FLASHD_OK) return rc;
-    if (max_q < 1 || (tree && (tree_words < 1 || tree_words > 1000000))) return FLASHD_E_SHAPE;
-    rc = take_stride(q_stride, T, Hq, c->d, dtype);
-    if (rc == FLASHD_OK) rc = take_stride(o_stride, T, Hq, c->d, dtype);
-    if (rc != FLASHD_OK) return rc;
-    if ((((uintptr_t)q | (uintptr_t)o | (uintptr_t)workspace) & 15u) != 0 || ((uintptr_t)tree & 7u) != 0) return FLASHD_E_ALIGN;
-    const size_t need = flashd::attn_tree_workspace(Hq, c->Hkv, max_q, c->d, dtype);
-    const Span out{o, extent(o_stride, T, Hq, c->d, dtype)}, in{q, extent(q_stride, T, Hq, c->d, dtype)}, kp{p.k, layer_extent(p)},
-        vp{p.v, layer_extent(p)}, table = table_of(p), lens = lens_of(p), starts = starts_of(p), bits{tree, (int64_t)T * tree_words * 8};
-    if (overlaps_any(out, {in, kp, vp, table, lens, starts, bits})) return FLASHD_E_OVERLAP;
-    if (workspace != nullptr && workspace_bytes < need) return FLASHD_E_WORKSPACE;
-    if (overlaps_any({workspace, (int64_t)need}, {out, in, kp, vp, table, lens, starts, bits})) return FLASHD_E_OVERLAP;
-    rc = flashd::api_check_arch();
-    if (rc != FLASHD_OK || T == 0) return rc;
-    rc = stream_workspace(stream, need, &workspace);
-    if (rc != FLASHD_OK) return rc;
-    TreeArgs a;
-    a.q = q;
-    a.o = o;
-    a.tree = reinterpret_cast<const uint32_t*>(tree);
-    a.q_stride = q_stride;
-    a.o_stride = o_stride;
-    a.words = tree != nullptr ? 2 * tree_words : 0;
-    a.Hq = Hq;
-    a.max_q = max_q;
-    a.dtype = dtype;
-    a.fp8 = c->dtype == FLASHD_CACHE_FP8;
-    a.scale = scale;
-    a.ws = static_cast<float*>(workspace);
-    return done(flashd::launch_attn_tree(p, a, static_cast<hipStream_t>(stream)));
+    return attn_fwd_tree(c, layer, q, q_stride, o, o_stride, T, max_q, Hq, q_start, tree, tree_words, scale, dtype, nullptr, stream,
+                         workspace, workspace_bytes);
+}
+
+int flashd_attn_fwd_tree_lse(const flashd_cache* c, int layer, const void* q, long long q_stride, void* o,
+                             long long o_stride, int T, int max_q, int Hq, const int* q_start,
+                             const unsigned long long* tree, int tree_words, float scale, int dtype, float* lse,
+                             void* stream, void* workspace, size_t workspace_bytes) {
+    if (!lse) return FLASHD_E_NULL;
+    return attn_fwd_tree(c, layer, q, q_stride, o, o_stride, T, max_q, Hq, q_start, tree, tree_words, scale, dtype, lse, stream,
+                         workspace, workspace_bytes);
 }
 
 int flashd_cache_commit(const flashd_cache* c, const int* q_start, const int* keep, int max_keep,

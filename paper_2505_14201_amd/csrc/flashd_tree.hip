@@ -12,6 +12,9 @@
 // row's (Walk).  A unit that ends up in several workgroups is
 // left as partial states (at most two per workgroup: its first unit, begun by the one before, and its
 // last) that merge_tree_kernel joins in the order of the keys: the result does not depend on timing.
+//
+// LSE: the rows' log-sum-exps are wanted as well.  Where rows are divided by the sum of the rounded weights (bf16) the sum of the unrounded ones is then
+// carried beside it: what later weights are held against is the true one.  Instances of their own: the others are as they were.
 #include "flashd_common.h"
 #include "flashd_kernels.h"
 #include "flashd_mma.h"
@@ -72,6 +75,7 @@ struct TreeRun {
     float* parts;           // [2 groups][rows of a tile][d] unnormalised outputs
     float2* stats;          // [2 groups][rows of a tile] reference and sum of weights
     TreeSplit* splits;      // [groups], of the unit that a workgroup begins and does not end
+    float* sums;            // [2 groups][rows of a tile] sums of unrounded weights (LSE of bf16)
     int groups;             // workgroups of the launch
 };
 
@@ -404,17 +408,32 @@ __device__ __forceinline__ size_t row_at(const TreeRun& r, const W& u, int rw, i
     return (size_t)(u.s.row0 + token) * stride + (size_t)(u.h * (int)r.group.d + rw - token * (int)r.group.d) * d;
 }
 
+// Whether the sum of the unrounded weights is carried
+template <typename T, bool LSE> constexpr bool kTrueSum = LSE && std::is_same_v<T, BF16>;
+
+// f32's weights: see tree_rows_f32_kernel.
+constexpr float kF32Move = 8.0f, kF32Unit = 0x1p-40f, kF32UnitLog2 = -40.0f;
+
+// The log-sum-exp of a row whose weights against `top` (log2 units) sum to lt; -infinity without a key
+template <typename T>
+__device__ __forceinline__ float lse_of(float top, float lt) {
+    if (lt == 0.0f) return -__builtin_inff();
+    return (top + (log2_fast(lt) - (std::is_same_v<T, F32> ? kF32UnitLog2 : 0.0f))) * kLn2;
+}
+
 // A finished row's four columns from t on: the output, or the unit's partial state.
-template <typename T, int D, int M, class W>
+template <typename T, int D, int M, bool LSE, class W>
 __device__ __forceinline__ void put_row(const TreeRun& r, const W& u, int fr, int t, f32x4 o, float top, float lt,
-                                        float vscale) {
+                                        float vscale, float tr) {
     if (u.whole()) {
         if (lt != 0.0f) o *= vscale / lt;
+        if (LSE && t == 0) r.a.lse[row_at(r, u, u.first + fr, r.a.Hq, 1)] = lse_of<T>(top, kTrueSum<T, LSE> ? tr : lt);
         Store<T>::store4(r.a.o, row_at(r, u, u.first + fr, r.a.o_stride, D) + t, {o[0], o[1], o[2], o[3]});
     } else {
         const size_t at = (size_t)u.slot() * M + fr;
         *reinterpret_cast<f32x4*>(r.parts + at * D + t) = o;
         if (t == 0) r.stats[at] = float2{top, lt};
+        if (kTrueSum<T, LSE> && t == 0) r.sums[at] = tr;
     }
 }
 
@@ -458,8 +477,8 @@ __device__ __forceinline__ float quad_sum(float x) {
 //
 // A block's scores, in log2 units and -inf where the row does not see the key: moves the reference
 // where the top one lies more than `limit` above it and turns the scores into weights, a power of two (`unit`) at the reference.
-template <int NDB>
-__device__ __forceinline__ void weigh(float (&x)[8], f32x8& p, f32x4 (&U)[NDB], float& R, float& l, float limit, float unit = 1.0f) {
+template <bool TR, int NDB>
+__device__ __forceinline__ void weigh(float (&x)[8], f32x8& p, f32x4 (&U)[NDB], float& R, float& l, float& tr, float limit, float unit = 1.0f) {
     const float ninf = -__builtin_inff();
     float top = x[0];
 #pragma unroll
@@ -470,25 +489,28 @@ __device__ __forceinline__ void weigh(float (&x)[8], f32x8& p, f32x4 (&U)[NDB], 
         const float f = move ? exp2_fast(R - top) : 1.0f;       // 0 for a row without keys
         R = move ? top : R;
         l *= f;
+        if (TR) tr *= f;
 #pragma unroll
         for (int i = 0; i < NDB; ++i) U[i] *= f;
     }
     const float ref = R == ninf ? 0.0f : R;
 #pragma unroll
     for (int e = 0; e < 8; ++e) p[e] = exp2_fast(x[e] - ref) * unit;
+    if (TR) tr += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
 }
 
 // Joins the four wavefronts' states of a piece whose keys they have shared out: row tiles of 16 NR rows.
 // BY16: U[i] of lane (q, col) is columns 16 i + 4 q .. + 3, else 64 (i / 4) + 16 q + 4 (i % 4) .. + 3.
-template <typename T, int D, int NR, bool BY16, class Wk>
+template <typename T, int D, int NR, bool BY16, bool LSE, class Wk>
 __device__ __forceinline__ void finish_rows(const TreeRun& r, const Wk& u, const f32x4 (&U)[NR][D / 16],
-                                            const float (&R)[NR], const float (&l)[NR], float* fold, float vscale) {
+                                            const float (&R)[NR], const float (&l)[NR], const float (&tr)[NR], float* fold, float vscale) {
     constexpr int W = kTreeWaves, FROW = D + 4, NDB = D / 16;
-    __shared__ float fold_r[W][16], fold_l[W][16];
+    constexpr bool TR = kTrueSum<T, LSE>;
+    __shared__ float fold_r[W][16], fold_l[W][16], fold_t[TR ? W : 1][16];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, col = lane & 15, q = lane >> 4;
 #pragma unroll
     for (int k = 0; k < NR; ++k) {
-        const float lk = quad_sum(l[k]);
+        const float lk = quad_sum(l[k]), tk = TR ? quad_sum(tr[k]) : 0.0f;
         __syncthreads();                                 // stages are dead, `fold` is their memory
 #pragma unroll
         for (int i = 0; i < NDB; ++i)
@@ -497,6 +519,7 @@ __device__ __forceinline__ void finish_rows(const TreeRun& r, const Wk& u, const
         if (q == 0) {
             fold_r[wave][col] = R[k];
             fold_l[wave][col] = lk;
+            if (TR) fold_t[TR ? wave : 0][col] = tk;
         }
         __syncthreads();
         for (int idx = tid; idx < min(u.nrows - 16 * k, 16) * (D / 4); idx += W * kWave) {
@@ -505,7 +528,7 @@ __device__ __forceinline__ void finish_rows(const TreeRun& r, const Wk& u, const
             float top = fold_r[0][fr];
 #pragma unroll
             for (int w = 1; w < W; ++w) top = fmaxf(top, fold_r[w][fr]);
-            float lt = 0.0f;
+            float lt = 0.0f, tt = 0.0f;
             f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
             for (int w = 0; w < W; ++w) {
@@ -514,10 +537,11 @@ __device__ __forceinline__ void finish_rows(const TreeRun& r, const Wk& u, const
                 const float f = none ? 0.0f : exp2_fast(fold_r[w][fr] - top);
                 const f32x4 x = *reinterpret_cast<const f32x4*>(&fold[(w * 16 + fr) * FROW + t]);
                 lt = fmaf(f, fold_l[w][fr], lt);
+                if (TR) tt = fmaf(f, fold_t[TR ? w : 0][fr], tt);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) o[e] = fmaf(f, none ? 0.0f : x[e], o[e]);
             }
-            put_row<T, D, 16 * NR>(r, u, 16 * k + fr, t, o, top, lt, vscale);
+            put_row<T, D, 16 * NR, LSE>(r, u, 16 * k + fr, t, o, top, lt, vscale, tt);
         }
     }
     if (u.blk0 == 0 && !u.whole() && tid == 0) u.note_split(r);
@@ -633,7 +657,7 @@ __device__ __forceinline__ int lane_now() {
 // d = 64, that is half as much, and three workgroups' registers fit.
 constexpr int rows_per_cu(int D, bool FP8, int NR) { return (D == 64 || FP8) && NR == 1 ? 3 : 2; }
 
-template <typename T, int D, bool FP8, int NR>
+template <typename T, int D, bool FP8, int NR, bool LSE>
 __global__ __launch_bounds__(kTreeWaves * kWave, rows_per_cu(D, FP8, NR)) void tree_rows_kernel(TreeRun r) {
     constexpr int W = kTreeWaves;
     constexpr int NKK = D / 32;
@@ -731,11 +755,12 @@ __global__ __launch_bounds__(kTreeWaves * kWave, rows_per_cu(D, FP8, NR)) void t
         };
 
         f32x4 U[NR][NDB];
-        float R[NR], l[NR];
+        float R[NR], l[NR], tr[NR];
 #pragma unroll
         for (int k = 0; k < NR; ++k) {
             R[k] = ninf;
             l[k] = 0.0f;
+            tr[k] = 0.0f;
 #pragma unroll
             for (int i = 0; i < NDB; ++i) U[k][i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
         }
@@ -803,7 +828,7 @@ __global__ __launch_bounds__(kTreeWaves * kWave, rows_per_cu(D, FP8, NR)) void t
                     if (masked) x[e] = if_seen(bits[k] >> (4 * q), 16 * (e >> 2) + (e & 3), x[e]);
                 }
                 f32x8 pv;
-                weigh(x, pv, U[k], R[k], l[k], LazyLimit<T>::kMoveLog2);
+                weigh<kTrueSum<T, LSE>>(x, pv, U[k], R[k], l[k], tr[k], LazyLimit<T>::kMoveLog2);
                 bfrag[k] = Mma<T>::pack8(pv);
                 f32x4 ps = {0.0f, 0.0f, 0.0f, 0.0f};
                 Mma<T>::sum8(pv, bfrag[k], ps);
@@ -856,7 +881,7 @@ __global__ __launch_bounds__(kTreeWaves * kWave, rows_per_cu(D, FP8, NR)) void t
             n1 = m1;
         }
         const TreeRun end_r = args_now();
-        finish_rows<T, D, NR, true>(end_r, u, U, R, l, reinterpret_cast<float*>(lds), FP8 ? end_r.c.vscale : 1.0f);
+        finish_rows<T, D, NR, true, LSE>(end_r, u, U, R, l, tr, reinterpret_cast<float*>(lds), FP8 ? end_r.c.vscale : 1.0f);
     } while (u.next(args_now()));
 }
 
@@ -1007,7 +1032,7 @@ template <typename T, int D, bool ONCE> struct TileLoader<T, D, true, ONCE> {
 // The scores (acc, overwritten) of NB 32-key blocks of a row: the reference moves to their top score where that lies more
 // than kMoveLog2 above it, as in top_first_pack() of flashd_rows.h, looked at once for all of them; keys that the
 // row does not see are -inf and scale is positive.
-template <typename T, int NB, int NDB>
+template <typename T, bool TR, int NB, int NDB>
 __device__ __forceinline__ void weigh_blocks(f32x16 (&acc)[NB], u32x4 (&bfrag)[2 * NB], RowState& st, f32x16 (&U)[NDB],
                                              float scale) {
     const float ninf = -__builtin_inff();
@@ -1025,6 +1050,7 @@ __device__ __forceinline__ void weigh_blocks(f32x16 (&acc)[NB], u32x4 (&bfrag)[2
         const float f = move ? exp2_fast(st.R - t) : 1.0f;       // 0 for a row without keys
         st.R = move ? t : st.R;
         st.l *= f;
+        if (TR) st.ltrue *= f;
 #pragma unroll
         for (int i = 0; i < NDB; ++i)
 #pragma unroll
@@ -1039,11 +1065,12 @@ __device__ __forceinline__ void weigh_blocks(f32x16 (&acc)[NB], u32x4 (&bfrag)[2
         for (int e = 0; e < 8; ++e) p[e] = exp2_fast(fmaf(acc[g >> 1][8 * (g & 1) + e], scale, -ref));
         bfrag[g] = Mma<T>::pack8(p);
         Mma<T>::sum8(p, bfrag[g], ps);
+        if (TR) st.ltrue += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
     }
     st.l += (ps[0] + ps[1]) + (ps[2] + ps[3]);
 }
 
-template <typename T, int D, bool FP8, int RW>
+template <typename T, int D, bool FP8, int RW, bool LSE>
 __global__ __launch_bounds__(kTreeWaves * kWave, 2) void tree_tile_kernel(TreeRun r) {
     using C = TileCfg<D>;
     constexpr int KW = kTreeWaves / RW;
@@ -1061,8 +1088,9 @@ __global__ __launch_bounds__(kTreeWaves * kWave, 2) void tree_tile_kernel(TreeRu
     uint16_t* const vlds = lds + (FP8 ? 1 : 3) * kTile;
     uint16_t* const raw = lds + 2 * kTile;
     static_assert(!FP8 || 4 * TileLoader<T, D, true, RW == 2>::kRaw == kTile * 2, "a tile's bytes");
-    float (*fold_r)[32] = reinterpret_cast<float (*)[32]>(lds + 4 * kTile), (*fold_l)[32] = fold_r + kTreeWaves;
-    static_assert(kTreeWaves * 32 * D * 4 <= 4 * kTile * 2 && 2 * kTreeWaves * 32 * 4 <= kTile * 2, "the fold lies in the tiles' LDS");
+    constexpr bool TR = kTrueSum<T, LSE>;
+    float (*fold_r)[32] = reinterpret_cast<float (*)[32]>(lds + 4 * kTile), (*fold_l)[32] = fold_r + kTreeWaves, (*fold_t)[32] = fold_l + kTreeWaves;
+    static_assert(kTreeWaves * 32 * D * 4 <= 4 * kTile * 2 && 3 * kTreeWaves * 32 * 4 <= kTile * 2, "the fold lies in the tiles' LDS");
 
     (void)r;                                    // read through args_now()
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -1273,7 +1301,7 @@ __global__ __launch_bounds__(kTreeWaves * kWave, 2) void tree_tile_kernel(TreeRu
                     }
                 }
                 u32x4 bfrag[2 * NB];
-                weigh_blocks<T, NB, NDB>(acc, bfrag, st, U, scale);
+                weigh_blocks<T, TR, NB, NDB>(acc, bfrag, st, U, scale);
                 bool apart = false;
                 if (masked) {
                     // (operands are read anew here, a few at a time: the registers are taken)
@@ -1326,7 +1354,7 @@ __global__ __launch_bounds__(kTreeWaves * kWave, 2) void tree_tile_kernel(TreeRu
         __syncthreads();
 
         // ---- rows through LDS; with KW = 2 the two states of a row are joined.  Chunk t of row c lies at t ^ c.
-        const float l = pair_sum(st.l);
+        const float l = pair_sum(st.l), tr = TR ? pair_sum(st.ltrue) : 0.0f;
         float* fold = reinterpret_cast<float*>(lds);
         const int elane = lane_now(), ecol = elane & 31, tid = 64 * wave + elane;
         const TreeRun end_r = args_now();
@@ -1339,6 +1367,7 @@ __global__ __launch_bounds__(kTreeWaves * kWave, 2) void tree_tile_kernel(TreeRu
         if (elane < 32) {
             fold_r[wave][ecol] = st.R;
             fold_l[wave][ecol] = l;
+            if (TR) fold_t[wave][ecol] = tr;
         }
         __syncthreads();
         for (int idx = tid; idx < u.nrows * CH; idx += kTreeWaves * kWave) {
@@ -1347,7 +1376,7 @@ __global__ __launch_bounds__(kTreeWaves * kWave, 2) void tree_tile_kernel(TreeRu
             float top = fold_r[w0][rc];
 #pragma unroll
             for (int k = 1; k < KW; ++k) top = fmaxf(top, fold_r[w0 + RW * k][rc]);
-            float lt = 0.0f;
+            float lt = 0.0f, tt = 0.0f;
             f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
             for (int k = 0; k < KW; ++k) {
@@ -1356,10 +1385,11 @@ __global__ __launch_bounds__(kTreeWaves * kWave, 2) void tree_tile_kernel(TreeRu
                 const float f = none ? 0.0f : exp2_fast(fold_r[w][rc] - top);
                 const f32x4 x = *reinterpret_cast<const f32x4*>(&fold[((w * 32 + rc) * CH + (ch ^ (rc & (CH - 1)))) * 4]);
                 lt = fmaf(f, fold_l[w][rc], lt);
+                if (TR) tt = fmaf(f, fold_t[w][rc], tt);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) o[e] = fmaf(f, none ? 0.0f : x[e], o[e]);
             }
-            put_row<T, D, M>(end_r, u, fr, 4 * ch, o, top, lt, FP8 ? end_r.c.vscale : 1.0f);
+            put_row<T, D, M, LSE>(end_r, u, fr, 4 * ch, o, top, lt, FP8 ? end_r.c.vscale : 1.0f, tt);
         }
         if (u.blk0 == 0 && !u.whole() && tid == 0) u.note_split(end_r);
         __syncthreads();
@@ -1383,9 +1413,8 @@ __global__ __launch_bounds__(kTreeWaves * kWave, 2) void tree_tile_kernel(TreeRu
 // applied to the weights: with the reference 40 above the top score the exponential's argument would be rounded to 2^-19 instead of
 // 2^-22, which made outputs 9e-7 from fp64 where they are 3.4 to 4.9e-7 now (2-norm, N(0, 1) inputs).  Weights below 2^-86 of the one at the
 // reference lose bits, and below 2^-109 they are zero.
-constexpr float kF32Move = 8.0f, kF32Unit = 0x1p-40f;
 constexpr int f32_per_cu(int D, int NR) { return D == 64 && NR == 1 ? 2 : 1; }
-template <int D, int NR>
+template <int D, int NR, bool LSE>
 __global__ __launch_bounds__(kTreeWaves * kWave, f32_per_cu(D, NR)) void tree_rows_f32_kernel(TreeRun r) {
     constexpr int W = kTreeWaves;
     constexpr int NDB = D / 16;
@@ -1458,11 +1487,12 @@ __global__ __launch_bounds__(kTreeWaves * kWave, f32_per_cu(D, NR)) void tree_ro
         };
 
         f32x4 U[NR][NDB];                                // [4 g + j][d]: column 64 g + 16 q + 4 d + j
-        float R[NR], l[NR];
+        float R[NR], l[NR], none[NR];
 #pragma unroll
         for (int k = 0; k < NR; ++k) {
             R[k] = ninf;
             l[k] = 0.0f;
+            none[k] = 0.0f;
 #pragma unroll
             for (int i = 0; i < NDB; ++i) U[k][i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
         }
@@ -1511,7 +1541,7 @@ __global__ __launch_bounds__(kTreeWaves * kWave, f32_per_cu(D, NR)) void tree_ro
                     x[e] = acc[k][e >> 2][e & 3] * c_log2;
                     if (masked) x[e] = if_seen(bits[k] >> (4 * q), 16 * (e >> 2) + (e & 3), x[e]);
                 }
-                weigh(x, pv[k], U[k], R[k], l[k], kF32Move, kF32Unit);
+                weigh<false>(x, pv[k], U[k], R[k], l[k], none[k], kF32Move, kF32Unit);
                 l[k] += ((pv[k][0] + pv[k][1]) + (pv[k][2] + pv[k][3])) + ((pv[k][4] + pv[k][5]) + (pv[k][6] + pv[k][7]));
             }
             bool apart = false;
@@ -1576,7 +1606,7 @@ __global__ __launch_bounds__(kTreeWaves * kWave, f32_per_cu(D, NR)) void tree_ro
 #pragma unroll
                 for (int d = 0; d < 4; ++d) U[k][4 * g + d] = x[d];
             }
-        finish_rows<F32, D, NR, false>(args_now(), u, U, R, l, fold, 1.0f);
+        finish_rows<F32, D, NR, false, LSE>(args_now(), u, U, R, l, none, fold, 1.0f);
     } while (u.next(args_now()));
 }
 
@@ -1594,19 +1624,21 @@ constexpr int kMergeShare = 12;
 constexpr int merge_groups(int M) { return M <= 32 ? 512 : M == 64 ? 1024 : 2048; }
 
 // One row's parts k0, k0 + step, ...: unnormalised sum against `top`.
-template <int D, int M>
+template <int D, int M, bool TR>
 __device__ __forceinline__ f32x4 merge_parts(const TreeRun& r, int w, int parts, int fr, int t, int k0, int step,
-                                             float& top, float& lt) {
+                                             float& top, float& lt, float& tr) {
     constexpr int AHEAD = 4;             // parts read together
     f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
     for (int k = k0; k < parts; k += AHEAD * step) {
         float2 st[AHEAD];
+        float ts[AHEAD];
         f32x4 u[AHEAD];
 #pragma unroll
         for (int i = 0; i < AHEAD; ++i) {
             const int part = min(k + i * step, parts - 1);
             const size_t at = (size_t)(2 * (w + part) + (part == 0 ? 1 : 0)) * M + fr;
             st[i] = r.stats[at];
+            ts[i] = TR ? r.sums[at] : 0.0f;
             u[i] = *reinterpret_cast<const f32x4*>(r.parts + at * D + t);
         }
 #pragma unroll
@@ -1615,6 +1647,7 @@ __device__ __forceinline__ f32x4 merge_parts(const TreeRun& r, int w, int parts,
             const float now = fmaxf(top, st[i].x);
             const float f0 = top == -__builtin_inff() ? 0.0f : exp2_fast(top - now), f1 = exp2_fast(st[i].x - now);
             lt = fmaf(lt, f0, st[i].y * f1);
+            if (TR) tr = fmaf(tr, f0, ts[i] * f1);
 #pragma unroll
             for (int e = 0; e < 4; ++e) o[e] = fmaf(o[e], f0, u[i][e] * f1);
             top = now;
@@ -1623,13 +1656,15 @@ __device__ __forceinline__ f32x4 merge_parts(const TreeRun& r, int w, int parts,
     return o;
 }
 
-template <typename T, int D, int M>
+template <typename T, int D, int M, bool LSE>
 __global__ __launch_bounds__(256, 4) void merge_tree_kernel(TreeRun r, float vscale) {
+    constexpr bool TR = kTrueSum<T, LSE>;
     constexpr int LPR = D / 4;
     constexpr int NG = 256 / LPR;
     constexpr int EACH = kTreeMostGroups / 256;
     __shared__ __align__(16) float sum[NG][D];
     __shared__ float2 part_stat[NG];
+    __shared__ float part_true[TR ? NG : 1];
     __shared__ int next[sizeof(TreeSplit) / 4];
     __shared__ int next_item;
     __shared__ int wave_sum[EACH][kTreeWaves];
@@ -1681,20 +1716,23 @@ __global__ __launch_bounds__(256, 4) void merge_tree_kernel(TreeRun r, float vsc
         TreeSplit sp;
         __builtin_memcpy(&sp, next, sizeof(sp));
         const int w = uniform(sp.w), parts = uniform(sp.parts), of = uniform(next_item);
-        float top = ninf, lt = 0.0f;
+        float top = ninf, lt = 0.0f, tr = 0.0f;
         f32x4 o;
         int fr;
         if (parts > kMergeShare) {
             fr = of;
-            o = merge_parts<D, M>(r, w, parts, fr, t, g, NG, top, lt);
+            o = merge_parts<D, M, TR>(r, w, parts, fr, t, g, NG, top, lt, tr);
             *reinterpret_cast<f32x4*>(&sum[g][t]) = o;
             if (t == 0) part_stat[g] = float2{top, lt};
+            if (TR && t == 0) part_true[TR ? g : 0] = tr;
             __syncthreads();
             if (g != 0) continue;
             float all = ninf;
 #pragma unroll
             for (int k = 0; k < NG; ++k) all = fmaxf(all, part_stat[k].x);
             lt = 0.0f;
+            tr = 0.0f;
+            top = all;
             o = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
             for (int k = 0; k < NG; ++k) {
@@ -1702,17 +1740,19 @@ __global__ __launch_bounds__(256, 4) void merge_tree_kernel(TreeRun r, float vsc
                 const float f = st.y == 0.0f ? 0.0f : exp2_fast(st.x - all);
                 const f32x4 u = *reinterpret_cast<const f32x4*>(&sum[k][t]);
                 lt = fmaf(f, st.y, lt);
+                if (TR) tr = fmaf(f, part_true[TR ? k : 0], tr);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) o[e] = fmaf(f, u[e], o[e]);
             }
         } else {
             fr = of * NG + g;
             if (fr >= sp.rows) continue;
-            o = merge_parts<D, M>(r, w, parts, fr, t, 0, 1, top, lt);
+            o = merge_parts<D, M, TR>(r, w, parts, fr, t, 0, 1, top, lt, tr);
         }
         if (lt != 0.0f) o *= vscale / lt;
         const int rw = sp.first + fr;
         const int tk = (int)fast_div((uint32_t)rw, r.group);
+        if (LSE && t == 0) r.a.lse[(size_t)(sp.row0 + tk) * r.a.Hq + sp.h * G + rw - tk * G] = lse_of<T>(top, TR ? tr : lt);
         Store<T>::store4(r.a.o, (size_t)(sp.row0 + tk) * r.a.o_stride + (size_t)(sp.h * G + rw - tk * G) * D + t,
                          {o[0], o[1], o[2], o[3]});
     }
@@ -1734,43 +1774,48 @@ static int tree_rows(int Hq, int Hkv, int max_q, int dtype, bool fp8) {
 
 size_t attn_tree_workspace(int Hq, int Hkv, int max_q, int d, int dtype) {
     const int rows = tree_rows(Hq, Hkv, max_q, dtype, false);
-    return (size_t)2 * kTreeMostGroups * rows * (d + 2) * sizeof(float) + kTreeMostGroups * sizeof(TreeSplit);
+    return (size_t)2 * kTreeMostGroups * rows * (d + 3) * sizeof(float) + kTreeMostGroups * sizeof(TreeSplit);
 }
 
-template <typename T, int D, int M>
+template <typename T, int D, int M, bool LSE>
 static hipError_t launch_tree_m(TreeRun& r, hipStream_t st) {
     const dim3 block(kTreeWaves * kWave);
     r.stats = reinterpret_cast<float2*>(r.parts + (size_t)2 * kTreeMostGroups * M * D);
     r.splits = reinterpret_cast<TreeSplit*>(r.stats + (size_t)2 * kTreeMostGroups * M);
+    r.sums = reinterpret_cast<float*>(r.splits + kTreeMostGroups);
     auto launch = [&](auto* kernel, int groups) {
         r.groups = groups;
         hipLaunchKernelGGL(kernel, dim3((unsigned)groups), block, 0, st, r);
     };
-    if constexpr (std::is_same_v<T, F32>) launch(tree_rows_f32_kernel<D, M / 16>, 256 * f32_per_cu(D, M / 16));
-    else if constexpr (M == 32) launch(tree_rows_kernel<T, D, true, 2>, 256 * rows_per_cu(D, true, 2));
+    if constexpr (std::is_same_v<T, F32>) launch(tree_rows_f32_kernel<D, M / 16, LSE>, 256 * f32_per_cu(D, M / 16));
+    else if constexpr (M == 32) launch(tree_rows_kernel<T, D, true, 2, LSE>, 256 * rows_per_cu(D, true, 2));
     else if constexpr (M == 16) {
-        if (r.a.fp8) launch(tree_rows_kernel<T, D, true, 1>, 256 * rows_per_cu(D, true, 1));
-        else launch(tree_rows_kernel<T, D, false, 1>, 256 * rows_per_cu(D, false, 1));
+        if (r.a.fp8) launch(tree_rows_kernel<T, D, true, 1, LSE>, 256 * rows_per_cu(D, true, 1));
+        else launch(tree_rows_kernel<T, D, false, 1, LSE>, 256 * rows_per_cu(D, false, 1));
     } else {
-        if (r.a.fp8) launch(tree_tile_kernel<T, D, true, M / 32>, 512);
-        else launch(tree_tile_kernel<T, D, false, M / 32>, 512);
+        if (r.a.fp8) launch(tree_tile_kernel<T, D, true, M / 32, LSE>, 512);
+        else launch(tree_tile_kernel<T, D, false, M / 32, LSE>, 512);
     }
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((merge_tree_kernel<T, D, M>), dim3(merge_groups(M)), block, 0, st, r,
+    hipLaunchKernelGGL((merge_tree_kernel<T, D, M, LSE>), dim3(merge_groups(M)), block, 0, st, r,
                        r.a.fp8 ? r.c.vscale : 1.0f);
     return hipGetLastError();
 }
 
-template <typename T, int D>
-static hipError_t launch_tree_t(TreeRun& r, hipStream_t st) {
+template <typename T, int D, bool LSE>
+static hipError_t launch_tree_l(TreeRun& r, hipStream_t st) {
     const int rows = tree_rows(r.a.Hq, r.c.Hkv, r.a.max_q, r.a.dtype, r.a.fp8 != 0);
     switch (rows) {
-    case 16: return launch_tree_m<T, D, 16>(r, st);
-    case 32: return launch_tree_m<T, D, 32>(r, st);
+    case 16: return launch_tree_m<T, D, 16, LSE>(r, st);
+    case 32: return launch_tree_m<T, D, 32, LSE>(r, st);
     }
     if constexpr (std::is_same_v<T, F32>) return hipErrorInvalidValue;          // tree_rows() has no more for it
-    else return rows == 64 ? launch_tree_m<T, D, 64>(r, st) : launch_tree_m<T, D, 128>(r, st);
+    else return rows == 64 ? launch_tree_m<T, D, 64, LSE>(r, st) : launch_tree_m<T, D, 128, LSE>(r, st);
+}
+template <typename T, int D>
+static hipError_t launch_tree_t(TreeRun& r, hipStream_t st) {
+    return r.a.lse != nullptr ? launch_tree_l<T, D, true>(r, st) : launch_tree_l<T, D, false>(r, st);
 }
 
 hipError_t launch_attn_tree(const Paged& c, const TreeArgs& a, hipStream_t st) {

@@ -37,7 +37,7 @@ EXPORTS = ("flashd_attn_fwd", "flashd_attn_fwd_ex", "flashd_workspace_bytes",
            "flashd_release_workspace", "flashd_cache_fork", "flashd_cache_reserve", "flashd_cache_append",
            "flashd_attn_fwd_tree", "flashd_tree_workspace_bytes", "flashd_cache_commit",
            "flashd_draft_verify", "flashd_verify_workspace_bytes", "flashd_cache_score",
-           "flashd_cache_evict", "flashd_evict_workspace_bytes")
+           "flashd_cache_evict", "flashd_evict_workspace_bytes", "flashd_attn_fwd_tree_lse")
 
 
 class Cache(ctypes.Structure):
@@ -92,6 +92,8 @@ def _load() -> ctypes.CDLL:
         fn.restype, fn.argtypes = i, args
     lib.flashd_attn_fwd_tree.restype = i
     lib.flashd_attn_fwd_tree.argtypes = [c, i, p, n, p, n, i, i, i, p, p, i, f, i, p, p, z]
+    lib.flashd_attn_fwd_tree_lse.restype = i
+    lib.flashd_attn_fwd_tree_lse.argtypes = [c, i, p, n, p, n, i, i, i, p, p, i, f, i, p, p, p, z]
     lib.flashd_tree_workspace_bytes.restype = z
     lib.flashd_tree_workspace_bytes.argtypes = [i] * 5
     lib.flashd_draft_verify.restype = i
@@ -533,13 +535,13 @@ def tree_workspace_bytes(Hq, Hkv, max_q, d, dtype) -> int:
 
 
 def attn_fwd_tree(q, kcache, vcache, o, table, lens, q_start, max_q: int, scale: float, tree=None,
-                  kscale: float = 1.0, vscale: float = 1.0, workspace=None, stream=None) -> None:
+                  kscale: float = 1.0, vscale: float = 1.0, workspace=None, stream=None, lse=None) -> None:
     """flashd_attn_fwd_tree: o [T, Hq, d] <- attention of the new tokens' queries q over one layer's
     cache.  `tree`: int64 [T, words], the new tokens of its sequence that each token sees, one bit
     each; without it token i sees tokens 0 .. i.  max_q: the most new tokens of a sequence (a hint).
     `workspace`: a contiguous tensor of at least tree_workspace_bytes(...) bytes; without it scratch
-    memory is kept per stream."""
-    if stream is None and _taken(_native.attn_fwd_tree(q, kcache, vcache, o, table, lens, q_start, max_q, scale, tree, kscale, vscale,
+    memory is kept per stream.  `lse`: float32 [T, Hq], receives the queries' log-sum-exps (flashd_attn_fwd_tree_lse)."""
+    if stream is None and lse is None and _taken(_native.attn_fwd_tree(q, kcache, vcache, o, table, lens, q_start, max_q, scale, tree, kscale, vscale,
                                                        workspace)):
         return
     c = _cache(kcache, vcache, table, lens, kscale, vscale)
@@ -555,7 +557,13 @@ def attn_fwd_tree(q, kcache, vcache, o, table, lens, q_start, max_q: int, scale:
     words = _words(tree, T, device)
     _fit(words, max_q)
     ws_ptr, ws_bytes = _workspace(workspace, device)
+    if lse is not None:
+        _floats("lse", lse, (T, Hq), device)
     if T == 0:
+        return
+    if lse is not None:
+        _enqueue(_lib.flashd_attn_fwd_tree_lse, device, stream, (c, 0, q.data_ptr(), qs, o.data_ptr(), os_, T, int(max_q), Hq,
+                 q_start.data_ptr(), _ptr(tree), words, float(scale), _DTYPE[q.dtype], lse.data_ptr()), (ws_ptr, ws_bytes))
         return
     _enqueue(_lib.flashd_attn_fwd_tree, device, stream, (c, 0, q.data_ptr(), qs, o.data_ptr(), os_, T, int(max_q), Hq,
              q_start.data_ptr(), _ptr(tree), words, float(scale), _DTYPE[q.dtype]), (ws_ptr, ws_bytes))
