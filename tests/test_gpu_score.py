@@ -112,6 +112,16 @@ def test_chunks(dtype, fp8, n):
     check(make([40, 0, 190], [n, n // 2, 2 * n], 2, 64, 32, dtype, fp8, seed=n), 8, dtype)
 
 
+@pytest.mark.parametrize("Hq,n", [(130, 3), (257, 2), (129, 1), (128, 3), (127, 2), (65, 4), (7, 40), (3, 100)])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_many_heads_to_one(Hq, n, dtype):
+    """Groups of 64 or 128 rows are of whole tokens, or of a token's heads where those are more."""
+    c = make([70, 5, 130], [n, 1, n], 1, 64, 16, dtype, seed=Hq)
+    check(c, Hq, dtype)
+    tree, seen = random_tree([n, 1, n], 2, holes=True)
+    check(c, Hq, dtype, tree=tree, seen=seen, weight=torch.arange(2 * n + 1.0))
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("words,some", [(1, [7, 33, 1, 0, 64]), (2, [70, 100, 5]), (1, [90])])
 @pytest.mark.parametrize("holes", [False, True])
