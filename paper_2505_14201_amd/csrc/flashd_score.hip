@@ -8,14 +8,8 @@
 // registers.  K is the B operand and goes from the pages to registers as it lies there; a row's w exp(-lse) is one number in
 // the exponent: 2^(c s - bias).
 //
-// By the rows of a sequence and kv head there are three ways:
-//   few   (up to 16) HBM bounds it.  Products of 16 x 16 x 32; a wavefront by itself has the queries in registers and takes 64 or 128 keys at a time, the
-//         next ones under way.
-//   mid   (one group of rows: 128, of f32 64) HBM, and products and exponentials.  32 x 32 x 16; the rows stay in LDS, a wavefront takes 32 keys
-//         at a time, the next 64 under way.
-//   long  Products and exponentials.  A workgroup keeps 256 keys while the rows go by in LDS, group by group, the next one under way; a
-//         wavefront has 64 of the keys and every other tile of rows.  (With 32 keys and all tiles LDS bounded it: an operand of 1 KB read for every
-//         product.)
+// Up to 16 rows to a sequence and kv head HBM bounds it (score_few_kernel); with more the products and exponentials do as well, then alone
+// (score_many_kernel).  Both are launched where the call may have either.
 #include "flashd_common.h"
 #include "flashd_kernels.h"
 #include "flashd_mma.h"
@@ -27,6 +21,10 @@ namespace flashd {
 
 constexpr int kScoreWaves = 8, kScoreThreads = kScoreWaves * kWave;
 constexpr int kScoreGroups = 256;       // workgroups of a launch: one per compute unit, two wavefronts per SIMD
+constexpr int kFewRows = 16;            // rows of a unit that the first kernel takes
+constexpr int kOwnTiles = 16;           // tiles of 32 rows up to which a wavefront takes a unit's turn by itself; of more the workgroup shares out the tiles
+constexpr int kBiasTiles = 128;         // tiles whose rows' bias lies in LDS
+constexpr int kScoreRuns = 128;         // runs of sequences
 
 struct ScoreRun {
     Paged c;
@@ -38,29 +36,35 @@ template <typename T, int D, bool FP8> struct ScoreCfg {
     static constexpr bool F = std::is_same_v<T, F32>;
     static constexpr int ROWB = D * (F ? 4 : FP8 ? 1 : 2);       // bytes of a key
     static constexpr int QSZ = F ? 4 : 2;
-    // few: 16-key blocks of a wavefront's turn, and loads of 16 bytes per lane and block
+    static constexpr int KPITCH = ROWB + 16;                     // of a key in LDS: 16 of them fall on all banks
+    // few: 16-key blocks of a turn, and loads of 16 bytes per lane and block
     static constexpr int TURN = ROWB >= 512 ? 2 : ROWB >= 256 ? 4 : 8;
     static constexpr int FEW = 16 * TURN;
     static constexpr int NF = ROWB / 64;
-    static constexpr int KPITCH = ROWB + 16;                     // of a key of the block in LDS
-    // mid and long: keys of a workgroup's turn; loads of a lane for 32 keys, 2 lanes to 32 bytes
-    static constexpr int MANY = 32 * kScoreWaves;
+    // more: 32-key blocks of a turn, as many as there are registers for, beside those of the next turn where a wavefront takes it alone; 16-byte loads of
+    // a lane for a block; operands of a lane
+    static constexpr int LONG = F ? (D == 128 ? 1 : 2) : 4, MID = LONG > 1 ? LONG / 2 : 1;
     static constexpr int NM = ROWB / 32;
-    // long: 32-key blocks of a wavefront, and wavefronts that share out the tiles of rows (f32 has no registers for the keys of two)
-    static constexpr int KB = F ? 1 : 2;
-    // rows of a group in LDS, padded so that 16 of them fall on all banks
-    static constexpr int ROWS = F ? 64 : 128;
-    static constexpr int PITCH = D * QSZ + 16;
-    static constexpr int STEPS = D * QSZ / 32;                   // operands of a lane
-    static constexpr int QL = ROWS * D * QSZ / (16 * kScoreThreads);
-    // Tokens of a group: with all their heads, or one where that is more than a group's rows, or where offsets within the group would pass 32 bits
+    static constexpr int STEPS = D * QSZ / 32;
+    // a tile of 32 rows in LDS, and how many of them a wavefront has.  Rows lie one behind the other as copies of 1 KB leave them, the 16-byte chunk c of row r
+    // at c ^ swz(r), so that 16 rows' chunks fall on all banks.
+    static constexpr int QROW = D * QSZ, CH = QROW / 16;
+    static constexpr int TILE = 32 * QROW;
+    static constexpr int SLOTS = TILE > 8192 ? 1 : 2;
+    static __device__ __forceinline__ int swz(int row) { return CH == 8 ? row >> 1 & 7 : row & 15; }
+    // Tokens of a tile: with all their heads, or one where that is more than a tile's rows, or where offsets within the tile would pass 32 bits
     static __device__ __forceinline__ int tokens(const ScoreRun& r) {
         const int heads = (int)r.group.d;
-        return heads > ROWS || r.a.q_stride * QSZ * ROWS > (1ll << 30) ? 1 : ROWS / heads;
+        return heads > 32 || r.a.q_stride * QSZ * 32 > (1ll << 30) ? 1 : 32 / heads;
+    }
+    static __device__ __forceinline__ int tiles(const ScoreRun& r, int n) {
+        const int heads = (int)r.group.d, of = tokens(r);
+        return heads > 32 ? n * ((heads + 31) / 32) : (n + of - 1) / of;
     }
     // Byte of a row at which a lane's operand s begins, in the order in which the loads of K bring the elements: of fp8 16 at a time
     static __device__ __forceinline__ int few_at(int s, int q) { return FP8 ? 128 * (s >> 1) + 32 * q + 16 * (s & 1) : 64 * s + 16 * q; }
-    static __device__ __forceinline__ int many_at(int s, int hh) { return FP8 ? 64 * (s >> 1) + 32 * hh + 16 * (s & 1) : 32 * s + 16 * hh; }
+    static constexpr int many_at(int s) { return FP8 ? 64 * (s >> 1) + 16 * (s & 1) : 32 * s; }
+    static constexpr int kHalf = FP8 ? 32 : 16;                  // and what the upper half of the lanes adds
 };
 
 template <typename T> struct Few;
@@ -91,12 +95,6 @@ __device__ __forceinline__ void have_loads() {
     __builtin_amdgcn_s_waitcnt(0x0f70);
     asm volatile("" ::: "memory");
 }
-// The same for these registers alone
-template <int N> __device__ __forceinline__ void have(u32x4 (&x)[N]) {
-#pragma unroll
-    for (int i = 0; i < N; ++i) asm volatile("" : "+v"(x[i]));
-}
-
 // a / b rounded up, of whole numbers 0 <= a < 2^52 and b > 0, by a division of doubles (the rounded quotient's ceiling can be one off)
 __device__ __forceinline__ long long ceil_div(long long a, long long b) {
     long long q = (long long)((double)a / (double)b);
@@ -104,20 +102,24 @@ __device__ __forceinline__ long long ceil_div(long long a, long long b) {
     return (q - 1) * b >= a ? q - 1 : q;
 }
 
+// The workgroup's place: neighbours in the order of the turns, which read the same queries, are on one XCD.
+__device__ __forceinline__ int place_of_group() { return ((int)blockIdx.x & 7) * (kScoreGroups / 8) + ((int)blockIdx.x >> 3); }
+
 // ---- the work of a launch -----------------------------------------------------------------------
 //
-// Units are (sequence, kv head), cut into turns of keys.  Turns of few rows lie in a row of which each workgroup has a stretch, those of mid ones in
-// another.  Turns of long units take many times what
-// it takes to bring their keys: turn i of all of them is that of workgroup i modulo their number, every other time backwards, in the order of falling
-// rows (up to 512 sequences), so that none has much more than another.
+// Units are (sequence, kv head), cut into turns of keys.  Turns of few rows lie in a row of which each workgroup has a stretch, those of more rows in
+// another.  Of a stretch the wavefronts take turn after turn as they come to it: of the two on a SIMD the older one is served first, and with stretches
+// of their own the older ones ended after 66 us, the younger after 112 (a token for each of 64 sequences of 500 to 8192 keys).
+// Units of many rows, whose turns take long, are the workgroups' in turn: turn i of all of them is that of workgroup i modulo their number, every other time
+// backwards, in the order of falling rows (up to 128 sequences), so that none has much more than another.
 enum ScoreKind { kFew, kMid, kLong };
 
 struct ScoreScratch {
-    long long first[3][kScoreThreads];   // of each thread's run of sequences: turns of all runs before
-    long long sum[3][kScoreWaves];
-    int rows[kScoreThreads];
-    int order[kScoreThreads];            // long ones: sequences by falling rows
-    int taken;                           // turns of the workgroup's stretch of few rows
+    long long first[3][kScoreRuns];      // of each thread's run of sequences: turns of all runs before
+    long long sum[3][kScoreRuns / kWave];
+    int rows[kScoreRuns];
+    int order[kScoreRuns];               // long ones: sequences by falling rows
+    int taken;                           // turns of the workgroup's stretch
 };
 
 template <typename C>
@@ -131,8 +133,8 @@ struct ScoreWalk {
         b = seq;
         s = seq_at(r.c, b);
         rows = s.n * (int)r.group.d;             // (T Hq is below 2^31)
-        kind = rows <= 16 ? kFew : rows <= C::ROWS && s.n <= C::tokens(r) ? kMid : kLong;
-        const int keys = kind == kFew ? C::FEW : C::MANY;
+        kind = rows <= kFewRows ? kFew : C::tiles(r, s.n) <= kOwnTiles ? kMid : kLong;
+        const int keys = kind == kFew ? C::FEW : 32 * (kind == kMid ? C::MID : C::LONG);
         chunks = s.n == 0 ? 0 : (s.len + s.n + keys - 1) / keys;
     }
     __device__ __forceinline__ long long turns(const ScoreRun& r, int of) const { return of == kind ? (long long)chunks * r.c.Hkv : 0; }
@@ -148,12 +150,13 @@ struct ScoreWalk {
         at = same(at);
         end = same(end);
     }
-    static __device__ __forceinline__ int each(const ScoreRun& r) { return (r.c.B + kScoreThreads - 1) / kScoreThreads; }
+    static __device__ __forceinline__ int each(const ScoreRun& r) { return (r.c.B + kScoreRuns - 1) / kScoreRuns; }
 
-    // Every thread takes a run of sequences, whose turns are then summed over the threads.
+    // Every thread takes a run of sequences, whose turns are then summed over the threads.  FROM, TO: the kinds that are asked for.
+    template <int FROM, int TO>
     static __device__ __forceinline__ void begin(const ScoreRun& r, ScoreScratch* sh, long long (&total)[3]) {
         const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-        const int n = each(r), b0 = tid * n, b1 = min(b0 + n, r.c.B);
+        const int n = each(r), b0 = tid * n, b1 = tid < kScoreRuns ? min(b0 + n, r.c.B) : 0;
         if (tid == 0) sh->taken = 0;
         long long mine[3] = {0, 0, 0};
         ScoreWalk any;
@@ -165,41 +168,45 @@ struct ScoreWalk {
 #pragma unroll
             for (int k = 0; k < 3; ++k) mine[k] += any.turns(r, k);
         }
-        if (n == 1 && __syncthreads_or(mine[kLong] != 0)) {
+        if (TO == kLong && n == 1 && __syncthreads_or(mine[kLong] != 0)) {
             const int rows = any.kind == kLong ? any.rows : -1;
-            sh->rows[tid] = rows;
-            sh->first[kLong][tid] = mine[kLong];
+            if (tid < kScoreRuns) {
+                sh->rows[tid] = rows;
+                sh->first[kLong][tid] = mine[kLong];
+            }
             __syncthreads();
-            int rank = 0;
-            for (int i = 0; i < kScoreThreads; ++i) rank += sh->rows[i] > rows || (sh->rows[i] == rows && i < tid);
-            sh->order[rank] = tid;
+            if (tid < kScoreRuns) {
+                int rank = 0;
+                for (int i = 0; i < kScoreRuns; ++i) rank += sh->rows[i] > rows || (sh->rows[i] == rows && i < tid);
+                sh->order[rank] = tid;
+            }
             __syncthreads();
-            mine[kLong] = sh->first[kLong][sh->order[tid]];
+            if (tid < kScoreRuns) mine[kLong] = sh->first[kLong][sh->order[tid]];
             __syncthreads();
         }
         long long in[3];
 #pragma unroll
-        for (int k = 0; k < 3; ++k) {
+        for (int k = FROM; k <= TO; ++k) {
             in[k] = mine[k];
 #pragma unroll
             for (int d = 1; d < 64; d <<= 1) {
                 const long long y = __shfl_up(in[k], d);
                 if (lane >= d) in[k] += y;
             }
-            if (lane == 63) sh->sum[k][wave] = in[k];
+            if (lane == 63 && wave < kScoreRuns / kWave) sh->sum[k][wave] = in[k];
         }
         __syncthreads();
 #pragma unroll
-        for (int k = 0; k < 3; ++k) {
+        for (int k = FROM; k <= TO; ++k) {
             long long before = in[k] - mine[k];
             total[k] = 0;
 #pragma unroll
-            for (int i = 0; i < kScoreWaves; ++i) {
+            for (int i = 0; i < kScoreRuns / kWave; ++i) {
                 before += i < wave ? sh->sum[k][i] : 0;
                 total[k] += sh->sum[k][i];
             }
             total[k] = same(total[k]);
-            sh->first[k][tid] = before;
+            if (tid < kScoreRuns) sh->first[k][tid] = before;
         }
         __syncthreads();
     }
@@ -209,7 +216,7 @@ struct ScoreWalk {
         const int lane = threadIdx.x & 63;
         int run = -1;
 #pragma unroll
-        for (int i = 0; i < kScoreThreads; i += kWave) {
+        for (int i = 0; i < kScoreRuns; i += kWave) {
             const uint64_t before = __builtin_amdgcn_ballot_w64(sh->first[of][i + lane] <= x);
             if (before != 0) run = i + 63 - __builtin_clzll(before);
         }
@@ -236,8 +243,6 @@ struct ScoreWalk {
         end = same(to);
         return true;
     }
-    // Turns of this unit from the present one on that are the stretch's
-    __device__ __forceinline__ int here() const { return same(end - at < chunks - chunk ? (int)(end - at) : chunks - chunk); }
     // On to turn x (not before the present one) of the same list; false: not in the stretch
     __device__ __forceinline__ bool advance_to(const ScoreRun& r, long long x) {
         if (x >= end) return false;
@@ -251,20 +256,6 @@ struct ScoreWalk {
                 while (turns(r, of) == 0);
                 h = 0;
             }
-        }
-        settle();
-        return true;
-    }
-    // past n turns of this unit
-    __device__ __forceinline__ bool advance(const ScoreRun& r, int n) {
-        at += n;
-        if (at >= end) return false;
-        chunk = 0;
-        if (++h == r.c.Hkv) {
-            const int of = kind;
-            do enter(r, b + 1);                  // (there is one: the stretch has turns left)
-            while (turns(r, of) == 0);
-            h = 0;
         }
         settle();
         return true;
@@ -309,9 +300,6 @@ __device__ __forceinline__ float if_bit(uint32_t bits, int i, float x) {
 //
 // Lane (q, c) = (lane / 16, lane % 16): of S = Q K^T it holds key c and the rows 4 q .. 4 q + 3.
 // Keys go through LDS, so that a load brings 1 KB as it lies in memory: with 64 bytes of each of 16 keys, as the operand has them, HBM gave 5.0 TB/s.
-//
-// The wavefronts of a workgroup take the turns of its stretch one by one as they come to them: of the two on a SIMD the older one is served first, and with stretches
-// of their own the older ones ended after 66 us, the younger after 112 (a token for each of 64 sequences of 500 to 8192 keys).
 template <typename T, int D, bool FP8, class W>
 __device__ __forceinline__ void few_rows(const ScoreRun& r, W u, int* taken, char* stage, int lane) {
     using C = ScoreCfg<T, D, FP8>;
@@ -436,120 +424,216 @@ __device__ __forceinline__ void few_rows(const ScoreRun& r, W u, int* taken, cha
     }
 }
 
-// ---- mid and long --------------------------------------------------------------------------------
+template <typename T, int D, bool FP8>
+__global__ __launch_bounds__(kScoreThreads, 2) void score_few_kernel(ScoreRun r) {
+    using C = ScoreCfg<T, D, FP8>;
+    using W = ScoreWalk<C>;
+    __shared__ __align__(16) char keys[kScoreWaves][16 * C::KPITCH];
+    __shared__ ScoreScratch scratch;
+    const int lane = threadIdx.x & 63, wave = same((int)threadIdx.x >> 6);
+    long long total[3];
+    W::template begin<kFew, kFew>(r, &scratch, total);
+    W u;
+    if (u.start(r, &scratch, kFew, total[kFew], place_of_group(), kScoreGroups)) few_rows<T, D, FP8>(r, u, &scratch.taken, keys[wave], lane);
+}
+
+// ---- many rows -----------------------------------------------------------------------------------
 //
-// Lane (hh, c) = (lane / 32, lane % 32): of a tile of 32 rows it holds key c (of each of KB blocks) and the rows 8 y + 4 hh .. + 3, y = 0 .. 3.
-template <typename C> struct ScoreRows {
-    char q[2][C::ROWS * C::PITCH];
-    float bias[2][C::ROWS];
-    int off[2][kScoreWaves];             // some row of the group does not count
-    float sums[kScoreWaves / 2][64];     // of wavefronts that share their keys
+// Lane (hh, c) = (lane / 32, lane % 32): of a tile of 32 rows it holds key c of each of KB blocks of 32 keys, and the rows 8 y + 4 hh .. + 3, y = 0 .. 3.
+//
+// A wavefront keeps its keys' operands in registers, of 16 bits those of 64 keys, or 128 of a turn that the workgroup shares, and takes the unit's tiles of rows one after
+// the other, or every eighth one of a shared turn.  It has places of its own in LDS for two tiles, which are copied there one ahead, and so waits for nobody; the keys of
+// its next turn are read before the last tile.  The exponentials of a block run between the products of the next one.
+// Chunks of 1000 tokens after 2000 to 7000 keys, 138 GFLOP: 207 us, where rows staged by the workgroup with a barrier for each 128 of them took 251.  32 tokens after 10000
+// to 32000 keys, 202 MB: 79 us.
+template <typename C> struct ScorePlaces {
+    union {
+        char tile[kScoreWaves][C::SLOTS][C::TILE];
+        char keys[kScoreWaves][16 * C::KPITCH];          // 16 keys of a wavefront, or all of the workgroup's, on their way to the operands
+        float sums[kScoreWaves][32 * C::LONG];
+    };
+    float bias[kBiasTiles][32];          // of a wavefront's unit kOwnTiles of them
+};
+
+__device__ __forceinline__ uint32_t lds_at(const void* p) {
+    return (uint32_t)same((int)(uint32_t)(uintptr_t)(const __attribute__((address_space(3))) char*)p);
+}
+// N loads of 16 bytes per lane, at off[i] of the window, to 1 KB each of LDS from `to` on.  (The compiler does not know of copies under way, and so does not wait for them wherever LDS is
+// read.  M0 holds the target, with a wait state before the copy, and is left as it was.)  What was read of LDS before is there first.
+template <int N> struct Copies;
+template <> struct Copies<4> {
+    static __device__ __forceinline__ void start(u32x4 w, uint32_t to, const int* off) {
+        uint32_t m0;
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_mov_b32 %0, m0\n\ts_mov_b32 m0, %2\n\ts_nop 0\n\t"
+                     "buffer_load_dwordx4 %3, %1, 0 offen lds\n\ts_add_u32 m0, m0, 0x400\n\ts_nop 0\n\t"
+                     "buffer_load_dwordx4 %4, %1, 0 offen lds\n\ts_add_u32 m0, m0, 0x400\n\ts_nop 0\n\t"
+                     "buffer_load_dwordx4 %5, %1, 0 offen lds\n\ts_add_u32 m0, m0, 0x400\n\ts_nop 0\n\t"
+                     "buffer_load_dwordx4 %6, %1, 0 offen lds\n\ts_mov_b32 m0, %0"
+                     : "=&s"(m0) : "s"(w), "s"(to), "v"(off[0]), "v"(off[1]), "v"(off[2]), "v"(off[3]) : "memory", "scc");
+    }
+};
+template <> struct Copies<8> {
+    static __device__ __forceinline__ void start(u32x4 w, uint32_t to, const int* off) {
+        uint32_t m0;
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_mov_b32 %0, m0\n\ts_mov_b32 m0, %2\n\ts_nop 0\n\t"
+                     "buffer_load_dwordx4 %3, %1, 0 offen lds\n\ts_add_u32 m0, m0, 0x400\n\ts_nop 0\n\t"
+                     "buffer_load_dwordx4 %4, %1, 0 offen lds\n\ts_add_u32 m0, m0, 0x400\n\ts_nop 0\n\t"
+                     "buffer_load_dwordx4 %5, %1, 0 offen lds\n\ts_add_u32 m0, m0, 0x400\n\ts_nop 0\n\t"
+                     "buffer_load_dwordx4 %6, %1, 0 offen lds\n\ts_add_u32 m0, m0, 0x400\n\ts_nop 0\n\t"
+                     "buffer_load_dwordx4 %7, %1, 0 offen lds\n\ts_add_u32 m0, m0, 0x400\n\ts_nop 0\n\t"
+                     "buffer_load_dwordx4 %8, %1, 0 offen lds\n\ts_add_u32 m0, m0, 0x400\n\ts_nop 0\n\t"
+                     "buffer_load_dwordx4 %9, %1, 0 offen lds\n\ts_add_u32 m0, m0, 0x400\n\ts_nop 0\n\t"
+                     "buffer_load_dwordx4 %10, %1, 0 offen lds\n\ts_mov_b32 m0, %0"
+                     : "=&s"(m0)
+                     : "s"(w), "s"(to), "v"(off[0]), "v"(off[1]), "v"(off[2]), "v"(off[3]), "v"(off[4]), "v"(off[5]), "v"(off[6]), "v"(off[7])
+                     : "memory", "scc");
+    }
+};
+template <> struct Copies<16> {
+    static __device__ __forceinline__ void start(u32x4 w, uint32_t to, const int* off) {
+        Copies<8>::start(w, to, off);
+        Copies<8>::start(w, to + 8192, off + 8);
+    }
 };
 
 template <typename T, int D, bool FP8, int KB, class W> struct ManyRows {
     using C = ScoreCfg<T, D, FP8>;
-    static constexpr int NM = C::NM, STEPS = C::STEPS, ROWS = C::ROWS, PITCH = C::PITCH, QL = C::QL, CPR = D * C::QSZ / 16;
+    static constexpr int MANY = 32 * KB, NM = C::NM, STEPS = C::STEPS, COPIES = C::TILE / 1024;
     const ScoreRun& r;
     const W& u;
-    ScoreRows<C>& lds;
+    ScorePlaces<C>& lds;
     int wave, lane, keys;
-    int lead, odd;               // the wavefront's first key in a turn, and its first tile: it has every KB-th
     float c_log2;
-    const char* pool;
-    // A group: `tpg` tokens with all their heads (one token and `hpg` of them where they are more than ROWS); its row i is head i % hpg of
-    // token i / hpg.  So the lane's pieces of a group lie at fixed distances from its first token.
-    int tpg, hpg, of_token;      // of_token: groups of a token (of tpg tokens)
-    int voff[QL], brow;
+    int tpt, hpt, of_token, tiles;       // tokens and heads of a tile, tiles of a token (of tpt), of the unit
+    int off[COPIES];                     // of the lane's pieces of a tile from its first row
+    int qat;                             // the lane's first operand in a tile; operand s lies at qat ^ many_at(s)
 
-    __device__ __forceinline__ ManyRows(const ScoreRun& run, const W& unit, ScoreRows<C>& rows, int wv, int ln)
-        : r(run), u(unit), lds(rows), wave(wv), lane(ln), keys(unit.s.len + unit.s.n), lead(32 * KB * (wv / KB)), odd(wv % KB),
-          c_log2((FP8 ? run.a.scale * run.c.kscale : run.a.scale) * kLog2e), pool(run.c.k + unit.h * run.c.head_bytes) {
-        const int G = (int)r.group.d, tid = wave * kWave + lane;
-        const int64_t stride = r.a.q_stride * C::QSZ;
-        hpg = min(G, ROWS);
-        of_token = (G + ROWS - 1) / ROWS;
-        tpg = C::tokens(r);
+    __device__ __forceinline__ ManyRows(const ScoreRun& run, const W& unit, ScorePlaces<C>& places, int wv, int ln)
+        : r(run), u(unit), lds(places), wave(wv), lane(ln), keys(unit.s.len + unit.s.n), c_log2((FP8 ? run.a.scale * run.c.kscale : run.a.scale) * kLog2e) {
+        const int G = (int)r.group.d;
+        hpt = min(G, 32);
+        of_token = (G + 31) / 32;
+        tpt = C::tokens(r);
+        tiles = C::tiles(r, u.s.n);
 #pragma unroll
-        for (int i = 0; i < QL; ++i) {
-            const int at = i * kScoreThreads + tid, row = at / CPR, token = row / hpg;
-            // (rows behind the group's last lie behind its window)
-            voff[i] = token < tpg ? (int)(token * stride) + (row - token * hpg) * (D * C::QSZ) + 16 * (at % CPR) : 0x7ffffff0;
+        for (int i = 0; i < COPIES; ++i) {
+            const int row = i * (1024 / C::QROW) + lane / C::CH, token = row / hpt;
+            // (rows behind the tile's last lie behind its window)
+            off[i] = token < tpt ? (int)(token * r.a.q_stride * C::QSZ) + (row - token * hpt) * C::QROW + 16 * (lane % C::CH ^ C::swz(row)) : 0x7ffffff0;
         }
-        brow = tid / hpg;
+        qat = (lane & 31) * C::QROW + (16 * C::swz(lane & 31) ^ C::kHalf * (lane >> 5));
     }
-    __device__ __forceinline__ int count() const { return (u.s.n + tpg - 1) / tpg * of_token; }
-    __device__ __forceinline__ int token0(int g) const { return of_token > 1 ? g / of_token : g * tpg; }
-    __device__ __forceinline__ int head0(int g) const { return of_token > 1 ? g % of_token * ROWS : 0; }
-    __device__ __forceinline__ int rows_in(int g) const { return min(tpg, u.s.n - token0(g)) * min(hpg, (int)r.group.d - head0(g)); }
+    __device__ __forceinline__ int token0(int t) const { return of_token > 1 ? t / of_token : t * tpt; }
+    __device__ __forceinline__ int head0(int t) const { return of_token > 1 ? t % of_token * 32 : 0; }
 
-    // Rows on their way to LDS, and what their bias is made of (-infinity: no row)
-    __device__ __forceinline__ void load_rows(int g, u32x4 (&x)[QL], float& l, float& wt) const {
-        const int tid = wave * kWave + lane, G = (int)r.group.d, t0 = token0(g), h0 = head0(g), tokens = min(tpg, u.s.n - t0);
-        const int64_t stride = r.a.q_stride * C::QSZ;
-        const char* from = static_cast<const char*>(r.a.q) + (u.s.row0 + t0) * stride + (int64_t)(u.h * G + h0) * (D * C::QSZ);
-        const auto w = window(from, (int)((tokens - 1) * stride) + min(hpg, G - h0) * (D * C::QSZ));
-#pragma unroll
-        for (int i = 0; i < QL; ++i) x[i] = kv_load<0>(w, voff[i]);
-        const int head = h0 + tid - brow * hpg;
-        const bool row = tid < ROWS && brow < tokens && head < G;
-        l = -__builtin_inff();
-        wt = 1.0f;
-        if (row) l = r.a.lse[(size_t)(u.s.row0 + t0 + brow) * r.a.Hq + u.h * G + head];
-        if (row && r.a.weight != nullptr) wt = r.a.weight[u.s.row0 + t0 + brow];
-    }
-    __device__ __forceinline__ void store_rows(int slot, const u32x4 (&x)[QL], float l, float wt) const {
-        const int tid = wave * kWave + lane;
-#pragma unroll
-        for (int i = 0; i < QL; ++i) {
-            const int at = i * kScoreThreads + tid;
-            *reinterpret_cast<u32x4*>(&lds.q[slot][(at / CPR) * PITCH + 16 * (at % CPR)]) = x[i];
-        }
-        if (tid < ROWS) {
-            const float bs = bias(l, wt, r.a.weight != nullptr);
-            lds.bias[slot][tid] = bs;
-            const bool off = __builtin_amdgcn_ballot_w64(!(bs < __builtin_inff())) != 0;
-            if (lane == 0) lds.off[slot][wave] = off;
+    // The bias of the rows of tiles t0 .. t1 - 1, by the threads `me` of `all`
+    __device__ __forceinline__ void put_bias(float (*to)[32], int t0, int t1, int me, int all) const {
+        const int G = (int)r.group.d;
+        for (int i = me; i < 32 * (t1 - t0); i += all) {
+            const int t = t0 + i / 32, row = i % 32, token = row / hpt, head = head0(t) + row - token * hpt, at = token0(t) + token;
+            float bs = __builtin_inff();
+            if (token < tpt && at < u.s.n && head < G)
+                bs = bias(r.a.lse[(size_t)(u.s.row0 + at) * r.a.Hq + u.h * G + head], r.a.weight != nullptr ? r.a.weight[u.s.row0 + at] : 1.0f, r.a.weight != nullptr);
+            to[i / 32][row] = bs;
         }
     }
-    __device__ __forceinline__ bool off(int slot) const {
-        int any = 0;
-#pragma unroll
-        for (int i = 0; i < ROWS / kWave; ++i) any |= lds.off[slot][i];
-        return same(any) != 0;
-    }
 
-    __device__ __forceinline__ int key_of(int chunk, int kb) const { return chunk * C::MANY + lead + 32 * kb + (lane & 31); }
-    __device__ __forceinline__ int page_of(int chunk, int kb, int last) const {
-        const int j = key_of(chunk, kb);
-        return chunk < last && j < keys ? page_at(r.c, u.b, j >> r.c.page_log2) : -1;
+    // 16 keys of the turn, as they lie in memory, 1 KB to a load; zeros behind the sequence's last key and where there is no page
+    __device__ __forceinline__ int page_of(int i) const {
+        typedef const __attribute__((address_space(4))) int* table_ptr;
+        const table_ptr trow = (table_ptr)(uintptr_t)(r.c.table + (size_t)u.b * r.c.max_pages);
+        const int j = u.chunk * MANY + 16 * i;
+        const int p = j < keys ? same(trow[j >> r.c.page_log2]) : -1;
+        return (unsigned)p < (unsigned)r.c.P ? p : -1;
     }
-    __device__ __forceinline__ void fetch(int chunk, int kb, int page, u32x4 (&to)[NM]) const {
-        // (a key without a page reads the pool's first: its column of products is dropped)
-        const int j = key_of(chunk, kb) & ((1 << r.c.page_log2) - 1);
-        const char* from = pool + (page < 0 ? 0 : page * r.c.page_bytes + (int64_t)j * C::ROWB) + 16 * (lane >> 5);
+    __device__ __forceinline__ void fetch(int i, int page, u32x4 (&k)[NM / 2]) const {
+        const int j = u.chunk * MANY + 16 * i;
+        const char* at = r.c.k + u.h * r.c.head_bytes + max(page, 0) * r.c.page_bytes + (int64_t)(j & ((1 << r.c.page_log2) - 1)) * C::ROWB;
+        const auto w = window(at, page < 0 ? 0 : min(keys - j, 16) * C::ROWB);
 #pragma unroll
-        for (int i = 0; i < NM; ++i) to[i] = *reinterpret_cast<const u32x4*>(from + 32 * i);
+        for (int x = 0; x < NM / 2; ++x) k[x] = kv_load<0>(w, 1024 * x + 16 * lane);
     }
-    static __device__ __forceinline__ void widen(const u32x4 (&k)[NM], u32x4 (&kf)[STEPS]) {
+    __device__ __forceinline__ void stage(char* to, const u32x4 (&k)[NM / 2]) const {
+#pragma unroll
+        for (int i = 0; i < NM / 2; ++i) {
+            const int at = 1024 * i + 16 * lane;
+            *reinterpret_cast<u32x4*>(to + at / C::ROWB * C::KPITCH + at % C::ROWB) = k[i];
+        }
+    }
+    static __device__ __forceinline__ void widen(const u32x4 (&x)[NM], u32x4 (&kf)[STEPS]) {
 #pragma unroll
         for (int s = 0; s < STEPS; ++s) {
-            if constexpr (FP8) kf[s] = widen8<T>(k[s >> 1][2 * (s & 1)], k[s >> 1][2 * (s & 1) + 1]);
-            else kf[s] = k[s];
+            if constexpr (FP8) kf[s] = widen8<T>(x[s >> 1][2 * (s & 1)], x[s >> 1][2 * (s & 1) + 1]);
+            else kf[s] = x[s];
         }
     }
-    // tokens before it see none of the wavefront's keys (of a chain; all tokens where there are no keys)
-    __device__ __forceinline__ int first_token(int chunk) const {
-        const int j0 = chunk * C::MANY + lead;
-        return j0 >= keys ? u.s.n : r.a.tree == nullptr ? max(j0 - u.s.len, 0) : 0;
+    // whether the lane's key of block b has a page
+    __device__ __forceinline__ uint32_t has_page(int b, int p0, int p1) const {
+        return u.chunk * MANY + 32 * b + (lane & 31) < keys && ((lane & 16) != 0 ? p1 : p0) >= 0;
+    }
+    // The turn's keys through LDS to the operands, by a wavefront for itself or by the workgroup.  there: whether the lane's keys have pages, a bit for each block.
+    struct Own {
+        u32x4 k[2 * KB][NM / 2];
+        int page[2 * KB];
+    };
+    __device__ __forceinline__ void fetch(Own& x) const {
+#pragma unroll
+        for (int i = 0; i < 2 * KB; ++i) x.page[i] = page_of(i);
+#pragma unroll
+        for (int i = 0; i < 2 * KB; ++i) fetch(i, x.page[i], x.k[i]);
+    }
+    __device__ __forceinline__ void own_keys(const Own& own, u32x4 (&kf)[KB][STEPS], uint32_t& there) const {
+        char* const mine = lds.tile[wave][0];            // (its accesses reach it in their order)
+        there = 0;
+#pragma unroll
+        for (int b = 0; b < KB; ++b) {
+            there |= has_page(b, own.page[2 * b], own.page[2 * b + 1]) << b;
+            u32x4 x[NM];
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                stage(mine, own.k[2 * b + half]);
+                if ((lane >> 4 & 1) == half) {
+#pragma unroll
+                    for (int i = 0; i < NM; ++i) x[i] = *reinterpret_cast<const u32x4*>(mine + (lane & 15) * C::KPITCH + 32 * i + 16 * (lane >> 5));
+                }
+            }
+            widen(x, kf[b]);
+        }
+    }
+    __device__ __forceinline__ void shared_keys(u32x4 (&kf)[KB][STEPS], uint32_t& there) const {
+        static_assert(2 * KB <= kScoreWaves, "16 keys to a wavefront");
+        __syncthreads();                 // the turn before has been read
+        if (wave < 2 * KB) {
+            u32x4 k[NM / 2];
+            fetch(wave, page_of(wave), k);
+            stage(lds.keys[wave], k);
+        }
+        there = 0;
+#pragma unroll
+        for (int b = 0; b < KB; ++b) there |= has_page(b, page_of(2 * b), page_of(2 * b + 1)) << b;
+        __syncthreads();
+#pragma unroll
+        for (int b = 0; b < KB; ++b) {
+            u32x4 x[NM];
+#pragma unroll
+            for (int i = 0; i < NM; ++i)
+                x[i] = *reinterpret_cast<const u32x4*>(lds.keys[2 * b + (lane >> 4 & 1)] + (lane & 15) * C::KPITCH + 32 * i + 16 * (lane >> 5));
+            widen(x, kf[b]);
+        }
     }
 
-    // Operand s of tile t of the group in `slot`, and the bias of its rows 8 y + 4 hh .. + 3
-    __device__ __forceinline__ u32x4 operand(int t, int slot, int s) const {
-        return *reinterpret_cast<const u32x4*>(&lds.q[slot][(32 * t + (lane & 31)) * PITCH + C::many_at(s, lane >> 5)]);
+    // the copies of a tile of rows
+    __device__ __forceinline__ void start(int t, int slot) const {
+        const int t0 = token0(t), h0 = head0(t), G = (int)r.group.d;
+        const int64_t stride = r.a.q_stride * C::QSZ;
+        const uint64_t from = (uint64_t)(static_cast<const char*>(r.a.q) + (u.s.row0 + t0) * stride + (int64_t)(u.h * G + h0) * C::QROW);
+        const int bytes = (int)((min(tpt, u.s.n - t0) - 1) * stride) + min(hpt, G - h0) * C::QROW;
+        const u32x4 w = {(uint32_t)same((int)from), (uint32_t)same((int)(from >> 32)), (uint32_t)same(bytes), 0x00020000u};
+        Copies<COPIES>::start(w, lds_at(lds.tile[wave][slot]), off);
     }
-    __device__ __forceinline__ f32x4 bias_at(int t, int slot, int y) const {
-        return *reinterpret_cast<const f32x4*>(&lds.bias[slot][32 * t + 8 * y + 4 * (lane >> 5)]);
-    }
+    // waits until all but the last LOADS loads and copies have landed
+    template <int LOADS> static __device__ __forceinline__ void landed() { asm volatile("s_waitcnt vmcnt(%0)" :: "n"(LOADS) : "memory"); }
+
     static __device__ __forceinline__ void multiply(u32x4 q, u32x4 k, f32x16& acc) {
         if constexpr (C::F) {
             const f32x4 y = __builtin_bit_cast(f32x4, q), z = __builtin_bit_cast(f32x4, k);
@@ -559,265 +643,237 @@ template <typename T, int D, bool FP8, int KB, class W> struct ManyRows {
             acc = Mma<T>::mfma(q, k, acc);
         }
     }
-    // A tile whose products are there and whose weights are not
-    struct Pending {
-        f32x16 acc[KB];
-        f32x4 b[4];
-        bool any;
-    };
-    // The weights of the pending tile are added to part; in between, NEXT: the products of a tile (operands q).  An in-order wavefront would else wait for one
-    // product after the other, and for the exponentials in turn.  The operands that are used up are read for tile `then`.
-    template <bool NEXT>
-    __device__ __forceinline__ void step(Pending& w, u32x4 (&q)[STEPS], const u32x4 (&kf)[KB][STEPS], int then, int slot, f32x4 (&part)[KB]) const {
+    // The weights of one tile and all blocks, added to part.  The exponentials of a block run between the products of the next: an in-order wavefront would else wait
+    // for one product after the other, and for the exponentials in turn.
+    template <bool MASKED>
+    __device__ __forceinline__ void weigh_tile(const u32x4 (&q)[STEPS], const u32x4 (&kf)[KB][STEPS], const f32x4 (&b)[4], const uint32_t (&bits)[KB],
+                                               float (&sum)[KB]) const {
         constexpr int PER = 16 / STEPS;          // weights of a block to an operand
         static_assert(STEPS == 4 || STEPS == 8 || STEPS == 16, "weights are dealt out over the operands");
-        f32x16 next[KB];
+        f32x16 acc[2];
 #pragma unroll
-        for (int k = 0; k < KB; ++k)
+        for (int k = 0; k <= KB; ++k) {
+            f32x4 part = {0.0f, 0.0f, 0.0f, 0.0f};
+            if (k < KB) {
 #pragma unroll
-            for (int e = 0; e < 16; ++e) next[k][e] = 0.0f;
-#pragma unroll
-        for (int s = 0; s < STEPS; ++s) {
-#pragma unroll
-            for (int k = 0; k < KB; ++k) {
-                if (NEXT) multiply(q[s], kf[k][s], next[k]);
-                if (NEXT && k == KB - 1) q[s] = operand(then, slot, s);
-#pragma unroll
-                for (int i = s * PER; i < s * PER + PER; ++i) part[k][i & 3] += exp2_fast(fmaf(w.acc[k][i], c_log2, -w.b[i >> 2][i & 3]));
-                if (NEXT) __builtin_amdgcn_sched_barrier(0);
+                for (int e = 0; e < 16; ++e) acc[k & 1][e] = 0.0f;
             }
-        }
-        if (NEXT) {
-#pragma unroll
-            for (int k = 0; k < KB; ++k) w.acc[k] = next[k];
-        }
-    }
-    __device__ __forceinline__ void finish(Pending& w, const u32x4 (&kf)[KB][STEPS], f32x4 (&part)[KB]) const {
-        u32x4 none[STEPS];
-        if (w.any) step<false>(w, none, kf, 0, 0, part);
-        w.any = false;
-    }
-    // The wavefront's tiles of the group in `slot`, of tokens from `from` on, the last of which may stay pending.  `first`: what the tile pending so far is added to.
-    __device__ __forceinline__ void tiles(int chunk, int g, int slot, const u32x4 (&kf)[KB][STEPS], int from, const bool (&there)[KB], bool all_there,
-                                          Pending& w, f32x4 (&first)[KB], f32x4 (&part)[KB]) const {
-        const int j0 = chunk * C::MANY + lead, rel = j0 + (lane & 31) - u.s.len;
-        const int t0 = token0(g), n = (rows_in(g) + 31) / 32;
-        int t = from >= u.s.n ? n : min(max(from - t0, 0), tpg) * hpg / 32;
-        // tiles from `clear` on have only rows that count and see all of the wavefront's keys: of a chain those from the last key's token on
-        const int clear = off(slot) || !all_there ? n
-                          : j0 + 32 * KB <= u.s.len ? t
-                          : r.a.tree != nullptr || of_token > 1 ? n
-                                                                : (min(max(j0 + 32 * KB - 1 - u.s.len - t0, 0), tpg) * hpg + 31) / 32;
-        t += (t ^ odd) & (KB - 1);
-        if (t < min(clear, n) || t >= n) finish(w, kf, first);
-#pragma unroll 1
-        for (; t < min(clear, n); t += KB) {
-            const FastDiv heads = of_token > 1 ? FastDiv{(uint32_t)ROWS, 0, 0, 31} : r.group;
-#pragma unroll 1
-            for (int k = 0; k < KB; ++k) {
-                const uint32_t bits = (k == 0 ? there[0] : there[KB - 1]) ? seen_by<16>(r, u, t0, heads, 32 * t + 4 * (lane >> 5), rel + 32 * k) : 0u;
-                f32x16 acc;
-#pragma unroll
-                for (int e = 0; e < 16; ++e) acc[e] = 0.0f;
-                if (k == 0) {
-#pragma unroll
-                    for (int s = 0; s < STEPS; ++s) multiply(operand(t, slot, s), kf[0][s], acc);
-                } else {
-#pragma unroll
-                    for (int s = 0; s < STEPS; ++s) multiply(operand(t, slot, s), kf[KB - 1][s], acc);
-                }
-                f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const float b = bias_at(t, slot, i >> 2)[i & 3];
-                    const float p = exp2_fast(fmaf(acc[i], c_log2, -b));
-                    sum[i & 3] += b < __builtin_inff() ? if_bit(bits, i, p) : 0.0f;
-                }
-                if (k == 0) part[0] += sum;
-                else part[KB - 1] += sum;
-            }
-        }
-        if (t >= n) return;
-        u32x4 q[STEPS];
-#pragma unroll
-        for (int s = 0; s < STEPS; ++s) q[s] = operand(t, slot, s);
-        __builtin_amdgcn_sched_barrier(0);
-        if (w.any) {
-            step<true>(w, q, kf, min(t + KB, n - 1), slot, first);
-        } else {
-#pragma unroll
-            for (int k = 0; k < KB; ++k)
-#pragma unroll
-                for (int e = 0; e < 16; ++e) w.acc[k][e] = 0.0f;
 #pragma unroll
             for (int s = 0; s < STEPS; ++s) {
+                if (k < KB) multiply(q[s], kf[k < KB ? k : 0][s], acc[k & 1]);
+                if (k > 0) {
 #pragma unroll
-                for (int k = 0; k < KB; ++k) multiply(q[s], kf[k][s], w.acc[k]);
-                q[s] = operand(min(t + KB, n - 1), slot, s);
+                    for (int i = s * PER; i < s * PER + PER; ++i) {
+                        float p = exp2_fast(fmaf(acc[(k - 1) & 1][i], c_log2, -b[i >> 2][i & 3]));
+                        if (MASKED) p = b[i >> 2][i & 3] < __builtin_inff() ? if_bit(bits[k > 0 ? k - 1 : 0], i, p) : 0.0f;
+                        part[i & 3] = i < 4 ? p : part[i & 3] + p;
+                    }
+                }
+                __builtin_amdgcn_sched_barrier(0);
             }
-        }
-        w.any = true;
-#pragma unroll 1
-        for (;;) {
-#pragma unroll
-            for (int y = 0; y < 4; ++y) w.b[y] = bias_at(t, slot, y);
-            __builtin_amdgcn_sched_barrier(0);
-            t += KB;
-            if (t >= n) break;
-            step<true>(w, q, kf, min(t + KB, n - 1), slot, part);
-        }
-    }
-    static __device__ __forceinline__ float sum_of(f32x4 x) { return (x[0] + x[1]) + (x[2] + x[3]); }
-    static __device__ __forceinline__ void clear_sums(f32x4 (&x)[KB]) {
-#pragma unroll
-        for (int k = 0; k < KB; ++k) x[k] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    }
-    // The sum over all rows of the lane's key (half of it in either half of the wavefront is `sum`) becomes its score.
-    __device__ __forceinline__ void put(int chunk, int kb, float all) const {
-        const int j = key_of(chunk, kb);
-        if (lane < 32 && j < keys) {
-            float* to = r.a.score + ((size_t)u.b * r.c.Hkv + u.h) * r.a.score_stride + j;
-            *to = j < u.s.len && r.a.decay != 0.0f ? fmaf(*to, r.a.decay, all) : all;
+            if (k > 0) sum[k > 0 ? k - 1 : 0] += (part[0] + part[1]) + (part[2] + part[3]);
         }
     }
 
-    // n turns of a mid unit (KB 1): the rows stay, and the wavefronts go their own ways, each with its next 64 keys under way.
-    __device__ __forceinline__ void one_group(int n) const {
-        static_assert(KB == 1, "every wavefront has all tiles");
-        const int last = u.chunk + n;
-        constexpr int RING = NM > 8 ? 1 : 2;     // (of f32 with d = 128 there are registers for 32 keys)
-        u32x4 ring[RING][NM];
-        int page[RING + 1];              // of the present turn and those behind it
+    // Tiles t, t + step, ... below `end`, whose bias begins at `from` with that of tile `base`.  Before the last one, whose copies are then under way or done,
+    // `ahead` starts LOADS loads, or none and says so.
+    struct Tiles {
+        const float (*from)[32];
+        int base, clear;                 // clear: tokens from this one on see all of the keys
+        uint32_t there;
+    };
+    __device__ __forceinline__ void tile(const Tiles& x, int t, int next, int slot, const u32x4 (&kf)[KB][STEPS], float (&sum)[KB]) const {
+        u32x4 q[STEPS];
+        f32x4 b[4];
+        const char* at = lds.tile[wave][slot];
 #pragma unroll
-        for (int i = 0; i < RING; ++i) page[i] = page_of(u.chunk + i, 0, last);
-        {
-            u32x4 x[QL];
-            float l, wt;
-            load_rows(0, x, l, wt);
+        for (int s = 0; s < STEPS; ++s) q[s] = *reinterpret_cast<const u32x4*>(at + (qat ^ C::many_at(s)));
 #pragma unroll
-            for (int i = 0; i < RING; ++i) fetch(u.chunk + i, 0, page[i], ring[i]);
-            __syncthreads();             // what another unit has left in LDS has been read
-            store_rows(0, x, l, wt);
-            __syncthreads();
+        for (int y = 0; y < 4; ++y) b[y] = *reinterpret_cast<const f32x4*>(&x.from[t - x.base][8 * y + 4 * (lane >> 5)]);
+        if (next >= 0) start(next, slot);
+        // (a row that does not count has an infinite bias: one of them in 8 y + 4 hh .. + 3 makes the sum of those infinite, or NaN)
+        bool off_rows = false;
+#pragma unroll
+        for (int y = 0; y < 4; ++y) off_rows |= !((b[y][0] + b[y][1]) + (b[y][2] + b[y][3]) < __builtin_inff());
+        uint32_t bits[KB];
+#pragma unroll
+        for (int k = 0; k < KB; ++k) bits[k] = 0;
+        // A row that does not count takes nothing, e^(s - inf) = 0, but for a product that is infinite or no number; then the tile is weighed again with the masks.
+        bool masks = token0(t) < x.clear;
+        if (!masks) {
+            float before[KB];
+#pragma unroll
+            for (int k = 0; k < KB; ++k) before[k] = sum[k];
+            weigh_tile<false>(q, kf, b, bits, sum);
+            if (__builtin_amdgcn_ballot_w64(off_rows) != 0) {
+                bool odd = false;
+#pragma unroll
+                for (int k = 0; k < KB; ++k) odd |= !(sum[k] < __builtin_inff());
+                masks = __builtin_amdgcn_ballot_w64(odd) != 0;
+                if (masks) {
+#pragma unroll
+                    for (int k = 0; k < KB; ++k) sum[k] = before[k];
+                }
+            }
         }
-        page[RING] = page_of(u.chunk + RING, 0, last);
-        Pending w;
-        w.any = false;
-        f32x4 part[1];
-        clear_sums(part);
-        u32x4 kf[1][STEPS];
-        auto turn = [&](int chunk, u32x4 (&kreg)[NM]) __attribute__((always_inline)) {
-            have(kreg);
-            widen(kreg, kf[0]);
-            have(kf[0]);
-            const bool there[1] = {page[0] >= 0}, all_there = __builtin_amdgcn_ballot_w64(!there[0]) == 0;
+        if (masks) {
 #pragma unroll
-            for (int i = 0; i < RING; ++i) page[i] = page[i + 1];
-            fetch(chunk + RING, 0, page[RING], kreg);
-            page[RING] = page_of(chunk + RING + 1, 0, last);
-            // (the last tile of the keys before is pending still)
-            f32x4 before[1] = {part[0]};
-            clear_sums(part);
-            tiles(chunk, 0, 0, kf, first_token(chunk), there, all_there, w, before, part);
-            if (chunk > u.chunk) put(chunk - 1, 0, pair_sum(sum_of(before[0])));
-        };
-        for (int chunk = u.chunk; chunk < last; chunk += RING) {
-            turn(chunk, ring[0]);
-            if (RING == 2 && chunk + 1 < last) turn(chunk + 1, ring[RING - 1]);
+            for (int k = 0; k < KB; ++k)
+                bits[k] = (x.there >> k & 1u) != 0 ? seen_by<16>(r, u, token0(t), of_token > 1 ? FastDiv{32, 0, 0, 31} : r.group, 4 * (lane >> 5),
+                                                                 u.chunk * MANY + 32 * k + (lane & 31) - u.s.len)
+                                                   : 0u;
+            weigh_tile<true>(q, kf, b, bits, sum);
         }
-        finish(w, kf, part);
-        put(last - 1, 0, pair_sum(sum_of(part[0])));
     }
-    // One turn of a long unit: the rows go by, the next ones under way.
-    __device__ __forceinline__ void groups() const {
-        const int chunk = u.chunk, n = count(), from = first_token(chunk);
-        // a chain's first group with a token that sees a key of the turn
-        const int g0 = r.a.tree == nullptr ? max(chunk * C::MANY - u.s.len, 0) / tpg * of_token : 0;
-        u32x4 x[QL], kf[KB][STEPS];
-        float l, wt;
-        bool there[KB], all_there = true;
-        load_rows(g0, x, l, wt);
-#pragma unroll
-        for (int k = 0; k < KB; ++k) {
-            const int page = page_of(chunk, k, chunk + 1);
-            u32x4 kreg[NM];
-            fetch(chunk, k, page, kreg);
-            there[k] = page >= 0;
-            all_there = all_there && __builtin_amdgcn_ballot_w64(!there[k]) == 0;
-            widen(kreg, kf[k]);
+    template <int LOADS, class Ahead>
+    __device__ __forceinline__ void run(int t, int step, int end, const u32x4 (&kf)[KB][STEPS], uint32_t there, const float (*from)[32], int base,
+                                        float (&sum)[KB], const Ahead& ahead) const {
+        if (t >= end) {
+            ahead();
+            return;
         }
-        __syncthreads();                 // what another unit has left in LDS has been read
-        store_rows(0, x, l, wt);
-        have_loads();
-        __syncthreads();
-        Pending w;
-        w.any = false;
-        f32x4 part[KB];
-        float sum[KB];
+        const int j0 = u.chunk * MANY;
+        const bool all_there = __builtin_amdgcn_ballot_w64(there != (1u << KB) - 1u) == 0;
+        // (none before the end in a tree's new keys)
+        const Tiles x{from, base, !all_there ? 0x7fffffff : j0 + MANY <= u.s.len ? 0 : r.a.tree == nullptr ? j0 + MANY - 1 - u.s.len : 0x7fffffff, there};
+        start(t, 0);
+        int slot = 0;
+        if constexpr (C::SLOTS == 2) {
+            if (t + step < end) start(t + step, 1);
+        }
+#pragma unroll 1
+        for (; t + step < end; t += step) {
+            if constexpr (C::SLOTS == 2) {
+                landed<COPIES>();
+                tile(x, t, t + 2 * step < end ? t + 2 * step : -1, slot, kf, sum);
+                slot ^= 1;
+            } else {
+                landed<0>();
+                tile(x, t, t + step, 0, kf, sum);
+            }
+        }
+        if (ahead()) landed<LOADS>();
+        else landed<0>();
+        tile(x, t, -1, slot, kf, sum);
+    }
+    // A turn: sum is over half of the rows, the other half is in the other half of the lanes.
+    __device__ __forceinline__ int first_tile() const {
+        // a chain's first one with a row that sees a key of the turn
+        const int rel = u.chunk * MANY - u.s.len;
+        return r.a.tree == nullptr && rel > 0 ? rel / tpt * of_token : 0;
+    }
+    template <class Ahead> __device__ __forceinline__ void own_turn(const Own& own, bool fresh, float (&sum)[KB], const Ahead& ahead) const {
+        u32x4 kf[KB][STEPS];
+        uint32_t there;
 #pragma unroll
         for (int k = 0; k < KB; ++k) sum[k] = 0.0f;
-        int slot = 0;
-        for (int g = g0; g < n; ++g) {
-            const bool more = g + 1 < n;
-            if (more) load_rows(g + 1, x, l, wt);
-            clear_sums(part);
-            tiles(chunk, g, slot, kf, from, there, all_there, w, part, part);
+        if (fresh) put_bias(lds.bias + kOwnTiles * wave, 0, tiles, lane, kWave);
+        own_keys(own, kf, there);
+        have_loads();
+        run<2 * KB * (NM / 2)>(first_tile(), 1, tiles, kf, there, lds.bias + kOwnTiles * wave, 0, sum, ahead);
+    }
+    __device__ __forceinline__ void shared_turn(float (&sum)[KB]) const {
+        u32x4 kf[KB][STEPS];
+        uint32_t there;
 #pragma unroll
-            for (int k = 0; k < KB; ++k) sum[k] += sum_of(part[k]);
-            if (more) store_rows(slot ^ 1, x, l, wt);
+        for (int k = 0; k < KB; ++k) sum[k] = 0.0f;
+        shared_keys(kf, there);
+        int base = first_tile();
+        do {
+            const int end = min(base + kBiasTiles, tiles);
+            __syncthreads();             // the keys, or the tiles before, have been read
+            put_bias(lds.bias, base, end, threadIdx.x, kScoreThreads);
             __syncthreads();
-            slot ^= 1;
-        }
-        clear_sums(part);
-        finish(w, kf, part);
-#pragma unroll
-        for (int k = 0; k < KB; ++k) {
-            sum[k] = pair_sum(sum[k] + sum_of(part[k]));
-            if (KB == 2 && odd == 1 && lane < 32) lds.sums[wave / 2][32 * k + lane] = sum[k];
-        }
-        if (KB == 2) __syncthreads();
-        if (odd == 0) {
-#pragma unroll
-            for (int k = 0; k < KB; ++k) put(chunk, k, KB == 2 ? sum[k] + lds.sums[wave / 2][32 * k + (lane & 31)] : sum[k]);
+            have_loads();
+            run<0>(base + wave, kScoreWaves, end, kf, there, lds.bias, base, sum, [] { return false; });
+            base = end;
+        } while (base < tiles);
+    }
+    // The sum over all rows of the turn's key `j` becomes its score.
+    __device__ __forceinline__ void put(int j, float all) const {
+        if (j < keys) {
+            float* to = r.a.score + ((size_t)u.b * r.c.Hkv + u.h) * r.a.score_stride + j;
+            *to = j < u.s.len && r.a.decay != 0.0f ? fmaf(*to, r.a.decay, all) : all;
         }
     }
 };
 
 template <typename T, int D, bool FP8>
-__global__ __launch_bounds__(kScoreThreads, 2) void score_kernel(ScoreRun r) {
+__global__ __launch_bounds__(kScoreThreads, 2) void score_many_kernel(ScoreRun r) {
     using C = ScoreCfg<T, D, FP8>;
     using W = ScoreWalk<C>;
-    __shared__ __align__(16) ScoreRows<C> lds;
+    __shared__ __align__(1024) ScorePlaces<C> places;
     __shared__ ScoreScratch scratch;
-    const int lane = threadIdx.x & 63, wave = same((int)threadIdx.x >> 6);
-    // neighbours in the order of the turns, which read the same queries, are on one XCD
-    const int w = ((int)blockIdx.x & 7) * (kScoreGroups / 8) + ((int)blockIdx.x >> 3);
+    const int lane = threadIdx.x & 63, wave = same((int)threadIdx.x >> 6), w = place_of_group();
     long long total[3];
-    W::begin(r, &scratch, total);
+    W::template begin<kMid, kLong>(r, &scratch, total);
     W u;
     for (long long i = 0; i < total[kLong]; i += kScoreGroups) {
         const long long x = i + ((i & kScoreGroups) != 0 ? kScoreGroups - 1 - w : w);
         if (x >= total[kLong]) continue;
         u.end = 0;
         u.take(r, &scratch, kLong, x);
-        ManyRows<T, D, FP8, C::KB, W>(r, u, lds, wave, lane).groups();
+        const ManyRows<T, D, FP8, C::LONG, W> m(r, u, places, wave, lane);
+        float sum[C::LONG];
+        m.shared_turn(sum);
+        __syncthreads();                 // all tiles have been read
+#pragma unroll
+        for (int k = 0; k < C::LONG; ++k) {
+            const float all = pair_sum(sum[k]);
+            if (lane < 32) places.sums[wave][32 * k + lane] = all;
+        }
+        // the wavefronts' sums one after the other
+        __syncthreads();
+        for (int j = threadIdx.x; j < 32 * C::LONG; j += kScoreThreads) {
+            float all = 0.0f;
+#pragma unroll
+            for (int v = 0; v < kScoreWaves; ++v) all += places.sums[v][j];
+            m.put(u.chunk * 32 * C::LONG + j, all);
+        }
+        __syncthreads();
     }
-    if (u.start(r, &scratch, kMid, total[kMid], w, kScoreGroups)) {
-        int n;
-        do {
-            n = u.here();
-            ManyRows<T, D, FP8, 1, W>(r, u, lds, wave, lane).one_group(n);
-        } while (u.advance(r, n));
+    if (!u.start(r, &scratch, kMid, total[kMid], w, kScoreGroups)) return;
+    const long long begin = u.at;
+    const auto next = [&] {
+        int k = 0;
+        if (lane == 0) k = atomicAdd(&scratch.taken, 1);
+        return begin + same(k);
+    };
+    using M = ManyRows<T, D, FP8, C::MID, W>;
+    if (!u.advance_to(r, next())) return;
+    typename M::Own own;
+    M(r, u, places, wave, lane).fetch(own);
+    bool fresh = true;                   // another unit than the turn before
+    for (;;) {
+        W v = u;
+        const bool more = v.advance_to(r, next());
+        const M m(r, u, places, wave, lane);
+        float sum[C::MID];
+        m.own_turn(own, fresh, sum, [&] {
+            if (more) M(r, v, places, wave, lane).fetch(own);
+            return more;
+        });
+#pragma unroll
+        for (int k = 0; k < C::MID; ++k) {
+            const float all = pair_sum(sum[k]);
+            if (lane < 32) m.put(u.chunk * 32 * C::MID + 32 * k + lane, all);
+        }
+        if (!more) return;
+        fresh = v.b != u.b || v.h != u.h;
+        u = v;
     }
-    __syncthreads();                     // the rows of mid units have been read
-    static_assert(sizeof(lds.q) >= kScoreWaves * 16 * C::KPITCH, "a block of keys for each wavefront");
-    if (u.start(r, &scratch, kFew, total[kFew], w, kScoreGroups))
-        few_rows<T, D, FP8>(r, u, &scratch.taken, &lds.q[0][0] + wave * 16 * C::KPITCH, lane);
 }
 
 template <typename T, int D, bool FP8>
 static hipError_t launch_score_d(const ScoreRun& r, hipStream_t st) {
-    hipLaunchKernelGGL((score_kernel<T, D, FP8>), dim3(kScoreGroups), dim3(kScoreThreads), 0, st, r);
+    // (units of more than a few rows: there are none where all of the call's rows are not more)
+    if ((int64_t)r.c.T * r.group.d > kFewRows) {
+        hipLaunchKernelGGL((score_many_kernel<T, D, FP8>), dim3(kScoreGroups), dim3(kScoreThreads), 0, st, r);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    if (r.group.d > kFewRows) return hipSuccess;
+    hipLaunchKernelGGL((score_few_kernel<T, D, FP8>), dim3(kScoreGroups), dim3(kScoreThreads), 0, st, r);
     return hipGetLastError();
 }
 template <typename T, bool FP8>
