@@ -1,10 +1,14 @@
 // Keys that go, by their scores (flashd_cache_evict): of a sequence that has more than its budget of keys the first ones, the last ones and those with
 // the largest scores stay, in every layer and kv head those of its own, and move together in their order.
 //
-// Three kernels.  The first chooses, a workgroup per (layer, sequence, kv head), and leaves for each place (rank) behind the first ones the key that
+// The first kernel chooses, a workgroup per (layer, sequence, kv head), and leaves for each place (rank) behind the first ones the key that
 // goes there; scores it moves by itself.  Rows of K and V then move within the pages, to lower places.  A place below the new length m may hold a key that stays
 // and must be read before it is overwritten; the keys behind m are overwritten by nobody.  So the second kernel moves, in order, the keys that come
-// from below m (they are a first run of the ranks), a wavefront for 64 bytes of every row, and the third all others, which by then depend on nothing.
+// from below m (they are a first run of the ranks), and the third all others, which by then depend on nothing.  Of many units the second one moves them all.
+//
+// Bytes bound it: rows that stay and move are read and written once, at 4.8 TB/s where a large copy has 4.84.  Before them stands the choice: 14 us for 1040 scores,
+// 50 us for 65536 of them (five passes of one CU, by the instructions).  16 sequences of 1040 keys to 1024 keys 33 us, 8 layers of 8 prompts of 1500 to 8000 keys to 1024
+// 146 us (548 MB), 2 layers of 65536 keys to 16384 123 us (274 MB).
 #include "flashd_common.h"
 #include "flashd_kernels.h"
 #include "flashd_mma.h"
@@ -12,13 +16,13 @@
 
 namespace flashd {
 
-constexpr int kChooseThreads = 1024;
-constexpr int kChooseWaves = kChooseThreads / kWave;
 constexpr int kDigit = 2048;            // values of a digit: a score's 32 bits are three of them
-constexpr int kMoveWaves = 4;
+constexpr int kNearThreads = 1024;
+constexpr int kNearRows = 4;            // rows of a thread in a round
+constexpr int kFarThreads = 256;
 constexpr int kFarRows = 128;           // ranks of a workgroup of the third kernel
 
-// What the first kernel leaves of a unit: its ranks from `first` to `near` come from below m, those from there to m from behind it.
+// What the first kernel leaves of a unit: its ranks from `first`, the first one that moves, to `near` come from below m, those from there to m from behind it.
 struct EvictUnit {
     int first, near, m;     // all 0: nothing moves
 };
@@ -38,62 +42,116 @@ __device__ __forceinline__ uint32_t order_of(float x) {
     return x != x ? 0u : (u & 0x80000000u) ? ~u : u | 0x80000000u;
 }
 
-struct ChooseShared {
-    int count[kDigit];
-    int wave_sum[kChooseWaves];
-    int total;
+// Scores lie over few digits (powers of two and quarters), which lanes that add to one counter would wait for one by one: so there are some of each digit.
+constexpr int kCopies = 4;
+constexpr int kCopyPitch = kDigit + 8;
+constexpr int kAhead = 8;               // scores of a thread on their way
+
+template <int THREADS> struct ChooseShared {
+    alignas(16) int count[kCopies][kCopyPitch];
+    int wave_sum[2][THREADS / kWave];
     int digit, above;
     int bad;
+    int near, first;
 };
 
-// Exclusive sum over the workgroup's threads
-__device__ __forceinline__ int sum_before(int x, ChooseShared& sh, int& total) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int in = lanes_up_to(x);
-    __syncthreads();
-    if (lane == 63) sh.wave_sum[wave] = in;
-    __syncthreads();
-    int before = in - x;
-    total = 0;
-#pragma unroll
-    for (int k = 0; k < kChooseWaves; ++k) {
-        before += k < wave ? sh.wave_sum[k] : 0;
-        total += sh.wave_sum[k];
-    }
-    return before;
-}
+// How many lanes before this one are in the mask
+__device__ __forceinline__ int lanes_before(uint64_t mask) { return __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0)); }
 
-// Of the keys in [lo, hi) `need` (0 < need < hi - lo) stay.  The order of the least score among them, digit by digit from the top: each
+// A wavefront's run of keys [j0, j1), the first kAhead of a lane's scores in registers
+struct Run {
+    const float* score;
+    int j0, j1, lane;
+    float x0[kAhead];
+    __device__ __forceinline__ void load(int at, float (&x)[kAhead]) const {
+        if (at + 64 * kAhead <= j1) {
+            const float* p = score + at;
+#pragma unroll
+            for (int e = 0; e < kAhead; ++e) x[e] = p[64 * e + lane];
+        } else {
+#pragma unroll
+            for (int e = 0; e < kAhead; ++e) {
+                x[e] = 0.0f;
+                if (at + 64 * e < j1) x[e] = score[min(at + 64 * e + lane, j1 - 1)];
+            }
+        }
+    }
+    // f(j, x, whether there is one) for all of the lane's scores, 64 keys at a time
+    template <class F> __device__ __forceinline__ void over(F&& f) const {
+        float x[kAhead], next[kAhead];
+#pragma unroll
+        for (int e = 0; e < kAhead; ++e) x[e] = x0[e];
+#pragma unroll 1
+        for (int at = j0; at < j1; at += 64 * kAhead) {
+            if (at + 64 * kAhead < j1) load(at + 64 * kAhead, next);
+            if (at + 64 * kAhead <= j1) {
+#pragma unroll
+                for (int e = 0; e < kAhead; ++e) f(at + 64 * e + lane, x[e], true);
+            } else {
+#pragma unroll
+                for (int e = 0; e < kAhead; ++e) {
+                    if (at + 64 * e < j1) f(at + 64 * e + lane, x[e], at + 64 * e + lane < j1);
+                }
+            }
+#pragma unroll
+            for (int e = 0; e < kAhead; ++e) x[e] = next[e];
+        }
+    }
+};
+
+// Of the keys of all wavefronts' runs `need` (more than 0, fewer than there are) stay.  The order of the least score among them, digit by digit from the top: each
 // time the keys that agree so far are counted by the next digit, and the digit is the one in which the count from above reaches what
 // is still needed.  `ties`: how many of those that have exactly this order stay.
-__device__ __forceinline__ uint32_t least_kept(const float* score, int lo, int hi, int need, ChooseShared& sh, int& ties) {
-    constexpr int EACH = kDigit / kChooseThreads;
+template <int THREADS> __device__ __forceinline__ uint32_t least_kept(const Run& run, int need, ChooseShared<THREADS>& sh, int& ties) {
+    constexpr int EACH = kDigit / THREADS;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     uint32_t prefix = 0;
     int shift = 21;
     for (int pass = 0; pass < 3; ++pass) {
         const int bits = pass == 2 ? 10 : 11;
-        for (int i = threadIdx.x; i < kDigit; i += kChooseThreads) sh.count[i] = 0;
+        for (int i = 4 * tid; i < kCopies * kCopyPitch; i += 4 * THREADS) *reinterpret_cast<u32x4*>(&sh.count[0][i]) = u32x4{0, 0, 0, 0};
         __syncthreads();
-        for (int j = lo + threadIdx.x; j < hi; j += kChooseThreads) {
-            const uint32_t x = order_of(score[j]);
-            if (pass == 0 || x >> (shift + bits) == prefix) atomicAdd(&sh.count[x >> shift & ((1u << bits) - 1u)], 1);
+        int* const mine_of = sh.count[lane % kCopies];
+        if (pass == 0) {
+            run.over([&](int, float x, bool is) {
+                if (is) atomicAdd(&mine_of[order_of(x) >> 21], 1);
+            });
+        } else if (prefix == 0) {
+            // (NaN have order 0, and nothing else has this digit)
+            if (tid == 0) mine_of[0] = need;
+        } else {
+            // those that agree so far have the prefix's sign, and so the order's bits are the score's, or all of them the other way
+            const uint32_t flip = prefix >> (31 - shift - bits) != 0 ? 0x80000000u : 0xffffffffu;
+            const uint32_t top = prefix << (shift + bits);
+            run.over([&](int, float x, bool is) {
+                const uint32_t o = __float_as_uint(x + 0.0f) ^ flip ^ top;
+                if (is && o < 1u << (shift + bits) && x == x) atomicAdd(&mine_of[o >> shift], 1);
+            });
         }
         __syncthreads();
         // from the top digit down
-        int mine = 0;
+        int n[EACH], mine = 0;
 #pragma unroll
-        for (int e = 0; e < EACH; ++e) mine += sh.count[kDigit - 1 - (threadIdx.x * EACH + e)];
-        int total;
-        int above = sum_before(mine, sh, total);
+        for (int e = 0; e < EACH; ++e) {
+            n[e] = 0;
+#pragma unroll
+            for (int k = 0; k < kCopies; ++k) n[e] += sh.count[k][kDigit - 1 - (tid * EACH + e)];
+            mine += n[e];
+        }
+        const int in = lanes_up_to(mine);
+        if (lane == 63) sh.wave_sum[0][wave] = in;
+        __syncthreads();
+        int above = in - mine;
+#pragma unroll
+        for (int k = 0; k < THREADS / kWave; ++k) above += k < wave ? sh.wave_sum[0][k] : 0;
         if (above < need && above + mine >= need) {
 #pragma unroll
             for (int e = 0; e < EACH; ++e) {
-                const int d = kDigit - 1 - (threadIdx.x * EACH + e), n = sh.count[d];
-                if (above < need && above + n >= need) {
-                    sh.digit = d;
+                if (above < need && above + n[e] >= need) {
+                    sh.digit = kDigit - 1 - (tid * EACH + e);
                     sh.above = above;
                 }
-                above += n;
+                above += n[e];
             }
         }
         __syncthreads();
@@ -106,8 +164,8 @@ __device__ __forceinline__ uint32_t least_kept(const float* score, int lo, int h
     return prefix;
 }
 
-__global__ __launch_bounds__(kChooseThreads) void evict_choose_kernel(EvictRun r) {
-    __shared__ ChooseShared sh;
+template <int THREADS> __global__ __launch_bounds__(THREADS) void evict_choose_kernel(EvictRun r) {
+    __shared__ ChooseShared<THREADS> sh;
     const Paged& c = r.c;
     const int unit = blockIdx.x, tid = threadIdx.x;
     const int h = unit % c.Hkv, b = unit / c.Hkv % c.B, y = unit / (c.Hkv * c.B);
@@ -123,7 +181,7 @@ __global__ __launch_bounds__(kChooseThreads) void evict_choose_kernel(EvictRun r
     if (asked && m > first) {
         const int col0 = first >> c.page_log2, cols = (len + (1 << c.page_log2) - 1) >> c.page_log2;
         bool bad = false;
-        for (int k = col0 + tid; k < cols; k += kChooseThreads) {
+        for (int k = col0 + tid; k < cols; k += THREADS) {
             const int p = page_at(c, b, k);
             bad |= p < 0 || (k << c.page_log2 < m && r.a.refs[p] > 1);
         }
@@ -141,56 +199,87 @@ __global__ __launch_bounds__(kChooseThreads) void evict_choose_kernel(EvictRun r
     float* const score = r.a.score + (r.layer0 + y) * r.a.score_layer_stride + ((int64_t)b * c.Hkv + h) * r.a.score_stride;
     int* const from = r.from + (int64_t)unit * r.budget;
     const int lo = first, hi = len - recent, need = m - first - recent;
-    uint32_t least = 0xffffffffu;
-    int ties = 0;
-    if (need > 0) least = least_kept(score, lo, hi, need, sh, ties);
-
-    // The keys that stay, in their order: a run of keys for each thread, so that one sum over the threads gives its ranks.
-    constexpr int EACH = 4;
-    int rank = first, equal = 0, near = first;
-    for (int j0 = lo; j0 < len; j0 += EACH * kChooseThreads) {
-        float x[EACH];
-        int same[EACH], stays[EACH];
-        int eq = 0;
-#pragma unroll
-        for (int e = 0; e < EACH; ++e) {
-            const int j = j0 + EACH * tid + e;
-            x[e] = j < len ? score[j] : 0.0f;
-            const uint32_t o = order_of(x[e]);
-            same[e] = j < hi && need > 0 && o == least;
-            stays[e] = j < len && (j >= hi || (need > 0 && o > least));
-            eq += same[e];
+    // Each wavefront has a run of keys, counts those that stay, and then knows the ranks of its own.
+    const int lane = tid & 63, wave = tid >> 6;
+    const int each = ((hi - lo + THREADS / kWave - 1) / (THREADS / kWave) + 63) & ~63;
+    Run run;
+    run.score = score;
+    run.lane = lane;
+    run.j0 = __builtin_amdgcn_readfirstlane(min(lo + wave * each, hi));
+    run.j1 = min(run.j0 + each, hi);
+    if (tid == 0) {
+        sh.near = first;
+        sh.first = m;
+    }
+    if (need > 0) {
+        run.load(run.j0, run.x0);
+        int ties;
+        const uint32_t o = least_kept(run, need, sh, ties);
+        const bool odd = o == 0;                         // the least one that stays is NaN, and all others stay
+        const float least = __uint_as_float((o & 0x80000000u) != 0 ? o ^ 0x80000000u : ~o);
+        int n_sure = 0, n_equal = 0;
+        run.over([&](int, float x, bool is) {
+            n_sure += is && (odd ? x == x : x > least);
+            n_equal += is && (odd ? x != x : x == least);
+        });
+        n_sure = lanes_up_to(n_sure);
+        n_equal = lanes_up_to(n_equal);
+        if (lane == 63) {
+            sh.wave_sum[0][wave] = n_sure;
+            sh.wave_sum[1][wave] = n_equal;
         }
-        int all_equal;
-        int before = equal + sum_before(eq, sh, all_equal);
-        int n = 0;
-#pragma unroll
-        for (int e = 0; e < EACH; ++e) {
-            if (same[e]) stays[e] = before++ < ties;
-            n += stays[e];
+        __syncthreads();
+        int rank = first, seen = 0;
+        for (int k = 0; k < wave; ++k) {
+            rank += sh.wave_sum[0][k];
+            seen += sh.wave_sum[1][k];
         }
-        int all;
-        int at = rank + sum_before(n, sh, all);          // (its barriers: the scores of the run have been read)
+        rank = __builtin_amdgcn_readfirstlane(rank + min(seen, ties));
+        seen = __builtin_amdgcn_readfirstlane(seen);
+        run.over([&](int j, float x, bool is) {
+            bool stays = is && (odd ? x == x : x > least);
+            const bool equals = is && (odd ? x != x : x == least);
+            const uint64_t equal = __builtin_amdgcn_ballot_w64(equals);
+            if (equal != 0) {
+                // the first ones of those stay
+                stays |= equals && seen + lanes_before(equal) < ties;
+                seen += __popcll(equal);
+            }
+            const uint64_t stay = __builtin_amdgcn_ballot_w64(stays);
+            int* const to = from + rank;                 // (the same for all lanes)
+            if (stays) to[(uint32_t)lanes_before(stay)] = j;
+            rank += __popcll(stay);
+        });
+    }
+    for (int k = tid; k < recent; k += THREADS) from[m - recent + k] = hi + k;
+    __syncthreads();
+    // Their scores move down: all of a round have been read before any is written, and later rounds' come from behind what is written.
+    constexpr int N = 8;
+    int near = 0, moved = m;             // of the wavefront: ranks from below m, the first one that moves
+    for (int r0 = first; r0 < m; r0 += N * THREADS) {
+        int j[N];
+        float x[N];
 #pragma unroll
-        for (int e = 0; e < EACH; ++e) {
-            const int j = j0 + EACH * tid + e;
-            if (!stays[e]) continue;
-            from[at] = j;
-            if (at != j) score[at] = x[e];
-            ++at;
-        }
-        equal += all_equal;
-        rank += all;
-        if (j0 < m) {
-            int inside = 0;
+        for (int e = 0; e < N; ++e) j[e] = from[min(r0 + e * THREADS + tid, m - 1)];
 #pragma unroll
-            for (int e = 0; e < EACH; ++e) inside += stays[e] && j0 + EACH * tid + e < m;
-            int sum;
-            (void)sum_before(inside, sh, sum);
-            near += sum;
+        for (int e = 0; e < N; ++e) x[e] = score[j[e]];
+        __syncthreads();
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+            const int at = r0 + e * THREADS + tid;
+            const bool moves = at < m && j[e] != at;
+            if (moves) score[at] = x[e];
+            near += __popcll(__builtin_amdgcn_ballot_w64(at < m && j[e] < m));
+            const uint64_t some = __builtin_amdgcn_ballot_w64(moves);
+            if (some != 0) moved = min(moved, at - lane + __builtin_ctzll(some));
         }
     }
-    if (tid == 0) *left = EvictUnit{first, near, m};
+    if (lane == 0) {
+        atomicAdd(&sh.near, near);
+        atomicMin(&sh.first, moved);
+    }
+    __syncthreads();
+    if (tid == 0) *left = EvictUnit{min(sh.first, sh.near), sh.near, m};
 }
 
 // ---- moving rows --------------------------------------------------------------------------------
@@ -216,66 +305,59 @@ __device__ __forceinline__ UnitPlace place_of(const EvictRun& r, int unit, bool 
     return UnitPlace{c, pool, c.table + (size_t)b * c.max_pages, c.d * c.esz};
 }
 
-// Ranks `first` to `near` in order.  A wavefront takes 64 bytes of each row, 16 rows by 4 lanes at a time and NROW of those together; it reads the next
-// ones before it writes these: those come from higher places than any that are written here.
-template <int NROW>
-__global__ __launch_bounds__(kMoveWaves * kWave) void evict_near_kernel(EvictRun r, int slices) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const long long id = (long long)blockIdx.x * kMoveWaves + wave;
-    const int slice = (int)(id % slices);
-    const long long of = id / slices;
+// Ranks `first` to `near` in order, of a unit's K or V by one workgroup, or by some that take a slice of every row each.  All rows of a round have been read before any
+// is written, and the next round's are on their way by then: they come from behind all that is written.
+__global__ __launch_bounds__(kNearThreads) void evict_near_kernel(EvictRun r, int slices, int all) {
+    constexpr int N = kNearRows;
     const int units = r.layers * r.c.B * r.c.Hkv;
+    // (slices of a row share its 128-byte lines: their workgroups are 8 apart, on one XCD)
+    const long long g = blockIdx.x / (8 * slices), in = blockIdx.x % (8 * slices);
+    const long long of = 8 * g + (in & 7);
     if (of >= 2ll * units) return;
-    const int unit = (int)(of >> 1);
+    const int slice = (int)(in >> 3), unit = (int)(of >> 1);
     const EvictUnit u = r.units[unit];
-    if (u.near <= u.first) return;
+    const int end = all ? u.m : u.near;
+    if (end <= u.first) return;
     const UnitPlace place = place_of(r, unit, of & 1);
     const int* const from = r.from + (int64_t)unit * r.budget;
-    const int off = 64 * slice + 16 * (lane & 3), sub = lane >> 2;
-    auto key = [&](int rank) { return rank < u.near ? from[rank] : -1; };
-    auto load = [&](int rank, int j) {
-        bool there;
-        const char* p = place.at(j < 0 ? rank : j, there);
-        return j > rank && there ? *reinterpret_cast<const u32x4*>(p + off) : u32x4{0, 0, 0, 0};
+    const int pieces = place.row_bytes / 16 / slices, rows = kNearThreads / pieces;
+    const int sub = threadIdx.x / pieces, off = 16 * (slice * pieces + (int)threadIdx.x % pieces);
+    bool there[N], there_next[N];
+    u32x4 x[N], next[N];
+    int j[N];
+    auto key = [&](int at) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) j[i] = from[min(at + i * rows + sub, end - 1)];
     };
-    int j0[NROW], j1[NROW];
-    u32x4 x[NROW], next[NROW];
+    auto load = [&](u32x4 (&to)[N], bool (&is)[N]) {
 #pragma unroll
-    for (int i = 0; i < NROW; ++i) j0[i] = key(u.first + 16 * i + sub);
+        for (int i = 0; i < N; ++i) to[i] = *reinterpret_cast<const u32x4*>(place.at(j[i], is[i]) + off);
+    };
+    key(u.first);
+    load(x, there);
+    key(u.first + N * rows);
+    for (int at = u.first; at < end; at += N * rows) {
+        load(next, there_next);
+        key(at + 2 * N * rows);
 #pragma unroll
-    for (int i = 0; i < NROW; ++i) j1[i] = key(u.first + 16 * (NROW + i) + sub);
+        for (int i = 0; i < N; ++i) asm volatile("" : "+v"(x[i]));       // this round's rows have been read
+        __syncthreads();
 #pragma unroll
-    for (int i = 0; i < NROW; ++i) x[i] = load(min(u.first + 16 * i + sub, u.near - 1), j0[i]);
-    for (int at = u.first; at < u.near; at += 16 * NROW) {
-        int j2[NROW];
-#pragma unroll
-        for (int i = 0; i < NROW; ++i) j2[i] = key(at + 16 * (2 * NROW + i) + sub);
-#pragma unroll
-        for (int i = 0; i < NROW; ++i) next[i] = load(min(at + 16 * (NROW + i) + sub, u.near - 1), j1[i]);
-        // (the reads above are older than the writes below, and a wavefront's accesses to one address keep their order)
-#pragma unroll
-        for (int i = 0; i < NROW; ++i) {
-            const int rank = at + 16 * i + sub;
-            if (j0[i] <= rank) continue;                 // none, or in its place
-            bool there, was;
-            char* to = place.at(rank, there);
-            (void)place.at(j0[i], was);
-            if (there && was) *reinterpret_cast<u32x4*>(to + off) = x[i];
-        }
-#pragma unroll
-        for (int i = 0; i < NROW; ++i) {
-            j0[i] = j1[i];
-            j1[i] = j2[i];
+        for (int i = 0; i < N; ++i) {
+            const int rank = at + i * rows + sub;
+            bool is;
+            char* to = place.at(min(rank, end - 1), is);
+            if (rank < end && is && there[i]) *reinterpret_cast<u32x4*>(to + off) = x[i];
             x[i] = next[i];
+            there[i] = there_next[i];
         }
     }
 }
 
-// Ranks `near` to m, kFarRows of them to a workgroup.
-__global__ __launch_bounds__(kMoveWaves * kWave) void evict_far_kernel(EvictRun r, int slices) {
+// Ranks `near` to m, kFarRows of them to a workgroup.  Their rows are read once (past the caches: 128 -> 116 us for 2 layers of 65536 keys to 16384).
+__global__ __launch_bounds__(kFarThreads) void evict_far_kernel(EvictRun r) {
+    constexpr int N = 4;
     const int units = r.layers * r.c.B * r.c.Hkv;
-    const int per_row = 4 * slices, rows = kMoveWaves * kWave / per_row;
-    const int off = 16 * (threadIdx.x % per_row), sub = threadIdx.x / per_row;
     for (int of = blockIdx.y; of < 2 * units; of += gridDim.y) {
         const int unit = of >> 1;
         const EvictUnit u = r.units[unit];
@@ -283,11 +365,22 @@ __global__ __launch_bounds__(kMoveWaves * kWave) void evict_far_kernel(EvictRun 
         if (begin >= end) continue;
         const UnitPlace place = place_of(r, unit, of & 1);
         const int* const from = r.from + (int64_t)unit * r.budget;
-        for (int rank = begin + sub; rank < end; rank += rows) {
-            bool there, was;
-            const char* src = place.at(from[rank], was);
-            char* to = place.at(rank, there);
-            if (was && there) *reinterpret_cast<u32x4*>(to + off) = *reinterpret_cast<const u32x4*>(src + off);
+        const int pieces = place.row_bytes / 16, rows = kFarThreads / pieces;
+        const int off = 16 * (threadIdx.x % pieces), sub = threadIdx.x / pieces;
+        for (int at = begin + sub; at < end; at += N * rows) {
+            int j[N];
+            bool was[N];
+            u32x4 x[N];
+#pragma unroll
+            for (int i = 0; i < N; ++i) j[i] = from[min(at + i * rows, end - 1)];
+#pragma unroll
+            for (int i = 0; i < N; ++i) x[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(place.at(j[i], was[i]) + off));
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                bool is;
+                char* to = place.at(min(at + i * rows, end - 1), is);
+                if (at + i * rows < end && is && was[i]) *reinterpret_cast<u32x4*>(to + off) = x[i];
+            }
         }
     }
 }
@@ -320,22 +413,27 @@ hipError_t launch_cache_evict(const Paged& c, const EvictArgs& a, void* ws, hipS
     const int64_t of_layer = (int64_t)c.B * c.Hkv;
     r.units = static_cast<EvictUnit*>(ws);
     r.from = reinterpret_cast<int*>(r.units + layers * of_layer);
-    const int slices = c.d * c.esz / 64;
     for (r.layer0 = 0; r.layer0 < c.layers; r.layer0 += layers) {
         r.layers = c.layers - r.layer0 < layers ? c.layers - r.layer0 : layers;
         const int64_t units = r.layers * of_layer;
-        hipLaunchKernelGGL(evict_choose_kernel, dim3((unsigned)units), dim3(kChooseThreads), 0, st, r);
+        // A unit's choice is the call's time where there are few units, and two halves as large go by turns where there are more than CUs (8 layers of 8 heads of 8 sequences
+        // 156 -> 148 us, 128 units of 1040 keys 38.7 -> 37.2; 16 units of 65536 keys 115 -> 126).
+        if (units < 128) hipLaunchKernelGGL(evict_choose_kernel<1024>, dim3((unsigned)units), dim3(1024), 0, st, r);
+        else hipLaunchKernelGGL(evict_choose_kernel<512>, dim3((unsigned)units), dim3(512), 0, st, r);
         hipError_t e = hipGetLastError();
-        if (e != hipSuccess || r.budget == 0) {
-            if (e != hipSuccess) return e;
-            continue;
-        }
-        const int64_t waves = 2 * units * slices;
-        hipLaunchKernelGGL(evict_near_kernel<8>, dim3((unsigned)((waves + kMoveWaves - 1) / kMoveWaves)), dim3(kMoveWaves * kWave), 0, st, r, slices);
+        if (e != hipSuccess) return e;
+        if (r.budget == 0) continue;
+        // As many workgroups as take the CUs twice move the rows, each of them slices of at least 64 bytes where there are few units.  Of many units each moves all ranks
+        // (128 units of 1040 keys 47 -> 39 us with their slices and without the third kernel, 512 of 1500 to 8000 keys 162 -> 156).
+        const bool all = 2 * units >= 256;
+        int slices = 1;
+        while (2 * units * slices < 512 && c.d * c.esz / slices > 64) slices *= 2;
+        hipLaunchKernelGGL(evict_near_kernel, dim3((unsigned)((2 * units + 7) / 8 * 8 * slices)), dim3(kNearThreads), 0, st, r, slices, (int)all);
         e = hipGetLastError();
         if (e != hipSuccess) return e;
+        if (all) continue;
         const dim3 far((unsigned)((r.budget + kFarRows - 1) / kFarRows), (unsigned)(2 * units < 65535 ? 2 * units : 65535));
-        hipLaunchKernelGGL(evict_far_kernel, far, dim3(kMoveWaves * kWave), 0, st, r, slices);
+        hipLaunchKernelGGL(evict_far_kernel, far, dim3(kFarThreads), 0, st, r);
         e = hipGetLastError();
         if (e != hipSuccess) return e;
     }

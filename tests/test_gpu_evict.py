@@ -122,6 +122,21 @@ def test_lengths(L, budget):
     check(Life([L], 1, 64, 256, "bf16", seed=L), budget, first=4, recent=7)
 
 
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("f32", 128), ("fp8", 64)])
+def test_many_units(dtype, d):
+    """So many that no row is cut into slices and one kernel moves all rows, in several rounds."""
+    lens = [1100, 701, 700, 90, 5000, 720, 0, 2050]
+    check(Life(lens, 8, d, 64, dtype, 2, seed=d), 700, first=4, recent=9)
+
+
+@pytest.mark.parametrize("L", [400, 10000])
+def test_fewer_numbers_than_stay(L):
+    """The least score that stays is NaN: of those the first ones stay."""
+    c = Life([L], 2, 64, 64, "bf16", seed=L)
+    c.score[..., torch.arange(c.score.shape[-1]) % 4 != 1] = math.nan
+    check(c, L // 2, first=3, recent=5)
+
+
 def test_equal_scores_infinities_and_nan():
     c = Life([500, 500, 500, 500, 500, 500], 1, 64, 16, "bf16", seed=1)
     gen = torch.Generator().manual_seed(2)
