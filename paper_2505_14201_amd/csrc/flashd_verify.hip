@@ -8,7 +8,7 @@
 //
 // All of it is in 64 bits.  V tokens cut the unit interval at V places, so that sums of 32 bits would put a random number on
 // the wrong side of one of them about once in a thousand draws (131072 tokens, sums off by 1e-8); with 64 it is
-// once in 1e9.  An exponential is then 17 instructions of full rate, and each logit has one.
+// once in 1e9.  An exponential is then 13 instructions of full rate, and each logit has one.
 #include "flashd_common.h"
 #include "flashd_kernels.h"
 #include "flashd_paged.h"
@@ -35,41 +35,112 @@ struct RowStat {
     double p, q;
 };
 
+// log2(e) / temperature, and the least distance to the largest logit that counts, 1023 / scale, which is exponent 0: none; a scale below 0 where the sequence takes the largest logit
+// (a temperature of 0, below, or NaN).  An infinite temperature leaves the least scale with which the rules for infinities hold.
+struct Heat {
+    double scale, least;
+};
+__device__ __forceinline__ Heat heat_of(float t) {
+    if (!(t > 0.0f)) return Heat{-1.0, 0.0};
+    const double scale = fmax(1.4426950408889634 / (double)t, 1e-290);
+    return Heat{scale, -1023.0 / scale};
+}
+
+// What is left behind the present token: max(scale w - by q, 0) for the weights w of its row; without q the weights but those of
+// the tokens refused.
+struct Rest {
+    int row;            // row of the packed tensors
+    float top;
+    Heat heat;
+    double scale, by;   // with q
+    int refused;        // without q: how many
+};
+
+// Where a sequence's walk has ended
+struct WalkEnd {
+    Rest rest;
+    double old_scale, old_by;   // of what was left before the last refusal, if that has not been divided by its sum
+    int open;
+    int draw;           // 0: the next token is known
+};
+
 struct VerifyRun {
     VerifyArgs a;
     ChunkStat* chunks;      // [T][nc]
     RowStat* rows;          // [T]
-    int* refused;           // [T] tokens refused behind the present one, from the sequence's first row on
+    WalkEnd* ends;          // [T] of a sequence at its first row, as the others:
+    double* left;           // [T][nc] sums of what is left over the chunks
+    int* refused;           // [T] tokens refused behind the present one
     int nc;
 };
 
 // ---- numbers ------------------------------------------------------------------------------------
 
 // A logit as it counts: NaN like -infinity, +infinity like the largest number.
+__device__ __forceinline__ bool is_odd(float x) { return __builtin_amdgcn_classf(x, 0x203); }        // NaN or +infinity
 __device__ __forceinline__ float clean(float x) {
     return x != x ? -__builtin_inff() : fminf(x, 3.4028234663852886e38f);
 }
 
-// 2^x for x <= 0, by the series of e^(f ln 2) on [-1/2, 1/2]; 6e-15 off.  0 for NaN (of -infinity - -infinity, or times 0).
-__device__ __forceinline__ double exp2_down(double x) {
-    x = fmax(x, -1100.0);
-    const double n = __builtin_rint(x), f = x - n;
-    double y = 4.4455382718708115e-10;
-    y = fma(y, f, 7.0549116208011233e-9);
-    y = fma(y, f, 1.0178086009239699e-7);
-    y = fma(y, f, 1.3215486790144310e-6);
-    y = fma(y, f, 1.5252733804059840e-5);
-    y = fma(y, f, 1.5403530393381609e-4);
-    y = fma(y, f, 1.3333558146428443e-3);
-    y = fma(y, f, 9.6181291076284771e-3);
-    y = fma(y, f, 5.5504108664821580e-2);
-    y = fma(y, f, 2.4022650695910072e-1);
-    y = fma(y, f, 6.9314718055994531e-1);
-    y = fma(y, f, 1.0);
-    return ldexp(y, (int)n);
+// 2^(d heat.scale) for d <= 0, by a polynomial for 2^f on [-1/2, 1/2] through its values at the ten zeros of a Chebyshev polynomial; 1.9e-14 off.  0 for
+// d = -infinity and NaN (of -infinity - -infinity).
+__device__ __forceinline__ double weight_of(float l, float top, Heat heat) {
+    const double d = fmax((double)l - (double)top, heat.least);
+    const double whole = 6755399441055744.0;                     // 1.5 2^52: what is added to it is rounded to a whole number, in its low bits
+    const double t = fma(d, heat.scale, whole), f = fma(d, heat.scale, whole - t);
+    double y = 1.0205905413765595e-07;
+    y = fma(y, f, 1.3259645244887111e-06);
+    y = fma(y, f, 1.5252672924850737e-05);
+    y = fma(y, f, 1.5403433751251010e-04);
+    y = fma(y, f, 1.3333558200794592e-03);
+    y = fma(y, f, 9.6181291939343126e-03);
+    y = fma(y, f, 5.5504108664651670e-02);
+    y = fma(y, f, 2.4022650695640341e-01);
+    y = fma(y, f, 6.9314718055994617e-01);
+    y = fma(y, f, 1.0000000000000135);
+    return ldexp(y, (int)(uint32_t)__double_as_longlong(t));
 }
-__device__ __forceinline__ double weight_of(float l, float top, double heat) {
-    return exp2_down(((double)l - (double)top) * heat);
+
+// The same where there are many, with a table of 2^(j / 256): of the exponent's 256th parts the whole ones' low 8 bits are j, the others go to the number's exponent, and
+// of the rest a polynomial of degree 3 is 1.8e-14 off.  13 instructions instead of 19 (and a read of LDS, which is idle: the lanes of a wavefront meet a bank about
+// three at a time).
+constexpr int kParts = 256;
+struct Powers {
+    uint64_t bits[kParts];          // of the number less j << 44: what j adds to the exponent's place is in it already
+    constexpr Powers() : bits() {
+        for (int j = 0; j < kParts; ++j) {
+            // e^x of x = j ln 2 / 256 < 0.7
+            const double x = j * (0.69314718055994530942 / kParts);
+            double y = 1.0;
+            for (int k = 22; k > 0; --k) y = 1.0 + x / k * y;
+            bits[j] = (uint64_t)((y - 1.0) * 4503599627370496.0) + (1023ull << 52) - ((uint64_t)j << 44);
+        }
+    }
+};
+__device__ constexpr Powers kPowers;
+template <int THREADS> __device__ __forceinline__ void take_powers(uint64_t (&to)[kParts]) {
+    for (int j = threadIdx.x; j < kParts; j += THREADS) to[j] = kPowers.bits[j];
+}
+__device__ __forceinline__ void weights_of(const float* l, float top, Heat heat, const uint64_t* powers, double (&w)[4]) {
+    const double scale = heat.scale * kParts, whole = 6755399441055744.0;
+    double f[4];
+    uint64_t power[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const double d = fmax((double)l[e] - (double)top, heat.least), t = fma(d, scale, whole);
+        f[e] = fma(d, scale, whole - t);
+        const uint32_t n = (uint32_t)__double_as_longlong(t);
+        power[e] = powers[n & (kParts - 1)];
+        w[e] = __longlong_as_double((long long)((uint64_t)(n << 12) << 32));
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        double y = 3.3083029837113951e-09;
+        y = fma(y, f[e], 3.6655661567589336e-06);
+        y = fma(y, f[e], 0.0027076061740622767);
+        y = fma(y, f[e], 0.99999999999998246);
+        w[e] = __longlong_as_double((long long)(power[e] + (uint64_t)__double_as_longlong(w[e]))) * y;
+    }
 }
 
 template <typename T> struct Raw;
@@ -110,24 +181,51 @@ __device__ __forceinline__ void elements(const void* p, int64_t row, int v, int 
     }
 }
 
-__device__ __forceinline__ double wave_sum(double x) {
-#pragma unroll
-    for (int k = 1; k < 64; k <<= 1) x += __shfl_xor(x, k);
-    return x;
+// What 1, 2, 4 and 8 lanes before have, then lane 15 of a row for rows 1 and 3, then lane 31 for rows 2 and 3; `none` where there is no such lane.  After all six steps lane 63
+// has met all of them.
+template <int STEP> __device__ __forceinline__ int lane_before(int none, int x) {
+    constexpr int CTRL[6] = {0x111, 0x112, 0x114, 0x118, 0x142, 0x143}, ROWS[6] = {0xf, 0xf, 0xf, 0xf, 0xa, 0xc};
+    return __builtin_amdgcn_update_dpp(none, x, CTRL[STEP], ROWS[STEP], 0xf, false);
 }
+template <int STEP> __device__ __forceinline__ double lane_before(double x) {
+    const long long y = __double_as_longlong(x);
+    return __hiloint2double(lane_before<STEP>(0, (int)(y >> 32)), lane_before<STEP>(0, (int)y));
+}
+template <int STEP> __device__ __forceinline__ float lane_before(float x) {
+    return __int_as_float(lane_before<STEP>(__float_as_int(x), __float_as_int(x)));
+}
+// Sum of the lanes up to this one
+__device__ __forceinline__ double sum_up_to(double x) {
+    x += lane_before<0>(x);
+    x += lane_before<1>(x);
+    x += lane_before<2>(x);
+    x += lane_before<3>(x);
+    x += lane_before<4>(x);
+    return x + lane_before<5>(x);
+}
+__device__ __forceinline__ double of_lane(double x, int lane) {
+    const long long y = __double_as_longlong(x);
+    return __hiloint2double(__builtin_amdgcn_readlane((int)(y >> 32), lane), __builtin_amdgcn_readlane((int)y, lane));
+}
+__device__ __forceinline__ double wave_sum(double x) { return of_lane(sum_up_to(x), 63); }
 __device__ __forceinline__ float wave_max(float x) {
-#pragma unroll
-    for (int k = 1; k < 64; k <<= 1) x = fmaxf(x, __shfl_xor(x, k));
-    return x;
+    x = fmaxf(x, lane_before<0>(x));
+    x = fmaxf(x, lane_before<1>(x));
+    x = fmaxf(x, lane_before<2>(x));
+    x = fmaxf(x, lane_before<3>(x));
+    x = fmaxf(x, lane_before<4>(x));
+    x = fmaxf(x, lane_before<5>(x));
+    return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), 63));
 }
 __device__ __forceinline__ int wave_min(int x) {
-#pragma unroll
-    for (int k = 1; k < 64; k <<= 1) x = min(x, __shfl_xor(x, k));
-    return x;
+    x = min(x, lane_before<0>(x, x));
+    x = min(x, lane_before<1>(x, x));
+    x = min(x, lane_before<2>(x, x));
+    x = min(x, lane_before<3>(x, x));
+    x = min(x, lane_before<4>(x, x));
+    x = min(x, lane_before<5>(x, x));
+    return __builtin_amdgcn_readlane(x, 63);
 }
-
-// log2(e) / temperature; 0 where the sequence takes the largest logit (a temperature of 0, below, or NaN)
-__device__ __forceinline__ double heat_of(float t) { return t > 0.0f ? 1.4426950408889634 / (double)t : -1.0; }
 
 // ---- sums of chunks -----------------------------------------------------------------------------
 //
@@ -135,36 +233,41 @@ __device__ __forceinline__ double heat_of(float t) { return t > 0.0f ? 1.4426950
 template <typename T>
 __global__ __launch_bounds__(kStatThreads) void verify_stats_kernel(VerifyRun r) {
     constexpr int E = Elements<T>::E, W = kStatThreads / kWave;
+    __shared__ uint64_t powers[kParts];
     __shared__ float tops[W];
     __shared__ double sums[W];
     __shared__ int places[W];
-    __shared__ int owner;
     const VerifyArgs& a = r.a;
     const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, v0 = blockIdx.x * kChunk;
     const float ninf = -__builtin_inff();
+    take_powers<kStatThreads>(powers);
     for (int t = blockIdx.y; t < a.T; t += gridDim.y) {
+        // (with temperatures: whose row it is; every wavefront looks for itself)
+        Heat heat = heat_of(1.0f);
+        if (a.temperature != nullptr) {
+            int owner = -1;
+            for (int b0 = 0; b0 < a.B && owner < 0; b0 += kWave) {
+                const int b = min(b0 + lane, a.B - 1), row0 = max(a.q_start[b], 0);
+                const uint64_t mine = __builtin_amdgcn_ballot_w64(t >= row0 && t < row0 + tokens_of(row0, a.q_start[b + 1], a.T));
+                if (mine != 0) owner = min(b0 + __builtin_ctzll(mine), a.B - 1);
+            }
+            if (owner < 0) continue;                     // (the same in every wavefront)
+            heat = heat_of(a.temperature[owner]);
+        }
         float x[kEach];
 #pragma unroll
         for (int k = 0; k < kEach / E; ++k) {
             float y[E];
             elements<T, E>(a.logits, (int64_t)t * a.logits_stride, v0 + E * (kStatThreads * k + tid), a.V, ninf, y);
 #pragma unroll
-            for (int e = 0; e < E; ++e) x[E * k + e] = clean(y[e]);
+            for (int e = 0; e < E; ++e) x[E * k + e] = y[e];
         }
-        double heat = 1.4426950408889634;
-        if (a.temperature != nullptr) {
-            if (tid == 0) owner = a.B;
-            __syncthreads();
-            for (int b = tid; b < a.B; b += kStatThreads) {
-                const int row0 = max(a.q_start[b], 0);
-                if (t >= row0 && t < row0 + tokens_of(row0, a.q_start[b + 1], a.T)) atomicMin(&owner, b);
-            }
-            __syncthreads();
-            if (owner == a.B) {                          // (the same in every thread)
-                __syncthreads();
-                continue;
-            }
-            heat = heat_of(a.temperature[owner]);
+        bool odd = false;
+#pragma unroll
+        for (int e = 0; e < kEach; ++e) odd |= is_odd(x[e]);
+        if (__builtin_amdgcn_ballot_w64(odd) != 0) {
+#pragma unroll
+            for (int e = 0; e < kEach; ++e) x[e] = clean(x[e]);
         }
         float top = x[0];
 #pragma unroll
@@ -177,9 +280,13 @@ __global__ __launch_bounds__(kStatThreads) void verify_stats_kernel(VerifyRun r)
         for (int w = 1; w < W; ++w) top = fmaxf(top, tops[w]);
         double sum = 0.0;
         int at = 0x7fffffff;
-        if (heat >= 0.0) {
+        if (heat.scale >= 0.0) {
 #pragma unroll
-            for (int e = 0; e < kEach; ++e) sum += weight_of(x[e], top, heat);
+            for (int e = 0; e < kEach; e += 4) {
+                double w[4];
+                weights_of(x + e, top, heat, powers, w);
+                sum += (w[0] + w[1]) + (w[2] + w[3]);
+            }
             sum = wave_sum(sum);
         } else {
 #pragma unroll
@@ -208,16 +315,6 @@ __global__ __launch_bounds__(kStatThreads) void verify_stats_kernel(VerifyRun r)
 
 // ---- the walk -----------------------------------------------------------------------------------
 
-// What is left behind the present token: max(scale w - by q, 0) for the weights w of its row; without q the weights but those of
-// the tokens refused.
-struct Rest {
-    int row;            // row of the packed tensors
-    float top;
-    double heat;
-    double scale, by;   // with q
-    int refused;        // without q: how many
-};
-
 struct WalkShared {
     double part[kWalkWaves];
     int found[kWalkWaves];
@@ -239,13 +336,19 @@ __device__ __forceinline__ double block_sum(double x, double* part) {
 
 // The weights of 4 tokens from v on
 template <typename T, typename Q>
-__device__ __forceinline__ void rest_of(const VerifyRun& r, const Rest& s, const int* refused, int v, double (&w)[4]) {
+__device__ __forceinline__ void rest_of(const VerifyRun& r, const Rest& s, const int* refused, int v, double (&w)[4], const uint64_t* powers = nullptr) {
     const VerifyArgs& a = r.a;
     float x[4], q[4];
     elements<T, 4>(a.logits, (int64_t)s.row * a.logits_stride, v, a.V, -__builtin_inff(), x);
     if (a.draft != nullptr) elements<Q, 4>(a.draft, (int64_t)s.row * a.draft_stride, v, a.V, 0.0f, q);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) w[e] = weight_of(clean(x[e]), s.top, s.heat);
+    for (int e = 0; e < 4; ++e) x[e] = clean(x[e]);
+    if (powers != nullptr) {
+        weights_of(x, s.top, s.heat, powers, w);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w[e] = weight_of(x[e], s.top, s.heat);
+    }
     if (a.draft != nullptr) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) w[e] = fmax(s.scale * w[e] - s.by * (double)(q[e] > 0.0f ? q[e] : 0.0f), 0.0);
@@ -256,6 +359,129 @@ __device__ __forceinline__ void rest_of(const VerifyRun& r, const Rest& s, const
             for (int e = 0; e < 4; ++e) w[e] = v + e == x0 ? 0.0 : w[e];
         }
     }
+}
+
+// The next token, drawn from what is left where the walk has ended; by the whole workgroup.
+template <typename T, typename Q>
+__device__ __forceinline__ void draw_next(const VerifyRun& r, int b, int row0, const WalkEnd& end, double* chunk_sums, WalkShared& sh) {
+    const VerifyArgs& a = r.a;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const bool plain = a.draft == nullptr;
+    const int* const list = r.refused + row0;
+    Rest rest = end.rest;
+    const int row = rest.row;
+    const RowStat s = r.rows[row];
+    double total = 0.0;
+    for (int turn = 0;; ++turn) {
+        // sums of the chunks
+        __syncthreads();
+        if (plain || rest.by == 0.0) {
+            const ChunkStat* of = r.chunks + (size_t)row * r.nc;
+            for (int c = tid; c < r.nc; c += kWalkThreads) chunk_sums[c] = of[c].sum * weight_of(of[c].top, s.top, rest.heat) * (plain ? 1.0 : rest.scale);
+            __syncthreads();
+            for (int k = 0; k < (plain ? rest.refused : 0); ++k) {       // chunks that lack a token are summed again
+                const int c = list[k] / kChunk;
+                double w[4];
+                rest_of<T, Q>(r, rest, list, c * kChunk + 4 * tid, w);
+                const double sum = block_sum((w[0] + w[1]) + (w[2] + w[3]), sh.part);
+                if (tid == 0) chunk_sums[c] = sum;
+            }
+        } else if (turn == 0) {
+            for (int c = tid; c < r.nc; c += kWalkThreads) chunk_sums[c] = r.left[(size_t)row0 * r.nc + c];
+        } else {
+            for (int c = wave; c < r.nc; c += kWalkWaves) {
+                double sum = 0.0;
+#pragma unroll 4
+                for (int k = 0; k < kChunk / 256; ++k) {
+                    const int v = c * kChunk + 256 * k + 4 * lane;
+                    if (v >= a.V) continue;
+                    double w[4];
+                    rest_of<T, Q>(r, rest, list, v, w);
+                    sum += (w[0] + w[1]) + (w[2] + w[3]);
+                }
+                sum = wave_sum(sum);
+                if (lane == 0) chunk_sums[c] = sum;
+            }
+        }
+        __syncthreads();
+        double mine = 0.0;
+        for (int c = tid; c < r.nc; c += kWalkThreads) mine += chunk_sums[c];
+        total = block_sum(mine, sh.part);
+        if (total > 0.0 || turn == 1 || !end.open) break;
+        rest.scale = end.old_scale / s.sum;      // nothing is left: r as it was before the last refusal
+        rest.by = end.old_by;
+    }
+    // the chunk with the wanted place: the first up to which the sum passes it, or the last that has any
+    if (wave == 0) {
+        const double place = (double)a.uniform[row0] * total;
+        double before_sum = 0.0, left = 0.0;
+        int chunk = -1, last = -1;
+        double last_before = 0.0;
+        for (int c0 = 0; c0 < r.nc && chunk < 0; c0 += kWave) {
+            const int c = c0 + lane;
+            const double sum = c < r.nc ? chunk_sums[c] : 0.0;
+            const double upto = sum_up_to(sum) + before_sum;
+            const uint64_t over = __builtin_amdgcn_ballot_w64(sum > 0.0 && upto > place), any = __builtin_amdgcn_ballot_w64(sum > 0.0);
+            if (any != 0) {
+                const int k = 63 - __builtin_clzll(any);
+                last = c0 + k;
+                last_before = __shfl(upto - sum, k);
+            }
+            if (over != 0) {
+                const int k = __builtin_ctzll(over);
+                chunk = c0 + k;
+                left = place - __shfl(upto - sum, k);
+            }
+            before_sum = __shfl(upto, 63);
+        }
+        if (chunk < 0) {
+            chunk = last;
+            left = place - last_before;
+        }
+        if (lane == 0) {
+            sh.found[0] = chunk;
+            sh.sum = left;
+        }
+    }
+    __syncthreads();
+    const int chunk = sh.found[0];
+    const double left = sh.sum;
+    __syncthreads();
+    if (chunk < 0) {
+        if (tid == 0) a.next[b] = -1;
+        return;
+    }
+    double w[4];
+    const int v = chunk * kChunk + 4 * tid;
+    rest_of<T, Q>(r, rest, list, v, w);
+    const double own = (w[0] + w[1]) + (w[2] + w[3]);
+    const double upto = sum_up_to(own);
+    if (lane == 63) sh.part[wave] = upto;
+    __syncthreads();
+    double sum = upto - own;
+#pragma unroll
+    for (int k = 0; k < kWalkWaves; ++k) sum += k < wave ? sh.part[k] : 0.0;
+    int first = 0x7fffffff, last = -1;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        sum += w[e];
+        if (w[e] > 0.0) {
+            last = v + e;
+            if (sum > left) first = min(first, v + e);
+        }
+    }
+    first = wave_min(first);
+    last = -wave_min(-last);
+    if (lane == 0) sh.found[wave] = first;
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < kWalkWaves; ++k) first = min(first, sh.found[k]);
+    __syncthreads();
+    if (lane == 0) sh.found[wave] = last;
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < kWalkWaves; ++k) last = max(last, sh.found[k]);
+    if (tid == 0) a.next[b] = first != 0x7fffffff ? first : last;
 }
 
 // A workgroup per sequence.
@@ -275,7 +501,7 @@ __global__ __launch_bounds__(kWalkThreads) void verify_walk_kernel(VerifyRun r) 
         }
         return;
     }
-    const double heat = a.temperature != nullptr ? heat_of(a.temperature[b]) : 1.4426950408889634;
+    const Heat heat = heat_of(a.temperature != nullptr ? a.temperature[b] : 1.0f);
     const float ninf = -__builtin_inff();
 
     // rows: their chunks joined, a wavefront each
@@ -288,7 +514,7 @@ __global__ __launch_bounds__(kWalkThreads) void verify_walk_kernel(VerifyRun r) 
         int at = 0x7fffffff;
         for (int c = lane; c < r.nc; c += kWave) {
             const ChunkStat s = of[c];
-            if (heat >= 0.0) sum += s.sum * weight_of(s.top, top, heat);
+            if (heat.scale >= 0.0) sum += s.sum * weight_of(s.top, top, heat);
             else if (s.top == top) at = min(at, s.at);
         }
         sum = wave_sum(sum);
@@ -308,7 +534,7 @@ __global__ __launch_bounds__(kWalkThreads) void verify_walk_kernel(VerifyRun r) 
         if (before >= 0 && before < i && x >= 0 && x < a.V) {
             const RowStat s = r.rows[row0 + before];
             const int64_t t = row0 + before;
-            if (heat < 0.0) p = x == s.at ? 1.0 : 0.0;
+            if (heat.scale < 0.0) p = x == s.at ? 1.0 : 0.0;
             else if (s.top != ninf) p = weight_of(clean(Elements<T>::one(a.logits, t * a.logits_stride + x)), s.top, heat) / s.sum;
             if (a.draft != nullptr) {
                 const float d = Elements<Q>::one(a.draft, t * a.draft_stride + x);
@@ -367,7 +593,7 @@ __global__ __launch_bounds__(kWalkThreads) void verify_walk_kernel(VerifyRun r) 
                 const float uk = __shfl(u, k);
                 double rk = pk;
                 bool twice = false;
-                if (heat >= 0.0) {
+                if (heat.scale >= 0.0) {
                     if (a.draft != nullptr) {
                         rk = fmax(scale * pk - by * qk, 0.0);
                     } else {
@@ -383,7 +609,7 @@ __global__ __launch_bounds__(kWalkThreads) void verify_walk_kernel(VerifyRun r) 
                     refused = 0;
                     scale = 1.0;
                     by = 0.0;
-                } else if (heat >= 0.0) {
+                } else if (heat.scale >= 0.0) {
                     if (a.draft != nullptr) {
                         want_scale = scale;
                         want_by = by + 1.0;
@@ -423,144 +649,70 @@ __global__ __launch_bounds__(kWalkThreads) void verify_walk_kernel(VerifyRun r) 
     }
 
     // ---- the next token
-    Rest rest = sh.rest;
+    WalkEnd end;
+    end.rest = sh.rest;
     __syncthreads();                         // (what the first wavefront writes now has been read)
     if (wave == 0 && lane == 0) {
         a.n_keep[b] = kept;
-        sh.sum = open ? scale : 0.0;
+        sh.sum = scale;
         sh.part[0] = by;
         sh.ask = open;
     }
     __syncthreads();
-    const bool was_open = sh.ask != 0;
-    const double old_scale = sh.sum, old_by = sh.part[0];
-    const int row = rest.row;
-    const RowStat s = r.rows[row];
-    if (heat < 0.0 || s.top == ninf) {
-        if (tid == 0) a.next[b] = s.top == ninf ? -1 : s.at;
+    end.open = sh.ask;
+    end.old_scale = sh.sum;
+    end.old_by = sh.part[0];
+    const RowStat s = r.rows[end.rest.row];
+    end.draw = heat.scale >= 0.0 && s.top != ninf;
+    if (!end.draw && tid == 0) a.next[b] = s.top == ninf ? -1 : s.at;
+    if (a.draft != nullptr) {
+        if (tid == 0) r.ends[row0] = end;
         return;
     }
-    const bool plain = a.draft == nullptr;
-    double total = 0.0;
-    for (int turn = 0;; ++turn) {
-        // sums of the chunks
+    if (end.draw) draw_next<T, Q>(r, b, row0, end, chunk_sums, sh);
+}
+
+// With the drafts' probabilities: sums of what is left over a chunk of a sequence's row.
+template <typename T, typename Q>
+__global__ __launch_bounds__(kStatThreads) void verify_left_kernel(VerifyRun r) {
+    __shared__ uint64_t powers[kParts];
+    __shared__ double part[kStatThreads / kWave];
+    const VerifyArgs& a = r.a;
+    const int tid = threadIdx.x;
+    take_powers<kStatThreads>(powers);
+    __syncthreads();
+    for (int b = blockIdx.y; b < a.B; b += gridDim.y) {
+        const int row0 = max(a.q_start[b], 0);
+        if (tokens_of(row0, a.q_start[b + 1], a.T) == 0) continue;
+        const WalkEnd end = r.ends[row0];
+        if (!end.draw || end.rest.by == 0.0) continue;
+        double sum = 0.0;
+#pragma unroll
+        for (int k = 0; k < kEach / 4; ++k) {
+            double w[4];
+            rest_of<T, Q>(r, end.rest, nullptr, blockIdx.x * kChunk + 4 * (kStatThreads * k + tid), w, powers);
+            sum += (w[0] + w[1]) + (w[2] + w[3]);
+        }
+        sum = wave_sum(sum);
+        if ((tid & 63) == 0) part[tid >> 6] = sum;
         __syncthreads();
-        if (plain || rest.by == 0.0) {
-            const ChunkStat* of = r.chunks + (size_t)row * r.nc;
-            for (int c = tid; c < r.nc; c += kWalkThreads) chunk_sums[c] = of[c].sum * weight_of(of[c].top, s.top, heat) * (plain ? 1.0 : rest.scale);
-            __syncthreads();
-            for (int k = 0; k < (plain ? rest.refused : 0); ++k) {       // chunks that lack a token are summed again
-                const int c = list[k] / kChunk;
-                double w[4];
-                rest_of<T, Q>(r, rest, list, c * kChunk + 4 * tid, w);
-                const double sum = block_sum((w[0] + w[1]) + (w[2] + w[3]), sh.part);
-                if (tid == 0) chunk_sums[c] = sum;
-            }
-        } else {
-            for (int c = wave; c < r.nc; c += kWalkWaves) {
-                double sum = 0.0;
-#pragma unroll 4
-                for (int k = 0; k < kChunk / 256; ++k) {
-                    const int v = c * kChunk + 256 * k + 4 * lane;
-                    if (v >= a.V) continue;
-                    double w[4];
-                    rest_of<T, Q>(r, rest, list, v, w);
-                    sum += (w[0] + w[1]) + (w[2] + w[3]);
-                }
-                sum = wave_sum(sum);
-                if (lane == 0) chunk_sums[c] = sum;
-            }
+        if (tid == 0) {
+#pragma unroll
+            for (int w = 1; w < kStatThreads / kWave; ++w) sum += part[w];
+            r.left[(size_t)row0 * r.nc + blockIdx.x] = sum;
         }
         __syncthreads();
-        double mine = 0.0;
-        for (int c = tid; c < r.nc; c += kWalkThreads) mine += chunk_sums[c];
-        total = block_sum(mine, sh.part);
-        if (total > 0.0 || turn == 1 || !was_open) break;
-        rest.scale = old_scale / s.sum;      // nothing is left: r as it was before the last refusal
-        rest.by = old_by;
     }
-    // the chunk with the wanted place: the first up to which the sum passes it, or the last that has any
-    if (wave == 0) {
-        const double place = (double)a.uniform[row0] * total;
-        double before_sum = 0.0, left = 0.0;
-        int chunk = -1, last = -1;
-        double last_before = 0.0;
-        for (int c0 = 0; c0 < r.nc && chunk < 0; c0 += kWave) {
-            const int c = c0 + lane;
-            const double sum = c < r.nc ? chunk_sums[c] : 0.0;
-            double upto = sum;
-#pragma unroll
-            for (int k = 1; k < 64; k <<= 1) {
-                const double y = __shfl_up(upto, k);
-                if (lane >= k) upto += y;
-            }
-            upto += before_sum;
-            const uint64_t over = __builtin_amdgcn_ballot_w64(sum > 0.0 && upto > place), any = __builtin_amdgcn_ballot_w64(sum > 0.0);
-            if (any != 0) {
-                const int k = 63 - __builtin_clzll(any);
-                last = c0 + k;
-                last_before = __shfl(upto - sum, k);
-            }
-            if (over != 0) {
-                const int k = __builtin_ctzll(over);
-                chunk = c0 + k;
-                left = place - __shfl(upto - sum, k);
-            }
-            before_sum = __shfl(upto, 63);
-        }
-        if (chunk < 0) {
-            chunk = last;
-            left = place - last_before;
-        }
-        if (lane == 0) {
-            sh.found[0] = chunk;
-            sh.sum = left;
-        }
-    }
-    __syncthreads();
-    const int chunk = sh.found[0];
-    const double left = sh.sum;
-    __syncthreads();
-    if (chunk < 0) {
-        if (tid == 0) a.next[b] = -1;
-        return;
-    }
-    double w[4];
-    const int v = chunk * kChunk + 4 * tid;
-    rest_of<T, Q>(r, rest, list, v, w);
-    const double own = (w[0] + w[1]) + (w[2] + w[3]);
-    double upto = own;
-#pragma unroll
-    for (int k = 1; k < 64; k <<= 1) {
-        const double y = __shfl_up(upto, k);
-        if (lane >= k) upto += y;
-    }
-    if (lane == 63) sh.part[wave] = upto;
-    __syncthreads();
-    double sum = upto - own;
-#pragma unroll
-    for (int k = 0; k < kWalkWaves; ++k) sum += k < wave ? sh.part[k] : 0.0;
-    int first = 0x7fffffff, last = -1;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        sum += w[e];
-        if (w[e] > 0.0) {
-            last = v + e;
-            if (sum > left) first = min(first, v + e);
-        }
-    }
-    first = wave_min(first);
-    last = -wave_min(-last);
-    if (lane == 0) sh.found[wave] = first;
-    __syncthreads();
-#pragma unroll
-    for (int k = 0; k < kWalkWaves; ++k) first = min(first, sh.found[k]);
-    __syncthreads();
-    if (lane == 0) sh.found[wave] = last;
-    __syncthreads();
-#pragma unroll
-    for (int k = 0; k < kWalkWaves; ++k) last = max(last, sh.found[k]);
-    if (tid == 0) a.next[b] = first != 0x7fffffff ? first : last;
+}
+// And the next token.
+template <typename T, typename Q>
+__global__ __launch_bounds__(kWalkThreads) void verify_draw_kernel(VerifyRun r) {
+    extern __shared__ double chunk_sums[];               // [nc]
+    __shared__ WalkShared sh;
+    const int b = blockIdx.x, row0 = max(r.a.q_start[b], 0);
+    if (tokens_of(row0, r.a.q_start[b + 1], r.a.T) == 0) return;
+    const WalkEnd end = r.ends[row0];
+    if (end.draw) draw_next<T, Q>(r, b, row0, end, chunk_sums, sh);
 }
 
 // ---- host ---------------------------------------------------------------------------------------
@@ -568,7 +720,21 @@ __global__ __launch_bounds__(kWalkThreads) void verify_walk_kernel(VerifyRun r) 
 static int chunks_of(int V) { return (V + kChunk - 1) / kChunk; }
 
 size_t verify_workspace(int T, int V) {
-    return (size_t)T * ((size_t)chunks_of(V) * sizeof(ChunkStat) + sizeof(RowStat) + 8);
+    return (size_t)T * ((size_t)chunks_of(V) * (sizeof(ChunkStat) + sizeof(double)) + sizeof(RowStat) + sizeof(WalkEnd) + 8);
+}
+
+template <typename T, typename Q>
+static hipError_t launch_walk(const VerifyRun& r, hipStream_t st) {
+    const dim3 seqs((unsigned)r.a.B), block(kWalkThreads);
+    const size_t lds = (size_t)r.nc * sizeof(double);
+    hipLaunchKernelGGL((verify_walk_kernel<T, Q>), seqs, block, lds, st, r);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess || r.a.draft == nullptr || r.a.T == 0) return e;
+    hipLaunchKernelGGL((verify_left_kernel<T, Q>), dim3((unsigned)r.nc, (unsigned)(r.a.B < 65535 ? r.a.B : 65535)), dim3(kStatThreads), 0, st, r);
+    e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL((verify_draw_kernel<T, Q>), seqs, block, lds, st, r);
+    return hipGetLastError();
 }
 
 template <typename T>
@@ -579,14 +745,11 @@ static hipError_t launch_verify_t(const VerifyRun& r, hipStream_t st) {
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
-    const dim3 seqs((unsigned)r.a.B), block(kWalkThreads);
-    const size_t lds = (size_t)r.nc * sizeof(double);
     switch (r.a.draft_dtype) {
-    case 0: hipLaunchKernelGGL((verify_walk_kernel<T, F32>), seqs, block, lds, st, r); break;
-    case 1: hipLaunchKernelGGL((verify_walk_kernel<T, F16>), seqs, block, lds, st, r); break;
-    default: hipLaunchKernelGGL((verify_walk_kernel<T, BF16>), seqs, block, lds, st, r); break;
+    case 0: return launch_walk<T, F32>(r, st);
+    case 1: return launch_walk<T, F16>(r, st);
+    default: return launch_walk<T, BF16>(r, st);
     }
-    return hipGetLastError();
 }
 
 hipError_t launch_verify(const VerifyArgs& a, void* ws, hipStream_t st) {
@@ -595,7 +758,9 @@ hipError_t launch_verify(const VerifyArgs& a, void* ws, hipStream_t st) {
     r.nc = chunks_of(a.V);
     r.chunks = static_cast<ChunkStat*>(ws);
     r.rows = reinterpret_cast<RowStat*>(r.chunks + (size_t)a.T * r.nc);
-    r.refused = reinterpret_cast<int*>(r.rows + a.T);
+    r.ends = reinterpret_cast<WalkEnd*>(r.rows + a.T);
+    r.left = reinterpret_cast<double*>(r.ends + a.T);
+    r.refused = reinterpret_cast<int*>(r.left + (size_t)a.T * r.nc);
     switch (a.dtype) {
     case 0: return launch_verify_t<F32>(r, st);
     case 1: return launch_verify_t<F16>(r, st);
