@@ -59,6 +59,7 @@ struct Rest {
 // Where a sequence's walk has ended
 struct WalkEnd {
     Rest rest;
+    RowStat row;        // of the rest
     double old_scale, old_by;   // of what was left before the last refusal, if that has not been divided by its sum
     int open;
     int draw;           // 0: the next token is known
@@ -77,6 +78,12 @@ struct VerifyRun {
 // ---- numbers ------------------------------------------------------------------------------------
 
 // A logit as it counts: NaN like -infinity, +infinity like the largest number.
+// The largest of three numbers, none of them NaN.  (The compiler, which cannot know that, has each operand of fmaxf go through an instruction of its own.)
+__device__ __forceinline__ float max3(float x, float y, float z) {
+    float m;
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(m) : "v"(x), "v"(y), "v"(z));
+    return m;
+}
 __device__ __forceinline__ bool is_odd(float x) { return __builtin_amdgcn_classf(x, 0x203); }        // NaN or +infinity
 __device__ __forceinline__ float clean(float x) {
     return x != x ? -__builtin_inff() : fminf(x, 3.4028234663852886e38f);
@@ -124,6 +131,7 @@ template <int THREADS> __device__ __forceinline__ void take_powers(uint64_t (&to
 __device__ __forceinline__ void weights_of(const float* l, float top, Heat heat, const uint64_t* powers, double (&w)[4]) {
     const double scale = heat.scale * kParts, whole = 6755399441055744.0;
     double f[4];
+    uint32_t lift[4];
     uint64_t power[4];
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
@@ -131,7 +139,7 @@ __device__ __forceinline__ void weights_of(const float* l, float top, Heat heat,
         f[e] = fma(d, scale, whole - t);
         const uint32_t n = (uint32_t)__double_as_longlong(t);
         power[e] = powers[n & (kParts - 1)];
-        w[e] = __longlong_as_double((long long)((uint64_t)(n << 12) << 32));
+        lift[e] = n << 12;
     }
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
@@ -139,7 +147,7 @@ __device__ __forceinline__ void weights_of(const float* l, float top, Heat heat,
         y = fma(y, f[e], 3.6655661567589336e-06);
         y = fma(y, f[e], 0.0027076061740622767);
         y = fma(y, f[e], 0.99999999999998246);
-        w[e] = __longlong_as_double((long long)(power[e] + (uint64_t)__double_as_longlong(w[e]))) * y;
+        w[e] = __hiloint2double((int)((uint32_t)(power[e] >> 32) + lift[e]), (int)(uint32_t)power[e]) * y;
     }
 }
 
@@ -229,7 +237,8 @@ __device__ __forceinline__ int wave_min(int x) {
 
 // ---- sums of chunks -----------------------------------------------------------------------------
 //
-// A workgroup per chunk and row.
+// A workgroup per chunk and row.  f32 logits come at 5.1 TB/s (8 x 31 rows of 100003: 19 us); of 16 bits the sums of 64 bits take as long again: 84 MB of bf16, 320 rows of 131072,
+// 30 us, of which 18 without the exponentials.  (Workgroups that take several chunks, reading the next while they sum the present one: 32 us, and 23 for the f32.)
 template <typename T>
 __global__ __launch_bounds__(kStatThreads) void verify_stats_kernel(VerifyRun r) {
     constexpr int E = Elements<T>::E, W = kStatThreads / kWave;
@@ -269,25 +278,28 @@ __global__ __launch_bounds__(kStatThreads) void verify_stats_kernel(VerifyRun r)
 #pragma unroll
             for (int e = 0; e < kEach; ++e) x[e] = clean(x[e]);
         }
-        float top = x[0];
+        float top = ninf;
 #pragma unroll
-        for (int e = 1; e < kEach; ++e) top = fmaxf(top, x[e]);
+        for (int e = 0; e < kEach; e += 2) top = max3(top, x[e], x[e + 1]);
         top = wave_max(top);
         if (lane == 0) tops[wave] = top;
         __syncthreads();
         top = tops[0];
 #pragma unroll
         for (int w = 1; w < W; ++w) top = fmaxf(top, tops[w]);
-        double sum = 0.0;
+        double sum = 0.0, odd_sum = 0.0;
         int at = 0x7fffffff;
         if (heat.scale >= 0.0) {
 #pragma unroll
             for (int e = 0; e < kEach; e += 4) {
                 double w[4];
                 weights_of(x + e, top, heat, powers, w);
-                sum += (w[0] + w[1]) + (w[2] + w[3]);
+                sum += w[0];
+                odd_sum += w[1];
+                sum += w[2];
+                odd_sum += w[3];
             }
-            sum = wave_sum(sum);
+            sum = wave_sum(sum + odd_sum);
         } else {
 #pragma unroll
             for (int k = kEach / E - 1; k >= 0; --k)
@@ -315,7 +327,12 @@ __global__ __launch_bounds__(kStatThreads) void verify_stats_kernel(VerifyRun r)
 
 // ---- the walk -----------------------------------------------------------------------------------
 
+constexpr int kNear = 256;               // rows and refused tokens of a sequence that have a place in LDS
+
 struct WalkShared {
+    RowStat rows[kNear];
+    int list[kNear];
+    double weight[kNear];   // of a refused token
     double part[kWalkWaves];
     int found[kWalkWaves];
     Rest rest;
@@ -334,9 +351,20 @@ __device__ __forceinline__ double block_sum(double x, double* part) {
     return s;
 }
 
+// The refused tokens, the first ones in LDS
+struct Refused {
+    int* near;
+    int* far;
+    __device__ __forceinline__ int operator[](int k) const { return k < kNear ? near[k] : far[k]; }
+    __device__ __forceinline__ void put(int k, int x) const {
+        if (k < kNear) near[k] = x;
+        else far[k] = x;
+    }
+};
+
 // The weights of 4 tokens from v on
 template <typename T, typename Q>
-__device__ __forceinline__ void rest_of(const VerifyRun& r, const Rest& s, const int* refused, int v, double (&w)[4], const uint64_t* powers = nullptr) {
+__device__ __forceinline__ void rest_of(const VerifyRun& r, const Rest& s, const Refused& refused, int v, double (&w)[4], const uint64_t* powers = nullptr) {
     const VerifyArgs& a = r.a;
     float x[4], q[4];
     elements<T, 4>(a.logits, (int64_t)s.row * a.logits_stride, v, a.V, -__builtin_inff(), x);
@@ -367,24 +395,58 @@ __device__ __forceinline__ void draw_next(const VerifyRun& r, int b, int row0, c
     const VerifyArgs& a = r.a;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const bool plain = a.draft == nullptr;
-    const int* const list = r.refused + row0;
+    const Refused list{sh.list, r.refused + row0};
     Rest rest = end.rest;
     const int row = rest.row;
-    const RowStat s = r.rows[row];
+    const RowStat s = end.row;
     double total = 0.0;
     for (int turn = 0;; ++turn) {
         // sums of the chunks
         __syncthreads();
         if (plain || rest.by == 0.0) {
             const ChunkStat* of = r.chunks + (size_t)row * r.nc;
-            for (int c = tid; c < r.nc; c += kWalkThreads) chunk_sums[c] = of[c].sum * weight_of(of[c].top, s.top, rest.heat) * (plain ? 1.0 : rest.scale);
-            __syncthreads();
-            for (int k = 0; k < (plain ? rest.refused : 0); ++k) {       // chunks that lack a token are summed again
-                const int c = list[k] / kChunk;
-                double w[4];
-                rest_of<T, Q>(r, rest, list, c * kChunk + 4 * tid, w);
-                const double sum = block_sum((w[0] + w[1]) + (w[2] + w[3]), sh.part);
-                if (tid == 0) chunk_sums[c] = sum;
+            // A chunk lacks its refused tokens: their weights are taken off its sum, unless they are most of it; then what is left is summed again.
+            const int refused = plain ? rest.refused : 0;
+            bool again = refused > kNear;
+            for (int c = tid; c < r.nc; c += kWalkThreads) {
+                const double sum = of[c].sum * weight_of(of[c].top, s.top, rest.heat) * (plain ? 1.0 : rest.scale);
+                double off = 0.0;
+                for (int k = 0; k < min(refused, kNear); ++k) off += list[k] / kChunk == c ? sh.weight[k] : 0.0;
+                const bool most = off > 0.5 * sum || refused > kNear;
+                chunk_sums[c] = most ? -1.0 : sum - off;
+                again |= most;
+            }
+            if (__syncthreads_or(again)) {
+                // four chunks at a time
+                constexpr int PARTS = kWalkWaves / 4, EACH = kChunk / (4 * kWave * PARTS);
+                for (int k0 = 0; k0 < refused; k0 += 4) {
+                    const int k = k0 + wave / PARTS;
+                    if (k < refused) {
+                        const int v = list[k] / kChunk * kChunk + 4 * (kWave * (wave % PARTS) + lane);
+                        double sum = 0.0;
+#pragma unroll
+                        for (int e = 0; e < EACH; ++e) {
+                            double w[4];
+                            rest_of<T, Q>(r, rest, list, v + e * 4 * kWave * PARTS, w);
+                            sum += (w[0] + w[1]) + (w[2] + w[3]);
+                        }
+                        sum = wave_sum(sum);
+                        if (lane == 0) sh.part[wave] = sum;
+                    }
+                    __syncthreads();
+                    if (k < refused && wave % PARTS == 0 && lane == 0) {
+                        double sum = 0.0;
+#pragma unroll
+                        for (int e = 0; e < PARTS; ++e) sum += sh.part[wave + e];
+                        chunk_sums[list[k] / kChunk] = sum;
+                    }
+                    __syncthreads();
+                }
+                // (of more refused tokens than have a place all of their chunks, and the others as they are)
+                if (refused > kNear) {
+                    for (int c = tid; c < r.nc; c += kWalkThreads)
+                        if (chunk_sums[c] < 0.0) chunk_sums[c] = of[c].sum * weight_of(of[c].top, s.top, rest.heat);
+                }
             }
         } else if (turn == 0) {
             for (int c = tid; c < r.nc; c += kWalkThreads) chunk_sums[c] = r.left[(size_t)row0 * r.nc + c];
@@ -504,23 +566,35 @@ __global__ __launch_bounds__(kWalkThreads) void verify_walk_kernel(VerifyRun r) 
     const Heat heat = heat_of(a.temperature != nullptr ? a.temperature[b] : 1.0f);
     const float ninf = -__builtin_inff();
 
+    // (read now, wanted later)
+    auto before_of = [&](int i) { return a.parent != nullptr ? a.parent[row0 + i] : i - 1; };
+    int before0 = -1, token0 = -1;
+    float u0 = 0.0f;
+    if (tid < n) {
+        if (tid > 0) before0 = before_of(tid);
+        token0 = a.tokens[row0 + tid];
+        u0 = a.uniform[row0 + tid];
+    }
+    auto row_of = [&](int i) { return i < kNear ? sh.rows + i : r.rows + row0 + i; };
+
     // rows: their chunks joined, a wavefront each
     for (int i = wave; i < n; i += kWalkWaves) {
         const ChunkStat* of = r.chunks + (size_t)(row0 + i) * r.nc;
-        float top = ninf;
-        for (int c = lane; c < r.nc; c += kWave) top = fmaxf(top, of[c].top);
+        const ChunkStat mine = lane < r.nc ? of[lane] : ChunkStat{0.0, ninf, 0x7fffffff};
+        float top = mine.top;
+        for (int c = kWave + lane; c < r.nc; c += kWave) top = fmaxf(top, of[c].top);
         top = wave_max(top);
         double sum = 0.0;
         int at = 0x7fffffff;
         for (int c = lane; c < r.nc; c += kWave) {
-            const ChunkStat s = of[c];
+            const ChunkStat s = c == lane ? mine : of[c];
             if (heat.scale >= 0.0) sum += s.sum * weight_of(s.top, top, heat);
             else if (s.top == top) at = min(at, s.at);
         }
         sum = wave_sum(sum);
         at = wave_min(at);
         if (lane == 0) {
-            RowStat* to = &r.rows[row0 + i];
+            RowStat* const to = row_of(i);
             to->sum = sum;
             to->top = top;
             to->at = top == ninf ? -1 : at;
@@ -528,11 +602,12 @@ __global__ __launch_bounds__(kWalkThreads) void verify_walk_kernel(VerifyRun r) 
     }
     __syncthreads();
     // tokens: their probabilities behind the one they continue
-    for (int i = 1 + tid; i < n; i += kWalkThreads) {
-        const int before = a.parent != nullptr ? a.parent[row0 + i] : i - 1, x = a.tokens[row0 + i];
+    for (int i = tid; i < n; i += kWalkThreads) {
+        if (i == 0) continue;
+        const int before = i == tid ? before0 : before_of(i), x = i == tid ? token0 : a.tokens[row0 + i];
         double p = 0.0, q = 1.0;
         if (before >= 0 && before < i && x >= 0 && x < a.V) {
-            const RowStat s = r.rows[row0 + before];
+            const RowStat s = *row_of(before);
             const int64_t t = row0 + before;
             if (heat.scale < 0.0) p = x == s.at ? 1.0 : 0.0;
             else if (s.top != ninf) p = weight_of(clean(Elements<T>::one(a.logits, t * a.logits_stride + x)), s.top, heat) / s.sum;
@@ -541,8 +616,9 @@ __global__ __launch_bounds__(kWalkThreads) void verify_walk_kernel(VerifyRun r) 
                 q = d > 0.0f ? (double)d : 0.0;
             }
         }
-        r.rows[row0 + i].p = p;
-        r.rows[row0 + i].q = q;
+        RowStat* const to = row_of(i);
+        to->p = p;
+        to->q = q;
     }
     __syncthreads();
 
@@ -552,7 +628,7 @@ __global__ __launch_bounds__(kWalkThreads) void verify_walk_kernel(VerifyRun r) 
     double scale = 1.0, by = 0.0;            // r = max(scale p - by q, 0); without q p / scale but for those refused
     double want_scale = 1.0, want_by = 0.0;  // r before it is divided by its sum
     bool open = false;                       // that sum is wanted for the next question
-    int* const list = r.refused + row0;
+    const Refused list{sh.list, r.refused + row0};
     int j0 = 0, done = 0;                    // the window of 64 tokens, and the tokens of it that are behind
     int before = -2, x = -1;
     double p = 0.0, q = 1.0;
@@ -566,11 +642,11 @@ __global__ __launch_bounds__(kWalkThreads) void verify_walk_kernel(VerifyRun r) 
                     const int i = j0 + lane;
                     before = -2;
                     if (i > 0 && i < n) {
-                        before = a.parent != nullptr ? a.parent[row0 + i] : i - 1;
-                        x = a.tokens[row0 + i];
-                        u = a.uniform[row0 + i];
-                        p = r.rows[row0 + i].p;
-                        q = r.rows[row0 + i].q;
+                        before = j0 == 0 ? before0 : before_of(i);
+                        x = j0 == 0 ? token0 : a.tokens[row0 + i];
+                        u = j0 == 0 ? u0 : a.uniform[row0 + i];
+                        p = row_of(i)->p;
+                        q = row_of(i)->q;
                         if (before >= i) before = -2;
                     }
                     load = false;
@@ -615,7 +691,10 @@ __global__ __launch_bounds__(kWalkThreads) void verify_walk_kernel(VerifyRun r) 
                         want_by = by + 1.0;
                         open = true;
                     } else if (!twice && token >= 0 && token < a.V && scale - pk > 0.0) {
-                        if (lane == 0) list[refused] = token;
+                        if (lane == 0) {
+                            list.put(refused, token);
+                            if (refused < kNear) sh.weight[refused] = pk * row_of(cur)->sum;
+                        }
                         __threadfence_block();
                         ++refused;
                         scale -= pk;
@@ -624,7 +703,7 @@ __global__ __launch_bounds__(kWalkThreads) void verify_walk_kernel(VerifyRun r) 
             }
             if (lane == 0) {
                 sh.ask = ask;
-                const RowStat s = r.rows[row0 + cur];
+                const RowStat s = *row_of(cur);
                 sh.rest = Rest{row0 + cur, s.top, heat, open ? want_scale / s.sum : scale / s.sum, open ? want_by : by, refused};
             }
         }
@@ -662,7 +741,8 @@ __global__ __launch_bounds__(kWalkThreads) void verify_walk_kernel(VerifyRun r) 
     end.open = sh.ask;
     end.old_scale = sh.sum;
     end.old_by = sh.part[0];
-    const RowStat s = r.rows[end.rest.row];
+    const RowStat s = *row_of(end.rest.row - row0);
+    end.row = s;
     end.draw = heat.scale >= 0.0 && s.top != ninf;
     if (!end.draw && tid == 0) a.next[b] = s.top == ninf ? -1 : s.at;
     if (a.draft != nullptr) {
@@ -690,7 +770,7 @@ __global__ __launch_bounds__(kStatThreads) void verify_left_kernel(VerifyRun r) 
 #pragma unroll
         for (int k = 0; k < kEach / 4; ++k) {
             double w[4];
-            rest_of<T, Q>(r, end.rest, nullptr, blockIdx.x * kChunk + 4 * (kStatThreads * k + tid), w, powers);
+            rest_of<T, Q>(r, end.rest, Refused{}, blockIdx.x * kChunk + 4 * (kStatThreads * k + tid), w, powers);
             sum += (w[0] + w[1]) + (w[2] + w[3]);
         }
         sum = wave_sum(sum);

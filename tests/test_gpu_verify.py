@@ -69,6 +69,19 @@ def test_many_tokens(n, draft):
     check(a, n)
 
 
+@pytest.mark.parametrize("n", [200, 330])
+@pytest.mark.parametrize("top", [0.0, 14.0])
+def test_refused_tokens_of_many_chunks(n, top):
+    """Fewer and more of them than have a place on the chip; with and without one that is most of its chunk."""
+    a = random_call([n, 2], 9001, BF16, True, None, seed=n)
+    a["parent"][:n] = 0
+    a["tokens"][:n] = (torch.arange(n) * 27 % 9001).to(torch.int32)
+    a["logits"][0, 27 * 5] += top
+    a["uniform"][1:n] = 0.99999994
+    _, kept, _ = check(a, 4)
+    assert kept[0] == 1
+
+
 def test_many_sequences():
     gen = torch.Generator().manual_seed(3)
     some = torch.randint(0, 4, (4096,), generator=gen).tolist()
