@@ -22,7 +22,6 @@ namespace flashd {
 constexpr int kScoreWaves = 8, kScoreThreads = kScoreWaves * kWave;
 constexpr int kScoreGroups = 256;       // workgroups of a launch: one per compute unit, two wavefronts per SIMD
 constexpr int kFewRows = 16;            // rows of a unit that the first kernel takes
-constexpr int kOwnTiles = 16;           // tiles of 32 rows up to which a wavefront takes a unit's turn by itself; of more the workgroup shares out the tiles
 constexpr int kBiasTiles = 128;         // tiles whose rows' bias lies in LDS
 constexpr int kScoreRuns = 128;         // runs of sequences
 
@@ -51,6 +50,8 @@ template <typename T, int D, bool FP8> struct ScoreCfg {
     static constexpr int QROW = D * QSZ, CH = QROW / 16;
     static constexpr int TILE = 32 * QROW;
     static constexpr int SLOTS = TILE > 8192 ? 1 : 2;
+    // Up to this many tiles lie in LDS for all of a unit's turns, beside 16 keys of each wavefront on their way to the operands; in more the workgroup shares out the tiles
+    static constexpr int STAGE = kScoreWaves * 16 * KPITCH, FIT = (131072 - STAGE) / TILE, OWN = FIT < 16 ? FIT : 16;
     static __device__ __forceinline__ int swz(int row) { return CH == 8 ? row >> 1 & 7 : row & 15; }
     // Tokens of a tile: with all their heads, or one where that is more than a tile's rows, or where offsets within the tile would pass 32 bits
     static __device__ __forceinline__ int tokens(const ScoreRun& r) {
@@ -133,7 +134,7 @@ struct ScoreWalk {
         b = seq;
         s = seq_at(r.c, b);
         rows = s.n * (int)r.group.d;             // (T Hq is below 2^31)
-        kind = rows <= kFewRows ? kFew : C::tiles(r, s.n) <= kOwnTiles ? kMid : kLong;
+        kind = rows <= kFewRows ? kFew : C::tiles(r, s.n) <= C::OWN ? kMid : kLong;
         const int keys = kind == kFew ? C::FEW : 32 * (kind == kMid ? C::MID : C::LONG);
         chunks = s.n == 0 ? 0 : (s.len + s.n + keys - 1) / keys;
     }
@@ -441,18 +442,22 @@ __global__ __launch_bounds__(kScoreThreads, 2) void score_few_kernel(ScoreRun r)
 //
 // Lane (hh, c) = (lane / 32, lane % 32): of a tile of 32 rows it holds key c of each of KB blocks of 32 keys, and the rows 8 y + 4 hh .. + 3, y = 0 .. 3.
 //
-// A wavefront keeps its keys' operands in registers, of 16 bits those of 64 keys, or 128 of a turn that the workgroup shares, and takes the unit's tiles of rows one after
-// the other, or every eighth one of a shared turn.  It has places of its own in LDS for two tiles, which are copied there one ahead, and so waits for nobody; the keys of
-// its next turn are read before the last tile.  The exponentials of a block run between the products of the next one.
-// Chunks of 1000 tokens after 2000 to 7000 keys, 138 GFLOP: 207 us, where rows staged by the workgroup with a barrier for each 128 of them took 251.  32 tokens after 10000
-// to 32000 keys, 202 MB: 79 us.
+// A wavefront keeps its keys' operands in registers, of 16 bits those of 64 keys, or 128 of a turn that the workgroup shares.  A unit's rows lie in LDS for all of its turns
+// if they fit, and the wavefronts take turns as they come to them, reading the keys of the next one before they weigh the present: keys bound it, and are to be under way all
+// the time (32 tokens after 10000 to 32000 keys, 202 MB: 65 us, and 79 where each wavefront copied the rows a tile ahead for itself and so read its next keys late).
+// Of more rows each wavefront of a shared turn takes every eighth tile, copied to a place of its own one ahead, and so waits for nobody.  The exponentials of a block run between
+// the products of the next one.  Chunks of 1000 tokens after 2000 to 7000 keys, 138 GFLOP: 207 to 216 us, where rows staged with a barrier for each 128 of them took 251.
 template <typename C> struct ScorePlaces {
     union {
         char tile[kScoreWaves][C::SLOTS][C::TILE];
         char keys[kScoreWaves][16 * C::KPITCH];          // 16 keys of a wavefront, or all of the workgroup's, on their way to the operands
         float sums[kScoreWaves][32 * C::LONG];
+        struct {
+            char rows[C::OWN][C::TILE];
+            char stage[kScoreWaves][16 * C::KPITCH];
+        } own;
     };
-    float bias[kBiasTiles][32];          // of a wavefront's unit kOwnTiles of them
+    float bias[kBiasTiles][32];
 };
 
 __device__ __forceinline__ uint32_t lds_at(const void* p) {
@@ -495,6 +500,13 @@ template <> struct Copies<16> {
         Copies<8>::start(w, to + 8192, off + 8);
     }
 };
+
+// The lane's number, asked for anew: what is kept of it across a turn is pushed out of the registers, and reading it back waits for all loads under way
+__device__ __forceinline__ int lane_now() {
+    int x;
+    asm volatile("v_mbcnt_lo_u32_b32 %0, -1, 0\n\tv_mbcnt_hi_u32_b32 %0, -1, %0" : "=v"(x));
+    return x;
+}
 
 template <typename T, int D, bool FP8, int KB, class W> struct ManyRows {
     using C = ScoreCfg<T, D, FP8>;
@@ -546,12 +558,12 @@ template <typename T, int D, bool FP8, int KB, class W> struct ManyRows {
         const int p = j < keys ? same(trow[j >> r.c.page_log2]) : -1;
         return (unsigned)p < (unsigned)r.c.P ? p : -1;
     }
-    __device__ __forceinline__ void fetch(int i, int page, u32x4 (&k)[NM / 2]) const {
+    __device__ __forceinline__ void fetch(int i, int page, int me, u32x4 (&k)[NM / 2]) const {
         const int j = u.chunk * MANY + 16 * i;
         const char* at = r.c.k + u.h * r.c.head_bytes + max(page, 0) * r.c.page_bytes + (int64_t)(j & ((1 << r.c.page_log2) - 1)) * C::ROWB;
         const auto w = window(at, page < 0 ? 0 : min(keys - j, 16) * C::ROWB);
 #pragma unroll
-        for (int x = 0; x < NM / 2; ++x) k[x] = kv_load<0>(w, 1024 * x + 16 * lane);
+        for (int x = 0; x < NM / 2; ++x) k[x] = kv_load<0>(w, 16 * me + 1024 * x);
     }
     __device__ __forceinline__ void stage(char* to, const u32x4 (&k)[NM / 2]) const {
 #pragma unroll
@@ -579,11 +591,12 @@ template <typename T, int D, bool FP8, int KB, class W> struct ManyRows {
     __device__ __forceinline__ void fetch(Own& x) const {
 #pragma unroll
         for (int i = 0; i < 2 * KB; ++i) x.page[i] = page_of(i);
+        const int me = lane_now();
 #pragma unroll
-        for (int i = 0; i < 2 * KB; ++i) fetch(i, x.page[i], x.k[i]);
+        for (int i = 0; i < 2 * KB; ++i) fetch(i, x.page[i], me, x.k[i]);
     }
     __device__ __forceinline__ void own_keys(const Own& own, u32x4 (&kf)[KB][STEPS], uint32_t& there) const {
-        char* const mine = lds.tile[wave][0];            // (its accesses reach it in their order)
+        char* const mine = lds.own.stage[wave];          // (its accesses reach it in their order)
         there = 0;
 #pragma unroll
         for (int b = 0; b < KB; ++b) {
@@ -605,7 +618,7 @@ template <typename T, int D, bool FP8, int KB, class W> struct ManyRows {
         __syncthreads();                 // the turn before has been read
         if (wave < 2 * KB) {
             u32x4 k[NM / 2];
-            fetch(wave, page_of(wave), k);
+            fetch(wave, page_of(wave), lane, k);
             stage(lds.keys[wave], k);
         }
         there = 0;
@@ -623,13 +636,13 @@ template <typename T, int D, bool FP8, int KB, class W> struct ManyRows {
     }
 
     // the copies of a tile of rows
-    __device__ __forceinline__ void start(int t, int slot) const {
+    __device__ __forceinline__ void start(int t, const char* to) const {
         const int t0 = token0(t), h0 = head0(t), G = (int)r.group.d;
         const int64_t stride = r.a.q_stride * C::QSZ;
         const uint64_t from = (uint64_t)(static_cast<const char*>(r.a.q) + (u.s.row0 + t0) * stride + (int64_t)(u.h * G + h0) * C::QROW);
         const int bytes = (int)((min(tpt, u.s.n - t0) - 1) * stride) + min(hpt, G - h0) * C::QROW;
         const u32x4 w = {(uint32_t)same((int)from), (uint32_t)same((int)(from >> 32)), (uint32_t)same(bytes), 0x00020000u};
-        Copies<COPIES>::start(w, lds_at(lds.tile[wave][slot]), off);
+        Copies<COPIES>::start(w, lds_at(to), off);
     }
     // waits until all but the last LOADS loads and copies have landed
     template <int LOADS> static __device__ __forceinline__ void landed() { asm volatile("s_waitcnt vmcnt(%0)" :: "n"(LOADS) : "memory"); }
@@ -675,22 +688,20 @@ template <typename T, int D, bool FP8, int KB, class W> struct ManyRows {
         }
     }
 
-    // Tiles t, t + step, ... below `end`, whose bias begins at `from` with that of tile `base`.  Before the last one, whose copies are then under way or done,
-    // `ahead` starts LOADS loads, or none and says so.
+    // Tiles, whose bias begins at `from` with that of tile `base`
     struct Tiles {
         const float (*from)[32];
         int base, clear;                 // clear: tokens from this one on see all of the keys
         uint32_t there;
     };
-    __device__ __forceinline__ void tile(const Tiles& x, int t, int next, int slot, const u32x4 (&kf)[KB][STEPS], float (&sum)[KB]) const {
+    __device__ __forceinline__ void tile(const Tiles& x, int t, int next, const char* at, const u32x4 (&kf)[KB][STEPS], float (&sum)[KB]) const {
         u32x4 q[STEPS];
         f32x4 b[4];
-        const char* at = lds.tile[wave][slot];
 #pragma unroll
         for (int s = 0; s < STEPS; ++s) q[s] = *reinterpret_cast<const u32x4*>(at + (qat ^ C::many_at(s)));
 #pragma unroll
         for (int y = 0; y < 4; ++y) b[y] = *reinterpret_cast<const f32x4*>(&x.from[t - x.base][8 * y + 4 * (lane >> 5)]);
-        if (next >= 0) start(next, slot);
+        if (next >= 0) start(next, at);
         // (a row that does not count has an infinite bias: one of them in 8 y + 4 hh .. + 3 makes the sum of those infinite, or NaN)
         bool off_rows = false;
 #pragma unroll
@@ -725,36 +736,35 @@ template <typename T, int D, bool FP8, int KB, class W> struct ManyRows {
             weigh_tile<true>(q, kf, b, bits, sum);
         }
     }
-    template <int LOADS, class Ahead>
-    __device__ __forceinline__ void run(int t, int step, int end, const u32x4 (&kf)[KB][STEPS], uint32_t there, const float (*from)[32], int base,
-                                        float (&sum)[KB], const Ahead& ahead) const {
-        if (t >= end) {
-            ahead();
-            return;
-        }
+    // there: of the lane's keys
+    __device__ __forceinline__ Tiles tiles_of(const float (*from)[32], int base, uint32_t there) const {
         const int j0 = u.chunk * MANY;
         const bool all_there = __builtin_amdgcn_ballot_w64(there != (1u << KB) - 1u) == 0;
         // (none before the end in a tree's new keys)
-        const Tiles x{from, base, !all_there ? 0x7fffffff : j0 + MANY <= u.s.len ? 0 : r.a.tree == nullptr ? j0 + MANY - 1 - u.s.len : 0x7fffffff, there};
-        start(t, 0);
+        return Tiles{from, base, !all_there ? 0x7fffffff : j0 + MANY <= u.s.len ? 0 : r.a.tree == nullptr ? j0 + MANY - 1 - u.s.len : 0x7fffffff, there};
+    }
+    __device__ __forceinline__ void run(int t, int end, const u32x4 (&kf)[KB][STEPS], const Tiles& x, float (&sum)[KB]) const {
+        constexpr int step = kScoreWaves;
+        if (t >= end) return;
+        const char (*const slots)[C::TILE] = lds.tile[wave];
+        start(t, slots[0]);
         int slot = 0;
         if constexpr (C::SLOTS == 2) {
-            if (t + step < end) start(t + step, 1);
+            if (t + step < end) start(t + step, slots[1]);
         }
 #pragma unroll 1
         for (; t + step < end; t += step) {
             if constexpr (C::SLOTS == 2) {
                 landed<COPIES>();
-                tile(x, t, t + 2 * step < end ? t + 2 * step : -1, slot, kf, sum);
+                tile(x, t, t + 2 * step < end ? t + 2 * step : -1, slots[slot], kf, sum);
                 slot ^= 1;
             } else {
                 landed<0>();
-                tile(x, t, t + step, 0, kf, sum);
+                tile(x, t, t + step, slots[0], kf, sum);
             }
         }
-        if (ahead()) landed<LOADS>();
-        else landed<0>();
-        tile(x, t, -1, slot, kf, sum);
+        landed<0>();
+        tile(x, t, -1, slots[slot], kf, sum);
     }
     // A turn: sum is over half of the rows, the other half is in the other half of the lanes.
     __device__ __forceinline__ int first_tile() const {
@@ -762,15 +772,23 @@ template <typename T, int D, bool FP8, int KB, class W> struct ManyRows {
         const int rel = u.chunk * MANY - u.s.len;
         return r.a.tree == nullptr && rel > 0 ? rel / tpt * of_token : 0;
     }
-    template <class Ahead> __device__ __forceinline__ void own_turn(const Own& own, bool fresh, float (&sum)[KB], const Ahead& ahead) const {
+    // The unit's tiles and their bias, by the workgroup
+    __device__ __forceinline__ void take_rows() const {
+        for (int t = wave; t < tiles; t += kScoreWaves) start(t, lds.own.rows[t]);
+        put_bias(lds.bias, 0, tiles, threadIdx.x, kScoreThreads);
+        landed<0>();
+    }
+    // `ahead` starts loads of the next turn's keys
+    template <class Ahead> __device__ __forceinline__ void own_turn(const Own& own, float (&sum)[KB], const Ahead& ahead) const {
         u32x4 kf[KB][STEPS];
         uint32_t there;
 #pragma unroll
         for (int k = 0; k < KB; ++k) sum[k] = 0.0f;
-        if (fresh) put_bias(lds.bias + kOwnTiles * wave, 0, tiles, lane, kWave);
         own_keys(own, kf, there);
-        have_loads();
-        run<2 * KB * (NM / 2)>(first_tile(), 1, tiles, kf, there, lds.bias + kOwnTiles * wave, 0, sum, ahead);
+        ahead();
+        const Tiles x = tiles_of(lds.bias, 0, there);
+#pragma unroll 1
+        for (int t = first_tile(); t < tiles; ++t) tile(x, t, -1, lds.own.rows[t], kf, sum);
     }
     __device__ __forceinline__ void shared_turn(float (&sum)[KB]) const {
         u32x4 kf[KB][STEPS];
@@ -785,7 +803,7 @@ template <typename T, int D, bool FP8, int KB, class W> struct ManyRows {
             put_bias(lds.bias, base, end, threadIdx.x, kScoreThreads);
             __syncthreads();
             have_loads();
-            run<0>(base + wave, kScoreWaves, end, kf, there, lds.bias, base, sum, [] { return false; });
+            run(base + wave, end, kf, tiles_of(lds.bias, base, there), sum);
             base = end;
         } while (base < tiles);
     }
@@ -833,34 +851,40 @@ __global__ __launch_bounds__(kScoreThreads, 2) void score_many_kernel(ScoreRun r
         __syncthreads();
     }
     if (!u.start(r, &scratch, kMid, total[kMid], w, kScoreGroups)) return;
-    const long long begin = u.at;
-    const auto next = [&] {
-        int k = 0;
-        if (lane == 0) k = atomicAdd(&scratch.taken, 1);
-        return begin + same(k);
-    };
     using M = ManyRows<T, D, FP8, C::MID, W>;
-    if (!u.advance_to(r, next())) return;
-    typename M::Own own;
-    M(r, u, places, wave, lane).fetch(own);
-    bool fresh = true;                   // another unit than the turn before
     for (;;) {
-        W v = u;
-        const bool more = v.advance_to(r, next());
-        const M m(r, u, places, wave, lane);
-        float sum[C::MID];
-        m.own_turn(own, fresh, sum, [&] {
-            if (more) M(r, v, places, wave, lane).fetch(own);
-            return more;
-        });
+        // the turns of the stretch that are this unit's: the wavefronts begin with one each, and take more as they come to them
+        const int from = u.chunk, n = (int)min((long long)(u.chunks - from), u.end - u.at);
+        bool any = wave < n;
+        u.chunk = from + wave;
+        typename M::Own own;
+        if (any) M(r, u, places, wave, lane).fetch(own);
+        __syncthreads();                 // the unit before is done
+        if (threadIdx.x == 0) scratch.taken = kScoreWaves;
+        M(r, u, places, wave, lane).take_rows();
+        __syncthreads();
+        while (any) {
+            const M m(r, u, places, wave, lane);
+            W v = u;
+            float sum[C::MID];
+            m.own_turn(own, sum, [&] {
+                int k = 0;
+                if (lane == 0) k = atomicAdd(&scratch.taken, 1);
+                k = same(k);
+                any = k < n;
+                v.chunk = from + k;
+                if (any) M(r, v, places, wave, lane).fetch(own);
+            });
 #pragma unroll
-        for (int k = 0; k < C::MID; ++k) {
-            const float all = pair_sum(sum[k]);
-            if (lane < 32) m.put(u.chunk * 32 * C::MID + 32 * k + lane, all);
+            for (int k = 0; k < C::MID; ++k) {
+                const float all = pair_sum(sum[k]);
+                const int me = lane_now();
+                if (me < 32) m.put(u.chunk * 32 * C::MID + 32 * k + me, all);
+            }
+            u.chunk = v.chunk;
         }
-        if (!more) return;
-        fresh = v.b != u.b || v.h != u.h;
-        u = v;
+        u.chunk = from;
+        if (!u.advance_to(r, u.at + n)) return;
     }
 }
 

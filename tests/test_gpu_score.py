@@ -190,6 +190,24 @@ def test_pages_that_are_none():
     check(c, 4, "bf16")
 
 
+@pytest.mark.parametrize("dtype,fp8,d,n", [("bf16", False, 128, 88), ("f32", False, 128, 24), ("bf16", False, 64, 128),
+                                           ("bf16", True, 128, 104), ("f32", False, 64, 88), ("f16", True, 64, 128)])
+@pytest.mark.parametrize("more", [0, 1])
+def test_rows_that_fit_on_the_chip_and_that_do_not(dtype, fp8, d, n, more):
+    some = [n + more, 5, n + more - 1, 33]
+    c = make([70, 900, 1500, 3], some, 2, d, 64, dtype, fp8, seed=n)
+    check(c, 8, dtype, decay=0.9, weight=torch.arange(sum(some)) % 3 * 0.5)
+
+
+@pytest.mark.parametrize("tree", [False, True])
+def test_many_units_of_a_few_turns(tree):
+    gen = torch.Generator().manual_seed(17)
+    some = torch.randint(4, 30, (60,), generator=gen).tolist()
+    c = make(torch.randint(0, 700, (60,), generator=gen).tolist(), some, 3, 64, 32, "bf16", seed=18)
+    words, seen = random_tree(some, 1) if tree else (None, None)
+    check(c, 15, "bf16", tree=words, seen=seen)
+
+
 def test_long_and_many():
     gen = torch.Generator().manual_seed(7)
     some = torch.randint(0, 3, (700,), generator=gen).tolist()
