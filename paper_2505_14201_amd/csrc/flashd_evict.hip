@@ -305,7 +305,7 @@ __device__ __forceinline__ UnitPlace place_of(const EvictRun& r, int unit, bool 
     return UnitPlace{c, pool, c.table + (size_t)b * c.max_pages, c.d * c.esz};
 }
 
-// Ranks `first` to `near` in order, of a unit's K or V by one workgroup, or by some that take a slice of every row each.  All rows of a round have been read before any
+// Ranks `first` to `near` in order (to m with `all`), of a unit's K or V by one workgroup, or by some that take a slice of every row each.  All rows of a round have been read before any
 // is written, and the next round's are on their way by then: they come from behind all that is written.
 __global__ __launch_bounds__(kNearThreads) void evict_near_kernel(EvictRun r, int slices, int all) {
     constexpr int N = kNearRows;
