@@ -613,14 +613,12 @@ template <typename T, int D, bool FP8, int KB, class W> struct ManyRows {
             widen(x, kf[b]);
         }
     }
-    __device__ __forceinline__ void shared_keys(u32x4 (&kf)[KB][STEPS], uint32_t& there) const {
+    template <class Meanwhile> __device__ __forceinline__ void shared_keys(u32x4 (&kf)[KB][STEPS], uint32_t& there, const Meanwhile& meanwhile) const {
         static_assert(2 * KB <= kScoreWaves, "16 keys to a wavefront");
-        __syncthreads();                 // the turn before has been read
-        if (wave < 2 * KB) {
-            u32x4 k[NM / 2];
-            fetch(wave, page_of(wave), lane, k);
-            stage(lds.keys[wave], k);
-        }
+        u32x4 k[NM / 2];
+        if (wave < 2 * KB) fetch(wave, page_of(wave), lane, k);
+        meanwhile();
+        if (wave < 2 * KB) stage(lds.keys[wave], k);
         there = 0;
 #pragma unroll
         for (int b = 0; b < KB; ++b) there |= has_page(b, page_of(2 * b), page_of(2 * b + 1)) << b;
@@ -795,17 +793,19 @@ template <typename T, int D, bool FP8, int KB, class W> struct ManyRows {
         uint32_t there;
 #pragma unroll
         for (int k = 0; k < KB; ++k) sum[k] = 0.0f;
-        shared_keys(kf, there);
-        int base = first_tile();
-        do {
-            const int end = min(base + kBiasTiles, tiles);
-            __syncthreads();             // the keys, or the tiles before, have been read
-            put_bias(lds.bias, base, end, threadIdx.x, kScoreThreads);
-            __syncthreads();
+        int base = first_tile(), end = min(base + kBiasTiles, tiles);
+        // (nobody reads the turn before any more)
+        shared_keys(kf, there, [&] { put_bias(lds.bias, base, end, threadIdx.x, kScoreThreads); });
+        for (;;) {
+            __syncthreads();             // the keys have been read, and the bias is there
             have_loads();
             run(base + wave, end, kf, tiles_of(lds.bias, base, there), sum);
             base = end;
-        } while (base < tiles);
+            if (base >= tiles) return;
+            end = min(base + kBiasTiles, tiles);
+            __syncthreads();             // the tiles before have been read
+            put_bias(lds.bias, base, end, threadIdx.x, kScoreThreads);
+        }
     }
     // The sum over all rows of the turn's key `j` becomes its score.
     __device__ __forceinline__ void put(int j, float all) const {
