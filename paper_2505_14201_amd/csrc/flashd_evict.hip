@@ -6,8 +6,8 @@
 // and must be read before it is overwritten; the keys behind m are overwritten by nobody.  So the second kernel moves, in order, the keys that come
 // from below m (they are a first run of the ranks), and the third all others, which by then depend on nothing.  Of many units the second one moves them all.
 //
-// Bytes bound it: rows that stay and move are read and written once, at 4.8 TB/s where a large copy has 4.84.  Before them stands the choice: 14 us for 1040 scores,
-// 50 us for 65536 of them (five passes of one CU, by the instructions).  16 sequences of 1040 keys to 1024 keys 33 us, 8 layers of 8 prompts of 1500 to 8000 keys to 1024
+// Bytes bound it: rows that stay and move are read and written once, at 4.8 TB/s where a large copy has 4.84.  Before them stands the choice: 12 us for 1040 scores,
+// 47 us for 65536 of them (five passes of one CU, by the instructions).  16 sequences of 1040 keys to 1024 keys 33 us, 8 layers of 8 prompts of 1500 to 8000 keys to 1024
 // 146 us (548 MB), 2 layers of 65536 keys to 16384 123 us (274 MB).
 #include "flashd_common.h"
 #include "flashd_kernels.h"

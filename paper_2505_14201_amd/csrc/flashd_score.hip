@@ -301,6 +301,7 @@ __device__ __forceinline__ float if_bit(uint32_t bits, int i, float x) {
 //
 // Lane (q, c) = (lane / 16, lane % 16): of S = Q K^T it holds key c and the rows 4 q .. 4 q + 3.
 // Keys go through LDS, so that a load brings 1 KB as it lies in memory: with 64 bytes of each of 16 keys, as the operand has them, HBM gave 5.0 TB/s.
+// A token for each of 64 sequences of 500 to 8192 keys, 593 MB: 105 us (5.7 TB/s); trees of 4 tokens over an fp8 cache, 312 MB: 73 us.
 template <typename T, int D, bool FP8, class W>
 __device__ __forceinline__ void few_rows(const ScoreRun& r, W u, int* taken, char* stage, int lane) {
     using C = ScoreCfg<T, D, FP8>;
