@@ -35,7 +35,7 @@ struct RowStat {
     double p, q;
 };
 
-// log2(e) / temperature, and the least distance to the largest logit that counts, 1023 / scale, which is exponent 0: none; a scale below 0 where the sequence takes the largest logit
+// log2(e) / temperature, and what distances to the largest logit are cut to, -1023 / scale, which is exponent 0: no weight; a scale below 0 where the sequence takes the largest logit
 // (a temperature of 0, below, or NaN).  An infinite temperature leaves the least scale with which the rules for infinities hold.
 struct Heat {
     double scale, least;
@@ -89,8 +89,8 @@ __device__ __forceinline__ float clean(float x) {
     return x != x ? -__builtin_inff() : fminf(x, 3.4028234663852886e38f);
 }
 
-// 2^(d heat.scale) for d <= 0, by a polynomial for 2^f on [-1/2, 1/2] through its values at the ten zeros of a Chebyshev polynomial; 1.9e-14 off.  0 for
-// d = -infinity and NaN (of -infinity - -infinity).
+// 2^(d heat.scale) for d <= 0, by a polynomial for 2^f on [-1/2, 1/2] through its values at the ten zeros of a Chebyshev polynomial; 1.9e-14 off.  0 where
+// it is below 2^-1022.5, and so for d = -infinity and NaN (of -infinity - -infinity), which `least` makes 2^-1023.
 __device__ __forceinline__ double weight_of(float l, float top, Heat heat) {
     const double d = fmax((double)l - (double)top, heat.least);
     const double whole = 6755399441055744.0;                     // 1.5 2^52: what is added to it is rounded to a whole number, in its low bits
@@ -105,7 +105,8 @@ __device__ __forceinline__ double weight_of(float l, float top, Heat heat) {
     y = fma(y, f, 2.4022650695640341e-01);
     y = fma(y, f, 6.9314718055994617e-01);
     y = fma(y, f, 1.0000000000000135);
-    return ldexp(y, (int)(uint32_t)__double_as_longlong(t));
+    const int n = (int)(uint32_t)__double_as_longlong(t);
+    return n > -1023 ? ldexp(y, n) : 0.0;
 }
 
 // The same where there are many, with a table of 2^(j / 256): of the exponent's 256th parts the whole ones' low 8 bits are j, the others go to the number's exponent, and
