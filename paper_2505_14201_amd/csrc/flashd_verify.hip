@@ -363,13 +363,14 @@ struct Refused {
     }
 };
 
-// The weights of 4 tokens from v on
+// The weights of 4 tokens from v on.  `less`: the draft's row is taken off (what it holds is not read where nothing has been refused: it may be nobody's).
 template <typename T, typename Q>
-__device__ __forceinline__ void rest_of(const VerifyRun& r, const Rest& s, const Refused& refused, int v, double (&w)[4], const uint64_t* powers = nullptr) {
+__device__ __forceinline__ void rest_of(const VerifyRun& r, const Rest& s, const Refused& refused, int v, bool less, double (&w)[4],
+                                        const uint64_t* powers = nullptr) {
     const VerifyArgs& a = r.a;
     float x[4], q[4];
     elements<T, 4>(a.logits, (int64_t)s.row * a.logits_stride, v, a.V, -__builtin_inff(), x);
-    if (a.draft != nullptr) elements<Q, 4>(a.draft, (int64_t)s.row * a.draft_stride, v, a.V, 0.0f, q);
+    if (less) elements<Q, 4>(a.draft, (int64_t)s.row * a.draft_stride, v, a.V, 0.0f, q);
 #pragma unroll
     for (int e = 0; e < 4; ++e) x[e] = clean(x[e]);
     if (powers != nullptr) {
@@ -378,9 +379,12 @@ __device__ __forceinline__ void rest_of(const VerifyRun& r, const Rest& s, const
 #pragma unroll
         for (int e = 0; e < 4; ++e) w[e] = weight_of(x[e], s.top, s.heat);
     }
-    if (a.draft != nullptr) {
+    if (less) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) w[e] = fmax(s.scale * w[e] - s.by * (double)(q[e] > 0.0f ? q[e] : 0.0f), 0.0);
+    } else if (a.draft != nullptr) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w[e] *= s.scale;
     } else {
         for (int k = 0; k < s.refused; ++k) {
             const int x0 = refused[k];
@@ -428,7 +432,7 @@ __device__ __forceinline__ void draw_next(const VerifyRun& r, int b, int row0, c
 #pragma unroll
                         for (int e = 0; e < EACH; ++e) {
                             double w[4];
-                            rest_of<T, Q>(r, rest, list, v + e * 4 * kWave * PARTS, w);
+                            rest_of<T, Q>(r, rest, list, v + e * 4 * kWave * PARTS, false, w);
                             sum += (w[0] + w[1]) + (w[2] + w[3]);
                         }
                         sum = wave_sum(sum);
@@ -459,7 +463,7 @@ __device__ __forceinline__ void draw_next(const VerifyRun& r, int b, int row0, c
                     const int v = c * kChunk + 256 * k + 4 * lane;
                     if (v >= a.V) continue;
                     double w[4];
-                    rest_of<T, Q>(r, rest, list, v, w);
+                    rest_of<T, Q>(r, rest, list, v, true, w);
                     sum += (w[0] + w[1]) + (w[2] + w[3]);
                 }
                 sum = wave_sum(sum);
@@ -516,7 +520,7 @@ __device__ __forceinline__ void draw_next(const VerifyRun& r, int b, int row0, c
     }
     double w[4];
     const int v = chunk * kChunk + 4 * tid;
-    rest_of<T, Q>(r, rest, list, v, w);
+    rest_of<T, Q>(r, rest, list, v, rest.by != 0.0, w);
     const double own = (w[0] + w[1]) + (w[2] + w[3]);
     const double upto = sum_up_to(own);
     if (lane == 63) sh.part[wave] = upto;
@@ -716,7 +720,7 @@ __global__ __launch_bounds__(kWalkThreads) void verify_walk_kernel(VerifyRun r) 
         double sum = 0.0;
         for (int v = 4 * tid; v < a.V; v += 4 * kWalkThreads) {
             double w[4];
-            rest_of<T, Q>(r, rest, list, v, w);
+            rest_of<T, Q>(r, rest, list, v, true, w);
             sum += (w[0] + w[1]) + (w[2] + w[3]);
         }
         sum = block_sum(sum, sh.part);
@@ -772,7 +776,7 @@ __global__ __launch_bounds__(kStatThreads) void verify_left_kernel(VerifyRun r) 
 #pragma unroll
         for (int k = 0; k < kEach / 4; ++k) {
             double w[4];
-            rest_of<T, Q>(r, end.rest, Refused{}, blockIdx.x * kChunk + 4 * (kStatThreads * k + tid), w, powers);
+            rest_of<T, Q>(r, end.rest, Refused{}, blockIdx.x * kChunk + 4 * (kStatThreads * k + tid), true, w, powers);
             sum += (w[0] + w[1]) + (w[2] + w[3]);
         }
         sum = wave_sum(sum);
