@@ -456,7 +456,7 @@ int flashd_cache_commit(const flashd_cache* c, const int* q_start, const int* ke
  *   tokens   int [T]: ids; those outside [0, V) have probability 0 (token 0's is not looked at)
  *   parent   int [T]: the token of its sequence that a token continues, an earlier one (a token with another number here is not
  *            reached); NULL: chains, token i continues i - 1
- *   uniform  float [T]: random numbers in [0, 1)
+ *   uniform  float [T]: random numbers in [0, 1).  (With others next still is an id that the target allows.)
  *   temperature   float [B], or NULL: 1
  *   keep     int [B][max_keep], overwritten: the tokens kept, ascending, as flashd_cache_commit takes them, -1 behind them.
  *            A sequence ends at max_keep of them.

@@ -381,7 +381,7 @@ __device__ __forceinline__ void rest_of(const VerifyRun& r, const Rest& s, const
     }
     if (less) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) w[e] = fmax(s.scale * w[e] - s.by * (double)(q[e] > 0.0f ? q[e] : 0.0f), 0.0);
+        for (int e = 0; e < 4; ++e) w[e] = fmax(fma(s.scale, w[e], -(s.by * (double)(q[e] > 0.0f ? q[e] : 0.0f))), 0.0);
     } else if (a.draft != nullptr) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) w[e] *= s.scale;
@@ -394,9 +394,11 @@ __device__ __forceinline__ void rest_of(const VerifyRun& r, const Rest& s, const
     }
 }
 
-// The next token, drawn from what is left where the walk has ended; by the whole workgroup.
+// The next token, drawn from what is left where the walk has ended; by the whole workgroup.  The chunks' sums and the weights within a chunk are the same numbers (with
+// `powers`, as verify_left_kernel sums them), or positive together: a chunk that is chosen has a token.
 template <typename T, typename Q>
-__device__ __forceinline__ void draw_next(const VerifyRun& r, int b, int row0, const WalkEnd& end, double* chunk_sums, WalkShared& sh) {
+__device__ __forceinline__ void draw_next(const VerifyRun& r, int b, int row0, const WalkEnd& end, double* chunk_sums, WalkShared& sh,
+                                          const uint64_t* powers = nullptr) {
     const VerifyArgs& a = r.a;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const bool plain = a.draft == nullptr;
@@ -463,7 +465,7 @@ __device__ __forceinline__ void draw_next(const VerifyRun& r, int b, int row0, c
                     const int v = c * kChunk + 256 * k + 4 * lane;
                     if (v >= a.V) continue;
                     double w[4];
-                    rest_of<T, Q>(r, rest, list, v, true, w);
+                    rest_of<T, Q>(r, rest, list, v, true, w, powers);
                     sum += (w[0] + w[1]) + (w[2] + w[3]);
                 }
                 sum = wave_sum(sum);
@@ -474,9 +476,19 @@ __device__ __forceinline__ void draw_next(const VerifyRun& r, int b, int row0, c
         double mine = 0.0;
         for (int c = tid; c < r.nc; c += kWalkThreads) mine += chunk_sums[c];
         total = block_sum(mine, sh.part);
-        if (total > 0.0 || turn == 1 || !end.open) break;
-        rest.scale = end.old_scale / s.sum;      // nothing is left: r as it was before the last refusal
-        rest.by = end.old_by;
+        if (total > 0.0 || turn == 2) break;
+        // nothing is left: r as it was before the last refusal
+        if (turn == 0 && plain && rest.refused > 0) {
+            --rest.refused;
+        } else if (turn == 0 && end.open) {
+            rest.scale = end.old_scale / s.sum;
+            rest.by = end.old_by;
+        } else {
+            // that was rounding, or random numbers were none
+            rest.scale = 1.0 / s.sum;
+            rest.by = 0.0;
+            rest.refused = 0;
+        }
     }
     // the chunk with the wanted place: the first up to which the sum passes it, or the last that has any
     if (wave == 0) {
@@ -520,7 +532,7 @@ __device__ __forceinline__ void draw_next(const VerifyRun& r, int b, int row0, c
     }
     double w[4];
     const int v = chunk * kChunk + 4 * tid;
-    rest_of<T, Q>(r, rest, list, v, rest.by != 0.0, w);
+    rest_of<T, Q>(r, rest, list, v, rest.by != 0.0, w, powers);
     const double own = (w[0] + w[1]) + (w[2] + w[3]);
     const double upto = sum_up_to(own);
     if (lane == 63) sh.part[wave] = upto;
@@ -532,7 +544,7 @@ __device__ __forceinline__ void draw_next(const VerifyRun& r, int b, int row0, c
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
         sum += w[e];
-        if (w[e] > 0.0) {
+        if (w[e] > 0.0 && v + e < a.V) {
             last = v + e;
             if (sum > left) first = min(first, v + e);
         }
@@ -795,10 +807,12 @@ template <typename T, typename Q>
 __global__ __launch_bounds__(kWalkThreads) void verify_draw_kernel(VerifyRun r) {
     extern __shared__ double chunk_sums[];               // [nc]
     __shared__ WalkShared sh;
+    __shared__ uint64_t powers[kParts];
+    take_powers<kWalkThreads>(powers);                   // (draw_next begins with a barrier)
     const int b = blockIdx.x, row0 = max(r.a.q_start[b], 0);
     if (tokens_of(row0, r.a.q_start[b + 1], r.a.T) == 0) return;
     const WalkEnd end = r.ends[row0];
-    if (end.draw) draw_next<T, Q>(r, b, row0, end, chunk_sums, sh);
+    if (end.draw) draw_next<T, Q>(r, b, row0, end, chunk_sums, sh, powers);
 }
 
 // ---- host ---------------------------------------------------------------------------------------
