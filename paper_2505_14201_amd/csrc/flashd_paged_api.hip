@@ -155,7 +155,10 @@ int take_scores(const flashd_cache* c, long long stride) {
     return stride < (long long)c->max_pages * c->page || stride > most || (long double)stride * c->B * c->Hkv > 1.0e12L ? FLASHD_E_SHAPE
                                                                                                                      : FLASHD_OK;
 }
-int64_t score_extent(const flashd_cache* c, long long stride) { return (int64_t)c->B * c->Hkv * stride * 4; }
+// bytes from the first score of a layer to behind the last
+int64_t score_extent(const flashd_cache* c, long long stride) {
+    return (((int64_t)c->B * c->Hkv - 1) * stride + (int64_t)c->max_pages * c->page) * 4;
+}
 
 // Where the caller has brought no workspace: the stream's.
 int stream_workspace(void* stream, size_t need, void** workspace) {
@@ -413,7 +416,7 @@ int flashd_cache_evict(const flashd_cache* c, const int* refs, float* score, lon
         return FLASHD_E_ALIGN;
     const size_t need = flashd::evict_workspace(p, budget);
     if (workspace != nullptr && workspace_bytes < need) return FLASHD_E_WORKSPACE;
-    const Span out{lens_out, (int64_t)c->B * 4}, scores{score, ((c->layers - 1) * layer + of_layer) * 4}, ws{workspace, (int64_t)need},
+    const Span out{lens_out, (int64_t)c->B * 4}, scores{score, (c->layers - 1) * layer * 4 + score_extent(c, score_stride)}, ws{workspace, (int64_t)need},
         table = table_of(p), lens = lens_of(p), counts{refs, (int64_t)c->P * 4}, most{budgets, (int64_t)c->B * 4};
     if (overlaps_any(out, {scores, ws, table, lens, counts, most}) || overlaps_any(scores, {ws, table, lens, counts, most}) ||
         overlaps_any(ws, {table, lens, counts, most}))
