@@ -71,7 +71,8 @@ struct VerifyRun {
     RowStat* rows;          // [T]
     WalkEnd* ends;          // [T] of a sequence at its first row, as the others:
     double* left;           // [T][nc] sums of what is left over the chunks
-    int* refused;           // [T] tokens refused behind the present one
+    uint8_t* marks;         // [longest sequences][nc * kChunk] tokens refused behind the present one
+    int* refused;           // [T] their list
     int nc;
 };
 
@@ -330,10 +331,20 @@ __global__ __launch_bounds__(kStatThreads) void verify_stats_kernel(VerifyRun r)
 
 constexpr int kNear = 256;               // rows and refused tokens of a sequence that have a place in LDS
 
+// Sequences of more than kNear tokens, of which there are fewer than T / kNear, have a byte for each token of the vocabulary: whether it has been refused behind the
+// present one.  (By the list alone each of R refused tokens would be looked for among all others, and in every sum: R^2.)
+__host__ __device__ constexpr int64_t mark_maps(int T) { return T > 0 ? (T - 1) / kNear : 0; }
+__device__ __forceinline__ uint8_t* marks_of(const VerifyRun& r, int row0, int n) {
+    // (starts of such sequences are more than kNear apart)
+    return n > kNear ? r.marks + (int64_t)(row0 / kNear) * r.nc * kChunk : nullptr;
+}
+
 struct WalkShared {
     RowStat rows[kNear];
     int list[kNear];
     double weight[kNear];   // of a refused token
+    int queue[kNear];       // chunks whose sum is to be taken again, `queued` of them
+    int queued;
     double part[kWalkWaves];
     int found[kWalkWaves];
     Rest rest;
@@ -352,14 +363,30 @@ __device__ __forceinline__ double block_sum(double x, double* part) {
     return s;
 }
 
-// The refused tokens, the first ones in LDS
+// The refused tokens: the first ones in LDS, where there are more the others in `far`, and all of them marked
 struct Refused {
     int* near;
     int* far;
+    uint8_t* marks;
     __device__ __forceinline__ int operator[](int k) const { return k < kNear ? near[k] : far[k]; }
     __device__ __forceinline__ void put(int k, int x) const {
         if (k < kNear) near[k] = x;
         else far[k] = x;
+        if (marks != nullptr) marks[x] = 1;
+    }
+    // the first n of them out of the weights of 4 tokens from v on (a multiple of 4)
+    __device__ __forceinline__ void out(int n, int v, double (&w)[4]) const {
+        if (n > kNear) {
+            const uint32_t gone = *reinterpret_cast<const uint32_t*>(marks + v);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) w[e] = (gone >> (8 * e) & 0xffu) != 0 ? 0.0 : w[e];
+        } else {
+            for (int k = 0; k < n; ++k) {
+                const int x = near[k];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) w[e] = v + e == x ? 0.0 : w[e];
+            }
+        }
     }
 };
 
@@ -386,23 +413,18 @@ __device__ __forceinline__ void rest_of(const VerifyRun& r, const Rest& s, const
 #pragma unroll
         for (int e = 0; e < 4; ++e) w[e] *= s.scale;
     } else {
-        for (int k = 0; k < s.refused; ++k) {
-            const int x0 = refused[k];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) w[e] = v + e == x0 ? 0.0 : w[e];
-        }
+        refused.out(s.refused, v, w);
     }
 }
 
 // The next token, drawn from what is left where the walk has ended; by the whole workgroup.  The chunks' sums and the weights within a chunk are the same numbers (with
 // `powers`, as verify_left_kernel sums them), or positive together: a chunk that is chosen has a token.
 template <typename T, typename Q>
-__device__ __forceinline__ void draw_next(const VerifyRun& r, int b, int row0, const WalkEnd& end, double* chunk_sums, WalkShared& sh,
+__device__ __forceinline__ void draw_next(const VerifyRun& r, int b, const WalkEnd& end, const Refused& list, int row0, double* chunk_sums, WalkShared& sh,
                                           const uint64_t* powers = nullptr) {
     const VerifyArgs& a = r.a;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const bool plain = a.draft == nullptr;
-    const Refused list{sh.list, r.refused + row0};
     Rest rest = end.rest;
     const int row = rest.row;
     const RowStat s = end.row;
@@ -414,22 +436,24 @@ __device__ __forceinline__ void draw_next(const VerifyRun& r, int b, int row0, c
             const ChunkStat* of = r.chunks + (size_t)row * r.nc;
             // A chunk lacks its refused tokens: their weights are taken off its sum, unless they are most of it; then what is left is summed again.
             const int refused = plain ? rest.refused : 0;
-            bool again = refused > kNear;
-            for (int c = tid; c < r.nc; c += kWalkThreads) {
-                const double sum = of[c].sum * weight_of(of[c].top, s.top, rest.heat) * (plain ? 1.0 : rest.scale);
-                double off = 0.0;
-                for (int k = 0; k < min(refused, kNear); ++k) off += list[k] / kChunk == c ? sh.weight[k] : 0.0;
-                const bool most = off > 0.5 * sum || refused > kNear;
-                chunk_sums[c] = most ? -1.0 : sum - off;
-                again |= most;
-            }
-            if (__syncthreads_or(again)) {
+            if (tid == 0) sh.queued = 0;
+            __syncthreads();
+            if (refused <= kNear) {
+                for (int c = tid; c < r.nc; c += kWalkThreads) {
+                    const double sum = of[c].sum * weight_of(of[c].top, s.top, rest.heat) * (plain ? 1.0 : rest.scale);
+                    double off = 0.0;
+                    for (int k = 0; k < refused; ++k) off += list[k] / kChunk == c ? sh.weight[k] : 0.0;
+                    chunk_sums[c] = sum - off;
+                    if (off > 0.5 * sum) sh.queue[atomicAdd(&sh.queued, 1)] = c;        // (has one of the refused)
+                }
+                __syncthreads();
                 // four chunks at a time
                 constexpr int PARTS = kWalkWaves / 4, EACH = kChunk / (4 * kWave * PARTS);
-                for (int k0 = 0; k0 < refused; k0 += 4) {
+                const int queued = sh.queued;
+                for (int k0 = 0; k0 < queued; k0 += 4) {
                     const int k = k0 + wave / PARTS;
-                    if (k < refused) {
-                        const int v = list[k] / kChunk * kChunk + 4 * (kWave * (wave % PARTS) + lane);
+                    if (k < queued) {
+                        const int v = sh.queue[k] * kChunk + 4 * (kWave * (wave % PARTS) + lane);
                         double sum = 0.0;
 #pragma unroll
                         for (int e = 0; e < EACH; ++e) {
@@ -441,18 +465,26 @@ __device__ __forceinline__ void draw_next(const VerifyRun& r, int b, int row0, c
                         if (lane == 0) sh.part[wave] = sum;
                     }
                     __syncthreads();
-                    if (k < refused && wave % PARTS == 0 && lane == 0) {
+                    if (k < queued && wave % PARTS == 0 && lane == 0) {
                         double sum = 0.0;
 #pragma unroll
                         for (int e = 0; e < PARTS; ++e) sum += sh.part[wave + e];
-                        chunk_sums[list[k] / kChunk] = sum;
+                        chunk_sums[sh.queue[k]] = sum;
                     }
                     __syncthreads();
                 }
-                // (of more refused tokens than have a place all of their chunks, and the others as they are)
-                if (refused > kNear) {
-                    for (int c = tid; c < r.nc; c += kWalkThreads)
-                        if (chunk_sums[c] < 0.0) chunk_sums[c] = of[c].sum * weight_of(of[c].top, s.top, rest.heat);
+            } else {
+                // (of so many all chunks, a wavefront each)
+                for (int c = wave; c < r.nc; c += kWalkWaves) {
+                    double sum = 0.0;
+#pragma unroll 4
+                    for (int k = 0; k < kChunk / 256; ++k) {
+                        double w[4];
+                        rest_of<T, Q>(r, rest, list, c * kChunk + 256 * k + 4 * lane, false, w);
+                        sum += (w[0] + w[1]) + (w[2] + w[3]);
+                    }
+                    sum = wave_sum(sum);
+                    if (lane == 0) chunk_sums[c] = sum;
                 }
             }
         } else if (turn == 0) {
@@ -480,6 +512,7 @@ __device__ __forceinline__ void draw_next(const VerifyRun& r, int b, int row0, c
         // nothing is left: r as it was before the last refusal
         if (turn == 0 && plain && rest.refused > 0) {
             --rest.refused;
+            if (rest.refused >= kNear && tid == 0) list.marks[list[rest.refused]] = 0;
         } else if (turn == 0 && end.open) {
             rest.scale = end.old_scale / s.sum;
             rest.by = end.old_by;
@@ -583,6 +616,9 @@ __global__ __launch_bounds__(kWalkThreads) void verify_walk_kernel(VerifyRun r) 
     }
     const Heat heat = heat_of(a.temperature != nullptr ? a.temperature[b] : 1.0f);
     const float ninf = -__builtin_inff();
+    uint8_t* const marks = a.draft == nullptr ? marks_of(r, row0, n) : nullptr;
+    if (marks != nullptr)
+        for (int v = 16 * tid; v < r.nc * kChunk; v += 16 * kWalkThreads) *reinterpret_cast<uint4*>(marks + v) = uint4{0, 0, 0, 0};
 
     // (read now, wanted later)
     auto before_of = [&](int i) { return a.parent != nullptr ? a.parent[row0 + i] : i - 1; };
@@ -646,7 +682,7 @@ __global__ __launch_bounds__(kWalkThreads) void verify_walk_kernel(VerifyRun r) 
     double scale = 1.0, by = 0.0;            // r = max(scale p - by q, 0); without q p / scale but for those refused
     double want_scale = 1.0, want_by = 0.0;  // r before it is divided by its sum
     bool open = false;                       // that sum is wanted for the next question
-    const Refused list{sh.list, r.refused + row0};
+    const Refused list{sh.list, r.refused + row0, marks};
     int j0 = 0, done = 0;                    // the window of 64 tokens, and the tokens of it that are behind
     int before = -2, x = -1;
     double p = 0.0, q = 1.0;
@@ -691,7 +727,11 @@ __global__ __launch_bounds__(kWalkThreads) void verify_walk_kernel(VerifyRun r) 
                     if (a.draft != nullptr) {
                         rk = fmax(scale * pk - by * qk, 0.0);
                     } else {
-                        for (int i = lane; i < refused; i += kWave) twice |= list[i] == token;
+                        if (refused <= kNear) {
+                            for (int i = lane; i < refused; i += kWave) twice |= sh.list[i] == token;
+                        } else if (token >= 0 && token < a.V) {
+                            twice = marks[token] != 0;
+                        }
                         twice = __builtin_amdgcn_ballot_w64(twice) != 0;
                         rk = twice ? 0.0 : pk / scale;
                     }
@@ -700,6 +740,10 @@ __global__ __launch_bounds__(kWalkThreads) void verify_walk_kernel(VerifyRun r) 
                     cur = j0 + k;
                     if (lane == 0) keep[kept] = cur;
                     ++kept;
+                    if (marks != nullptr) {
+                        for (int i = lane; i < refused; i += kWave) marks[list[i]] = 0;
+                        __threadfence_block();
+                    }
                     refused = 0;
                     scale = 1.0;
                     by = 0.0;
@@ -767,7 +811,7 @@ __global__ __launch_bounds__(kWalkThreads) void verify_walk_kernel(VerifyRun r) 
         if (tid == 0) r.ends[row0] = end;
         return;
     }
-    if (end.draw) draw_next<T, Q>(r, b, row0, end, chunk_sums, sh);
+    if (end.draw) draw_next<T, Q>(r, b, end, list, row0, chunk_sums, sh);
 }
 
 // With the drafts' probabilities: sums of what is left over a chunk of a sequence's row.  64 sequences of 131072 logits, 50 MB: 11.5 us, where the walk's workgroups took 45 for it.
@@ -812,7 +856,7 @@ __global__ __launch_bounds__(kWalkThreads) void verify_draw_kernel(VerifyRun r) 
     const int b = blockIdx.x, row0 = max(r.a.q_start[b], 0);
     if (tokens_of(row0, r.a.q_start[b + 1], r.a.T) == 0) return;
     const WalkEnd end = r.ends[row0];
-    if (end.draw) draw_next<T, Q>(r, b, row0, end, chunk_sums, sh, powers);
+    if (end.draw) draw_next<T, Q>(r, b, end, Refused{}, row0, chunk_sums, sh, powers);
 }
 
 // ---- host ---------------------------------------------------------------------------------------
@@ -820,7 +864,8 @@ __global__ __launch_bounds__(kWalkThreads) void verify_draw_kernel(VerifyRun r) 
 static int chunks_of(int V) { return (V + kChunk - 1) / kChunk; }
 
 size_t verify_workspace(int T, int V) {
-    return (size_t)T * ((size_t)chunks_of(V) * (sizeof(ChunkStat) + sizeof(double)) + sizeof(RowStat) + sizeof(WalkEnd) + 8);
+    return (size_t)T * ((size_t)chunks_of(V) * (sizeof(ChunkStat) + sizeof(double)) + sizeof(RowStat) + sizeof(WalkEnd) + 8) +
+           (size_t)mark_maps(T) * chunks_of(V) * kChunk;
 }
 
 template <typename T, typename Q>
@@ -857,7 +902,9 @@ hipError_t launch_verify(const VerifyArgs& a, void* ws, hipStream_t st) {
     r.a = a;
     r.nc = chunks_of(a.V);
     r.chunks = static_cast<ChunkStat*>(ws);
-    r.rows = reinterpret_cast<RowStat*>(r.chunks + (size_t)a.T * r.nc);
+    static_assert(sizeof(ChunkStat) % 16 == 0, "marks lie at 16 bytes");
+    r.marks = reinterpret_cast<uint8_t*>(r.chunks + (size_t)a.T * r.nc);
+    r.rows = reinterpret_cast<RowStat*>(r.marks + (size_t)mark_maps(a.T) * r.nc * kChunk);
     r.ends = reinterpret_cast<WalkEnd*>(r.rows + a.T);
     r.left = reinterpret_cast<double*>(r.ends + a.T);
     r.refused = reinterpret_cast<int*>(r.left + (size_t)a.T * r.nc);
