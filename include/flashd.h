@@ -448,7 +448,8 @@ int flashd_cache_commit(const flashd_cache* c, const int* q_start, const int* ke
  *
  * With temperature 0 (or below, or NaN) p_i is 1 at the largest logit, the first of equal ones, and 0 elsewhere.  Logits of -infinity
  * and NaN have probability 0 (and those 708 temperatures or more below the largest may have it), those of +infinity share everything; behind a row of nothing else no token is accepted and next is -1.
- * The arithmetic is fp64: results do not depend on the order of sums but where a random number is within some 1e-13 of a border.
+ * The arithmetic is fp64: results do not depend on the order of sums but where a random number is within some 1e-13 of a border; behind tokens
+ * refused with `draft`, where r is a difference, within that divided by the part of r that each refusal has left.
  *   logits   [T][V] in storage type `dtype`, rows logits_stride elements apart, at any multiple of an element; V at most
  *            FLASHD_VERIFY_MAX_V
  *   draft    [T][V] in `draft_dtype` (FLASHD_F32, F16 or BF16), rows draft_stride apart, or NULL: row i is the distribution that the tokens continuing

@@ -417,6 +417,67 @@ __device__ __forceinline__ void rest_of(const VerifyRun& r, const Rest& s, const
     }
 }
 
+// What is left of the chunks of a row of which no draft's row has been taken off, by the whole workgroup (without a barrier at the end).
+template <typename T, typename Q>
+__device__ __forceinline__ void chunks_left(const VerifyRun& r, const Rest& rest, const RowStat& s, const Refused& list, double* chunk_sums, WalkShared& sh) {
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const ChunkStat* of = r.chunks + (size_t)rest.row * r.nc;
+    // A chunk lacks its refused tokens: their weights are taken off its sum, unless they are most of it; then what is left is summed again.
+    const bool plain = r.a.draft == nullptr;
+    const int refused = plain ? rest.refused : 0;
+    if (tid == 0) sh.queued = 0;
+    __syncthreads();
+    if (refused <= kNear) {
+        for (int c = tid; c < r.nc; c += kWalkThreads) {
+            const double sum = of[c].sum * weight_of(of[c].top, s.top, rest.heat) * (plain ? 1.0 : rest.scale);
+            double off = 0.0;
+            for (int k = 0; k < refused; ++k) off += list[k] / kChunk == c ? sh.weight[k] : 0.0;
+            chunk_sums[c] = sum - off;
+            if (off > 0.5 * sum) sh.queue[atomicAdd(&sh.queued, 1)] = c;        // (has one of the refused)
+        }
+        __syncthreads();
+        // four chunks at a time
+        constexpr int PARTS = kWalkWaves / 4, EACH = kChunk / (4 * kWave * PARTS);
+        const int queued = sh.queued;
+        for (int k0 = 0; k0 < queued; k0 += 4) {
+            const int k = k0 + wave / PARTS;
+            if (k < queued) {
+                const int v = sh.queue[k] * kChunk + 4 * (kWave * (wave % PARTS) + lane);
+                double sum = 0.0;
+#pragma unroll
+                for (int e = 0; e < EACH; ++e) {
+                    double w[4];
+                    rest_of<T, Q>(r, rest, list, v + e * 4 * kWave * PARTS, false, w);
+                    sum += (w[0] + w[1]) + (w[2] + w[3]);
+                }
+                sum = wave_sum(sum);
+                if (lane == 0) sh.part[wave] = sum;
+            }
+            __syncthreads();
+            if (k < queued && wave % PARTS == 0 && lane == 0) {
+                double sum = 0.0;
+#pragma unroll
+                for (int e = 0; e < PARTS; ++e) sum += sh.part[wave + e];
+                chunk_sums[sh.queue[k]] = sum;
+            }
+            __syncthreads();
+        }
+    } else {
+        // (of so many all chunks, a wavefront each)
+        for (int c = wave; c < r.nc; c += kWalkWaves) {
+            double sum = 0.0;
+#pragma unroll 4
+            for (int k = 0; k < kChunk / 256; ++k) {
+                double w[4];
+                rest_of<T, Q>(r, rest, list, c * kChunk + 256 * k + 4 * lane, false, w);
+                sum += (w[0] + w[1]) + (w[2] + w[3]);
+            }
+            sum = wave_sum(sum);
+            if (lane == 0) chunk_sums[c] = sum;
+        }
+    }
+}
+
 // The next token, drawn from what is left where the walk has ended; by the whole workgroup.  The chunks' sums and the weights within a chunk are the same numbers (with
 // `powers`, as verify_left_kernel sums them), or positive together: a chunk that is chosen has a token.
 template <typename T, typename Q>
@@ -426,67 +487,13 @@ __device__ __forceinline__ void draw_next(const VerifyRun& r, int b, const WalkE
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const bool plain = a.draft == nullptr;
     Rest rest = end.rest;
-    const int row = rest.row;
     const RowStat s = end.row;
     double total = 0.0;
     for (int turn = 0;; ++turn) {
         // sums of the chunks
         __syncthreads();
         if (plain || rest.by == 0.0) {
-            const ChunkStat* of = r.chunks + (size_t)row * r.nc;
-            // A chunk lacks its refused tokens: their weights are taken off its sum, unless they are most of it; then what is left is summed again.
-            const int refused = plain ? rest.refused : 0;
-            if (tid == 0) sh.queued = 0;
-            __syncthreads();
-            if (refused <= kNear) {
-                for (int c = tid; c < r.nc; c += kWalkThreads) {
-                    const double sum = of[c].sum * weight_of(of[c].top, s.top, rest.heat) * (plain ? 1.0 : rest.scale);
-                    double off = 0.0;
-                    for (int k = 0; k < refused; ++k) off += list[k] / kChunk == c ? sh.weight[k] : 0.0;
-                    chunk_sums[c] = sum - off;
-                    if (off > 0.5 * sum) sh.queue[atomicAdd(&sh.queued, 1)] = c;        // (has one of the refused)
-                }
-                __syncthreads();
-                // four chunks at a time
-                constexpr int PARTS = kWalkWaves / 4, EACH = kChunk / (4 * kWave * PARTS);
-                const int queued = sh.queued;
-                for (int k0 = 0; k0 < queued; k0 += 4) {
-                    const int k = k0 + wave / PARTS;
-                    if (k < queued) {
-                        const int v = sh.queue[k] * kChunk + 4 * (kWave * (wave % PARTS) + lane);
-                        double sum = 0.0;
-#pragma unroll
-                        for (int e = 0; e < EACH; ++e) {
-                            double w[4];
-                            rest_of<T, Q>(r, rest, list, v + e * 4 * kWave * PARTS, false, w);
-                            sum += (w[0] + w[1]) + (w[2] + w[3]);
-                        }
-                        sum = wave_sum(sum);
-                        if (lane == 0) sh.part[wave] = sum;
-                    }
-                    __syncthreads();
-                    if (k < queued && wave % PARTS == 0 && lane == 0) {
-                        double sum = 0.0;
-#pragma unroll
-                        for (int e = 0; e < PARTS; ++e) sum += sh.part[wave + e];
-                        chunk_sums[sh.queue[k]] = sum;
-                    }
-                    __syncthreads();
-                }
-            } else {
-                // (of so many all chunks, a wavefront each)
-                for (int c = wave; c < r.nc; c += kWalkWaves) {
-                    double sum = 0.0;
-#pragma unroll 4
-                    for (int k = 0; k < kChunk / 256; ++k) {
-                        double w[4];
-                        rest_of<T, Q>(r, rest, list, c * kChunk + 256 * k + 4 * lane, false, w);
-                        sum += (w[0] + w[1]) + (w[2] + w[3]);
-                    }
-                    sum = wave_sum(sum);
-                    if (lane == 0) chunk_sums[c] = sum;
-                }
-            }
+            chunks_left<T, Q>(r, rest, s, list, chunk_sums, sh);
         } else if (turn == 0) {
             for (int c = tid; c < r.nc; c += kWalkThreads) chunk_sums[c] = r.left[(size_t)row0 * r.nc + c];
         } else {
@@ -680,7 +687,8 @@ __global__ __launch_bounds__(kWalkThreads) void verify_walk_kernel(VerifyRun r) 
     // others wait to be asked for the sum of what is left.
     int cur = 0, kept = 1, refused = 0;
     double scale = 1.0, by = 0.0;            // r = max(scale p - by q, 0); without q p / scale but for those refused
-    double want_scale = 1.0, want_by = 0.0;  // r before it is divided by its sum
+    double want_scale = 1.0, want_by = 0.0;  // r before it is divided by its sum; without q want_scale is `scale` before the last refusal
+    double summed = 1.0;                     // without q: `scale` when it was last summed
     bool open = false;                       // that sum is wanted for the next question
     const Refused list{sh.list, r.refused + row0, marks};
     int j0 = 0, done = 0;                    // the window of 64 tokens, and the tokens of it that are behind
@@ -745,28 +753,32 @@ __global__ __launch_bounds__(kWalkThreads) void verify_walk_kernel(VerifyRun r) 
                         __threadfence_block();
                     }
                     refused = 0;
-                    scale = 1.0;
+                    scale = summed = 1.0;
                     by = 0.0;
                 } else if (heat.scale >= 0.0) {
                     if (a.draft != nullptr) {
                         want_scale = scale;
                         want_by = by + 1.0;
                         open = true;
-                    } else if (!twice && token >= 0 && token < a.V && scale - pk > 0.0) {
+                    } else if (!twice && token >= 0 && token < a.V) {
                         if (lane == 0) {
                             list.put(refused, token);
                             if (refused < kNear) sh.weight[refused] = pk * row_of(cur)->sum;
                         }
                         __threadfence_block();
                         ++refused;
+                        // The difference is off by 4e-14, which is much of it where little is left: when half of the last sum is refused it is summed anew
+                        // (chunk by chunk, and of mostly refused chunks the tokens; a border is then off by 1.2e-13 of itself at most).
+                        want_scale = scale;
                         scale -= pk;
+                        open = scale < 0.5 * summed;
                     }
                 }
             }
             if (lane == 0) {
                 sh.ask = ask;
                 const RowStat s = *row_of(cur);
-                sh.rest = Rest{row0 + cur, s.top, heat, open ? want_scale / s.sum : scale / s.sum, open ? want_by : by, refused};
+                sh.rest = Rest{row0 + cur, s.top, heat, open ? want_scale / s.sum : scale / s.sum, open ? want_by : by, refused};     // (without q neither counts)
             }
         }
         __syncthreads();
@@ -774,17 +786,33 @@ __global__ __launch_bounds__(kWalkThreads) void verify_walk_kernel(VerifyRun r) 
         const Rest rest = sh.rest;
         if (!ask) break;
         double sum = 0.0;
-        for (int v = 4 * tid; v < a.V; v += 4 * kWalkThreads) {
-            double w[4];
-            rest_of<T, Q>(r, rest, list, v, true, w);
-            sum += (w[0] + w[1]) + (w[2] + w[3]);
+        if (a.draft == nullptr) {
+            chunks_left<T, Q>(r, rest, *row_of(rest.row - row0), list, chunk_sums, sh);
+            __syncthreads();
+            for (int c = tid; c < r.nc; c += kWalkThreads) sum += chunk_sums[c];
+        } else {
+            for (int v = 4 * tid; v < a.V; v += 4 * kWalkThreads) {
+                double w[4];
+                rest_of<T, Q>(r, rest, list, v, true, w);
+                sum += (w[0] + w[1]) + (w[2] + w[3]);
+            }
         }
         sum = block_sum(sum, sh.part);
         if (wave == 0) {
             open = false;
-            if (sum > 0.0) {                 // else nothing is left, and r stays
-                scale = want_scale / sum;
-                by = want_by / sum;
+            // (where nothing is left r stays)
+            if (a.draft != nullptr) {
+                if (sum > 0.0) {
+                    scale = want_scale / sum;
+                    by = want_by / sum;
+                }
+            } else if (sum > 0.0) {
+                scale = summed = sum / row_of(cur)->sum;
+            } else {
+                --refused;
+                if (marks != nullptr && lane == 0) marks[list[refused]] = 0;
+                __threadfence_block();
+                scale = want_scale;
             }
         }
     }
