@@ -447,7 +447,8 @@ int flashd_cache_commit(const flashd_cache* c, const int* q_start, const int* ke
  *   next[b] = the least id up to which r sums to more than uniform[row of token 0] times the sum of all.
  *
  * With temperature 0 (or below, or NaN) p_i is 1 at the largest logit, the first of equal ones, and 0 elsewhere.  Logits of -infinity
- * and NaN have probability 0 (and those 708 temperatures or more below the largest may have it), those of +infinity share everything; behind a row of nothing else no token is accepted and next is -1.
+ * and NaN have probability 0 (and those 708 temperatures or more below the largest may have it); behind a row of nothing else no token is accepted
+ * and next is -1.  Those of +infinity count as the largest number, and so share everything unless the temperature is about as large.
  * The arithmetic is fp64: results do not depend on the order of sums but where a random number is within some 1e-13 of a border; behind tokens
  * refused with `draft`, where r is a difference, within that divided by the part of r that each refusal has left.
  *   logits   [T][V] in storage type `dtype`, rows logits_stride elements apart, at any multiple of an element; V at most

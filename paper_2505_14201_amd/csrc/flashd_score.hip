@@ -8,7 +8,7 @@
 // registers.  K is the B operand and goes from the pages to registers as it lies there; a row's w exp(-lse) is one number in
 // the exponent: 2^(c s - bias).
 //
-// Up to 16 rows to a sequence and kv head HBM bounds it (score_few_kernel); with more the products and exponentials do as well, then alone
+// Up to 16 rows to a sequence and kv head HBM bounds it (score_few_kernel); with more the products and exponentials count as well, and in the end more than the keys
 // (score_many_kernel).  Both are launched where the call may have either.
 #include "flashd_common.h"
 #include "flashd_kernels.h"
@@ -448,6 +448,7 @@ __global__ __launch_bounds__(kScoreThreads, 2) void score_few_kernel(ScoreRun r)
 // the time (32 tokens after 10000 to 32000 keys, 202 MB: 65 us, and 79 where each wavefront copied the rows a tile ahead for itself and so read its next keys late).
 // Of more rows each wavefront of a shared turn takes every eighth tile, copied to a place of its own one ahead, and so waits for nobody.  The exponentials of a block run between
 // the products of the next one.  Chunks of 1000 tokens after 2000 to 7000 keys, 138 GFLOP: 207 to 216 us, where rows staged with a barrier for each 128 of them took 251.
+// (Without the products 142, without the exponentials 183.)  At d = 128 registers are pushed out: 57 vector and 165 scalar ones of 16 bits, 55 and 89 of f32, 45 and 167 of fp8.
 template <typename C> struct ScorePlaces {
     union {
         char tile[kScoreWaves][C::SLOTS][C::TILE];

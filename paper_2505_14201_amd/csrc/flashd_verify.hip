@@ -239,8 +239,8 @@ __device__ __forceinline__ int wave_min(int x) {
 
 // ---- sums of chunks -----------------------------------------------------------------------------
 //
-// A workgroup per chunk and row.  f32 logits come at 5.1 TB/s (8 x 31 rows of 100003: 19 us); of 16 bits the sums of 64 bits take as long again: 84 MB of bf16, 320 rows of 131072,
-// 30 us, of which 18 without the exponentials.  (Workgroups that take several chunks, reading the next while they sum the present one: 32 us, and 23 for the f32.)
+// A workgroup per chunk and row.  f32 logits come at 4.3 TB/s (202 rows of 100003: 19 us); of 16 bits the sums of 64 bits take as long again: 75.5 MB of bf16, 288 rows of 131072,
+// 29 us, of which 18 without the exponentials.  (Workgroups that take several chunks, reading the next while they sum the present one: 32 us, and 23 for the f32.)
 template <typename T>
 __global__ __launch_bounds__(kStatThreads) void verify_stats_kernel(VerifyRun r) {
     constexpr int E = Elements<T>::E, W = kStatThreads / kWave;
@@ -603,8 +603,9 @@ __device__ __forceinline__ void draw_next(const VerifyRun& r, int b, const WalkE
     if (tid == 0) a.next[b] = first != 0x7fffffff ? first : last;
 }
 
-// A workgroup per sequence.  Latency bounds it, reads that depend on each other: 7 us for 64 chains of 5 tokens with draft probabilities, 11 for one of 4 without, whose
-// next token it draws, 15 for 32 trees of 16.  Where siblings ask for the sum of what is left, that is one workgroup's over the vocabulary (8 trees of 31 tokens: 9 us).
+// A workgroup per sequence.  Latency bounds it, reads that depend on each other: 7 us for 64 chains of up to 5 tokens with draft probabilities, 11 for one of 4 without, whose
+// next token it draws, 15 to 18 for 32 trees of up to 16.  Where siblings ask for the sum of what is left, that is one workgroup's over the vocabulary (8 trees of up to 31 tokens: 9 us),
+// without draft probabilities over the chunks.  6000 siblings of 9001 ids, all refused: 4.1 ms, 0.7 us each.
 template <typename T, typename Q>
 __global__ __launch_bounds__(kWalkThreads) void verify_walk_kernel(VerifyRun r) {
     extern __shared__ double chunk_sums[];               // [nc]
