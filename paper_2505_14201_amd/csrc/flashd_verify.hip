@@ -78,7 +78,6 @@ struct VerifyRun {
 
 // ---- numbers ------------------------------------------------------------------------------------
 
-// A logit as it counts: NaN like -infinity, +infinity like the largest number.
 // The largest of three numbers, none of them NaN.  (The compiler, which cannot know that, has each operand of fmaxf go through an instruction of its own.)
 __device__ __forceinline__ float max3(float x, float y, float z) {
     float m;
@@ -86,6 +85,7 @@ __device__ __forceinline__ float max3(float x, float y, float z) {
     return m;
 }
 __device__ __forceinline__ bool is_odd(float x) { return __builtin_amdgcn_classf(x, 0x203); }        // NaN or +infinity
+// A logit as it counts: NaN like -infinity, +infinity like the largest number.
 __device__ __forceinline__ float clean(float x) {
     return x != x ? -__builtin_inff() : fminf(x, 3.4028234663852886e38f);
 }
